@@ -624,6 +624,100 @@ typedef struct lv_sched_params {
 lv_status lv_schedule(lv_pool* pool, const lv_sched_params* params, const lv_request* reqs, int32_t n,
                       int32_t* order_out, int32_t* batch_out, lv_stream stream);
 
+/* ------------------------------------------- a serving step on resident KV */
+
+/* What a model's forward pass does with the paged cache, between the calls above: a step
+   takes new tokens of several sessions (single tokens of a reply, chunks of user input, or
+   both), writes their K and V rows and computes their attention, layer by layer.  Not from
+   the paper, whose engine leaves this to its substrate.
+
+   A batch is the handle of such steps over a pool: lv_batch_plan makes a step's tables once
+   on the device, and lv_kv_write and lv_attention use them for every layer.  A batch serves
+   one kind of attention layer (query heads, window, sinks); a model that mixes kinds keeps a
+   batch for each.  The pool's elements are read as dtype, so elem_bytes must be 2, and
+   head_dim a multiple of 8 up to 256.
+
+   row_starts, kv_lens, tables, positions and slots are the caller's device arrays (kept
+   alive until the batch is destroyed); lv_batch_plan writes them and the other calls read
+   them, so that the caller's own kernels may use them too.  The calls of one batch must be
+   ordered with respect to each other; distinct batches are independent. */
+enum { LV_BF16 = 1, LV_F16 = 2, LV_F32 = 3 };
+
+typedef struct lv_batch lv_batch;   /* opaque */
+
+typedef struct lv_batch_desc {
+  int32_t num_q_heads;         /* Hq, a multiple of the pool's H, at most 256 H; query head h
+                                  reads KV head h / (Hq / H) */
+  int32_t max_requests;        /* 1..4096 */
+  int32_t max_tokens;          /* rows of a step's tensors at most, 1..2^24; Hq * max_tokens < 2^31 */
+  int32_t dtype;               /* LV_BF16 or LV_F16: the pool's elements, queries and outputs */
+  int32_t window;              /* > 0: a query at position p sees keys p - window + 1 .. p; 0: all up to p */
+  int32_t sinks;               /* >= 0: and, beside the window, keys 0 .. sinks - 1 up to p */
+  int32_t* row_starts;         /* [max_requests + 1] first row of each request; the end */
+  int32_t* kv_lens;            /* [max_requests] context length at the step's end */
+  int32_t* tables;             /* [max_requests][max_blocks] HBM pages, -1 where there is none */
+  int32_t* positions;          /* [max_tokens] each row's position in its session, -1: no request's row */
+  int64_t* slots;              /* [max_tokens] page * T + offset of each row's token; -1: none; a
+                                  value s <= -2: slot -(s + 2), whose block has a clean host copy
+                                  (LV_TIERS_INCLUSIVE), so that its rows must not change */
+  int32_t reserved[2];         /* must be 0 */
+} lv_batch_desc;
+
+/* A tensor [rows][heads][head_dim] with head_dim contiguous; the strides count elements. */
+typedef struct lv_heads {
+  void* data;                  /* device memory, aligned to its element */
+  int64_t row_stride;
+  int64_t head_stride;
+  int32_t dtype;               /* LV_BF16, LV_F16 or LV_F32 */
+  int32_t reserved;            /* must be 0 */
+} lv_heads;
+
+/* Validates the descriptor and allocates the batch's work lists and workspace (about
+   80 MiB at 128 head_dim).  LV_ERR_INVALID, LV_ERR_OOM or LV_ERR_CUDA. */
+lv_status lv_batch_create(lv_pool* pool, const lv_batch_desc* desc, lv_batch** out);
+
+/* Waits for `stream` and frees the batch; call it before lv_pool_destroy of its pool. */
+lv_status lv_batch_destroy(lv_batch* batch, lv_stream stream);
+
+/* Plans a step of n requests (0..max_requests).  Request i is session sids[i] with lens[i]
+   new tokens at positions firsts[i] .. firsts[i] + lens[i] - 1, within the session's context
+   (lv_session_append or a turn's growth made room for them); firsts NULL, or firsts[i] < 0:
+   the last lens[i] tokens of the context.  The requests' rows follow one another in the
+   step's tensors of num_tokens rows (0..max_tokens); rows past the last request's belong to
+   none.  max_len: no lens[i] is larger (it selects the kernels; num_tokens always holds).
+   Arrays: row_starts[0..n], kv_lens[i] = firsts[i] + lens[i], tables[i][b] the HBM page of
+   block b < ceil(kv_lens[i] / T) (-1 for one that is not in HBM, and past the end),
+   positions[0..num_tokens) and slots[0..num_tokens).
+   Every block that some row of the request sees must be in HBM; under a window the others may
+   be in the host tier.  A request that breaks a rule is left out (kv_lens 0, table -1, its
+   rows as rows of none) and the others go on.  Device-detected: LV_ERR_BOUNDS for a session
+   id, a length or a position out of range or rows past num_tokens, LV_ERR_STATE for a visible
+   block that is not in HBM; the detail is the request's index. */
+lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* firsts, const int32_t* lens,
+                        int32_t n, int32_t num_tokens, int32_t max_len, lv_stream stream);
+
+/* Writes the planned step's new K and V rows ([num_tokens][H][D], any of the three types,
+   rounded to nearest even where the pool's type is narrower) into their pages of `layer`;
+   rows of no request are skipped.  The sessions' pages must stay where the plan found them
+   until the step's last call has run (running sessions are never victims).  LV_ERR_INVALID for
+   a layer out of range, no plan, or a tensor that is not device memory or misaligned.
+   Device-detected: LV_ERR_STATE for a row whose block has a clean host copy (it is skipped). */
+lv_status lv_kv_write(lv_batch* batch, int32_t layer, const lv_heads* k, const lv_heads* v, lv_stream stream);
+
+/* Attention of the planned step's rows over the paged context, in one layer:
+   out[r][h] = sum_j softmax_j(scale * q[r][h] . k[j][h']) v[j][h'] over the keys j that row
+   r sees (up to its own position, within the window and the sinks), h' = h / (Hq / H).
+   q and out are [num_tokens][Hq][D] of the batch's dtype and must not overlap.  Statistics and sums are held in 32
+   bits; the weights are rounded to dtype for the product with V.  lse (float [num_tokens][Hq],
+   or NULL) receives the natural logarithm of each row's sum of exponentials.  A row of no
+   request gets out = 0 and lse = -inf.  scale is finite and > 0.
+   What a cache page holds past a request's context, and in blocks that none of its rows
+   sees, has no effect, not even as NaN; a non-finite V row that some rows of a chunk see may
+   also reach other rows of that chunk.  LV_ERR_INVALID as for lv_kv_write.  Device-detected:
+   LV_ERR_TIMEOUT if a bounded wait inside the kernel ran out. */
+lv_status lv_attention(lv_batch* batch, int32_t layer, const lv_heads* q, const lv_heads* out, float* lse,
+                       float scale, lv_stream stream);
+
 /* ------------------------------------------------------------- status */
 
 /* Synchronous: waits for `stream`, returns the sticky device error (LV_OK if

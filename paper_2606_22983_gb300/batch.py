@@ -1,0 +1,133 @@
+"""KVBatch: serving steps on a pool's resident KV (include/lv.h, "a serving step on resident KV").
+
+A step takes new tokens of several sessions -- single tokens of a reply, chunks of user input, or
+both -- whose room in the context a turn or ``KVPool.append`` has made:
+
+    batch = KVBatch(pool, q_heads=32, max_requests=64, max_tokens=4096)
+    batch.plan(sids, lens)                       # once a step: tables, positions, slot map
+    for layer in range(pool.L):                  # q, k, v: [rows, heads, head_dim]
+        batch.write(layer, k, v)
+        out = batch.attention(layer, q)
+
+``row_starts``, ``kv_lens``, ``tables``, ``positions`` and ``slots`` are device tensors that
+``plan`` fills.  PyTorch holds the memory; every operation is a liblv call on the given stream (None:
+the current one).
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+from . import lv
+from .pool import KVPool
+
+
+class KVBatch:
+    """One kind of attention layer over ``pool``: ``q_heads`` query heads, and with ``window`` > 0 a
+    sliding window of that many keys beside which the first ``sinks`` keys stay visible."""
+
+    def __init__(self, pool: KVPool, *, q_heads: int, max_requests: int, max_tokens: int,
+                 dtype=torch.bfloat16, window: int = 0, sinks: int = 0):
+        kinds = {torch.bfloat16: lv.LV_BF16, torch.float16: lv.LV_F16}
+        if dtype not in kinds:
+            raise ValueError("dtype must be torch.bfloat16 or torch.float16")
+        self.pool, self.q_heads, self.dtype = pool, q_heads, dtype
+        self.max_requests, self.max_tokens = max_requests, max_tokens
+        self.num_tokens = 0
+        self.handle = None
+        i32 = dict(dtype=torch.int32, device=pool.device)
+        rows, requests = max(max_tokens, 0), max(max_requests, 0)
+        with torch.cuda.device(pool.device):
+            self.row_starts = torch.zeros(requests + 1, **i32)
+            self.kv_lens = torch.zeros(max(requests, 1), **i32)
+            self.tables = torch.full((max(requests, 1), pool.max_blocks), -1, **i32)
+            self.positions = torch.full((max(rows, 1),), -1, **i32)
+            self.slots = torch.full((max(rows, 1),), -1, dtype=torch.int64, device=pool.device)
+            # the library may write them on any stream next
+            torch.cuda.current_stream().synchronize()
+        d = lv.lv_batch_desc(num_q_heads=q_heads, max_requests=max_requests, max_tokens=max_tokens,
+                             dtype=kinds[dtype], window=window, sinks=sinks,
+                             row_starts=self.row_starts.data_ptr(), kv_lens=self.kv_lens.data_ptr(),
+                             tables=self.tables.data_ptr(), positions=self.positions.data_ptr(),
+                             slots=self.slots.data_ptr())
+        self.handle = lv.lv_batch_create(pool.handle, d)
+        pool.attach(self)          # destroyed before the pool
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lv.lv_batch_destroy(self.handle, self.pool.stream)
+            self.handle = None
+
+    def _ints(self, x, n=None):
+        """An int32 array the library can read: a device tensor as it is, else a numpy array."""
+        if x is None:
+            return None
+        if isinstance(x, torch.Tensor):
+            if x.dtype != torch.int32 or not x.is_contiguous():
+                raise ValueError("expected a contiguous int32 tensor")
+            if x.is_cuda and x.device != self.pool.device:
+                raise ValueError("expected a tensor on the pool's device")
+        else:
+            x = np.ascontiguousarray(x, dtype=np.int32)
+        if n is not None and len(x) != n:
+            raise ValueError(f"expected {n} entries, got {len(x)}")
+        return x
+
+    def plan(self, sids, lens, firsts=None, *, num_tokens=None, max_len=None, stream=None):
+        """Plans a step: request i is session sids[i] with lens[i] new tokens from position firsts[i]
+        on (None: the last ones of its context).  With lengths on the device, ``num_tokens`` (rows of
+        the step's tensors) has to be given, and ``max_len`` (a bound of the lengths) should be."""
+        sids = self._ints(sids)
+        n = len(sids)
+        lens, firsts = self._ints(lens, n), self._ints(firsts, n)
+        if isinstance(lens, torch.Tensor) and lens.is_cuda:
+            if num_tokens is None:
+                raise ValueError("num_tokens is needed with lengths on the device")
+        else:
+            have = np.asarray(lens)
+            num_tokens = int(have.sum()) if num_tokens is None else num_tokens
+            max_len = int(have.max(initial=0)) if max_len is None else max_len
+        lv.lv_batch_plan(self.handle, sids, firsts, lens, n, num_tokens,
+                         num_tokens if max_len is None else max_len, self._stream(stream))
+        self.num_tokens = num_tokens
+        self.pool.launches += 1
+
+    def _stream(self, stream):
+        return self.pool.stream if stream is None else stream
+
+    def _tensor(self, x, heads, name):
+        if x.device != self.pool.device or x.dim() != 3 or x.shape[0] < self.num_tokens or \
+                x.shape[1] != heads or x.shape[2] != self.pool.head_dim:
+            raise ValueError(f"{name}: expected [{self.num_tokens}, {heads}, {self.pool.head_dim}] on "
+                             f"{self.pool.device}, got {tuple(x.shape)} on {x.device}")
+        return lv.heads(x)
+
+    def write(self, layer: int, k, v, *, stream=None):
+        """The step's new K and V rows ([rows, kv_heads, head_dim], any strides, bf16, f16 or f32)
+        into their pages."""
+        H = self.pool.kv_heads
+        lv.lv_kv_write(self.handle, layer, self._tensor(k, H, "k"), self._tensor(v, H, "v"),
+                       self._stream(stream))
+        self.pool.launches += 1
+
+    def attention(self, layer: int, q, *, out=None, scale=None, return_lse=False, stream=None):
+        """Attention of the step's rows over their paged contexts: [rows, q_heads, head_dim], and with
+        ``return_lse`` the logarithms of the sums of exponentials [rows, q_heads] (f32).  Rows of
+        no request give zeros (and -inf).  scale: 1 / sqrt(head_dim) unless given."""
+        qh = self._tensor(q, self.q_heads, "q")
+        if out is None:
+            out = torch.empty((q.shape[0], self.q_heads, self.pool.head_dim), dtype=self.dtype,
+                              device=q.device)
+            if q.shape[0] > self.num_tokens:
+                out[self.num_tokens:].zero_()
+        lse = torch.full((q.shape[0], self.q_heads), -math.inf, dtype=torch.float32, device=q.device) \
+            if return_lse and q.shape[0] > self.num_tokens else \
+            torch.empty((q.shape[0], self.q_heads), dtype=torch.float32, device=q.device) \
+            if return_lse else None
+        lv.lv_attention(self.handle, layer, qh, self._tensor(out, self.q_heads, "out"), lse,
+                        1.0 / math.sqrt(self.pool.head_dim) if scale is None else scale,
+                        self._stream(stream))
+        self.pool.launches += 2
+        return (out, lse) if return_lse else out

@@ -10,6 +10,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "lv_batch.cuh"
 #include "lv_internal.cuh"
 
 // One NVTX range per entry point, so that a profiler's timeline shows which liblv call
@@ -91,6 +92,9 @@ struct lv_pool {
   std::vector<lv::EventPair> ev_free;
   // a deque: the pointer timing_pair returns stays valid while later pairs are added
   std::deque<lv::EventPair> ev_used[LV_TIMING_KINDS];
+  // for lv_batch: the shape behind P, and the sub-page arrays' addresses on the host
+  int32_t kv_heads = 0, head_dim = 0, elem_bytes = 0;
+  std::vector<uint8_t*> kv;
   bool own_host = false;
   void* host_base = nullptr;       // host-visible address of the host pool
   std::vector<void*> dev_allocs;
@@ -651,6 +655,10 @@ lv_status create_impl(const lv_pool_desc* desc, cudaStream_t s, lv_pool** out) {
     if (!p || (reinterpret_cast<uintptr_t>(p) & 15) || !is_device_ptr(p)) return fail(LV_ERR_INVALID);
     kv[j] = static_cast<uint8_t*>(p);
   }
+  pool->kv = kv;
+  pool->kv_heads = desc->num_kv_heads;
+  pool->head_dim = desc->head_dim;
+  pool->elem_bytes = desc->elem_bytes;
   // the host pool
   const size_t host_bytes = (size_t)d.host_pages * d.J * d.P;
   if (desc->host_kv) {
@@ -1619,6 +1627,343 @@ lv_status lv_selftest_wait(lv_pool* pool, int64_t limit_us, lv_stream stream) {
   if (!pool || limit_us < 1 || limit_us > 10000000) return LV_ERR_INVALID;
   DeviceGuard g(pool->device);
   LV_TRY(lv::launch_selftest_wait(pool->d, limit_us * 1000, as_stream(stream)));
+  return LV_OK;
+}
+
+// ------------------------------------------------- a serving step on resident KV
+}  // extern "C"
+
+struct lv_batch {
+  lv_pool* pool = nullptr;
+  lv_batch_desc d{};
+  std::vector<void*> allocs;
+  lv::PlanReq* reqs = nullptr;
+  lv::AttnTile* tiles = nullptr;
+  int32_t max_tiles = 0;
+  int32_t* cta_tile = nullptr;
+  lv::PlanHead* head = nullptr;
+  float* part_o = nullptr;
+  float2* part_ml = nullptr;
+  int32_t G = 1;             // query heads a KV head
+  int32_t dp = 128;          // the kernels' columns: head_dim rounded up to 64, 128 or 256
+  int32_t hg = 1;            // KV heads that a CTA of the rows kernel takes
+  int32_t box_rows = 0;      // keys in a TMA box; 0: the pages cannot be read by TMA
+  std::vector<CUtensorMap> maps;   // [2L]
+  // the planned step
+  bool planned = false;
+  int32_t num_tokens = 0;
+  lv::AttnKind kind = lv::ATTN_ROWS16;
+  int32_t ctas = 0;
+};
+
+namespace {
+
+void free_batch(lv_batch* b) {
+  for (void* p : b->allocs) cudaFree(p);
+  delete b;
+}
+
+template <typename T>
+lv_status batch_alloc(lv_batch* b, T** ptr, size_t count) {
+  void* p = nullptr;
+  const cudaError_t e = cudaMalloc(&p, (count ? count : 1) * sizeof(T));
+  if (e != cudaSuccess) return lv_cuda_fail(e);
+  b->allocs.push_back(p);
+  *ptr = static_cast<T*>(p);
+  return LV_OK;
+}
+
+int32_t gcd(int32_t a, int32_t b) {
+  while (b) {
+    const int32_t t = a % b;
+    a = b;
+    b = t;
+  }
+  return a;
+}
+
+// Tensor maps of the 2L sub-page arrays, [page][T][H][D] with boxes of box_rows keys and 64
+// columns: pages whose T is a multiple of 8 hold whole groups of eight 128-byte rows, which the
+// swizzle repeats over.
+lv_status make_maps(lv_batch* b) {
+  const lv_pool* pool = b->pool;
+  const int32_t box = gcd(pool->d.T, lv::kTcUnit);
+  if (box < 8 || b->dp > 128) return LV_OK;
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found{};
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+      found != cudaDriverEntryPointSuccess || !fn)
+    return LV_ERR_CUDA;
+  const auto encode = reinterpret_cast<Encode>(fn);
+  const cuuint64_t D = pool->head_dim, H = pool->kv_heads, T = pool->d.T;
+  const cuuint64_t dims[4] = {D, H, T, (cuuint64_t)pool->d.hbm_pages};
+  const cuuint64_t strides[3] = {D * 2, H * D * 2, (cuuint64_t)pool->d.P};
+  const cuuint32_t boxes[4] = {64, 1, (cuuint32_t)box, 1}, ones[4] = {1, 1, 1, 1};
+  b->maps.resize(pool->d.J);
+  for (int j = 0; j < pool->d.J; ++j)
+    if (encode(&b->maps[j],
+               b->d.dtype == LV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+               pool->kv[j], dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return LV_ERR_CUDA;
+  b->box_rows = box;
+  return LV_OK;
+}
+
+bool device_array(const lv_pool* pool, const void* p, size_t align) {
+  if (!p || (reinterpret_cast<uintptr_t>(p) & (align - 1))) return false;
+  cudaPointerAttributes a{};
+  if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return a.type == cudaMemoryTypeManaged || (a.type == cudaMemoryTypeDevice && a.device == pool->device);
+}
+
+// CTAs of the rows kernel
+int rows_ctas(const lv_batch* b, bool wide) { return b->pool->num_sms * lv::attend_rows_ctas(b->dp, wide); }
+
+lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
+  const int H = pool->kv_heads, D = pool->head_dim;
+  if (pool->elem_bytes != 2 || D % 8 != 0 || D > 256) return LV_ERR_INVALID;
+  if (d->dtype != LV_BF16 && d->dtype != LV_F16) return LV_ERR_INVALID;
+  if (d->num_q_heads < H || d->num_q_heads % H != 0 || d->num_q_heads / H > 256) return LV_ERR_INVALID;
+  if (d->max_requests < 1 || d->max_requests > 4096 || d->max_tokens < 1 || d->max_tokens > 1 << 24)
+    return LV_ERR_INVALID;
+  if ((long long)d->num_q_heads * d->max_tokens >= 1ll << 31) return LV_ERR_INVALID;
+  if (d->window < 0 || d->sinks < 0 || d->reserved[0] != 0 || d->reserved[1] != 0) return LV_ERR_INVALID;
+  if (!device_array(pool, d->row_starts, 4) || !device_array(pool, d->kv_lens, 4) ||
+      !device_array(pool, d->tables, 4) || !device_array(pool, d->positions, 4) || !device_array(pool, d->slots, 8))
+    return LV_ERR_INVALID;
+  lv_batch* b = new (std::nothrow) lv_batch();
+  if (!b) return LV_ERR_OOM;
+  auto fail = [&](lv_status code) {
+    free_batch(b);
+    return code;
+  };
+  b->pool = pool;
+  b->d = *d;
+  b->G = d->num_q_heads / H;
+  b->dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  b->hg = 1;
+  lv_status st;
+  try {
+    if ((st = make_maps(b)) != LV_OK) return fail(st);
+  } catch (const std::bad_alloc&) {
+    return fail(LV_ERR_OOM);
+  }
+  if (lv::configure_attend() != cudaSuccess || lv::configure_attend_tc() != cudaSuccess) return fail(LV_ERR_CUDA);
+  b->max_tiles = d->max_requests + (int32_t)(((long long)d->max_tokens * b->G + 15) / 16);
+  const int most = std::max({rows_ctas(b, false), rows_ctas(b, true), pool->num_sms});
+  // rows of partial results: two slots a CTA
+  size_t rows = (size_t)2 * rows_ctas(b, false) * b->hg * 16;
+  rows = std::max(rows, (size_t)2 * rows_ctas(b, true) * b->hg * 32);
+  if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows);
+  try {
+    if ((st = batch_alloc(b, &b->reqs, d->max_requests)) != LV_OK ||
+        (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
+        (st = batch_alloc(b, &b->cta_tile, (size_t)most + 1)) != LV_OK ||
+        (st = batch_alloc(b, &b->head, 1)) != LV_OK || (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
+        (st = batch_alloc(b, &b->part_ml, rows)) != LV_OK)
+      return fail(st);
+  } catch (const std::bad_alloc&) {
+    return fail(LV_ERR_OOM);
+  }
+  // (waits: the batch may be used on any stream next)
+  if (cudaMemset(b->head, 0, sizeof(lv::PlanHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
+    return fail(LV_ERR_CUDA);
+  *out = b;
+  return LV_OK;
+}
+
+size_t elem_size(int32_t type) { return type == LV_F32 ? 4 : 2; }
+
+// A tensor argument: its type, its memory, and rows and heads that do not leave 63 bits.
+bool heads_ok(const lv_pool* pool, const lv_heads* x) {
+  if (!x || x->reserved != 0 || x->dtype < LV_BF16 || x->dtype > LV_F32) return false;
+  const int64_t lim = 1ll << 38;
+  if (x->row_stride < -lim || x->row_stride > lim || x->head_stride < -lim || x->head_stride > lim) return false;
+  return device_array(pool, x->data, elem_size(x->dtype));
+}
+
+// Every 8-element piece of every row starts on a multiple of `bytes`.
+bool heads_aligned(const lv_heads* x, size_t bytes) {
+  const size_t e = elem_size(x->dtype);
+  return reinterpret_cast<uintptr_t>(x->data) % bytes == 0 && (uint64_t)x->row_stride * e % bytes == 0 &&
+         (uint64_t)x->head_stride * e % bytes == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+lv_status lv_batch_create(lv_pool* pool, const lv_batch_desc* desc, lv_batch** out) {
+  NvtxRange nvtx_range("lv_batch_create");
+  if (!out) return LV_ERR_INVALID;
+  *out = nullptr;
+  if (!pool || !desc) return LV_ERR_INVALID;
+  DeviceGuard g(pool->device);
+  return create_batch(pool, desc, out);
+}
+
+lv_status lv_batch_destroy(lv_batch* batch, lv_stream stream) {
+  NvtxRange nvtx_range("lv_batch_destroy");
+  if (!batch) return LV_ERR_INVALID;
+  DeviceGuard g(batch->pool->device);
+  const cudaError_t e = cudaStreamSynchronize(as_stream(stream));
+  free_batch(batch);
+  return e == cudaSuccess ? LV_OK : LV_ERR_CUDA;
+}
+
+lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts, const int32_t* lens, int32_t n,
+                        int32_t num_tokens, int32_t max_len, lv_stream stream) {
+  NvtxRange nvtx_range("lv_batch_plan");
+  if (!b || n < 0 || n > b->d.max_requests || (n > 0 && (!sids || !lens)) || num_tokens < 0 ||
+      num_tokens > b->d.max_tokens || max_len < 0)
+    return LV_ERR_INVALID;
+  lv_pool* pool = b->pool;
+  DeviceGuard g(pool->device);
+  cudaStream_t s = as_stream(stream);
+  try {
+    LV_TRY(join_copies(pool, s));   // the step reads and writes KV bytes
+    Staging st(pool, s);
+    const void *si = nullptr, *fi = nullptr, *le = nullptr;
+    lv_status r;
+    // every CTA reads the lengths: host memory is copied in
+    if ((r = st.in(sids, (size_t)n * 4, &si, true)) != LV_OK || (r = st.in(lens, (size_t)n * 4, &le, true)) != LV_OK)
+      return r;
+    if (firsts && (r = st.in(firsts, (size_t)n * 4, &fi, true)) != LV_OK) return r;
+    max_len = std::min(max_len, num_tokens);
+    const long long rows = (long long)max_len * b->G;
+    b->kind = rows <= 16 ? lv::ATTN_ROWS16 : b->dp > 128 ? lv::ATTN_ROWS16
+              : rows <= 32 || !b->box_rows ? lv::ATTN_ROWS32 : lv::ATTN_TC;
+    b->num_tokens = num_tokens;
+    lv::PlanArgs a{};
+    a.p = pool->d;
+    a.sids = static_cast<const int32_t*>(si);
+    a.firsts = static_cast<const int32_t*>(fi);
+    a.lens = static_cast<const int32_t*>(le);
+    a.n = n;
+    a.num_tokens = num_tokens;
+    a.max_len = max_len;
+    a.G = b->G;
+    if (b->kind == lv::ATTN_TC) {
+      a.groups = pool->kv_heads;
+      a.tile_rows = lv::kTcRows;
+      a.unit = lv::kTcUnit;
+      a.min_share = 4;
+      b->ctas = pool->num_sms;
+    } else {
+      a.groups = pool->kv_heads / b->hg;
+      a.tile_rows = b->kind == lv::ATTN_ROWS32 ? 32 : 16;
+      a.unit = lv::kRowsUnit;
+      a.min_share = 4;
+      b->ctas = rows_ctas(b, b->kind == lv::ATTN_ROWS32);
+    }
+    a.ctas = b->ctas;
+    a.window = b->d.window;
+    a.sinks = b->d.sinks;
+    a.row_starts = b->d.row_starts;
+    a.kv_lens = b->d.kv_lens;
+    a.tables = b->d.tables;
+    a.positions = b->d.positions;
+    a.slots = b->d.slots;
+    a.reqs = b->reqs;
+    a.tiles = b->tiles;
+    a.max_tiles = b->max_tiles;
+    a.cta_tile = b->cta_tile;
+    a.head = b->head;
+    LV_TRY(lv::launch_plan(a, s));
+    b->planned = true;
+    return st.finish();
+  } catch (const std::bad_alloc&) {
+    return LV_ERR_OOM;
+  }
+}
+
+lv_status lv_kv_write(lv_batch* b, int32_t layer, const lv_heads* k, const lv_heads* v, lv_stream stream) {
+  NvtxRange nvtx_range("lv_kv_write");
+  if (!b || !b->planned || layer < 0 || 2 * layer >= b->pool->d.J) return LV_ERR_INVALID;
+  if (b->num_tokens == 0) return LV_OK;
+  const lv_pool* pool = b->pool;
+  DeviceGuard g(pool->device);
+  if (!heads_ok(pool, k) || !heads_ok(pool, v)) return LV_ERR_INVALID;
+  lv::WriteArgs a{};
+  const lv_heads* src[2] = {k, v};
+  for (int i = 0; i < 2; ++i) {
+    a.dst[i] = pool->kv[2 * layer + i];
+    a.src[i] = static_cast<const uint8_t*>(src[i]->data);
+    a.row_stride[i] = src[i]->row_stride;
+    a.head_stride[i] = src[i]->head_stride;
+    a.src_type[i] = src[i]->dtype;
+    a.vec[i] = heads_aligned(src[i], 16) ? 1 : 0;
+  }
+  a.slots = b->d.slots;
+  a.num_tokens = b->num_tokens;
+  a.H = pool->kv_heads;
+  a.D = pool->head_dim;
+  a.dtype = b->d.dtype;
+  a.num_slots = pool->d.hbm_pages * pool->d.T;
+  a.ctl = pool->d.ctl;
+  LV_TRY(lv::launch_kv_write(a, as_stream(stream), pool->num_sms));
+  return LV_OK;
+}
+
+lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_heads* out, float* lse, float scale,
+                       lv_stream stream) {
+  NvtxRange nvtx_range("lv_attention");
+  if (!b || !b->planned || layer < 0 || 2 * layer >= b->pool->d.J) return LV_ERR_INVALID;
+  if (!(scale > 0.f) || scale > 3e38f) return LV_ERR_INVALID;
+  if (b->num_tokens == 0) return LV_OK;
+  const lv_pool* pool = b->pool;
+  DeviceGuard g(pool->device);
+  if (!heads_ok(pool, q) || !heads_ok(pool, out) || q->dtype != b->d.dtype || out->dtype != b->d.dtype)
+    return LV_ERR_INVALID;
+  if (lse && !device_array(pool, lse, 4)) return LV_ERR_INVALID;
+  cudaStream_t s = as_stream(stream);
+  const bool bf16 = b->d.dtype == LV_BF16, tc = b->kind == lv::ATTN_TC;
+  lv::AttnArgs a{};
+  for (int i = 0; i < 2; ++i) a.kv[i] = pool->kv[2 * layer + i];
+  a.P = pool->d.P;
+  a.hbm_pages = (uint32_t)pool->d.hbm_pages;
+  a.T = pool->d.T;
+  a.H = pool->kv_heads;
+  a.D = pool->head_dim;
+  a.G = b->G;
+  a.maxB = pool->d.maxB;
+  a.tables = b->d.tables;
+  a.positions = b->d.positions;
+  a.tiles = b->tiles;
+  a.cta_tile = b->cta_tile;
+  a.head = b->head;
+  a.q = static_cast<const uint8_t*>(q->data);
+  a.out = static_cast<uint8_t*>(out->data);
+  a.lse = lse;
+  a.q_row = q->row_stride;
+  a.q_head = q->head_stride;
+  a.o_row = out->row_stride;
+  a.o_head = out->head_stride;
+  a.q_vec = heads_aligned(q, 16) ? 1 : 0;
+  a.o_vec = heads_aligned(out, 16) ? 1 : 0;
+  a.num_tokens = b->num_tokens;
+  a.window = b->d.window;
+  a.sinks = b->d.sinks;
+  a.groups = tc ? pool->kv_heads : pool->kv_heads / b->hg;
+  a.hg = tc ? 1 : b->hg;
+  a.tile_rows = tc ? lv::kTcRows : b->kind == lv::ATTN_ROWS32 ? 32 : 16;
+  a.dp = b->dp;
+  a.scale = scale * 1.44269504088896341f;
+  a.part_o = b->part_o;
+  a.part_ml = b->part_ml;
+  a.ctl = pool->d.ctl;
+  if (tc)
+    LV_TRY(lv::launch_attend_tc(a, b->maps[2 * layer], b->maps[2 * layer + 1], b->box_rows, bf16, b->ctas, s));
+  else
+    LV_TRY(lv::launch_attend_rows(a, b->kind == lv::ATTN_ROWS32, bf16, b->ctas, s));
+  LV_TRY(lv::launch_attend_join(a, bf16, b->ctas, s));
   return LV_OK;
 }
 

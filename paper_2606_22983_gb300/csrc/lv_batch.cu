@@ -1,0 +1,279 @@
+// The plan of a serving step and the write of its K and V rows (include/lv.h, "a serving step
+// on resident KV").
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "lv_batch.cuh"
+
+namespace lv {
+
+namespace {
+
+constexpr int kPlanThreads = 256;
+
+// Sum over the CTA, to every thread.  ws: one word a warp; a barrier lies between its uses.
+__device__ __forceinline__ long long cta_sum(long long v, long long* ws) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = v;
+  __syncthreads();
+  long long s = 0;
+  for (int w = 0; w < kPlanThreads / 32; ++w) s += ws[w];
+  return s;
+}
+
+// Exclusive prefix over the CTA; *total receives the sum.
+__device__ __forceinline__ long long cta_scan(long long v, long long* ws, long long* total) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  long long x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) ws[wid] = x;
+  __syncthreads();
+  long long before = 0, sum = 0;
+  for (int w = 0; w < kPlanThreads / 32; ++w) {
+    if (w < wid) before += ws[w];
+    sum += ws[w];
+  }
+  *total = sum;
+  return before + x - v;
+}
+
+__device__ __forceinline__ int tiles_of(const PlanArgs& a, int len) {
+  return len > 0 ? (int)(((long long)len * a.G + a.tile_rows - 1) / a.tile_rows) : 0;
+}
+
+__device__ __forceinline__ AttnTile make_tile(const PlanArgs& a, const PlanReq& r, int req, int k) {
+  AttnTile t;
+  t.before = 0;
+  t.req = req;
+  t.row0 = k * a.tile_rows;
+  const int all = r.len * a.G;
+  t.rows = min(a.tile_rows, all - t.row0);
+  t.first = r.first;
+  t.qrow = r.qrow;
+  t.kv_hi = r.first + (t.row0 + t.rows - 1) / a.G + 1;
+  const int p0 = r.first + t.row0 / a.G;
+  t.kv_lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
+  const int hi = (t.kv_hi + a.unit - 1) / a.unit;
+  t.sink_units = min((min(a.sinks, t.kv_lo) + a.unit - 1) / a.unit, hi);
+  t.win_unit = max(t.kv_lo / a.unit, t.sink_units);
+  t.units = t.sink_units + hi - t.win_unit;
+  return t;
+}
+
+// CTA i < n: request i's rows, table row and checks; CTA n: the rows of no request.  Every CTA
+// sums the lengths before its own (at most 16 KiB that stay in L2: less than a launch between
+// a scan and the rest would cost).  The CTA that finishes last cuts the requests into tiles
+// and the tiles' units into equal shares.
+__global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
+  __shared__ long long ws[kPlanThreads / 32];
+  __shared__ int last;
+  dep_wait();
+  dep_trigger();
+  const int i = blockIdx.x;
+  const DevPool& p = a.p;
+  long long mine = 0;
+  for (int j = threadIdx.x; j < i; j += kPlanThreads) mine += max(a.lens[j], 0);
+  const long long start = cta_sum(mine, ws);
+  const int row0 = (int)min(start, (long long)a.num_tokens);
+  if (threadIdx.x == 0) a.row_starts[i] = row0;
+  if (i == a.n) {
+    for (int r = row0 + threadIdx.x; r < a.num_tokens; r += kPlanThreads) {
+      a.positions[r] = -1;
+      a.slots[r] = -1;
+    }
+  } else {
+    const int sid = a.sids[i];
+    const int asked = a.lens[i];
+    const int len = max(asked, 0);
+    int err = 0;
+    int first = 0;
+    const bool known = sid >= 0 && sid < p.S;
+    if (!known || asked < 0 || asked > a.max_len || start + len > a.num_tokens) {
+      err = LV_ERR_BOUNDS;
+    } else {
+      const int ctx = p.sess[sid].ctx_tokens;
+      first = a.firsts ? a.firsts[i] : -1;
+      if (first < 0) first = ctx - len;
+      if (first < 0 || (long long)first + len > ctx || ((long long)ctx + p.T - 1) / p.T > p.maxB) err = LV_ERR_BOUNDS;
+    }
+    const int32_t* row = p.table + (size_t)(known ? sid : 0) * p.maxB;
+    int32_t* out = a.tables + (size_t)i * p.maxB;
+    const int kv_len = err ? 0 : first + len;
+    const int nb = (int)(((uint32_t)kv_len + (uint32_t)p.T - 1u) / (uint32_t)p.T);
+    // blocks that some row sees: from the first row's window on, and the sinks
+    const int lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
+    const int lo_blk = lo / p.T;
+    const int sink_blk = (int)(((uint32_t)min(a.sinks, kv_len) + (uint32_t)p.T - 1u) / (uint32_t)p.T);
+    bool absent = false;
+    for (int b = threadIdx.x; b < p.maxB; b += kPlanThreads) {
+      int e = -1;
+      if (b < nb) {
+        e = row[b];
+        if (e < 0 || e >= p.hbm_pages) {
+          e = -1;
+          absent |= len > 0 && (b >= lo_blk || b < sink_blk);
+        }
+      }
+      out[b] = e;
+    }
+    if (__syncthreads_or(absent)) {
+      err = LV_ERR_STATE;
+      for (int b = threadIdx.x; b < nb; b += kPlanThreads) out[b] = -1;   // its own entries again
+    }
+    if (threadIdx.x == 0) {
+      if (err) report(p.ctl, err, i);
+      a.kv_lens[i] = err ? 0 : kv_len;
+      a.reqs[i] = PlanReq{first, err ? 0 : len, row0, 0};
+    }
+    const int rows = (int)min((long long)len, a.num_tokens - (long long)row0);
+    for (int r = threadIdx.x; r < rows; r += kPlanThreads) {
+      int pos = -1;
+      long long slot = -1;
+      if (!err) {
+        pos = first + r;
+        const int b = (int)((uint32_t)pos / (uint32_t)p.T);
+        slot = (long long)row[b] * p.T + (pos - b * p.T);
+        if (p.incl && p.shadow[(size_t)sid * p.maxB + b] >= 0) slot = -slot - 2;
+      }
+      a.positions[row0 + r] = pos;
+      a.slots[row0 + r] = slot;
+    }
+  }
+
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(&a.head->ticket, 1) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  const volatile PlanReq* reqs = a.reqs;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  // each request's first tile: a scan over the requests, kept in its pad word
+  long long tiles = 0, live = 0;
+  for (int base = 0; base < a.n; base += kPlanThreads) {
+    const int q = base + threadIdx.x;
+    const int len = q < a.n ? reqs[q].len : 0;
+    long long total;
+    const long long at = cta_scan(tiles_of(a, len), ws, &total);
+    if (q < a.n) a.reqs[q].pad = (int)(tiles + at);
+    tiles += total;
+    live += len;
+  }
+  live = cta_sum(live, ws);
+  const int n_tiles = (int)min(tiles, (long long)a.max_tiles);
+  // a warp a request writes its tiles
+  for (int q = wid; q < a.n; q += kPlanThreads / 32) {
+    const PlanReq r{reqs[q].first, reqs[q].len, reqs[q].qrow, reqs[q].pad};
+    const int m = tiles_of(a, r.len);
+    for (int k = lane; k < m; k += 32)
+      if (r.pad + k < n_tiles) a.tiles[r.pad + k] = make_tile(a, r, q, k);
+  }
+  __syncthreads();
+  long long units = 0;
+  for (int base = 0; base < n_tiles; base += kPlanThreads) {
+    const int t = base + threadIdx.x;
+    const int u = t < n_tiles ? a.tiles[t].units : 0;
+    long long total;
+    const long long at = cta_scan(u, ws, &total);
+    if (t < n_tiles) a.tiles[t].before = (units + at) * a.groups;
+    units += total;
+  }
+  units *= a.groups;
+  const long long share = max((units + a.ctas - 1) / a.ctas, (long long)a.min_share);
+  if (threadIdx.x == 0)
+    *a.head = PlanHead{units, share, n_tiles, a.num_tokens - (int)live, 0, 0};
+  __syncthreads();
+  // the tile of each CTA's first unit
+  for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
+    const long long lo = a.tiles[t].before, hi = lo + (long long)a.tiles[t].units * a.groups;
+    for (long long c = (lo + share - 1) / share; c * share < hi && c <= a.ctas; ++c) a.cta_tile[c] = t;
+  }
+}
+
+// ---------------------------------------------------------------- KV write
+// A thread moves 8 elements: out[slot][h][8c..] <- src[r][h][8c..], both K and V in one launch.
+// What bounds it: the launch for a decode step; HBM for a prompt's rows.
+constexpr int kWriteThreads = 256;
+
+template <bool kBf16>
+__device__ __forceinline__ uint4 load8(const uint8_t* src, int64_t at, int type, bool vec) {
+  if (type == LV_F32) {
+    const float* f = reinterpret_cast<const float*>(src) + at;
+    float x[8];
+    if (vec) {
+      const float4 lo = __ldcs(reinterpret_cast<const float4*>(f)), hi = __ldcs(reinterpret_cast<const float4*>(f) + 1);
+      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
+      x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = f[e];
+    }
+    return make_uint4(pack16<kBf16>(x[0], x[1]), pack16<kBf16>(x[2], x[3]), pack16<kBf16>(x[4], x[5]),
+                      pack16<kBf16>(x[6], x[7]));
+  }
+  const uint16_t* h = reinterpret_cast<const uint16_t*>(src) + at;
+  uint4 w;
+  if (vec) {
+    w = __ldcs(reinterpret_cast<const uint4*>(h));
+  } else {
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (uint32_t)h[2 * e] | (uint32_t)h[2 * e + 1] << 16;
+    w = make_uint4(y[0], y[1], y[2], y[3]);
+  }
+  if ((type == LV_BF16) == kBf16) return w;
+  // the other 16-bit type: through 32 bits, which hold both exactly
+  uint32_t* y = &w.x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float2 f;
+    if (kBf16) f = __half22float2(*reinterpret_cast<const __half2*>(&y[e]));
+    else f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y[e]));
+    y[e] = pack16<kBf16>(f.x, f.y);
+  }
+  return w;
+}
+
+template <bool kBf16>
+__global__ void __launch_bounds__(kWriteThreads) k_kv_write(WriteArgs a) {
+  dep_wait();
+  const uint32_t cols = (uint32_t)a.D / 8u, per_kv = (uint32_t)a.H * cols, per_row = 2u * per_kv;
+  const uint64_t total = (uint64_t)a.num_tokens * per_row;
+  for (uint64_t i = (uint64_t)blockIdx.x * kWriteThreads + threadIdx.x; i < total;
+       i += (uint64_t)gridDim.x * kWriteThreads) {
+    const uint32_t r = (uint32_t)(i / per_row), x = (uint32_t)(i - (uint64_t)r * per_row);
+    const int kv = x >= per_kv;
+    const uint32_t y = kv ? x - per_kv : x;
+    const uint32_t h = y / cols, c = y - h * cols;
+    const int64_t slot = a.slots[r];
+    if (slot < 0 || slot >= a.num_slots) {
+      if (x == 0 && slot != -1) report(a.ctl, slot < 0 ? LV_ERR_STATE : LV_ERR_BOUNDS, r);
+      continue;
+    }
+    const uint4 w = load8<kBf16>(a.src[kv], r * a.row_stride[kv] + h * a.head_stride[kv] + 8 * c, a.src_type[kv],
+                                 a.vec[kv] != 0);
+    *reinterpret_cast<uint4*>(a.dst[kv] + ((uint64_t)slot * per_kv + y) * 16u) = w;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_plan(const PlanArgs& a, cudaStream_t s) {
+  return launch_dependent(k_batch_plan, dim3(a.n + 1), kPlanThreads, 0, s, a);
+}
+
+cudaError_t launch_kv_write(const WriteArgs& a, cudaStream_t s, int num_sms) {
+  const long long units = (long long)a.num_tokens * 2 * a.H * (a.D / 8);
+  const long long need = (units + kWriteThreads - 1) / kWriteThreads;
+  const dim3 grid((unsigned)(need < num_sms * 32ll ? need : num_sms * 32ll));
+  return launch_dependent(a.dtype == LV_BF16 ? k_kv_write<true> : k_kv_write<false>, grid, kWriteThreads, 0, s, a);
+}
+
+}  // namespace lv

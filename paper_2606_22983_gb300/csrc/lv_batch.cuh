@@ -1,0 +1,192 @@
+// A serving step on resident KV: what its plan leaves on the device, and the launches of
+// lv_batch.cu (plan, KV write), lv_attend.cu (attention of few rows a request, join of split
+// work) and lv_attend_tc.cu (attention of many rows, tcgen05).
+#pragma once
+
+#include <cuda.h>
+#include <utility>
+
+#include "lv_internal.cuh"
+
+namespace lv {
+
+// The rows of one request in one tile of the attention's work: up to the kernel's tile height
+// of packed rows, packed row R of a request being query head R % G (of its KV head) of new
+// token R / G, so that the G heads that share a KV head read it once.  Its keys are cut into
+// units of the kernel's size: first the units that hold sinks, then those from the window on.
+struct AttnTile {
+  int64_t before;       // units of every head group in the tiles before it
+  int32_t req;
+  int32_t row0;         // its first packed row
+  int32_t rows;         // its packed rows
+  int32_t units;        // units a head group
+  int32_t sink_units;   // unit u < sink_units starts at key u * unit,
+  int32_t win_unit;     // the others at key (win_unit + u - sink_units) * unit
+  int32_t first;        // position of the request's first new token
+  int32_t qrow;         // its row in the step's tensors
+  int32_t kv_lo;        // first key in the window of the tile's first row
+  int32_t kv_hi;        // keys up to the tile's last row
+};
+static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
+
+// What the kernels read of a plan besides its tiles.  The units of every (tile, head group)
+// pair, in that order, form one line of `units`; CTA c of the attention takes
+// [c * share, (c + 1) * share), whatever tiles that cuts, and the cut ones are joined.
+struct PlanHead {
+  int64_t units;
+  int64_t share;
+  int32_t tiles;
+  int32_t dead;         // rows of no request
+  int32_t ticket;       // CTAs of the plan that are done
+  int32_t pad;
+};
+
+struct PlanReq {        // per request, from the plan's first half to its second
+  int32_t first, len, qrow, pad;   // len 0: left out
+};
+
+struct PlanArgs {
+  DevPool p;
+  const int32_t* sids;
+  const int32_t* firsts;   // or null
+  const int32_t* lens;
+  int32_t n, num_tokens, max_len;
+  int32_t G;               // query heads a KV head
+  int32_t groups;          // head groups a tile is taken by (one CTA each)
+  int32_t tile_rows, unit; // of the attention kernel that will run
+  int32_t min_share;       // units a CTA takes at least
+  int32_t ctas;            // of the attention
+  int32_t window, sinks;
+  int32_t* row_starts;
+  int32_t* kv_lens;
+  int32_t* tables;
+  int32_t* positions;
+  int64_t* slots;
+  PlanReq* reqs;
+  AttnTile* tiles;
+  int32_t max_tiles;
+  int32_t* cta_tile;       // [ctas + 1] the tile that CTA c's first unit is in
+  PlanHead* head;
+};
+
+struct WriteArgs {
+  uint8_t* dst[2];         // the layer's K and V sub-page arrays
+  const uint8_t* src[2];
+  int64_t row_stride[2], head_stride[2];
+  int32_t src_type[2];
+  int32_t vec[2];          // 16-byte loads allowed
+  const int64_t* slots;
+  int32_t num_tokens, H, D, dtype;
+  int64_t num_slots;       // hbm_pages * T
+  long long* ctl;
+};
+
+struct AttnArgs {
+  const uint8_t* kv[2];    // the layer's K and V sub-page arrays
+  int64_t P;
+  uint32_t hbm_pages;
+  int32_t T, H, D, G;
+  int32_t maxB;
+  const int32_t* tables;
+  const int32_t* positions;
+  const AttnTile* tiles;
+  const int32_t* cta_tile;
+  const PlanHead* head;
+  const uint8_t* q;
+  uint8_t* out;
+  float* lse;
+  int64_t q_row, q_head, o_row, o_head;   // strides in elements
+  int32_t q_vec, o_vec;    // 16-byte accesses allowed
+  int32_t num_tokens;
+  int32_t window, sinks;
+  int32_t groups, hg;      // head groups, and KV heads in one
+  int32_t tile_rows;       // rows of a partial result's slot (per head of the group)
+  int32_t dp;              // columns of a partial result
+  float scale;             // scale * log2(e)
+  float* part_o;           // [2 * ctas][hg][tile_rows][dp] sums, and
+  float2* part_ml;         // [2 * ctas][hg][tile_rows] their maximum (in log2) and weight
+  long long* ctl;
+};
+
+// CTA c's slot for a piece of a (tile, head group) pair that it holds only part of: a piece
+// that does not start the pair is the first that the CTA does, one that starts it the last.
+__host__ __device__ inline int64_t part_slot(int64_t cta, bool starts) { return 2 * cta + (starts ? 1 : 0); }
+
+enum AttnKind : int { ATTN_ROWS16 = 0, ATTN_ROWS32 = 1, ATTN_TC = 2 };
+
+cudaError_t launch_plan(const PlanArgs& a, cudaStream_t s);
+cudaError_t launch_kv_write(const WriteArgs& a, cudaStream_t s, int num_sms);
+cudaError_t configure_attend();
+cudaError_t configure_attend_tc();
+// keys of a unit, and CTAs that an SM holds, of the rows kernel
+constexpr int kRowsUnit = 16;
+int attend_rows_ctas(int dp, bool wide);
+cudaError_t launch_attend_rows(const AttnArgs& a, bool wide, bool bf16, int ctas, cudaStream_t s);
+constexpr int kTcUnit = 128, kTcRows = 256;
+cudaError_t launch_attend_tc(const AttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int box_rows, bool bf16,
+                             int ctas, cudaStream_t s);
+cudaError_t launch_attend_join(const AttnArgs& a, bool bf16, int ctas, cudaStream_t s);
+
+// A launch that may be scheduled while the previous kernel on `s` still runs; the kernel waits
+// (pdl_wait) before it reads anything that kernel may have written.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t s,
+                             Args&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void report(long long* ctl, int code, long long detail) {
+  if (atomicCAS(reinterpret_cast<unsigned long long*>(&ctl[C_ERR]), 0ull, (unsigned long long)code) == 0ull)
+    ctl[C_ERR_DETAIL] = detail;
+}
+__device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ AttnTile load_tile(const AttnTile* t) {
+  union {
+    int4 w[3];
+    AttnTile t;
+  } x;
+  const int4* q = reinterpret_cast<const int4*>(t);
+  x.w[0] = q[0];
+  x.w[1] = q[1];
+  x.w[2] = q[2];
+  return x.t;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two floats rounded to 16 bits, the first in the low half.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  uint32_t r;
+  if (kBf16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// A weight is at most 2^(kLazy + bias) times its row's true one: the running maximum is only
+// raised when a row outgrows it by 2^kLazy, so that the sums are seldom rescaled.  In f16 the
+// weights are kept near the top of the type's range (2^15 at most): one that is 2^-22 of the
+// row's largest still has full precision, where 2^-14 would be the end without the bias.
+constexpr float kLazy = 8.0f;
+template <bool kBf16>
+__device__ __forceinline__ constexpr float weight_bias() {
+  return kBf16 ? 0.0f : 7.0f;
+}
+#endif
+
+}  // namespace lv

@@ -83,6 +83,22 @@ class lv_controller_counters(ctypes.Structure):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
 
 
+class lv_batch_desc(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("max_requests", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("row_starts", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p),
+                ("tables", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("reserved", ctypes.c_int32 * 2)]
+
+
+class lv_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+LV_BF16, LV_F16, LV_F32 = 1, 2, 3
+
+
 class lv_stats(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in (
         "hbm_allocated", "host_allocated", "hbm_budget_pages", "host_pages", "error",
@@ -187,6 +203,12 @@ def _load():
         "lv_session_counts": [vp, vp, vp, vp],
         "lv_session_blocks": [vp, i32, i32, vp, vp, vp],
         "lv_read_tables": [vp, vp, vp, vp, vp],
+        "lv_batch_create": [vp, ctypes.POINTER(lv_batch_desc), ctypes.POINTER(vp)],
+        "lv_batch_destroy": [vp, vp],
+        "lv_batch_plan": [vp, vp, vp, vp, i32, i32, i32, vp],
+        "lv_kv_write": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp],
+        "lv_attention": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp,
+                         ctypes.c_float, vp],
         "lv_sync": [vp, vp],
         "lv_get_stats": [vp, ctypes.POINTER(lv_stats), vp],
         "lv_clear_error": [vp, vp],
@@ -223,7 +245,8 @@ EXPORTED = ("lv_pool_create", "lv_pool_destroy", "lv_pool_host_ptr", "lv_pool_im
             "lv_selftest_wait", "lv_turn", "lv_evict", "lv_join", "lv_page_checksums",
             "lv_controller_create", "lv_controller_destroy", "lv_controller_tick",
             "lv_controller_speech", "lv_controller_turn_begin", "lv_controller_turn_loaded",
-            "lv_controller_records", "lv_controller_counters_get")
+            "lv_controller_records", "lv_controller_counters_get", "lv_batch_create",
+            "lv_batch_destroy", "lv_batch_plan", "lv_kv_write", "lv_attention")
 
 
 def lib():
@@ -438,6 +461,42 @@ def lv_session_blocks(pool, sid, where, blks_out, count_out, stream=None):
 def lv_read_tables(pool, tables, hbm_owner, host_owner, stream=None):
     _check(_lib.lv_read_tables(pool, ptr(tables), ptr(hbm_owner), ptr(host_owner),
                                stream_handle(stream)), "lv_read_tables")
+
+
+def lv_batch_create(pool, desc: lv_batch_desc):
+    h = ctypes.c_void_p()
+    _check(_lib.lv_batch_create(pool, ctypes.byref(desc), ctypes.byref(h)), "lv_batch_create")
+    return h.value
+
+
+def lv_batch_destroy(batch, stream=None):
+    _check(_lib.lv_batch_destroy(batch, stream_handle(stream)), "lv_batch_destroy")
+
+
+def lv_batch_plan(batch, sids, firsts, lens, n, num_tokens, max_len, stream=None):
+    _check(_lib.lv_batch_plan(batch, ptr(sids), ptr(firsts), ptr(lens), n, num_tokens, max_len,
+                              stream_handle(stream)), "lv_batch_plan")
+
+
+def heads(x) -> lv_heads:
+    """The lv_heads of a torch tensor [rows][heads][head_dim] (the last dimension contiguous)."""
+    import torch
+    kinds = {torch.bfloat16: LV_BF16, torch.float16: LV_F16, torch.float32: LV_F32}
+    if x.dim() != 3 or x.dtype not in kinds or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("expected a [rows, heads, head_dim] tensor of bf16, f16 or f32 with "
+                         "contiguous head_dim")
+    return lv_heads(data=x.data_ptr(), row_stride=x.stride(0), head_stride=x.stride(1),
+                    dtype=kinds[x.dtype], reserved=0)
+
+
+def lv_kv_write(batch, layer, k: lv_heads, v: lv_heads, stream=None):
+    _check(_lib.lv_kv_write(batch, layer, ctypes.byref(k), ctypes.byref(v), stream_handle(stream)),
+           "lv_kv_write")
+
+
+def lv_attention(batch, layer, q: lv_heads, out: lv_heads, lse, scale, stream=None):
+    _check(_lib.lv_attention(batch, layer, ctypes.byref(q), ctypes.byref(out), ptr(lse), scale,
+                             stream_handle(stream)), "lv_attention")
 
 
 def lv_sync(pool, stream=None, raise_on_error=True) -> int:

@@ -34,6 +34,7 @@ class KVPool:
             if device is None else torch.device(device)
         self.stream = stream
         self.L, self.T = layers, page_tokens
+        self.kv_heads, self.head_dim = kv_heads, head_dim
         self.J = 2 * layers
         self.P = page_tokens * kv_heads * head_dim * elem_bytes
         self.S, self.max_blocks = max_sessions, max_blocks
