@@ -1633,6 +1633,10 @@ lv_status lv_selftest_wait(lv_pool* pool, int64_t limit_us, lv_stream stream) {
 // ------------------------------------------------- a serving step on resident KV
 }  // extern "C"
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct lv_batch {
   lv_pool* pool = nullptr;
   lv_batch_desc d{};
@@ -1648,6 +1652,7 @@ struct lv_batch {
   int32_t dp = 128;          // the kernels' columns: head_dim rounded up to 64, 128 or 256
   int32_t hg = 1;            // KV heads that a CTA of the rows kernel takes
   int32_t box_rows = 0;      // keys in a TMA box; 0: the pages cannot be read by TMA
+  EncodeTiled encode = nullptr;    // cuTensorMapEncodeTiled
   std::vector<CUtensorMap> maps;   // [2L]
   // the planned step
   bool planned = false;
@@ -1682,6 +1687,16 @@ int32_t gcd(int32_t a, int32_t b) {
   return a;
 }
 
+// A four-dimensional map of 16-bit elements, read in boxes whose first 64 elements are one
+// swizzled row of 128 bytes.
+bool encode_map(const lv_batch* b, CUtensorMap* m, void* at, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3],
+                const cuuint32_t (&box)[4]) {
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  return b->encode(m, b->d.dtype == LV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, at,
+                   dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Tensor maps of the 2L sub-page arrays, [page][T][H][D] with boxes of box_rows keys and 64
 // columns: pages whose T is a multiple of 8 hold whole groups of eight 128-byte rows, which the
 // swizzle repeats over.
@@ -1689,28 +1704,31 @@ lv_status make_maps(lv_batch* b) {
   const lv_pool* pool = b->pool;
   const int32_t box = gcd(pool->d.T, lv::kTcUnit);
   if (box < 8 || b->dp > 128) return LV_OK;
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult found{};
   if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
       found != cudaDriverEntryPointSuccess || !fn)
     return LV_ERR_CUDA;
-  const auto encode = reinterpret_cast<Encode>(fn);
+  b->encode = reinterpret_cast<EncodeTiled>(fn);
   const cuuint64_t D = pool->head_dim, H = pool->kv_heads, T = pool->d.T;
-  const cuuint64_t dims[4] = {D, H, T, (cuuint64_t)pool->d.hbm_pages};
-  const cuuint64_t strides[3] = {D * 2, H * D * 2, (cuuint64_t)pool->d.P};
-  const cuuint32_t boxes[4] = {64, 1, (cuuint32_t)box, 1}, ones[4] = {1, 1, 1, 1};
   b->maps.resize(pool->d.J);
   for (int j = 0; j < pool->d.J; ++j)
-    if (encode(&b->maps[j],
-               b->d.dtype == LV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
-               pool->kv[j], dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    if (!encode_map(b, &b->maps[j], pool->kv[j], {D, H, T, (cuuint64_t)pool->d.hbm_pages},
+                    {D * 2, H * D * 2, (cuuint64_t)pool->d.P}, {64, 1, (cuuint32_t)box, 1}))
       return LV_ERR_CUDA;
   b->box_rows = box;
   return LV_OK;
+}
+
+// A map of the queries [rows][H][G][D], a box 64 columns of the G heads of 128 / G rows; false
+// where their strides or G do not allow one.
+bool query_map(const lv_batch* b, const lv_heads* q, CUtensorMap* m) {
+  const int64_t lim = 1ll << 39;      // (a map's strides are below 2^40 bytes)
+  const int64_t head = q->head_stride * 2, row = q->row_stride * 2;
+  if (b->G > 128 || head <= 0 || row <= 0 || head * b->G >= lim || row >= lim) return false;
+  const cuuint64_t D = b->pool->head_dim, H = b->pool->kv_heads, G = b->G;
+  return encode_map(b, m, q->data, {D, G, H, (cuuint64_t)b->num_tokens},
+                    {(cuuint64_t)head, G * (cuuint64_t)head, (cuuint64_t)row}, {64, (cuuint32_t)G, 1, (cuuint32_t)(128 / G)});
 }
 
 bool device_array(const lv_pool* pool, const void* p, size_t align) {
@@ -1852,7 +1870,7 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     a.G = b->G;
     if (b->kind == lv::ATTN_TC) {
       a.groups = pool->kv_heads;
-      a.tile_rows = lv::kTcRows;
+      a.tile_rows = lv::tc_tile_rows(b->G);
       a.unit = lv::kTcUnit;
       a.min_share = 4;
       b->ctas = pool->num_sms;
@@ -1953,15 +1971,18 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.sinks = b->d.sinks;
   a.groups = tc ? pool->kv_heads : pool->kv_heads / b->hg;
   a.hg = tc ? 1 : b->hg;
-  a.tile_rows = tc ? lv::kTcRows : b->kind == lv::ATTN_ROWS32 ? 32 : 16;
+  a.tile_rows = tc ? lv::tc_tile_rows(b->G) : b->kind == lv::ATTN_ROWS32 ? 32 : 16;
   a.dp = b->dp;
   a.scale = scale * 1.44269504088896341f;
   a.part_o = b->part_o;
   a.part_ml = b->part_ml;
   a.ctl = pool->d.ctl;
-  if (tc)
-    LV_TRY(lv::launch_attend_tc(a, b->maps[2 * layer], b->maps[2 * layer + 1], b->box_rows, bf16, b->ctas, s));
-  else
+  if (tc) {
+    CUtensorMap qmap;
+    const lv::TcMaps m{&b->maps[2 * layer], &b->maps[2 * layer + 1],
+                       a.q_vec && query_map(b, q, &qmap) ? &qmap : nullptr, b->box_rows};
+    LV_TRY(lv::launch_attend_tc(a, m, bf16, b->ctas, s));
+  } else
     LV_TRY(lv::launch_attend_rows(a, b->kind == lv::ATTN_ROWS32, bf16, b->ctas, s));
   LV_TRY(lv::launch_attend_join(a, bf16, b->ctas, s));
   return LV_OK;

@@ -7,7 +7,7 @@ namespace lv {
 namespace {
 
 // Roles of a CTA's twelve warps.
-constexpr int kSoftWarps = 8;             // two warpgroups, one for each tile of 128 rows
+constexpr int kSoftWarps = 8;             // two warpgroups, one for each half of a tile
 constexpr int kWarpKv = 8, kWarpMma = 9, kWarpQ = 10;   // and 11: queries of tile 0 and 1
 constexpr int kThreads = 384;
 constexpr int kKeys = kTcUnit;            // keys of a unit
@@ -21,17 +21,20 @@ struct TcShape {
   static constexpr int kHalves = DP / 64;                  // 128-byte wide column blocks
   static constexpr int kBlock = kKeys * DP * 2;            // bytes of a K or V unit, and of a Q tile
   static constexpr int kStages = DP == 128 ? 5 : 8;
-  static constexpr int kSmem = 2 * kBlock + kStages * kBlock + 1024;
+  static constexpr int kData = 2 * kBlock + kStages * kBlock;
+  static constexpr int kSmem = kData + 256;                // then the barriers
   static constexpr int kColO = 256;                        // S0 at column 0, S1 at 128, O0, O1
+  static_assert(kSmem + 1024 <= 227 * 1024, "shared memory of a CTA");
 };
 
 struct Bars {
   uint64_t kv_full[8], kv_empty[8];
-  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2];
   uint64_t drain;
   uint32_t tmem;
   volatile int bad;
 };
+static_assert(sizeof(Bars) <= 256, "its room in shared memory");
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
@@ -79,6 +82,19 @@ __device__ __forceinline__ bool bar_wait(Bars* b, uint64_t* bar, uint32_t parity
 }
 
 // ---- tcgen05
+// One lane of the warp, always the same.  (With a test of the lane number in its place the
+// compiler cannot tell that one thread issues, and a product took 109 cycles to issue, not 64.)
+__device__ __forceinline__ bool elected() {
+  uint32_t e;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(e)
+      :
+      : "memory");
+  return e != 0;
+}
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
@@ -121,6 +137,14 @@ __device__ __forceinline__ void tc_ld16(uint32_t* x, uint32_t at) {
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : LV_R8(x, 0), LV_R8(x, 8)
       : "r"(at));
+}
+__device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* x) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+      "%30,%31};" ::LV_W8(x, 0),
+      LV_W8(x, 8), LV_W8(x, 16), LV_W8(x, 24), "r"(at)
+      : "memory");
 }
 __device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t* x) {
   asm volatile(
@@ -213,26 +237,57 @@ struct Pairs {
   }
 };
 
-// Weights of one tile's rows for one unit: a thread a row.  S is read from TMEM, and the weights
-// replace it there in 16 bits, two to a column, as the left operand of the product with V.
+// The n lowest bits, all of them from 32 on, none below 1.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Weights of 64 keys, s[0..64) scaled by c and moved by b, in 16 bits; returns their sum.
+template <bool kBf16>
+__device__ __forceinline__ float weights64(const float* s, float c, float b, uint32_t* w) {
+  const float2 c2 = make_float2(c, c), b2 = make_float2(b, b);
+  float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    float2 y = fma2(make_float2(s[2 * j], s[2 * j + 1]), c2, b2);
+    y.x = exp2_fast(y.x);
+    y.y = exp2_fast(y.y);
+    if (j & 1) acc1 = add2(acc1, y);
+    else acc0 = add2(acc0, y);
+    w[j] = pack16<kBf16>(y.x, y.y);
+  }
+  acc0 = add2(acc0, acc1);
+  return acc0.x + acc0.y;
+}
+
+// One unit's weights of one half of a tile: a thread a row.  S is read from TMEM, and the weights
+// replace it there in 16 bits, two to a column, as the left operand of the product with V, which
+// starts on the first 64 keys while the others' weights are computed.  The first 64 are taken
+// against the maximum so far, beside the search for this unit's; only where that shows a row to
+// have outgrown it are they taken again (and in a pair's first unit).
 template <int DP, bool kBf16>
 struct Softmax {
-  float top, sum;      // of the raw scores; sum of the weights
+  float top, sum;      // of the raw scores; of the weights
   __device__ __forceinline__ void step(const AttnArgs& a, uint32_t s_at, uint32_t o_at, bool fresh, bool open, int key0,
-                                       int pos, float c) {
+                                       int pos, uint64_t* first_half) {
+    const float c = a.scale;
     uint32_t x[128];
+    float* s = reinterpret_cast<float*>(x);
 #pragma unroll
     for (int i = 0; i < 4; ++i) tc_ld32(x + 32 * i, s_at + 32 * i);
     tc_wait_ld();
     tc_loaded<128>(x);
-    float* s = reinterpret_cast<float*>(x);
     if (!open) {
       // keys key0 + i: seen up to pos, from the window's start or among the sinks
-      const int hi = pos - key0, lo = a.window > 0 ? pos - a.window - key0 : -1, sk = a.sinks - key0;
+      const int upto = pos + 1 - key0, before = a.window > 0 ? upto - a.window : 0, sinks = a.sinks - key0;
 #pragma unroll
-      for (int i = 0; i < 128; ++i)
-        if (i > hi || (i <= lo && i >= sk)) s[i] = -INFINITY;
+      for (int i = 0; i < 128; i += 32) {
+        const uint32_t m = low_bits(upto - i) & (~low_bits(before - i) | low_bits(sinks - i));
+#pragma unroll
+        for (int j = 0; j < 32; ++j) s[i + j] = m >> j & 1u ? s[i + j] : -INFINITY;
+      }
     }
+    float b = weight_bias<kBf16>() - (top == -INFINITY ? 0.f : top * c);
+    uint32_t w[32];
+    float part = weights64<kBf16>(s, c, b, w);
     float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
 #pragma unroll
     for (int i = 4; i < 128; i += 4) {
@@ -240,52 +295,39 @@ struct Softmax {
       m1 = fmaxf(fmaxf(m1, s[i + 2]), s[i + 3]);
     }
     const float high = fmaxf(fmaxf(m0, m1), top);
-    const bool raise = (high - top) * c > kLazy;      // (NaN from -inf - -inf: no)
-    if (fresh) {
-      top = high;
-    } else if (__any_sync(0xffffffffu, raise)) {
-      // S of this unit follows the previous unit's product with V: O is at rest
+    if (__any_sync(0xffffffffu, (high - top) * c > kLazy)) {      // (also from -inf; -inf - -inf: no)
       const float f = high == top ? 1.f : exp2_fast((top - high) * c);
       top = high;
       sum *= f;
+      if (!fresh) {
+        // S of this unit follows the previous unit's product with V: O is at rest
 #pragma unroll
-      for (int i = 0; i < DP; i += 16) {
-        uint32_t o[16];
-        tc_ld16(o, o_at + i);
-        tc_wait_ld();
-        tc_loaded<16>(o);
+        for (int i = 0; i < DP; i += 16) {
+          uint32_t o[16];
+          tc_ld16(o, o_at + i);
+          tc_wait_ld();
+          tc_loaded<16>(o);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-        tc_st16(o_at + i, o);
+          for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+          tc_st16(o_at + i, o);
+        }
       }
+      b = weight_bias<kBf16>() - (top == -INFINITY ? 0.f : top * c);
+      part = weights64<kBf16>(s, c, b, w);
     }
-    const float b = weight_bias<kBf16>() - (top == -INFINITY ? 0.f : top * c);
-    const float2 c2 = make_float2(c, c), b2 = make_float2(b, b);
-    float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t w[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int k = 32 * i + 2 * j;
-        float2 y = fma2(make_float2(s[k], s[k + 1]), c2, b2);
-        y.x = exp2_fast(y.x);
-        y.y = exp2_fast(y.y);
-        if (j & 1) acc1 = add2(acc1, y);
-        else acc0 = add2(acc0, y);
-        w[j] = pack16<kBf16>(y.x, y.y);
-      }
-      tc_st16(s_at + 16 * i, w);
-    }
-    acc0 = add2(acc0, acc1);
-    sum += acc0.x + acc0.y;
+    tc_st32(s_at, w);
+    tc_wait_st();
+    tc_fence_before();
+    bar_arrive(first_half);
+    sum += part + weights64<kBf16>(s + 64, c, b, w);
+    tc_st32(s_at + 32, w);
     tc_wait_st();
   }
 };
 
-// One CTA an SM: its share of the line of units.  A tile is 256 packed rows, two halves of 128
-// (an M = 128 tile of the tensor core each) whose softmaxes take turns: while one half's
-// weights are computed, the tensor core runs the other half's products.
+// One CTA an SM: its share of the line of units.  A tile is two halves of half_rows packed rows
+// (whole tokens; an M = 128 tile of the tensor core each) that take turns: while one half's weights are
+// computed, the tensor core runs the other half's products.
 //   warp 8   K and V units into a ring of shared memory, by TMA: a box a page and 64 columns;
 //            what the table has no page for, and rows past a tile's keys, reads as zeros
 //   warp 9   S = Q K^T (tcgen05, operands in shared memory), O += P V (P in TMEM)
@@ -294,23 +336,28 @@ struct Softmax {
 template <int DP, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1)
 k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap kmap,
-            const __grid_constant__ CUtensorMap vmap, int box_rows) {
+            const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap, int box_rows,
+            int half_rows, int q_tma) {
   using S = TcShape<DP>;
   extern __shared__ __align__(1024) unsigned char dyn[];
-  __shared__ Bars bars;
+  Bars& bars = *reinterpret_cast<Bars*>(dyn + S::kData);
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const uint32_t base = (smem_u32(dyn) + 1023u) & ~1023u;
-  const uint32_t q_s = base, ring_s = base + 2 * S::kBlock;
+  const uint32_t q_s = smem_u32(dyn), ring_s = q_s + 2 * S::kBlock;
+  if (q_s & 1023u) {      // (the swizzle's pattern starts at multiples of 1024 bytes)
+    if (threadIdx.x == 0) report(a.ctl, LV_ERR_CUDA, blockIdx.x);
+    return;
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
       bar_init(&bars.kv_full[i], 1);
       bar_init(&bars.kv_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      bar_init(&bars.q_full[i], 32);
+      bar_init(&bars.q_full[i], 1);
       bar_init(&bars.q_empty[i], 1);
       bar_init(&bars.s_full[i], 1);
-      bar_init(&bars.p_full[i], 128);
+      bar_init(&bars.p_full[i][0], 128);
+      bar_init(&bars.p_full[i][1], 128);
       bar_init(&bars.o_full[i], 1);
     }
     bar_init(&bars.drain, 1);
@@ -330,75 +377,75 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 
   if (wid < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
-    const int half = wid >> 2;
-    const int row = 128 * half + (threadIdx.x & 127);       // of the tile
-    const uint32_t lanes = (uint32_t)(wid & 3) << 21;       // this warp's 32 lanes of TMEM
-    const uint32_t s_at = tmem + lanes + 128 * half, o_at = tmem + lanes + S::kColO + DP * half;
+    const int half = wid >> 2, row = threadIdx.x & 127;                   // of the half
+    const uint32_t lanes = tmem + ((uint32_t)(wid & 3) << 21);            // this warp's 32 lanes of TMEM
+    const uint32_t s_at = lanes + 128 * half, o_at = lanes + S::kColO + DP * half;
     uint32_t s_par = 0, o_par = 0;
     Pairs pr;
     pr.init(a);
     bool ok = true;
     while (ok && pr.next(a)) {
-      if (pr.t.rows <= 128 * half) continue;                // nothing in this half
-      const bool live = pr.t.rows > (row & ~31);            // rows in this warp
-      const int R = pr.t.row0 + min(row, pr.t.rows - 1), token = R / a.G;
+      const int rows = min(half_rows, pr.t.rows - half * half_rows);
+      if (rows <= 0) continue;                              // nothing in this half
+      const bool live = rows > (row & ~31);                 // rows in this warp
+      const int R0 = pr.t.row0 + half * half_rows;
+      const int R = R0 + min(row, rows - 1), token = R / a.G;
       const int pos = pr.t.first + token;
-      const int p_lo = pr.t.first + (pr.t.row0 + 128 * half) / a.G;
-      const int p_hi = pr.t.first + (pr.t.row0 + min(128 * half + 127, pr.t.rows - 1)) / a.G;
+      const int p_lo = pr.t.first + R0 / a.G, p_hi = pr.t.first + (R0 + rows - 1) / a.G;
       Softmax<DP, kBf16> sm{-INFINITY, 0.f};
       for (int u = pr.u0; u < pr.u1; ++u) {
-        if (!bar_wait(&bars, &bars.s_full[half], s_par)) {
-          ok = false;
-          break;
-        }
+        if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par))) break;
         s_par ^= 1;
         if (live) {
           tc_fence_after();
           const int key0 = pr.key_of(u);
           const bool open =
               key0 + kKeys - 1 <= p_lo && (a.window == 0 || key0 > p_hi - a.window || key0 + kKeys <= a.sinks);
-          sm.step(a, s_at, o_at, u == pr.u0, open, key0, pos, a.scale);
+          sm.step(a, s_at, o_at, u == pr.u0, open, key0, pos, &bars.p_full[half][0]);
           tc_fence_before();
+        } else {
+          bar_arrive(&bars.p_full[half][0]);
         }
-        bar_arrive(&bars.p_full[half]);
+        bar_arrive(&bars.p_full[half][1]);
       }
-      if (!ok || !bar_wait(&bars, &bars.o_full[half], o_par)) break;
+      if (!ok || !(ok = bar_wait(&bars, &bars.o_full[half], o_par))) break;
       o_par ^= 1;
       if (!live) continue;
+      // the pair's end
       tc_fence_after();
       const bool whole = pr.u0 == 0 && pr.u1 == pr.t.units;
-      const int h = pr.head * a.G + (R - token * a.G);
+      const int hq = pr.head * a.G + (R - token * a.G);
       const int64_t r = pr.t.qrow + token;
-      const bool mine = row < pr.t.rows;
+      const bool mine = row < rows;
       const float inv = !whole ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
-      const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0) * a.tile_rows + row;
-      uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head;
+      const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0) * a.tile_rows + half * half_rows + row;
+      uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + hq * a.o_head;
 #pragma unroll
-      for (int i = 0; i < DP; i += 32) {
+      for (int col = 0; col < DP; col += 32) {
         uint32_t o[32];
-        tc_ld32(o, o_at + i);
+        tc_ld32(o, o_at + col);
         tc_wait_ld();
         tc_loaded<32>(o);
         if (mine && whole) {
 #pragma unroll
           for (int j = 0; j < 32; j += 8) {
-            if (i + j >= a.D) continue;
+            if (col + j >= a.D) continue;
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               w[e] = pack16<kBf16>(__uint_as_float(o[j + 2 * e]) * inv, __uint_as_float(o[j + 2 * e + 1]) * inv);
             if (a.o_vec) {
-              *reinterpret_cast<uint4*>(out + i + j) = make_uint4(w[0], w[1], w[2], w[3]);
+              *reinterpret_cast<uint4*>(out + col + j) = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                out[i + j + 2 * e] = (uint16_t)w[e];
-                out[i + j + 2 * e + 1] = (uint16_t)(w[e] >> 16);
+                out[col + j + 2 * e] = (uint16_t)w[e];
+                out[col + j + 2 * e + 1] = (uint16_t)(w[e] >> 16);
               }
             }
           }
         } else if (mine) {
-          float4* po = reinterpret_cast<float4*>(a.part_o + slot * DP + i);
+          float4* po = reinterpret_cast<float4*>(a.part_o + slot * DP + col);
 #pragma unroll
           for (int j = 0; j < 32; j += 4)
             po[j / 4] = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]),
@@ -410,9 +457,10 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       if (mine && !whole) {
         a.part_ml[slot] = make_float2(top2, sm.sum);
       } else if (mine && a.lse) {
-        a.lse[r * (a.H * a.G) + h] =
+        a.lse[r * (a.H * a.G) + hq] =
             sm.sum == 0.f ? -INFINITY : (top2 - weight_bias<kBf16>()) * 0.693147180559945f + logf(sm.sum);
       }
+      __syncwarp();
     }
     tc_fence_before();
   } else {
@@ -421,39 +469,43 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     pr.init(a);
     if (wid == kWarpKv) {
       // ---- K and V
+      // a lane a box: 64 columns of box_rows keys (at least 8, so that 32 lanes do)
       int stage = 0;
       uint32_t par = 0;               // of the ring's current round
       long long loads = 0;
       bool ok = true;
-      auto unit = [&](const CUtensorMap* map, int key0) -> bool {
-        if (!bar_wait(&bars, &bars.kv_empty[stage], par ^ 1)) return false;
-        if (lane == 0) bar_expect(&bars.kv_full[stage], S::kBlock);
-        __syncwarp();
-        const uint32_t dst = ring_s + stage * S::kBlock;
-        for (int i = lane; i < kKeys / box_rows * S::kHalves; i += 32) {
-          const int box = i / S::kHalves, x = i % S::kHalves;
-          const int key = key0 + box * box_rows;
-          const int b = key / a.T;
-          int page = -1;
-          if (key < pr.t.kv_hi && (key + box_rows > pr.t.kv_lo || key < a.sinks))
-            page = a.tables[(size_t)pr.t.req * a.maxB + b];
-          // no page: a box outside the array, which reads as zeros
-          if ((uint32_t)page >= a.hbm_pages) page = (int)a.hbm_pages;
-          tma_box(dst + x * kKeys * 128 + box * box_rows * 128, map, 64 * x, pr.head, key - b * a.T, page,
-                  &bars.kv_full[stage]);
-        }
-        ++loads;
-        if (++stage == S::kStages) {
-          stage = 0;
-          par ^= 1;
-        }
-        return true;
+      const int box = lane / S::kHalves, x = lane % S::kHalves;
+      const bool mine = box < kKeys / box_rows;
+      const uint32_t at = x * kKeys * 128 + box * box_rows * 128;
+      auto page_of = [&](int u) {
+        const int key = pr.key_of(u) + box * box_rows;
+        if (!mine || u >= pr.u1 || key >= pr.t.kv_hi || (key + box_rows <= pr.t.kv_lo && key >= a.sinks)) return -1;
+        return a.tables[(size_t)pr.t.req * a.maxB + key / a.T];
       };
-      while (ok && pr.next(a))
+      while (ok && pr.next(a)) {
+        int next = page_of(pr.u0);
         for (int u = pr.u0; ok && u < pr.u1; ++u) {
-          const int key0 = pr.key_of(u);
-          ok = unit(&kmap, key0) && unit(&vmap, key0);
+          // no page: a box outside the array, which reads as zeros
+          const int page = (uint32_t)next < a.hbm_pages ? next : (int)a.hbm_pages;
+          next = page_of(u + 1);
+          const int off = (pr.key_of(u) + box * box_rows) % a.T;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            if (!(ok = bar_wait(&bars, &bars.kv_empty[stage], par ^ 1))) break;
+            if (elected()) bar_expect(&bars.kv_full[stage], S::kBlock);
+            __syncwarp();
+            if (mine)
+              tma_box(ring_s + stage * S::kBlock + at, kv ? &vmap : &kmap, 64 * x, pr.head, off, page,
+                      &bars.kv_full[stage]);
+            __syncwarp();
+            ++loads;
+            if (++stage == S::kStages) {
+              stage = 0;
+              par ^= 1;
+            }
+          }
         }
+      }
       if (!ok) {      // let what is on its way land before the shared memory is given up
         const long long n = loads < S::kStages ? loads : S::kStages;
         for (long long i = loads - n; i < loads; ++i) {
@@ -475,32 +527,33 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
       };
       auto scores = [&](int half, int st) {      // S_half = Q_half K^T
-        if (lane == 0) {
+        const uint64_t qd = smem_desc(q_s + half * S::kBlock, 16, 1024), kd = smem_desc(ring_s + st * S::kBlock, 16, 1024);
+        if (elected()) {
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
-            const uint32_t at = (k / 4) * (kKeys * 128) + (k % 4) * 32;
-            tc_mma_ss(tmem + 128 * half, smem_desc(q_s + half * S::kBlock + at, 16, 1024),
-                      smem_desc(ring_s + st * S::kBlock + at, 16, 1024), kDescS, k > 0);
+            const uint32_t at = ((k / 4) * (kKeys * 128) + (k % 4) * 32) >> 4;
+            tc_mma_ss(tmem + 128 * half, qd + at, kd + at, kDescS, k > 0);
           }
           tc_commit(&bars.s_full[half]);
         }
         __syncwarp();
       };
-      auto values = [&](int half, int st, bool add) {      // O_half (+)= P_half V
-        if (lane == 0) {
+      auto values = [&](int half, int st, int part, bool add) {      // O_half (+)= P_half V, 64 keys of it
+        const uint64_t vd = smem_desc(ring_s + st * S::kBlock, kKeys * 128, 1024);
+        if (elected()) {
 #pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k)
-            tc_mma_ts(tmem + S::kColO + DP * half, tmem + 128 * half + 8 * k,
-                      smem_desc(ring_s + st * S::kBlock + k * 2048, kKeys * 128, 1024), kDescO, add || k > 0);
+          for (int k = 0; k < 4; ++k)
+            tc_mma_ts(tmem + S::kColO + DP * half, tmem + 128 * half + 32 * part + 8 * k,
+                      vd + (4 * part + k) * (2048 >> 4), kDescO, add || k > 0);
         }
         __syncwarp();
       };
       auto release = [&](uint64_t* bar) {
-        if (lane == 0) tc_commit(bar);
+        if (elected()) tc_commit(bar);
         __syncwarp();
       };
       while (ok && pr.next(a)) {
-        const int halves = pr.t.rows > 128 ? 2 : 1;
+        const int halves = pr.t.rows > half_rows ? 2 : 1;
         // the first unit's scores
         if (!(ok = bar_wait(&bars, &bars.kv_full[stage], par))) break;
         for (int h = 0; h < halves && ok; ++h) {
@@ -536,17 +589,20 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           }
           const bool more = u + 1 < pr.u1;
           const int ks = stage;
+          if (more && !(ok = bar_wait(&bars, &bars.kv_full[ks], par))) break;
           for (int h = 0; h < halves && ok; ++h) {
-            if (!(ok = bar_wait(&bars, &bars.p_full[h], p_par[h]))) break;
+            if (!(ok = bar_wait(&bars, &bars.p_full[h][0], p_par[h]))) break;
+            tc_fence_after();
+            values(h, vs, 0, u > pr.u0);
+            if (!(ok = bar_wait(&bars, &bars.p_full[h][1], p_par[h]))) break;
             p_par[h] ^= 1;
             tc_fence_after();
-            values(h, vs, u > pr.u0);
+            values(h, vs, 1, true);
             if (h == halves - 1) release(&bars.kv_empty[vs]);
             if (!more) {
               release(&bars.o_full[h]);
               continue;
             }
-            if (h == 0 && !(ok = bar_wait(&bars, &bars.kv_full[ks], par))) break;
             scores(h, ks);
             if (u + 2 == pr.u1) release(&bars.q_empty[h]);
           }
@@ -568,35 +624,55 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const int half = wid - kWarpQ;
       uint32_t par = 0;
       bool ok = true;
-      constexpr int kChunks = DP / 8;
       while (ok && pr.next(a)) {
-        const int rows = min(128, pr.t.rows - 128 * half);
+        const int rows = min(half_rows, pr.t.rows - half * half_rows);
         if (rows <= 0) continue;
         if (!(ok = bar_wait(&bars, &bars.q_empty[half], par ^ 1))) break;
         par ^= 1;
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q);
-#pragma unroll 4
-        for (int i = lane; i < 128 * kChunks; i += 32) {
-          const int row = i / kChunks, c = i % kChunks;
-          const bool in = row < rows && c * 8 < a.D;
-          const int R = pr.t.row0 + 128 * half + (row < rows ? row : 0), token = R / a.G, g = R - token * a.G;
-          const uint16_t* src = q + (pr.t.qrow + token) * a.q_row + (int64_t)(pr.head * a.G + g) * a.q_head + c * 8;
-          const uint32_t dst = q_s + half * S::kBlock + (c / 8) * (kKeys * 128) + row * 128 + (((c % 8) ^ (row & 7)) << 4);
-          if (a.q_vec || !in) {
-            const int n = in ? 16 : 0;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(in ? (const void*)src : a.q), "r"(n)
-                         : "memory");
-          } else {
-            uint32_t w[4];
+        const uint32_t to = q_s + half * S::kBlock;
+        const int R0 = pr.t.row0 + half * half_rows;
+        if (q_tma) {
+          if (elected()) {
+            bar_expect(&bars.q_full[half], half_rows * 128 * S::kHalves);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                         : "memory");
+            for (int x = 0; x < S::kHalves; ++x)
+              tma_box(to + x * kKeys * 128, &qmap, 64 * x, 0, pr.head, pr.t.qrow + R0 / a.G, &bars.q_full[half]);
           }
+          __syncwarp();
+        } else {
+          // lane i finds rows i, 32 + i, ...; a step copies kStep rows, kChunks lanes a row
+          constexpr int kChunks = DP / 8, kStep = 32 / kChunks;
+          const int c = lane % kChunks, sub = lane / kChunks;
+          const bool col = c * 8 < a.D;
+          for (int r0 = 0; r0 < rows; r0 += 32) {
+            const int R = R0 + min(r0 + lane, rows - 1), token = R / a.G;
+            const int64_t at = (pr.t.qrow + token) * a.q_row + (int64_t)(pr.head * a.G + (R - token * a.G)) * a.q_head;
+#pragma unroll 4
+            for (int i = 0; i < 32 / kStep; ++i) {
+              const int row = r0 + kStep * i + sub;
+              const uint16_t* src =
+                  reinterpret_cast<const uint16_t*>(a.q) + __shfl_sync(0xffffffffu, at, kStep * i + sub) + c * 8;
+              uint32_t w[4] = {0, 0, 0, 0};
+              if (col) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
+              }
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (c / 8) * (kKeys * 128) + row * 128 +
+                                                                           (((c % 8) ^ (row & 7)) << 4)),
+                           "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                           : "memory");
+            }
+          }
+          fence_async();
+          __syncwarp();
+          if (elected()) bar_arrive(&bars.q_full[half]);
+          __syncwarp();
         }
-        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-        fence_async();
-        bar_arrive(&bars.q_full[half]);
+      }
+      if (!ok && q_tma) {      // as above: the last queries asked for
+        const unsigned long long t0 = now_ns();
+        while (!bar_try(&bars.q_full[half], par ^ 1))
+          if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
       }
       // rows of no request
       if (ok && a.head->dead > 0) {
@@ -622,8 +698,10 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 }
 
 template <int DP, bool kBf16>
-cudaError_t run(const AttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int box_rows, int ctas, cudaStream_t s) {
-  return launch_dependent(k_attend_tc<DP, kBf16>, dim3(ctas), kThreads, TcShape<DP>::kSmem, s, a, k, v, box_rows);
+cudaError_t run(const AttnArgs& a, const TcMaps& m, int ctas, cudaStream_t s) {
+  static const CUtensorMap none{};
+  return launch_dependent(k_attend_tc<DP, kBf16>, dim3(ctas), kThreads, TcShape<DP>::kSmem, s, a, *m.k, *m.v,
+                          m.q ? *m.q : none, m.box_rows, a.tile_rows / 2, m.q ? 1 : 0);
 }
 
 }  // namespace
@@ -640,10 +718,9 @@ cudaError_t configure_attend_tc() {
   return cudaSuccess;
 }
 
-cudaError_t launch_attend_tc(const AttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int box_rows, bool bf16,
-                             int ctas, cudaStream_t s) {
-  if (a.dp == 64) return bf16 ? run<64, true>(a, k, v, box_rows, ctas, s) : run<64, false>(a, k, v, box_rows, ctas, s);
-  return bf16 ? run<128, true>(a, k, v, box_rows, ctas, s) : run<128, false>(a, k, v, box_rows, ctas, s);
+cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cudaStream_t s) {
+  if (a.dp == 64) return bf16 ? run<64, true>(a, m, ctas, s) : run<64, false>(a, m, ctas, s);
+  return bf16 ? run<128, true>(a, m, ctas, s) : run<128, false>(a, m, ctas, s);
 }
 
 }  // namespace lv

@@ -123,8 +123,15 @@ constexpr int kRowsUnit = 16;
 int attend_rows_ctas(int dp, bool wide);
 cudaError_t launch_attend_rows(const AttnArgs& a, bool wide, bool bf16, int ctas, cudaStream_t s);
 constexpr int kTcUnit = 128, kTcRows = 256;
-cudaError_t launch_attend_tc(const AttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int box_rows, bool bf16,
-                             int ctas, cudaStream_t s);
+// packed rows of a tile: two halves of whole tokens
+inline int tc_tile_rows(int G) { return G > 128 ? kTcRows : 2 * (128 / G * G); }
+struct TcMaps {
+  const CUtensorMap* k;    // the layer's, in boxes of 64 columns and box_rows keys
+  const CUtensorMap* v;
+  const CUtensorMap* q;    // boxes of 64 columns, G heads and 128 / G rows; null: plain loads
+  int box_rows;
+};
+cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cudaStream_t s);
 cudaError_t launch_attend_join(const AttnArgs& a, bool bf16, int ctas, cudaStream_t s);
 
 // A launch that may be scheduled while the previous kernel on `s` still runs; the kernel waits
