@@ -8,7 +8,7 @@ namespace {
 
 // Roles of a CTA's twelve warps.
 constexpr int kSoftWarps = 8;             // two warpgroups, one for each half of a tile
-constexpr int kWarpKv = 8, kWarpMma = 9, kWarpQ = 10;   // and 11: queries of tile 0 and 1
+constexpr int kWarpKv = 8, kWarpMma = 9, kWarpQ = 10;   // and 11: zeros
 constexpr int kThreads = 384;
 constexpr int kKeys = kTcUnit;            // keys of a unit
 // registers a thread: 168 at launch (384 * 168 = 64 512), then 208 for the softmax warps and 88
@@ -30,7 +30,7 @@ struct TcShape {
 struct Bars {
   uint64_t kv_full[8], kv_empty[8];
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2];
-  uint64_t drain;
+  uint64_t clean_ask, clean_done, drain;
   uint32_t tmem;
   volatile int bad;
 };
@@ -73,6 +73,10 @@ __device__ __forceinline__ bool bar_wait_slow(Bars* b, uint64_t* bar, uint32_t p
       return false;
     }
   }
+}
+// For one thread.
+__device__ __forceinline__ bool bar_wait1(Bars* b, uint64_t* bar, uint32_t parity) {
+  return bar_try(bar, parity) || bar_wait_slow(b, bar, parity);
 }
 // For a whole warp, whose lanes leave it together with one answer (what follows is .aligned).
 __device__ __forceinline__ bool bar_wait(Bars* b, uint64_t* bar, uint32_t parity) {
@@ -235,10 +239,39 @@ struct Pairs {
   __device__ __forceinline__ int key_of(int u) const {
     return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kKeys;
   }
+  // keys of unit u that no row of the tile sees
+  __device__ __forceinline__ bool hidden(int key, int sinks) const {
+    return key >= t.kv_hi || (key < t.kv_lo && key >= sinks);
+  }
+  __device__ __forceinline__ bool ragged(int u, int sinks) const {
+    const int key0 = key_of(u);
+    return key0 + kKeys > t.kv_hi || (key0 < t.kv_lo && key0 + kKeys > sinks);
+  }
 };
 
 // The n lowest bits, all of them from 32 on, none below 1.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Four 16-byte pieces of each lane's row to pieces of the rows of its group of four lanes: lane q
+// has piece q of row t in w[t] afterwards, so that a store of one piece a lane covers 64
+// consecutive bytes of eight rows.  (With each lane storing its own row, a store touched 32 lines.)
+__device__ __forceinline__ void rows_to_pieces(uint32_t (&w)[16], int lane) {
+#pragma unroll
+  for (int x = 1; x <= 2; x <<= 1) {
+    const bool up = lane & x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i & x) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t &lo = w[4 * i + e], &hi = w[4 * (i + x) + e];
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? lo : hi, x);
+        if (up) lo = got;
+        else hi = got;
+      }
+    }
+  }
+}
 
 // Weights of 64 keys, s[0..64) scaled by c and moved by b, in 16 bits; returns their sum.
 template <bool kBf16>
@@ -265,7 +298,7 @@ __device__ __forceinline__ float weights64(const float* s, float c, float b, uin
 // have outgrown it are they taken again (and in a pair's first unit).
 template <int DP, bool kBf16>
 struct Softmax {
-  float top, sum;      // of the raw scores; of the weights
+  float top = -INFINITY, b = weight_bias<kBf16>(), sum = 0.f;      // of the raw scores; what is added to scaled ones; of the weights
   __device__ __forceinline__ void step(const AttnArgs& a, uint32_t s_at, uint32_t o_at, bool fresh, bool open, int key0,
                                        int pos, uint64_t* first_half) {
     const float c = a.scale;
@@ -285,7 +318,6 @@ struct Softmax {
         for (int j = 0; j < 32; ++j) s[i + j] = m >> j & 1u ? s[i + j] : -INFINITY;
       }
     }
-    float b = weight_bias<kBf16>() - (top == -INFINITY ? 0.f : top * c);
     uint32_t w[32];
     float part = weights64<kBf16>(s, c, b, w);
     float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
@@ -312,7 +344,7 @@ struct Softmax {
           tc_st16(o_at + i, o);
         }
       }
-      b = weight_bias<kBf16>() - (top == -INFINITY ? 0.f : top * c);
+      if (top != -INFINITY) b = weight_bias<kBf16>() - top * c;
       part = weights64<kBf16>(s, c, b, w);
     }
     tc_st32(s_at, w);
@@ -331,7 +363,8 @@ struct Softmax {
 //   warp 8   K and V units into a ring of shared memory, by TMA: a box a page and 64 columns;
 //            what the table has no page for, and rows past a tile's keys, reads as zeros
 //   warp 9   S = Q K^T (tcgen05, operands in shared memory), O += P V (P in TMEM)
-//   10, 11   queries of the two halves, when the previous pair's last S has been issued
+//   warp 10  queries, when the previous pair's last S has been computed
+//   warp 11  zeros in the rows of V units that no row of the tile sees
 //   0 .. 7   softmax, a thread a row, and the pair's end: O / sum, or the sums of a cut pair
 template <int DP, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -360,6 +393,8 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       bar_init(&bars.p_full[i][1], 128);
       bar_init(&bars.o_full[i], 1);
     }
+    bar_init(&bars.clean_ask, 1);
+    bar_init(&bars.clean_done, 32);
     bar_init(&bars.drain, 1);
     bars.bad = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -384,15 +419,21 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     Pairs pr;
     pr.init(a);
     bool ok = true;
-    while (ok && pr.next(a)) {
+    Pairs nx = pr;
+    bool has = nx.next(a);
+    while (ok && has) {
+      pr = nx;
       const int rows = min(half_rows, pr.t.rows - half * half_rows);
-      if (rows <= 0) continue;                              // nothing in this half
+      if (rows <= 0) {                                      // nothing in this half
+        has = nx.next(a);
+        continue;
+      }
       const bool live = rows > (row & ~31);                 // rows in this warp
       const int R0 = pr.t.row0 + half * half_rows;
       const int R = R0 + min(row, rows - 1), token = R / a.G;
       const int pos = pr.t.first + token;
       const int p_lo = pr.t.first + R0 / a.G, p_hi = pr.t.first + (R0 + rows - 1) / a.G;
-      Softmax<DP, kBf16> sm{-INFINITY, 0.f};
+      Softmax<DP, kBf16> sm;
       for (int u = pr.u0; u < pr.u1; ++u) {
         if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par))) break;
         s_par ^= 1;
@@ -408,6 +449,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
         bar_arrive(&bars.p_full[half][1]);
       }
+      has = nx.next(a);
       if (!ok || !(ok = bar_wait(&bars, &bars.o_full[half], o_par))) break;
       o_par ^= 1;
       if (!live) continue;
@@ -420,36 +462,53 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const float inv = !whole ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
       const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0) * a.tile_rows + half * half_rows + row;
       uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + hq * a.o_head;
+      float* part = a.part_o + slot * DP;
+      // the rows of this lane's group of four
+      const uint32_t rows_in = __ballot_sync(0xffffffffu, mine);
+      uint64_t to[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        to[t] = __shfl_sync(0xffffffffu, whole ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part),
+                            (lane & 28) + t);
+      const int piece = lane & 3;
 #pragma unroll
       for (int col = 0; col < DP; col += 32) {
         uint32_t o[32];
         tc_ld32(o, o_at + col);
         tc_wait_ld();
         tc_loaded<32>(o);
-        if (mine && whole) {
+        uint32_t w[16];
+        if (whole) {
 #pragma unroll
-          for (int j = 0; j < 32; j += 8) {
-            if (col + j >= a.D) continue;
-            uint32_t w[4];
+          for (int e = 0; e < 16; ++e)
+            w[e] = pack16<kBf16>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+          if (a.o_vec) {
+            rows_to_pieces(w, lane);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = pack16<kBf16>(__uint_as_float(o[j + 2 * e]) * inv, __uint_as_float(o[j + 2 * e + 1]) * inv);
-            if (a.o_vec) {
-              *reinterpret_cast<uint4*>(out + col + j) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
+            for (int t = 0; t < 4; ++t)
+              if ((rows_in >> ((lane & 28) + t) & 1) && col + 8 * piece < a.D)
+                *reinterpret_cast<uint4*>(to[t] + 2 * (col + 8 * piece)) =
+                    make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
+          } else if (mine) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                out[col + j + 2 * e] = (uint16_t)w[e];
-                out[col + j + 2 * e + 1] = (uint16_t)(w[e] >> 16);
+            for (int e = 0; e < 16; ++e)
+              if (col + 2 * e < a.D) {
+                out[col + 2 * e] = (uint16_t)w[e];
+                out[col + 2 * e + 1] = (uint16_t)(w[e] >> 16);
               }
-            }
           }
-        } else if (mine) {
-          float4* po = reinterpret_cast<float4*>(a.part_o + slot * DP + col);
+        } else {
 #pragma unroll
-          for (int j = 0; j < 32; j += 4)
-            po[j / 4] = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]),
-                                    __uint_as_float(o[j + 3]));
+          for (int g = 0; g < 32; g += 16) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = o[g + e];
+            rows_to_pieces(w, lane);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (rows_in >> ((lane & 28) + t) & 1)
+                *reinterpret_cast<uint4*>(to[t] + 4 * (col + g + 4 * piece)) =
+                    make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
+          }
         }
         __syncwarp();
       }
@@ -515,169 +574,182 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
       }
     } else if (wid == kWarpMma) {
-      // ---- products
-      constexpr uint32_t kDescS = mma_desc<kBf16>(128, kKeys, false), kDescO = mma_desc<kBf16>(128, DP, true);
-      uint32_t par = 0, p_par[2] = {0, 0}, q_par[2] = {0, 0};
-      int stage = 0;
-      bool ok = true;
-      auto step = [&]() {
-        if (++stage == S::kStages) {
-          stage = 0;
-          par ^= 1;
-        }
-      };
-      auto scores = [&](int half, int st) {      // S_half = Q_half K^T
-        const uint64_t qd = smem_desc(q_s + half * S::kBlock, 16, 1024), kd = smem_desc(ring_s + st * S::kBlock, 16, 1024);
-        if (elected()) {
+      // ---- products, by one thread (a warp that votes at each wait took some 200 cycles for it)
+      if (elected()) {
+        constexpr uint32_t kDescS = mma_desc<kBf16>(128, kKeys, false), kDescO = mma_desc<kBf16>(128, DP, true);
+        const uint64_t kd0 = smem_desc(ring_s, 16, 1024), vd0 = smem_desc(ring_s, kKeys * 128, 1024);
+        const uint64_t qd0 = smem_desc(q_s, 16, 1024);
+        uint32_t par = 0, p_par = 0, q_par = 0, clean_par = 0;      // (the last three: a bit a half)
+        int stage = 0;
+        auto step = [&]() {
+          if (++stage == S::kStages) {
+            stage = 0;
+            par ^= 1;
+          }
+        };
+        auto scores = [&](int half, int st) {      // S_half = Q_half K^T
+          const uint64_t qd = qd0 + (uint32_t)(half * (S::kBlock >> 4)), kd = kd0 + (uint32_t)(st * (S::kBlock >> 4));
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
             const uint32_t at = ((k / 4) * (kKeys * 128) + (k % 4) * 32) >> 4;
             tc_mma_ss(tmem + 128 * half, qd + at, kd + at, kDescS, k > 0);
           }
           tc_commit(&bars.s_full[half]);
-        }
-        __syncwarp();
-      };
-      auto values = [&](int half, int st, int part, bool add) {      // O_half (+)= P_half V, 64 keys of it
-        const uint64_t vd = smem_desc(ring_s + st * S::kBlock, kKeys * 128, 1024);
-        if (elected()) {
+        };
+        auto values = [&](int half, int st, int part, bool add) {      // O_half (+)= P_half V, 64 keys of it
+          const uint64_t vd = vd0 + (uint32_t)(st * (S::kBlock >> 4));
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             tc_mma_ts(tmem + S::kColO + DP * half, tmem + 128 * half + 32 * part + 8 * k,
                       vd + (4 * part + k) * (2048 >> 4), kDescO, add || k > 0);
-        }
-        __syncwarp();
-      };
-      auto release = [&](uint64_t* bar) {
-        if (elected()) tc_commit(bar);
-        __syncwarp();
-      };
-      while (ok && pr.next(a)) {
-        const int halves = pr.t.rows > half_rows ? 2 : 1;
-        // the first unit's scores
-        if (!(ok = bar_wait(&bars, &bars.kv_full[stage], par))) break;
-        for (int h = 0; h < halves && ok; ++h) {
-          if (!(ok = bar_wait(&bars, &bars.q_full[h], q_par[h]))) break;
-          q_par[h] ^= 1;
-          tc_fence_after();
-          scores(h, stage);
-          if (pr.u1 - pr.u0 == 1) release(&bars.q_empty[h]);
-        }
-        if (!ok) break;
-        release(&bars.kv_empty[stage]);
-        step();
-        for (int u = pr.u0; ok && u < pr.u1; ++u) {
-          const int vs = stage;
-          if (!(ok = bar_wait(&bars, &bars.kv_full[vs], par))) break;
+        };
+        // a pair's units; false when a wait ran out.  nx: the pair after it, found meanwhile
+        Pairs nx = pr;
+        bool has = nx.next(a);
+        auto pair = [&]() -> bool {
+          pr = nx;
+          const int halves = pr.t.rows > half_rows ? 2 : 1;
+          if (!bar_wait1(&bars, &bars.kv_full[stage], par)) return false;
+          for (int h = 0; h < halves; ++h) {      // the first unit's scores
+            if (!bar_wait1(&bars, &bars.q_full[h], q_par >> h & 1)) return false;
+            q_par ^= 1u << h;
+            tc_fence_after();
+            scores(h, stage);
+            if (pr.u1 - pr.u0 == 1) tc_commit(&bars.q_empty[h]);
+          }
+          tc_commit(&bars.kv_empty[stage]);
           step();
-          // rows of V that no row of the tile sees hold whatever the page does: zeros, since a
-          // weight of zero does not cancel a NaN
-          const int key0 = pr.key_of(u);
-          if (key0 + kKeys > pr.t.kv_hi || (key0 < pr.t.kv_lo && key0 + kKeys > a.sinks)) {
-            for (int i = lane; i < kKeys * 8; i += 32) {
-              const int key = key0 + i / 8;
-              if (key < pr.t.kv_hi && (key >= pr.t.kv_lo || key < a.sinks)) continue;
+          has = nx.next(a);
+          for (int u = pr.u0; u < pr.u1; ++u) {
+            const int vs = stage;
+            if (!bar_wait1(&bars, &bars.kv_full[vs], par)) return false;
+            step();
+            const bool ragged = pr.ragged(u, a.sinks), more = u + 1 < pr.u1;
+            if (ragged) bar_arrive(&bars.clean_ask);
+            const int ks = stage;
+            if (more && !bar_wait1(&bars, &bars.kv_full[ks], par)) return false;
+            for (int h = 0; h < halves; ++h) {
+              if (!bar_wait1(&bars, &bars.p_full[h][0], p_par >> h & 1)) return false;
+              if (ragged && h == 0) {
+                if (!bar_wait1(&bars, &bars.clean_done, clean_par)) return false;
+                clean_par ^= 1;
+              }
+              tc_fence_after();
+              values(h, vs, 0, u > pr.u0);
+              if (!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1)) return false;
+              p_par ^= 1u << h;
+              tc_fence_after();
+              values(h, vs, 1, true);
+              if (!more) tc_commit(&bars.o_full[h]);
+              else scores(h, ks);
+              if (h == halves - 1) tc_commit(&bars.kv_empty[vs]);
+              if (u + 2 == pr.u1) tc_commit(&bars.q_empty[h]);
+            }
+            if (more) {
+              tc_commit(&bars.kv_empty[ks]);
+              step();
+            }
+          }
+          return true;
+        };
+        bool ok = true;
+        while (ok && has) ok = pair();
+        if (!ok) {      // let the products under way end
+          tc_commit(&bars.drain);
+          const unsigned long long t0 = now_ns();
+          while (!bar_try(&bars.drain, 0))
+            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+          report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
+        }
+      }
+      __syncwarp();
+    } else if (wid == kWarpQ) {
+      // ---- queries
+      uint32_t par = 0;      // a bit a half
+      bool ok = true;
+      while (ok && pr.next(a)) {
+        for (int half = 0; half < 2; ++half) {
+          const int rows = min(half_rows, pr.t.rows - half * half_rows);
+          if (rows <= 0) break;
+          if (!(ok = bar_wait(&bars, &bars.q_empty[half], ~par >> half & 1))) break;
+          par ^= 1u << half;
+          const uint32_t to = q_s + half * S::kBlock;
+          const int R0 = pr.t.row0 + half * half_rows;
+          if (q_tma) {
+            if (elected()) {
+              bar_expect(&bars.q_full[half], half_rows * 128 * S::kHalves);
 #pragma unroll
               for (int x = 0; x < S::kHalves; ++x)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring_s + vs * S::kBlock + x * kKeys * 128 +
-                                                                             (i / 8) * 128 + (i % 8) * 16),
-                             "r"(0)
+                tma_box(to + x * kKeys * 128, &qmap, 64 * x, 0, pr.head, pr.t.qrow + R0 / a.G, &bars.q_full[half]);
+            }
+            __syncwarp();
+          } else {
+            // lane i finds rows i, 32 + i, ...; a step copies kStep rows, kChunks lanes a row
+            constexpr int kChunks = DP / 8, kStep = 32 / kChunks;
+            const int c = lane % kChunks, sub = lane / kChunks;
+            const bool col = c * 8 < a.D;
+            for (int r0 = 0; r0 < rows; r0 += 32) {
+              const int R = R0 + min(r0 + lane, rows - 1), token = R / a.G;
+              const int64_t at =
+                  (pr.t.qrow + token) * a.q_row + (int64_t)(pr.head * a.G + (R - token * a.G)) * a.q_head;
+#pragma unroll 4
+              for (int i = 0; i < 32 / kStep; ++i) {
+                const int row = r0 + kStep * i + sub;
+                const uint16_t* src =
+                    reinterpret_cast<const uint16_t*>(a.q) + __shfl_sync(0xffffffffu, at, kStep * i + sub) + c * 8;
+                uint32_t w[4] = {0, 0, 0, 0};
+                if (col) {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
+                }
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (c / 8) * (kKeys * 128) + row * 128 +
+                                                                             (((c % 8) ^ (row & 7)) << 4)),
+                             "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
                              : "memory");
+              }
             }
             fence_async();
             __syncwarp();
+            if (elected()) bar_arrive(&bars.q_full[half]);
+            __syncwarp();
           }
-          const bool more = u + 1 < pr.u1;
-          const int ks = stage;
-          if (more && !(ok = bar_wait(&bars, &bars.kv_full[ks], par))) break;
-          for (int h = 0; h < halves && ok; ++h) {
-            if (!(ok = bar_wait(&bars, &bars.p_full[h][0], p_par[h]))) break;
-            tc_fence_after();
-            values(h, vs, 0, u > pr.u0);
-            if (!(ok = bar_wait(&bars, &bars.p_full[h][1], p_par[h]))) break;
-            p_par[h] ^= 1;
-            tc_fence_after();
-            values(h, vs, 1, true);
-            if (h == halves - 1) release(&bars.kv_empty[vs]);
-            if (!more) {
-              release(&bars.o_full[h]);
-              continue;
-            }
-            scores(h, ks);
-            if (u + 2 == pr.u1) release(&bars.q_empty[h]);
-          }
-          if (ok && more) {
-            release(&bars.kv_empty[ks]);
-            step();
-          }
-        }
-      }
-      if (!ok) {      // let the products under way end
-        release(&bars.drain);
-        const unsigned long long t0 = now_ns();
-        while (!bar_try(&bars.drain, 0))
-          if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
-        if (lane == 0) report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
-      }
-    } else {
-      // ---- queries of one half
-      const int half = wid - kWarpQ;
-      uint32_t par = 0;
-      bool ok = true;
-      while (ok && pr.next(a)) {
-        const int rows = min(half_rows, pr.t.rows - half * half_rows);
-        if (rows <= 0) continue;
-        if (!(ok = bar_wait(&bars, &bars.q_empty[half], par ^ 1))) break;
-        par ^= 1;
-        const uint32_t to = q_s + half * S::kBlock;
-        const int R0 = pr.t.row0 + half * half_rows;
-        if (q_tma) {
-          if (elected()) {
-            bar_expect(&bars.q_full[half], half_rows * 128 * S::kHalves);
-#pragma unroll
-            for (int x = 0; x < S::kHalves; ++x)
-              tma_box(to + x * kKeys * 128, &qmap, 64 * x, 0, pr.head, pr.t.qrow + R0 / a.G, &bars.q_full[half]);
-          }
-          __syncwarp();
-        } else {
-          // lane i finds rows i, 32 + i, ...; a step copies kStep rows, kChunks lanes a row
-          constexpr int kChunks = DP / 8, kStep = 32 / kChunks;
-          const int c = lane % kChunks, sub = lane / kChunks;
-          const bool col = c * 8 < a.D;
-          for (int r0 = 0; r0 < rows; r0 += 32) {
-            const int R = R0 + min(r0 + lane, rows - 1), token = R / a.G;
-            const int64_t at = (pr.t.qrow + token) * a.q_row + (int64_t)(pr.head * a.G + (R - token * a.G)) * a.q_head;
-#pragma unroll 4
-            for (int i = 0; i < 32 / kStep; ++i) {
-              const int row = r0 + kStep * i + sub;
-              const uint16_t* src =
-                  reinterpret_cast<const uint16_t*>(a.q) + __shfl_sync(0xffffffffu, at, kStep * i + sub) + c * 8;
-              uint32_t w[4] = {0, 0, 0, 0};
-              if (col) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
-              }
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (c / 8) * (kKeys * 128) + row * 128 +
-                                                                           (((c % 8) ^ (row & 7)) << 4)),
-                           "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                           : "memory");
-            }
-          }
-          fence_async();
-          __syncwarp();
-          if (elected()) bar_arrive(&bars.q_full[half]);
-          __syncwarp();
         }
       }
       if (!ok && q_tma) {      // as above: the last queries asked for
-        const unsigned long long t0 = now_ns();
-        while (!bar_try(&bars.q_full[half], par ^ 1))
-          if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+        for (int half = 0; half < 2; ++half) {
+          const unsigned long long t0 = now_ns();
+          while (!bar_try(&bars.q_full[half], ~par >> half & 1))
+            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+        }
+      }
+    } else {
+      // ---- rows of V that no row of a tile sees hold whatever the page does: zeros, since a
+      // weight of zero does not cancel a NaN.  The products ask for each such unit, in order
+      long long units = 0;
+      uint32_t par = 0;
+      bool ok = true;
+      while (ok && pr.next(a)) {
+        for (int u = pr.u0; u < pr.u1; ++u, ++units) {
+          if (!pr.ragged(u, a.sinks)) continue;
+          if (!(ok = bar_wait(&bars, &bars.clean_ask, par))) break;
+          par ^= 1;
+          const uint32_t v = ring_s + (uint32_t)((2 * units + 1) % S::kStages) * S::kBlock;
+          const int key0 = pr.key_of(u);
+          for (int i = lane; i < kKeys * 8; i += 32) {
+            if (!pr.hidden(key0 + i / 8, a.sinks)) continue;
+#pragma unroll
+            for (int x = 0; x < S::kHalves; ++x)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + x * kKeys * 128 + i * 16), "r"(0)
+                           : "memory");
+          }
+          fence_async();
+          bar_arrive(&bars.clean_done);
+        }
       }
       // rows of no request
       if (ok && a.head->dead > 0) {
         const int Hq = a.H * a.G;
-        for (int r = blockIdx.x * 2 + half; r < a.num_tokens; r += gridDim.x * 2) {
+        for (int r = blockIdx.x; r < a.num_tokens; r += gridDim.x) {
           if (a.positions[r] >= 0) continue;
           for (int h = 0; h < Hq; ++h) {
             uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head;
