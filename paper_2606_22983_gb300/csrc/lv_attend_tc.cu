@@ -1,5 +1,7 @@
 // Attention of requests with many rows (chunks of user input, prompts, and single tokens beside
 // them) over the paged context, on the fifth-generation tensor cores.
+#include <type_traits>
+
 #include "lv_batch.cuh"
 
 namespace lv {
@@ -8,13 +10,16 @@ namespace {
 
 // Roles of a CTA's twelve warps.
 constexpr int kSoftWarps = 8;             // two warpgroups, one for each half of a tile
-constexpr int kWarpKv = 8, kWarpMma = 9, kWarpQ = 10;   // and 11: zeros
+constexpr int kWarpK = 8, kWarpV = 9, kWarpMma = 10;    // and 11: queries and zeros
 constexpr int kThreads = 384;
 constexpr int kKeys = kTcUnit;            // keys of a unit
 // registers a thread: 168 at launch (384 * 168 = 64 512), then 208 for the softmax warps and 88
 // for the others (256 * 208 + 128 * 88 = 64 512)
 constexpr int kRegsSoft = 208, kRegsOther = 88;
 constexpr long long kWaitLimitNs = 1000000000ll;   // one second a wait
+// A warp that runs alone pays some 110 cycles for a taken branch: what is rare is laid out of line.
+#define LV_RARE(x) __builtin_expect(!!(x), 0)
+#define LV_MOSTLY(x) __builtin_expect(!!(x), 1)
 
 template <int DP>
 struct TcShape {
@@ -76,12 +81,13 @@ __device__ __forceinline__ bool bar_wait_slow(Bars* b, uint64_t* bar, uint32_t p
 }
 // For one thread.
 __device__ __forceinline__ bool bar_wait1(Bars* b, uint64_t* bar, uint32_t parity) {
-  return bar_try(bar, parity) || bar_wait_slow(b, bar, parity);
+  if (LV_MOSTLY(bar_try(bar, parity))) return true;
+  return bar_wait_slow(b, bar, parity);
 }
 // For a whole warp, whose lanes leave it together with one answer (what follows is .aligned).
 __device__ __forceinline__ bool bar_wait(Bars* b, uint64_t* bar, uint32_t parity) {
   bool ok = bar_try(bar, parity);
-  if (!ok) ok = bar_wait_slow(b, bar, parity);
+  if (LV_RARE(!ok)) ok = bar_wait_slow(b, bar, parity);
   return __all_sync(0xffffffffu, ok);
 }
 
@@ -360,11 +366,10 @@ struct Softmax {
 // One CTA an SM: its share of the line of units.  A tile is two halves of half_rows packed rows
 // (whole tokens; an M = 128 tile of the tensor core each) that take turns: while one half's weights are
 // computed, the tensor core runs the other half's products.
-//   warp 8   K and V units into a ring of shared memory, by TMA: a box a page and 64 columns;
-//            what the table has no page for, and rows past a tile's keys, reads as zeros
-//   warp 9   S = Q K^T (tcgen05, operands in shared memory), O += P V (P in TMEM)
-//   warp 10  queries, when the previous pair's last S has been computed
-//   warp 11  zeros in the rows of V units that no row of the tile sees
+//   8, 9     K and V units into a ring of shared memory, by TMA: a box a page and 64 columns;
+//            what the table has no page for reads as zeros
+//   warp 10  S = Q K^T (tcgen05, operands in shared memory), O += P V (P in TMEM)
+//   warp 11  queries, and zeros in the rows of V units that no row of the tile sees
 //   0 .. 7   softmax, a thread a row, and the pair's end: O / sum, or the sums of a cut pair
 template <int DP, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -526,50 +531,57 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     Pairs pr;
     pr.init(a);
-    if (wid == kWarpKv) {
-      // ---- K and V
-      // a lane a box: 64 columns of box_rows keys (at least 8, so that 32 lanes do)
-      int stage = 0;
-      uint32_t par = 0;               // of the ring's current round
-      long long loads = 0;
+    if (wid == kWarpK || wid == kWarpV) {
+      // ---- K (or V): lane i finds the page of a unit's box of box_rows keys; one thread then
+      // issues the copies.  (With each lane issuing its own, a unit's 16 took 1300 cycles.)
+      const int kv = wid == kWarpV;
+      const CUtensorMap* map = kv ? &vmap : &kmap;
+      const int boxes = kKeys / box_rows;
+      long long unit = 0;
       bool ok = true;
-      const int box = lane / S::kHalves, x = lane % S::kHalves;
-      const bool mine = box < kKeys / box_rows;
-      const uint32_t at = x * kKeys * 128 + box * box_rows * 128;
       auto page_of = [&](int u) {
-        const int key = pr.key_of(u) + box * box_rows;
-        if (!mine || u >= pr.u1 || key >= pr.t.kv_hi || (key + box_rows <= pr.t.kv_lo && key >= a.sinks)) return -1;
+        const int key = pr.key_of(u) + lane * box_rows;
+        if (lane >= boxes || u >= pr.u1 || key >= pr.t.kv_hi || (key + box_rows <= pr.t.kv_lo && key >= a.sinks)) return -1;
         return a.tables[(size_t)pr.t.req * a.maxB + key / a.T];
       };
       while (ok && pr.next(a)) {
         int next = page_of(pr.u0);
-        for (int u = pr.u0; ok && u < pr.u1; ++u) {
+        for (int u = pr.u0; ok && u < pr.u1; ++u, ++unit) {
           // no page: a box outside the array, which reads as zeros
           const int page = (uint32_t)next < a.hbm_pages ? next : (int)a.hbm_pages;
+          const int off = (pr.key_of(u) + lane * box_rows) % a.T;
           next = page_of(u + 1);
-          const int off = (pr.key_of(u) + box * box_rows) % a.T;
+          const int n = (int)((2 * unit + kv) % S::kStages);
+          const uint32_t round = (uint32_t)((2 * unit + kv) / S::kStages);
+          if (!(ok = bar_wait(&bars, &bars.kv_empty[n], ~round & 1u))) break;
+          uint64_t* full = &bars.kv_full[n];
+          const uint32_t dst = ring_s + n * S::kBlock;
+          if (elected()) bar_expect(full, S::kBlock);
+#pragma unroll 1
+          for (int i = 0; i < boxes; i += 4) {
+            int pages[4], offs[4];
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            if (!(ok = bar_wait(&bars, &bars.kv_empty[stage], par ^ 1))) break;
-            if (elected()) bar_expect(&bars.kv_full[stage], S::kBlock);
-            __syncwarp();
-            if (mine)
-              tma_box(ring_s + stage * S::kBlock + at, kv ? &vmap : &kmap, 64 * x, pr.head, off, page,
-                      &bars.kv_full[stage]);
-            __syncwarp();
-            ++loads;
-            if (++stage == S::kStages) {
-              stage = 0;
-              par ^= 1;
+            for (int e = 0; e < 4; ++e) {
+              pages[e] = __shfl_sync(0xffffffffu, page, (i + e) & 31);
+              offs[e] = __shfl_sync(0xffffffffu, off, (i + e) & 31);
             }
+            if (elected()) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (i + e >= boxes) break;
+#pragma unroll
+                for (int x = 0; x < S::kHalves; ++x)
+                  tma_box(dst + x * kKeys * 128 + (i + e) * box_rows * 128, map, 64 * x, pr.head, offs[e], pages[e], full);
+              }
+            }
+            __syncwarp();
           }
         }
       }
       if (!ok) {      // let what is on its way land before the shared memory is given up
-        const long long n = loads < S::kStages ? loads : S::kStages;
-        for (long long i = loads - n; i < loads; ++i) {
+        for (long long i = unit < S::kStages ? 0 : unit - S::kStages; i < unit; ++i) {
           const unsigned long long t0 = now_ns();
-          while (!bar_try(&bars.kv_full[i % S::kStages], (uint32_t)(i / S::kStages) & 1u))
+          while (!bar_try(&bars.kv_full[(2 * i + kv) % S::kStages], (uint32_t)((2 * i + kv) / S::kStages) & 1u))
             if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
         }
       }
@@ -606,11 +618,12 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         // a pair's units; false when a wait ran out.  nx: the pair after it, found meanwhile
         Pairs nx = pr;
         bool has = nx.next(a);
-        auto pair = [&]() -> bool {
+        auto pair = [&](auto halves_of) -> bool {
+          constexpr int kHalves = decltype(halves_of)::value;
           pr = nx;
-          const int halves = pr.t.rows > half_rows ? 2 : 1;
           if (!bar_wait1(&bars, &bars.kv_full[stage], par)) return false;
-          for (int h = 0; h < halves; ++h) {      // the first unit's scores
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) {      // the first unit's scores
             if (!bar_wait1(&bars, &bars.q_full[h], q_par >> h & 1)) return false;
             q_par ^= 1u << h;
             tc_fence_after();
@@ -620,32 +633,39 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           tc_commit(&bars.kv_empty[stage]);
           step();
           has = nx.next(a);
+#pragma unroll 1
           for (int u = pr.u0; u < pr.u1; ++u) {
             const int vs = stage;
-            if (!bar_wait1(&bars, &bars.kv_full[vs], par)) return false;
-            step();
             const bool ragged = pr.ragged(u, a.sinks), more = u + 1 < pr.u1;
-            if (ragged) bar_arrive(&bars.clean_ask);
+            if (LV_RARE(!bar_wait1(&bars, &bars.kv_full[vs], par))) return false;
+            step();
+            if (LV_RARE(ragged)) bar_arrive(&bars.clean_ask);
             const int ks = stage;
-            if (more && !bar_wait1(&bars, &bars.kv_full[ks], par)) return false;
-            for (int h = 0; h < halves; ++h) {
-              if (!bar_wait1(&bars, &bars.p_full[h][0], p_par >> h & 1)) return false;
-              if (ragged && h == 0) {
+            if (LV_MOSTLY(more)) {
+              if (LV_RARE(!bar_wait1(&bars, &bars.kv_full[ks], par))) return false;
+            }
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][0], p_par >> h & 1))) return false;
+              if (h == 0 && LV_RARE(ragged)) {
                 if (!bar_wait1(&bars, &bars.clean_done, clean_par)) return false;
                 clean_par ^= 1;
               }
               tc_fence_after();
               values(h, vs, 0, u > pr.u0);
-              if (!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1)) return false;
-              p_par ^= 1u << h;
+              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1))) return false;
               tc_fence_after();
               values(h, vs, 1, true);
-              if (!more) tc_commit(&bars.o_full[h]);
-              else scores(h, ks);
-              if (h == halves - 1) tc_commit(&bars.kv_empty[vs]);
-              if (u + 2 == pr.u1) tc_commit(&bars.q_empty[h]);
+              if (LV_MOSTLY(more)) {
+                scores(h, ks);
+                if (LV_RARE(u + 2 == pr.u1)) tc_commit(&bars.q_empty[h]);
+              } else {
+                tc_commit(&bars.o_full[h]);
+              }
             }
-            if (more) {
+            p_par ^= kHalves == 2 ? 3u : 1u;
+            tc_commit(&bars.kv_empty[vs]);
+            if (LV_MOSTLY(more)) {
               tc_commit(&bars.kv_empty[ks]);
               step();
             }
@@ -653,7 +673,8 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           return true;
         };
         bool ok = true;
-        while (ok && has) ok = pair();
+        while (ok && has)
+          ok = nx.t.rows > half_rows ? pair(std::integral_constant<int, 2>()) : pair(std::integral_constant<int, 1>());
         if (!ok) {      // let the products under way end
           tc_commit(&bars.drain);
           const unsigned long long t0 = now_ns();
@@ -663,9 +684,13 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
       }
       __syncwarp();
-    } else if (wid == kWarpQ) {
-      // ---- queries
+    } else {
+      // ---- queries of each pair, when the S of the pair before it has been computed; and zeros
+      // in the rows of V that no row of the tile sees, which hold whatever the page does (a weight
+      // of zero does not cancel a NaN): the products ask for each such unit, in order
       uint32_t par = 0;      // a bit a half
+      uint32_t z_par = 0;
+      long long units = 0;
       bool ok = true;
       while (ok && pr.next(a)) {
         for (int half = 0; half < 2; ++half) {
@@ -714,25 +739,10 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             __syncwarp();
           }
         }
-      }
-      if (!ok && q_tma) {      // as above: the last queries asked for
-        for (int half = 0; half < 2; ++half) {
-          const unsigned long long t0 = now_ns();
-          while (!bar_try(&bars.q_full[half], ~par >> half & 1))
-            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
-        }
-      }
-    } else {
-      // ---- rows of V that no row of a tile sees hold whatever the page does: zeros, since a
-      // weight of zero does not cancel a NaN.  The products ask for each such unit, in order
-      long long units = 0;
-      uint32_t par = 0;
-      bool ok = true;
-      while (ok && pr.next(a)) {
-        for (int u = pr.u0; u < pr.u1; ++u, ++units) {
+        for (int u = pr.u0; ok && u < pr.u1; ++u, ++units) {
           if (!pr.ragged(u, a.sinks)) continue;
-          if (!(ok = bar_wait(&bars, &bars.clean_ask, par))) break;
-          par ^= 1;
+          if (!(ok = bar_wait(&bars, &bars.clean_ask, z_par))) break;
+          z_par ^= 1;
           const uint32_t v = ring_s + (uint32_t)((2 * units + 1) % S::kStages) * S::kBlock;
           const int key0 = pr.key_of(u);
           for (int i = lane; i < kKeys * 8; i += 32) {
@@ -744,6 +754,13 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           }
           fence_async();
           bar_arrive(&bars.clean_done);
+        }
+      }
+      if (!ok && q_tma) {      // as above: the last queries asked for
+        for (int half = 0; half < 2; ++half) {
+          const unsigned long long t0 = now_ns();
+          while (!bar_try(&bars.q_full[half], ~par >> half & 1))
+            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
         }
       }
       // rows of no request
