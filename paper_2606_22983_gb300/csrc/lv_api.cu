@@ -1872,12 +1872,14 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
       a.groups = pool->kv_heads;
       a.tile_rows = lv::tc_tile_rows(b->G);
       a.unit = lv::kTcUnit;
+      a.lead = lv::kTcLead;
       a.min_share = 4;
       b->ctas = pool->num_sms;
     } else {
       a.groups = pool->kv_heads / b->hg;
       a.tile_rows = b->kind == lv::ATTN_ROWS32 ? 32 : 16;
       a.unit = lv::kRowsUnit;
+      a.lead = lv::kRowsLead;
       a.min_share = 4;
       b->ctas = rows_ctas(b, b->kind == lv::ATTN_ROWS32);
     }
@@ -1972,6 +1974,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.groups = tc ? pool->kv_heads : pool->kv_heads / b->hg;
   a.hg = tc ? 1 : b->hg;
   a.tile_rows = tc ? lv::tc_tile_rows(b->G) : b->kind == lv::ATTN_ROWS32 ? 32 : 16;
+  a.lead = tc ? lv::kTcLead : lv::kRowsLead;
   a.dp = b->dp;
   a.scale = scale * 1.44269504088896341f;
   a.part_o = b->part_o;

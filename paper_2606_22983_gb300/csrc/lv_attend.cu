@@ -117,29 +117,33 @@ __global__ void __launch_bounds__(kThreads) k_attend_rows(const __grid_constant_
     if (whole && x.u < x.u_end)
       x.page = a.tables[(size_t)x.t.req * a.maxB + (uint32_t)key_of(x.t, x.u) / (uint32_t)a.T];
   };
-  auto enter = [&](Walk& x) {      // the pair that unit x.w is in
+  auto enter = [&](Walk& x) -> bool {      // the pair that x.w is in; false where no unit of it is the CTA's
+    const int len = x.t.units + a.lead;
     const long long off = x.w - x.t.before;
-    x.group = (int)(off / x.t.units);
-    x.u_begin = (int)(off - (long long)x.group * x.t.units);
-    x.u_end = (int)min((long long)x.t.units, x.u_begin + (x.end - x.w));
+    x.group = (int)(off / len);
+    const int o0 = (int)(off - (long long)x.group * len), o1 = (int)min((long long)len, o0 + (x.end - x.w));
+    x.w += o1 - o0;
+    x.u_begin = max(o0 - a.lead, 0);
+    x.u_end = o1 - a.lead;
     x.u = x.u_begin + ki;
-    x.w += x.u_end - x.u_begin;
     find_page(x);
+    return x.u_end > x.u_begin;
   };
   auto next_pair = [&](Walk& x) -> bool {
-    if (x.w >= x.end) return false;
-    if (x.w >= x.t.before + (long long)x.t.units * a.groups) x.t = load_tile(&a.tiles[++x.tile]);
-    enter(x);
-    return true;
+    while (x.w < x.end) {
+      if (x.w >= x.t.before + (long long)(x.t.units + a.lead) * a.groups) x.t = load_tile(&a.tiles[++x.tile]);
+      if (enter(x)) return true;
+    }
+    return false;
   };
   Walk L;
   L.w = blockIdx.x * share;
   L.end = min(units, L.w + share);
-  const bool any = L.w < L.end;
+  bool any = L.w < L.end;
   if (any) {
     L.tile = a.cta_tile[blockIdx.x];
     L.t = load_tile(&a.tiles[L.tile]);
-    enter(L);
+    any = enter(L) || next_pair(L);
   }
   Walk C = L;
   bool more = any;
@@ -441,9 +445,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
   const long long c = blockIdx.x, edge = (c + 1) * share;
   if (edge >= units) return;
   const AttnTile t = load_tile(&a.tiles[a.cta_tile[c + 1]]);
-  const int group = (int)((edge - t.before) / t.units);
-  const long long start = t.before + (long long)group * t.units;
-  if (start == edge || start < c * share) return;
+  const int group = (int)((edge - t.before) / (t.units + a.lead));
+  const long long start = t.before + (long long)group * (t.units + a.lead) + a.lead;      // of its first unit
+  if (start >= edge || start < c * share) return;
   const int pieces = (int)((start + t.units - 1) / share - c) + 1;
   const int lane = threadIdx.x & 31;
   const int rows = t.rows * a.hg;

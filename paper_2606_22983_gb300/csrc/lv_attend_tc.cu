@@ -48,6 +48,11 @@ __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
 }
+// Once for a warp, after what its lanes did before.
+__device__ __forceinline__ void warp_arrive(uint64_t* b) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) bar_arrive(b);
+}
 __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
 }
@@ -92,6 +97,12 @@ __device__ __forceinline__ bool bar_wait(Bars* b, uint64_t* bar, uint32_t parity
 }
 
 // ---- tcgen05
+// Shared-memory matrix descriptors, 128-byte swizzle (rows of 128 bytes, the pattern repeating
+// every 8 rows = 1024 bytes).  K-major (Q, K): stride between 8-row groups 1024 bytes.
+// MN-major (V: rows are keys, columns are O's): 64 columns a block, blocks kKeys * 128 bytes
+// apart (leading offset), groups of 8 keys 1024 bytes apart (stride offset).
+constexpr uint32_t kDescHigh = 1024u >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_low(uint32_t at, uint32_t lead) { return (at & 0x3ffffu) >> 4 | (lead >> 4) << 16; }
 // One lane of the warp, always the same.  (With a test of the lane number in its place the
 // compiler cannot tell that one thread issues, and a product took 109 cycles to issue, not 64.)
 __device__ __forceinline__ bool elected() {
@@ -111,22 +122,27 @@ __device__ __forceinline__ void tc_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                : "memory");
 }
+// Matrix descriptors by their low words (address and leading offset); the high one is the same
+// for all operands here.
 // D[tmem] (+)= A[smem] B[smem]
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %5};\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
       "setp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(desc), "r"((uint32_t)add), "n"(kDescHigh)
       : "memory");
 }
 // D[tmem] (+)= A[tmem] B[smem]
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
       "setp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(desc), "r"((uint32_t)add), "n"(kDescHigh)
       : "memory");
 }
 #define LV_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), \
@@ -140,12 +156,6 @@ __device__ __forceinline__ void tc_ld32(uint32_t* x, uint32_t at) {
       "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
       "%30,%31}, [%32];"
       : LV_R8(x, 0), LV_R8(x, 8), LV_R8(x, 16), LV_R8(x, 24)
-      : "r"(at));
-}
-__device__ __forceinline__ void tc_ld16(uint32_t* x, uint32_t at) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : LV_R8(x, 0), LV_R8(x, 8)
       : "r"(at));
 }
 __device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* x) {
@@ -174,14 +184,6 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Shared-memory matrix descriptors, 128-byte swizzle (rows of 128 bytes, the pattern repeating
-// every 8 rows = 1024 bytes).  K-major (Q, K): stride between 8-row groups 1024 bytes.
-// MN-major (V: rows are keys, columns are O's): 64 columns a block, blocks kKeys * 128 bytes
-// apart (leading offset), groups of 8 keys 1024 bytes apart (stride offset).
-__device__ __forceinline__ uint64_t smem_desc(uint32_t at, uint32_t lead, uint32_t stride) {
-  return (uint64_t)((at & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 |
-         2ull << 61;
-}
 // Instruction descriptor of kind::f16: 32-bit accumulation, A and B of one 16-bit type.
 template <bool kBf16>
 __device__ __forceinline__ constexpr uint32_t mma_desc(int m, int n, bool b_mn_major) {
@@ -227,20 +229,24 @@ struct Pairs {
     started = false;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a) {
-    if (w >= end) return false;
-    if (!started) {
-      started = true;
-      tile = a.cta_tile[blockIdx.x];
-      t = load_tile(&a.tiles[tile]);
-    } else if (w >= t.before + (long long)t.units * a.groups) {
-      t = load_tile(&a.tiles[++tile]);
+    while (w < end) {
+      if (!started) {
+        started = true;
+        tile = a.cta_tile[blockIdx.x];
+        t = load_tile(&a.tiles[tile]);
+      } else if (w >= t.before + (long long)(t.units + a.lead) * a.groups) {
+        t = load_tile(&a.tiles[++tile]);
+      }
+      const int len = t.units + a.lead;
+      const long long off = w - t.before;
+      head = (int)(off / len);
+      const int o0 = (int)(off - (long long)head * len), o1 = (int)min((long long)len, o0 + (end - w));
+      w += o1 - o0;
+      u0 = max(o0 - a.lead, 0);
+      u1 = o1 - a.lead;
+      if (u1 > u0) return true;
     }
-    const long long off = w - t.before;
-    head = (int)(off / t.units);
-    u0 = (int)(off - (long long)head * t.units);
-    u1 = (int)min((long long)t.units, u0 + (end - w));
-    w += u1 - u0;
-    return true;
+    return false;
   }
   __device__ __forceinline__ int key_of(int u) const {
     return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kKeys;
@@ -279,13 +285,13 @@ __device__ __forceinline__ void rows_to_pieces(uint32_t (&w)[16], int lane) {
   }
 }
 
-// Weights of 64 keys, s[0..64) scaled by c and moved by b, in 16 bits; returns their sum.
-template <bool kBf16>
-__device__ __forceinline__ float weights64(const float* s, float c, float b, uint32_t* w) {
+// Weights of N keys, s[0..N) scaled by c and moved by b, in 16 bits; returns their sum.
+template <int N, bool kBf16>
+__device__ __forceinline__ float weights(const float* s, float c, float b, uint32_t* w) {
   const float2 c2 = make_float2(c, c), b2 = make_float2(b, b);
   float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
+  for (int j = 0; j < N / 2; ++j) {
     float2 y = fma2(make_float2(s[2 * j], s[2 * j + 1]), c2, b2);
     y.x = exp2_fast(y.x);
     y.y = exp2_fast(y.y);
@@ -297,16 +303,27 @@ __device__ __forceinline__ float weights64(const float* s, float c, float b, uin
   return acc0.x + acc0.y;
 }
 
+__device__ __forceinline__ float max128(const float* s) {
+  float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
+#pragma unroll
+  for (int i = 4; i < 128; i += 4) {
+    m0 = fmaxf(fmaxf(m0, s[i]), s[i + 1]);
+    m1 = fmaxf(fmaxf(m1, s[i + 2]), s[i + 3]);
+  }
+  return fmaxf(m0, m1);
+}
+
 // One unit's weights of one half of a tile: a thread a row.  S is read from TMEM, and the weights
 // replace it there in 16 bits, two to a column, as the left operand of the product with V, which
-// starts on the first 64 keys while the others' weights are computed.  The first 64 are taken
+// starts on the first kFirst keys while the others' weights are computed.  Those are taken
 // against the maximum so far, beside the search for this unit's; only where that shows a row to
 // have outgrown it are they taken again (and in a pair's first unit).
+constexpr int kFirst = 96;
 template <int DP, bool kBf16>
 struct Softmax {
   float top = -INFINITY, b = weight_bias<kBf16>(), sum = 0.f;      // of the raw scores; what is added to scaled ones; of the weights
   __device__ __forceinline__ void step(const AttnArgs& a, uint32_t s_at, uint32_t o_at, bool fresh, bool open, int key0,
-                                       int pos, uint64_t* first_half) {
+                                       int pos, uint64_t* first) {
     const float c = a.scale;
     uint32_t x[128];
     float* s = reinterpret_cast<float*>(x);
@@ -324,41 +341,43 @@ struct Softmax {
         for (int j = 0; j < 32; ++j) s[i + j] = m >> j & 1u ? s[i + j] : -INFINITY;
       }
     }
-    uint32_t w[32];
-    float part = weights64<kBf16>(s, c, b, w);
-    float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
+    // (one copy of the first weights' code: a second one for the second take, seldom run, was
+    // fetched anew in every pair)
+    uint32_t w[kFirst / 2];
+    float part, high = -INFINITY;
+    if (fresh) high = max128(s);
+#pragma unroll 1
+    for (bool again = fresh;; again = true) {
+      if (again) {
+        const float f = high == top ? 1.f : exp2_fast((top - high) * c);
+        top = high;
+        sum *= f;
+        if (!fresh) {
+          // S of this unit follows the previous unit's product with V: O is at rest
+#pragma unroll 1
+          for (int i = 0; i < DP; i += 32) {
+            uint32_t o[32];
+            tc_ld32(o, o_at + i);
+            tc_wait_ld();
+            tc_loaded<32>(o);
 #pragma unroll
-    for (int i = 4; i < 128; i += 4) {
-      m0 = fmaxf(fmaxf(m0, s[i]), s[i + 1]);
-      m1 = fmaxf(fmaxf(m1, s[i + 2]), s[i + 3]);
-    }
-    const float high = fmaxf(fmaxf(m0, m1), top);
-    if (__any_sync(0xffffffffu, (high - top) * c > kLazy)) {      // (also from -inf; -inf - -inf: no)
-      const float f = high == top ? 1.f : exp2_fast((top - high) * c);
-      top = high;
-      sum *= f;
-      if (!fresh) {
-        // S of this unit follows the previous unit's product with V: O is at rest
-#pragma unroll
-        for (int i = 0; i < DP; i += 16) {
-          uint32_t o[16];
-          tc_ld16(o, o_at + i);
-          tc_wait_ld();
-          tc_loaded<16>(o);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-          tc_st16(o_at + i, o);
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tc_st32(o_at + i, o);
+          }
         }
+        if (top != -INFINITY) b = weight_bias<kBf16>() - top * c;
       }
-      if (top != -INFINITY) b = weight_bias<kBf16>() - top * c;
-      part = weights64<kBf16>(s, c, b, w);
+      part = weights<kFirst, kBf16>(s, c, b, w);
+      high = fmaxf(max128(s), top);
+      if (!__any_sync(0xffffffffu, !again && (high - top) * c > kLazy)) break;      // (yes from -inf; no from there to there)
     }
     tc_st32(s_at, w);
+    tc_st16(s_at + 32, w + 32);
     tc_wait_st();
     tc_fence_before();
-    bar_arrive(first_half);
-    sum += part + weights64<kBf16>(s + 64, c, b, w);
-    tc_st32(s_at + 32, w);
+    warp_arrive(first);
+    sum += part + weights<128 - kFirst, kBf16>(s + kFirst, c, b, w);
+    tc_st16(s_at + kFirst / 2, w);
     tc_wait_st();
   }
 };
@@ -394,8 +413,8 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       bar_init(&bars.q_full[i], 1);
       bar_init(&bars.q_empty[i], 1);
       bar_init(&bars.s_full[i], 1);
-      bar_init(&bars.p_full[i][0], 128);
-      bar_init(&bars.p_full[i][1], 128);
+      bar_init(&bars.p_full[i][0], 4);
+      bar_init(&bars.p_full[i][1], 4);
       bar_init(&bars.o_full[i], 1);
     }
     bar_init(&bars.clean_ask, 1);
@@ -450,9 +469,9 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           sm.step(a, s_at, o_at, u == pr.u0, open, key0, pos, &bars.p_full[half][0]);
           tc_fence_before();
         } else {
-          bar_arrive(&bars.p_full[half][0]);
+          warp_arrive(&bars.p_full[half][0]);
         }
-        bar_arrive(&bars.p_full[half][1]);
+        warp_arrive(&bars.p_full[half][1]);
       }
       has = nx.next(a);
       if (!ok || !(ok = bar_wait(&bars, &bars.o_full[half], o_par))) break;
@@ -476,7 +495,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         to[t] = __shfl_sync(0xffffffffu, whole ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part),
                             (lane & 28) + t);
       const int piece = lane & 3;
-#pragma unroll
+#pragma unroll 1
       for (int col = 0; col < DP; col += 32) {
         uint32_t o[32];
         tc_ld32(o, o_at + col);
@@ -589,8 +608,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       // ---- products, by one thread (a warp that votes at each wait took some 200 cycles for it)
       if (elected()) {
         constexpr uint32_t kDescS = mma_desc<kBf16>(128, kKeys, false), kDescO = mma_desc<kBf16>(128, DP, true);
-        const uint64_t kd0 = smem_desc(ring_s, 16, 1024), vd0 = smem_desc(ring_s, kKeys * 128, 1024);
-        const uint64_t qd0 = smem_desc(q_s, 16, 1024);
+        const uint32_t kd0 = desc_low(ring_s, 16), vd0 = desc_low(ring_s, kKeys * 128), qd0 = desc_low(q_s, 16);
         uint32_t par = 0, p_par = 0, q_par = 0, clean_par = 0;      // (the last three: a bit a half)
         int stage = 0;
         auto step = [&]() {
@@ -600,7 +618,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           }
         };
         auto scores = [&](int half, int st) {      // S_half = Q_half K^T
-          const uint64_t qd = qd0 + (uint32_t)(half * (S::kBlock >> 4)), kd = kd0 + (uint32_t)(st * (S::kBlock >> 4));
+          const uint32_t qd = qd0 + half * (S::kBlock >> 4), kd = kd0 + st * (S::kBlock >> 4);
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
             const uint32_t at = ((k / 4) * (kKeys * 128) + (k % 4) * 32) >> 4;
@@ -608,12 +626,12 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           }
           tc_commit(&bars.s_full[half]);
         };
-        auto values = [&](int half, int st, int part, bool add) {      // O_half (+)= P_half V, 64 keys of it
-          const uint64_t vd = vd0 + (uint32_t)(st * (S::kBlock >> 4));
+        // O_half (+)= P_half V, steps of 16 keys from k0 to k1
+        auto values = [&](int half, int st, int k0, int k1, bool add) {
+          const uint32_t vd = vd0 + st * (S::kBlock >> 4);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            tc_mma_ts(tmem + S::kColO + DP * half, tmem + 128 * half + 32 * part + 8 * k,
-                      vd + (4 * part + k) * (2048 >> 4), kDescO, add || k > 0);
+          for (int k = k0; k < k1; ++k)
+            tc_mma_ts(tmem + S::kColO + DP * half, tmem + 128 * half + 8 * k, vd + k * (2048 >> 4), kDescO, add || k > k0);
         };
         // a pair's units; false when a wait ran out.  nx: the pair after it, found meanwhile
         Pairs nx = pr;
@@ -652,10 +670,10 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
                 clean_par ^= 1;
               }
               tc_fence_after();
-              values(h, vs, 0, u > pr.u0);
+              values(h, vs, 0, kFirst / 16, u > pr.u0);
               if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1))) return false;
               tc_fence_after();
-              values(h, vs, 1, true);
+              values(h, vs, kFirst / 16, kKeys / 16, true);
               if (LV_MOSTLY(more)) {
                 scores(h, ks);
                 if (LV_RARE(u + 2 == pr.u1)) tc_commit(&bars.q_empty[h]);

@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
   long long units = 0;
   for (int base = 0; base < n_tiles; base += kPlanThreads) {
     const int t = base + threadIdx.x;
-    const int u = t < n_tiles ? a.tiles[t].units : 0;
+    const int u = t < n_tiles ? a.tiles[t].units + a.lead : 0;
     long long total;
     const long long at = cta_scan(u, ws, &total);
     if (t < n_tiles) a.tiles[t].before = (units + at) * a.groups;
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
   __syncthreads();
   // the tile of each CTA's first unit
   for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
-    const long long lo = a.tiles[t].before, hi = lo + (long long)a.tiles[t].units * a.groups;
+    const long long lo = a.tiles[t].before, hi = lo + (long long)(a.tiles[t].units + a.lead) * a.groups;
     for (long long c = (lo + share - 1) / share; c * share < hi && c <= a.ctas; ++c) a.cta_tile[c] = t;
   }
 }

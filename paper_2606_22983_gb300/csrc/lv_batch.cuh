@@ -15,7 +15,7 @@ namespace lv {
 // token R / G, so that the G heads that share a KV head read it once.  Its keys are cut into
 // units of the kernel's size: first the units that hold sinks, then those from the window on.
 struct AttnTile {
-  int64_t before;       // units of every head group in the tiles before it
+  int64_t before;       // where it starts on the line
   int32_t req;
   int32_t row0;         // its first packed row
   int32_t rows;         // its packed rows
@@ -29,11 +29,12 @@ struct AttnTile {
 };
 static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
 
-// What the kernels read of a plan besides its tiles.  The units of every (tile, head group)
-// pair, in that order, form one line of `units`; CTA c of the attention takes
-// [c * share, (c + 1) * share), whatever tiles that cuts, and the cut ones are joined.
+// What the kernels read of a plan besides its tiles.  Every (tile, head group) pair takes a
+// stretch of one line, in that order: `lead` places for what it costs to begin and end a pair,
+// then one for each of its units.  CTA c of the attention takes the places [c * share,
+// (c + 1) * share), whatever pairs that cuts, and the cut ones are joined.
 struct PlanHead {
-  int64_t units;
+  int64_t units;        // the line's length
   int64_t share;
   int32_t tiles;
   int32_t dead;         // rows of no request
@@ -54,7 +55,8 @@ struct PlanArgs {
   int32_t G;               // query heads a KV head
   int32_t groups;          // head groups a tile is taken by (one CTA each)
   int32_t tile_rows, unit; // of the attention kernel that will run
-  int32_t min_share;       // units a CTA takes at least
+  int32_t lead;            // places of the line ahead of a pair's units
+  int32_t min_share;       // places a CTA takes at least
   int32_t ctas;            // of the attention
   int32_t window, sinks;
   int32_t* row_starts;
@@ -65,7 +67,7 @@ struct PlanArgs {
   PlanReq* reqs;
   AttnTile* tiles;
   int32_t max_tiles;
-  int32_t* cta_tile;       // [ctas + 1] the tile that CTA c's first unit is in
+  int32_t* cta_tile;       // [ctas + 1] the tile that CTA c's first place is in
   PlanHead* head;
 };
 
@@ -100,6 +102,7 @@ struct AttnArgs {
   int32_t num_tokens;
   int32_t window, sinks;
   int32_t groups, hg;      // head groups, and KV heads in one
+  int32_t lead;
   int32_t tile_rows;       // rows of a partial result's slot (per head of the group)
   int32_t dp;              // columns of a partial result
   float scale;             // scale * log2(e)
@@ -123,6 +126,8 @@ constexpr int kRowsUnit = 16;
 int attend_rows_ctas(int dp, bool wide);
 cudaError_t launch_attend_rows(const AttnArgs& a, bool wide, bool bf16, int ctas, cudaStream_t s);
 constexpr int kTcUnit = 128, kTcRows = 256;
+// places ahead of a pair's units: what a pair costs besides its units, in units
+constexpr int kRowsLead = 4, kTcLead = 2;
 // packed rows of a tile: two halves of whole tokens
 inline int tc_tile_rows(int G) { return G > 128 ? kTcRows : 2 * (128 / G * G); }
 struct TcMaps {
