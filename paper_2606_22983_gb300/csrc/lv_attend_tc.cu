@@ -27,19 +27,19 @@ struct TcShape {
   static constexpr int kBlock = kKeys * DP * 2;            // bytes of a K or V unit, and of a Q tile
   static constexpr int kStages = DP == 128 ? 5 : 8;
   static constexpr int kData = 2 * kBlock + kStages * kBlock;
-  static constexpr int kSmem = kData + 256;                // then the barriers
+  static constexpr int kSmem = kData + 512;                // then the barriers
   static constexpr int kColO = 256;                        // S0 at column 0, S1 at 128, O0, O1
   static_assert(kSmem + 1024 <= 227 * 1024, "shared memory of a CTA");
 };
 
 struct Bars {
   uint64_t kv_full[8], kv_empty[8];
-  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2];
+  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][3], o_full[2];
   uint64_t clean_ask, clean_done, drain;
   uint32_t tmem;
   volatile int bad;
 };
-static_assert(sizeof(Bars) <= 256, "its room in shared memory");
+static_assert(sizeof(Bars) <= 512, "its room in shared memory");
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
@@ -315,15 +315,15 @@ __device__ __forceinline__ float max128(const float* s) {
 
 // One unit's weights of one half of a tile: a thread a row.  S is read from TMEM, and the weights
 // replace it there in 16 bits, two to a column, as the left operand of the product with V, which
-// starts on the first kFirst keys while the others' weights are computed.  Those are taken
+// starts on the first 64 keys while the others' weights are computed, and on the next 32.  The first are taken
 // against the maximum so far, beside the search for this unit's; only where that shows a row to
 // have outgrown it are they taken again (and in a pair's first unit).
-constexpr int kFirst = 96;
+constexpr int kFirst = 64;
 template <int DP, bool kBf16>
 struct Softmax {
   float top = -INFINITY, b = weight_bias<kBf16>(), sum = 0.f;      // of the raw scores; what is added to scaled ones; of the weights
   __device__ __forceinline__ void step(const AttnArgs& a, uint32_t s_at, uint32_t o_at, bool fresh, bool open, int key0,
-                                       int pos, uint64_t* first) {
+                                       int pos, uint64_t* ready) {
     const float c = a.scale;
     uint32_t x[128];
     float* s = reinterpret_cast<float*>(x);
@@ -372,12 +372,16 @@ struct Softmax {
       if (!__any_sync(0xffffffffu, !again && (high - top) * c > kLazy)) break;      // (yes from -inf; no from there to there)
     }
     tc_st32(s_at, w);
-    tc_st16(s_at + 32, w + 32);
     tc_wait_st();
     tc_fence_before();
-    warp_arrive(first);
-    sum += part + weights<128 - kFirst, kBf16>(s + kFirst, c, b, w);
-    tc_st16(s_at + kFirst / 2, w);
+    warp_arrive(ready);
+    part += weights<32, kBf16>(s + 64, c, b, w);
+    tc_st16(s_at + 32, w);
+    tc_wait_st();
+    tc_fence_before();
+    warp_arrive(ready + 1);
+    sum += part + weights<32, kBf16>(s + 96, c, b, w);
+    tc_st16(s_at + 48, w);
     tc_wait_st();
   }
 };
@@ -413,8 +417,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       bar_init(&bars.q_full[i], 1);
       bar_init(&bars.q_empty[i], 1);
       bar_init(&bars.s_full[i], 1);
-      bar_init(&bars.p_full[i][0], 4);
-      bar_init(&bars.p_full[i][1], 4);
+      for (int k = 0; k < 3; ++k) bar_init(&bars.p_full[i][k], 4);
       bar_init(&bars.o_full[i], 1);
     }
     bar_init(&bars.clean_ask, 1);
@@ -470,8 +473,9 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           tc_fence_before();
         } else {
           warp_arrive(&bars.p_full[half][0]);
+          warp_arrive(&bars.p_full[half][1]);
         }
-        warp_arrive(&bars.p_full[half][1]);
+        warp_arrive(&bars.p_full[half][2]);
       }
       has = nx.next(a);
       if (!ok || !(ok = bar_wait(&bars, &bars.o_full[half], o_par))) break;
@@ -670,10 +674,13 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
                 clean_par ^= 1;
               }
               tc_fence_after();
-              values(h, vs, 0, kFirst / 16, u > pr.u0);
+              values(h, vs, 0, 4, u > pr.u0);
               if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1))) return false;
               tc_fence_after();
-              values(h, vs, kFirst / 16, kKeys / 16, true);
+              values(h, vs, 4, 6, true);
+              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][2], p_par >> h & 1))) return false;
+              tc_fence_after();
+              values(h, vs, 6, 8, true);
               if (LV_MOSTLY(more)) {
                 scores(h, ks);
                 if (LV_RARE(u + 2 == pr.u1)) tc_commit(&bars.q_empty[h]);
