@@ -129,5 +129,5 @@ class KVBatch:
         lv.lv_attention(self.handle, layer, qh, self._tensor(out, self.q_heads, "out"), lse,
                         1.0 / math.sqrt(self.pool.head_dim) if scale is None else scale,
                         self._stream(stream))
-        self.pool.launches += 2
+        self.pool.launches += 1
         return (out, lse) if return_lse else out

@@ -1644,16 +1644,17 @@ struct lv_batch {
   lv::PlanReq* reqs = nullptr;
   lv::AttnTile* tiles = nullptr;
   int32_t max_tiles = 0;
-  int32_t* cta_tile = nullptr;
+  lv::CtaWork* work = nullptr;
+  int32_t* arrived = nullptr;
   lv::PlanHead* head = nullptr;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
   int32_t G = 1;             // query heads a KV head
   int32_t dp = 128;          // the kernels' columns: head_dim rounded up to 64, 128 or 256
-  int32_t hg = 1;            // KV heads that a CTA of the rows kernel takes
   int32_t box_rows = 0;      // keys in a TMA box; 0: the pages cannot be read by TMA
   EncodeTiled encode = nullptr;    // cuTensorMapEncodeTiled
-  std::vector<CUtensorMap> maps;   // [2L]
+  std::vector<CUtensorMap> maps;   // [2L], boxes of box_rows keys
+  std::vector<CUtensorMap> rows_maps;   // [2L], boxes of the rows kernel's units; empty: T has no whole ones
   // the planned step
   bool planned = false;
   int32_t num_tokens = 0;
@@ -1711,11 +1712,15 @@ lv_status make_maps(lv_batch* b) {
     return LV_ERR_CUDA;
   b->encode = reinterpret_cast<EncodeTiled>(fn);
   const cuuint64_t D = pool->head_dim, H = pool->kv_heads, T = pool->d.T;
-  b->maps.resize(pool->d.J);
-  for (int j = 0; j < pool->d.J; ++j)
-    if (!encode_map(b, &b->maps[j], pool->kv[j], {D, H, T, (cuuint64_t)pool->d.hbm_pages},
-                    {D * 2, H * D * 2, (cuuint64_t)pool->d.P}, {64, 1, (cuuint32_t)box, 1}))
-      return LV_ERR_CUDA;
+  auto fill = [&](std::vector<CUtensorMap>& maps, cuuint32_t keys) {
+    maps.resize(pool->d.J);
+    for (int j = 0; j < pool->d.J; ++j)
+      if (!encode_map(b, &maps[j], pool->kv[j], {D, H, T, (cuuint64_t)pool->d.hbm_pages},
+                      {D * 2, H * D * 2, (cuuint64_t)pool->d.P}, {64, 1, keys, 1}))
+        return false;
+    return true;
+  };
+  if (!fill(b->maps, box) || (T % lv::kRowsUnit == 0 && !fill(b->rows_maps, lv::kRowsUnit))) return LV_ERR_CUDA;
   b->box_rows = box;
   return LV_OK;
 }
@@ -1766,7 +1771,6 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   b->d = *d;
   b->G = d->num_q_heads / H;
   b->dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  b->hg = 1;
   lv_status st;
   try {
     if ((st = make_maps(b)) != LV_OK) return fail(st);
@@ -1777,13 +1781,15 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   b->max_tiles = d->max_requests + (int32_t)(((long long)d->max_tokens * b->G + 15) / 16);
   const int most = std::max({rows_ctas(b, false), rows_ctas(b, true), pool->num_sms});
   // rows of partial results: two slots a CTA
-  size_t rows = (size_t)2 * rows_ctas(b, false) * b->hg * 16;
-  rows = std::max(rows, (size_t)2 * rows_ctas(b, true) * b->hg * 32);
-  if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows);
+  size_t rows = (size_t)2 * rows_ctas(b, false) * 16;
+  rows = std::max(rows, (size_t)2 * rows_ctas(b, true) * 32);
+  // (a warp joins 32 rows of a tile at a time, past its end where it has fewer)
+  if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows + 32);
   try {
     if ((st = batch_alloc(b, &b->reqs, d->max_requests)) != LV_OK ||
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
-        (st = batch_alloc(b, &b->cta_tile, (size_t)most + 1)) != LV_OK ||
+        (st = batch_alloc(b, &b->work, most)) != LV_OK ||
+        (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
         (st = batch_alloc(b, &b->head, 1)) != LV_OK || (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
         (st = batch_alloc(b, &b->part_ml, rows)) != LV_OK)
       return fail(st);
@@ -1868,15 +1874,14 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     a.num_tokens = num_tokens;
     a.max_len = max_len;
     a.G = b->G;
+    a.H = pool->kv_heads;
     if (b->kind == lv::ATTN_TC) {
-      a.groups = pool->kv_heads;
       a.tile_rows = lv::tc_tile_rows(b->G);
       a.unit = lv::kTcUnit;
       a.lead = lv::kTcLead;
       a.min_share = 4;
       b->ctas = pool->num_sms;
     } else {
-      a.groups = pool->kv_heads / b->hg;
       a.tile_rows = b->kind == lv::ATTN_ROWS32 ? 32 : 16;
       a.unit = lv::kRowsUnit;
       a.lead = lv::kRowsLead;
@@ -1894,7 +1899,8 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     a.reqs = b->reqs;
     a.tiles = b->tiles;
     a.max_tiles = b->max_tiles;
-    a.cta_tile = b->cta_tile;
+    a.work = b->work;
+    a.arrived = b->arrived;
     a.head = b->head;
     LV_TRY(lv::launch_plan(a, s));
     b->planned = true;
@@ -1957,8 +1963,8 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.tables = b->d.tables;
   a.positions = b->d.positions;
   a.tiles = b->tiles;
-  a.cta_tile = b->cta_tile;
-  a.head = b->head;
+  a.work = b->work;
+  a.arrived = b->arrived;
   a.q = static_cast<const uint8_t*>(q->data);
   a.out = static_cast<uint8_t*>(out->data);
   a.lse = lse;
@@ -1971,8 +1977,6 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.num_tokens = b->num_tokens;
   a.window = b->d.window;
   a.sinks = b->d.sinks;
-  a.groups = tc ? pool->kv_heads : pool->kv_heads / b->hg;
-  a.hg = tc ? 1 : b->hg;
   a.tile_rows = tc ? lv::tc_tile_rows(b->G) : b->kind == lv::ATTN_ROWS32 ? 32 : 16;
   a.lead = tc ? lv::kTcLead : lv::kRowsLead;
   a.dp = b->dp;
@@ -1985,9 +1989,10 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
     const lv::TcMaps m{&b->maps[2 * layer], &b->maps[2 * layer + 1],
                        a.q_vec && query_map(b, q, &qmap) ? &qmap : nullptr, b->box_rows};
     LV_TRY(lv::launch_attend_tc(a, m, bf16, b->ctas, s));
-  } else
-    LV_TRY(lv::launch_attend_rows(a, b->kind == lv::ATTN_ROWS32, bf16, b->ctas, s));
-  LV_TRY(lv::launch_attend_join(a, bf16, b->ctas, s));
+  } else {
+    const CUtensorMap* m = b->rows_maps.empty() ? nullptr : &b->rows_maps[2 * layer];
+    LV_TRY(lv::launch_attend_rows(a, m, m ? m + 1 : nullptr, b->kind == lv::ATTN_ROWS32, bf16, b->ctas, s));
+  }
   return LV_OK;
 }
 

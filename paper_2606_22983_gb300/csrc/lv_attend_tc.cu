@@ -17,9 +17,6 @@ constexpr int kKeys = kTcUnit;            // keys of a unit
 // for the others (256 * 208 + 128 * 88 = 64 512)
 constexpr int kRegsSoft = 208, kRegsOther = 88;
 constexpr long long kWaitLimitNs = 1000000000ll;   // one second a wait
-// A warp that runs alone pays some 110 cycles for a taken branch: what is rare is laid out of line.
-#define LV_RARE(x) __builtin_expect(!!(x), 0)
-#define LV_MOSTLY(x) __builtin_expect(!!(x), 1)
 
 template <int DP>
 struct TcShape {
@@ -216,27 +213,88 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
+// The join of a cut pair by one warp: rows row0 .. row0 + 31 of its tile (those in rows_in), every
+// piece's sums weighted by its maximum against the largest.  Lane i knows row i's output.
+template <int DP, bool kBf16>
+__device__ __forceinline__ void join_rows(const AttnArgs& a, const Pieces& ps, int row0, int lane, uint32_t rows_in,
+                                          uint16_t* out, int64_t r, int hq) {
+  constexpr int kCols = DP / 32;      // a lane's
+  const bool mine = rows_in >> lane & 1;
+  auto slot = [&](int p) { return part_slot(ps.first + p, p == 0) * a.tile_rows + row0; };
+  float top = -INFINITY, sum = 0.f;
+  for (int p = 0; p < ps.count; ++p)
+    if (mine) top = fmaxf(top, __ldcg(&a.part_ml[slot(p) + lane]).x);
+  float acc[32][kCols];
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) acc[i][e] = 0.f;
+#pragma unroll 1
+  for (int p = 0; p < ps.count; ++p) {
+    float f = 0.f;
+    if (mine) {
+      const float2 ml = __ldcg(&a.part_ml[slot(p) + lane]);
+      f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
+      sum += ml.y * f;
+    }
+    const float* o = a.part_o + slot(p) * DP + kCols * lane;
+    // (32 loads on their way at once; rows past the tile's read what is there and are not stored)
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float g = __shfl_sync(0xffffffffu, f, i);
+      if constexpr (kCols == 4) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + i * DP));
+        acc[i][0] += v.x * g;
+        acc[i][1] += v.y * g;
+        acc[i][2] += v.z * g;
+        acc[i][3] += v.w * g;
+      } else {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(o + i * DP));
+        acc[i][0] += v.x * g;
+        acc[i][1] += v.y * g;
+      }
+    }
+  }
+  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+  if (mine && a.lse)
+    a.lse[r * (a.H * a.G) + hq] =
+        sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const float g = __shfl_sync(0xffffffffu, inv, i);
+    uint16_t* to = reinterpret_cast<uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(out), i)) + kCols * lane;
+    if (!(rows_in >> i & 1) || kCols * lane >= a.D) continue;
+#pragma unroll
+    for (int e = 0; e < kCols; e += 2) {
+      const uint32_t w = pack16<kBf16>(acc[i][e] * g, acc[i][e + 1] * g);
+      if (a.o_vec) {
+        *reinterpret_cast<uint32_t*>(to + e) = w;
+      } else {
+        to[e] = (uint16_t)w;
+        to[e + 1] = (uint16_t)(w >> 16);
+      }
+    }
+  }
+}
+
 // The pairs (tile, head) of a CTA's share, one after the other.
 struct Pairs {
-  long long w, end;
+  long long w, end, share;
   AttnTile t;
   int tile, head, u0, u1;
-  bool started;
+  int dead;
   __device__ __forceinline__ void init(const AttnArgs& a) {
-    const long long units = a.head->units, share = a.head->share;
-    w = blockIdx.x * share;
-    end = min(units, w + share);
-    started = false;
+    const CtaWork x = load_words(&a.work[blockIdx.x]);
+    w = x.begin;
+    end = x.end;
+    share = x.share;
+    t = x.t;
+    tile = x.tile;
+    dead = x.dead;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a) {
     while (w < end) {
-      if (!started) {
-        started = true;
-        tile = a.cta_tile[blockIdx.x];
-        t = load_tile(&a.tiles[tile]);
-      } else if (w >= t.before + (long long)(t.units + a.lead) * a.groups) {
-        t = load_tile(&a.tiles[++tile]);
-      }
+      if (w >= t.before + (long long)(t.units + a.lead) * a.H) t = load_words(&a.tiles[++tile]);
       const int len = t.units + a.lead;
       const long long off = w - t.before;
       head = (int)(off / len);
@@ -541,8 +599,20 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         __syncwarp();
       }
       const float top2 = sm.top * a.scale;      // in log2
-      if (mine && !whole) {
-        a.part_ml[slot] = make_float2(top2, sm.sum);
+      if (!whole) {
+        if (mine) a.part_ml[slot] = make_float2(top2, sm.sum);
+        // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
+        __threadfence();
+        __syncwarp();
+        const Pieces ps = pieces_of(pr.t, pr.head, a.lead, pr.share);
+        int32_t* count = &a.arrived[ps.first * kArriveWords + wid];
+        int before = 0;
+        if (lane == 0) before = atomicAdd(count, 1);
+        if (__shfl_sync(0xffffffffu, before, 0) == ps.count - 1) {
+          if (lane == 0) *count = 0;
+          __threadfence();
+          join_rows<DP, kBf16>(a, ps, half * half_rows + (row & ~31), lane, rows_in, out, r, hq);
+        }
       } else if (mine && a.lse) {
         a.lse[r * (a.H * a.G) + hq] =
             sm.sum == 0.f ? -INFINITY : (top2 - weight_bias<kBf16>()) * 0.693147180559945f + logf(sm.sum);
@@ -789,7 +859,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
       }
       // rows of no request
-      if (ok && a.head->dead > 0) {
+      if (ok && pr.dead > 0) {
         const int Hq = a.H * a.G;
         for (int r = blockIdx.x; r < a.num_tokens; r += gridDim.x) {
           if (a.positions[r] >= 0) continue;

@@ -182,19 +182,23 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
     const int u = t < n_tiles ? a.tiles[t].units + a.lead : 0;
     long long total;
     const long long at = cta_scan(u, ws, &total);
-    if (t < n_tiles) a.tiles[t].before = (units + at) * a.groups;
+    if (t < n_tiles) a.tiles[t].before = (units + at) * a.H;
     units += total;
   }
-  units *= a.groups;
+  units *= a.H;
   const long long share = max((units + a.ctas - 1) / a.ctas, (long long)a.min_share);
-  if (threadIdx.x == 0)
-    *a.head = PlanHead{units, share, n_tiles, a.num_tokens - (int)live, 0, 0};
+  const int dead = a.num_tokens - (int)live;
+  if (threadIdx.x == 0) a.head->ticket = 0;
+  for (int i = threadIdx.x; i < a.ctas * kArriveWords; i += kPlanThreads) a.arrived[i] = 0;
   __syncthreads();
-  // the tile of each CTA's first unit
   for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
-    const long long lo = a.tiles[t].before, hi = lo + (long long)(a.tiles[t].units + a.lead) * a.groups;
-    for (long long c = (lo + share - 1) / share; c * share < hi && c <= a.ctas; ++c) a.cta_tile[c] = t;
+    const AttnTile tile = a.tiles[t];
+    const long long lo = tile.before, hi = lo + (long long)(tile.units + a.lead) * a.H;
+    for (long long c = (lo + share - 1) / share; c * share < hi; ++c)
+      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), share, t, dead};
   }
+  for (long long c = (units + share - 1) / share + threadIdx.x; c < a.ctas; c += kPlanThreads)
+    a.work[c] = CtaWork{AttnTile{}, 0, 0, share, 0, dead};
 }
 
 // ---------------------------------------------------------------- KV write
@@ -244,6 +248,7 @@ __device__ __forceinline__ uint4 load8(const uint8_t* src, int64_t at, int type,
 template <bool kBf16>
 __global__ void __launch_bounds__(kWriteThreads) k_kv_write(WriteArgs a) {
   dep_wait();
+  dep_trigger();
   const uint32_t cols = (uint32_t)a.D / 8u, per_kv = (uint32_t)a.H * cols, per_row = 2u * per_kv;
   const uint64_t total = (uint64_t)a.num_tokens * per_row;
   for (uint64_t i = (uint64_t)blockIdx.x * kWriteThreads + threadIdx.x; i < total;

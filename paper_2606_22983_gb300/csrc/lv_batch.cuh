@@ -29,17 +29,22 @@ struct AttnTile {
 };
 static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
 
-// What the kernels read of a plan besides its tiles.  Every (tile, head group) pair takes a
-// stretch of one line, in that order: `lead` places for what it costs to begin and end a pair,
-// then one for each of its units.  CTA c of the attention takes the places [c * share,
-// (c + 1) * share), whatever pairs that cuts, and the cut ones are joined.
-struct PlanHead {
-  int64_t units;        // the line's length
+// Every (tile, KV head) pair takes a stretch of one line, in that order: `lead` places for what
+// it costs to begin and end a pair, then one for each of its units.  CTA c of the attention takes
+// the places [c * share, (c + 1) * share), whatever pairs that cuts; the CTA that finishes the last
+// piece of a cut pair joins its pieces, in their order.
+struct CtaWork {        // what a CTA starts from
+  AttnTile t;           // of its first place
+  int64_t begin, end;   // its places; begin == end: none
   int64_t share;
-  int32_t tiles;
-  int32_t dead;         // rows of no request
+  int32_t tile;
+  int32_t dead;         // rows of no request in the step
+};
+static_assert(sizeof(CtaWork) == 80, "read as five 16-byte words");
+
+struct PlanHead {
   int32_t ticket;       // CTAs of the plan that are done
-  int32_t pad;
+  int32_t pad[3];
 };
 
 struct PlanReq {        // per request, from the plan's first half to its second
@@ -53,7 +58,7 @@ struct PlanArgs {
   const int32_t* lens;
   int32_t n, num_tokens, max_len;
   int32_t G;               // query heads a KV head
-  int32_t groups;          // head groups a tile is taken by (one CTA each)
+  int32_t H;               // KV heads
   int32_t tile_rows, unit; // of the attention kernel that will run
   int32_t lead;            // places of the line ahead of a pair's units
   int32_t min_share;       // places a CTA takes at least
@@ -67,7 +72,8 @@ struct PlanArgs {
   PlanReq* reqs;
   AttnTile* tiles;
   int32_t max_tiles;
-  int32_t* cta_tile;       // [ctas + 1] the tile that CTA c's first place is in
+  CtaWork* work;           // [ctas]
+  int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
   PlanHead* head;
 };
 
@@ -92,8 +98,8 @@ struct AttnArgs {
   const int32_t* tables;
   const int32_t* positions;
   const AttnTile* tiles;
-  const int32_t* cta_tile;
-  const PlanHead* head;
+  const CtaWork* work;
+  int32_t* arrived;
   const uint8_t* q;
   uint8_t* out;
   float* lse;
@@ -101,17 +107,20 @@ struct AttnArgs {
   int32_t q_vec, o_vec;    // 16-byte accesses allowed
   int32_t num_tokens;
   int32_t window, sinks;
-  int32_t groups, hg;      // head groups, and KV heads in one
   int32_t lead;
-  int32_t tile_rows;       // rows of a partial result's slot (per head of the group)
+  int32_t tile_rows;       // rows of a partial result's slot
   int32_t dp;              // columns of a partial result
   float scale;             // scale * log2(e)
-  float* part_o;           // [2 * ctas][hg][tile_rows][dp] sums, and
-  float2* part_ml;         // [2 * ctas][hg][tile_rows] their maximum (in log2) and weight
+  float* part_o;           // [2 * ctas][tile_rows][dp] sums, and
+  float2* part_ml;         // [2 * ctas][tile_rows] their maximum (in log2) and weight
   long long* ctl;
 };
 
-// CTA c's slot for a piece of a (tile, head group) pair that it holds only part of: a piece
+// Words of AttnArgs.arrived a CTA: the rows kernel counts a pair's pieces in the first, the other
+// one a warp's rows in each.
+constexpr int kArriveWords = 8;
+
+// CTA c's slot for a piece of a (tile, head) pair that it holds only part of: a piece
 // that does not start the pair is the first that the CTA does, one that starts it the last.
 __host__ __device__ inline int64_t part_slot(int64_t cta, bool starts) { return 2 * cta + (starts ? 1 : 0); }
 
@@ -124,7 +133,8 @@ cudaError_t configure_attend_tc();
 // keys of a unit, and CTAs that an SM holds, of the rows kernel
 constexpr int kRowsUnit = 16;
 int attend_rows_ctas(int dp, bool wide);
-cudaError_t launch_attend_rows(const AttnArgs& a, bool wide, bool bf16, int ctas, cudaStream_t s);
+cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool wide, bool bf16,
+                               int ctas, cudaStream_t s);      // maps: boxes of 64 columns and a unit's keys, or null
 constexpr int kTcUnit = 128, kTcRows = 256;
 // places ahead of a pair's units: what a pair costs besides its units, in units
 constexpr int kRowsLead = 4, kTcLead = 2;
@@ -137,7 +147,6 @@ struct TcMaps {
   int box_rows;
 };
 cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cudaStream_t s);
-cudaError_t launch_attend_join(const AttnArgs& a, bool bf16, int ctas, cudaStream_t s);
 
 // A launch that may be scheduled while the previous kernel on `s` still runs; the kernel waits
 // (pdl_wait) before it reads anything that kernel may have written.
@@ -158,22 +167,34 @@ cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, unsigned block
 }
 
 #ifdef __CUDACC__
+// A warp that runs alone pays some 110 cycles for a taken branch: what is rare is laid out of line.
+#define LV_RARE(x) __builtin_expect(!!(x), 0)
+#define LV_MOSTLY(x) __builtin_expect(!!(x), 1)
 __device__ __forceinline__ void report(long long* ctl, int code, long long detail) {
   if (atomicCAS(reinterpret_cast<unsigned long long*>(&ctl[C_ERR]), 0ull, (unsigned long long)code) == 0ull)
     ctl[C_ERR_DETAIL] = detail;
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ AttnTile load_tile(const AttnTile* t) {
+template <typename T>
+__device__ __forceinline__ T load_words(const T* p) {
   union {
-    int4 w[3];
-    AttnTile t;
+    int4 w[sizeof(T) / 16];
+    T t;
   } x;
-  const int4* q = reinterpret_cast<const int4*>(t);
-  x.w[0] = q[0];
-  x.w[1] = q[1];
-  x.w[2] = q[2];
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 16); ++i) x.w[i] = reinterpret_cast<const int4*>(p)[i];
   return x.t;
+}
+// The pieces of pair (tile, head) that unit 0 of it starts: CTAs first .. first + count - 1.
+struct Pieces {
+  int64_t first;
+  int count;
+};
+__device__ __forceinline__ Pieces pieces_of(const AttnTile& t, int head, int lead, int64_t share) {
+  const int64_t start = t.before + (int64_t)head * (t.units + lead) + lead;
+  const int64_t first = start / share;
+  return {first, (int)((start + t.units - 1) / share - first) + 1};
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
