@@ -114,17 +114,17 @@ struct Walk {
 template <int DP, int MT>
 struct RowsShape {
   static constexpr int kM = 16 * MT;
-  static constexpr int kStages = MT == 1 && DP <= 128 ? 3 : 2;
+  static constexpr int kStages = DP == 64 ? 4 : 2;
+  static constexpr int kCtas = DP == 256 ? 1 : MT == 1 ? 3 : 2;      // in an SM: 228 KiB, 64 K registers
   static constexpr int kHalves = DP / 64;                    // 64 columns, 128 bytes, wide
   static constexpr int kTile = kU * DP * 2;                  // bytes of a unit's K (or V) in a stage
   static constexpr int kRing = kStages * 2 * kTile;          // of a warp
-  static constexpr int kRegs = MT * DP / 2 + 4 * MT;         // floats a lane hands over: sums, maxima, weights
   static constexpr bool kQInRegs = MT * DP <= 128;
   static constexpr int kQ = kQInRegs ? 0 : kM * DP * 2;      // a warp's queries
-  static constexpr int kJoin = 2 * kRegs * 32 * 4;
+  static constexpr int kJoin = kM * DP * 4 + kM * 8;         // what a warp hands over: sums; maxima and weights
   static constexpr int kBars = 256;                          // a barrier a stage and warp, and a word
   static constexpr int kSmem = kWarps * (kRing + kQ) + kJoin + kBars;
-  static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+  static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
 };
 
 // The join of a cut pair by a CTA, a warp a row: every piece's sums weighted by its maximum against
@@ -204,7 +204,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
 // units (T a multiple of 16); else by 16-byte copies, a key at a time from its page.  In shared
 // memory a unit is [64-column block][key][128 bytes], swizzled as TMA does it.
 template <int DP, int MT, bool kBf16, bool kTma>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, RowsShape<DP, MT>::kCtas)
 k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap kmap,
               const __grid_constant__ CUtensorMap vmap) {
   using S = RowsShape<DP, MT>;
@@ -504,34 +504,34 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
     }
-    // ---- the warps joined: n / 2 of n hand over to the others
-#pragma unroll
-    for (int n = kWarps; n > 1; n >>= 1) {
-      if (C.u_end - C.u_begin <= n / 2) continue;      // the upper ones had no unit
-      float* box = join + (wid % (n / 2)) * S::kRegs * 32 + lane;
+    // ---- the warps that had a unit joined, one after the other, by the first
+    const int have = min(C.u_end - C.u_begin, kWarps);
+#pragma unroll 1
+    for (int n = 1; n < have; ++n) {
+      float* box = join + lane;
+      float2* ml = reinterpret_cast<float2*>(join + S::kM * DP) + lane / 4;
       __syncthreads();
-      if (wid >= n / 2 && wid < n) {
+      if (wid == n) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e) box[((m * (DP / 8) + d) * 4 + e) * 32] = o[m][d][e];
+        if ((lane & 3) == 0) {
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
-          box[(MT * DP / 2 + i) * 32] = top[i];
-          box[(MT * DP / 2 + 2 * MT + i) * 32] = sum[i];
+          for (int i = 0; i < 2 * MT; ++i) ml[8 * i] = make_float2(top[i], sum[i]);
         }
       }
       __syncthreads();
-      if (wid < n / 2) {
+      if (wid == 0) {
 #pragma unroll
         for (int i = 0; i < 2 * MT; ++i) {
-          const float t2 = box[(MT * DP / 2 + i) * 32];
-          const float t = fmaxf(top[i], t2);
-          const float f = top[i] == t ? 1.f : exp2_fast(top[i] - t), f2 = t2 == t ? 1.f : exp2_fast(t2 - t);
+          const float2 x = ml[8 * i];
+          const float t = fmaxf(top[i], x.x);
+          const float f = top[i] == t ? 1.f : exp2_fast(top[i] - t), f2 = x.x == t ? 1.f : exp2_fast(x.x - t);
           top[i] = t;
-          sum[i] = sum[i] * f + box[(MT * DP / 2 + 2 * MT + i) * 32] * f2;
+          sum[i] = sum[i] * f + x.y * f2;
 #pragma unroll
           for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
@@ -611,8 +611,10 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 template <int DP, int MT, bool kTma>
 cudaError_t set_rows() {
   for (auto k : {k_attend_rows<DP, MT, true, kTma>, k_attend_rows<DP, MT, false, kTma>}) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP, MT>::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP, MT>::kSmem);
+    // (the default split leaves room for one CTA)
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -635,14 +637,10 @@ cudaError_t configure_attend() {
   return cudaSuccess;
 }
 
-// CTAs that fit in an SM's 227 KiB of shared memory (and its registers)
+// CTAs of the kernel that an SM holds
 int attend_rows_ctas(int dp, bool wide) {
-  const int bytes = dp == 64 ? (wide ? RowsShape<64, 2>::kSmem : RowsShape<64, 1>::kSmem)
-                    : dp == 128 ? (wide ? RowsShape<128, 2>::kSmem : RowsShape<128, 1>::kSmem)
-                                : RowsShape<256, 1>::kSmem;
-  const int fit = 228 * 1024 / (bytes + 1024);
-  const int most = wide ? 2 : dp == 64 ? 4 : 2;
-  return fit < 1 ? 1 : fit > most ? most : fit;
+  if (dp == 256) return RowsShape<256, 1>::kCtas;
+  return wide ? RowsShape<128, 2>::kCtas : RowsShape<128, 1>::kCtas;
 }
 
 cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool wide, bool bf16,
