@@ -1746,8 +1746,11 @@ bool device_array(const lv_pool* pool, const void* p, size_t align) {
   return a.type == cudaMemoryTypeManaged || (a.type == cudaMemoryTypeDevice && a.device == pool->device);
 }
 
-// CTAs of the rows kernel
-int rows_ctas(const lv_batch* b, bool wide) { return b->pool->num_sms * lv::attend_rows_ctas(b->dp, wide); }
+// Shares of a head's line in the rows kernel, whose CTAs are that many times H: what the SMs hold.
+int rows_shares(const lv_batch* b, bool wide) {
+  return std::max(1, b->pool->num_sms * lv::attend_rows_ctas(b->dp, wide) / b->pool->kv_heads);
+}
+int rows_ctas(const lv_batch* b, bool wide) { return rows_shares(b, wide) * b->pool->kv_heads; }
 
 lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   const int H = pool->kv_heads, D = pool->head_dim;
@@ -1874,18 +1877,20 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     a.num_tokens = num_tokens;
     a.max_len = max_len;
     a.G = b->G;
-    a.H = pool->kv_heads;
     if (b->kind == lv::ATTN_TC) {
+      a.line_heads = pool->kv_heads;
       a.tile_rows = lv::tc_tile_rows(b->G);
       a.unit = lv::kTcUnit;
       a.lead = lv::kTcLead;
       a.min_share = 4;
-      b->ctas = pool->num_sms;
+      b->ctas = a.shares = pool->num_sms;
     } else {
+      a.line_heads = 1;
       a.tile_rows = b->kind == lv::ATTN_ROWS32 ? 32 : 16;
       a.unit = lv::kRowsUnit;
       a.lead = lv::kRowsLead;
       a.min_share = 4;
+      a.shares = rows_shares(b, b->kind == lv::ATTN_ROWS32);
       b->ctas = rows_ctas(b, b->kind == lv::ATTN_ROWS32);
     }
     a.ctas = b->ctas;

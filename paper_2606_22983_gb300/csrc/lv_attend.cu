@@ -100,12 +100,12 @@ __device__ __forceinline__ void clear_dead(const AttnArgs& a, int i, int of) {
   }
 }
 
-// A walk over the units of a CTA's share that one warp takes: of each pair the units
+// A walk over the units of a CTA's share that one warp takes: of each tile the units
 // first + wid, first + wid + kWarps, ...
 struct Walk {
-  int64_t w, end;          // the next pair's first place; the share's end
+  int64_t w, end;          // the next tile's first place; the share's end
   AttnTile t;
-  int tile, head;
+  int tile;
   int u, u_end;            // units of the pair, this warp's next and the CTA's end
   int u_begin;
   int32_t page;            // of unit u (where a unit lies in one page)
@@ -135,7 +135,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
   constexpr int kCols = DP / 32;
   constexpr int kBatch = 8;
   for (int row = threadIdx.x >> 5; row < t.rows; row += kWarps) {
-    auto at = [&](int p) { return part_slot(ps.first + p, p == 0) * a.tile_rows + row; };
+    auto at = [&](int p) { return part_slot((ps.first + p) * a.H + head, p == 0) * a.tile_rows + row; };
     float top = -INFINITY;
     for (int p = lane; p < ps.count; p += 32) top = fmaxf(top, __ldcg(&a.part_ml[at(p)]).x);
 #pragma unroll
@@ -194,8 +194,8 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
   }
 }
 
-// One CTA: its share of the line.  Its four warps take a pair's units in turn and are joined at the
-// pair's end; each streams its units' K and V rows through a ring of its own, so no barrier of the
+// One CTA: its share of one KV head's line.  Its four warps take a tile's units in turn and are joined at the
+// tile's end; each streams its units' K and V rows through a ring of its own, so no barrier of the
 // CTA lies in the loop.  S = Q K^T (16 rows x 16 keys a step), the running maximum and sum of the
 // softmax, O += P V, all in registers, by mma.sync: the rows are few, the work is reading the
 // cache, and m16n8k16 wastes half its rows where a 128-row tcgen05 tile would waste 15 of 16.
@@ -234,11 +234,12 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   };
   auto next_pair = [&](Walk& x) -> bool {
     while (x.w < x.end) {
-      if (x.w >= x.t.before + (int64_t)(x.t.units + a.lead) * a.H) x.t = load_words(&a.tiles[++x.tile]);
       const int len = x.t.units + a.lead;
-      const uint32_t off = (uint32_t)(x.w - x.t.before);      // (a tile's places: far below 2^32)
-      x.head = (int)(off / (uint32_t)len);
-      const int o0 = (int)(off - (uint32_t)x.head * len), o1 = (int)min((int64_t)len, o0 + (x.end - x.w));
+      if (x.w >= x.t.before + len) {
+        x.t = load_words(&a.tiles[++x.tile]);
+        continue;
+      }
+      const int o0 = (int)(x.w - x.t.before), o1 = (int)min((int64_t)len, o0 + (x.end - x.w));
       x.w += o1 - o0;
       x.u_begin = max(o0 - a.lead, 0);
       x.u_end = o1 - a.lead;
@@ -251,7 +252,8 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     return false;
   };
   Walk L;
-  const CtaWork work = load_words(&a.work[blockIdx.x]);
+  const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
+  const CtaWork work = load_words(&a.work[group]);
   L.w = work.begin;
   L.end = work.end;
   L.t = work.t;
@@ -274,13 +276,13 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
                      : "memory");
 #pragma unroll
         for (int x = 0; x < S::kHalves; ++x) {
-          tma_box(dst + x * kU * 128, &kmap, 64 * x, L.head, off, page, bar_s + 8 * s);
-          tma_box(dst + S::kTile + x * kU * 128, &vmap, 64 * x, L.head, off, page, bar_s + 8 * s);
+          tma_box(dst + x * kU * 128, &kmap, 64 * x, head, off, page, bar_s + 8 * s);
+          tma_box(dst + S::kTile + x * kU * 128, &vmap, 64 * x, head, off, page, bar_s + 8 * s);
         }
       }
       __syncwarp();
     } else {
-      const uint32_t head = (uint32_t)L.head * (uint32_t)a.D * 2;
+      const uint32_t head_at = (uint32_t)head * (uint32_t)a.D * 2;
       constexpr int kChunks = DP / 8;               // 16-byte pieces of a row
 #pragma unroll
       for (int n = 0; n < kU * kChunks / 32; ++n) {
@@ -292,7 +294,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         const uint32_t b = (uint32_t)key / (uint32_t)a.T;
         if (ok) page = a.tables[(size_t)L.t.req * a.maxB + b];
         ok = ok && (uint32_t)page < a.hbm_pages;
-        const size_t off = ok ? (size_t)page * a.P + (size_t)(key - b * a.T) * tok + head + c * 16 : 0;
+        const size_t off = ok ? (size_t)page * a.P + (size_t)(key - b * a.T) * tok + head_at + c * 16 : 0;
         const uint32_t to = dst + (c >> 3) * kU * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
         copy16(to, a.kv[0] + off, ok);
         copy16(to + S::kTile, a.kv[1] + off, ok);
@@ -320,7 +322,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q);
     auto q_row = [&](int row) -> const uint16_t* {
       const int R = C.t.row0 + row, token = R / a.G, g = R - token * a.G;
-      return q + (C.t.qrow + token) * a.q_row + (int64_t)(C.head * a.G + g) * a.q_head;
+      return q + (C.t.qrow + token) * a.q_row + (int64_t)(head * a.G + g) * a.q_head;
     };
     auto q_at = [&](const uint16_t* x, int row, int d) -> uint32_t {     // two elements, zeros past the rows and columns
       if (row >= C.t.rows || d >= a.D) return 0u;
@@ -550,7 +552,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         if (whole) {
           const int R = C.t.row0 + row, token = R / a.G, g = R - token * a.G;
           const int64_t r = C.t.qrow + token;
-          const int h = C.head * a.G + g;
+          const int h = head * a.G + g;
           const float inv = sum[i] > 0.f || sum[i] != sum[i] ? 1.f / sum[i] : 0.f;
           uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head;
 #pragma unroll
@@ -579,12 +581,12 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       }
     }
     if (!whole) {      // (the whole CTA: the pair is the same in all its warps)
-      const Pieces ps = pieces_of(C.t, C.head, a.lead, work.share);
+      const Pieces ps = pieces_of(C.t, 0, a.lead, work.share);
       if (wid == 0) {
         __threadfence();
         __syncwarp();
         if (lane == 0) {
-          int32_t* count = &a.arrived[ps.first * kArriveWords];
+          int32_t* count = &a.arrived[(ps.first * a.H + head) * kArriveWords];
           const int last = atomicAdd(count, 1) == ps.count - 1;
           if (last) *count = 0;
           __threadfence();
@@ -592,7 +594,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         }
       }
       __syncthreads();
-      if (*word) join_rows<DP, kBf16>(a, C.t, C.head, ps);
+      if (*word) join_rows<DP, kBf16>(a, C.t, head, ps);
       __syncthreads();
     }
   }

@@ -182,22 +182,22 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
     const int u = t < n_tiles ? a.tiles[t].units + a.lead : 0;
     long long total;
     const long long at = cta_scan(u, ws, &total);
-    if (t < n_tiles) a.tiles[t].before = (units + at) * a.H;
+    if (t < n_tiles) a.tiles[t].before = (units + at) * a.line_heads;
     units += total;
   }
-  units *= a.H;
-  const long long share = max((units + a.ctas - 1) / a.ctas, (long long)a.min_share);
+  units *= a.line_heads;
+  const long long share = max((units + a.shares - 1) / a.shares, (long long)a.min_share);
   const int dead = a.num_tokens - (int)live;
   if (threadIdx.x == 0) a.head->ticket = 0;
   for (int i = threadIdx.x; i < a.ctas * kArriveWords; i += kPlanThreads) a.arrived[i] = 0;
   __syncthreads();
   for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
     const AttnTile tile = a.tiles[t];
-    const long long lo = tile.before, hi = lo + (long long)(tile.units + a.lead) * a.H;
+    const long long lo = tile.before, hi = lo + (long long)(tile.units + a.lead) * a.line_heads;
     for (long long c = (lo + share - 1) / share; c * share < hi; ++c)
       a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), share, t, dead};
   }
-  for (long long c = (units + share - 1) / share + threadIdx.x; c < a.ctas; c += kPlanThreads)
+  for (long long c = (units + share - 1) / share + threadIdx.x; c < a.shares; c += kPlanThreads)
     a.work[c] = CtaWork{AttnTile{}, 0, 0, share, 0, dead};
 }
 

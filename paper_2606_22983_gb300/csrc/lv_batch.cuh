@@ -29,10 +29,13 @@ struct AttnTile {
 };
 static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
 
-// Every (tile, KV head) pair takes a stretch of one line, in that order: `lead` places for what
-// it costs to begin and end a pair, then one for each of its units.  CTA c of the attention takes
-// the places [c * share, (c + 1) * share), whatever pairs that cuts; the CTA that finishes the last
-// piece of a cut pair joins its pieces, in their order.
+// A pair of a tile and a KV head takes a stretch of a line: `lead` places for what it costs to begin
+// and end it, then one for each of its units.  A CTA takes `share` places on, whatever pairs that
+// cuts; the one that finishes the last piece of a cut pair joins its pieces, in their order.
+// The kernel for many rows has one line of all pairs, tile after tile and head after head in it.
+// The one for few rows has a line of the tiles for each KV head, and H CTAs beside one another take
+// the same places of theirs: they read the same pages, whose H rows of a token lie together, at
+// about the same time.
 struct CtaWork {        // what a CTA starts from
   AttnTile t;           // of its first place
   int64_t begin, end;   // its places; begin == end: none
@@ -58,10 +61,11 @@ struct PlanArgs {
   const int32_t* lens;
   int32_t n, num_tokens, max_len;
   int32_t G;               // query heads a KV head
-  int32_t H;               // KV heads
+  int32_t line_heads;      // KV heads in a line: all, or 1
   int32_t tile_rows, unit; // of the attention kernel that will run
   int32_t lead;            // places of the line ahead of a pair's units
   int32_t min_share;       // places a CTA takes at least
+  int32_t shares;          // of a line
   int32_t ctas;            // of the attention
   int32_t window, sinks;
   int32_t* row_starts;
@@ -72,7 +76,7 @@ struct PlanArgs {
   PlanReq* reqs;
   AttnTile* tiles;
   int32_t max_tiles;
-  CtaWork* work;           // [ctas]
+  CtaWork* work;           // [shares]
   int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
   PlanHead* head;
 };
@@ -186,7 +190,7 @@ __device__ __forceinline__ T load_words(const T* p) {
   for (int i = 0; i < (int)(sizeof(T) / 16); ++i) x.w[i] = reinterpret_cast<const int4*>(p)[i];
   return x.t;
 }
-// The pieces of pair (tile, head) that unit 0 of it starts: CTAs first .. first + count - 1.
+// The pieces of a pair (head: its head's number in the line): shares first .. first + count - 1.
 struct Pieces {
   int64_t first;
   int count;
