@@ -86,6 +86,13 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// The sum before, and what this warp wrote visible with it.
+__device__ __forceinline__ int add_release(int32_t* p, int v) {
+  int was;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(was) : "l"(p), "r"(v) : "memory");
+  return was;
+}
+
 // Rows of no request: out = 0, lse = -inf.  Thread i of `of` threads.
 __device__ __forceinline__ void clear_dead(const AttnArgs& a, int i, int of) {
   const int Hq = a.H * a.G;
@@ -111,6 +118,11 @@ struct Walk {
   int32_t page;            // of unit u (where a unit lies in one page)
 };
 
+struct CutTile {
+  AttnTile t;
+  int last, pad[3];        // this CTA's was its last piece to arrive
+};
+
 template <int DP, int MT>
 struct RowsShape {
   static constexpr int kM = 16 * MT;
@@ -122,7 +134,7 @@ struct RowsShape {
   static constexpr bool kQInRegs = MT * DP <= 128;
   static constexpr int kQ = kQInRegs ? 0 : kM * DP * 2;      // a warp's queries
   static constexpr int kJoin = kM * DP * 4 + kM * 8;         // what a warp hands over: sums; maxima and weights
-  static constexpr int kBars = 256;                          // a barrier a stage and warp, and a word
+  static constexpr int kBars = 8 * kWarps * kStages + 2 * (int)sizeof(CutTile);      // a barrier a stage and warp
   static constexpr int kSmem = kWarps * (kRing + kQ) + kJoin + kBars;
   static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
 };
@@ -214,7 +226,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   unsigned char* qbuf = dyn + kWarps * S::kRing + wid * S::kQ;
   float* join = reinterpret_cast<float*>(dyn + kWarps * (S::kRing + S::kQ));
   uint64_t* bars = reinterpret_cast<uint64_t*>(dyn + kWarps * (S::kRing + S::kQ) + S::kJoin);
-  int* word = reinterpret_cast<int*>(bars + kWarps * S::kStages);
+  CutTile* cut = reinterpret_cast<CutTile*>(bars + kWarps * S::kStages);      // [2]
   const uint32_t bar_s = smem_u32(bars + wid * S::kStages);
   const uint32_t tok = (uint32_t)a.H * a.D * 2;     // bytes from a token's row to the next
   if (kTma) {
@@ -313,6 +325,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   }
   int stage = 0;
   uint32_t par = 0;
+  int cuts = 0, was_first = 0, was_last = 0;      // (counts: thread 0's)
   bool bad = false;          // a wait ran out: the rest is done without waiting, and reported
 
   for (bool go = any; go; go = next_pair(C)) {
@@ -580,23 +593,38 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         }
       }
     }
-    if (!whole) {      // (the whole CTA: the pair is the same in all its warps)
+    if (!whole) {
       const Pieces ps = pieces_of(C.t, 0, a.lead, work.share);
+      const int n = C.w < C.end ? 0 : 1;      // a cut first tile, then the share's last
       if (wid == 0) {
-        __threadfence();
+        if (lane == 0) cut[n].t = C.t;
+        // the other lanes' sums, then the count: it is asked for here and looked at after the share,
+        // so that what it takes (some microseconds beside a cache read at full rate) is not waited for
         __syncwarp();
         if (lane == 0) {
-          int32_t* count = &a.arrived[(ps.first * a.H + head) * kArriveWords];
-          const int last = atomicAdd(count, 1) == ps.count - 1;
-          if (last) *count = 0;
-          __threadfence();
-          *word = last;
+          const int was = add_release(&a.arrived[(ps.first * a.H + head) * kArriveWords], 1);
+          if (n == 0) was_first = was;
+          else was_last = was;
         }
       }
-      __syncthreads();
-      if (*word) join_rows<DP, kBf16>(a, C.t, head, ps);
-      __syncthreads();
+      cuts |= 1 << n;
     }
+  }
+  if (cuts) {      // (the same in all warps)
+    if (threadIdx.x == 0) {
+      for (int n = 0; n < 2; ++n) {
+        if (!(cuts >> n & 1)) continue;
+        const Pieces ps = pieces_of(cut[n].t, 0, a.lead, work.share);
+        const bool last = (n == 0 ? was_first : was_last) == ps.count - 1;
+        if (last) a.arrived[(ps.first * a.H + head) * kArriveWords] = 0;
+        cut[n].last = last;
+      }
+      __threadfence();
+    }
+    __syncthreads();
+    for (int n = 0; n < 2; ++n)
+      if ((cuts >> n & 1) && cut[n].last)
+        join_rows<DP, kBf16>(a, cut[n].t, head, pieces_of(cut[n].t, 0, a.lead, work.share));
   }
   if (!kTma) copy_wait<0>();
   if (LV_RARE(bad)) {      // let what is on its way land before the shared memory is given up

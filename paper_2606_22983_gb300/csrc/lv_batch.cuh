@@ -141,7 +141,7 @@ cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CU
                                int ctas, cudaStream_t s);      // maps: boxes of 64 columns and a unit's keys, or null
 constexpr int kTcUnit = 128, kTcRows = 256;
 // places ahead of a pair's units: what a pair costs besides its units, in units
-constexpr int kRowsLead = 4, kTcLead = 2;
+constexpr int kRowsLead = 16, kTcLead = 2;
 // packed rows of a tile: two halves of whole tokens
 inline int tc_tile_rows(int G) { return G > 128 ? kTcRows : 2 * (128 / G * G); }
 struct TcMaps {
