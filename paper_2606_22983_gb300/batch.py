@@ -11,7 +11,7 @@ both -- whose room in the context a turn or ``KVPool.append`` has made:
 
 ``row_starts``, ``kv_lens``, ``tables``, ``positions`` and ``slots`` are device tensors that
 ``plan`` fills.  PyTorch holds the memory; every operation is a liblv call on the given stream (None:
-the current one).
+the pool's, or the current one).
 """
 from __future__ import annotations
 
@@ -23,6 +23,8 @@ import torch
 from . import lv
 from .pool import KVPool
 
+_KINDS = {torch.bfloat16: lv.LV_BF16, torch.float16: lv.LV_F16, torch.float32: lv.LV_F32}
+
 
 class KVBatch:
     """One kind of attention layer over ``pool``: ``q_heads`` query heads, and with ``window`` > 0 a
@@ -30,8 +32,7 @@ class KVBatch:
 
     def __init__(self, pool: KVPool, *, q_heads: int, max_requests: int, max_tokens: int,
                  dtype=torch.bfloat16, window: int = 0, sinks: int = 0):
-        kinds = {torch.bfloat16: lv.LV_BF16, torch.float16: lv.LV_F16}
-        if dtype not in kinds:
+        if dtype not in (torch.bfloat16, torch.float16):
             raise ValueError("dtype must be torch.bfloat16 or torch.float16")
         self.pool, self.q_heads, self.dtype = pool, q_heads, dtype
         self.max_requests, self.max_tokens = max_requests, max_tokens
@@ -47,8 +48,11 @@ class KVBatch:
             self.slots = torch.full((max(rows, 1),), -1, dtype=torch.int64, device=pool.device)
             # the library may write them on any stream next
             torch.cuda.current_stream().synchronize()
+        self._device = self.row_starts.get_device()
+        self._scale = 1.0 / math.sqrt(pool.head_dim)
+        self._a, self._b = lv.lv_heads(), lv.lv_heads()      # a call's two tensor arguments
         d = lv.lv_batch_desc(num_q_heads=q_heads, max_requests=max_requests, max_tokens=max_tokens,
-                             dtype=kinds[dtype], window=window, sinks=sinks,
+                             dtype=_KINDS[dtype], window=window, sinks=sinks,
                              row_starts=self.row_starts.data_ptr(), kv_lens=self.kv_lens.data_ptr(),
                              tables=self.tables.data_ptr(), positions=self.positions.data_ptr(),
                              slots=self.slots.data_ptr())
@@ -61,13 +65,11 @@ class KVBatch:
             self.handle = None
 
     def _ints(self, x, n=None):
-        """An int32 array the library can read: a device tensor as it is, else a numpy array."""
-        if x is None:
-            return None
+        """An int32 array the library can read: a tensor as it is, else a numpy array."""
         if isinstance(x, torch.Tensor):
-            if x.dtype != torch.int32 or not x.is_contiguous():
+            if x.dtype is not torch.int32 or not x.is_contiguous():
                 raise ValueError("expected a contiguous int32 tensor")
-            if x.is_cuda and x.device != self.pool.device:
+            if x.is_cuda and x.get_device() != self._device:
                 raise ValueError("expected a tensor on the pool's device")
         else:
             x = np.ascontiguousarray(x, dtype=np.int32)
@@ -81,11 +83,13 @@ class KVBatch:
         the step's tensors) has to be given, and ``max_len`` (a bound of the lengths) should be."""
         sids = self._ints(sids)
         n = len(sids)
-        lens, firsts = self._ints(lens, n), self._ints(firsts, n)
+        lens = self._ints(lens, n)
+        if firsts is not None:
+            firsts = self._ints(firsts, n)
         if isinstance(lens, torch.Tensor) and lens.is_cuda:
             if num_tokens is None:
                 raise ValueError("num_tokens is needed with lengths on the device")
-        else:
+        elif num_tokens is None or max_len is None:
             have = np.asarray(lens)
             num_tokens = int(have.sum()) if num_tokens is None else num_tokens
             max_len = int(have.max(initial=0)) if max_len is None else max_len
@@ -95,39 +99,48 @@ class KVBatch:
         self.pool.launches += 1
 
     def _stream(self, stream):
-        return self.pool.stream if stream is None else stream
+        if stream is None:
+            stream = self.pool.stream
+        return lv.stream_handle(stream, self._device)
 
-    def _tensor(self, x, heads, name):
-        if x.device != self.pool.device or x.dim() != 3 or x.shape[0] < self.num_tokens or \
-                x.shape[1] != heads or x.shape[2] != self.pool.head_dim:
-            raise ValueError(f"{name}: expected [{self.num_tokens}, {heads}, {self.pool.head_dim}] on "
-                             f"{self.pool.device}, got {tuple(x.shape)} on {x.device}")
-        return lv.heads(x)
+    def _put(self, h, x, heads, name):
+        """h describes tensor x, [rows, heads, head_dim] with head_dim contiguous."""
+        shape, (row, head, last) = x.shape, x.stride() if x.dim() == 3 else (0, 0, 0)
+        if len(shape) != 3 or shape[0] < self.num_tokens or shape[1] != heads or \
+                shape[2] != self.pool.head_dim or last != 1 or x.dtype not in _KINDS or \
+                x.get_device() != self._device:
+            raise ValueError(f"{name}: expected a bf16, f16 or f32 tensor [{self.num_tokens}, {heads}, "
+                             f"{self.pool.head_dim}] on {self.pool.device} with contiguous head_dim, got "
+                             f"{tuple(shape)} of {x.dtype} on {x.device}")
+        h.data, h.row_stride, h.head_stride, h.dtype = x.data_ptr(), row, head, _KINDS[x.dtype]
+        return h
 
     def write(self, layer: int, k, v, *, stream=None):
         """The step's new K and V rows ([rows, kv_heads, head_dim], any strides, bf16, f16 or f32)
         into their pages."""
         H = self.pool.kv_heads
-        lv.lv_kv_write(self.handle, layer, self._tensor(k, H, "k"), self._tensor(v, H, "v"),
+        lv.lv_kv_write(self.handle, layer, self._put(self._a, k, H, "k"), self._put(self._b, v, H, "v"),
                        self._stream(stream))
         self.pool.launches += 1
 
     def attention(self, layer: int, q, *, out=None, scale=None, return_lse=False, stream=None):
         """Attention of the step's rows over their paged contexts: [rows, q_heads, head_dim], and with
         ``return_lse`` the logarithms of the sums of exponentials [rows, q_heads] (f32).  Rows of
-        no request give zeros (and -inf).  scale: 1 / sqrt(head_dim) unless given."""
-        qh = self._tensor(q, self.q_heads, "q")
+        no request give zeros (and -inf).  scale: 1 / sqrt(head_dim) unless given.  With a stream
+        other than the current one, the caller orders the two."""
+        q_arg = self._put(self._a, q, self.q_heads, "q")
+        rows = q.shape[0]
+        past = rows - self.num_tokens            # rows that the step does not have
         if out is None:
-            out = torch.empty((q.shape[0], self.q_heads, self.pool.head_dim), dtype=self.dtype,
-                              device=q.device)
-            if q.shape[0] > self.num_tokens:
+            out = torch.empty_like(q, dtype=self.dtype, memory_format=torch.contiguous_format)
+            if past:
                 out[self.num_tokens:].zero_()
-        lse = torch.full((q.shape[0], self.q_heads), -math.inf, dtype=torch.float32, device=q.device) \
-            if return_lse and q.shape[0] > self.num_tokens else \
-            torch.empty((q.shape[0], self.q_heads), dtype=torch.float32, device=q.device) \
-            if return_lse else None
-        lv.lv_attention(self.handle, layer, qh, self._tensor(out, self.q_heads, "out"), lse,
-                        1.0 / math.sqrt(self.pool.head_dim) if scale is None else scale,
-                        self._stream(stream))
+        lse = None
+        if return_lse:
+            lse = torch.empty((rows, self.q_heads), dtype=torch.float32, device=q.device)
+            if past:
+                lse[self.num_tokens:].fill_(-math.inf)
+        lv.lv_attention(self.handle, layer, q_arg, self._put(self._b, out, self.q_heads, "out"), lse,
+                        self._scale if scale is None else scale, self._stream(stream))
         self.pool.launches += 1
         return (out, lse) if return_lse else out

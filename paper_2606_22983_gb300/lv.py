@@ -270,11 +270,23 @@ def ptr(x):
     raise TypeError(f"cannot pass {type(x).__name__} as an array argument")
 
 
-def stream_handle(stream):
-    """cudaStream_t of a torch stream (None: the current stream of the current device)."""
+_current_stream = False       # not looked for yet
+
+
+def stream_handle(stream, device=None):
+    """cudaStream_t of a torch stream (None: the current stream of the current device, or of
+    ``device``, its number)."""
     if stream is None:
+        global _current_stream
         import torch
-        stream = torch.cuda.current_stream()
+        if device is not None:
+            if _current_stream is False:
+                # torch's own way from a device's number to the handle, where it has one: it takes
+                # 0.2 us, a stream object 3 us, as long as a launch
+                _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            if _current_stream is not None:
+                return _current_stream(device)
+        stream = torch.cuda.current_stream(device)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -476,17 +488,6 @@ def lv_batch_destroy(batch, stream=None):
 def lv_batch_plan(batch, sids, firsts, lens, n, num_tokens, max_len, stream=None):
     _check(_lib.lv_batch_plan(batch, ptr(sids), ptr(firsts), ptr(lens), n, num_tokens, max_len,
                               stream_handle(stream)), "lv_batch_plan")
-
-
-def heads(x) -> lv_heads:
-    """The lv_heads of a torch tensor [rows][heads][head_dim] (the last dimension contiguous)."""
-    import torch
-    kinds = {torch.bfloat16: LV_BF16, torch.float16: LV_F16, torch.float32: LV_F32}
-    if x.dim() != 3 or x.dtype not in kinds or (x.shape[2] > 1 and x.stride(2) != 1):
-        raise ValueError("expected a [rows, heads, head_dim] tensor of bf16, f16 or f32 with "
-                         "contiguous head_dim")
-    return lv_heads(data=x.data_ptr(), row_stride=x.stride(0), head_stride=x.stride(1),
-                    dtype=kinds[x.dtype], reserved=0)
 
 
 def lv_kv_write(batch, layer, k: lv_heads, v: lv_heads, stream=None):
