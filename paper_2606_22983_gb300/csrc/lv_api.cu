@@ -1658,7 +1658,7 @@ struct lv_batch {
   // the planned step
   bool planned = false;
   int32_t num_tokens = 0;
-  lv::AttnKind kind = lv::ATTN_ROWS16;
+  lv::AttnKind kind = lv::ATTN_ROWS;
   int32_t ctas = 0;
 };
 
@@ -1747,10 +1747,10 @@ bool device_array(const lv_pool* pool, const void* p, size_t align) {
 }
 
 // Shares of a head's line in the rows kernel, whose CTAs are that many times H: what the SMs hold.
-int rows_shares(const lv_batch* b, bool wide) {
-  return std::max(1, b->pool->num_sms * lv::attend_rows_ctas(b->dp, wide) / b->pool->kv_heads);
+int rows_shares(const lv_batch* b) {
+  return std::max(1, b->pool->num_sms * lv::attend_rows_ctas(b->dp) / b->pool->kv_heads);
 }
-int rows_ctas(const lv_batch* b, bool wide) { return rows_shares(b, wide) * b->pool->kv_heads; }
+int rows_ctas(const lv_batch* b) { return rows_shares(b) * b->pool->kv_heads; }
 
 lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   const int H = pool->kv_heads, D = pool->head_dim;
@@ -1782,10 +1782,9 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   }
   if (lv::configure_attend() != cudaSuccess || lv::configure_attend_tc() != cudaSuccess) return fail(LV_ERR_CUDA);
   b->max_tiles = d->max_requests + (int32_t)(((long long)d->max_tokens * b->G + 15) / 16);
-  const int most = std::max({rows_ctas(b, false), rows_ctas(b, true), pool->num_sms});
+  const int most = std::max(rows_ctas(b), pool->num_sms);
   // rows of partial results: two slots a CTA
-  size_t rows = (size_t)2 * rows_ctas(b, false) * 16;
-  rows = std::max(rows, (size_t)2 * rows_ctas(b, true) * 32);
+  size_t rows = (size_t)2 * rows_ctas(b) * lv::kRowsRows;
   // (a warp joins 32 rows of a tile at a time, past its end where it has fewer)
   if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows + 32);
   try {
@@ -1864,9 +1863,10 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
       return r;
     if (firsts && (r = st.in(firsts, (size_t)n * 4, &fi, true)) != LV_OK) return r;
     max_len = std::min(max_len, num_tokens);
-    const long long rows = (long long)max_len * b->G;
-    b->kind = rows <= 16 ? lv::ATTN_ROWS16 : b->dp > 128 ? lv::ATTN_ROWS16
-              : rows <= 32 || !b->box_rows ? lv::ATTN_ROWS32 : lv::ATTN_TC;
+    // more rows a request than one m16n8k16 tile holds: the kernel for many rows, where pages can be
+    // read by TMA (32 sessions of 1000 to 4000 keys with 4 new tokens, 32 rows, took 42 us with it and
+    // 115 in tiles of 32 rows of the other; with 1 token, 8 rows, the other reads at 6 TB/s)
+    b->kind = (long long)max_len * b->G > lv::kRowsRows && b->box_rows ? lv::ATTN_TC : lv::ATTN_ROWS;
     b->num_tokens = num_tokens;
     lv::PlanArgs a{};
     a.p = pool->d;
@@ -1886,12 +1886,12 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
       b->ctas = a.shares = pool->num_sms;
     } else {
       a.line_heads = 1;
-      a.tile_rows = b->kind == lv::ATTN_ROWS32 ? 32 : 16;
+      a.tile_rows = lv::kRowsRows;
       a.unit = lv::kRowsUnit;
       a.lead = lv::kRowsLead;
-      a.min_share = 4;
-      a.shares = rows_shares(b, b->kind == lv::ATTN_ROWS32);
-      b->ctas = rows_ctas(b, b->kind == lv::ATTN_ROWS32);
+      a.min_share = 32;
+      a.shares = rows_shares(b);
+      b->ctas = rows_ctas(b);
     }
     a.ctas = b->ctas;
     a.window = b->d.window;
@@ -1982,8 +1982,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.num_tokens = b->num_tokens;
   a.window = b->d.window;
   a.sinks = b->d.sinks;
-  a.tile_rows = tc ? lv::tc_tile_rows(b->G) : b->kind == lv::ATTN_ROWS32 ? 32 : 16;
-  a.lead = tc ? lv::kTcLead : lv::kRowsLead;
+  a.tile_rows = tc ? lv::tc_tile_rows(b->G) : lv::kRowsRows;
   a.dp = b->dp;
   a.scale = scale * 1.44269504088896341f;
   a.part_o = b->part_o;
@@ -1996,7 +1995,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
     LV_TRY(lv::launch_attend_tc(a, m, bf16, b->ctas, s));
   } else {
     const CUtensorMap* m = b->rows_maps.empty() ? nullptr : &b->rows_maps[2 * layer];
-    LV_TRY(lv::launch_attend_rows(a, m, m ? m + 1 : nullptr, b->kind == lv::ATTN_ROWS32, bf16, b->ctas, s));
+    LV_TRY(lv::launch_attend_rows(a, m, m ? m + 1 : nullptr, bf16, b->ctas, s));
   }
   return LV_OK;
 }

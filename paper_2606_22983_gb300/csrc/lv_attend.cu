@@ -123,58 +123,60 @@ struct CutTile {
   int last, pad[3];        // this CTA's was its last piece to arrive
 };
 
-template <int DP, int MT>
+template <int DP>
 struct RowsShape {
-  static constexpr int kM = 16 * MT;
   static constexpr int kStages = DP == 64 ? 4 : 2;
-  static constexpr int kCtas = DP == 256 ? 1 : MT == 1 ? 3 : 2;      // in an SM: 228 KiB, 64 K registers
-  static constexpr int kHalves = DP / 64;                    // 64 columns, 128 bytes, wide
+  static constexpr int kCtas = DP == 256 ? 1 : 3;            // in an SM: 228 KiB, 64 K registers
+  static constexpr int kBlocks = DP / 64;                    // of 64 columns, 128 bytes
   static constexpr int kTile = kU * DP * 2;                  // bytes of a unit's K (or V) in a stage
   static constexpr int kRing = kStages * 2 * kTile;          // of a warp
-  static constexpr bool kQInRegs = MT * DP <= 128;
-  static constexpr int kQ = kQInRegs ? 0 : kM * DP * 2;      // a warp's queries
-  static constexpr int kJoin = kM * DP * 4 + kM * 8;         // what a warp hands over: sums; maxima and weights
+  static constexpr int kJoin = kRowsRows * (DP * 4 + 8);     // what a warp hands over: sums; maxima and weights
   static constexpr int kBars = 8 * kWarps * kStages + 2 * (int)sizeof(CutTile);      // a barrier a stage and warp
-  static constexpr int kSmem = kWarps * (kRing + kQ) + kJoin + kBars;
+  static constexpr int kSmem = kWarps * kRing + kJoin + kBars;
   static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
 };
 
-// The join of a cut pair by a CTA, a warp a row: every piece's sums weighted by its maximum against
-// the largest, in the pieces' order.
-template <int DP, bool kBf16>
-__device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, int head, const Pieces& ps) {
+// Pieces p0, p0 + step, ... (count of them) of a cut pair joined by a CTA, a warp a row: every piece's
+// sums weighted by its maximum against the largest, in the pieces' order.  To the output, or
+// (not kLast) to the first of the pieces' own slots.
+template <int DP, bool kBf16, bool kLast>
+__device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, int head, int64_t first, int p0,
+                                          int step, int count) {
   const int lane = threadIdx.x & 31;
   constexpr int kCols = DP / 32;
   constexpr int kBatch = 8;
   for (int row = threadIdx.x >> 5; row < t.rows; row += kWarps) {
-    auto at = [&](int p) { return part_slot((ps.first + p) * a.H + head, p == 0) * a.tile_rows + row; };
+    auto at = [&](int i) {
+      const int p = p0 + i * step;
+      return part_slot((first + p) * a.H + head, p == 0) * kRowsRows + row;
+    };
     float top = -INFINITY;
-    for (int p = lane; p < ps.count; p += 32) top = fmaxf(top, __ldcg(&a.part_ml[at(p)]).x);
+    for (int i = lane; i < count; i += 32) top = fmaxf(top, __ldcg(&a.part_ml[at(i)]).x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     float sum = 0.f, acc[kCols];
 #pragma unroll
     for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
-    for (int p0 = 0; p0 < ps.count; p0 += 32) {
+    for (int i0 = 0; i0 < count; i0 += 32) {
       float f = 0.f;
-      if (p0 + lane < ps.count) {
-        const float2 ml = __ldcg(&a.part_ml[at(p0 + lane)]);
+      if (i0 + lane < count) {
+        const float2 ml = __ldcg(&a.part_ml[at(i0 + lane)]);
         f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
         sum += ml.y * f;
       }
-      for (int p = p0; p < min(p0 + 32, ps.count); p += kBatch) {
+      for (int i = i0; i < min(i0 + 32, count); i += kBatch) {
         float v[kBatch][kCols];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const float* o = a.part_o + at(min(p + b, ps.count - 1)) * DP + kCols * lane;
+          const float* o = a.part_o + at(min(i + b, count - 1)) * DP + kCols * lane;
 #pragma unroll
           for (int e = 0; e < kCols; e += 2)
             *reinterpret_cast<float2*>(&v[b][e]) = __ldcg(reinterpret_cast<const float2*>(o + e));
         }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const float g = __shfl_sync(0xffffffffu, f, (p - p0 + b) & 31);
-          if (p + b < ps.count) {
+          const float g = __shfl_sync(0xffffffffu, f, (i - i0 + b) & 31);
+          if (i + b < count) {
 #pragma unroll
             for (int e = 0; e < kCols; ++e) acc[e] += v[b][e] * g;
           }
@@ -183,6 +185,13 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if constexpr (!kLast) {
+      float* o = a.part_o + at(0) * DP + kCols * lane;
+#pragma unroll
+      for (int e = 0; e < kCols; e += 2) *reinterpret_cast<float2*>(o + e) = make_float2(acc[e], acc[e + 1]);
+      if (lane == 0) a.part_ml[at(0)] = make_float2(top, sum);
+      continue;
+    }
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     const int R = t.row0 + row, token = R / a.G, g = R - token * a.G;
     const int64_t r = t.qrow + token;
@@ -206,6 +215,11 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
   }
 }
 
+// A pair of more pieces than this is joined in two steps, groups of kGroup pieces first: the last CTA
+// of a group joins the group, the last of those the groups (one CTA alone took some 25 us for the
+// 114 pieces of a context of 60 000 keys).
+constexpr int kGroup = 12;
+
 // One CTA: its share of one KV head's line.  Its four warps take a tile's units in turn and are joined at the
 // tile's end; each streams its units' K and V rows through a ring of its own, so no barrier of the
 // CTA lies in the loop.  S = Q K^T (16 rows x 16 keys a step), the running maximum and sum of the
@@ -215,17 +229,16 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
 // kTma: a unit's K and V come by TMA, a box of 16 keys and 64 columns each, where pages hold whole
 // units (T a multiple of 16); else by 16-byte copies, a key at a time from its page.  In shared
 // memory a unit is [64-column block][key][128 bytes], swizzled as TMA does it.
-template <int DP, int MT, bool kBf16, bool kTma>
-__global__ void __launch_bounds__(kThreads, RowsShape<DP, MT>::kCtas)
+template <int DP, bool kBf16, bool kTma>
+__global__ void __launch_bounds__(kThreads, RowsShape<DP>::kCtas)
 k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap kmap,
               const __grid_constant__ CUtensorMap vmap) {
-  using S = RowsShape<DP, MT>;
+  using S = RowsShape<DP>;
   extern __shared__ __align__(1024) unsigned char dyn[];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const uint32_t ring_s = smem_u32(dyn) + wid * S::kRing;
-  unsigned char* qbuf = dyn + kWarps * S::kRing + wid * S::kQ;
-  float* join = reinterpret_cast<float*>(dyn + kWarps * (S::kRing + S::kQ));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(dyn + kWarps * (S::kRing + S::kQ) + S::kJoin);
+  float* join = reinterpret_cast<float*>(dyn + kWarps * S::kRing);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(dyn + kWarps * S::kRing + S::kJoin);
   CutTile* cut = reinterpret_cast<CutTile*>(bars + kWarps * S::kStages);      // [2]
   const uint32_t bar_s = smem_u32(bars + wid * S::kStages);
   const uint32_t tok = (uint32_t)a.H * a.D * 2;     // bytes from a token's row to the next
@@ -238,6 +251,8 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   dep_wait();
   dep_trigger();
 
+  const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
+  const CtaWork work = load_words(&a.work[group]);
   auto key_of = [&](const AttnTile& t, int u) { return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kU; };
   auto hidden = [&](const AttnTile& t, int key) { return key >= t.kv_hi || (key < t.kv_lo && key >= a.sinks); };
   auto find_page = [&](Walk& x) {
@@ -246,15 +261,16 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   };
   auto next_pair = [&](Walk& x) -> bool {
     while (x.w < x.end) {
-      const int len = x.t.units + a.lead;
+      const int len = stretch_of(x.t.units, work.lead, work.share);
       if (x.w >= x.t.before + len) {
         x.t = load_words(&a.tiles[++x.tile]);
         continue;
       }
       const int o0 = (int)(x.w - x.t.before), o1 = (int)min((int64_t)len, o0 + (x.end - x.w));
       x.w += o1 - o0;
-      x.u_begin = max(o0 - a.lead, 0);
-      x.u_end = o1 - a.lead;
+      const int2 in = units_of(o0, o1, x.t.units, work.lead);
+      x.u_begin = in.x;
+      x.u_end = in.y;
       x.u = x.u_begin + wid;
       if (x.u_end > x.u_begin) {
         find_page(x);
@@ -264,8 +280,6 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     return false;
   };
   Walk L;
-  const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
-  const CtaWork work = load_words(&a.work[group]);
   L.w = work.begin;
   L.end = work.end;
   L.t = work.t;
@@ -287,7 +301,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_s + 8 * s), "r"(2 * S::kTile)
                      : "memory");
 #pragma unroll
-        for (int x = 0; x < S::kHalves; ++x) {
+        for (int x = 0; x < S::kBlocks; ++x) {
           tma_box(dst + x * kU * 128, &kmap, 64 * x, head, off, page, bar_s + 8 * s);
           tma_box(dst + S::kTile + x * kU * 128, &vmap, 64 * x, head, off, page, bar_s + 8 * s);
         }
@@ -330,52 +344,33 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 
   for (bool go = any; go; go = next_pair(C)) {
     // ---- queries of this pair's head: packed rows lane / 4 + 8 i
-    int pos[2 * MT];
-    uint32_t qr[S::kQInRegs ? MT : 1][S::kQInRegs ? DP / 16 : 1][4];
+    int pos[2];
+    uint32_t qr[DP / 16][4];
     const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q);
-    auto q_row = [&](int row) -> const uint16_t* {
-      const int R = C.t.row0 + row, token = R / a.G, g = R - token * a.G;
-      return q + (C.t.qrow + token) * a.q_row + (int64_t)(head * a.G + g) * a.q_head;
-    };
-    auto q_at = [&](const uint16_t* x, int row, int d) -> uint32_t {     // two elements, zeros past the rows and columns
-      if (row >= C.t.rows || d >= a.D) return 0u;
-      if (a.q_vec) return *reinterpret_cast<const uint32_t*>(x + d);
-      return (uint32_t)x[d] | (uint32_t)x[d + 1] << 16;
-    };
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) pos[i] = C.t.first + (C.t.row0 + min(lane / 4 + 8 * i, C.t.rows - 1)) / a.G;
-    if constexpr (S::kQInRegs) {
+    for (int i = 0; i < 2; ++i) {
+      const int row = lane / 4 + 8 * i, R = C.t.row0 + min(row, C.t.rows - 1), token = R / a.G;
+      pos[i] = C.t.first + token;
+      const uint16_t* x = q + (C.t.qrow + token) * a.q_row + (int64_t)(head * a.G + (R - token * a.G)) * a.q_head;
+      auto two = [&](int d) -> uint32_t {      // elements d, d + 1; zeros past the rows and columns
+        if (row >= C.t.rows || d >= a.D) return 0u;
+        if (a.q_vec) return *reinterpret_cast<const uint32_t*>(x + d);
+        return (uint32_t)x[d] | (uint32_t)x[d + 1] << 16;
+      };
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const int row = 16 * m + lane / 4 + 8 * hf;
-          const uint16_t* x = q_row(row);
-#pragma unroll
-          for (int k = 0; k < DP / 16; ++k) {
-            qr[m][k][hf] = q_at(x, row, 16 * k + 2 * (lane & 3));
-            qr[m][k][hf + 2] = q_at(x, row, 16 * k + 2 * (lane & 3) + 8);
-          }
-        }
-    } else {
-      __syncwarp();
-      for (int i = lane; i < S::kM * DP / 2; i += 32) {
-        const int row = i / (DP / 2), d = 2 * (i % (DP / 2));
-        *reinterpret_cast<uint32_t*>(qbuf + row * DP * 2 + (((d >> 3) ^ (row & 7)) << 4) + (d & 7) * 2) =
-            q_at(q_row(row), row, d);
+      for (int k = 0; k < DP / 16; ++k) {
+        qr[k][i] = two(16 * k + 2 * (lane & 3));
+        qr[k][i + 2] = two(16 * k + 2 * (lane & 3) + 8);
       }
-      __syncwarp();
     }
-    float o[MT][DP / 8][4];
-    float top[2 * MT], sum[2 * MT];      // per row: maximum in log2 (the scale folded in), the lane's weights
+    float o[DP / 8][4];
+    float top[2], sum[2];      // per row: maximum in log2 (the scale folded in), the lane's weights
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
-      for (int n = 0; n < DP / 8; ++n)
+      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[m][n][e] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) top[i] = -INFINITY, sum[i] = 0.f;
+    for (int i = 0; i < 2; ++i) top[i] = -INFINITY, sum[i] = 0.f;
     const int p_lo = C.t.first + C.t.row0 / a.G, p_hi = C.t.kv_hi - 1;
 
 #pragma unroll 1
@@ -401,7 +396,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
           for (int i = lane; i < kU * 8; i += 32)
             if (hidden(C.t, key0 + i / 8)) {
 #pragma unroll
-              for (int x = 0; x < S::kHalves; ++x)
+              for (int x = 0; x < S::kBlocks; ++x)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vs + x * kU * 128 + i * 16), "r"(0)
                              : "memory");
             }
@@ -420,11 +415,9 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         stage = 0;
         par ^= 1;
       }
-      float s[MT][2][4];
+      float s[2][4];
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[m][0][e] = s[m][1][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[0][e] = s[1][e] = 0.f;
       {
         const int key = (lane & 7) + ((lane >> 4) << 3), half = (lane >> 3) & 1;
         const uint32_t row = ks + key * 128;
@@ -432,41 +425,27 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         for (int k = 0; k < DP / 16; ++k) {
           uint32_t b[4];
           ldsm4(b, row + (k >> 2) * kU * 128 + (((2 * (k & 3) + half) ^ (key & 7)) << 4));
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            uint32_t qa[4];
-            if constexpr (S::kQInRegs) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) qa[e] = qr[m][k][e];
-            } else {
-              const int r = 16 * m + (lane & 15);
-              ldsm4(qa, smem_u32(qbuf) + r * DP * 2 + (((2 * k + (lane >> 4)) ^ (r & 7)) << 4));
-            }
-            mma<kBf16>(s[m][0], qa, b[0], b[1]);
-            mma<kBf16>(s[m][1], qa, b[2], b[3]);
-          }
+          mma<kBf16>(s[0], qr[k], b[0], b[1]);
+          mma<kBf16>(s[1], qr[k], b[2], b[3]);
         }
       }
       const bool open = key0 + kU - 1 <= p_lo && (a.window == 0 || key0 > p_hi - a.window || key0 + kU <= a.sinks);
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[m][n][e] *= a.scale;
-            if (!open) {
-              const int key = key0 + 8 * n + 2 * (lane & 3) + (e & 1), p = pos[2 * m + (e >> 1)];
-              const bool seen = key <= p && (a.window == 0 || key > p - a.window || key < a.sinks);
-              if (!seen) s[m][n][e] = -INFINITY;
-            }
+        for (int e = 0; e < 4; ++e) {
+          s[n][e] *= a.scale;
+          if (!open) {
+            const int key = key0 + 8 * n + 2 * (lane & 3) + (e & 1), p = pos[e >> 1];
+            const bool seen = key <= p && (a.window == 0 || key > p - a.window || key < a.sinks);
+            if (!seen) s[n][e] = -INFINITY;
           }
-      float top_new[2 * MT];
+        }
+      float top_new[2];
       bool raise = false;
 #pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) {
-        const int m = i >> 1, e = 2 * (i & 1);
-        float x = fmaxf(fmaxf(s[m][0][e], s[m][0][e + 1]), fmaxf(s[m][1][e], s[m][1][e + 1]));
+      for (int i = 0; i < 2; ++i) {
+        float x = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
         top_new[i] = fmaxf(x, top[i]);
@@ -474,30 +453,27 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
+        for (int i = 0; i < 2; ++i) {
           const float f = top_new[i] == top[i] ? 1.f : exp2_fast(top[i] - top_new[i]);
           top[i] = top_new[i];
           sum[i] *= f;
 #pragma unroll
           for (int n = 0; n < DP / 8; ++n) {
-            o[i >> 1][n][2 * (i & 1)] *= f;
-            o[i >> 1][n][2 * (i & 1) + 1] *= f;
+            o[n][2 * i] *= f;
+            o[n][2 * i + 1] *= f;
           }
         }
       }
-      uint32_t pa[MT][4];
+      uint32_t pa[4];
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const int i = 2 * m + hf;
-            const float at = (top[i] == -INFINITY ? 0.f : top[i]) - weight_bias<kBf16>();
-            const float x = exp2_fast(s[m][n][2 * hf] - at), y = exp2_fast(s[m][n][2 * hf + 1] - at);
-            sum[i] += x + y;
-            pa[m][2 * n + hf] = pack16<kBf16>(x, y);
-          }
+        for (int i = 0; i < 2; ++i) {
+          const float at = (top[i] == -INFINITY ? 0.f : top[i]) - weight_bias<kBf16>();
+          const float x = exp2_fast(s[n][2 * i] - at), y = exp2_fast(s[n][2 * i + 1] - at);
+          sum[i] += x + y;
+          pa[2 * n + i] = pack16<kBf16>(x, y);
+        }
       {
         const int key = (lane & 7) + (((lane >> 3) & 1) << 3);
         const uint32_t row = vs + key * 128;
@@ -505,17 +481,14 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         for (int d = 0; d < DP / 16; ++d) {
           uint32_t b[4];
           ldsm4t(b, row + (d >> 2) * kU * 128 + (((2 * (d & 3) + (lane >> 4)) ^ (key & 7)) << 4));
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            mma<kBf16>(o[m][2 * d], pa[m], b[0], b[1]);
-            mma<kBf16>(o[m][2 * d + 1], pa[m], b[2], b[3]);
-          }
+          mma<kBf16>(o[2 * d], pa, b[0], b[1]);
+          mma<kBf16>(o[2 * d + 1], pa, b[2], b[3]);
         }
       }
       __syncwarp();
     }
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
+    for (int i = 0; i < 2; ++i) {
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
     }
@@ -524,24 +497,22 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 #pragma unroll 1
     for (int n = 1; n < have; ++n) {
       float* box = join + lane;
-      float2* ml = reinterpret_cast<float2*>(join + S::kM * DP) + lane / 4;
+      float2* ml = reinterpret_cast<float2*>(join + kRowsRows * DP) + lane / 4;
       __syncthreads();
       if (wid == n) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
-          for (int d = 0; d < DP / 8; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) box[((m * (DP / 8) + d) * 4 + e) * 32] = o[m][d][e];
+          for (int e = 0; e < 4; ++e) box[(d * 4 + e) * 32] = o[d][e];
         if ((lane & 3) == 0) {
 #pragma unroll
-          for (int i = 0; i < 2 * MT; ++i) ml[8 * i] = make_float2(top[i], sum[i]);
+          for (int i = 0; i < 2; ++i) ml[8 * i] = make_float2(top[i], sum[i]);
         }
       }
       __syncthreads();
       if (wid == 0) {
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
+        for (int i = 0; i < 2; ++i) {
           const float2 x = ml[8 * i];
           const float t = fmaxf(top[i], x.x);
           const float f = top[i] == t ? 1.f : exp2_fast(top[i] - t), f2 = x.x == t ? 1.f : exp2_fast(x.x - t);
@@ -550,8 +521,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 #pragma unroll
           for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
-            for (int e = 2 * (i & 1); e < 2 * (i & 1) + 2; ++e)
-              o[i >> 1][d][e] = o[i >> 1][d][e] * f + box[(((i >> 1) * (DP / 8) + d) * 4 + e) * 32] * f2;
+            for (int e = 2 * i; e < 2 * i + 2; ++e) o[d][e] = o[d][e] * f + box[(d * 4 + e) * 32] * f2;
         }
       }
     }
@@ -559,7 +529,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     if (wid == 0) {
       const int64_t slot = part_slot(blockIdx.x, C.u_begin == 0);
 #pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) {
+      for (int i = 0; i < 2; ++i) {
         const int row = lane / 4 + 8 * i;
         if (row >= C.t.rows) continue;
         if (whole) {
@@ -572,7 +542,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
           for (int d = 0; d < DP / 8; ++d) {
             const int col = 8 * d + 2 * (lane & 3);
             if (col >= a.D) break;
-            const uint32_t w = pack16<kBf16>(o[i >> 1][d][2 * (i & 1)] * inv, o[i >> 1][d][2 * (i & 1) + 1] * inv);
+            const uint32_t w = pack16<kBf16>(o[d][2 * i] * inv, o[d][2 * i + 1] * inv);
             if (a.o_vec) {
               *reinterpret_cast<uint32_t*>(out + col) = w;
             } else {
@@ -584,17 +554,16 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
             a.lse[r * (a.H * a.G) + h] =
                 sum[i] == 0.f ? -INFINITY : (top[i] - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum[i]);
         } else {
-          float* po = a.part_o + (slot * a.tile_rows + row) * DP;
+          float* po = a.part_o + (slot * kRowsRows + row) * DP;
 #pragma unroll
           for (int d = 0; d < DP / 8; ++d)
-            *reinterpret_cast<float2*>(po + 8 * d + 2 * (lane & 3)) =
-                make_float2(o[i >> 1][d][2 * (i & 1)], o[i >> 1][d][2 * (i & 1) + 1]);
-          if ((lane & 3) == 0) a.part_ml[slot * a.tile_rows + row] = make_float2(top[i], sum[i]);
+            *reinterpret_cast<float2*>(po + 8 * d + 2 * (lane & 3)) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
+          if ((lane & 3) == 0) a.part_ml[slot * kRowsRows + row] = make_float2(top[i], sum[i]);
         }
       }
     }
     if (!whole) {
-      const Pieces ps = pieces_of(C.t, 0, a.lead, work.share);
+      const Pieces ps = pieces_of(C.t, 0, work.lead, work.share);
       const int n = C.w < C.end ? 0 : 1;      // a cut first tile, then the share's last
       if (wid == 0) {
         if (lane == 0) cut[n].t = C.t;
@@ -602,7 +571,9 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         // so that what it takes (some microseconds beside a cache read at full rate) is not waited for
         __syncwarp();
         if (lane == 0) {
-          const int was = add_release(&a.arrived[(ps.first * a.H + head) * kArriveWords], 1);
+          const int p = (int)(group - ps.first);
+          const int64_t of = ps.first + (ps.count > kGroup ? p / kGroup * kGroup : 0);
+          const int was = add_release(&a.arrived[(of * a.H + head) * kArriveWords + (ps.count > kGroup)], 1);
           if (n == 0) was_first = was;
           else was_last = was;
         }
@@ -610,21 +581,41 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       cuts |= 1 << n;
     }
   }
-  if (cuts) {      // (the same in all warps)
-    if (threadIdx.x == 0) {
-      for (int n = 0; n < 2; ++n) {
-        if (!(cuts >> n & 1)) continue;
-        const Pieces ps = pieces_of(cut[n].t, 0, a.lead, work.share);
-        const bool last = (n == 0 ? was_first : was_last) == ps.count - 1;
-        if (last) a.arrived[(ps.first * a.H + head) * kArriveWords] = 0;
-        cut[n].last = last;
-      }
-      __threadfence();
-    }
+  if (cuts) {
     __syncthreads();
-    for (int n = 0; n < 2; ++n)
-      if ((cuts >> n & 1) && cut[n].last)
-        join_rows<DP, kBf16>(a, cut[n].t, head, pieces_of(cut[n].t, 0, a.lead, work.share));
+#pragma unroll 1
+    for (int n = 0; n < 2; ++n) {
+      if (!(cuts >> n & 1)) continue;
+      const AttnTile t = cut[n].t;
+      const Pieces ps = pieces_of(t, 0, work.lead, work.share);
+      const int p = (int)(group - ps.first), g0 = p / kGroup * kGroup, g_count = min(kGroup, ps.count - g0);
+      const bool grouped = ps.count > kGroup;
+      // true in the whole CTA when its piece (or its group) was the last to arrive
+      auto last = [&](int was, int of, int count, int word) {
+        if (threadIdx.x == 0) {
+          const bool yes = was == count - 1;
+          if (yes) a.arrived[((ps.first + of) * a.H + head) * kArriveWords + word] = 0;
+          cut[n].last = yes;
+          __threadfence();
+        }
+        __syncthreads();
+        const bool yes = cut[n].last;
+        __syncthreads();
+        return yes;
+      };
+      const int was = n == 0 ? was_first : was_last;
+      if (!grouped) {
+        if (last(was, 0, ps.count, 0)) join_rows<DP, kBf16, true>(a, t, head, ps.first, 0, 1, ps.count);
+        continue;
+      }
+      if (!last(was, g0, g_count, 1)) continue;
+      join_rows<DP, kBf16, false>(a, t, head, ps.first, g0, 1, g_count);
+      const int groups = (ps.count + kGroup - 1) / kGroup;
+      __syncthreads();
+      int was2 = 0;
+      if (threadIdx.x == 0) was2 = add_release(&a.arrived[(ps.first * a.H + head) * kArriveWords], 1);
+      if (last(was2, 0, groups, 0)) join_rows<DP, kBf16, true>(a, t, head, ps.first, 0, kGroup, groups);
+    }
   }
   if (!kTma) copy_wait<0>();
   if (LV_RARE(bad)) {      // let what is on its way land before the shared memory is given up
@@ -638,10 +629,10 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   if (work.dead > 0) clear_dead(a, blockIdx.x * kThreads + threadIdx.x, gridDim.x * kThreads);
 }
 
-template <int DP, int MT, bool kTma>
+template <int DP, bool kTma>
 cudaError_t set_rows() {
-  for (auto k : {k_attend_rows<DP, MT, true, kTma>, k_attend_rows<DP, MT, false, kTma>}) {
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP, MT>::kSmem);
+  for (auto k : {k_attend_rows<DP, true, kTma>, k_attend_rows<DP, false, kTma>}) {
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP>::kSmem);
     // (the default split leaves room for one CTA)
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
@@ -650,38 +641,30 @@ cudaError_t set_rows() {
   return cudaSuccess;
 }
 
-template <int DP, int MT, bool kTma>
+template <int DP, bool kTma>
 cudaError_t run_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16, int ctas, cudaStream_t s) {
   static const CUtensorMap none{};
-  return launch_dependent(bf16 ? k_attend_rows<DP, MT, true, kTma> : k_attend_rows<DP, MT, false, kTma>, dim3(ctas),
-                          kThreads, RowsShape<DP, MT>::kSmem, s, a, k ? *k : none, v ? *v : none);
+  return launch_dependent(bf16 ? k_attend_rows<DP, true, kTma> : k_attend_rows<DP, false, kTma>, dim3(ctas), kThreads,
+                          RowsShape<DP>::kSmem, s, a, k ? *k : none, v ? *v : none);
 }
 
 }  // namespace
 
 cudaError_t configure_attend() {
-  for (cudaError_t e : {set_rows<64, 1, true>(), set_rows<64, 2, true>(), set_rows<128, 1, true>(),
-                        set_rows<128, 2, true>(), set_rows<64, 1, false>(), set_rows<64, 2, false>(),
-                        set_rows<128, 1, false>(), set_rows<128, 2, false>(), set_rows<256, 1, false>()})
+  for (cudaError_t e : {set_rows<64, true>(), set_rows<128, true>(), set_rows<64, false>(), set_rows<128, false>(),
+                        set_rows<256, false>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }
 
 // CTAs of the kernel that an SM holds
-int attend_rows_ctas(int dp, bool wide) {
-  if (dp == 256) return RowsShape<256, 1>::kCtas;
-  return wide ? RowsShape<128, 2>::kCtas : RowsShape<128, 1>::kCtas;
-}
+int attend_rows_ctas(int dp) { return dp == 256 ? RowsShape<256>::kCtas : RowsShape<128>::kCtas; }
 
-cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool wide, bool bf16,
-                               int ctas, cudaStream_t s) {
-  if (a.dp == 256) return run_rows<256, 1, false>(a, k, v, bf16, ctas, s);
-  if (a.dp == 64) {
-    if (k) return wide ? run_rows<64, 2, true>(a, k, v, bf16, ctas, s) : run_rows<64, 1, true>(a, k, v, bf16, ctas, s);
-    return wide ? run_rows<64, 2, false>(a, k, v, bf16, ctas, s) : run_rows<64, 1, false>(a, k, v, bf16, ctas, s);
-  }
-  if (k) return wide ? run_rows<128, 2, true>(a, k, v, bf16, ctas, s) : run_rows<128, 1, true>(a, k, v, bf16, ctas, s);
-  return wide ? run_rows<128, 2, false>(a, k, v, bf16, ctas, s) : run_rows<128, 1, false>(a, k, v, bf16, ctas, s);
+cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16, int ctas,
+                               cudaStream_t s) {
+  if (a.dp == 256) return run_rows<256, false>(a, k, v, bf16, ctas, s);
+  if (a.dp == 64) return k ? run_rows<64, true>(a, k, v, bf16, ctas, s) : run_rows<64, false>(a, k, v, bf16, ctas, s);
+  return k ? run_rows<128, true>(a, k, v, bf16, ctas, s) : run_rows<128, false>(a, k, v, bf16, ctas, s);
 }
 
 }  // namespace lv

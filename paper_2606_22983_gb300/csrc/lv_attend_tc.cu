@@ -279,7 +279,8 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Pieces& ps, i
 
 // The pairs (tile, head) of a CTA's share, one after the other.
 struct Pairs {
-  long long w, end, share;
+  long long w, end;
+  int share, lead;
   AttnTile t;
   int tile, head, u0, u1;
   int dead;
@@ -288,20 +289,22 @@ struct Pairs {
     w = x.begin;
     end = x.end;
     share = x.share;
+    lead = x.lead;
     t = x.t;
     tile = x.tile;
     dead = x.dead;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a) {
     while (w < end) {
-      if (w >= t.before + (long long)(t.units + a.lead) * a.H) t = load_words(&a.tiles[++tile]);
-      const int len = t.units + a.lead;
+      if (w >= t.before + (long long)stretch_of(t.units, lead, share) * a.H) t = load_words(&a.tiles[++tile]);
+      const int len = stretch_of(t.units, lead, share);
       const long long off = w - t.before;
       head = (int)(off / len);
       const int o0 = (int)(off - (long long)head * len), o1 = (int)min((long long)len, o0 + (end - w));
       w += o1 - o0;
-      u0 = max(o0 - a.lead, 0);
-      u1 = o1 - a.lead;
+      const int2 u = units_of(o0, o1, t.units, lead);
+      u0 = u.x;
+      u1 = u.y;
       if (u1 > u0) return true;
     }
     return false;
@@ -604,7 +607,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
         __threadfence();
         __syncwarp();
-        const Pieces ps = pieces_of(pr.t, pr.head, a.lead, pr.share);
+        const Pieces ps = pieces_of(pr.t, pr.head, pr.lead, pr.share);
         int32_t* count = &a.arrived[ps.first * kArriveWords + wid];
         int before = 0;
         if (lane == 0) before = atomicAdd(count, 1);

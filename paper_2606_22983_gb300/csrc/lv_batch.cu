@@ -10,6 +10,7 @@ namespace lv {
 namespace {
 
 constexpr int kPlanThreads = 256;
+constexpr long long kManyShares = 1 << 20;   // more than there are CTAs
 constexpr int kMaxRequests = 4096;      // lv_batch_create's limit
 
 // Sum over the CTA, to every thread.  ws: one word a warp; a barrier lies between its uses.
@@ -170,7 +171,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
   live = cta_sum(live, ws);
   const int n_tiles = (int)min(tiles, (long long)a.max_tiles);
   // the tiles, a thread each (its request found by bisection), and where they lie on the line
-  long long units = 0;
+  long long units = 0, padded = 0;
   for (int base = 0; base < n_tiles; base += kPlanThreads) {
     const int t = base + threadIdx.x;
     AttnTile tile{};
@@ -185,27 +186,37 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
       tile = make_tile(a, PlanReq{r.x, r.y, r.z, 0}, lo, t - first_tile[lo]);
     }
     long long total;
-    const long long at = cta_scan(t < n_tiles ? tile.units + a.lead : 0, ws, &total);
+    const long long at = cta_scan(t < n_tiles ? tile.units : 0, ws, &total);
+    long long total_padded;
+    const long long at_padded =
+        cta_scan(t < n_tiles ? (tile.units + a.min_share - 1) / a.min_share : 0, ws, &total_padded);
     if (t < n_tiles) {
-      tile.before = (units + at) * a.line_heads;
+      // what comes before it, in units and (above bit 40) in shares of min_share
+      tile.before = units + at + (min(padded + at_padded, kManyShares) << 40);
       a.tiles[t] = tile;
     }
     units += total;
+    padded += total_padded;
   }
-  units *= a.line_heads;
-  const long long share = max((units + a.shares - 1) / a.shares, (long long)a.min_share);
+  const bool apart = padded * a.line_heads <= a.shares;
+  const int lead = apart ? -1 : a.lead;
+  units = apart ? padded * a.min_share * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
+  const long long share = apart ? a.min_share : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
   const int dead = a.num_tokens - (int)live;
   if (threadIdx.x == 0) a.head->ticket = 0;
   for (int i = threadIdx.x; i < a.ctas * kArriveWords; i += kPlanThreads) a.arrived[i] = 0;
   __syncthreads();
   for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
-    const AttnTile tile = a.tiles[t];
-    const long long lo = tile.before, hi = lo + (long long)(tile.units + a.lead) * a.line_heads;
+    AttnTile tile = a.tiles[t];      // (this thread's own)
+    tile.before = apart ? (tile.before >> 40) * a.min_share * a.line_heads
+                        : ((tile.before & ((1ll << 40) - 1)) + (long long)t * lead) * a.line_heads;
+    a.tiles[t].before = tile.before;
+    const long long lo = tile.before, hi = lo + (long long)stretch_of(tile.units, lead, (int)share) * a.line_heads;
     for (long long c = (lo + share - 1) / share; c * share < hi; ++c)
-      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), share, t, dead};
+      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), (int)share, lead, t, dead};
   }
   for (long long c = (units + share - 1) / share + threadIdx.x; c < a.shares; c += kPlanThreads)
-    a.work[c] = CtaWork{AttnTile{}, 0, 0, share, 0, dead};
+    a.work[c] = CtaWork{AttnTile{}, 0, 0, (int)share, lead, 0, dead};
 }
 
 // ---------------------------------------------------------------- KV write

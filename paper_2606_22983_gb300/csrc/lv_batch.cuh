@@ -31,7 +31,9 @@ static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
 
 // A pair of a tile and a KV head takes a stretch of a line: `lead` places for what it costs to begin
 // and end it, then one for each of its units.  A CTA takes `share` places on, whatever pairs that
-// cuts; the one that finishes the last piece of a cut pair joins its pieces, in their order.
+// cuts; the one that finishes the last piece of a cut pair joins its pieces, in their order.  Where
+// there are CTAs enough that each pair may begin one of its own, the stretches are whole shares
+// instead, with empty places at their ends (lead -1), and short pairs are not cut.
 // The kernel for many rows has one line of all pairs, tile after tile and head after head in it.
 // The one for few rows has a line of the tiles for each KV head, and H CTAs beside one another take
 // the same places of theirs: they read the same pages, whose H rows of a token lie together, at
@@ -39,7 +41,7 @@ static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
 struct CtaWork {        // what a CTA starts from
   AttnTile t;           // of its first place
   int64_t begin, end;   // its places; begin == end: none
-  int64_t share;
+  int32_t share, lead;
   int32_t tile;
   int32_t dead;         // rows of no request in the step
 };
@@ -111,7 +113,6 @@ struct AttnArgs {
   int32_t q_vec, o_vec;    // 16-byte accesses allowed
   int32_t num_tokens;
   int32_t window, sinks;
-  int32_t lead;
   int32_t tile_rows;       // rows of a partial result's slot
   int32_t dp;              // columns of a partial result
   float scale;             // scale * log2(e)
@@ -120,24 +121,24 @@ struct AttnArgs {
   long long* ctl;
 };
 
-// Words of AttnArgs.arrived a CTA: the rows kernel counts a pair's pieces in the first, the other
-// one a warp's rows in each.
+// Words of AttnArgs.arrived a CTA: the kernel for few rows counts a pair's pieces in the first and
+// those of a group of them in the second, the other one a warp's rows in each.
 constexpr int kArriveWords = 8;
 
 // CTA c's slot for a piece of a (tile, head) pair that it holds only part of: a piece
 // that does not start the pair is the first that the CTA does, one that starts it the last.
 __host__ __device__ inline int64_t part_slot(int64_t cta, bool starts) { return 2 * cta + (starts ? 1 : 0); }
 
-enum AttnKind : int { ATTN_ROWS16 = 0, ATTN_ROWS32 = 1, ATTN_TC = 2 };
+enum AttnKind : int { ATTN_ROWS = 0, ATTN_TC = 1 };
 
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t s);
 cudaError_t launch_kv_write(const WriteArgs& a, cudaStream_t s, int num_sms);
 cudaError_t configure_attend();
 cudaError_t configure_attend_tc();
 // keys of a unit, and CTAs that an SM holds, of the rows kernel
-constexpr int kRowsUnit = 16;
-int attend_rows_ctas(int dp, bool wide);
-cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool wide, bool bf16,
+constexpr int kRowsUnit = 16, kRowsRows = 16;
+int attend_rows_ctas(int dp);
+cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16,
                                int ctas, cudaStream_t s);      // maps: boxes of 64 columns and a unit's keys, or null
 constexpr int kTcUnit = 128, kTcRows = 256;
 // places ahead of a pair's units: what a pair costs besides its units, in units
@@ -190,13 +191,22 @@ __device__ __forceinline__ T load_words(const T* p) {
   for (int i = 0; i < (int)(sizeof(T) / 16); ++i) x.w[i] = reinterpret_cast<const int4*>(p)[i];
   return x.t;
 }
+// Places of a pair's stretch.
+__device__ __forceinline__ int stretch_of(int units, int lead, int share) {
+  return lead < 0 ? (units + share - 1) / share * share : units + lead;
+}
+// Units [u0, u1) of a pair that places [o0, o1) of its stretch hold.
+__device__ __forceinline__ int2 units_of(int o0, int o1, int units, int lead) {
+  const int ahead = max(lead, 0);
+  return make_int2(max(o0 - ahead, 0), min(o1 - ahead, units));
+}
 // The pieces of a pair (head: its head's number in the line): shares first .. first + count - 1.
 struct Pieces {
   int64_t first;
   int count;
 };
-__device__ __forceinline__ Pieces pieces_of(const AttnTile& t, int head, int lead, int64_t share) {
-  const int64_t start = t.before + (int64_t)head * (t.units + lead) + lead;
+__device__ __forceinline__ Pieces pieces_of(const AttnTile& t, int head, int lead, int share) {
+  const int64_t start = t.before + (int64_t)head * stretch_of(t.units, lead, share) + max(lead, 0);
   const int64_t first = start / share;
   return {first, (int)((start + t.units - 1) / share - first) + 1};
 }
