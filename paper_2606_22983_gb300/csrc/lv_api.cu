@@ -1883,13 +1883,15 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
       a.unit = lv::kTcUnit;
       a.lead = lv::kTcLead;
       a.min_share = 4;
+      a.uncut = 4;
       b->ctas = a.shares = pool->num_sms;
     } else {
       a.line_heads = 1;
       a.tile_rows = lv::kRowsRows;
       a.unit = lv::kRowsUnit;
       a.lead = lv::kRowsLead;
-      a.min_share = 32;
+      a.min_share = 8;
+      a.uncut = 24;
       a.shares = rows_shares(b);
       b->ctas = rows_ctas(b);
     }
@@ -1961,6 +1963,9 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.P = pool->d.P;
   a.hbm_pages = (uint32_t)pool->d.hbm_pages;
   a.T = pool->d.T;
+  a.t_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (a.T == 1 << i) a.t_shift = i;
   a.H = pool->kv_heads;
   a.D = pool->head_dim;
   a.G = b->G;

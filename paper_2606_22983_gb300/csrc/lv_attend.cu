@@ -115,7 +115,7 @@ struct Walk {
   int tile;
   int u, u_end;            // units of the pair, this warp's next and the CTA's end
   int u_begin;
-  int32_t page;            // of unit u (where a unit lies in one page)
+  int32_t page, off;       // of unit u (where a unit lies in one page)
 };
 
 struct CutTile {
@@ -215,10 +215,10 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
   }
 }
 
-// A pair of more pieces than this is joined in two steps, groups of kGroup pieces first: the last CTA
+// A pair of more than kAlone pieces is joined in two steps, groups of kGroup pieces first: the last CTA
 // of a group joins the group, the last of those the groups (one CTA alone took some 25 us for the
 // 114 pieces of a context of 60 000 keys).
-constexpr int kGroup = 12;
+constexpr int kAlone = 32, kGroup = 12;
 
 // One CTA: its share of one KV head's line.  Its four warps take a tile's units in turn and are joined at the
 // tile's end; each streams its units' K and V rows through a ring of its own, so no barrier of the
@@ -256,8 +256,11 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   auto key_of = [&](const AttnTile& t, int u) { return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kU; };
   auto hidden = [&](const AttnTile& t, int key) { return key >= t.kv_hi || (key < t.kv_lo && key >= a.sinks); };
   auto find_page = [&](Walk& x) {
-    if (kTma && x.u < x.u_end)
-      x.page = a.tables[(size_t)x.t.req * a.maxB + (uint32_t)key_of(x.t, x.u) / (uint32_t)a.T];
+    if (kTma && x.u < x.u_end) {
+      const uint32_t key = key_of(x.t, x.u), b = a.t_shift >= 0 ? key >> a.t_shift : key / (uint32_t)a.T;
+      x.page = a.tables[(size_t)x.t.req * a.maxB + b];
+      x.off = key - b * a.T;
+    }
   };
   auto next_pair = [&](Walk& x) -> bool {
     while (x.w < x.end) {
@@ -292,22 +295,21 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   long long loads = 0;
   // unit L.u of L's pair into stage s
   auto load = [&](int s) {
-    const int key0 = key_of(L.t, L.u);
     const uint32_t dst = ring_s + s * 2 * S::kTile;
     if constexpr (kTma) {
       const int page = (uint32_t)L.page < a.hbm_pages ? L.page : (int)a.hbm_pages;      // none: zeros
-      const int off = key0 % a.T;
       if (elected()) {
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_s + 8 * s), "r"(2 * S::kTile)
                      : "memory");
 #pragma unroll
         for (int x = 0; x < S::kBlocks; ++x) {
-          tma_box(dst + x * kU * 128, &kmap, 64 * x, head, off, page, bar_s + 8 * s);
-          tma_box(dst + S::kTile + x * kU * 128, &vmap, 64 * x, head, off, page, bar_s + 8 * s);
+          tma_box(dst + x * kU * 128, &kmap, 64 * x, head, L.off, page, bar_s + 8 * s);
+          tma_box(dst + S::kTile + x * kU * 128, &vmap, 64 * x, head, L.off, page, bar_s + 8 * s);
         }
       }
       __syncwarp();
     } else {
+      const int key0 = key_of(L.t, L.u);
       const uint32_t head_at = (uint32_t)head * (uint32_t)a.D * 2;
       constexpr int kChunks = DP / 8;               // 16-byte pieces of a row
 #pragma unroll
@@ -572,8 +574,8 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         __syncwarp();
         if (lane == 0) {
           const int p = (int)(group - ps.first);
-          const int64_t of = ps.first + (ps.count > kGroup ? p / kGroup * kGroup : 0);
-          const int was = add_release(&a.arrived[(of * a.H + head) * kArriveWords + (ps.count > kGroup)], 1);
+          const int64_t of = ps.first + (ps.count > kAlone ? p / kGroup * kGroup : 0);
+          const int was = add_release(&a.arrived[(of * a.H + head) * kArriveWords + (ps.count > kAlone)], 1);
           if (n == 0) was_first = was;
           else was_last = was;
         }
@@ -589,7 +591,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       const AttnTile t = cut[n].t;
       const Pieces ps = pieces_of(t, 0, work.lead, work.share);
       const int p = (int)(group - ps.first), g0 = p / kGroup * kGroup, g_count = min(kGroup, ps.count - g0);
-      const bool grouped = ps.count > kGroup;
+      const bool grouped = ps.count > kAlone;
       // true in the whole CTA when its piece (or its group) was the last to arrive
       auto last = [&](int was, int of, int count, int word) {
         if (threadIdx.x == 0) {

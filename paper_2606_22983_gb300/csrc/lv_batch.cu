@@ -10,7 +10,7 @@ namespace lv {
 namespace {
 
 constexpr int kPlanThreads = 256;
-constexpr long long kManyShares = 1 << 20;   // more than there are CTAs
+constexpr long long kManyShares = (1 << 11) - 1;   // more than there are CTAs, in 11 bits
 constexpr int kMaxRequests = 4096;      // lv_batch_create's limit
 
 // Sum over the CTA, to every thread.  ws: one word a warp; a barrier lies between its uses.
@@ -171,7 +171,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
   live = cta_sum(live, ws);
   const int n_tiles = (int)min(tiles, (long long)a.max_tiles);
   // the tiles, a thread each (its request found by bisection), and where they lie on the line
-  long long units = 0, padded = 0;
+  long long units = 0, shorts = 0, longs = 0;
+  bool cut_free = true;      // no pair has more units than one CTA may well take
   for (int base = 0; base < n_tiles; base += kPlanThreads) {
     const int t = base + threadIdx.x;
     AttnTile tile{};
@@ -187,28 +188,35 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
     }
     long long total;
     const long long at = cta_scan(t < n_tiles ? tile.units : 0, ws, &total);
-    long long total_padded;
-    const long long at_padded =
-        cta_scan(t < n_tiles ? (tile.units + a.min_share - 1) / a.min_share : 0, ws, &total_padded);
+    long long total_short, total_long;
+    const long long at_short =
+        cta_scan(t < n_tiles ? (tile.units + a.min_share - 1) / a.min_share : 0, ws, &total_short);
+    const long long at_long = cta_scan(t < n_tiles ? (tile.units + a.uncut - 1) / a.uncut : 0, ws, &total_long);
     if (t < n_tiles) {
-      // what comes before it, in units and (above bit 40) in shares of min_share
-      tile.before = units + at + (min(padded + at_padded, kManyShares) << 40);
+      // what comes before it, in units, in short shares (from bit 40 on) and in long ones (from 51)
+      tile.before = units + at + (min(shorts + at_short, kManyShares) << 40) + (min(longs + at_long, kManyShares) << 51);
       a.tiles[t] = tile;
+      cut_free &= tile.units <= a.uncut;
     }
     units += total;
-    padded += total_padded;
+    shorts += total_short;
+    longs += total_long;
   }
-  const bool apart = padded * a.line_heads <= a.shares;
-  const int lead = apart ? -1 : a.lead;
-  units = apart ? padded * a.min_share * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
-  const long long share = apart ? a.min_share : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
+  // Pairs apart in shares of their own: uncut ones of up to `uncut` units where that holds them all,
+  // else cut short (a cut costs what some 8 units of a warp do, so in the middle there is nothing).
+  cut_free = __syncthreads_and(cut_free);
+  const long long needed = cut_free ? longs : shorts;
+  const bool apart = needed * a.line_heads <= a.shares;
+  const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
+  units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
+  const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
   const int dead = a.num_tokens - (int)live;
   if (threadIdx.x == 0) a.head->ticket = 0;
   for (int i = threadIdx.x; i < a.ctas * kArriveWords; i += kPlanThreads) a.arrived[i] = 0;
   __syncthreads();
   for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
     AttnTile tile = a.tiles[t];      // (this thread's own)
-    tile.before = apart ? (tile.before >> 40) * a.min_share * a.line_heads
+    tile.before = apart ? (tile.before >> (cut_free ? 51 : 40) & kManyShares) * size * a.line_heads
                         : ((tile.before & ((1ll << 40) - 1)) + (long long)t * lead) * a.line_heads;
     a.tiles[t].before = tile.before;
     const long long lo = tile.before, hi = lo + (long long)stretch_of(tile.units, lead, (int)share) * a.line_heads;

@@ -67,6 +67,7 @@ struct PlanArgs {
   int32_t tile_rows, unit; // of the attention kernel that will run
   int32_t lead;            // places of the line ahead of a pair's units
   int32_t min_share;       // places a CTA takes at least
+  int32_t uncut;           // units of a pair that is better not cut
   int32_t shares;          // of a line
   int32_t ctas;            // of the attention
   int32_t window, sinks;
@@ -100,6 +101,7 @@ struct AttnArgs {
   int64_t P;
   uint32_t hbm_pages;
   int32_t T, H, D, G;
+  int32_t t_shift;         // log2(T), -1 where T is no power of two
   int32_t maxB;
   const int32_t* tables;
   const int32_t* positions;
