@@ -651,8 +651,8 @@ typedef struct lv_batch_desc {
   int32_t max_requests;        /* 1..4096 */
   int32_t max_tokens;          /* rows of a step's tensors at most, 1..2^24; Hq * max_tokens < 2^31 */
   int32_t dtype;               /* LV_BF16 or LV_F16: the pool's elements, queries and outputs */
-  int32_t window;              /* > 0: a query at position p sees keys p - window + 1 .. p; 0: all up to p */
-  int32_t sinks;               /* >= 0: and, beside the window, keys 0 .. sinks - 1 up to p */
+  int32_t window;              /* 1..2^30: a query at position p sees keys p - window + 1 .. p; 0: all up to p */
+  int32_t sinks;               /* 0..2^30: and, beside the window, keys 0 .. sinks - 1 up to p */
   int32_t* row_starts;         /* [max_requests + 1] first row of each request; the end */
   int32_t* kv_lens;            /* [max_requests] context length at the step's end */
   int32_t* tables;             /* [max_requests][max_blocks] HBM pages, -1 where there is none */
@@ -672,8 +672,8 @@ typedef struct lv_heads {
   int32_t reserved;            /* must be 0 */
 } lv_heads;
 
-/* Validates the descriptor and allocates the batch's work lists and workspace (about
-   80 MiB at 128 head_dim).  LV_ERR_INVALID, LV_ERR_OOM or LV_ERR_CUDA. */
+/* Validates the descriptor and allocates the batch's work lists and workspace (some 40 MiB
+   at 128 head_dim).  LV_ERR_INVALID, LV_ERR_OOM or LV_ERR_CUDA. */
 lv_status lv_batch_create(lv_pool* pool, const lv_batch_desc* desc, lv_batch** out);
 
 /* Waits for `stream` and frees the batch; call it before lv_pool_destroy of its pool. */

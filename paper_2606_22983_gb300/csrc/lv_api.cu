@@ -1760,7 +1760,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   if (d->max_requests < 1 || d->max_requests > 4096 || d->max_tokens < 1 || d->max_tokens > 1 << 24)
     return LV_ERR_INVALID;
   if ((long long)d->num_q_heads * d->max_tokens >= 1ll << 31) return LV_ERR_INVALID;
-  if (d->window < 0 || d->sinks < 0 || d->reserved[0] != 0 || d->reserved[1] != 0) return LV_ERR_INVALID;
+  if (d->window < 0 || d->window > 1 << 30 || d->sinks < 0 || d->sinks > 1 << 30 || d->reserved[0] != 0 || d->reserved[1] != 0) return LV_ERR_INVALID;
   if (!device_array(pool, d->row_starts, 4) || !device_array(pool, d->kv_lens, 4) ||
       !device_array(pool, d->tables, 4) || !device_array(pool, d->positions, 4) || !device_array(pool, d->slots, 8))
     return LV_ERR_INVALID;

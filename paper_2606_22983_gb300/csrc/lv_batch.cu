@@ -104,7 +104,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
       const int ctx = p.sess[sid].ctx_tokens;
       first = a.firsts ? a.firsts[i] : -1;
       if (first < 0) first = ctx - len;
-      if (first < 0 || (long long)first + len > ctx || ((long long)ctx + p.T - 1) / p.T > p.maxB) err = LV_ERR_BOUNDS;
+      // (positions stay far enough below 2^31 for a unit's keys past them)
+      if (first < 0 || (long long)first + len > ctx || (long long)first + len > 0x7ffff000ll ||
+          ((long long)first + len + p.T - 1) / p.T > p.maxB)
+        err = LV_ERR_BOUNDS;
     }
     const int32_t* row = p.table + (size_t)(known ? sid : 0) * p.maxB;
     int32_t* out = a.tables + (size_t)i * p.maxB;
