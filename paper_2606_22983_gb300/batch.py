@@ -132,7 +132,8 @@ class KVBatch:
         rows = q.shape[0]
         past = rows - self.num_tokens            # rows that the step does not have
         if out is None:
-            out = torch.empty_like(q, dtype=self.dtype, memory_format=torch.contiguous_format)
+            out = torch.empty_like(q) if q.is_contiguous() and q.dtype is self.dtype else \
+                torch.empty(q.shape, dtype=self.dtype, device=q.device)
             if past:
                 out[self.num_tokens:].zero_()
         lse = None

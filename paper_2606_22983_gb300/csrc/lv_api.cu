@@ -1883,7 +1883,7 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
       a.unit = lv::kTcUnit;
       a.lead = lv::kTcLead;
       a.min_share = 4;
-      a.uncut = 4;
+      a.uncut = 12;
       b->ctas = a.shares = pool->num_sms;
     } else {
       a.line_heads = 1;

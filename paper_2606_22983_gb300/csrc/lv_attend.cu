@@ -86,13 +86,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The sum before, and what this warp wrote visible with it.
-__device__ __forceinline__ int add_release(int32_t* p, int v) {
-  int was;
-  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(was) : "l"(p), "r"(v) : "memory");
-  return was;
-}
-
 // Rows of no request: out = 0, lse = -inf.  Thread i of `of` threads.
 __device__ __forceinline__ void clear_dead(const AttnArgs& a, int i, int of) {
   const int Hq = a.H * a.G;

@@ -213,69 +213,100 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// The join of a cut pair by one warp: rows row0 .. row0 + 31 of its tile (those in rows_in), every
-// piece's sums weighted by its maximum against the largest.  Lane i knows row i's output.
+// Pieces p0, p0 + step, ... (count of them) of a cut pair joined by one warp: rows row0 .. row0 + 31 of
+// its tile (those in rows_in), every piece's sums weighted by its maximum against the largest, in
+// the pieces' order.  To the output (lane i knows row i's), or (not last) to the first of the
+// pieces' own slots.
 template <int DP, bool kBf16>
-__device__ __forceinline__ void join_rows(const AttnArgs& a, const Pieces& ps, int row0, int lane, uint32_t rows_in,
-                                          uint16_t* out, int64_t r, int hq) {
+__device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int p0, int step, int count, bool last,
+                                          int row0, int lane, uint32_t rows_in, uint16_t* out, int64_t r, int hq) {
   constexpr int kCols = DP / 32;      // a lane's
   const bool mine = rows_in >> lane & 1;
-  auto slot = [&](int p) { return part_slot(ps.first + p, p == 0) * a.tile_rows + row0; };
+  auto slot = [&](int i) {
+    const int p = p0 + min(i, count - 1) * step;
+    return part_slot(first + p, p == 0) * a.tile_rows + row0;
+  };
   float top = -INFINITY, sum = 0.f;
-  for (int p = 0; p < ps.count; ++p)
-    if (mine) top = fmaxf(top, __ldcg(&a.part_ml[slot(p) + lane]).x);
-  float acc[32][kCols];
+  for (int i = 0; i < count; i += 4) {
+    float x[4];
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-#pragma unroll
-    for (int e = 0; e < kCols; ++e) acc[i][e] = 0.f;
+    for (int e = 0; e < 4; ++e) x[e] = mine ? __ldcg(&a.part_ml[slot(i + e) + lane]).x : -INFINITY;
+    top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
+  }
+  // (half of the rows at a time: all 32 rows' sums would spill what the softmax holds)
+  constexpr int kAt = 16;
+  float inv = 0.f;
 #pragma unroll 1
-  for (int p = 0; p < ps.count; ++p) {
-    float f = 0.f;
-    if (mine) {
-      const float2 ml = __ldcg(&a.part_ml[slot(p) + lane]);
-      f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
-      sum += ml.y * f;
-    }
-    const float* o = a.part_o + slot(p) * DP + kCols * lane;
-    // (32 loads on their way at once; rows past the tile's read what is there and are not stored)
+  for (int i0 = 0; i0 < 32; i0 += kAt) {
+    float acc[kAt][kCols];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float g = __shfl_sync(0xffffffffu, f, i);
-      if constexpr (kCols == 4) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + i * DP));
-        acc[i][0] += v.x * g;
-        acc[i][1] += v.y * g;
-        acc[i][2] += v.z * g;
-        acc[i][3] += v.w * g;
-      } else {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(o + i * DP));
-        acc[i][0] += v.x * g;
-        acc[i][1] += v.y * g;
+    for (int i = 0; i < kAt; ++i)
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) acc[i][e] = 0.f;
+    float2 next = mine ? __ldcg(&a.part_ml[slot(0) + lane]) : make_float2(-INFINITY, 0.f);
+    sum = 0.f;
+#pragma unroll 1
+    for (int p = 0; p < count; ++p) {
+      const float2 ml = next;
+      if (mine) next = __ldcg(&a.part_ml[slot(p + 1) + lane]);
+      const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
+      sum += ml.y * f;
+      const float* o = a.part_o + (slot(p) + i0) * DP + kCols * lane;
+      // (all loads on their way at once; rows past the tile's read what is there and are not stored)
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) {
+        const float g = __shfl_sync(0xffffffffu, f, i0 + i);
+        if constexpr (kCols == 4) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(o + i * DP));
+          acc[i][0] += v.x * g;
+          acc[i][1] += v.y * g;
+          acc[i][2] += v.z * g;
+          acc[i][3] += v.w * g;
+        } else {
+          const float2 v = __ldcg(reinterpret_cast<const float2*>(o + i * DP));
+          acc[i][0] += v.x * g;
+          acc[i][1] += v.y * g;
+        }
+      }
+    }
+    if (!last) {
+      float* o = a.part_o + (slot(0) + i0) * DP + kCols * lane;
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) {
+        if (!(rows_in >> (i0 + i) & 1)) continue;
+#pragma unroll
+        for (int e = 0; e < kCols; e += 2) *reinterpret_cast<float2*>(o + i * DP + e) = make_float2(acc[i][e], acc[i][e + 1]);
+      }
+      continue;
+    }
+    inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int i = 0; i < kAt; ++i) {
+      const float g = __shfl_sync(0xffffffffu, inv, i0 + i);
+      uint16_t* to =
+          reinterpret_cast<uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(out), i0 + i)) + kCols * lane;
+      if (!(rows_in >> (i0 + i) & 1) || kCols * lane >= a.D) continue;
+#pragma unroll
+      for (int e = 0; e < kCols; e += 2) {
+        const uint32_t w = pack16<kBf16>(acc[i][e] * g, acc[i][e + 1] * g);
+        if (a.o_vec) {
+          *reinterpret_cast<uint32_t*>(to + e) = w;
+        } else {
+          to[e] = (uint16_t)w;
+          to[e + 1] = (uint16_t)(w >> 16);
+        }
       }
     }
   }
-  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-  if (mine && a.lse)
+  if (mine && !last) a.part_ml[slot(0) + lane] = make_float2(top, sum);
+  if (mine && last && a.lse)
     a.lse[r * (a.H * a.G) + hq] =
         sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const float g = __shfl_sync(0xffffffffu, inv, i);
-    uint16_t* to = reinterpret_cast<uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(out), i)) + kCols * lane;
-    if (!(rows_in >> i & 1) || kCols * lane >= a.D) continue;
-#pragma unroll
-    for (int e = 0; e < kCols; e += 2) {
-      const uint32_t w = pack16<kBf16>(acc[i][e] * g, acc[i][e + 1] * g);
-      if (a.o_vec) {
-        *reinterpret_cast<uint32_t*>(to + e) = w;
-      } else {
-        to[e] = (uint16_t)w;
-        to[e + 1] = (uint16_t)(w >> 16);
-      }
-    }
-  }
 }
+
+// A pair of more than kAlone pieces is joined in two steps, groups of kGroup pieces first: the last
+// warp of a group joins the group, the last of those the groups.
+constexpr int kAlone = 6, kGroup = 5;
 
 // The pairs (tile, head) of a CTA's share, one after the other.
 struct Pairs {
@@ -605,16 +636,36 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       if (!whole) {
         if (mine) a.part_ml[slot] = make_float2(top2, sm.sum);
         // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
-        __threadfence();
-        __syncwarp();
         const Pieces ps = pieces_of(pr.t, pr.head, pr.lead, pr.share);
-        int32_t* count = &a.arrived[ps.first * kArriveWords + wid];
-        int before = 0;
-        if (lane == 0) before = atomicAdd(count, 1);
-        if (__shfl_sync(0xffffffffu, before, 0) == ps.count - 1) {
-          if (lane == 0) *count = 0;
+        const int row0 = half * half_rows + (row & ~31);
+        // true when `count` warps have come to word `word` of the first piece's, this one last
+        auto last = [&](int of, int count, int word) {
+          __syncwarp();
+          int was = 0;
+          if (lane == 0) {
+            int32_t* at = &a.arrived[(ps.first + of) * kArriveWords + word + wid];
+            was = add_release(at, 1);
+            if (was == count - 1) *at = 0;
+          }
+          was = __shfl_sync(0xffffffffu, was, 0);
+          if (was != count - 1) return false;
           __threadfence();
-          join_rows<DP, kBf16>(a, ps, half * half_rows + (row & ~31), lane, rows_in, out, r, hq);
+          return true;
+        };
+        if (ps.count <= kAlone) {
+          if (last(0, ps.count, 0))
+            join_rows<DP, kBf16>(a, ps.first, 0, 1, ps.count, true, row0, lane, rows_in, out, r, hq);
+        } else {
+          const int g0 = (int)(blockIdx.x - ps.first) / kGroup * kGroup, n = min(kGroup, ps.count - g0);
+          const int groups = (ps.count + kGroup - 1) / kGroup;
+          if (last(g0, n, kSoftWarps)) {
+#pragma unroll 1
+            for (int step = 0; step < 2; ++step) {
+              join_rows<DP, kBf16>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, row0, lane,
+                                   rows_in, out, r, hq);
+              if (step || !last(0, groups, 0)) break;
+            }
+          }
         }
       } else if (mine && a.lse) {
         a.lse[r * (a.H * a.G) + hq] =

@@ -124,8 +124,8 @@ struct AttnArgs {
 };
 
 // Words of AttnArgs.arrived a CTA: the kernel for few rows counts a pair's pieces in the first and
-// those of a group of them in the second, the other one a warp's rows in each.
-constexpr int kArriveWords = 8;
+// those of a group of them in the second; the other one so for each of its eight warps' rows.
+constexpr int kArriveWords = 16;
 
 // CTA c's slot for a piece of a (tile, head) pair that it holds only part of: a piece
 // that does not start the pair is the first that the CTA does, one that starts it the last.
@@ -180,6 +180,12 @@ cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, unsigned block
 __device__ __forceinline__ void report(long long* ctl, int code, long long detail) {
   if (atomicCAS(reinterpret_cast<unsigned long long*>(&ctl[C_ERR]), 0ull, (unsigned long long)code) == 0ull)
     ctl[C_ERR_DETAIL] = detail;
+}
+// The sum before, and what this warp wrote visible with it.
+__device__ __forceinline__ int add_release(int32_t* p, int v) {
+  int was;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(was) : "l"(p), "r"(v) : "memory");
+  return was;
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
