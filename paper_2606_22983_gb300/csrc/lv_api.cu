@@ -1785,8 +1785,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   const int most = std::max(rows_ctas(b), pool->num_sms);
   // rows of partial results: two slots a CTA
   size_t rows = (size_t)2 * rows_ctas(b) * lv::kRowsRows;
-  // (a warp joins 32 rows of a tile at a time, past its end where it has fewer)
-  if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows + 32);
+  if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows);
   try {
     if ((st = batch_alloc(b, &b->reqs, d->max_requests)) != LV_OK ||
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||

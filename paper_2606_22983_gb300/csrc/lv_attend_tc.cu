@@ -213,95 +213,88 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// Pieces p0, p0 + step, ... (count of them) of a cut pair joined by one warp: rows row0 .. row0 + 31 of
-// its tile (those in rows_in), every piece's sums weighted by its maximum against the largest, in
-// the pieces' order.  To the output (lane i knows row i's), or (not last) to the first of the
-// pieces' own slots.
+// A piece's sums lie [4 columns][row of the tile][4], so that a warp, a lane a row, writes and reads
+// 512 bytes at once.
+template <int DP>
+__device__ __forceinline__ float4* part_at(const AttnArgs& a, int64_t slot, int col, int row) {
+  return reinterpret_cast<float4*>(a.part_o) + (slot * (DP / 4) + col / 4) * a.tile_rows + row;
+}
+
+// Pieces p0, p0 + step, ... (count of them) of a cut pair joined by one warp, a lane a row of the
+// tile: every piece's sums weighted by its maximum against the largest, in the pieces' order.  To
+// the output, or (not last) to the first of the pieces' own slots.
 template <int DP, bool kBf16>
 __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int p0, int step, int count, bool last,
-                                          int row0, int lane, uint32_t rows_in, uint16_t* out, int64_t r, int hq) {
-  constexpr int kCols = DP / 32;      // a lane's
-  const bool mine = rows_in >> lane & 1;
+                                          int row, bool mine, uint16_t* out, int64_t r, int hq) {
   auto slot = [&](int i) {
     const int p = p0 + min(i, count - 1) * step;
-    return part_slot(first + p, p == 0) * a.tile_rows + row0;
+    return part_slot(first + p, p == 0);
   };
+  auto ml_of = [&](int i) { return __ldcg(&a.part_ml[slot(i) * a.tile_rows + row]); };
   float top = -INFINITY, sum = 0.f;
-  for (int i = 0; i < count; i += 4) {
-    float x[4];
+  if (mine) {
+    for (int i = 0; i < count; i += 4) {
+      float x[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = mine ? __ldcg(&a.part_ml[slot(i + e) + lane]).x : -INFINITY;
-    top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
-  }
-  // (half of the rows at a time: all 32 rows' sums would spill what the softmax holds)
-  constexpr int kAt = 16;
-  float inv = 0.f;
+      for (int e = 0; e < 4; ++e) x[e] = ml_of(i + e).x;
+      top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
+    }
 #pragma unroll 1
-  for (int i0 = 0; i0 < 32; i0 += kAt) {
-    float acc[kAt][kCols];
+    for (int c0 = 0; c0 < DP; c0 += 64) {
+      float4 acc[16];
 #pragma unroll
-    for (int i = 0; i < kAt; ++i)
-#pragma unroll
-      for (int e = 0; e < kCols; ++e) acc[i][e] = 0.f;
-    float2 next = mine ? __ldcg(&a.part_ml[slot(0) + lane]) : make_float2(-INFINITY, 0.f);
-    sum = 0.f;
+      for (int c = 0; c < 16; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+      float2 next = ml_of(0);
+      sum = 0.f;
 #pragma unroll 1
-    for (int p = 0; p < count; ++p) {
-      const float2 ml = next;
-      if (mine) next = __ldcg(&a.part_ml[slot(p + 1) + lane]);
-      const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
-      sum += ml.y * f;
-      const float* o = a.part_o + (slot(p) + i0) * DP + kCols * lane;
-      // (all loads on their way at once; rows past the tile's read what is there and are not stored)
+      for (int p = 0; p < count; ++p) {
+        const float2 ml = next;
+        next = ml_of(p + 1);
+        const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
+        sum += ml.y * f;
+        const float4* o = part_at<DP>(a, slot(p), c0, row);
 #pragma unroll
-      for (int i = 0; i < kAt; ++i) {
-        const float g = __shfl_sync(0xffffffffu, f, i0 + i);
-        if constexpr (kCols == 4) {
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(o + i * DP));
-          acc[i][0] += v.x * g;
-          acc[i][1] += v.y * g;
-          acc[i][2] += v.z * g;
-          acc[i][3] += v.w * g;
-        } else {
-          const float2 v = __ldcg(reinterpret_cast<const float2*>(o + i * DP));
-          acc[i][0] += v.x * g;
-          acc[i][1] += v.y * g;
+        for (int c = 0; c < 16; ++c) {
+          const float4 v = __ldcg(o + c * a.tile_rows);
+          acc[c].x += v.x * f;
+          acc[c].y += v.y * f;
+          acc[c].z += v.z * f;
+          acc[c].w += v.w * f;
         }
       }
-    }
-    if (!last) {
-      float* o = a.part_o + (slot(0) + i0) * DP + kCols * lane;
+      if (!last) {
+        float4* o = part_at<DP>(a, slot(0), c0, row);
 #pragma unroll
-      for (int i = 0; i < kAt; ++i) {
-        if (!(rows_in >> (i0 + i) & 1)) continue;
-#pragma unroll
-        for (int e = 0; e < kCols; e += 2) *reinterpret_cast<float2*>(o + i * DP + e) = make_float2(acc[i][e], acc[i][e + 1]);
+        for (int c = 0; c < 16; ++c) o[c * a.tile_rows] = acc[c];
+        continue;
       }
-      continue;
-    }
-    inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+      const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
 #pragma unroll
-    for (int i = 0; i < kAt; ++i) {
-      const float g = __shfl_sync(0xffffffffu, inv, i0 + i);
-      uint16_t* to =
-          reinterpret_cast<uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(out), i0 + i)) + kCols * lane;
-      if (!(rows_in >> (i0 + i) & 1) || kCols * lane >= a.D) continue;
-#pragma unroll
-      for (int e = 0; e < kCols; e += 2) {
-        const uint32_t w = pack16<kBf16>(acc[i][e] * g, acc[i][e + 1] * g);
+      for (int c = 0; c < 16; c += 2) {
+        if (c0 + 4 * c >= a.D) break;
+        const uint4 w = make_uint4(pack16<kBf16>(acc[c].x * inv, acc[c].y * inv), pack16<kBf16>(acc[c].z * inv, acc[c].w * inv),
+                                   pack16<kBf16>(acc[c + 1].x * inv, acc[c + 1].y * inv),
+                                   pack16<kBf16>(acc[c + 1].z * inv, acc[c + 1].w * inv));
+        uint16_t* to = out + c0 + 4 * c;
         if (a.o_vec) {
-          *reinterpret_cast<uint32_t*>(to + e) = w;
+          *reinterpret_cast<uint4*>(to) = w;
         } else {
-          to[e] = (uint16_t)w;
-          to[e + 1] = (uint16_t)(w >> 16);
+          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            to[2 * e] = (uint16_t)x[e];
+            to[2 * e + 1] = (uint16_t)(x[e] >> 16);
+          }
         }
       }
     }
+    if (!last)
+      a.part_ml[slot(0) * a.tile_rows + row] = make_float2(top, sum);
+    else if (a.lse)
+      a.lse[r * (a.H * a.G) + hq] =
+          sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
   }
-  if (mine && !last) a.part_ml[slot(0) + lane] = make_float2(top, sum);
-  if (mine && last && a.lse)
-    a.lse[r * (a.H * a.G) + hq] =
-        sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
+  __syncwarp();
 }
 
 // A pair of more than kAlone pieces is joined in two steps, groups of kGroup pieces first: the last
@@ -580,16 +573,14 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const int64_t r = pr.t.qrow + token;
       const bool mine = row < rows;
       const float inv = !whole ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
-      const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0) * a.tile_rows + half * half_rows + row;
+      const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0);
+      const int t_row = half * half_rows + row;
       uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + hq * a.o_head;
-      float* part = a.part_o + slot * DP;
       // the rows of this lane's group of four
       const uint32_t rows_in = __ballot_sync(0xffffffffu, mine);
       uint64_t to[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        to[t] = __shfl_sync(0xffffffffu, whole ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part),
-                            (lane & 28) + t);
+      for (int t = 0; t < 4; ++t) to[t] = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(out), (lane & 28) + t);
       const int piece = lane & 3;
 #pragma unroll 1
       for (int col = 0; col < DP; col += 32) {
@@ -617,27 +608,20 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
                 out[col + 2 * e + 1] = (uint16_t)(w[e] >> 16);
               }
           }
-        } else {
+        } else if (mine) {
+          float4* po = part_at<DP>(a, slot, col, t_row);
 #pragma unroll
-          for (int g = 0; g < 32; g += 16) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = o[g + e];
-            rows_to_pieces(w, lane);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-              if (rows_in >> ((lane & 28) + t) & 1)
-                *reinterpret_cast<uint4*>(to[t] + 4 * (col + g + 4 * piece)) =
-                    make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
-          }
+          for (int e = 0; e < 8; ++e)
+            po[e * a.tile_rows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]),
+                                              __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
         }
         __syncwarp();
       }
       const float top2 = sm.top * a.scale;      // in log2
       if (!whole) {
-        if (mine) a.part_ml[slot] = make_float2(top2, sm.sum);
+        if (mine) a.part_ml[slot * a.tile_rows + t_row] = make_float2(top2, sm.sum);
         // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
         const Pieces ps = pieces_of(pr.t, pr.head, pr.lead, pr.share);
-        const int row0 = half * half_rows + (row & ~31);
         // true when `count` warps have come to word `word` of the first piece's, this one last
         auto last = [&](int of, int count, int word) {
           __syncwarp();
@@ -654,15 +638,15 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         };
         if (ps.count <= kAlone) {
           if (last(0, ps.count, 0))
-            join_rows<DP, kBf16>(a, ps.first, 0, 1, ps.count, true, row0, lane, rows_in, out, r, hq);
+            join_rows<DP, kBf16>(a, ps.first, 0, 1, ps.count, true, t_row, mine, out, r, hq);
         } else {
           const int g0 = (int)(blockIdx.x - ps.first) / kGroup * kGroup, n = min(kGroup, ps.count - g0);
           const int groups = (ps.count + kGroup - 1) / kGroup;
           if (last(g0, n, kSoftWarps)) {
 #pragma unroll 1
             for (int step = 0; step < 2; ++step) {
-              join_rows<DP, kBf16>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, row0, lane,
-                                   rows_in, out, r, hq);
+              join_rows<DP, kBf16>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, t_row, mine,
+                                   out, r, hq);
               if (step || !last(0, groups, 0)) break;
             }
           }
