@@ -566,9 +566,10 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         // so that what it takes (some microseconds beside a cache read at full rate) is not waited for
         __syncwarp();
         if (lane == 0) {
-          const int p = (int)(group - ps.first);
-          const int64_t of = ps.first + (ps.count > kAlone ? p / kGroup * kGroup : 0);
-          const int was = add_release(&a.arrived[(of * a.H + head) * kArriveWords + (ps.count > kAlone)], 1);
+          const int p = (int)(group - ps.first), g0 = ps.count > kAlone ? p / kGroup * kGroup : 0;
+          const int set = ps.count <= kAlone ? 0 : g0 ? 2 : 1;
+          const int was =
+              add_release(&a.arrived[((ps.first + g0) * a.H + head) * kArriveWords + set * kArriveSet], 1);
           if (n == 0) was_first = was;
           else was_last = was;
         }
@@ -586,10 +587,10 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       const int p = (int)(group - ps.first), g0 = p / kGroup * kGroup, g_count = min(kGroup, ps.count - g0);
       const bool grouped = ps.count > kAlone;
       // true in the whole CTA when its piece (or its group) was the last to arrive
-      auto last = [&](int was, int of, int count, int word) {
+      auto last = [&](int was, int of, int count, int set) {
         if (threadIdx.x == 0) {
           const bool yes = was == count - 1;
-          if (yes) a.arrived[((ps.first + of) * a.H + head) * kArriveWords + word] = 0;
+          if (yes) a.arrived[((ps.first + of) * a.H + head) * kArriveWords + set * kArriveSet] = 0;
           cut[n].last = yes;
           __threadfence();
         }
@@ -603,7 +604,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         if (last(was, 0, ps.count, 0)) join_rows<DP, kBf16, true>(a, t, head, ps.first, 0, 1, ps.count);
         continue;
       }
-      if (!last(was, g0, g_count, 1)) continue;
+      if (!last(was, g0, g_count, g0 ? 2 : 1)) continue;
       join_rows<DP, kBf16, false>(a, t, head, ps.first, g0, 1, g_count);
       const int groups = (ps.count + kGroup - 1) / kGroup;
       __syncthreads();

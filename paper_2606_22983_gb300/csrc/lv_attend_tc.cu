@@ -622,12 +622,12 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         if (mine) a.part_ml[slot * a.tile_rows + t_row] = make_float2(top2, sm.sum);
         // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
         const Pieces ps = pieces_of(pr.t, pr.head, pr.lead, pr.share);
-        // true when `count` warps have come to word `word` of the first piece's, this one last
-        auto last = [&](int of, int count, int word) {
+        // true when `count` warps have come to set `set` of piece `of`, this one last
+        auto last = [&](int of, int count, int set) {
           __syncwarp();
           int was = 0;
           if (lane == 0) {
-            int32_t* at = &a.arrived[(ps.first + of) * kArriveWords + word + wid];
+            int32_t* at = &a.arrived[(ps.first + of) * kArriveWords + set * kArriveSet + wid];
             was = add_release(at, 1);
             if (was == count - 1) *at = 0;
           }
@@ -642,7 +642,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         } else {
           const int g0 = (int)(blockIdx.x - ps.first) / kGroup * kGroup, n = min(kGroup, ps.count - g0);
           const int groups = (ps.count + kGroup - 1) / kGroup;
-          if (last(g0, n, kSoftWarps)) {
+          if (last(g0, n, g0 ? 2 : 1)) {
 #pragma unroll 1
             for (int step = 0; step < 2; ++step) {
               join_rows<DP, kBf16>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, t_row, mine,

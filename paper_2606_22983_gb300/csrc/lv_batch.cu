@@ -215,7 +215,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
   const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
   const int dead = a.num_tokens - (int)live;
   if (threadIdx.x == 0) a.head->ticket = 0;
-  for (int i = threadIdx.x; i < a.ctas * kArriveWords; i += kPlanThreads) a.arrived[i] = 0;
+  // (zero already but after an attention that ran out of a wait)
+  static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
+  for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += kPlanThreads)
+    reinterpret_cast<int4*>(a.arrived)[i] = make_int4(0, 0, 0, 0);
   __syncthreads();
   for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
     AttnTile tile = a.tiles[t];      // (this thread's own)

@@ -123,9 +123,12 @@ struct AttnArgs {
   long long* ctl;
 };
 
-// Words of AttnArgs.arrived a CTA: the kernel for few rows counts a pair's pieces in the first and
-// those of a group of them in the second; the other one so for each of its eight warps' rows.
-constexpr int kArriveWords = 16;
+// Words of AttnArgs.arrived a CTA, in sets of kArriveSet (a warp's rows each, where warps count for
+// themselves).  The pieces of a cut pair, or their groups, are counted at the CTA of its first piece,
+// in set 0; the pieces of a group at the CTA of the group's first piece, in set 1 for a pair's first
+// group and in set 2 for another (which may begin with the pair's last piece, in a CTA where the
+// next pair begins too).
+constexpr int kArriveSet = 8, kArriveWords = 3 * kArriveSet;
 
 // CTA c's slot for a piece of a (tile, head) pair that it holds only part of: a piece
 // that does not start the pair is the first that the CTA does, one that starts it the last.

@@ -75,3 +75,18 @@ def test_windows(cached, new, window, sinks):
         _attend(s)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("heads", [1, 4])
+def test_neighbouring_long_joins(heads, new):
+    """Long contexts side by side, each cut into so many pieces that they are joined in groups, of
+    lengths that let a group begin with a context's last piece, where the next context begins."""
+    rng = np.random.default_rng(heads)
+    for n in (3, 5, 8):
+        s = _step(rng.integers(9000 // heads, 60000 // heads, n).tolist(), [new] * n, heads=heads, group=8, dim=64)
+        try:
+            for _ in range(3):
+                _attend(s)
+        finally:
+            s.close()
