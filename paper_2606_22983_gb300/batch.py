@@ -23,6 +23,7 @@ import torch
 from . import lv
 from .pool import KVPool
 
+_PLAN_ONE_LAUNCH = 256         # requests up to which a plan is one kernel
 _KINDS = {torch.bfloat16: lv.LV_BF16, torch.float16: lv.LV_F16, torch.float32: lv.LV_F32}
 
 
@@ -96,7 +97,7 @@ class KVBatch:
         lv.lv_batch_plan(self.handle, sids, firsts, lens, n, num_tokens,
                          num_tokens if max_len is None else max_len, self._stream(stream))
         self.num_tokens = num_tokens
-        self.pool.launches += 1
+        self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH)
 
     def _stream(self, stream):
         if stream is None:

@@ -1646,7 +1646,7 @@ struct lv_batch {
   int32_t max_tiles = 0;
   lv::CtaWork* work = nullptr;
   int32_t* arrived = nullptr;
-  lv::PlanHead* head = nullptr;
+  int32_t* ticket = nullptr;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
   int32_t G = 1;             // query heads a KV head
@@ -1791,14 +1791,14 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
-        (st = batch_alloc(b, &b->head, 1)) != LV_OK || (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
+        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
         (st = batch_alloc(b, &b->part_ml, rows)) != LV_OK)
       return fail(st);
   } catch (const std::bad_alloc&) {
     return fail(LV_ERR_OOM);
   }
   // (waits: the batch may be used on any stream next)
-  if (cudaMemset(b->head, 0, sizeof(lv::PlanHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
+  if (cudaMemset(b->ticket, 0, sizeof(int32_t)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
     return fail(LV_ERR_CUDA);
   *out = b;
   return LV_OK;
@@ -1879,7 +1879,7 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     if (b->kind == lv::ATTN_TC) {
       a.line_heads = pool->kv_heads;
       a.tile_rows = lv::tc_tile_rows(b->G);
-      a.unit = lv::kTcUnit;
+      a.unit_shift = lv::kTcUnitShift;
       a.lead = lv::kTcLead;
       a.min_share = 4;
       a.uncut = 12;
@@ -1887,7 +1887,7 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     } else {
       a.line_heads = 1;
       a.tile_rows = lv::kRowsRows;
-      a.unit = lv::kRowsUnit;
+      a.unit_shift = lv::kRowsUnitShift;
       a.lead = lv::kRowsLead;
       a.min_share = 8;
       a.uncut = 24;
@@ -1907,7 +1907,7 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     a.max_tiles = b->max_tiles;
     a.work = b->work;
     a.arrived = b->arrived;
-    a.head = b->head;
+    a.ticket = b->ticket;
     LV_TRY(lv::launch_plan(a, s));
     b->planned = true;
     return st.finish();

@@ -9,23 +9,13 @@ namespace lv {
 
 namespace {
 
-constexpr int kPlanThreads = 256;
-constexpr long long kManyShares = (1 << 11) - 1;   // more than there are CTAs, in 11 bits
+constexpr int kPlanThreads = 256, kCutThreads = 1024;
 constexpr int kMaxRequests = 4096;      // lv_batch_create's limit
+constexpr int kOneLaunch = kPlanOneLaunch;
 
-// Sum over the CTA, to every thread.  ws: one word a warp; a barrier lies between its uses.
-__device__ __forceinline__ long long cta_sum(long long v, long long* ws) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = v;
-  __syncthreads();
-  long long s = 0;
-  for (int w = 0; w < kPlanThreads / 32; ++w) s += ws[w];
-  return s;
-}
-
-// Exclusive prefix over the CTA; *total receives the sum.
+// Exclusive prefix over the CTA of NT threads; *total receives the sum.  ws: a word a warp; a barrier
+// lies between its uses.
+template <int NT>
 __device__ __forceinline__ long long cta_scan(long long v, long long* ws, long long* total) {
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   long long x = v;
@@ -37,53 +27,151 @@ __device__ __forceinline__ long long cta_scan(long long v, long long* ws, long l
   __syncthreads();
   if (lane == 31) ws[wid] = x;
   __syncthreads();
-  long long before = 0, sum = 0;
-  for (int w = 0; w < kPlanThreads / 32; ++w) {
-    if (w < wid) before += ws[w];
-    sum += ws[w];
+  // every warp scans the warps' sums
+  const long long own = lane < NT / 32 ? ws[lane] : 0;
+  long long y = own;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long z = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) y += z;
   }
-  *total = sum;
-  return before + x - v;
+  *total = __shfl_sync(0xffffffffu, y, 31);
+  return __shfl_sync(0xffffffffu, y - own, wid) + x - v;
+}
+template <int NT>
+__device__ __forceinline__ long long cta_sum(long long v, long long* ws) {
+  long long total;
+  cta_scan<NT>(v, ws, &total);
+  return total;
 }
 
+// (32-bit divisions: len * G is below 2^31)
 __device__ __forceinline__ int tiles_of(const PlanArgs& a, int len) {
-  return len > 0 ? (int)(((long long)len * a.G + a.tile_rows - 1) / a.tile_rows) : 0;
+  return len > 0 ? (int)(((uint32_t)len * (uint32_t)a.G + (uint32_t)a.tile_rows - 1u) / (uint32_t)a.tile_rows) : 0;
 }
 
 __device__ __forceinline__ AttnTile make_tile(const PlanArgs& a, const PlanReq& r, int req, int k) {
+  const int up = (1 << a.unit_shift) - 1;
   AttnTile t;
   t.before = 0;
   t.req = req;
   t.row0 = k * a.tile_rows;
-  const int all = r.len * a.G;
-  t.rows = min(a.tile_rows, all - t.row0);
+  t.rows = min(a.tile_rows, r.len * a.G - t.row0);
   t.first = r.first;
   t.qrow = r.qrow;
-  t.kv_hi = r.first + (t.row0 + t.rows - 1) / a.G + 1;
-  const int p0 = r.first + t.row0 / a.G;
+  t.kv_hi = r.first + (int)((uint32_t)(t.row0 + t.rows - 1) / (uint32_t)a.G) + 1;
+  const int p0 = r.first + (int)((uint32_t)t.row0 / (uint32_t)a.G);
   t.kv_lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
-  const int hi = (t.kv_hi + a.unit - 1) / a.unit;
-  t.sink_units = min((min(a.sinks, t.kv_lo) + a.unit - 1) / a.unit, hi);
-  t.win_unit = max(t.kv_lo / a.unit, t.sink_units);
+  const int hi = (t.kv_hi + up) >> a.unit_shift;
+  t.sink_units = min((min(a.sinks, t.kv_lo) + up) >> a.unit_shift, hi);
+  t.win_unit = max(t.kv_lo >> a.unit_shift, t.sink_units);
   t.units = t.sink_units + hi - t.win_unit;
   return t;
 }
 
+// One CTA of NT threads cuts the requests into tiles and the tiles' units into shares.
+template <int NT>
+__device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* first_tile) {
+  // each request's first tile: a scan over the requests, a thread taking several in a row
+  const int per = (a.n + NT - 1) / NT, q0 = min((int)threadIdx.x * per, a.n), q1 = min(q0 + per, a.n);
+  long long own = 0, tiles, live = 0;
+  for (int q = q0; q < q1; ++q) {
+    const int len = __ldcg(&a.reqs[q].len);
+    first_tile[q] = tiles_of(a, len);
+    own += first_tile[q];
+    live += len;
+  }
+  long long at_tile = cta_scan<NT>(own, ws, &tiles);
+  for (int q = q0; q < q1; ++q) {
+    const int m = first_tile[q];
+    first_tile[q] = (int)min(at_tile, (long long)a.max_tiles);
+    at_tile += m;
+  }
+  live = cta_sum<NT>(live, ws);      // (with a barrier after the writes above)
+  const int n_tiles = (int)min(tiles, (long long)a.max_tiles);
+  // the tiles, a thread several in a row (its first one's request found by bisection), and where
+  // they lie on the line: what comes before each in units, and in short and long shares
+  const int per_tile = (n_tiles + NT - 1) / NT;
+  const int t0 = min((int)threadIdx.x * per_tile, n_tiles), t1 = min(t0 + per_tile, n_tiles);
+  int req0 = 0;
+  if (t0 < t1) {
+    int hi = a.n - 1;      // the last request whose first tile is not after t0
+    while (req0 < hi) {
+      const int mid = (req0 + hi + 1) >> 1;
+      if (first_tile[mid] <= t0) req0 = mid;
+      else hi = mid - 1;
+    }
+  }
+  auto each_tile = [&](auto&& f) {
+    int q = req0, loaded = -1;
+    PlanReq r{};
+    for (int t = t0; t < t1; ++t) {
+      while (q + 1 < a.n && first_tile[q + 1] <= t) ++q;
+      if (q != loaded) {
+        const int4 w = __ldcg(reinterpret_cast<const int4*>(&a.reqs[q]));
+        r = PlanReq{w.x, w.y, w.z, 0};
+        loaded = q;
+      }
+      f(t, make_tile(a, r, q, t - first_tile[q]));
+    }
+  };
+  long long my_units = 0, my_short = 0, my_long = 0;
+  bool cut_free = true;      // no pair has more units than one CTA may well take
+  each_tile([&](int, const AttnTile& t) {
+    my_units += t.units;
+    my_short += (uint32_t)(t.units + a.min_share - 1) / (uint32_t)a.min_share;
+    my_long += (uint32_t)(t.units + a.uncut - 1) / (uint32_t)a.uncut;
+    cut_free &= t.units <= a.uncut;
+  });
+  long long units, shorts = 0, longs = 0, at_short = 0, at_long = 0;
+  const long long at_unit = cta_scan<NT>(my_units, ws, &units);
+  const bool few = (long long)n_tiles * a.line_heads <= a.shares;      // (or no pair has shares of its own)
+  if (few) {
+    at_short = cta_scan<NT>(my_short, ws, &shorts);
+    at_long = cta_scan<NT>(my_long, ws, &longs);
+    cut_free = __syncthreads_and(cut_free);
+  }
+  // Pairs apart in shares of their own: uncut ones of up to `uncut` units where that holds them all,
+  // else cut short (a cut costs what some 8 units of a warp do, so in the middle there is nothing).
+  const long long needed = cut_free ? longs : shorts;
+  const bool apart = few && needed * a.line_heads <= a.shares;
+  const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
+  units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
+  const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
+  const int dead = a.num_tokens - (int)live;
+  // (zero already but after an attention that ran out of a wait)
+  static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
+  for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += NT)
+    reinterpret_cast<int4*>(a.arrived)[i] = make_int4(0, 0, 0, 0);
+  long long before = apart ? (cut_free ? at_long : at_short) * size : at_unit + (long long)t0 * lead;
+  long long c = -1;      // the next share to begin
+  each_tile([&](int t, AttnTile tile) {
+    const int stretch = stretch_of(tile.units, lead, (int)share);
+    tile.before = before * a.line_heads;
+    a.tiles[t] = tile;
+    const long long hi = tile.before + (long long)stretch * a.line_heads;
+    if (c < 0) c = (tile.before + share - 1) / share;
+    for (; c * share < hi; ++c)
+      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), (int)share, lead, t, dead};
+    before += stretch;
+  });
+  for (c = (units + share - 1) / share + threadIdx.x; c < a.shares; c += NT)
+    a.work[c] = CtaWork{AttnTile{}, 0, 0, (int)share, lead, 0, dead};
+}
+
 // CTA i < n: request i's rows, table row and checks; CTA n: the rows of no request.  Every CTA
 // sums the lengths before its own (at most 16 KiB that stay in L2: less than a launch between
-// a scan and the rest would cost).  The CTA that finishes last cuts the requests into tiles
-// and the tiles' units into equal shares.
-__global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
+// a scan and the rest would cost).  kCut: the CTA that finishes last cuts the line too.
+template <bool kCut>
+__global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_constant__ PlanArgs a) {
   __shared__ long long ws[kPlanThreads / 32];
-  __shared__ int last;
-  __shared__ int first_tile[kMaxRequests];
   dep_wait();
   dep_trigger();
   const int i = blockIdx.x;
   const DevPool& p = a.p;
   long long mine = 0;
   for (int j = threadIdx.x; j < i; j += kPlanThreads) mine += max(a.lens[j], 0);
-  const long long start = cta_sum(mine, ws);
+  const long long start = cta_sum<kPlanThreads>(mine, ws);
   const int row0 = (int)min(start, (long long)a.num_tokens);
   if (threadIdx.x == 0) a.row_starts[i] = row0;
   if (i == a.n) {
@@ -153,84 +241,28 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_plan(PlanArgs a) {
       a.slots[row0 + r] = slot;
     }
   }
+  if constexpr (kCut) {
+    __shared__ int last;
+    __shared__ int first_tile[kOneLaunch];
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
+      if (last) *a.ticket = 0;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    cut_line<kPlanThreads>(a, ws, first_tile);
+  }
+}
 
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(&a.head->ticket, 1) == (int)gridDim.x - 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  // each request's first tile: a scan over the requests
-  long long tiles = 0, live = 0;
-  for (int base = 0; base < a.n; base += kPlanThreads) {
-    const int q = base + threadIdx.x;
-    const int len = q < a.n ? __ldcg(&a.reqs[q].len) : 0;
-    long long total;
-    const long long at = cta_scan(tiles_of(a, len), ws, &total);
-    if (q < a.n) first_tile[q] = (int)min(tiles + at, (long long)a.max_tiles);
-    tiles += total;
-    live += len;
-  }
-  live = cta_sum(live, ws);
-  const int n_tiles = (int)min(tiles, (long long)a.max_tiles);
-  // the tiles, a thread each (its request found by bisection), and where they lie on the line
-  long long units = 0, shorts = 0, longs = 0;
-  bool cut_free = true;      // no pair has more units than one CTA may well take
-  for (int base = 0; base < n_tiles; base += kPlanThreads) {
-    const int t = base + threadIdx.x;
-    AttnTile tile{};
-    if (t < n_tiles) {
-      int lo = 0, hi = a.n - 1;      // the last request whose first tile is not after t
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (first_tile[mid] <= t) lo = mid;
-        else hi = mid - 1;
-      }
-      const int4 r = __ldcg(reinterpret_cast<const int4*>(&a.reqs[lo]));
-      tile = make_tile(a, PlanReq{r.x, r.y, r.z, 0}, lo, t - first_tile[lo]);
-    }
-    long long total;
-    const long long at = cta_scan(t < n_tiles ? tile.units : 0, ws, &total);
-    long long total_short, total_long;
-    const long long at_short =
-        cta_scan(t < n_tiles ? (tile.units + a.min_share - 1) / a.min_share : 0, ws, &total_short);
-    const long long at_long = cta_scan(t < n_tiles ? (tile.units + a.uncut - 1) / a.uncut : 0, ws, &total_long);
-    if (t < n_tiles) {
-      // what comes before it, in units, in short shares (from bit 40 on) and in long ones (from 51)
-      tile.before = units + at + (min(shorts + at_short, kManyShares) << 40) + (min(longs + at_long, kManyShares) << 51);
-      a.tiles[t] = tile;
-      cut_free &= tile.units <= a.uncut;
-    }
-    units += total;
-    shorts += total_short;
-    longs += total_long;
-  }
-  // Pairs apart in shares of their own: uncut ones of up to `uncut` units where that holds them all,
-  // else cut short (a cut costs what some 8 units of a warp do, so in the middle there is nothing).
-  cut_free = __syncthreads_and(cut_free);
-  const long long needed = cut_free ? longs : shorts;
-  const bool apart = needed * a.line_heads <= a.shares;
-  const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
-  units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
-  const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
-  const int dead = a.num_tokens - (int)live;
-  if (threadIdx.x == 0) a.head->ticket = 0;
-  // (zero already but after an attention that ran out of a wait)
-  static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
-  for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += kPlanThreads)
-    reinterpret_cast<int4*>(a.arrived)[i] = make_int4(0, 0, 0, 0);
-  __syncthreads();
-  for (int t = threadIdx.x; t < n_tiles; t += kPlanThreads) {
-    AttnTile tile = a.tiles[t];      // (this thread's own)
-    tile.before = apart ? (tile.before >> (cut_free ? 51 : 40) & kManyShares) * size * a.line_heads
-                        : ((tile.before & ((1ll << 40) - 1)) + (long long)t * lead) * a.line_heads;
-    a.tiles[t].before = tile.before;
-    const long long lo = tile.before, hi = lo + (long long)stretch_of(tile.units, lead, (int)share) * a.line_heads;
-    for (long long c = (lo + share - 1) / share; c * share < hi; ++c)
-      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), (int)share, lead, t, dead};
-  }
-  for (long long c = (units + share - 1) / share + threadIdx.x; c < a.shares; c += kPlanThreads)
-    a.work[c] = CtaWork{AttnTile{}, 0, 0, (int)share, lead, 0, dead};
+__global__ void __launch_bounds__(kCutThreads) k_batch_cut(const __grid_constant__ PlanArgs a) {
+  __shared__ long long ws[kCutThreads / 32];
+  __shared__ int first_tile[kMaxRequests];
+  dep_wait();
+  dep_trigger();
+  cut_line<kCutThreads>(a, ws, first_tile);
 }
 
 // ---------------------------------------------------------------- KV write
@@ -314,8 +346,13 @@ __global__ void __launch_bounds__(kWriteThreads) k_kv_write(const __grid_constan
 
 }  // namespace
 
+// One launch up to kOneLaunch requests (64 decoding sessions: 8.8 us, in two 10.2), else one CTA of
+// 1024 threads cuts the line by itself (1024 requests: 17 us; by the last CTA of the rows' 24).
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t s) {
-  return launch_dependent(k_batch_plan, dim3(a.n + 1), kPlanThreads, 0, s, a);
+  if (a.n <= kOneLaunch) return launch_dependent(k_batch_rows<true>, dim3(a.n + 1), kPlanThreads, 0, s, a);
+  const cudaError_t e = launch_dependent(k_batch_rows<false>, dim3(a.n + 1), kPlanThreads, 0, s, a);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(k_batch_cut, dim3(1), kCutThreads, 0, s, a);
 }
 
 // One unit a thread while the GPU holds all of them at once, else two: 64 rows of 4 heads of 128

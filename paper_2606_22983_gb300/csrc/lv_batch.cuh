@@ -47,12 +47,7 @@ struct CtaWork {        // what a CTA starts from
 };
 static_assert(sizeof(CtaWork) == 80, "read as five 16-byte words");
 
-struct PlanHead {
-  int32_t ticket;       // CTAs of the plan that are done
-  int32_t pad[3];
-};
-
-struct PlanReq {        // per request, from the plan's first half to its second
+struct PlanReq {        // per request, from the plan's first kernel to its second
   int32_t first, len, qrow, pad;   // len 0: left out
 };
 
@@ -64,7 +59,7 @@ struct PlanArgs {
   int32_t n, num_tokens, max_len;
   int32_t G;               // query heads a KV head
   int32_t line_heads;      // KV heads in a line: all, or 1
-  int32_t tile_rows, unit; // of the attention kernel that will run
+  int32_t tile_rows, unit_shift;   // of the attention kernel that will run (its unit's log2)
   int32_t lead;            // places of the line ahead of a pair's units
   int32_t min_share;       // places a CTA takes at least
   int32_t uncut;           // units of a pair that is better not cut
@@ -81,7 +76,7 @@ struct PlanArgs {
   int32_t max_tiles;
   CtaWork* work;           // [shares]
   int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
-  PlanHead* head;
+  int32_t* ticket;         // CTAs of the plan that are done, zero between calls
 };
 
 struct WriteArgs {
@@ -136,16 +131,17 @@ __host__ __device__ inline int64_t part_slot(int64_t cta, bool starts) { return 
 
 enum AttnKind : int { ATTN_ROWS = 0, ATTN_TC = 1 };
 
+constexpr int kPlanOneLaunch = 256;      // requests up to which a plan is one launch
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t s);
 cudaError_t launch_kv_write(const WriteArgs& a, cudaStream_t s, int num_sms);
 cudaError_t configure_attend();
 cudaError_t configure_attend_tc();
 // keys of a unit, and CTAs that an SM holds, of the rows kernel
-constexpr int kRowsUnit = 16, kRowsRows = 16;
+constexpr int kRowsUnitShift = 4, kRowsUnit = 1 << kRowsUnitShift, kRowsRows = 16;
 int attend_rows_ctas(int dp);
 cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16,
                                int ctas, cudaStream_t s);      // maps: boxes of 64 columns and a unit's keys, or null
-constexpr int kTcUnit = 128, kTcRows = 256;
+constexpr int kTcUnitShift = 7, kTcUnit = 1 << kTcUnitShift, kTcRows = 256;
 // places ahead of a pair's units: what a pair costs besides its units, in units
 constexpr int kRowsLead = 16, kTcLead = 2;
 // packed rows of a tile: two halves of whole tokens

@@ -480,3 +480,20 @@ def test_refusals():
         s.check(b.attention(0, s.q), None, 0, 0.125)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 700])
+def test_plan_of_many_requests(n):
+    """On both sides of the size from which the plan is two kernels."""
+    rng = np.random.default_rng(n)
+    new = rng.integers(0, 4, n)
+    new[rng.integers(0, n)] = 37
+    s = Step(rng.integers(0, 90, n).tolist(), new.tolist(), heads=2, group=2, dim=16, pad=3)
+    try:
+        s.plan()
+        assert s.pool.sync(raise_on_error=False) == 0
+        _check_plan(s, _plan_by_hand(s))
+        out, lse = s.batch.attention(1, s.q, return_lse=True)
+        s.check(out, lse, 1, 0.25)
+    finally:
+        s.close()
