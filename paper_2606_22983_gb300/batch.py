@@ -52,6 +52,9 @@ class KVBatch:
         self._device = self.row_starts.get_device()
         self._scale = 1.0 / math.sqrt(pool.head_dim)
         self._a, self._b = lv.lv_heads(), lv.lv_heads()      # a call's two tensor arguments
+        # an output that attention() makes itself
+        self._own = lv.lv_heads(row_stride=q_heads * pool.head_dim, head_stride=pool.head_dim,
+                                dtype=_KINDS[dtype])
         d = lv.lv_batch_desc(num_q_heads=q_heads, max_requests=max_requests, max_tokens=max_tokens,
                              dtype=_KINDS[dtype], window=window, sinks=sinks,
                              row_starts=self.row_starts.data_ptr(), kv_lens=self.kv_lens.data_ptr(),
@@ -130,19 +133,21 @@ class KVBatch:
         no request give zeros (and -inf).  scale: 1 / sqrt(head_dim) unless given.  With a stream
         other than the current one, the caller orders the two."""
         q_arg = self._put(self._a, q, self.q_heads, "q")
-        rows = q.shape[0]
-        past = rows - self.num_tokens            # rows that the step does not have
+        lse = None
         if out is None:
             out = torch.empty_like(q) if q.is_contiguous() and q.dtype is self.dtype else \
                 torch.empty(q.shape, dtype=self.dtype, device=q.device)
-            if past:
+            out_arg = self._own
+            out_arg.data = out.data_ptr()
+            if len(out) > self.num_tokens:       # rows that the step does not have
                 out[self.num_tokens:].zero_()
-        lse = None
+        else:
+            out_arg = self._put(self._b, out, self.q_heads, "out")
         if return_lse:
-            lse = torch.empty((rows, self.q_heads), dtype=torch.float32, device=q.device)
-            if past:
+            lse = torch.empty((len(q), self.q_heads), dtype=torch.float32, device=q.device)
+            if len(q) > self.num_tokens:
                 lse[self.num_tokens:].fill_(-math.inf)
-        lv.lv_attention(self.handle, layer, q_arg, self._put(self._b, out, self.q_heads, "out"), lse,
-                        self._scale if scale is None else scale, self._stream(stream))
+        lv.lv_attention(self.handle, layer, q_arg, out_arg, lse, self._scale if scale is None else scale,
+                        self._stream(stream))
         self.pool.launches += 1
         return (out, lse) if return_lse else out
