@@ -1982,7 +1982,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.o_row = out->row_stride;
   a.o_head = out->head_stride;
   a.q_vec = heads_aligned(q, 16) ? 1 : 0;
-  a.o_vec = heads_aligned(out, 16) ? 1 : 0;
+  a.o_vec = heads_aligned(out, 32) && a.D % 16 == 0 ? 2 : heads_aligned(out, 16) ? 1 : 0;
   a.num_tokens = b->num_tokens;
   a.window = b->d.window;
   a.sinks = b->d.sinks;

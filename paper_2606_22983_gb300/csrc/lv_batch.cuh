@@ -107,7 +107,7 @@ struct AttnArgs {
   uint8_t* out;
   float* lse;
   int64_t q_row, q_head, o_row, o_head;   // strides in elements
-  int32_t q_vec, o_vec;    // 16-byte accesses allowed
+  int32_t q_vec, o_vec;    // 16-byte accesses allowed (o_vec 2: of 32 bytes, D a multiple of 16)
   int32_t num_tokens;
   int32_t window, sinks;
   int32_t tile_rows;       // rows of a partial result's slot

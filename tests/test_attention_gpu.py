@@ -90,3 +90,23 @@ def test_neighbouring_long_joins(heads, new):
                 _attend(s)
         finally:
             s.close()
+
+
+@pytest.mark.parametrize("new", [[1, 3], [70, 1, 33]])
+@pytest.mark.parametrize("dim", [64, 128, 72])
+@pytest.mark.parametrize("offset,gap", [(0, 0), (8, 0), (16, 16), (24, 8), (3, 5)])
+def test_output_alignments(offset, gap, dim, new):
+    """Outputs whose rows lie at any offset and stride; what is beside them is left alone."""
+    import torch
+    s = _step([40] * len(new), new, heads=2, group=4, dim=dim)
+    s.plan()
+    Hq = 8
+    row = Hq * (dim + gap) + gap
+    buf = torch.full((offset + s.rows * row + 64,), 7.0, dtype=s.dtype, device="cuda")
+    out = buf[offset:].as_strided((s.rows, Hq, dim), (row, dim + gap, 1))
+    assert s.batch.attention(0, s.q, out=out) is out
+    assert s.pool.sync(raise_on_error=False) == 0
+    s.check(out, None, 0, dim ** -0.5)
+    out.fill_(7.0)
+    assert (buf == 7.0).all()
+    s.close()
