@@ -1,7 +1,5 @@
 // Attention of requests with few rows (single tokens of a reply, drafts to verify) over the
 // paged context (see lv_batch.cuh for how the work is cut).
-#include <type_traits>
-
 #include "lv_batch.cuh"
 
 namespace lv {
@@ -213,6 +211,15 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
 // 114 pieces of a context of 60 000 keys).
 constexpr int kAlone = 32, kGroup = 12;
 
+// o = sum_j w_j v_j / sum_j w_j with w_j = 2^(c q.k_j - m), c = scale log2(e): over each unit of 16 keys with
+// the maximum m so far, the sums rescaled when it grows; pieces with sums (O, l) and maximum m join as
+// sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
+// What bounds it: the cache's bytes (16 flops a byte with 8 heads a KV head).  61 tokens over 2 to 16 k keys
+// each, 4 KV heads of 128: 0.82 GB in 139 us, 5.9 TB/s; 16 tokens over 33 to 65 k: 1.5 GB in 233 to 242 us, 6.3 to 6.5.
+// Some SMs read at a rate up to 15 % below others'; twice to four times as many shares, for CTAs to even that out,
+// took more for their begins and ends (64 tokens of a 4000-key window 80 us, 89 to 99).  Three CTAs of
+// four warps an SM: 61 tokens 202 us with one of them, 141 with three.
+//
 // One CTA: its share of one KV head's line.  Its four warps take a tile's units in turn and are joined at the
 // tile's end; each streams its units' K and V rows through a ring of its own, so no barrier of the
 // CTA lies in the loop.  S = Q K^T (16 rows x 16 keys a step), the running maximum and sum of the

@@ -69,7 +69,10 @@ __device__ __forceinline__ AttnTile make_tile(const PlanArgs& a, const PlanReq& 
   return t;
 }
 
-// One CTA of NT threads cuts the requests into tiles and the tiles' units into shares.
+// One CTA of NT threads cuts the requests into tiles and the tiles' units into shares: prefix sums over
+// the requests' tiles and over the tiles' units, a thread taking several in a row, so that a tile is made
+// twice (once to be counted, once to be written) rather than kept.  What bounds it is the chain: four
+// scans of two barriers each, some 5 us for 64 requests of one tile and 10 for 1024.
 template <int NT>
 __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* first_tile) {
   // each request's first tile: a scan over the requests, a thread taking several in a row
@@ -159,7 +162,12 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
     a.work[c] = CtaWork{AttnTile{}, 0, 0, (int)share, lead, 0, dead};
 }
 
-// CTA i < n: request i's rows, table row and checks; CTA n: the rows of no request.  Every CTA
+// CTA i < n: request i's rows, table row and checks; CTA n: the rows of no request.
+//   row_start_i = sum of len_j over j < i;  position of row r: first_i + r - row_start_i;
+//   slot: table[sid][position / T] * T + position % T
+// It reads the tables once and writes them once, 8 KiB a request of 16 000 tokens, and 12 bytes a row:
+// latency bounds it, not bytes (64 requests with the cut of their work 9.2 us, 1024 in two launches 17.4).
+// Every CTA
 // sums the lengths before its own (at most 16 KiB that stay in L2: less than a launch between
 // a scan and the rest would cost).  kCut: the CTA that finishes last cuts the line too.
 template <bool kCut>
@@ -269,7 +277,9 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut(const __grid_constant
 // A unit is 8 elements, out[slot][h][8c..] <- src[r][h][8c..]; a row's are those of K, then V's.  A
 // CTA takes kWriteThreads * U of them in a row, a thread U with all its loads on their way before
 // the first store.
-// What bounds it: the launch for a decode step; HBM for prompts' rows.
+// What bounds it: the launch for a decode step (64 rows of 4 heads of 128, 1.9 us); HBM for prompts' rows
+// (13 706 of them from 32 to 16 bits, 84 MB in and out, 10.7 us, some of it from L2).  Each row's K and V are
+// read and written once: 2 H D (source bytes + 2), and the 8 bytes of its slot.  Rounding is to nearest even.
 constexpr int kWriteThreads = 256;
 
 template <bool kBf16>
