@@ -640,7 +640,17 @@ lv_status lv_schedule(lv_pool* pool, const lv_sched_params* params, const lv_req
    row_starts, kv_lens, tables, positions and slots are the caller's device arrays (kept
    alive until the batch is destroyed); lv_batch_plan writes them and the other calls read
    them, so that the caller's own kernels may use them too.  The calls of one batch must be
-   ordered with respect to each other; distinct batches are independent. */
+   ordered with respect to each other; distinct batches are independent.
+
+   Stream capture.  Captured lv_kv_write and lv_attention calls work on the step that the device
+   planned last when they are replayed, by a later lv_batch_plan, captured or not.  What they keep
+   from the plan before their capture is num_tokens, the rows of their tensors, and the kernel of
+   the attention, which lv_batch_plan chooses by whether min(max_len, num_tokens) * Hq / H is
+   above 16.  They may be replayed after a plan of no more rows (the rows past its num_tokens are
+   of no request) that chooses the same kernel; after another they do nothing, and the device
+   reports LV_ERR_STATE with detail -1 (lv_kv_write only where the plan has more rows).  A captured
+   lv_batch_plan keeps n, num_tokens and max_len, and reads sids, firsts and lens when it is
+   replayed. */
 enum { LV_BF16 = 1, LV_F16 = 2, LV_F32 = 3 };
 
 typedef struct lv_batch lv_batch;   /* opaque */

@@ -10,7 +10,10 @@ both -- whose room in the context a turn or ``KVPool.append`` has made:
         out = batch.attention(layer, q)
 
 ``row_starts``, ``kv_lens``, ``tables``, ``positions`` and ``slots`` are device tensors that
-``plan`` fills.  PyTorch holds the memory; every operation is a liblv call on the given stream (None:
+``plan`` fills.  A captured ``write`` or ``attention`` works on the step planned last when it is replayed;
+it keeps the rows and the attention's kernel (chosen from the rows a request) of the plan before its
+capture, and does nothing but report LV_ERR_STATE where a later plan has more rows or the other kernel:
+plan with the same ``num_tokens`` and ``max_len`` each time.  PyTorch holds the memory; every operation is a liblv call on the given stream (None:
 the pool's, or the current one).
 """
 from __future__ import annotations

@@ -1647,6 +1647,7 @@ struct lv_batch {
   lv::CtaWork* work = nullptr;
   int32_t* arrived = nullptr;
   int32_t* ticket = nullptr;
+  lv::StepHead* head = nullptr;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
   int32_t G = 1;             // query heads a KV head
@@ -1791,14 +1792,16 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
-        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
+        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->head, 1)) != LV_OK ||
+        (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
         (st = batch_alloc(b, &b->part_ml, rows)) != LV_OK)
       return fail(st);
   } catch (const std::bad_alloc&) {
     return fail(LV_ERR_OOM);
   }
   // (waits: the batch may be used on any stream next)
-  if (cudaMemset(b->ticket, 0, sizeof(int32_t)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
+  if (cudaMemset(b->ticket, 0, sizeof(int32_t)) != cudaSuccess ||
+      cudaMemset(b->head, 0xff, sizeof(lv::StepHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
     return fail(LV_ERR_CUDA);
   *out = b;
   return LV_OK;
@@ -1865,8 +1868,8 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     // more rows a request than one m16n8k16 tile holds: the kernel for many rows, where pages can be
     // read by TMA (32 sessions of 1000 to 4000 keys with 4 new tokens, 32 rows, took 42 us with it and
     // 115 in tiles of 32 rows of the other; with 1 token, 8 rows, the other reads at 6 TB/s)
-    b->kind = (long long)max_len * b->G > lv::kRowsRows && b->box_rows ? lv::ATTN_TC : lv::ATTN_ROWS;
-    b->num_tokens = num_tokens;
+    const lv::AttnKind kind =
+        (long long)max_len * b->G > lv::kRowsRows && b->box_rows ? lv::ATTN_TC : lv::ATTN_ROWS;
     lv::PlanArgs a{};
     a.p = pool->d;
     a.sids = static_cast<const int32_t*>(si);
@@ -1881,14 +1884,14 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     // longer steps alike; 64 tokens at 1000 keys 19.7, and 22.2 at 6 uncut units.  Few rows: 1000 keys
     // 13.1 us, 14.7 at 16 units, 4000 keys 17.4, 18.6 at 4; 64 sessions of 100 to 300 keys 12.1, and 16.6
     // at 12 uncut units).
-    if (b->kind == lv::ATTN_TC) {
+    if (kind == lv::ATTN_TC) {
       a.line_heads = pool->kv_heads;
       a.tile_rows = lv::tc_tile_rows(b->G);
       a.unit_shift = lv::kTcUnitShift;
       a.lead = lv::kTcLead;
       a.min_share = 3;
       a.uncut = 12;
-      b->ctas = a.shares = pool->num_sms;
+      a.ctas = a.shares = pool->num_sms;
     } else {
       a.line_heads = 1;
       a.tile_rows = lv::kRowsRows;
@@ -1897,9 +1900,8 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
       a.min_share = 8;
       a.uncut = 24;
       a.shares = rows_shares(b);
-      b->ctas = rows_ctas(b);
+      a.ctas = rows_ctas(b);
     }
-    a.ctas = b->ctas;
     a.window = b->d.window;
     a.sinks = b->d.sinks;
     a.row_starts = b->d.row_starts;
@@ -1913,8 +1915,14 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     a.work = b->work;
     a.arrived = b->arrived;
     a.ticket = b->ticket;
+    a.kind = kind;
+    a.head = b->head;
+    b->planned = false;      // (the old step's arrays are being written over)
     LV_TRY(lv::launch_plan(a, s));
     b->planned = true;
+    b->num_tokens = num_tokens;
+    b->kind = kind;
+    b->ctas = a.ctas;
     return st.finish();
   } catch (const std::bad_alloc&) {
     return LV_ERR_OOM;
@@ -1939,6 +1947,7 @@ lv_status lv_kv_write(lv_batch* b, int32_t layer, const lv_heads* k, const lv_he
     a.vec[i] = heads_aligned(src[i], 16) ? 1 : 0;
   }
   a.slots = b->d.slots;
+  a.head = b->head;
   a.num_tokens = b->num_tokens;
   a.H = pool->kv_heads;
   a.D = pool->head_dim;
@@ -1978,6 +1987,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.positions = b->d.positions;
   a.tiles = b->tiles;
   a.work = b->work;
+  a.head = b->head;
   a.arrived = b->arrived;
   a.q = static_cast<const uint8_t*>(q->data);
   a.out = static_cast<uint8_t*>(out->data);

@@ -86,9 +86,9 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 
 // Rows of no request: out = 0, lse = -inf.  Thread i of `of` threads.
 __device__ __forceinline__ void clear_dead(const AttnArgs& a, int i, int of) {
-  const int Hq = a.H * a.G;
+  const int Hq = a.H * a.G, planned = a.head->num_tokens;
   for (int r = i >> 5; r < a.num_tokens; r += of >> 5) {
-    if (a.positions[r] >= 0) continue;
+    if (r < planned && a.positions[r] >= 0) continue;
     for (int h = 0; h < Hq; ++h) {
       uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head;
       for (int d = i & 31; d < a.D; d += 32) o[d] = 0;
@@ -253,6 +253,12 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 
   const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
   const CtaWork work = load_words(&a.work[group]);
+  const StepHead step = load_words(a.head);
+  if (LV_RARE(!step_fits(step, ATTN_ROWS, a.num_tokens))) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
+    return;
+  }
+  const bool dead = step.live < a.num_tokens;
   auto key_of = [&](const AttnTile& t, int u) { return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kU; };
   auto hidden = [&](const AttnTile& t, int key) { return key >= t.kv_hi || (key < t.kv_lo && key >= a.sinks); };
   auto find_page = [&](Walk& x) {
@@ -629,7 +635,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     }
     if (lane == 0) report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
   }
-  if (work.dead > 0) clear_dead(a, blockIdx.x * kThreads + threadIdx.x, gridDim.x * kThreads);
+  if (dead) clear_dead(a, blockIdx.x * kThreads + threadIdx.x, gridDim.x * kThreads);
 }
 
 template <int DP, bool kTma>

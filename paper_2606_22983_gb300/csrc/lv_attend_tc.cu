@@ -307,16 +307,16 @@ struct Pairs {
   int share, lead;
   AttnTile t;
   int tile, head, u0, u1;
-  int dead;
+  // (no pairs where the step is not one that this call may work on)
   __device__ __forceinline__ void init(const AttnArgs& a) {
+    const StepHead step = load_words(a.head);
     const CtaWork x = load_words(&a.work[blockIdx.x]);
     w = x.begin;
-    end = x.end;
+    end = step_fits(step, ATTN_TC, a.num_tokens) ? x.end : x.begin;
     share = x.share;
     lead = x.lead;
     t = x.t;
     tile = x.tile;
-    dead = x.dead;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a) {
     while (w < end) {
@@ -917,10 +917,13 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
       }
       // rows of no request
-      if (ok && pr.dead > 0) {
+      const StepHead step = load_words(a.head);
+      const bool fits = step_fits(step, ATTN_TC, a.num_tokens);
+      if (LV_RARE(!fits) && blockIdx.x == 0 && lane == 0) report(a.ctl, LV_ERR_STATE, -1);
+      if (ok && fits && step.live < a.num_tokens) {
         const int Hq = a.H * a.G;
         for (int r = blockIdx.x; r < a.num_tokens; r += gridDim.x) {
-          if (a.positions[r] >= 0) continue;
+          if (r < step.num_tokens && a.positions[r] >= 0) continue;
           for (int h = 0; h < Hq; ++h) {
             uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head;
             for (int d = lane; d < a.D; d += 32) o[d] = 0;

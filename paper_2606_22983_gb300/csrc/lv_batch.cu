@@ -141,7 +141,7 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
   const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
   units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
   const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
-  const int dead = a.num_tokens - (int)live;
+  if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, 0};
   // (zero already but after an attention that ran out of a wait)
   static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
   for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += NT)
@@ -155,11 +155,11 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
     const long long hi = tile.before + (long long)stretch * a.line_heads;
     if (c < 0) c = (tile.before + share - 1) / share;
     for (; c * share < hi; ++c)
-      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), (int)share, lead, t, dead};
+      a.work[c] = CtaWork{tile, c * share, min(units, (c + 1) * share), (int)share, lead, t, 0};
     before += stretch;
   });
   for (c = (units + share - 1) / share + threadIdx.x; c < a.shares; c += NT)
-    a.work[c] = CtaWork{AttnTile{}, 0, 0, (int)share, lead, 0, dead};
+    a.work[c] = CtaWork{AttnTile{}, 0, 0, (int)share, lead, 0, 0};
 }
 
 // CTA i < n: request i's rows, table row and checks; CTA n: the rows of no request.
@@ -325,6 +325,9 @@ template <bool kBf16, int U>
 __global__ void __launch_bounds__(kWriteThreads) k_kv_write(const __grid_constant__ WriteArgs a) {
   dep_wait();
   dep_trigger();
+  const StepHead head = load_words(a.head);
+  // rows of the planned step, none where it has more than this call's tensors
+  const int rows = head.num_tokens <= a.num_tokens ? head.num_tokens : 0;
   const uint32_t cols = (uint32_t)a.D / 8u, per_kv = (uint32_t)a.H * cols, per_row = 2u * per_kv;
   const uint64_t base = (uint64_t)blockIdx.x * (kWriteThreads * U);
   const uint32_t r0 = (uint32_t)(base / per_row), off0 = (uint32_t)(base - (uint64_t)r0 * per_row);
@@ -339,7 +342,8 @@ __global__ void __launch_bounds__(kWriteThreads) k_kv_write(const __grid_constan
     const bool kv = x >= per_kv;
     const uint32_t y = kv ? x - per_kv : x;
     const uint32_t h = y / cols, c = y - h * cols;
-    const int64_t slot = a.slots[r];
+    const int64_t slot = a.slots[r];      // (asked for beside the step's head)
+    if (r >= (uint32_t)rows) continue;
     if (slot < 0 || slot >= a.num_slots) {
       if (x == 0 && slot != -1) report(a.ctl, slot < 0 ? LV_ERR_STATE : LV_ERR_BOUNDS, r);
       continue;
@@ -352,6 +356,7 @@ __global__ void __launch_bounds__(kWriteThreads) k_kv_write(const __grid_constan
 #pragma unroll
   for (int k = 0; k < U; ++k)
     if (to[k]) *reinterpret_cast<uint4*>(to[k]) = w[k];
+  if (LV_RARE(head.num_tokens > a.num_tokens) && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
 }
 
 }  // namespace

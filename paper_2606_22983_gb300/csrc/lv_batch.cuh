@@ -43,9 +43,21 @@ struct CtaWork {        // what a CTA starts from
   int64_t begin, end;   // its places; begin == end: none
   int32_t share, lead;
   int32_t tile;
-  int32_t dead;         // rows of no request in the step
+  int32_t pad;
 };
 static_assert(sizeof(CtaWork) == 80, "read as five 16-byte words");
+
+// What the step's tables and work list are for, written by the plan after them.  The calls that use them
+// take their kernel and their rows from the plan that the host made last, which in a replayed graph need
+// not be the plan that the device made last: they compare, and do nothing where a list of the other
+// kernel's units or a step of more rows than their tensors have would be read.
+struct StepHead {
+  int32_t kind;         // AttnKind of the work list; -1: nothing planned
+  int32_t num_tokens;   // the plan's; rows past it are of no request whatever positions and slots hold
+  int32_t live;         // rows of requests
+  int32_t pad;
+};
+static_assert(sizeof(StepHead) == 16, "read as one word");
 
 struct PlanReq {        // per request, from the plan's first kernel to its second
   int32_t first, len, qrow, pad;   // len 0: left out
@@ -77,6 +89,8 @@ struct PlanArgs {
   CtaWork* work;           // [shares]
   int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
   int32_t* ticket;         // CTAs of the plan that are done, zero between calls
+  int32_t kind;            // AttnKind
+  StepHead* head;
 };
 
 struct WriteArgs {
@@ -86,6 +100,7 @@ struct WriteArgs {
   int32_t src_type[2];
   int32_t vec[2];          // 16-byte loads allowed
   const int64_t* slots;
+  const StepHead* head;
   int32_t num_tokens, H, D, dtype;
   int64_t num_slots;       // hbm_pages * T
   long long* ctl;
@@ -102,6 +117,7 @@ struct AttnArgs {
   const int32_t* positions;
   const AttnTile* tiles;
   const CtaWork* work;
+  const StepHead* head;
   int32_t* arrived;
   const uint8_t* q;
   uint8_t* out;
@@ -187,6 +203,10 @@ __device__ __forceinline__ int add_release(int32_t* p, int v) {
   int was;
   asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(was) : "l"(p), "r"(v) : "memory");
   return was;
+}
+// True where the step on the device is one that an attention over num_tokens rows may work on.
+__device__ __forceinline__ bool step_fits(const StepHead& head, int kind, int num_tokens) {
+  return head.kind == kind && head.num_tokens <= num_tokens;
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
