@@ -772,6 +772,12 @@ lv_status lv_timing_read(lv_pool* pool, lv_kernel_timing* out /* [LV_TIMING_KIND
 enum { LV_FAULT_NONE = 0, LV_FAULT_HOST_ALLOC = 1, LV_FAULT_HBM_ALLOC = 2, LV_FAULT_COPY = 3 };
 lv_status lv_inject_fault(lv_pool* pool, int32_t kind, int32_t after);
 lv_status lv_selftest_wait(lv_pool* pool, int64_t limit_us, lv_stream stream);
+/* The same inside the attention kernels: in the batch's later lv_attention calls every second CTA
+   waits for copies (LV_HOLD_COPIES; only pages that are read by TMA are waited for), or for a pair's
+   last product (LV_HOLD_PRODUCTS; the kernel of many rows), that are never counted as done, with
+   a limit of limit_us (1000 to 1000000) a wait.  LV_HOLD_NONE: as usual again. */
+enum { LV_HOLD_NONE = 0, LV_HOLD_COPIES = 1, LV_HOLD_PRODUCTS = 2 };
+lv_status lv_selftest_attention(lv_batch* batch, int32_t what, int64_t limit_us);
 
 /* ------------------------------------------------------ preload controller */
 

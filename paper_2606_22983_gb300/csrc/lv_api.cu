@@ -1661,6 +1661,9 @@ struct lv_batch {
   int32_t num_tokens = 0;
   lv::AttnKind kind = lv::ATTN_ROWS;
   int32_t ctas = 0;
+  // lv_selftest_attention
+  int32_t hold = LV_HOLD_NONE;
+  long long wait_ns = lv::kAttnWaitNs;
 };
 
 namespace {
@@ -2007,6 +2010,8 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.part_o = b->part_o;
   a.part_ml = b->part_ml;
   a.ctl = pool->d.ctl;
+  a.wait_ns = b->wait_ns;
+  a.hold = b->hold;
   if (tc) {
     CUtensorMap qmap;
     const lv::TcMaps m{&b->maps[2 * layer], &b->maps[2 * layer + 1],
@@ -2016,6 +2021,15 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
     const CUtensorMap* m = b->rows_maps.empty() ? nullptr : &b->rows_maps[2 * layer];
     LV_TRY(lv::launch_attend_rows(a, m, m ? m + 1 : nullptr, bf16, b->ctas, s));
   }
+  return LV_OK;
+}
+
+lv_status lv_selftest_attention(lv_batch* b, int32_t what, int64_t limit_us) {
+  NvtxRange nvtx_range("lv_selftest_attention");
+  if (!b || what < LV_HOLD_NONE || what > LV_HOLD_PRODUCTS) return LV_ERR_INVALID;
+  if (what != LV_HOLD_NONE && (limit_us < 1000 || limit_us > 1000000)) return LV_ERR_INVALID;
+  b->hold = what;
+  b->wait_ns = what == LV_HOLD_NONE ? lv::kAttnWaitNs : limit_us * 1000;
   return LV_OK;
 }
 

@@ -9,7 +9,6 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kU = kRowsUnit;
-constexpr long long kWaitLimitNs = 1000000000ll;   // one second a wait
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -244,7 +243,9 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   const uint32_t tok = (uint32_t)a.H * a.D * 2;     // bytes from a token's row to the next
   if (kTma) {
     if (lane < S::kStages)
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_s + 8 * lane) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar_s + 8 * lane),
+                   "r"(arrivals_of(a, LV_HOLD_COPIES))
+                   : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
   }
@@ -348,7 +349,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   int stage = 0;
   uint32_t par = 0;
   int cuts = 0, was_first = 0, was_last = 0;      // (counts: thread 0's)
-  bool bad = false;          // a wait ran out: the rest is done without waiting, and reported
+  bool bad = false;          // a wait ran out: the rest is done without copies and waits, and reported
 
   for (bool go = any; go; go = next_pair(C)) {
     // ---- queries of this pair's head: packed rows lane / 4 + 8 i
@@ -395,9 +396,10 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         if (!ok) {
           const unsigned long long t0 = now_ns();
           while (!(ok = bar_try(bar_s + 8 * stage, par)))
-            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+            if ((long long)(now_ns() - t0) > a.wait_ns) break;
         }
         bad = bad || !__all_sync(0xffffffffu, ok);
+        more = more && !bad;      // (the stage's barrier is still in its old phase)
         if (key0 + kU > C.t.kv_hi || (key0 < C.t.kv_lo && key0 + kU > a.sinks)) {
           // V rows that no row sees hold whatever the page does: zeros, since a weight of zero does
           // not cancel a NaN
@@ -631,7 +633,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     for (long long i = loads < S::kStages ? 0 : loads - S::kStages; i < loads; ++i) {
       const unsigned long long t0 = now_ns();
       while (!bar_try(bar_s + 8 * (int)(i % S::kStages), (uint32_t)(i / S::kStages) & 1u))
-        if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+        if ((long long)(now_ns() - t0) > a.wait_ns) break;
     }
     if (lane == 0) report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
   }

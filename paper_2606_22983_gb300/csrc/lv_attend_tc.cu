@@ -16,7 +16,6 @@ constexpr int kKeys = kTcUnit;            // keys of a unit
 // registers a thread: 168 at launch (384 * 168 = 64 512), then 208 for the softmax warps and 88
 // for the others (256 * 208 + 128 * 88 = 64 512)
 constexpr int kRegsSoft = 208, kRegsOther = 88;
-constexpr long long kWaitLimitNs = 1000000000ll;   // one second a wait
 
 template <int DP>
 struct TcShape {
@@ -69,27 +68,28 @@ __device__ __forceinline__ unsigned long long now_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// False once the limit has passed, here or in another role: every role then leaves its loop.
-__device__ __forceinline__ bool bar_wait_slow(Bars* b, uint64_t* bar, uint32_t parity) {
+// False once the limit has passed, here or in another role: every role then leaves its loop.  (The limit is
+// a kernel argument: kept in shared memory beside the barriers, it cost 8 prompts of 4096 742 us for 718.)
+__device__ __forceinline__ bool bar_wait_slow(Bars* b, uint64_t* bar, uint32_t parity, long long limit) {
   const unsigned long long t0 = now_ns();
   for (;;) {
     if (bar_try(bar, parity)) return true;
     if (b->bad) return false;
-    if ((long long)(now_ns() - t0) > kWaitLimitNs) {
+    if ((long long)(now_ns() - t0) > limit) {
       b->bad = 1;
       return false;
     }
   }
 }
 // For one thread.
-__device__ __forceinline__ bool bar_wait1(Bars* b, uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait1(Bars* b, uint64_t* bar, uint32_t parity, long long limit) {
   if (LV_MOSTLY(bar_try(bar, parity))) return true;
-  return bar_wait_slow(b, bar, parity);
+  return bar_wait_slow(b, bar, parity, limit);
 }
 // For a whole warp, whose lanes leave it together with one answer (what follows is .aligned).
-__device__ __forceinline__ bool bar_wait(Bars* b, uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(Bars* b, uint64_t* bar, uint32_t parity, long long limit) {
   bool ok = bar_try(bar, parity);
-  if (LV_RARE(!ok)) ok = bar_wait_slow(b, bar, parity);
+  if (LV_RARE(!ok)) ok = bar_wait_slow(b, bar, parity, limit);
   return __all_sync(0xffffffffu, ok);
 }
 
@@ -507,7 +507,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
-      bar_init(&bars.kv_full[i], 1);
+      bar_init(&bars.kv_full[i], arrivals_of(a, LV_HOLD_COPIES));
       bar_init(&bars.kv_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -515,7 +515,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       bar_init(&bars.q_empty[i], 1);
       bar_init(&bars.s_full[i], 1);
       for (int k = 0; k < 3; ++k) bar_init(&bars.p_full[i][k], 4);
-      bar_init(&bars.o_full[i], 1);
+      bar_init(&bars.o_full[i], arrivals_of(a, LV_HOLD_PRODUCTS));
     }
     bar_init(&bars.clean_ask, 1);
     bar_init(&bars.clean_done, 32);
@@ -559,7 +559,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const int p_lo = pr.t.first + R0 / a.G, p_hi = pr.t.first + (R0 + rows - 1) / a.G;
       Softmax<DP, kBf16> sm;
       for (int u = pr.u0; u < pr.u1; ++u) {
-        if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par))) break;
+        if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par, a.wait_ns))) break;
         s_par ^= 1;
         if (live) {
           tc_fence_after();
@@ -575,7 +575,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         warp_arrive(&bars.p_full[half][2]);
       }
       has = nx.next(a);
-      if (!ok || !(ok = bar_wait(&bars, &bars.o_full[half], o_par))) break;
+      if (!ok || !(ok = bar_wait(&bars, &bars.o_full[half], o_par, a.wait_ns))) break;
       o_par ^= 1;
       if (!live) continue;
       // the pair's end
@@ -704,7 +704,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           next = page_of(u + 1);
           const int n = (int)((2 * unit + kv) % S::kStages);
           const uint32_t round = (uint32_t)((2 * unit + kv) / S::kStages);
-          if (!(ok = bar_wait(&bars, &bars.kv_empty[n], ~round & 1u))) break;
+          if (!(ok = bar_wait(&bars, &bars.kv_empty[n], ~round & 1u, a.wait_ns))) break;
           uint64_t* full = &bars.kv_full[n];
           const uint32_t dst = ring_s + n * S::kBlock;
           if (elected()) bar_expect(full, S::kBlock);
@@ -733,7 +733,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         for (long long i = unit < S::kStages ? 0 : unit - S::kStages; i < unit; ++i) {
           const unsigned long long t0 = now_ns();
           while (!bar_try(&bars.kv_full[(2 * i + kv) % S::kStages], (uint32_t)((2 * i + kv) / S::kStages) & 1u))
-            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+            if ((long long)(now_ns() - t0) > a.wait_ns) break;
         }
       }
     } else if (wid == kWarpMma) {
@@ -771,10 +771,10 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         auto pair = [&](auto halves_of) -> bool {
           constexpr int kHalves = decltype(halves_of)::value;
           pr = nx;
-          if (!bar_wait1(&bars, &bars.kv_full[stage], par)) return false;
+          if (!bar_wait1(&bars, &bars.kv_full[stage], par, a.wait_ns)) return false;
 #pragma unroll
           for (int h = 0; h < kHalves; ++h) {      // the first unit's scores
-            if (!bar_wait1(&bars, &bars.q_full[h], q_par >> h & 1)) return false;
+            if (!bar_wait1(&bars, &bars.q_full[h], q_par >> h & 1, a.wait_ns)) return false;
             q_par ^= 1u << h;
             tc_fence_after();
             scores(h, stage);
@@ -787,26 +787,26 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           for (int u = pr.u0; u < pr.u1; ++u) {
             const int vs = stage;
             const bool ragged = pr.ragged(u, a.sinks), more = u + 1 < pr.u1;
-            if (LV_RARE(!bar_wait1(&bars, &bars.kv_full[vs], par))) return false;
+            if (LV_RARE(!bar_wait1(&bars, &bars.kv_full[vs], par, a.wait_ns))) return false;
             step();
             if (LV_RARE(ragged)) bar_arrive(&bars.clean_ask);
             const int ks = stage;
             if (LV_MOSTLY(more)) {
-              if (LV_RARE(!bar_wait1(&bars, &bars.kv_full[ks], par))) return false;
+              if (LV_RARE(!bar_wait1(&bars, &bars.kv_full[ks], par, a.wait_ns))) return false;
             }
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) {
-              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][0], p_par >> h & 1))) return false;
+              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][0], p_par >> h & 1, a.wait_ns))) return false;
               if (h == 0 && LV_RARE(ragged)) {
-                if (!bar_wait1(&bars, &bars.clean_done, clean_par)) return false;
+                if (!bar_wait1(&bars, &bars.clean_done, clean_par, a.wait_ns)) return false;
                 clean_par ^= 1;
               }
               tc_fence_after();
               values(h, vs, 0, 4, u > pr.u0);
-              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1))) return false;
+              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][1], p_par >> h & 1, a.wait_ns))) return false;
               tc_fence_after();
               values(h, vs, 4, 6, true);
-              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][2], p_par >> h & 1))) return false;
+              if (LV_RARE(!bar_wait1(&bars, &bars.p_full[h][2], p_par >> h & 1, a.wait_ns))) return false;
               tc_fence_after();
               values(h, vs, 6, 8, true);
               if (LV_MOSTLY(more)) {
@@ -832,8 +832,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           tc_commit(&bars.drain);
           const unsigned long long t0 = now_ns();
           while (!bar_try(&bars.drain, 0))
-            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
-          report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
+            if ((long long)(now_ns() - t0) > a.wait_ns) break;
         }
       }
       __syncwarp();
@@ -849,7 +848,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         for (int half = 0; half < 2; ++half) {
           const int rows = min(half_rows, pr.t.rows - half * half_rows);
           if (rows <= 0) break;
-          if (!(ok = bar_wait(&bars, &bars.q_empty[half], ~par >> half & 1))) break;
+          if (!(ok = bar_wait(&bars, &bars.q_empty[half], ~par >> half & 1, a.wait_ns))) break;
           par ^= 1u << half;
           const uint32_t to = q_s + half * S::kBlock;
           const int R0 = pr.t.row0 + half * half_rows;
@@ -894,7 +893,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
         for (int u = pr.u0; ok && u < pr.u1; ++u, ++units) {
           if (!pr.ragged(u, a.sinks)) continue;
-          if (!(ok = bar_wait(&bars, &bars.clean_ask, z_par))) break;
+          if (!(ok = bar_wait(&bars, &bars.clean_ask, z_par, a.wait_ns))) break;
           z_par ^= 1;
           const uint32_t v = ring_s + (uint32_t)((2 * units + 1) % S::kStages) * S::kBlock;
           const int key0 = pr.key_of(u);
@@ -913,7 +912,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         for (int half = 0; half < 2; ++half) {
           const unsigned long long t0 = now_ns();
           while (!bar_try(&bars.q_full[half], ~par >> half & 1))
-            if ((long long)(now_ns() - t0) > kWaitLimitNs) break;
+            if ((long long)(now_ns() - t0) > a.wait_ns) break;
         }
       }
       // rows of no request
@@ -936,6 +935,8 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     tc_fence_before();
   }
   __syncthreads();
+  // (whichever role's wait it was: the products' thread may have ended well before)
+  if (threadIdx.x == 0 && LV_RARE(bars.bad)) report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
   if (wid == kWarpMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");

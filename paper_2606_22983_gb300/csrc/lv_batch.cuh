@@ -132,7 +132,11 @@ struct AttnArgs {
   float* part_o;           // [2 * ctas][tile_rows][dp] sums, and
   float2* part_ml;         // [2 * ctas][tile_rows] their maximum (in log2) and weight
   long long* ctl;
+  long long wait_ns;       // of each wait on a copy or a product
+  int32_t hold;            // LV_HOLD_NONE but in a self-test
 };
+
+constexpr long long kAttnWaitNs = 1000000000ll;   // one second a wait
 
 // Words of AttnArgs.arrived a CTA, in sets of kArriveSet (a warp's rows each, where warps count for
 // themselves).  The pieces of a cut pair, or their groups, are counted at the CTA of its first piece,
@@ -207,6 +211,11 @@ __device__ __forceinline__ int add_release(int32_t* p, int v) {
 // True where the step on the device is one that an attention over num_tokens rows may work on.
 __device__ __forceinline__ bool step_fits(const StepHead& head, int kind, int num_tokens) {
   return head.kind == kind && head.num_tokens <= num_tokens;
+}
+// Arrivals that a barrier of kind `what` waits for: one more than come, in every second CTA, where a
+// self-test holds them.
+__device__ __forceinline__ uint32_t arrivals_of(const AttnArgs& a, int what) {
+  return a.hold == what ? 1u + (blockIdx.x & 1u) : 1u;
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

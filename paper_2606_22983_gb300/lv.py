@@ -97,6 +97,7 @@ class lv_heads(ctypes.Structure):
 
 
 LV_BF16, LV_F16, LV_F32 = 1, 2, 3
+LV_HOLD_NONE, LV_HOLD_COPIES, LV_HOLD_PRODUCTS = 0, 1, 2
 
 
 class lv_stats(ctypes.Structure):
@@ -209,6 +210,7 @@ def _load():
         "lv_kv_write": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp],
         "lv_attention": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp,
                          ctypes.c_float, vp],
+        "lv_selftest_attention": [vp, i32, i64],
         "lv_sync": [vp, vp],
         "lv_get_stats": [vp, ctypes.POINTER(lv_stats), vp],
         "lv_clear_error": [vp, vp],
@@ -246,7 +248,8 @@ EXPORTED = ("lv_pool_create", "lv_pool_destroy", "lv_pool_host_ptr", "lv_pool_im
             "lv_controller_create", "lv_controller_destroy", "lv_controller_tick",
             "lv_controller_speech", "lv_controller_turn_begin", "lv_controller_turn_loaded",
             "lv_controller_records", "lv_controller_counters_get", "lv_batch_create",
-            "lv_batch_destroy", "lv_batch_plan", "lv_kv_write", "lv_attention")
+            "lv_batch_destroy", "lv_batch_plan", "lv_kv_write", "lv_attention",
+            "lv_selftest_attention")
 
 
 def lib():
@@ -498,6 +501,10 @@ def lv_kv_write(batch, layer, k: lv_heads, v: lv_heads, stream=None):
 def lv_attention(batch, layer, q: lv_heads, out: lv_heads, lse, scale, stream=None):
     _check(_lib.lv_attention(batch, layer, ctypes.byref(q), ctypes.byref(out), ptr(lse), scale,
                              stream_handle(stream)), "lv_attention")
+
+
+def lv_selftest_attention(batch, what, limit_us=0):
+    _check(_lib.lv_selftest_attention(batch, what, limit_us), "lv_selftest_attention")
 
 
 def lv_sync(pool, stream=None, raise_on_error=True) -> int:
