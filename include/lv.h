@@ -724,7 +724,8 @@ lv_status lv_kv_write(lv_batch* batch, int32_t layer, const lv_heads* k, const l
    What a cache page holds past a request's context, and in blocks that none of its rows
    sees, has no effect, not even as NaN; a non-finite V row that some rows of a chunk see may
    also reach other rows of that chunk.  LV_ERR_INVALID as for lv_kv_write.  Device-detected:
-   LV_ERR_TIMEOUT if a bounded wait inside the kernel ran out. */
+   LV_ERR_TIMEOUT if a bounded wait inside the kernel ran out; further calls on that step
+   do nothing and report LV_ERR_STATE with detail -1 until it is planned again. */
 lv_status lv_attention(lv_batch* batch, int32_t layer, const lv_heads* q, const lv_heads* out, float* lse,
                        float scale, lv_stream stream);
 

@@ -635,7 +635,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       while (!bar_try(bar_s + 8 * (int)(i % S::kStages), (uint32_t)(i / S::kStages) & 1u))
         if ((long long)(now_ns() - t0) > a.wait_ns) break;
     }
-    if (lane == 0) report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
+    if (lane == 0) give_up(a);
   }
   if (dead) clear_dead(a, blockIdx.x * kThreads + threadIdx.x, gridDim.x * kThreads);
 }

@@ -936,7 +936,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   }
   __syncthreads();
   // (whichever role's wait it was: the products' thread may have ended well before)
-  if (threadIdx.x == 0 && LV_RARE(bars.bad)) report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
+  if (threadIdx.x == 0 && LV_RARE(bars.bad)) give_up(a);
   if (wid == kWarpMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");

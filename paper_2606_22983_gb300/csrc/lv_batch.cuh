@@ -52,7 +52,8 @@ static_assert(sizeof(CtaWork) == 80, "read as five 16-byte words");
 // not be the plan that the device made last: they compare, and do nothing where a list of the other
 // kernel's units or a step of more rows than their tensors have would be read.
 struct StepHead {
-  int32_t kind;         // AttnKind of the work list; -1: nothing planned
+  int32_t kind;         // AttnKind of the work list; -1: none (nothing planned, or a wait ran out: the pieces
+                        // that came are counted, and another call on the list would join them as its own)
   int32_t num_tokens;   // the plan's; rows past it are of no request whatever positions and slots hold
   int32_t live;         // rows of requests
   int32_t pad;
@@ -117,7 +118,7 @@ struct AttnArgs {
   const int32_t* positions;
   const AttnTile* tiles;
   const CtaWork* work;
-  const StepHead* head;
+  StepHead* head;
   int32_t* arrived;
   const uint8_t* q;
   uint8_t* out;
@@ -216,6 +217,11 @@ __device__ __forceinline__ bool step_fits(const StepHead& head, int kind, int nu
 // self-test holds them.
 __device__ __forceinline__ uint32_t arrivals_of(const AttnArgs& a, int what) {
   return a.hold == what ? 1u + (blockIdx.x & 1u) : 1u;
+}
+// A wait ran out: later calls on the step are refused until it is planned again.
+__device__ __forceinline__ void give_up(const AttnArgs& a) {
+  report(a.ctl, LV_ERR_TIMEOUT, blockIdx.x);
+  a.head->kind = -1;
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

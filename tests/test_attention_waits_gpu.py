@@ -55,3 +55,28 @@ def test_selftest_refusals():
         assert s.pool.sync(raise_on_error=False) == 0
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("what,cached,new", [c for c in CASES if c[0] == COPIES])
+def test_a_step_with_a_timeout_is_planned_again(what, cached, new):
+    """Its counts of arrived pieces are not those of a fresh step: later calls refuse it."""
+    import torch
+    from paper_2606_22983_gb300 import lv
+    s = Step(cached, new, heads=2, group=8, dim=128, pad=1)
+    try:
+        s.plan()
+        want = s.batch.attention(1, s.q, return_lse=True)
+        assert _run_out(s, what) == lv.LV_ERR_TIMEOUT
+        s.pool.clear_error()
+        out = torch.full_like(s.q, 7.0)
+        s.batch.attention(1, s.q, out=out)
+        st = s.pool.stats()
+        assert st["error"] == lv.LV_ERR_STATE and st["error_detail"] == -1
+        assert (out == 7.0).all()
+        s.pool.clear_error()
+        s.plan()
+        again = s.batch.attention(1, s.q, return_lse=True)
+        assert s.pool.sync(raise_on_error=False) == 0
+        assert all(torch.equal(a, b) for a, b in zip(want, again))
+    finally:
+        s.close()
