@@ -53,6 +53,7 @@ class KVBatch:
             # the library may write them on any stream next
             torch.cuda.current_stream().synchronize()
         self._device = self.row_starts.get_device()
+        self._used_on = {lv.stream_handle(None, self._device)}      # streams that keep the arrays above in use
         self._scale = 1.0 / math.sqrt(pool.head_dim)
         self._a, self._b = lv.lv_heads(), lv.lv_heads()      # a call's two tensor arguments
         # an output that attention() makes itself
@@ -100,15 +101,35 @@ class KVBatch:
             have = np.asarray(lens)
             num_tokens = int(have.sum()) if num_tokens is None else num_tokens
             max_len = int(have.max(initial=0)) if max_len is None else max_len
+        s, away = self._stream(stream)
+        if away or s not in self._used_on:
+            self._use(s, sids, lens, firsts)
         lv.lv_batch_plan(self.handle, sids, firsts, lens, n, num_tokens,
-                         num_tokens if max_len is None else max_len, self._stream(stream))
+                         num_tokens if max_len is None else max_len, s)
         self.num_tokens = num_tokens
         self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH)
 
     def _stream(self, stream):
+        """The handle of a call's stream, and whether it is another than the current one."""
         if stream is None:
             stream = self.pool.stream
-        return lv.stream_handle(stream, self._device)
+        s = lv.stream_handle(stream, self._device)
+        return s, stream is not None and s != lv.stream_handle(None, self._device)
+
+    def _torch_stream(self, s):
+        return torch.cuda.ExternalStream(s, device=self.pool.device) if s else \
+            torch.cuda.default_stream(self.pool.device)
+
+    def _use(self, s, *tensors):
+        """Before a launch on the stream of handle s: PyTorch gives no memory that the launch uses to
+        others before it has run.  (On the current stream that holds for a call's own tensors already.)"""
+        t = self._torch_stream(s)
+        if s not in self._used_on:
+            self._used_on.add(s)
+            tensors += (self.row_starts, self.kv_lens, self.tables, self.positions, self.slots)
+        for x in tensors:
+            if isinstance(x, torch.Tensor) and x.is_cuda:
+                x.record_stream(t)
 
     def _put(self, h, x, heads, name):
         """h describes tensor x, [rows, heads, head_dim] with head_dim contiguous."""
@@ -126,15 +147,29 @@ class KVBatch:
         """The step's new K and V rows ([rows, kv_heads, head_dim], any strides, bf16, f16 or f32)
         into their pages."""
         H = self.pool.kv_heads
-        lv.lv_kv_write(self.handle, layer, self._put(self._a, k, H, "k"), self._put(self._b, v, H, "v"),
-                       self._stream(stream))
+        s, away = self._stream(stream)
+        k_arg, v_arg = self._put(self._a, k, H, "k"), self._put(self._b, v, H, "v")
+        if away or s not in self._used_on:
+            self._use(s, k, v)
+        lv.lv_kv_write(self.handle, layer, k_arg, v_arg, s)
         self.pool.launches += 1
 
     def attention(self, layer: int, q, *, out=None, scale=None, return_lse=False, stream=None):
         """Attention of the step's rows over their paged contexts: [rows, q_heads, head_dim], and with
         ``return_lse`` the logarithms of the sums of exponentials [rows, q_heads] (f32).  Rows of
         no request give zeros (and -inf).  scale: 1 / sqrt(head_dim) unless given.  With a stream
-        other than the current one, the caller orders the two."""
+        other than the current one, the caller orders the two: the stream after what made q, and what
+        reads the results after the stream."""
+        s, away = self._stream(stream)
+        if away or s not in self._used_on:
+            self._use(s, q, out)
+        if away:
+            # results from the launch's own stream: the current one's memory may be in use there
+            with torch.cuda.stream(self._torch_stream(s)):
+                made = self.attention(layer, q, out=out, scale=scale, return_lse=return_lse, stream=s)
+            for x in made if return_lse else (made,):
+                x.record_stream(torch.cuda.current_stream(self.pool.device))
+            return made
         q_arg = self._put(self._a, q, self.q_heads, "q")
         lse = None
         if out is None:
@@ -150,7 +185,6 @@ class KVBatch:
             lse = torch.empty((len(q), self.q_heads), dtype=torch.float32, device=q.device)
             if len(q) > self.num_tokens:
                 lse[self.num_tokens:].fill_(-math.inf)
-        lv.lv_attention(self.handle, layer, q_arg, out_arg, lse, self._scale if scale is None else scale,
-                        self._stream(stream))
+        lv.lv_attention(self.handle, layer, q_arg, out_arg, lse, self._scale if scale is None else scale, s)
         self.pool.launches += 1
         return (out, lse) if return_lse else out
