@@ -720,7 +720,8 @@ lv_status lv_kv_write(lv_batch* batch, int32_t layer, const lv_heads* k, const l
    q and out are [num_tokens][Hq][D] of the batch's dtype and must not overlap.  Statistics and sums are held in 32
    bits; the weights are rounded to dtype for the product with V.  lse (float [num_tokens][Hq],
    or NULL) receives the natural logarithm of each row's sum of exponentials.  A row of no
-   request gets out = 0 and lse = -inf.  scale is finite and > 0.
+   request gets out = 0 and lse = -inf.  scale is > 0 and scale * log2(e) finite in 32 bits (it is
+   up to 2.358e38).
    What a cache page holds past a request's context, and in blocks that none of its rows
    sees, has no effect, not even as NaN; a non-finite V row that some rows of a chunk see may
    also reach other rows of that chunk.  LV_ERR_INVALID as for lv_kv_write.  Device-detected:

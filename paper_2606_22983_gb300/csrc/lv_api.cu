@@ -1,6 +1,7 @@
 // C-ABI entry points of liblv (see include/lv.h): argument checks, device
 // metadata, staging of host-pointer arguments, and kernel launches.
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstdlib>
 #include <cstring>
@@ -1965,7 +1966,8 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
                        lv_stream stream) {
   NvtxRange nvtx_range("lv_attention");
   if (!b || !b->planned || layer < 0 || 2 * layer >= b->pool->d.J) return LV_ERR_INVALID;
-  if (!(scale > 0.f) || scale > 3e38f) return LV_ERR_INVALID;
+  const float scale2 = scale * 1.44269504088896341f;      // for powers of two
+  if (!(scale > 0.f) || !std::isfinite(scale2)) return LV_ERR_INVALID;
   if (b->num_tokens == 0) return LV_OK;
   const lv_pool* pool = b->pool;
   DeviceGuard g(pool->device);
@@ -2006,7 +2008,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.sinks = b->d.sinks;
   a.tile_rows = tc ? lv::tc_tile_rows(b->G) : lv::kRowsRows;
   a.dp = b->dp;
-  a.scale = scale * 1.44269504088896341f;
+  a.scale = scale2;
   a.part_o = b->part_o;
   a.part_ml = b->part_ml;
   a.ctl = pool->d.ctl;
