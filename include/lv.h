@@ -683,7 +683,8 @@ typedef struct lv_heads {
 } lv_heads;
 
 /* Validates the descriptor and allocates the batch's work lists and workspace (some 40 MiB
-   at 128 head_dim).  LV_ERR_INVALID, LV_ERR_OOM or LV_ERR_CUDA. */
+   at 128 head_dim, and 3 bytes for each of max_tokens * Hq / H packed rows and 64 a request).
+   LV_ERR_INVALID, LV_ERR_OOM or LV_ERR_CUDA. */
 lv_status lv_batch_create(lv_pool* pool, const lv_batch_desc* desc, lv_batch** out);
 
 /* Waits for `stream` and frees the batch; call it before lv_pool_destroy of its pool. */

@@ -32,7 +32,10 @@ _KINDS = {torch.bfloat16: lv.LV_BF16, torch.float16: lv.LV_F16, torch.float32: l
 
 class KVBatch:
     """One kind of attention layer over ``pool``: ``q_heads`` query heads, and with ``window`` > 0 a
-    sliding window of that many keys beside which the first ``sinks`` keys stay visible."""
+    sliding window of that many keys beside which the first ``sinks`` keys stay visible.
+
+    It holds device memory until ``close`` or the pool's: the library's workspace and work lists, and
+    the five arrays, of which ``tables`` has max_requests * max_blocks entries."""
 
     def __init__(self, pool: KVPool, *, q_heads: int, max_requests: int, max_tokens: int,
                  dtype=torch.bfloat16, window: int = 0, sinks: int = 0):
@@ -68,9 +71,13 @@ class KVBatch:
         pool.attach(self)          # destroyed before the pool
 
     def close(self):
+        """Waits for the pool's stream (or the current one) and frees the batch's memory; what is
+        captured over it cannot be replayed any more."""
         if getattr(self, "handle", None):
             lv.lv_batch_destroy(self.handle, self.pool.stream)
             self.handle = None
+            self.row_starts = self.kv_lens = self.tables = self.positions = self.slots = None
+            self.pool.detach(self)
 
     def _ints(self, x, n=None):
         """An int32 array the library can read: a tensor as it is, else a numpy array."""

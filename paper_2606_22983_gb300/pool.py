@@ -91,9 +91,13 @@ class KVPool:
             self._attached = []
         self._attached.append(obj)
 
+    def detach(self, obj):
+        """An attached object that has been closed."""
+        self._attached = [x for x in getattr(self, "_attached", []) if x is not obj]
+
     def close(self):
         if getattr(self, "handle", None):
-            for obj in getattr(self, "_attached", []):
+            for obj in list(getattr(self, "_attached", [])):
                 obj.close()
             self._attached = []
             self.host_dev = None
