@@ -650,7 +650,9 @@ lv_status lv_schedule(lv_pool* pool, const lv_sched_params* params, const lv_req
    of no request) that chooses the same kernel; after another they do nothing, and the device
    reports LV_ERR_STATE with detail -1 (lv_kv_write only where the plan has more rows).  A captured
    lv_batch_plan keeps n, num_tokens and max_len, and reads sids, firsts and lens when it is
-   replayed. */
+   replayed: they are device or page-locked memory that stays, and pageable memory is refused
+   (LV_ERR_INVALID).  It waits for the pool's asynchronous exchanges, which a capture cannot do: a
+   pool that has run one gives LV_ERR_CUDA there. */
 enum { LV_BF16 = 1, LV_F16 = 2, LV_F32 = 3 };
 
 typedef struct lv_batch lv_batch;   /* opaque */

@@ -171,7 +171,9 @@ class Staging {
   }
 
   // near: page-locked host memory is copied in too (for an argument that is read often)
-  lv_status in(const void* user, size_t bytes, const void** dev, bool near = false) {
+  // kept: pageable memory is refused in a stream capture, whose replays would read it again, when it
+  // may be gone
+  lv_status in(const void* user, size_t bytes, const void** dev, bool near = false, bool kept = false) {
     *dev = nullptr;
     if (bytes == 0) return LV_OK;
     if (user == nullptr) return LV_ERR_INVALID;
@@ -180,6 +182,10 @@ class Staging {
         *dev = v;
         return LV_OK;
       }
+    } else if (kept) {
+      cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+      LV_TRY(cudaStreamIsCapturing(s_, &capture));
+      if (capture != cudaStreamCaptureStatusNone) return LV_ERR_INVALID;
     }
     void* t = nullptr;
     lv_status st = temp(bytes, &t);
@@ -1865,9 +1871,10 @@ lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts,
     const void *si = nullptr, *fi = nullptr, *le = nullptr;
     lv_status r;
     // every CTA reads the lengths: host memory is copied in
-    if ((r = st.in(sids, (size_t)n * 4, &si, true)) != LV_OK || (r = st.in(lens, (size_t)n * 4, &le, true)) != LV_OK)
+    if ((r = st.in(sids, (size_t)n * 4, &si, true, true)) != LV_OK ||
+        (r = st.in(lens, (size_t)n * 4, &le, true, true)) != LV_OK)
       return r;
-    if (firsts && (r = st.in(firsts, (size_t)n * 4, &fi, true)) != LV_OK) return r;
+    if (firsts && (r = st.in(firsts, (size_t)n * 4, &fi, true, true)) != LV_OK) return r;
     max_len = std::min(max_len, num_tokens);
     // more rows a request than one m16n8k16 tile holds: the kernel for many rows, where pages can be
     // read by TMA (32 sessions of 1000 to 4000 keys with 4 new tokens, 32 rows, took 42 us with it and

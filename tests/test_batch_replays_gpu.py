@@ -157,3 +157,31 @@ def test_a_captured_plan(steps):
             assert (out[sum(new):] == 0).all()
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("which", ["sids", "lens", "firsts"])
+def test_a_captured_plan_takes_no_pageable_memory(which):
+    """A replay would read it again, when the program has given it back."""
+    import torch
+    from paper_2606_22983_gb300 import lv
+    s = Step([30, 7], [1, 1], heads=1, group=2, dim=8)
+    try:
+        host = {"sids": s.sids, "lens": np.array([1, 1], np.int32), "firsts": np.array([-1, -1], np.int32)}
+        dev = {n: torch.from_numpy(x).cuda() for n, x in host.items()}
+        s.batch.plan(*(dev[n] for n in ("sids", "lens", "firsts")), num_tokens=2, max_len=1)
+        out = torch.zeros_like(s.q)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            with pytest.raises(lv.LvError) as e:
+                s.batch.plan(*({**dev, which: host[which]}[n] for n in ("sids", "lens", "firsts")),
+                             num_tokens=2, max_len=1)
+            assert e.value.status == lv.LV_ERR_INVALID
+            s.batch.plan(*(dev[n] for n in ("sids", "lens", "firsts")), num_tokens=2, max_len=1)
+            s.batch.attention(0, s.q, out=out)
+        g.replay()
+        torch.cuda.synchronize()
+        assert s.pool.sync(raise_on_error=False) == 0
+        s.check(out, None, 0, 8 ** -0.5)
+    finally:
+        s.close()
