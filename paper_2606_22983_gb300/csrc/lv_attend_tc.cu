@@ -478,8 +478,9 @@ struct Softmax {
 // What bounds it: in a long context the tensor core and the softmax that feeds it.  A unit of both halves
 // is 2048 cycles of products at the tensor core's rate and took 2850: a half's chain of products (some 1400) and
 // softmax (1500) is as long as both halves' products, which hides in two halves' turns but for the waits.  500 tokens at 64 000
-// keys, 32 query heads of 128: 334 to 345 us, 1.53 to 1.57 PFLOP/s (the pipe is active 74 % of the time);
-// 8 prompts of 4096 from nothing 715 us, 1.54; 5 chunks of 1500 to 2100 under a window of 1024 149 us, 0.9.
+// keys, 32 query heads of 128: 334 to 353 us over boxes, 1.49 to 1.57 PFLOP/s (the pipe is active 74 % of the
+// time); 8 prompts of 4096 from nothing 715 to 727 us, 1.54; 5 chunks of 1500 to 2100 under a window of 1024
+// 145 us, 0.9.  These are launches in a graph after a pause; calls one after another take 388, 780 and 150.
 // Of a pair's time some 6000 cycles lie between its last weights and the next pair's first, some 3000 more
 // than between units.  Under a steady load the power limit lowers the clock, and all of this by 3 to 8 %.
 //

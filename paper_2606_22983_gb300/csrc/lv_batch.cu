@@ -71,8 +71,9 @@ __device__ __forceinline__ AttnTile make_tile(const PlanArgs& a, const PlanReq& 
 
 // One CTA of NT threads cuts the requests into tiles and the tiles' units into shares: prefix sums over
 // the requests' tiles and over the tiles' units, a thread taking several in a row, so that a tile is made
-// twice (once to be counted, once to be written) rather than kept.  What bounds it is the chain: four
-// scans of two barriers each, some 5 us for 64 requests of one tile and 10 for 1024.
+// twice (once to be counted, once to be written) rather than kept.  What bounds it is the chain: five
+// scans of two barriers each (tiles, owned rows, units, shares of either size; the last two and a vote only
+// where there may be pairs apart), some 5 us for 64 requests of one tile and 10 for 1024.
 template <int NT>
 __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* first_tile) {
   // each request's first tile: a scan over the requests, a thread taking several in a row
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut(const __grid_constant
 // CTA takes kWriteThreads * U of them in a row, a thread U with all its loads on their way before
 // the first store.
 // What bounds it: the launch for a decode step (64 rows of 4 heads of 128, 1.9 us); HBM for prompts' rows
-// (13 706 of them from 32 to 16 bits, 84 MB in and out, 10.7 us, some of it from L2).  Each row's K and V are
+// (13 706 of them from 32 to 16 bits, 84 MB in and out, 10.9 us, some of it from L2).  Each row's K and V are
 // read and written once: 2 H D (source bytes + 2), and the 8 bytes of its slot.  Rounding is to nearest even.
 constexpr int kWriteThreads = 256;
 

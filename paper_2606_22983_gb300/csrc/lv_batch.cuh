@@ -271,8 +271,11 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
 }
 // A weight is at most 2^(kLazy + bias) times its row's true one: the running maximum is only
 // raised when a row outgrows it by 2^kLazy, so that the sums are seldom rescaled.  In f16 the
-// weights are kept near the top of the type's range (2^15 at most): one that is 2^-22 of the
-// row's largest still has full precision, where 2^-14 would be the end without the bias.
+// weights are kept near the top of the type's range (2^15 at most): the row's largest is 2^7 at least,
+// so that one of 2^-21 of it still has full precision, where 2^-14 would be the end without the bias.
+// Weights are rounded to the pool's 16-bit type for the product with V, whose operands the tensor
+// cores take in one type: by at most 2^-8 (bf16) or 2^-11 (f16) of each.  Their sum is taken before
+// that, and it, the maxima and the products' sums are in 32 bits.
 constexpr float kLazy = 8.0f;
 template <bool kBf16>
 __device__ __forceinline__ constexpr float weight_bias() {
