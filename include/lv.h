@@ -709,6 +709,27 @@ lv_status lv_batch_destroy(lv_batch* batch, lv_stream stream);
 lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* firsts, const int32_t* lens,
                         int32_t n, int32_t num_tokens, int32_t max_len, lv_stream stream);
 
+/* A prefix that several sessions share (the instructions in front of an assistant's talks) is held
+   once, by a session of its own, and the others' contexts continue it.  lv_batch_share makes
+   room, once, for steps of up to `rows` rows (1..max_tokens) with prefixes: rows * Hq sums of
+   head_dim 32-bit values.  LV_ERR_INVALID for a batch with a window or that has the room.
+   Synchronous, as lv_batch_create.
+   lv_batch_plan_shared plans a step as lv_batch_plan does, in which request i's rows also see the
+   first prefix_lens[i] tokens of session prefixes[i] (prefix_lens NULL: all it holds; prefixes[i] < 0
+   or no tokens: no prefix), as if they came before its own.  positions count from the prefix's begin;
+   kv_lens, tables and slots are of the request's own session.  Requests that follow one another and
+   continue the same tokens of the same session read them once, for all their rows and heads together.
+   lv_attention works on such a step in two launches.  Device-detected, with the request left out:
+   LV_ERR_BOUNDS for a prefix's session id or length out of range, LV_ERR_STATE for a block of it that
+   is not in HBM; it must stay where it is until the step's last call.  LV_ERR_INVALID for a batch
+   without room for num_tokens rows.  A captured lv_attention also keeps whether the plan before its capture was given
+   prefixes (and the kernel for them, chosen by whether num_tokens * Hq / H is above 16): after a plan of the other
+   kind it does nothing and reports LV_ERR_STATE with detail -1. */
+lv_status lv_batch_share(lv_batch* batch, int32_t rows);
+lv_status lv_batch_plan_shared(lv_batch* batch, const int32_t* sids, const int32_t* firsts, const int32_t* lens,
+                               const int32_t* prefixes, const int32_t* prefix_lens, int32_t n, int32_t num_tokens,
+                               int32_t max_len, lv_stream stream);
+
 /* Writes the planned step's new K and V rows ([num_tokens][H][D], any of the three types,
    rounded to nearest even where the pool's type is narrower) into their pages of `layer`;
    rows of no request are skipped.  The sessions' pages must stay where the plan found them

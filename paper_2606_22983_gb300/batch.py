@@ -34,16 +34,20 @@ class KVBatch:
     """One kind of attention layer over ``pool``: ``q_heads`` query heads, and with ``window`` > 0 a
     sliding window of that many keys beside which the first ``sinks`` keys stay visible.
 
+    With ``prefix_rows`` > 0 steps of up to that many rows may continue shared prefixes (``plan``'s
+    ``prefixes``).
+
     It holds device memory until ``close`` or the pool's: the library's workspace and work lists, and
     the five arrays, of which ``tables`` has max_requests * max_blocks entries."""
 
     def __init__(self, pool: KVPool, *, q_heads: int, max_requests: int, max_tokens: int,
-                 dtype=torch.bfloat16, window: int = 0, sinks: int = 0):
+                 dtype=torch.bfloat16, window: int = 0, sinks: int = 0, prefix_rows: int = 0):
         if dtype not in (torch.bfloat16, torch.float16):
             raise ValueError("dtype must be torch.bfloat16 or torch.float16")
         self.pool, self.q_heads, self.dtype = pool, q_heads, dtype
         self.max_requests, self.max_tokens = max_requests, max_tokens
         self.num_tokens = 0
+        self._shared = False         # the planned step has prefixes
         self.handle = None
         i32 = dict(dtype=torch.int32, device=pool.device)
         rows, requests = max(max_tokens, 0), max(max_requests, 0)
@@ -68,6 +72,13 @@ class KVBatch:
                              tables=self.tables.data_ptr(), positions=self.positions.data_ptr(),
                              slots=self.slots.data_ptr())
         self.handle = lv.lv_batch_create(pool.handle, d)
+        if prefix_rows:
+            try:
+                lv.lv_batch_share(self.handle, prefix_rows)
+            except lv.LvError:
+                lv.lv_batch_destroy(self.handle, pool.stream)
+                self.handle = None
+                raise
         pool.attach(self)          # destroyed before the pool
 
     def close(self):
@@ -92,15 +103,25 @@ class KVBatch:
             raise ValueError(f"expected {n} entries, got {len(x)}")
         return x
 
-    def plan(self, sids, lens, firsts=None, *, num_tokens=None, max_len=None, stream=None):
+    def plan(self, sids, lens, firsts=None, *, prefixes=None, prefix_lens=None, num_tokens=None, max_len=None,
+             stream=None):
         """Plans a step: request i is session sids[i] with lens[i] new tokens from position firsts[i]
         on (None: the last ones of its context).  With lengths on the device, ``num_tokens`` (rows of
-        the step's tensors) has to be given, and ``max_len`` (a bound of the lengths) should be."""
+        the step's tensors) has to be given, and ``max_len`` (a bound of the lengths) should be.
+
+        prefixes: sessions whose first prefix_lens[i] tokens (None: all of them) the rows of request i see
+        before its own session's (-1: none).  Requests of one prefix that follow one another read it once."""
         sids = self._ints(sids)
         n = len(sids)
         lens = self._ints(lens, n)
         if firsts is not None:
             firsts = self._ints(firsts, n)
+        if prefixes is not None:
+            prefixes = self._ints(prefixes, n)
+            if prefix_lens is not None:
+                prefix_lens = self._ints(prefix_lens, n)
+        elif prefix_lens is not None:
+            raise ValueError("prefix_lens needs prefixes")
         if isinstance(lens, torch.Tensor) and lens.is_cuda:
             if num_tokens is None:
                 raise ValueError("num_tokens is needed with lengths on the device")
@@ -110,11 +131,16 @@ class KVBatch:
             max_len = int(have.max(initial=0)) if max_len is None else max_len
         s, away = self._stream(stream)
         if away or s not in self._used_on:
-            self._use(s, sids, lens, firsts)
-        lv.lv_batch_plan(self.handle, sids, firsts, lens, n, num_tokens,
-                         num_tokens if max_len is None else max_len, s)
+            self._use(s, sids, lens, firsts, prefixes, prefix_lens)
+        if max_len is None:
+            max_len = num_tokens
+        if prefixes is None:
+            lv.lv_batch_plan(self.handle, sids, firsts, lens, n, num_tokens, max_len, s)
+        else:
+            lv.lv_batch_plan_shared(self.handle, sids, firsts, lens, prefixes, prefix_lens, n, num_tokens, max_len, s)
         self.num_tokens = num_tokens
-        self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH)
+        self._shared = prefixes is not None and n > 0
+        self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH or self._shared)
 
     def _stream(self, stream):
         """The handle of a call's stream, and whether it is another than the current one."""
@@ -193,5 +219,5 @@ class KVBatch:
             if len(q) > self.num_tokens:
                 lse[self.num_tokens:].fill_(-math.inf)
         lv.lv_attention(self.handle, layer, q_arg, out_arg, lse, self._scale if scale is None else scale, s)
-        self.pool.launches += 1
+        self.pool.launches += 1 + self._shared
         return (out, lse) if return_lse else out

@@ -1668,6 +1668,18 @@ struct lv_batch {
   int32_t num_tokens = 0;
   lv::AttnKind kind = lv::ATTN_ROWS;
   int32_t ctas = 0;
+  // lv_batch_share: room for the sums over prefixes of share_rows rows, and the prefixes' line of work
+  int32_t share_rows = 0;
+  lv::PlanReq* pre_reqs = nullptr;
+  int2* continued = nullptr;
+  lv::AttnTile* pre_tiles = nullptr;
+  lv::CtaWork* pre_work = nullptr;
+  lv::StepHead* pre_head = nullptr;
+  float* pre_o = nullptr;
+  float2* pre_ml = nullptr;
+  bool shared = false;             // the planned step has prefixes, attended over by
+  lv::AttnKind pre_kind = lv::ATTN_ROWS;
+  int32_t pre_ctas = 0;
   // lv_selftest_attention
   int32_t hold = LV_HOLD_NONE;
   long long wait_ns = lv::kAttnWaitNs;
@@ -1817,6 +1829,122 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   return LV_OK;
 }
 
+// Where the line of an attention by `kind` is divided: the attention's CTAs and what they take.
+//
+// Shares of at least min_share units, pairs of up to uncut units in one piece where there is room
+// (many rows: 8 sessions with 4 new tokens after 1000 to 4000 keys 20.6 us, 23.2 at 4 units, and the
+// longer steps alike; 64 tokens at 1000 keys 19.7, and 22.2 at 6 uncut units.  Few rows: 1000 keys
+// 13.1 us, 14.7 at 16 units, 4000 keys 17.4, 18.6 at 4; 64 sessions of 100 to 300 keys 12.1, and 16.6
+// at 12 uncut units).
+lv::PlanLine line_of(const lv_batch* b, lv::AttnKind kind, int32_t num_tokens) {
+  const lv_pool* pool = b->pool;
+  lv::PlanLine a{};
+  a.G = b->G;
+  if (kind == lv::ATTN_TC) {
+    a.line_heads = pool->kv_heads;
+    a.tile_rows = lv::tc_tile_rows(b->G);
+    a.unit_shift = lv::kTcUnitShift;
+    a.lead = lv::kTcLead;
+    a.min_share = 3;
+    a.uncut = 12;
+    a.ctas = a.shares = pool->num_sms;
+  } else {
+    a.line_heads = 1;
+    a.tile_rows = lv::kRowsRows;
+    a.unit_shift = lv::kRowsUnitShift;
+    a.lead = lv::kRowsLead;
+    a.min_share = 8;
+    a.uncut = 24;
+    a.shares = rows_shares(b);
+    a.ctas = rows_ctas(b);
+  }
+  a.window = b->d.window;
+  a.sinks = b->d.sinks;
+  a.max_tiles = b->max_tiles;
+  a.kind = kind;
+  a.num_tokens = num_tokens;
+  a.reqs = b->reqs;
+  a.tiles = b->tiles;
+  a.work = b->work;
+  a.arrived = b->arrived;
+  a.head = b->head;
+  return a;
+}
+
+lv_status plan_step(lv_batch* b, const int32_t* sids, const int32_t* firsts, const int32_t* lens,
+                    const int32_t* prefixes, const int32_t* prefix_lens, int32_t n, int32_t num_tokens,
+                    int32_t max_len, lv_stream stream) {
+  if (!b || n < 0 || n > b->d.max_requests || (n > 0 && (!sids || !lens)) || num_tokens < 0 ||
+      num_tokens > b->d.max_tokens || max_len < 0)
+    return LV_ERR_INVALID;
+  lv_pool* pool = b->pool;
+  DeviceGuard g(pool->device);
+  cudaStream_t s = as_stream(stream);
+  try {
+    LV_TRY(join_copies(pool, s));   // the step reads and writes KV bytes
+    Staging st(pool, s);
+    const void *si = nullptr, *fi = nullptr, *le = nullptr, *pr = nullptr, *pl = nullptr;
+    lv_status r;
+    // every CTA reads the lengths: host memory is copied in
+    if ((r = st.in(sids, (size_t)n * 4, &si, true, true)) != LV_OK ||
+        (r = st.in(lens, (size_t)n * 4, &le, true, true)) != LV_OK)
+      return r;
+    if (firsts && (r = st.in(firsts, (size_t)n * 4, &fi, true, true)) != LV_OK) return r;
+    if (prefixes && (r = st.in(prefixes, (size_t)n * 4, &pr, true, true)) != LV_OK) return r;
+    if (prefix_lens && (r = st.in(prefix_lens, (size_t)n * 4, &pl, true, true)) != LV_OK) return r;
+    max_len = std::min(max_len, num_tokens);
+    // more rows a request than one m16n8k16 tile holds: the kernel for many rows, where pages can be
+    // read by TMA (32 sessions of 1000 to 4000 keys with 4 new tokens, 32 rows, took 42 us with it and
+    // 115 in tiles of 32 rows of the other; with 1 token, 8 rows, the other reads at 6 TB/s).
+    // One kernel a step: 47 single tokens and 3 chunks of 600 to 1500 took 165 us in one launch, and 62
+    // and 107 as a step of each kind
+    const lv::AttnKind kind =
+        (long long)max_len * b->G > lv::kRowsRows && b->box_rows ? lv::ATTN_TC : lv::ATTN_ROWS;
+    lv::PlanArgs a{};
+    a.p = pool->d;
+    a.sids = static_cast<const int32_t*>(si);
+    a.firsts = static_cast<const int32_t*>(fi);
+    a.lens = static_cast<const int32_t*>(le);
+    a.n = n;
+    a.num_tokens = num_tokens;
+    a.max_len = max_len;
+    a.window = b->d.window;
+    a.sinks = b->d.sinks;
+    a.row_starts = b->d.row_starts;
+    a.kv_lens = b->d.kv_lens;
+    a.tables = b->d.tables;
+    a.positions = b->d.positions;
+    a.slots = b->d.slots;
+    a.ticket = b->ticket;
+    a.own = line_of(b, kind, num_tokens);
+    // a prefix's rows are those of several requests: the kernel for many where there may be that many
+    const lv::AttnKind pre_kind =
+        (long long)num_tokens * b->G > lv::kRowsRows && b->box_rows ? lv::ATTN_TC : lv::ATTN_ROWS;
+    if (prefixes) {
+      a.prefixes = static_cast<const int32_t*>(pr);
+      a.prefix_lens = static_cast<const int32_t*>(pl);
+      a.continued = b->continued;
+      a.pre = line_of(b, pre_kind, num_tokens);
+      a.pre.reqs = b->pre_reqs;
+      a.pre.tiles = b->pre_tiles;
+      a.pre.work = b->pre_work;
+      a.pre.head = b->pre_head;
+    }
+    b->planned = false;      // (the old step's arrays are being written over)
+    LV_TRY(lv::launch_plan(a, s));
+    b->planned = true;
+    b->num_tokens = num_tokens;
+    b->kind = kind;
+    b->ctas = a.own.ctas;
+    b->shared = prefixes != nullptr;
+    b->pre_kind = pre_kind;
+    b->pre_ctas = a.pre.ctas;
+    return st.finish();
+  } catch (const std::bad_alloc&) {
+    return LV_ERR_OOM;
+  }
+}
+
 size_t elem_size(int32_t type) { return type == LV_F32 ? 4 : 2; }
 
 // A tensor argument: its type, its memory, and rows and heads that do not leave 63 bits.
@@ -1859,87 +1987,47 @@ lv_status lv_batch_destroy(lv_batch* batch, lv_stream stream) {
 lv_status lv_batch_plan(lv_batch* b, const int32_t* sids, const int32_t* firsts, const int32_t* lens, int32_t n,
                         int32_t num_tokens, int32_t max_len, lv_stream stream) {
   NvtxRange nvtx_range("lv_batch_plan");
-  if (!b || n < 0 || n > b->d.max_requests || (n > 0 && (!sids || !lens)) || num_tokens < 0 ||
-      num_tokens > b->d.max_tokens || max_len < 0)
-    return LV_ERR_INVALID;
-  lv_pool* pool = b->pool;
-  DeviceGuard g(pool->device);
-  cudaStream_t s = as_stream(stream);
+  return plan_step(b, sids, firsts, lens, nullptr, nullptr, n, num_tokens, max_len, stream);
+}
+
+lv_status lv_batch_share(lv_batch* b, int32_t rows) {
+  NvtxRange nvtx_range("lv_batch_share");
+  if (!b || b->share_rows || rows < 1 || rows > b->d.max_tokens || b->d.window > 0) return LV_ERR_INVALID;
+  DeviceGuard g(b->pool->device);
+  const size_t kept = b->allocs.size();
+  const int most = std::max(rows_ctas(b), b->pool->num_sms);
+  const size_t heads = (size_t)rows * b->d.num_q_heads;
+  lv_status st;
   try {
-    LV_TRY(join_copies(pool, s));   // the step reads and writes KV bytes
-    Staging st(pool, s);
-    const void *si = nullptr, *fi = nullptr, *le = nullptr;
-    lv_status r;
-    // every CTA reads the lengths: host memory is copied in
-    if ((r = st.in(sids, (size_t)n * 4, &si, true, true)) != LV_OK ||
-        (r = st.in(lens, (size_t)n * 4, &le, true, true)) != LV_OK)
-      return r;
-    if (firsts && (r = st.in(firsts, (size_t)n * 4, &fi, true, true)) != LV_OK) return r;
-    max_len = std::min(max_len, num_tokens);
-    // more rows a request than one m16n8k16 tile holds: the kernel for many rows, where pages can be
-    // read by TMA (32 sessions of 1000 to 4000 keys with 4 new tokens, 32 rows, took 42 us with it and
-    // 115 in tiles of 32 rows of the other; with 1 token, 8 rows, the other reads at 6 TB/s).
-    // One kernel a step: 47 single tokens and 3 chunks of 600 to 1500 took 165 us in one launch, and 62
-    // and 107 as a step of each kind
-    const lv::AttnKind kind =
-        (long long)max_len * b->G > lv::kRowsRows && b->box_rows ? lv::ATTN_TC : lv::ATTN_ROWS;
-    lv::PlanArgs a{};
-    a.p = pool->d;
-    a.sids = static_cast<const int32_t*>(si);
-    a.firsts = static_cast<const int32_t*>(fi);
-    a.lens = static_cast<const int32_t*>(le);
-    a.n = n;
-    a.num_tokens = num_tokens;
-    a.max_len = max_len;
-    a.G = b->G;
-    // Shares of at least min_share units, pairs of up to uncut units in one piece where there is room
-    // (many rows: 8 sessions with 4 new tokens after 1000 to 4000 keys 20.6 us, 23.2 at 4 units, and the
-    // longer steps alike; 64 tokens at 1000 keys 19.7, and 22.2 at 6 uncut units.  Few rows: 1000 keys
-    // 13.1 us, 14.7 at 16 units, 4000 keys 17.4, 18.6 at 4; 64 sessions of 100 to 300 keys 12.1, and 16.6
-    // at 12 uncut units).
-    if (kind == lv::ATTN_TC) {
-      a.line_heads = pool->kv_heads;
-      a.tile_rows = lv::tc_tile_rows(b->G);
-      a.unit_shift = lv::kTcUnitShift;
-      a.lead = lv::kTcLead;
-      a.min_share = 3;
-      a.uncut = 12;
-      a.ctas = a.shares = pool->num_sms;
-    } else {
-      a.line_heads = 1;
-      a.tile_rows = lv::kRowsRows;
-      a.unit_shift = lv::kRowsUnitShift;
-      a.lead = lv::kRowsLead;
-      a.min_share = 8;
-      a.uncut = 24;
-      a.shares = rows_shares(b);
-      a.ctas = rows_ctas(b);
+    if ((st = batch_alloc(b, &b->pre_reqs, b->d.max_requests)) == LV_OK &&
+        (st = batch_alloc(b, &b->continued, b->d.max_requests)) == LV_OK &&
+        (st = batch_alloc(b, &b->pre_tiles, b->max_tiles)) == LV_OK &&
+        (st = batch_alloc(b, &b->pre_work, most)) == LV_OK && (st = batch_alloc(b, &b->pre_head, 1)) == LV_OK &&
+        (st = batch_alloc(b, &b->pre_o, heads * b->dp)) == LV_OK && (st = batch_alloc(b, &b->pre_ml, heads)) == LV_OK) {
+      // (waits: the batch may be used on any stream next)
+      if (cudaMemset(b->pre_head, 0xff, sizeof(lv::StepHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
+        st = LV_ERR_CUDA;
     }
-    a.window = b->d.window;
-    a.sinks = b->d.sinks;
-    a.row_starts = b->d.row_starts;
-    a.kv_lens = b->d.kv_lens;
-    a.tables = b->d.tables;
-    a.positions = b->d.positions;
-    a.slots = b->d.slots;
-    a.reqs = b->reqs;
-    a.tiles = b->tiles;
-    a.max_tiles = b->max_tiles;
-    a.work = b->work;
-    a.arrived = b->arrived;
-    a.ticket = b->ticket;
-    a.kind = kind;
-    a.head = b->head;
-    b->planned = false;      // (the old step's arrays are being written over)
-    LV_TRY(lv::launch_plan(a, s));
-    b->planned = true;
-    b->num_tokens = num_tokens;
-    b->kind = kind;
-    b->ctas = a.ctas;
-    return st.finish();
   } catch (const std::bad_alloc&) {
-    return LV_ERR_OOM;
+    st = LV_ERR_OOM;
   }
+  if (st != LV_OK) {
+    while (b->allocs.size() > kept) {
+      cudaFree(b->allocs.back());
+      b->allocs.pop_back();
+    }
+    return st;
+  }
+  b->share_rows = rows;
+  return LV_OK;
+}
+
+lv_status lv_batch_plan_shared(lv_batch* b, const int32_t* sids, const int32_t* firsts, const int32_t* lens,
+                               const int32_t* prefixes, const int32_t* prefix_lens, int32_t n, int32_t num_tokens,
+                               int32_t max_len, lv_stream stream) {
+  NvtxRange nvtx_range("lv_batch_plan_shared");
+  if (!b || !b->share_rows || num_tokens > b->share_rows || n < 0 || (n > 0 && !prefixes)) return LV_ERR_INVALID;
+  return plan_step(b, sids, firsts, lens, n > 0 ? prefixes : nullptr, n > 0 ? prefix_lens : nullptr, n, num_tokens, max_len, stream);
 }
 
 lv_status lv_kv_write(lv_batch* b, int32_t layer, const lv_heads* k, const lv_heads* v, lv_stream stream) {
@@ -1984,7 +2072,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
     return LV_ERR_INVALID;
   if (lse && !device_array(pool, lse, 4)) return LV_ERR_INVALID;
   cudaStream_t s = as_stream(stream);
-  const bool bf16 = b->d.dtype == LV_BF16, tc = b->kind == lv::ATTN_TC;
+  const bool bf16 = b->d.dtype == LV_BF16;
   lv::AttnArgs a{};
   for (int i = 0; i < 2; ++i) a.kv[i] = pool->kv[2 * layer + i];
   a.P = pool->d.P;
@@ -2015,7 +2103,6 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.num_tokens = b->num_tokens;
   a.window = b->d.window;
   a.sinks = b->d.sinks;
-  a.tile_rows = tc ? lv::tc_tile_rows(b->G) : lv::kRowsRows;
   a.dp = b->dp;
   a.scale = scale2;
   a.part_o = b->part_o;
@@ -2023,15 +2110,36 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.ctl = pool->d.ctl;
   a.wait_ns = b->wait_ns;
   a.hold = b->hold;
-  if (tc) {
-    CUtensorMap qmap;
-    const lv::TcMaps m{&b->maps[2 * layer], &b->maps[2 * layer + 1],
-                       a.q_vec && query_map(b, q, &qmap) ? &qmap : nullptr, b->box_rows};
-    LV_TRY(lv::launch_attend_tc(a, m, bf16, b->ctas, s));
-  } else {
+  CUtensorMap qmap;
+  const bool any_tc = b->kind == lv::ATTN_TC || (b->shared && b->pre_kind == lv::ATTN_TC);
+  const bool q_tma = any_tc && a.q_vec && query_map(b, q, &qmap);
+  auto launch = [&](const lv::AttnArgs& x, lv::AttnKind kind, int ctas, lv::AttnMode mode) {
+    if (kind == lv::ATTN_TC) {
+      const lv::TcMaps m{&b->maps[2 * layer], &b->maps[2 * layer + 1], q_tma ? &qmap : nullptr, b->box_rows};
+      return lv::launch_attend_tc(x, m, bf16, ctas, mode, s);
+    }
     const CUtensorMap* m = b->rows_maps.empty() ? nullptr : &b->rows_maps[2 * layer];
-    LV_TRY(lv::launch_attend_rows(a, m, m ? m + 1 : nullptr, bf16, b->ctas, s));
+    return lv::launch_attend_rows(x, m, m ? m + 1 : nullptr, bf16, ctas, mode, s);
+  };
+  auto tile_rows = [&](lv::AttnKind kind) { return kind == lv::ATTN_TC ? lv::tc_tile_rows(b->G) : lv::kRowsRows; };
+  a.tile_rows = tile_rows(b->kind);
+  if (!b->shared) {
+    LV_TRY(launch(a, b->kind, b->ctas, lv::kWhole));
+    return LV_OK;
   }
+  a.own_head = b->head;
+  a.pre_head = b->pre_head;
+  a.pre_kind = b->pre_kind;
+  a.pre_o = b->pre_o;
+  a.pre_ml = b->pre_ml;
+  lv::AttnArgs x = a;      // over the prefixes, by the pool's tables
+  x.tables = pool->d.table;
+  x.tiles = b->pre_tiles;
+  x.work = b->pre_work;
+  x.head = b->pre_head;
+  x.tile_rows = tile_rows(b->pre_kind);
+  LV_TRY(launch(x, b->pre_kind, b->pre_ctas, lv::kPrefix));
+  LV_TRY(launch(a, b->kind, b->ctas, lv::kJoined));
   return LV_OK;
 }
 

@@ -129,7 +129,7 @@ struct RowsShape {
 // Pieces p0, p0 + step, ... (count of them) of a cut pair joined by a CTA, a warp a row: every piece's
 // sums weighted by its maximum against the largest, in the pieces' order.  To the output, or
 // (not kLast) to the first of the pieces' own slots.
-template <int DP, bool kBf16, bool kLast>
+template <int DP, bool kBf16, bool kLast, int kMode>
 __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, int head, int64_t first, int p0,
                                           int step, int count) {
   const int lane = threadIdx.x & 31;
@@ -140,7 +140,13 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
       const int p = p0 + i * step;
       return part_slot((first + p) * a.H + head, p == 0) * kRowsRows + row;
     };
-    float top = -INFINITY;
+    const int R = t.row0 + row, token = R / a.G, g = R - token * a.G;
+    const int64_t r = t.qrow + token;
+    const int h = head * a.G + g;
+    const bool joined = kMode == kJoined && kLast && t.req >= kSharedTile;
+    float2 pre = make_float2(-INFINITY, 0.f);
+    if (joined) pre = __ldcg(&a.pre_ml[r * (a.H * a.G) + h]);
+    float top = pre.x;
     for (int i = lane; i < count; i += 32) top = fmaxf(top, __ldcg(&a.part_ml[at(i)]).x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -182,10 +188,25 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
       if (lane == 0) a.part_ml[at(0)] = make_float2(top, sum);
       continue;
     }
+    if constexpr (kMode == kPrefix) {
+      float* o = a.pre_o + (r * (a.H * a.G) + h) * DP + kCols * lane;
+#pragma unroll
+      for (int e = 0; e < kCols; e += 2) *reinterpret_cast<float2*>(o + e) = make_float2(acc[e], acc[e + 1]);
+      if (lane == 0) a.pre_ml[r * (a.H * a.G) + h] = make_float2(top, sum);
+      continue;
+    }
+    if (joined) {
+      const float f = pre.x == top ? 1.f : exp2_fast(pre.x - top);
+      const float* o = a.pre_o + (r * (a.H * a.G) + h) * DP + kCols * lane;
+      sum += pre.y * f;
+#pragma unroll
+      for (int e = 0; e < kCols; e += 2) {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(o + e));
+        acc[e] += v.x * f;
+        acc[e + 1] += v.y * f;
+      }
+    }
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    const int R = t.row0 + row, token = R / a.G, g = R - token * a.G;
-    const int64_t r = t.qrow + token;
-    const int h = head * a.G + g;
     uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head + kCols * lane;
     if (kCols * lane < a.D) {
 #pragma unroll
@@ -228,7 +249,9 @@ constexpr int kAlone = 32, kGroup = 12;
 // kTma: a unit's K and V come by TMA, a box of 16 keys and 64 columns each, where pages hold whole
 // units (T a multiple of 16); else by 16-byte copies, a key at a time from its page.  In shared
 // memory a unit is [64-column block][key][128 bytes], swizzled as TMA does it.
-template <int DP, bool kBf16, bool kTma>
+// kMode: over the requests' contexts, over prefixes (whose table rows are the pool's, and all of whose keys every
+// row sees), or over the contexts behind prefixes, whose sums are one more piece of each row.
+template <int DP, bool kBf16, bool kTma, int kMode>
 __global__ void __launch_bounds__(kThreads, RowsShape<DP>::kCtas)
 k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap kmap,
               const __grid_constant__ CUtensorMap vmap) {
@@ -255,17 +278,18 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
   const CtaWork work = load_words(&a.work[group]);
   const StepHead step = load_words(a.head);
-  if (LV_RARE(!step_fits(step, ATTN_ROWS, a.num_tokens))) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
+  if (LV_RARE(!step_fits<kMode>(a, step, ATTN_ROWS))) {
+    if (kMode != kPrefix && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
     return;
   }
-  const bool dead = step.live < a.num_tokens;
+  const bool dead = kMode != kPrefix && step.live < a.num_tokens;
+  auto req_of = [&](const AttnTile& t) { return (size_t)(kMode == kJoined ? t.req & (kSharedTile - 1) : t.req); };
   auto key_of = [&](const AttnTile& t, int u) { return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kU; };
   auto hidden = [&](const AttnTile& t, int key) { return key >= t.kv_hi || (key < t.kv_lo && key >= a.sinks); };
   auto find_page = [&](Walk& x) {
     if (kTma && x.u < x.u_end) {
       const uint32_t key = key_of(x.t, x.u), b = a.t_shift >= 0 ? key >> a.t_shift : key / (uint32_t)a.T;
-      x.page = a.tables[(size_t)x.t.req * a.maxB + b];
+      x.page = a.tables[req_of(x.t) * a.maxB + b];
       x.off = key - b * a.T;
     }
   };
@@ -327,7 +351,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         bool ok = !hidden(L.t, key) && c * 8 < a.D;
         int32_t page = -1;
         const uint32_t b = (uint32_t)key / (uint32_t)a.T;
-        if (ok) page = a.tables[(size_t)L.t.req * a.maxB + b];
+        if (ok) page = a.tables[req_of(L.t) * a.maxB + b];
         ok = ok && (uint32_t)page < a.hbm_pages;
         const size_t off = ok ? (size_t)page * a.P + (size_t)(key - b * a.T) * tok + head_at + c * 16 : 0;
         const uint32_t to = dst + (c >> 3) * kU * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
@@ -359,7 +383,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = lane / 4 + 8 * i, R = C.t.row0 + min(row, C.t.rows - 1), token = R / a.G;
-      pos[i] = C.t.first + token;
+      pos[i] = kMode == kPrefix ? C.t.kv_hi - 1 : C.t.first + token;
       const uint16_t* x = q + (C.t.qrow + token) * a.q_row + (int64_t)(head * a.G + (R - token * a.G)) * a.q_head;
       auto two = [&](int d) -> uint32_t {      // elements d, d + 1; zeros past the rows and columns
         if (row >= C.t.rows || d >= a.D) return 0u;
@@ -380,7 +404,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) top[i] = -INFINITY, sum[i] = 0.f;
-    const int p_lo = C.t.first + C.t.row0 / a.G, p_hi = C.t.kv_hi - 1;
+    const int p_hi = C.t.kv_hi - 1, p_lo = kMode == kPrefix ? p_hi : C.t.first + C.t.row0 / a.G;
 
 #pragma unroll 1
     for (int u = C.u; u < C.u_end; u += kWarps) {
@@ -546,6 +570,26 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
           const int R = C.t.row0 + row, token = R / a.G, g = R - token * a.G;
           const int64_t r = C.t.qrow + token;
           const int h = head * a.G + g;
+          if constexpr (kMode == kPrefix) {
+            float* po = a.pre_o + (r * (a.H * a.G) + h) * DP;
+#pragma unroll
+            for (int d = 0; d < DP / 8; ++d)
+              *reinterpret_cast<float2*>(po + 8 * d + 2 * (lane & 3)) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
+            if ((lane & 3) == 0) a.pre_ml[r * (a.H * a.G) + h] = make_float2(top[i], sum[i]);
+            continue;
+          }
+          if (kMode == kJoined && C.t.req >= kSharedTile) {
+            const float2 pre = __ldcg(&a.pre_ml[r * (a.H * a.G) + h]);
+            const float* po = a.pre_o + (r * (a.H * a.G) + h) * DP + 2 * (lane & 3);
+            const float2 f = join_factors(top[i], pre, &top[i]);
+            sum[i] = sum[i] * f.x + pre.y * f.y;
+#pragma unroll
+            for (int d = 0; d < DP / 8; ++d) {
+              const float2 v = __ldcg(reinterpret_cast<const float2*>(po + 8 * d));
+              o[d][2 * i] = o[d][2 * i] * f.x + v.x * f.y;
+              o[d][2 * i + 1] = o[d][2 * i + 1] * f.x + v.y * f.y;
+            }
+          }
           const float inv = sum[i] > 0.f || sum[i] != sum[i] ? 1.f / sum[i] : 0.f;
           uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head;
 #pragma unroll
@@ -616,16 +660,16 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       };
       const int was = n == 0 ? was_first : was_last;
       if (!grouped) {
-        if (last(was, 0, ps.count, 0)) join_rows<DP, kBf16, true>(a, t, head, ps.first, 0, 1, ps.count);
+        if (last(was, 0, ps.count, 0)) join_rows<DP, kBf16, true, kMode>(a, t, head, ps.first, 0, 1, ps.count);
         continue;
       }
       if (!last(was, g0, g_count, g0 ? 2 : 1)) continue;
-      join_rows<DP, kBf16, false>(a, t, head, ps.first, g0, 1, g_count);
+      join_rows<DP, kBf16, false, kMode>(a, t, head, ps.first, g0, 1, g_count);
       const int groups = (ps.count + kGroup - 1) / kGroup;
       __syncthreads();
       int was2 = 0;
       if (threadIdx.x == 0) was2 = add_release(&a.arrived[(ps.first * a.H + head) * kArriveWords], 1);
-      if (last(was2, 0, groups, 0)) join_rows<DP, kBf16, true>(a, t, head, ps.first, 0, kGroup, groups);
+      if (last(was2, 0, groups, 0)) join_rows<DP, kBf16, true, kMode>(a, t, head, ps.first, 0, kGroup, groups);
     }
   }
   if (!kTma) copy_wait<0>();
@@ -640,9 +684,9 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   if (dead) clear_dead(a, blockIdx.x * kThreads + threadIdx.x, gridDim.x * kThreads);
 }
 
-template <int DP, bool kTma>
+template <int DP, bool kTma, int kMode>
 cudaError_t set_rows() {
-  for (auto k : {k_attend_rows<DP, true, kTma>, k_attend_rows<DP, false, kTma>}) {
+  for (auto k : {k_attend_rows<DP, true, kTma, kMode>, k_attend_rows<DP, false, kTma, kMode>}) {
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP>::kSmem);
     // (the default split leaves room for one CTA)
     if (e == cudaSuccess)
@@ -652,18 +696,33 @@ cudaError_t set_rows() {
   return cudaSuccess;
 }
 
-template <int DP, bool kTma>
+template <int kMode>
+cudaError_t set_mode() {
+  for (cudaError_t e : {set_rows<64, true, kMode>(), set_rows<128, true, kMode>(), set_rows<64, false, kMode>(),
+                        set_rows<128, false, kMode>(), set_rows<256, false, kMode>()})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
+}
+
+template <int DP, bool kTma, int kMode>
 cudaError_t run_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16, int ctas, cudaStream_t s) {
   static const CUtensorMap none{};
-  return launch_dependent(bf16 ? k_attend_rows<DP, true, kTma> : k_attend_rows<DP, false, kTma>, dim3(ctas), kThreads,
-                          RowsShape<DP>::kSmem, s, a, k ? *k : none, v ? *v : none);
+  return launch_dependent(bf16 ? k_attend_rows<DP, true, kTma, kMode> : k_attend_rows<DP, false, kTma, kMode>, dim3(ctas),
+                          kThreads, RowsShape<DP>::kSmem, s, a, k ? *k : none, v ? *v : none);
+}
+
+template <int kMode>
+cudaError_t run_mode(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16, int ctas, cudaStream_t s) {
+  if (a.dp == 256) return run_rows<256, false, kMode>(a, k, v, bf16, ctas, s);
+  if (a.dp == 64)
+    return k ? run_rows<64, true, kMode>(a, k, v, bf16, ctas, s) : run_rows<64, false, kMode>(a, k, v, bf16, ctas, s);
+  return k ? run_rows<128, true, kMode>(a, k, v, bf16, ctas, s) : run_rows<128, false, kMode>(a, k, v, bf16, ctas, s);
 }
 
 }  // namespace
 
 cudaError_t configure_attend() {
-  for (cudaError_t e : {set_rows<64, true>(), set_rows<128, true>(), set_rows<64, false>(), set_rows<128, false>(),
-                        set_rows<256, false>()})
+  for (cudaError_t e : {set_mode<kWhole>(), set_mode<kPrefix>(), set_mode<kJoined>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }
@@ -672,10 +731,10 @@ cudaError_t configure_attend() {
 int attend_rows_ctas(int dp) { return dp == 256 ? RowsShape<256>::kCtas : RowsShape<128>::kCtas; }
 
 cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16, int ctas,
-                               cudaStream_t s) {
-  if (a.dp == 256) return run_rows<256, false>(a, k, v, bf16, ctas, s);
-  if (a.dp == 64) return k ? run_rows<64, true>(a, k, v, bf16, ctas, s) : run_rows<64, false>(a, k, v, bf16, ctas, s);
-  return k ? run_rows<128, true>(a, k, v, bf16, ctas, s) : run_rows<128, false>(a, k, v, bf16, ctas, s);
+                               AttnMode mode, cudaStream_t s) {
+  return mode == kPrefix   ? run_mode<kPrefix>(a, k, v, bf16, ctas, s)
+         : mode == kJoined ? run_mode<kJoined>(a, k, v, bf16, ctas, s)
+                           : run_mode<kWhole>(a, k, v, bf16, ctas, s);
 }
 
 }  // namespace lv

@@ -223,16 +223,21 @@ __device__ __forceinline__ float4* part_at(const AttnArgs& a, int64_t slot, int 
 // Pieces p0, p0 + step, ... (count of them) of a cut pair joined by one warp, a lane a row of the
 // tile: every piece's sums weighted by its maximum against the largest, in the pieces' order.  To
 // the output, or (not last) to the first of the pieces' own slots.
-template <int DP, bool kBf16>
+template <int DP, bool kBf16, int kMode>
 __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int p0, int step, int count, bool last,
-                                          int row, bool mine, uint16_t* out, int64_t r, int hq) {
+                                          int row, bool mine, bool shared, uint16_t* out, int64_t r, int hq) {
   auto slot = [&](int i) {
     const int p = p0 + min(i, count - 1) * step;
     return part_slot(first + p, p == 0);
   };
   auto ml_of = [&](int i) { return __ldcg(&a.part_ml[slot(i) * a.tile_rows + row]); };
+  const int64_t at_pre = r * (a.H * a.G) + hq;
+  const bool joined = kMode == kJoined && shared && last;
   float top = -INFINITY, sum = 0.f;
   if (mine) {
+    float2 pre = make_float2(-INFINITY, 0.f);
+    if (joined) pre = __ldcg(&a.pre_ml[at_pre]);
+    top = pre.x;
     for (int i = 0; i < count; i += 4) {
       float x[4];
 #pragma unroll
@@ -268,6 +273,25 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
         for (int c = 0; c < 16; ++c) o[c * a.tile_rows] = acc[c];
         continue;
       }
+      if constexpr (kMode == kPrefix) {
+        float4* o = reinterpret_cast<float4*>(a.pre_o + at_pre * DP + c0);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) o[c] = acc[c];
+        continue;
+      }
+      if (joined) {
+        const float f = pre.x == top ? 1.f : exp2_fast(pre.x - top);
+        const float4* o = reinterpret_cast<const float4*>(a.pre_o + at_pre * DP + c0);
+        sum += pre.y * f;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          const float4 v = __ldcg(o + c);
+          acc[c].x += v.x * f;
+          acc[c].y += v.y * f;
+          acc[c].z += v.z * f;
+          acc[c].w += v.w * f;
+        }
+      }
       const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
 #pragma unroll
       for (int c = 0; c < 16; c += 2) {
@@ -290,6 +314,8 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
     }
     if (!last)
       a.part_ml[slot(0) * a.tile_rows + row] = make_float2(top, sum);
+    else if (kMode == kPrefix)
+      a.pre_ml[at_pre] = make_float2(top, sum);
     else if (a.lse)
       a.lse[r * (a.H * a.G) + hq] =
           sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
@@ -302,6 +328,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
 constexpr int kAlone = 6, kGroup = 5;
 
 // The pairs (tile, head) of a CTA's share, one after the other.
+template <int kMode>
 struct Pairs {
   long long w, end;
   int share, lead;
@@ -312,7 +339,7 @@ struct Pairs {
     const StepHead step = load_words(a.head);
     const CtaWork x = load_words(&a.work[blockIdx.x]);
     w = x.begin;
-    end = step_fits(step, ATTN_TC, a.num_tokens) ? x.end : x.begin;
+    end = step_fits<kMode>(a, step, ATTN_TC) ? x.end : x.begin;
     share = x.share;
     lead = x.lead;
     t = x.t;
@@ -333,6 +360,8 @@ struct Pairs {
     }
     return false;
   }
+  __device__ __forceinline__ size_t req() const { return kMode == kJoined ? t.req & (kSharedTile - 1) : t.req; }
+  __device__ __forceinline__ bool shared() const { return kMode == kJoined && t.req >= kSharedTile; }
   __device__ __forceinline__ int key_of(int u) const {
     return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kKeys;
   }
@@ -492,7 +521,9 @@ struct Softmax {
 //   warp 10  S = Q K^T (tcgen05, operands in shared memory), O += P V (P in TMEM)
 //   warp 11  queries, and zeros in the rows of V units that no row of the tile sees
 //   0 .. 7   softmax, a thread a row, and the pair's end: O / sum, or the sums of a cut pair
-template <int DP, bool kBf16>
+// kMode: over the requests' contexts, over prefixes (whose table rows are the pool's, and all of whose keys every
+// row sees), or over the contexts behind prefixes, whose sums are one more piece of each row.
+template <int DP, bool kBf16, int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
 k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap kmap,
             const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap, int box_rows,
@@ -541,10 +572,10 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     const uint32_t lanes = tmem + ((uint32_t)(wid & 3) << 21);            // this warp's 32 lanes of TMEM
     const uint32_t s_at = lanes + 128 * half, o_at = lanes + S::kColO + DP * half;
     uint32_t s_par = 0, o_par = 0;
-    Pairs pr;
+    Pairs<kMode> pr;
     pr.init(a);
     bool ok = true;
-    Pairs nx = pr;
+    Pairs<kMode> nx = pr;
     bool has = nx.next(a);
     while (ok && has) {
       pr = nx;
@@ -556,8 +587,9 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const bool live = rows > (row & ~31);                 // rows in this warp
       const int R0 = pr.t.row0 + half * half_rows;
       const int R = R0 + min(row, rows - 1), token = R / a.G;
-      const int pos = pr.t.first + token;
-      const int p_lo = pr.t.first + R0 / a.G, p_hi = pr.t.first + (R0 + rows - 1) / a.G;
+      const int end = pr.t.kv_hi - 1, pos = kMode == kPrefix ? end : pr.t.first + token;
+      const int p_lo = kMode == kPrefix ? end : pr.t.first + R0 / a.G;
+      const int p_hi = kMode == kPrefix ? end : pr.t.first + (R0 + rows - 1) / a.G;
       Softmax<DP, kBf16> sm;
       for (int u = pr.u0; u < pr.u1; ++u) {
         if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par, a.wait_ns))) break;
@@ -585,7 +617,17 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const int hq = pr.head * a.G + (R - token * a.G);
       const int64_t r = pr.t.qrow + token;
       const bool mine = row < rows;
-      const float inv = !whole ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
+      float top2 = sm.top * a.scale;      // in log2
+      // whole pairs behind a prefix: this and its sums, joined
+      const int64_t at_pre = r * (a.H * a.G) + hq;
+      const bool joined = kMode == kJoined && whole && pr.shared();
+      float2 f = make_float2(1.f, 0.f);
+      if (joined) {
+        const float2 pre = __ldcg(&a.pre_ml[at_pre]);
+        f = join_factors(top2, pre, &top2);
+        sm.sum = sm.sum * f.x + pre.y * f.y;
+      }
+      const float inv = !whole || kMode == kPrefix ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
       const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0);
       const int t_row = half * half_rows + row;
       uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + hq * a.o_head;
@@ -603,7 +645,26 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         tc_wait_ld();
         tc_loaded<32>(o);
         uint32_t w[16];
-        if (whole) {
+        if (kMode == kPrefix && whole) {
+          float4* po = reinterpret_cast<float4*>(a.pre_o + at_pre * DP + col);
+          if (mine) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              po[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                  __uint_as_float(o[4 * e + 3]));
+          }
+        } else if (whole) {
+          if (joined) {
+            const float4* po = reinterpret_cast<const float4*>(a.pre_o + at_pre * DP + col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 v = __ldcg(po + e);
+              const float add[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                o[4 * e + k] = __float_as_uint(__uint_as_float(o[4 * e + k]) * f.x + add[k] * f.y);
+            }
+          }
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             w[e] = pack16<kBf16>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
@@ -638,7 +699,6 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
         __syncwarp();
       }
-      const float top2 = sm.top * a.scale;      // in log2
       if (!whole) {
         if (mine) a.part_ml[slot * a.tile_rows + t_row] = make_float2(top2, sm.sum);
         // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
@@ -659,19 +719,21 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         };
         if (ps.count <= kAlone) {
           if (last(0, ps.count, 0))
-            join_rows<DP, kBf16>(a, ps.first, 0, 1, ps.count, true, t_row, mine, out, r, hq);
+            join_rows<DP, kBf16, kMode>(a, ps.first, 0, 1, ps.count, true, t_row, mine, pr.shared(), out, r, hq);
         } else {
           const int g0 = (int)(blockIdx.x - ps.first) / kGroup * kGroup, n = min(kGroup, ps.count - g0);
           const int groups = (ps.count + kGroup - 1) / kGroup;
           if (last(g0, n, g0 ? 2 : 1)) {
 #pragma unroll 1
             for (int step = 0; step < 2; ++step) {
-              join_rows<DP, kBf16>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, t_row, mine,
-                                   out, r, hq);
+              join_rows<DP, kBf16, kMode>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, t_row,
+                                          mine, pr.shared(), out, r, hq);
               if (step || !last(0, groups, 0)) break;
             }
           }
         }
+      } else if (kMode == kPrefix) {
+        if (mine) a.pre_ml[at_pre] = make_float2(top2, sm.sum);
       } else if (mine && a.lse) {
         a.lse[r * (a.H * a.G) + hq] =
             sm.sum == 0.f ? -INFINITY : (top2 - weight_bias<kBf16>()) * 0.693147180559945f + logf(sm.sum);
@@ -681,7 +743,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     tc_fence_before();
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-    Pairs pr;
+    Pairs<kMode> pr;
     pr.init(a);
     if (wid == kWarpK || wid == kWarpV) {
       // ---- K (or V): lane i finds the page of a unit's box of box_rows keys; one thread then
@@ -694,7 +756,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       auto page_of = [&](int u) {
         const int key = pr.key_of(u) + lane * box_rows;
         if (lane >= boxes || u >= pr.u1 || key >= pr.t.kv_hi || (key + box_rows <= pr.t.kv_lo && key >= a.sinks)) return -1;
-        return a.tables[(size_t)pr.t.req * a.maxB + key / a.T];
+        return a.tables[pr.req() * a.maxB + key / a.T];
       };
       while (ok && pr.next(a)) {
         int next = page_of(pr.u0);
@@ -767,7 +829,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             tc_mma_ts(tmem + S::kColO + DP * half, tmem + 128 * half + 8 * k, vd + k * (2048 >> 4), kDescO, add || k > k0);
         };
         // a pair's units; false when a wait ran out.  nx: the pair after it, found meanwhile
-        Pairs nx = pr;
+        Pairs<kMode> nx = pr;
         bool has = nx.next(a);
         auto pair = [&](auto halves_of) -> bool {
           constexpr int kHalves = decltype(halves_of)::value;
@@ -918,8 +980,8 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       }
       // rows of no request
       const StepHead step = load_words(a.head);
-      const bool fits = step_fits(step, ATTN_TC, a.num_tokens);
-      if (LV_RARE(!fits) && blockIdx.x == 0 && lane == 0) report(a.ctl, LV_ERR_STATE, -1);
+      const bool fits = kMode != kPrefix && step_fits<kMode>(a, step, ATTN_TC);
+      if (kMode != kPrefix && LV_RARE(!fits) && blockIdx.x == 0 && lane == 0) report(a.ctl, LV_ERR_STATE, -1);
       if (ok && fits && step.live < a.num_tokens) {
         const int Hq = a.H * a.G;
         for (int r = blockIdx.x; r < a.num_tokens; r += gridDim.x) {
@@ -944,30 +1006,41 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   }
 }
 
-template <int DP, bool kBf16>
+template <int DP, bool kBf16, int kMode>
 cudaError_t run(const AttnArgs& a, const TcMaps& m, int ctas, cudaStream_t s) {
   static const CUtensorMap none{};
-  return launch_dependent(k_attend_tc<DP, kBf16>, dim3(ctas), kThreads, TcShape<DP>::kSmem, s, a, *m.k, *m.v,
+  return launch_dependent(k_attend_tc<DP, kBf16, kMode>, dim3(ctas), kThreads, TcShape<DP>::kSmem, s, a, *m.k, *m.v,
                           m.q ? *m.q : none, m.box_rows, a.tile_rows / 2, m.q ? 1 : 0);
 }
 
-}  // namespace
-
-cudaError_t configure_attend_tc() {
-  for (auto k : {k_attend_tc<64, true>, k_attend_tc<64, false>}) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<64>::kSmem);
-    if (e != cudaSuccess) return e;
-  }
-  for (auto k : {k_attend_tc<128, true>, k_attend_tc<128, false>}) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<128>::kSmem);
+template <int DP, int kMode>
+cudaError_t set() {
+  for (auto k : {k_attend_tc<DP, true, kMode>, k_attend_tc<DP, false, kMode>}) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<DP>::kSmem);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
-cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cudaStream_t s) {
-  if (a.dp == 64) return bf16 ? run<64, true>(a, m, ctas, s) : run<64, false>(a, m, ctas, s);
-  return bf16 ? run<128, true>(a, m, ctas, s) : run<128, false>(a, m, ctas, s);
+template <int kMode>
+cudaError_t run_mode(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cudaStream_t s) {
+  if (a.dp == 64) return bf16 ? run<64, true, kMode>(a, m, ctas, s) : run<64, false, kMode>(a, m, ctas, s);
+  return bf16 ? run<128, true, kMode>(a, m, ctas, s) : run<128, false, kMode>(a, m, ctas, s);
+}
+
+}  // namespace
+
+cudaError_t configure_attend_tc() {
+  for (cudaError_t e : {set<64, kWhole>(), set<128, kWhole>(), set<64, kPrefix>(), set<128, kPrefix>(),
+                        set<64, kJoined>(), set<128, kJoined>()})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
+}
+
+cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, AttnMode mode, cudaStream_t s) {
+  return mode == kPrefix   ? run_mode<kPrefix>(a, m, bf16, ctas, s)
+         : mode == kJoined ? run_mode<kJoined>(a, m, bf16, ctas, s)
+                           : run_mode<kWhole>(a, m, bf16, ctas, s);
 }
 
 }  // namespace lv

@@ -46,20 +46,21 @@ __device__ __forceinline__ long long cta_sum(long long v, long long* ws) {
 }
 
 // (32-bit divisions: len * G is below 2^31)
-__device__ __forceinline__ int tiles_of(const PlanArgs& a, int len) {
+__device__ __forceinline__ int tiles_of(const PlanLine& a, int len) {
   return len > 0 ? (int)(((uint32_t)len * (uint32_t)a.G + (uint32_t)a.tile_rows - 1u) / (uint32_t)a.tile_rows) : 0;
 }
 
-__device__ __forceinline__ AttnTile make_tile(const PlanArgs& a, const PlanReq& r, int req, int k) {
+template <bool kGroups>
+__device__ __forceinline__ AttnTile make_tile(const PlanLine& a, const PlanReq& r, int req, int k) {
   const int up = (1 << a.unit_shift) - 1;
   AttnTile t;
   t.before = 0;
-  t.req = req;
+  t.req = kGroups ? r.sid : req | (r.sid >= kSharedReq ? kSharedTile : 0);
   t.row0 = k * a.tile_rows;
   t.rows = min(a.tile_rows, r.len * a.G - t.row0);
   t.first = r.first;
   t.qrow = r.qrow;
-  t.kv_hi = r.first + (int)((uint32_t)(t.row0 + t.rows - 1) / (uint32_t)a.G) + 1;
+  t.kv_hi = r.first + 1 + (kGroups ? 0 : (int)((uint32_t)(t.row0 + t.rows - 1) / (uint32_t)a.G));
   const int p0 = r.first + (int)((uint32_t)t.row0 / (uint32_t)a.G);
   t.kv_lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
   const int hi = (t.kv_hi + up) >> a.unit_shift;
@@ -74,10 +75,10 @@ __device__ __forceinline__ AttnTile make_tile(const PlanArgs& a, const PlanReq& 
 // twice (once to be counted, once to be written) rather than kept.  What bounds it is the chain: five
 // scans of two barriers each (tiles, owned rows, units, shares of either size; the last two and a vote only
 // where there may be pairs apart), some 5 us for 64 requests of one tile and 10 for 1024.
-template <int NT>
-__device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* first_tile) {
+template <int NT, bool kGroups>
+__device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests, long long* ws, int* first_tile) {
   // each request's first tile: a scan over the requests, a thread taking several in a row
-  const int per = (a.n + NT - 1) / NT, q0 = min((int)threadIdx.x * per, a.n), q1 = min(q0 + per, a.n);
+  const int per = (n + NT - 1) / NT, q0 = min((int)threadIdx.x * per, n), q1 = min(q0 + per, n);
   long long own = 0, tiles, live = 0;
   for (int q = q0; q < q1; ++q) {
     const int len = __ldcg(&a.reqs[q].len);
@@ -99,7 +100,7 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
   const int t0 = min((int)threadIdx.x * per_tile, n_tiles), t1 = min(t0 + per_tile, n_tiles);
   int req0 = 0;
   if (t0 < t1) {
-    int hi = a.n - 1;      // the last request whose first tile is not after t0
+    int hi = n - 1;      // the last request whose first tile is not after t0
     while (req0 < hi) {
       const int mid = (req0 + hi + 1) >> 1;
       if (first_tile[mid] <= t0) req0 = mid;
@@ -110,13 +111,13 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
     int q = req0, loaded = -1;
     PlanReq r{};
     for (int t = t0; t < t1; ++t) {
-      while (q + 1 < a.n && first_tile[q + 1] <= t) ++q;
+      while (q + 1 < n && first_tile[q + 1] <= t) ++q;
       if (q != loaded) {
         const int4 w = __ldcg(reinterpret_cast<const int4*>(&a.reqs[q]));
-        r = PlanReq{w.x, w.y, w.z, 0};
+        r = PlanReq{w.x, w.y, w.z, w.w};
         loaded = q;
       }
-      f(t, make_tile(a, r, q, t - first_tile[q]));
+      f(t, make_tile<kGroups>(a, r, q, t - first_tile[q]));
     }
   };
   long long my_units = 0, my_short = 0, my_long = 0;
@@ -142,7 +143,7 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
   const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
   units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
   const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
-  if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, 0};
+  if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, requests};
   // (zero already but after an attention that ran out of a wait)
   static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
   for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += NT)
@@ -171,7 +172,8 @@ __device__ __forceinline__ void cut_line(const PlanArgs& a, long long* ws, int* 
 // Every CTA
 // sums the lengths before its own (at most 16 KiB that stay in L2: less than a launch between
 // a scan and the rest would cost).  kCut: the CTA that finishes last cuts the line too.
-template <bool kCut>
+// kShared: requests may continue prefixes, whose blocks have to be in HBM too.
+template <bool kCut, bool kShared>
 __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_constant__ PlanArgs a) {
   __shared__ long long ws[kPlanThreads / 32];
   dep_wait();
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
     const int asked = a.lens[i];
     const int len = max(asked, 0);
     int err = 0;
-    int first = 0;
+    int first = 0, psid = -1, plen = 0;
     const bool known = sid >= 0 && sid < p.S;
     if (!known || asked < 0 || asked > a.max_len || start + len > a.num_tokens) {
       err = LV_ERR_BOUNDS;
@@ -205,6 +207,18 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
       if (first < 0 || (long long)first + len > ctx || (long long)first + len > 0x7ffff000ll ||
           ((long long)first + len + p.T - 1) / p.T > p.maxB)
         err = LV_ERR_BOUNDS;
+      if constexpr (kShared) {
+        psid = max(a.prefixes[i], -1);
+        if (psid >= p.S) {
+          err = LV_ERR_BOUNDS;
+        } else if (psid >= 0) {
+          const int all = p.sess[psid].ctx_tokens;
+          plen = a.prefix_lens ? a.prefix_lens[i] : all;
+          if (plen < 0 || plen > all || (long long)plen + first + len > 0x7ffff000ll) err = LV_ERR_BOUNDS;
+          if (plen == 0) psid = -1;
+        }
+        if (err) psid = -1, plen = 0;
+      }
     }
     const int32_t* row = p.table + (size_t)(known ? sid : 0) * p.maxB;
     int32_t* out = a.tables + (size_t)i * p.maxB;
@@ -227,6 +241,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
       }
       out[b] = e;
     }
+    if constexpr (kShared) {
+      const int pb = psid < 0 || len == 0 ? 0 : (int)(((uint32_t)plen + (uint32_t)p.T - 1u) / (uint32_t)p.T);
+      for (int b = threadIdx.x; b < pb; b += kPlanThreads) {
+        const int e = p.table[(size_t)psid * p.maxB + b];
+        absent |= e < 0 || e >= p.hbm_pages;
+      }
+    }
     if (__syncthreads_or(absent)) {
       err = LV_ERR_STATE;
       for (int b = threadIdx.x; b < nb; b += kPlanThreads) out[b] = -1;   // its own entries again
@@ -234,7 +255,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
     if (threadIdx.x == 0) {
       if (err) report(p.ctl, err, i);
       a.kv_lens[i] = err ? 0 : kv_len;
-      a.reqs[i] = PlanReq{first, err ? 0 : len, row0, 0};
+      if constexpr (kShared) a.continued[i] = err ? make_int2(-1, 0) : make_int2(psid, plen);
+      a.own.reqs[i] = PlanReq{first, err ? 0 : len, row0, known ? sid | (!err && psid >= 0 ? kSharedReq : 0) : 0};
     }
     const int rows = (int)min((long long)len, a.num_tokens - (long long)row0);
     for (int r = threadIdx.x; r < rows; r += kPlanThreads) {
@@ -246,7 +268,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
         slot = (long long)row[b] * p.T + (pos - b * p.T);
         if (p.incl && p.shadow[(size_t)sid * p.maxB + b] >= 0) slot = -slot - 2;
       }
-      a.positions[row0 + r] = pos;
+      a.positions[row0 + r] = kShared && !err ? pos + plen : pos;
       a.slots[row0 + r] = slot;
     }
   }
@@ -262,7 +284,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
     __syncthreads();
     if (!last) return;
     __threadfence();
-    cut_line<kPlanThreads>(a, ws, first_tile);
+    cut_line<kPlanThreads, false>(a.own, a.n, a.n, ws, first_tile);
   }
 }
 
@@ -271,7 +293,47 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut(const __grid_constant
   __shared__ int first_tile[kMaxRequests];
   dep_wait();
   dep_trigger();
-  cut_line<kCutThreads>(a, ws, first_tile);
+  cut_line<kCutThreads, false>(a.own, a.n, a.n, ws, first_tile);
+}
+
+// The same for a step with prefixes: CTA 0 cuts the requests' own contexts, CTA 1 finds the runs of requests
+// that continue the same tokens of the same session, makes each a request of all their rows, and cuts the
+// prefixes.  A run ends before the next request that begins one or has none: a bit a request, and the words
+// after a request's own searched for the next.
+__global__ void __launch_bounds__(kCutThreads) k_batch_cut_shared(const __grid_constant__ PlanArgs a) {
+  __shared__ long long ws[kCutThreads / 32];
+  __shared__ int first_tile[kMaxRequests];
+  __shared__ uint32_t ends[kMaxRequests / 32 + 1];
+  dep_wait();
+  dep_trigger();
+  if (blockIdx.x == 0) {
+    cut_line<kCutThreads, false>(a.own, a.n, a.n | kSharedStep, ws, first_tile);
+    return;
+  }
+  for (int i0 = 0; i0 < a.n; i0 += kCutThreads) {
+    const int i = i0 + (int)threadIdx.x;
+    const int2 none = make_int2(-1, 0);
+    const int2 me = i < a.n ? __ldcg(&a.continued[i]) : none, before = i > 0 && i < a.n ? __ldcg(&a.continued[i - 1]) : none;
+    const uint32_t w = __ballot_sync(0xffffffffu, i >= a.n || me.x < 0 || me.x != before.x || me.y != before.y);
+    if ((threadIdx.x & 31) == 0 && i < kMaxRequests) ends[i >> 5] = w;
+  }
+  __syncthreads();
+  const int words = (a.n + 31) >> 5;
+  for (int i = threadIdx.x; i < a.n; i += kCutThreads) {
+    const int2 me = __ldcg(&a.continued[i]);
+    PlanReq g{0, 0, 0, 0};
+    if (me.x >= 0 && (ends[i >> 5] >> (i & 31) & 1u)) {
+      int w = i >> 5;
+      uint32_t x = ends[w] & ~(0xffffffffu >> (31 - (i & 31)));      // bits after i's
+      while (!x && ++w < words) x = ends[w];
+      const int end = x ? min(32 * w + __ffs(x) - 1, a.n) : a.n;
+      const int r0 = __ldcg(&a.row_starts[i]);
+      g = PlanReq{me.y - 1, __ldcg(&a.row_starts[end]) - r0, r0, me.x};
+    }
+    a.pre.reqs[i] = g;
+  }
+  __syncthreads();      // (before other threads of this CTA read them)
+  cut_line<kCutThreads, true>(a.pre, a.n, a.n, ws, first_tile);
 }
 
 // ---------------------------------------------------------------- KV write
@@ -365,8 +427,13 @@ __global__ void __launch_bounds__(kWriteThreads) k_kv_write(const __grid_constan
 // One launch up to kOneLaunch requests (64 decoding sessions: 8.8 us, in two 10.2), else one CTA of
 // 1024 threads cuts the line by itself (1024 requests: 17 us; by the last CTA of the rows' 24).
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t s) {
-  if (a.n <= kOneLaunch) return launch_dependent(k_batch_rows<true>, dim3(a.n + 1), kPlanThreads, 0, s, a);
-  const cudaError_t e = launch_dependent(k_batch_rows<false>, dim3(a.n + 1), kPlanThreads, 0, s, a);
+  if (a.prefixes) {
+    const cudaError_t e = launch_dependent(k_batch_rows<false, true>, dim3(a.n + 1), kPlanThreads, 0, s, a);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(k_batch_cut_shared, dim3(2), kCutThreads, 0, s, a);
+  }
+  if (a.n <= kOneLaunch) return launch_dependent(k_batch_rows<true, false>, dim3(a.n + 1), kPlanThreads, 0, s, a);
+  const cudaError_t e = launch_dependent(k_batch_rows<false, false>, dim3(a.n + 1), kPlanThreads, 0, s, a);
   if (e != cudaSuccess) return e;
   return launch_dependent(k_batch_cut, dim3(1), kCutThreads, 0, s, a);
 }

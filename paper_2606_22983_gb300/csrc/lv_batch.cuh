@@ -16,7 +16,7 @@ namespace lv {
 // units of the kernel's size: first the units that hold sinks, then those from the window on.
 struct AttnTile {
   int64_t before;       // where it starts on the line
-  int32_t req;
+  int32_t req;          // and kSharedTile where its rows continue a prefix; a prefix's own tiles: its session
   int32_t row0;         // its first packed row
   int32_t rows;         // its packed rows
   int32_t units;        // units a head group
@@ -28,6 +28,7 @@ struct AttnTile {
   int32_t kv_hi;        // keys up to the tile's last row
 };
 static_assert(sizeof(AttnTile) == 48, "read as three 16-byte words");
+constexpr int32_t kSharedTile = 1 << 16;      // (requests are numbered below 4096)
 
 // A pair of a tile and a KV head takes a stretch of a line: `lead` places for what it costs to begin
 // and end it, then one for each of its units.  A CTA takes `share` places on, whatever pairs that
@@ -56,20 +57,23 @@ struct StepHead {
                         // that came are counted, and another call on the list would join them as its own)
   int32_t num_tokens;   // the plan's; rows past it are of no request whatever positions and slots hold
   int32_t live;         // rows of requests
-  int32_t pad;
+  int32_t requests;     // how many, and kSharedStep where the plan was given prefixes
 };
+constexpr int32_t kSharedStep = 1 << 16;
 static_assert(sizeof(StepHead) == 16, "read as one word");
 
-struct PlanReq {        // per request, from the plan's first kernel to its second
-  int32_t first, len, qrow, pad;   // len 0: left out
+// Per request, from the plan's first kernel to its second and for the calls on the step.  And the same of a
+// prefix's rows: those of requests that follow one another and continue the same tokens of the same session, as
+// one request with as many rows, all of which see all keys (entries of the others have len 0).
+struct PlanReq {
+  int32_t first;        // position of its first new token in its session; a prefix's last token
+  int32_t len, qrow;    // its rows (0: left out), and the first of them
+  int32_t sid;          // and kSharedReq where it continues a prefix
 };
+constexpr int32_t kSharedReq = 1 << 16;
 
-struct PlanArgs {
-  DevPool p;
-  const int32_t* sids;
-  const int32_t* firsts;   // or null
-  const int32_t* lens;
-  int32_t n, num_tokens, max_len;
+// A line of the attention's work and what its division goes by: the requests' own contexts, or the prefixes.
+struct PlanLine {
   int32_t G;               // query heads a KV head
   int32_t line_heads;      // KV heads in a line: all, or 1
   int32_t tile_rows, unit_shift;   // of the attention kernel that will run (its unit's log2)
@@ -79,19 +83,33 @@ struct PlanArgs {
   int32_t shares;          // of a line
   int32_t ctas;            // of the attention
   int32_t window, sinks;
+  int32_t max_tiles;
+  int32_t kind;            // AttnKind
+  int32_t num_tokens;
+  PlanReq* reqs;
+  AttnTile* tiles;
+  CtaWork* work;           // [shares]
+  int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
+  StepHead* head;
+};
+
+struct PlanArgs {
+  DevPool p;
+  const int32_t* sids;
+  const int32_t* firsts;   // or null
+  const int32_t* lens;
+  const int32_t* prefixes;      // or null: sessions whose tokens come before the requests', -1: none
+  const int32_t* prefix_lens;   // or null: all of their tokens
+  int32_t n, num_tokens, max_len;
+  int32_t window, sinks;
   int32_t* row_starts;
   int32_t* kv_lens;
   int32_t* tables;
   int32_t* positions;
   int64_t* slots;
-  PlanReq* reqs;
-  AttnTile* tiles;
-  int32_t max_tiles;
-  CtaWork* work;           // [shares]
-  int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
+  int2* continued;         // [n] each request's prefix and how much of it, for prefixes (else null)
   int32_t* ticket;         // CTAs of the plan that are done, zero between calls
-  int32_t kind;            // AttnKind
-  StepHead* head;
+  PlanLine own, pre;
 };
 
 struct WriteArgs {
@@ -135,7 +153,17 @@ struct AttnArgs {
   long long* ctl;
   long long wait_ns;       // of each wait on a copy or a product
   int32_t hold;            // LV_HOLD_NONE but in a self-test
+  // steps behind prefixes (kPrefix, kJoined)
+  const StepHead* own_head;     // the step's, where head is the prefixes'
+  const StepHead* pre_head;     // and the prefixes', with the kernel that attended over them
+  int32_t pre_kind;
+  float* pre_o;            // [rows][Hq][dp] sums over each row's prefix, and
+  float2* pre_ml;          // [rows][Hq] their maximum (in log2) and weight
 };
+
+// What an attention kernel works on: the requests' contexts (kWhole), the prefixes, whose sums it leaves in
+// pre_o and pre_ml (kPrefix), or the requests' own contexts, joined with those sums (kJoined).
+enum AttnMode : int { kWhole = 0, kPrefix = 1, kJoined = 2 };
 
 constexpr long long kAttnWaitNs = 1000000000ll;   // one second a wait
 
@@ -161,7 +189,7 @@ cudaError_t configure_attend_tc();
 constexpr int kRowsUnitShift = 4, kRowsUnit = 1 << kRowsUnitShift, kRowsRows = 16;
 int attend_rows_ctas(int dp);
 cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16,
-                               int ctas, cudaStream_t s);      // maps: boxes of 64 columns and a unit's keys, or null
+                               int ctas, AttnMode mode, cudaStream_t s);      // maps: boxes of 64 columns and a unit's keys, or null
 constexpr int kTcUnitShift = 7, kTcUnit = 1 << kTcUnitShift, kTcRows = 256;
 // places ahead of a pair's units: what a pair costs besides its units, in units (8 prompts of 4096: 722 us
 // with 2, 794 with 1, 739 with 4; 20 single tokens over 2000 to 4000 keys: 31.2 with 16, 33.8 with 8, 30 to
@@ -175,7 +203,7 @@ struct TcMaps {
   const CUtensorMap* q;    // boxes of 64 columns, G heads and 128 / G rows; null: plain loads
   int box_rows;
 };
-cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cudaStream_t s);
+cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, AttnMode mode, cudaStream_t s);
 
 // A launch that may be scheduled while the previous kernel on `s` still runs; the kernel waits
 // (pdl_wait) before it reads anything that kernel may have written.
@@ -209,9 +237,39 @@ __device__ __forceinline__ int add_release(int32_t* p, int v) {
   asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(was) : "l"(p), "r"(v) : "memory");
   return was;
 }
-// True where the step on the device is one that an attention over num_tokens rows may work on.
-__device__ __forceinline__ bool step_fits(const StepHead& head, int kind, int num_tokens) {
-  return head.kind == kind && head.num_tokens <= num_tokens;
+template <typename T>
+__device__ __forceinline__ T load_words(const T* p) {
+  union {
+    int4 w[sizeof(T) / 16];
+    T t;
+  } x;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 16); ++i) x.w[i] = reinterpret_cast<const int4*>(p)[i];
+  return x.t;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// True where the step on the device is one that an attention over a.num_tokens rows may work on; head: the one
+// of the kernel's own work list, of `kind`.
+template <int kMode>
+__device__ __forceinline__ bool step_fits(const AttnArgs& a, const StepHead& head, int kind) {
+  bool fits = head.kind == kind && head.num_tokens <= a.num_tokens;
+  if constexpr (kMode == kWhole) return fits && head.requests < kSharedStep;
+  if constexpr (kMode == kJoined) {
+    const StepHead pre = load_words(a.pre_head);
+    return fits && head.requests >= kSharedStep && pre.kind == a.pre_kind && pre.num_tokens == head.num_tokens;
+  }
+  const StepHead own = load_words(a.own_head);
+  return fits && own.requests >= kSharedStep && own.kind >= 0 && own.num_tokens == head.num_tokens;
+}
+// Sums (with maximum and weight ml.x, ml.y) that are joined with others of maximum top: the factor of either.
+__device__ __forceinline__ float2 join_factors(float top, float2 ml, float* joint) {
+  const float t = fmaxf(top, ml.x);
+  *joint = t;
+  return make_float2(top == t ? 1.f : exp2_fast(top - t), ml.x == t ? 1.f : exp2_fast(ml.x - t));
 }
 // Arrivals that a barrier of kind `what` waits for: one more than come, in every second CTA, where a
 // self-test holds them.
@@ -225,16 +283,6 @@ __device__ __forceinline__ void give_up(const AttnArgs& a) {
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-template <typename T>
-__device__ __forceinline__ T load_words(const T* p) {
-  union {
-    int4 w[sizeof(T) / 16];
-    T t;
-  } x;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(T) / 16); ++i) x.w[i] = reinterpret_cast<const int4*>(p)[i];
-  return x.t;
-}
 // Places of a pair's stretch.
 __device__ __forceinline__ int stretch_of(int units, int lead, int share) {
   return lead < 0 ? (units + share - 1) / share * share : units + lead;
@@ -253,11 +301,6 @@ __device__ __forceinline__ Pieces pieces_of(const AttnTile& t, int head, int lea
   const int64_t start = t.before + (int64_t)head * stretch_of(t.units, lead, share) + max(lead, 0);
   const int64_t first = start / share;
   return {first, (int)((start + t.units - 1) / share - first) + 1};
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 // Two floats rounded to 16 bits, the first in the low half.
 template <bool kBf16>

@@ -207,6 +207,8 @@ def _load():
         "lv_batch_create": [vp, ctypes.POINTER(lv_batch_desc), ctypes.POINTER(vp)],
         "lv_batch_destroy": [vp, vp],
         "lv_batch_plan": [vp, vp, vp, vp, i32, i32, i32, vp],
+        "lv_batch_share": [vp, i32],
+        "lv_batch_plan_shared": [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp],
         "lv_kv_write": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp],
         "lv_attention": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp,
                          ctypes.c_float, vp],
@@ -248,7 +250,7 @@ EXPORTED = ("lv_pool_create", "lv_pool_destroy", "lv_pool_host_ptr", "lv_pool_im
             "lv_controller_create", "lv_controller_destroy", "lv_controller_tick",
             "lv_controller_speech", "lv_controller_turn_begin", "lv_controller_turn_loaded",
             "lv_controller_records", "lv_controller_counters_get", "lv_batch_create",
-            "lv_batch_destroy", "lv_batch_plan", "lv_kv_write", "lv_attention",
+            "lv_batch_destroy", "lv_batch_plan", "lv_batch_share", "lv_batch_plan_shared", "lv_kv_write", "lv_attention",
             "lv_selftest_attention")
 
 
@@ -491,6 +493,15 @@ def lv_batch_destroy(batch, stream=None):
 def lv_batch_plan(batch, sids, firsts, lens, n, num_tokens, max_len, stream=None):
     _check(_lib.lv_batch_plan(batch, ptr(sids), ptr(firsts), ptr(lens), n, num_tokens, max_len,
                               stream_handle(stream)), "lv_batch_plan")
+
+
+def lv_batch_share(batch, rows):
+    _check(_lib.lv_batch_share(batch, rows), "lv_batch_share")
+
+
+def lv_batch_plan_shared(batch, sids, firsts, lens, prefixes, prefix_lens, n, num_tokens, max_len, stream=None):
+    _check(_lib.lv_batch_plan_shared(batch, ptr(sids), ptr(firsts), ptr(lens), ptr(prefixes), ptr(prefix_lens), n,
+                                     num_tokens, max_len, stream_handle(stream)), "lv_batch_plan_shared")
 
 
 def lv_kv_write(batch, layer, k: lv_heads, v: lv_heads, stream=None):
