@@ -160,7 +160,7 @@ typedef struct lv_pool_desc {
 } lv_pool_desc;
 
 /* Per-session interaction state (72 bytes).  ctx_tokens is maintained by
-   lv_pool_import and lv_session_append and ignored by lv_session_set. */
+   lv_pool_import, lv_session_append and lv_session_truncate and ignored by lv_session_set. */
 typedef struct lv_session_state {
   int32_t ctx_tokens;
   int32_t flags;               /* LV_RUNNING | LV_IMMEDIATE | LV_RESP_OPEN | LV_DONE_VALID */
@@ -753,6 +753,55 @@ lv_status lv_kv_write(lv_batch* batch, int32_t layer, const lv_heads* k, const l
    do nothing and report LV_ERR_STATE with detail -1 until it is planned again. */
 lv_status lv_attention(lv_batch* batch, int32_t layer, const lv_heads* q, const lv_heads* out, float* lse,
                        float scale, lv_stream stream);
+
+/* ------------------------------------- keeping a part of the cache */
+
+/* A long session may keep only the tokens that its queries look at: those whose attention weights add up to
+   most, for each layer and KV head its own.  lv_select_kept chooses them by weights that
+   lv_attention_weights (or the caller) adds up, lv_kv_compact moves their K and V to the front of the
+   session's pages, and lv_session_truncate gives the pages behind them back.  Attention does not depend on the
+   order of keys, and they stay in it; what it needs of their positions is in the K rows as they were written.  The
+   positions of later steps (lv_batch_plan) count the tokens that are left: a caller that rotates K and Q by
+   position adds the number of tokens evicted so far.  Not from the paper, which moves whole sessions. */
+
+/* A weight for every layer, session, KV head and token of the context:
+   float [num_layers][max_sessions][H][tokens], tokens contiguous; the strides count elements. */
+typedef struct lv_weights {
+  float* data;                 /* device memory, aligned to 4 bytes */
+  int64_t layer_stride;
+  int64_t session_stride;
+  int64_t head_stride;
+  int32_t tokens;              /* 0..2^31 - 1: contexts are no longer */
+  int32_t reserved;            /* must be 0 */
+} lv_weights;
+
+/* Chooses keeps[i] tokens of session sids[i] (all, where it has fewer) for each layer and KV head: the first `first`
+   of the context, as many of the last `last` as then fit, and of the others those of the largest weight,
+   the lowest position first where weights are equal (the zeros are; a NaN is above every number, and NaNs
+   are equal).  kept (int32 [n][num_layers][H][most]) receives their positions, ascending, and -1 behind them.
+   n is 0..4096; first, last >= 0; most 1..2^31 - 1.  Device-detected: LV_ERR_BOUNDS, with nothing kept, for a session id
+   or keeps[i] out of range (0..most) or a context longer than weights->tokens; the detail is the request's
+   index. */
+lv_status lv_select_kept(lv_pool* pool, const lv_weights* weights, const int32_t* sids, const int32_t* keeps,
+                         int32_t n, int32_t first, int32_t last, int32_t* kept, int32_t most, lv_stream stream);
+
+/* Moves, in every layer and KV head, the K and V rows of tokens kept[i][layer][head][0..keeps[i]) of session sids[i]
+   to its tokens 0..keeps[i), and (weights not NULL) their weights with them, with zeros behind them up to the
+   context's end.  The lists ascend strictly and end within the context, whose blocks are all in HBM; keeps[i] at
+   or above the context's length moves nothing.  The context stays as long as it is, and rows behind keeps[i] as they
+   are.  Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE) are given up.  lens (int32 [n]) receives
+   what lv_session_truncate takes: min(keeps[i], context), or -1 for a request that was refused, of which
+   nothing moved.  n and most as above.  Device-detected: LV_ERR_BOUNDS for an id, a length or a list out of range,
+   LV_ERR_STATE for a block that is not in HBM, LV_ERR_DOUBLE_MAP for a session that an earlier request names;
+   the detail is the request's index. */
+lv_status lv_kv_compact(lv_pool* pool, const int32_t* sids, const int32_t* keeps, int32_t n, const int32_t* kept,
+                        int32_t most, const lv_weights* weights, int32_t* lens, lv_stream stream);
+
+/* Shortens the contexts of sessions sids[i] to lens[i] tokens (one that is no longer, and lens[i] < 0:
+   nothing).  Blocks behind the end are freed, in whichever tier they are, with their clean copies.  n is 0..4096.
+   Device-detected: LV_ERR_BOUNDS for a session id out of range, LV_ERR_DOUBLE_MAP for a session that an
+   earlier request names (the first one holds); the detail is the request's index. */
+lv_status lv_session_truncate(lv_pool* pool, const int32_t* sids, const int32_t* lens, int32_t n, lv_stream stream);
 
 /* ------------------------------------------------------------- status */
 

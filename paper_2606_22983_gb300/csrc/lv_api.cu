@@ -12,6 +12,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "lv_batch.cuh"
+#include "lv_keep.cuh"
 #include "lv_internal.cuh"
 
 // One NVTX range per entry point, so that a profiler's timeline shows which liblv call
@@ -1947,6 +1948,23 @@ lv_status plan_step(lv_batch* b, const int32_t* sids, const int32_t* firsts, con
 
 size_t elem_size(int32_t type) { return type == LV_F32 ? 4 : 2; }
 
+constexpr int32_t kMostRequests = 4096;      // of a call that takes sessions
+
+// log2(x), -1 where x is no power of two
+int32_t shift_of(int32_t x) {
+  for (int i = 0; i < 31; ++i)
+    if (x == 1 << i) return i;
+  return -1;
+}
+
+// Weights: their memory, and places that do not leave 63 bits.
+bool weights_ok(const lv_pool* pool, const lv_weights* w) {
+  const int64_t lim = 1ll << 38;
+  for (int64_t x : {w->layer_stride, w->session_stride, w->head_stride})
+    if (x < -lim || x > lim) return false;
+  return w->reserved == 0 && w->tokens >= 0 && device_array(pool, w->data, 4);
+}
+
 // A tensor argument: its type, its memory, and rows and heads that do not leave 63 bits.
 bool heads_ok(const lv_pool* pool, const lv_heads* x) {
   if (!x || x->reserved != 0 || x->dtype < LV_BF16 || x->dtype > LV_F32) return false;
@@ -2078,9 +2096,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.P = pool->d.P;
   a.hbm_pages = (uint32_t)pool->d.hbm_pages;
   a.T = pool->d.T;
-  a.t_shift = -1;
-  for (int i = 0; i < 31; ++i)
-    if (a.T == 1 << i) a.t_shift = i;
+  a.t_shift = shift_of(a.T);
   a.H = pool->kv_heads;
   a.D = pool->head_dim;
   a.G = b->G;
@@ -2150,6 +2166,100 @@ lv_status lv_selftest_attention(lv_batch* b, int32_t what, int64_t limit_us) {
   b->hold = what;
   b->wait_ns = what == LV_HOLD_NONE ? lv::kAttnWaitNs : limit_us * 1000;
   return LV_OK;
+}
+
+// ------------------------------------------------- keeping a part of the cache
+lv_status lv_select_kept(lv_pool* pool, const lv_weights* weights, const int32_t* sids, const int32_t* keeps,
+                         int32_t n, int32_t first, int32_t last, int32_t* kept, int32_t most, lv_stream stream) {
+  NvtxRange nvtx_range("lv_select_kept");
+  if (!pool || n < 0 || n > kMostRequests || first < 0 || last < 0 || most < 1 || !weights) return LV_ERR_INVALID;
+  if (n == 0) return LV_OK;
+  if (!sids || !keeps || !kept) return LV_ERR_INVALID;
+  DeviceGuard g(pool->device);
+  if (!weights_ok(pool, weights)) return LV_ERR_INVALID;
+  cudaStream_t s = as_stream(stream);
+  try {
+    Staging st(pool, s);
+    const void *si = nullptr, *ke = nullptr;
+    void* out = nullptr;
+    lv_status r;
+    lv::SelectArgs a{};
+    a.p = pool->d;
+    a.w = *weights;
+    a.H = pool->kv_heads;
+    a.first = first;
+    a.last = last;
+    a.most = most;
+    if ((r = st.in(sids, (size_t)n * 4, &si, true, true)) != LV_OK ||
+        (r = st.in(keeps, (size_t)n * 4, &ke, true, true)) != LV_OK ||
+        (r = st.out(kept, (size_t)n * (a.p.J / 2) * a.H * most * 4, &out, true)) != LV_OK)
+      return r;
+    a.sids = static_cast<const int32_t*>(si);
+    a.keeps = static_cast<const int32_t*>(ke);
+    a.kept = static_cast<int32_t*>(out);
+    LV_TRY(lv::launch_select_kept(a, n, s));
+    return st.finish();
+  } catch (const std::bad_alloc&) {
+    return LV_ERR_OOM;
+  }
+}
+
+lv_status lv_kv_compact(lv_pool* pool, const int32_t* sids, const int32_t* keeps, int32_t n, const int32_t* kept,
+                        int32_t most, const lv_weights* weights, int32_t* lens, lv_stream stream) {
+  NvtxRange nvtx_range("lv_kv_compact");
+  if (!pool || n < 0 || n > kMostRequests || most < 1) return LV_ERR_INVALID;
+  if (n == 0) return LV_OK;
+  if (!sids || !keeps || !kept || !lens) return LV_ERR_INVALID;
+  DeviceGuard g(pool->device);
+  if (weights && !weights_ok(pool, weights)) return LV_ERR_INVALID;
+  cudaStream_t s = as_stream(stream);
+  try {
+    LV_TRY(join_copies(pool, s));   // reads and writes KV bytes
+    Staging st(pool, s);
+    const void *si = nullptr, *ke = nullptr, *ka = nullptr;
+    void* out = nullptr;
+    lv_status r;
+    lv::CompactArgs a{};
+    a.p = pool->d;
+    if (weights) a.w = *weights;
+    a.H = pool->kv_heads;
+    a.most = most;
+    a.t_shift = shift_of(pool->d.T);
+    if ((r = st.in(sids, (size_t)n * 4, &si, true, true)) != LV_OK ||
+        (r = st.in(keeps, (size_t)n * 4, &ke, true, true)) != LV_OK ||
+        (r = st.in(kept, (size_t)n * (a.p.J / 2) * a.H * most * 4, &ka, true, true)) != LV_OK ||
+        (r = st.out(lens, (size_t)n * 4, &out, true)) != LV_OK)
+      return r;
+    a.sids = static_cast<const int32_t*>(si);
+    a.keeps = static_cast<const int32_t*>(ke);
+    a.kept = static_cast<const int32_t*>(ka);
+    a.lens = static_cast<int32_t*>(out);
+    LV_TRY(lv::launch_compact(a, n, pool->head_dim * pool->elem_bytes, pool->num_sms, s));
+    return st.finish();
+  } catch (const std::bad_alloc&) {
+    return LV_ERR_OOM;
+  }
+}
+
+lv_status lv_session_truncate(lv_pool* pool, const int32_t* sids, const int32_t* lens, int32_t n, lv_stream stream) {
+  NvtxRange nvtx_range("lv_session_truncate");
+  if (!pool || n < 0 || n > kMostRequests || (n > 0 && (!sids || !lens))) return LV_ERR_INVALID;
+  if (n == 0) return LV_OK;
+  DeviceGuard g(pool->device);
+  cudaStream_t s = as_stream(stream);
+  try {
+    LV_TRY(join_copies(pool, s));   // a copy under way may still use what is freed
+    Staging st(pool, s);
+    const void *si = nullptr, *le = nullptr;
+    lv_status r;
+    if ((r = st.in(sids, (size_t)n * 4, &si, true, true)) != LV_OK ||
+        (r = st.in(lens, (size_t)n * 4, &le, true, true)) != LV_OK)
+      return r;
+    LV_TRY(lv::launch_truncate(pool->d, static_cast<const int32_t*>(si), static_cast<const int32_t*>(le), n, s));
+    return st.finish();
+  } catch (const std::bad_alloc&) {
+    return LV_ERR_OOM;
+  }
 }
 
 const char* lv_status_str(lv_status s) {

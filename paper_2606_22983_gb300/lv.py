@@ -96,6 +96,11 @@ class lv_heads(ctypes.Structure):
                 ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class lv_weights(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("session_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("tokens", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 LV_BF16, LV_F16, LV_F32 = 1, 2, 3
 LV_HOLD_NONE, LV_HOLD_COPIES, LV_HOLD_PRODUCTS = 0, 1, 2
 
@@ -209,6 +214,9 @@ def _load():
         "lv_batch_plan": [vp, vp, vp, vp, i32, i32, i32, vp],
         "lv_batch_share": [vp, i32],
         "lv_batch_plan_shared": [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp],
+        "lv_select_kept": [vp, ctypes.POINTER(lv_weights), vp, vp, i32, i32, i32, vp, i32, vp],
+        "lv_kv_compact": [vp, vp, vp, i32, vp, i32, ctypes.POINTER(lv_weights), vp, vp],
+        "lv_session_truncate": [vp, vp, vp, i32, vp],
         "lv_kv_write": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp],
         "lv_attention": [vp, i32, ctypes.POINTER(lv_heads), ctypes.POINTER(lv_heads), vp,
                          ctypes.c_float, vp],
@@ -250,7 +258,8 @@ EXPORTED = ("lv_pool_create", "lv_pool_destroy", "lv_pool_host_ptr", "lv_pool_im
             "lv_controller_create", "lv_controller_destroy", "lv_controller_tick",
             "lv_controller_speech", "lv_controller_turn_begin", "lv_controller_turn_loaded",
             "lv_controller_records", "lv_controller_counters_get", "lv_batch_create",
-            "lv_batch_destroy", "lv_batch_plan", "lv_batch_share", "lv_batch_plan_shared", "lv_kv_write", "lv_attention",
+            "lv_batch_destroy", "lv_batch_plan", "lv_batch_share", "lv_batch_plan_shared",
+            "lv_select_kept", "lv_kv_compact", "lv_session_truncate", "lv_kv_write", "lv_attention",
             "lv_selftest_attention")
 
 
@@ -516,6 +525,21 @@ def lv_attention(batch, layer, q: lv_heads, out: lv_heads, lse, scale, stream=No
 
 def lv_selftest_attention(batch, what, limit_us=0):
     _check(_lib.lv_selftest_attention(batch, what, limit_us), "lv_selftest_attention")
+
+
+def lv_select_kept(pool, weights: lv_weights, sids, keeps, n, first, last, kept, most, stream=None):
+    _check(_lib.lv_select_kept(pool, ctypes.byref(weights), ptr(sids), ptr(keeps), n, first, last, ptr(kept), most,
+                               stream_handle(stream)), "lv_select_kept")
+
+
+def lv_kv_compact(pool, sids, keeps, n, kept, most, weights, lens, stream=None):
+    _check(_lib.lv_kv_compact(pool, ptr(sids), ptr(keeps), n, ptr(kept), most,
+                              None if weights is None else ctypes.byref(weights), ptr(lens),
+                              stream_handle(stream)), "lv_kv_compact")
+
+
+def lv_session_truncate(pool, sids, lens, n, stream=None):
+    _check(_lib.lv_session_truncate(pool, ptr(sids), ptr(lens), n, stream_handle(stream)), "lv_session_truncate")
 
 
 def lv_sync(pool, stream=None, raise_on_error=True) -> int:

@@ -49,6 +49,7 @@ class KVPool:
                 # one allocation, viewed as 2L sub-page arrays [hbm_pages][P]
                 kv = torch.zeros((self.J, hbm_pages, self.P), dtype=torch.uint8, device=self.device)
             self.kv = kv
+            self._device = kv[0].get_device()
             ptrs = (ctypes.c_void_p * self.J)(*[self.kv[j].data_ptr() for j in range(self.J)])
             self._ptrs = ptrs
             d = lv.lv_pool_desc()
@@ -181,6 +182,107 @@ class KVPool:
         self.launches += 1
         self.sync()
         return pages[:int(cnt[0])]
+
+    # ----------------------------------------------- keeping a part of the cache
+    def _ints(self, x, n=None):
+        """An int32 array the library can read: a tensor as it is, else a numpy array."""
+        if isinstance(x, torch.Tensor):
+            if x.dtype is not torch.int32 or not x.is_contiguous():
+                raise ValueError("expected a contiguous int32 tensor")
+            if x.is_cuda and x.get_device() != self._device:
+                raise ValueError("expected a tensor on the pool's device")
+        else:
+            x = np.ascontiguousarray(x, dtype=np.int32)
+        if n is not None and len(x) != n:
+            raise ValueError(f"expected {n} entries, got {len(x)}")
+        return x
+
+    def weights_arg(self, w, layers=None):
+        """What the library reads of weights ``w``, [layers, sessions, kv_heads, tokens] of f32 on the
+        pool's device with tokens contiguous."""
+        want = (self.L if layers is None else layers, self.S, self.kv_heads)
+        if w.dim() != 4 or tuple(w.shape[:3]) != want or w.dtype is not torch.float32 or \
+                (w.stride(3) != 1 and w.shape[3] > 1) or w.get_device() != self._device:
+            raise ValueError(f"weights: expected an f32 tensor {[*want, 'tokens']} on {self.device} with contiguous "
+                             f"tokens, got {tuple(w.shape)} of {w.dtype} on {w.device}")
+        a, b, c, _ = w.stride()
+        return lv.lv_weights(data=w.data_ptr(), layer_stride=a, session_stride=b, head_stride=c, tokens=w.shape[3])
+
+    def _on_stream(self):
+        """The handle of the pool's stream, and that stream for PyTorch where it is not the current one."""
+        s = lv.stream_handle(self.stream, self._device)
+        if self.stream is None or s == lv.stream_handle(None, self._device):
+            return s, None
+        return s, (torch.cuda.ExternalStream(s, device=self.device) if s else torch.cuda.default_stream(self.device))
+
+    def _new_ints(self, shape, away, *used):
+        """An int32 tensor that a launch on the pool's stream fills; PyTorch gives neither its memory nor that
+        of the tensors ``used`` to others before the launch has run."""
+        if away is None:
+            return torch.empty(shape, dtype=torch.int32, device=self.device)
+        for x in used:
+            if isinstance(x, torch.Tensor) and x.is_cuda:
+                x.record_stream(away)
+        with torch.cuda.stream(away):
+            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        out.record_stream(torch.cuda.current_stream(self.device))
+        return out
+
+    def select_kept(self, sids, keeps, weights, *, first=0, last=0, most=None):
+        """The tokens of sessions ``sids`` to keep, keeps[i] of each (all of a shorter one) in every layer and
+        KV head: the ``first`` ones of the context, the ``last`` ones, and of the others those of the largest
+        of ``weights`` [layers, sessions, kv_heads, tokens] (f32; ``KVBatch.add_weights`` adds them up).
+        Returns their positions, ascending, int32 [len(sids), layers, kv_heads, most], -1 behind them; most: the
+        largest of keeps (has to be given where they are on the device).  With a stream of the pool's own, the
+        caller orders it with what made the arguments and what reads the result."""
+        sids = self._ints(sids)
+        n = len(sids)
+        keeps = self._ints(keeps, n)
+        if most is None:
+            if isinstance(keeps, torch.Tensor) and keeps.is_cuda:
+                raise ValueError("most is needed with keeps on the device")
+            most = max(int(np.asarray(keeps).max(initial=1)), 1)
+        s, away = self._on_stream()
+        kept = self._new_ints((n, self.L, self.kv_heads, most), away, sids, keeps, weights)
+        lv.lv_select_kept(self.handle, self.weights_arg(weights), sids, keeps, n, first, last, kept, most, s)
+        self.launches += n > 0
+        return kept
+
+    def compact(self, sids, keeps, kept, weights=None):
+        """K and V of the ``kept`` tokens (as ``select_kept`` gives them) to the front of their sessions' pages,
+        and their weights with them.  Returns the lengths that ``truncate`` takes: int32 [len(sids)] on the
+        device, -1 for a request that was refused."""
+        sids = self._ints(sids)
+        n = len(sids)
+        keeps, kept = self._ints(keeps, n), self._ints(kept, n)
+        if kept.ndim != 4 or tuple(kept.shape[1:3]) != (self.L, self.kv_heads):
+            raise ValueError(f"kept: expected {[n, self.L, self.kv_heads, 'most']}, got {list(kept.shape)}")
+        s, away = self._on_stream()
+        lens = self._new_ints((n,), away, sids, keeps, kept, weights)
+        lv.lv_kv_compact(self.handle, sids, keeps, n, kept, kept.shape[3],
+                         None if weights is None else self.weights_arg(weights), lens, s)
+        self.launches += 2 * (n > 0)
+        return lens
+
+    def truncate(self, sids, lens):
+        """Cuts the contexts of sessions ``sids`` to ``lens`` tokens and frees the blocks behind them."""
+        sids = self._ints(sids)
+        lens = self._ints(lens, len(sids))
+        s, away = self._on_stream()
+        if away is not None:
+            for x in (sids, lens):
+                if isinstance(x, torch.Tensor) and x.is_cuda:
+                    x.record_stream(away)
+        lv.lv_session_truncate(self.handle, sids, lens, len(sids), s)
+        self.launches += len(sids) > 0
+
+    def evict_tokens(self, sids, keeps, weights, *, first=0, last=0, most=None):
+        """``select_kept``, ``compact`` and ``truncate``: sessions ``sids`` keep keeps[i] tokens in every layer and
+        KV head.  Returns the kept tokens' old positions."""
+        kept = self.select_kept(sids, keeps, weights, first=first, last=last, most=most)
+        if len(kept):
+            self.truncate(sids, self.compact(sids, keeps, kept, weights))
+        return kept
 
     def counts(self):
         a = np.zeros(self.S, dtype=np.int32)
