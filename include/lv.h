@@ -754,16 +754,6 @@ lv_status lv_kv_write(lv_batch* batch, int32_t layer, const lv_heads* k, const l
 lv_status lv_attention(lv_batch* batch, int32_t layer, const lv_heads* q, const lv_heads* out, float* lse,
                        float scale, lv_stream stream);
 
-/* ------------------------------------- keeping a part of the cache */
-
-/* A long session may keep only the tokens that its queries look at: those whose attention weights add up to
-   most, for each layer and KV head its own.  lv_select_kept chooses them by weights that
-   lv_attention_weights (or the caller) adds up, lv_kv_compact moves their K and V to the front of the
-   session's pages, and lv_session_truncate gives the pages behind them back.  Attention does not depend on the
-   order of keys, and they stay in it; what it needs of their positions is in the K rows as they were written.  The
-   positions of later steps (lv_batch_plan) count the tokens that are left: a caller that rotates K and Q by
-   position adds the number of tokens evicted so far.  Not from the paper, which moves whole sessions. */
-
 /* A weight for every layer, session, KV head and token of the context:
    float [num_layers][max_sessions][H][tokens], tokens contiguous; the strides count elements. */
 typedef struct lv_weights {
@@ -774,6 +764,30 @@ typedef struct lv_weights {
   int32_t tokens;              /* 0..2^31 - 1: contexts are no longer */
   int32_t reserved;            /* must be 0 */
 } lv_weights;
+
+/* Adds up the attention weights that the cached tokens of `layer` get from the planned step's rows, after its
+   lv_attention: w[s][h][j] += sum of exp(scale * q[r][g] . k[j][h] - lse[r][g]) over the rows r of session s that
+   see token j and the query heads g of KV head h; for a row behind a prefix, the prefix's tokens too, in the row of the
+   session that holds them.  q, scale and lse are those of that call (lse is needed); last > 0: only the
+   last `last` rows of each request count (a prompt's end, say), 0: all.  A row whose lse is -inf has no weights.
+   weights: the layer's, with layer_stride not looked at (data is where the layer begins).  Sums are made in 32 bits, in an
+   order that does not change from call to call.  LV_ERR_INVALID as for lv_attention, and for last < 0.  Device-detected, and those weights
+   left as they are: LV_ERR_BOUNDS for a request (or one whose prefix has) more tokens than weights->tokens, LV_ERR_DOUBLE_MAP
+   for one whose session an earlier one of the step has (the first request's tokens are added; prefixes come
+   after all requests, those of one session and length that do not follow one another count as several); LV_ERR_STATE
+   with detail -1 where lv_kv_write reports it, and for a step whose attention ran out of a wait. */
+lv_status lv_attention_weights(lv_batch* batch, int32_t layer, const lv_heads* q, const float* lse,
+                               const lv_weights* weights, int32_t last, float scale, lv_stream stream);
+
+/* ------------------------------------- keeping a part of the cache */
+
+/* A long session may keep only the tokens that its queries look at: those whose attention weights add up to
+   most, for each layer and KV head its own.  lv_select_kept chooses them by weights that
+   lv_attention_weights (or the caller) adds up, lv_kv_compact moves their K and V to the front of the
+   session's pages, and lv_session_truncate gives the pages behind them back.  Attention does not depend on the
+   order of keys, and they stay in it; what it needs of their positions is in the K rows as they were written.  The
+   positions of later steps (lv_batch_plan) count the tokens that are left: a caller that rotates K and Q by
+   position adds the number of tokens evicted so far.  Not from the paper, which moves whole sessions. */
 
 /* Chooses keeps[i] tokens of session sids[i] (all, where it has fewer) for each layer and KV head: the first `first`
    of the context, as many of the last `last` as then fit, and of the others those of the largest weight,

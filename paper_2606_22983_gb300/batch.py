@@ -221,3 +221,21 @@ class KVBatch:
         lv.lv_attention(self.handle, layer, q_arg, out_arg, lse, self._scale if scale is None else scale, s)
         self.pool.launches += 1 + self._shared
         return (out, lse) if return_lse else out
+
+    def add_weights(self, layer: int, q, lse, weights, *, last=0, scale=None, stream=None):
+        """Adds the attention weights that the step's rows give to each cached token of ``layer`` to ``weights``,
+        the layer's [sessions, kv_heads, tokens] of f32: the sums over the rows, and over the query heads of each
+        KV head, of exp(scale q.k - lse), in place.  q, scale and lse are those of ``attention`` with
+        ``return_lse``; last > 0: only the last rows of each request count.  A prefix's tokens have
+        theirs in the row of the session that holds it.  ``KVPool.select_kept`` chooses by such weights."""
+        s, away = self._stream(stream)
+        q_arg = self._put(self._a, q, self.q_heads, "q")
+        if lse.shape[0] < self.num_tokens or lse.dim() != 2 or lse.shape[1] != self.q_heads or \
+                lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.get_device() != self._device:
+            raise ValueError(f"lse: expected a contiguous f32 tensor [{self.num_tokens}, {self.q_heads}] on "
+                             f"{self.pool.device}, got {tuple(lse.shape)} of {lse.dtype} on {lse.device}")
+        w = self.pool.weights_arg(weights[None], 1)
+        if away or s not in self._used_on:
+            self._use(s, q, lse, weights)
+        lv.lv_attention_weights(self.handle, layer, q_arg, lse, w, last, self._scale if scale is None else scale, s)
+        self.pool.launches += 1

@@ -13,6 +13,7 @@
 
 #include "lv_batch.cuh"
 #include "lv_keep.cuh"
+#include "lv_weights.cuh"
 #include "lv_internal.cuh"
 
 // One NVTX range per entry point, so that a profiler's timeline shows which liblv call
@@ -1655,6 +1656,7 @@ struct lv_batch {
   lv::CtaWork* work = nullptr;
   int32_t* arrived = nullptr;
   int32_t* ticket = nullptr;
+  int32_t* unit_tickets = nullptr;      // lv_attention_weights
   lv::StepHead* head = nullptr;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
@@ -1804,7 +1806,9 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   } catch (const std::bad_alloc&) {
     return fail(LV_ERR_OOM);
   }
-  if (lv::configure_attend() != cudaSuccess || lv::configure_attend_tc() != cudaSuccess) return fail(LV_ERR_CUDA);
+  if (lv::configure_attend() != cudaSuccess || lv::configure_attend_tc() != cudaSuccess ||
+      lv::configure_weights() != cudaSuccess)
+    return fail(LV_ERR_CUDA);
   b->max_tiles = d->max_requests + (int32_t)(((long long)d->max_tokens * b->G + 15) / 16);
   const int most = std::max(rows_ctas(b), pool->num_sms);
   // rows of partial results: two slots a CTA
@@ -1815,7 +1819,8 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
-        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->head, 1)) != LV_OK ||
+        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->unit_tickets, 2)) != LV_OK ||
+        (st = batch_alloc(b, &b->head, 1)) != LV_OK ||
         (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
         (st = batch_alloc(b, &b->part_ml, rows)) != LV_OK)
       return fail(st);
@@ -1824,6 +1829,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   }
   // (waits: the batch may be used on any stream next)
   if (cudaMemset(b->ticket, 0, sizeof(int32_t)) != cudaSuccess ||
+      cudaMemset(b->unit_tickets, 0, 2 * sizeof(int32_t)) != cudaSuccess ||
       cudaMemset(b->head, 0xff, sizeof(lv::StepHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
     return fail(LV_ERR_CUDA);
   *out = b;
@@ -2156,6 +2162,54 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   x.tile_rows = tile_rows(b->pre_kind);
   LV_TRY(launch(x, b->pre_kind, b->pre_ctas, lv::kPrefix));
   LV_TRY(launch(a, b->kind, b->ctas, lv::kJoined));
+  return LV_OK;
+}
+
+lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, const float* lse,
+                               const lv_weights* weights, int32_t last, float scale, lv_stream stream) {
+  NvtxRange nvtx_range("lv_attention_weights");
+  if (!b || !b->planned || layer < 0 || 2 * layer >= b->pool->d.J || last < 0 || !weights) return LV_ERR_INVALID;
+  const float scale2 = scale * 1.44269504088896341f;      // for powers of two
+  if (!(scale > 0.f) || !std::isfinite(scale2)) return LV_ERR_INVALID;
+  if (b->num_tokens == 0) return LV_OK;
+  const lv_pool* pool = b->pool;
+  DeviceGuard g(pool->device);
+  if (!heads_ok(pool, q) || q->dtype != b->d.dtype || !device_array(pool, lse, 4) || !weights_ok(pool, weights))
+    return LV_ERR_INVALID;
+  lv::WeightArgs a{};
+  a.k = pool->kv[2 * layer];
+  a.P = pool->d.P;
+  a.hbm_pages = (uint32_t)pool->d.hbm_pages;
+  a.T = pool->d.T;
+  a.t_shift = shift_of(a.T);
+  a.H = pool->kv_heads;
+  a.D = pool->head_dim;
+  a.G = b->G;
+  a.S = pool->d.S;
+  a.maxB = pool->d.maxB;
+  a.tables = b->d.tables;
+  a.pool_table = pool->d.table;
+  a.row_starts = b->d.row_starts;
+  a.reqs = b->reqs;
+  a.pre_reqs = b->pre_reqs;
+  a.head = b->head;
+  a.tickets = b->unit_tickets;
+  a.q = static_cast<const uint8_t*>(q->data);
+  a.q_row = q->row_stride;
+  a.q_head = q->head_stride;
+  a.lse = lse;
+  a.w = weights->data;
+  a.w_session = weights->session_stride;
+  a.w_head = weights->head_stride;
+  a.w_tokens = weights->tokens;
+  a.num_tokens = b->num_tokens;
+  a.last = last;
+  a.window = b->d.window;
+  a.sinks = b->d.sinks;
+  a.scale = scale2;
+  a.ctl = pool->d.ctl;
+  a.wait_ns = b->wait_ns;
+  LV_TRY(lv::launch_weights_plain(a, b->d.dtype == LV_BF16, pool->num_sms, as_stream(stream)));
   return LV_OK;
 }
 

@@ -1,0 +1,178 @@
+// Attention weights added up for the cached tokens: the launches of lv_weights.cu, and how its kernels find
+// their work.
+#pragma once
+
+#include "lv_batch.cuh"
+
+namespace lv {
+
+struct WeightArgs {
+  const uint8_t* k;        // the layer's K sub-page array
+  int64_t P;
+  uint32_t hbm_pages;
+  int32_t T, t_shift, H, D, G, S;
+  int32_t maxB;
+  const int32_t* tables;       // the step's, by request
+  const int32_t* pool_table;   // the pool's, by session
+  const int32_t* row_starts;
+  const PlanReq* reqs;
+  const PlanReq* pre_reqs;     // of the prefixes; null: no room for them
+  const StepHead* head;
+  int32_t* tickets;            // units given out, CTAs done; zero between calls
+  const uint8_t* q;
+  int64_t q_row, q_head;       // in elements
+  const float* lse;            // [num_tokens][Hq]
+  float* w;                    // of the layer
+  int64_t w_session, w_head;
+  int32_t w_tokens;
+  int32_t num_tokens, last;
+  int32_t window, sinks;
+  float scale;                 // scale * log2(e)
+  long long* ctl;
+  long long wait_ns;
+};
+
+cudaError_t launch_weights_plain(const WeightArgs& a, bool bf16, int num_sms, cudaStream_t s);
+cudaError_t configure_weights();
+
+#ifdef __CUDACC__
+// The weights' work: a segment is the context of one request with the request's rows, or a prefix with the rows
+// of all that continue it; a unit is kKeys keys of a segment for one KV head, with all rows that see some of
+// them.  So every word of the weights belongs to one unit, whose sums are made in one order.
+struct Segment {
+  int first, tokens, qrow;     // position of its first row; its rows' tokens; the first of them in the step
+  int keys;
+  int sid, req;                // req: -1 for a prefix
+};
+
+struct Unit {
+  Segment g;
+  int head, key0;
+  int t0, t1;                  // tokens [t0, t1) of the segment see some of its keys
+};
+
+constexpr int kMostSegments = 2 * 4096;
+
+// What a CTA of NT threads knows of the segments.
+template <int NT>
+struct SegmentIndex {
+  int before[NT + 1];                        // units before thread t's segments
+  uint32_t refused[kMostSegments / 32];
+  long long ws[NT / 32];
+};
+
+__device__ __forceinline__ Segment segment_of(const WeightArgs& a, int n, int s) {
+  const bool pre = s >= n;
+  const PlanReq r = load_words(pre ? &a.pre_reqs[s - n] : &a.reqs[s]);
+  Segment g;
+  g.first = r.first;
+  g.tokens = r.len;
+  g.qrow = r.qrow;
+  g.keys = r.len == 0 ? 0 : r.first + (pre ? 1 : r.len);
+  g.sid = r.sid & (kSharedReq - 1);
+  g.req = pre ? -1 : s;
+  return g;
+}
+
+// Which tokens of g see keys of [key0, key0 + keys): those from the first key's position on, and under a
+// window up to where it has left the last one.
+__device__ __forceinline__ Unit unit_of(const WeightArgs& a, const Segment& g, int head, int key0, int keys) {
+  Unit u{g, head, key0, 0, g.tokens};
+  if (g.req < 0) return u;
+  if (a.last > 0) u.t0 = max(0, g.tokens - a.last);
+  u.t0 = max(u.t0, key0 - g.first);
+  if (a.window > 0 && key0 >= a.sinks)
+    u.t1 = (int)min((long long)u.t1, (long long)key0 + keys - 1 + a.window - g.first);
+  return u;
+}
+
+// Whether a token of a segment counts, and whether it sees a key.
+__device__ __forceinline__ bool sees(const WeightArgs& a, const Segment& g, int token, int key) {
+  if (g.req < 0) return key < g.keys;
+  const int p = g.first + token;
+  return key <= p && (a.window == 0 || key > p - a.window || key < a.sinks);
+}
+__device__ __forceinline__ bool counts(const WeightArgs& a, const Segment& g, int n, int token) {
+  if (a.last <= 0) return true;
+  if (g.req >= 0) return token >= g.tokens - a.last;
+  // the request of this row: the last one that does not begin after it and has rows
+  const int r = g.qrow + token;
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.row_starts[mid] <= r) lo = mid;
+    else hi = mid - 1;
+  }
+  return r >= a.row_starts[lo + 1] - a.last;
+}
+
+// Every thread of the CTA calls it: fills x and returns the units in all.  first_of: room for a word a session.
+// The segments whose session an earlier one has, or that the weights have no room for, are refused (their
+// units are empty).
+template <int NT, int kKeys>
+__device__ int index_segments(const WeightArgs& a, const StepHead& step, SegmentIndex<NT>& x, int* first_of) {
+  const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
+  const int tid = threadIdx.x, lane = tid & 31;
+  for (int s = tid; s < a.S; s += NT) first_of[s] = kMostSegments;
+  for (int s = tid; s < (count + 31) / 32; s += NT) x.refused[s] = 0;
+  __syncthreads();
+  for (int s = tid; s < count; s += NT) {
+    const Segment g = segment_of(a, n, s);
+    if (g.keys > 0) atomicMin(&first_of[g.sid], s);
+  }
+  __syncthreads();
+  const int per = (count + NT - 1) / NT;
+  int mine = 0;
+  for (int s = min(tid * per, count); s < min((tid + 1) * per, count); ++s) {
+    const Segment g = segment_of(a, n, s);
+    if (g.keys == 0) continue;
+    const bool again = first_of[g.sid] != s, far = g.keys > a.w_tokens;
+    if (again || far) {
+      atomicOr(&x.refused[s >> 5], 1u << (s & 31));
+      if (blockIdx.x == 0) report(a.ctl, again ? LV_ERR_DOUBLE_MAP : LV_ERR_BOUNDS, s < n ? s : s - n);
+    }
+    mine += a.H * ((g.keys + kKeys - 1) / kKeys);
+  }
+  int sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += y;
+  }
+  if (lane == 31) x.ws[tid >> 5] = sum;
+  __syncthreads();
+  int before = 0;
+  for (int v = 0; v < tid >> 5; ++v) before += (int)x.ws[v];
+  x.before[tid + 1] = before + sum;
+  if (tid == 0) x.before[0] = 0;
+  __syncthreads();
+  return x.before[NT];
+}
+
+// Unit u of all; no tokens where there is nothing to do.
+template <int NT, int kKeys>
+__device__ __forceinline__ Unit find_unit(const WeightArgs& a, const StepHead& step, const SegmentIndex<NT>& x, int u) {
+  const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
+  const int per = (count + NT - 1) / NT;
+  int lo = 0, hi = NT - 1;      // the last thread whose segments do not begin after u
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (x.before[mid] <= u) lo = mid;
+    else hi = mid - 1;
+  }
+  int s = lo * per, off = u - x.before[lo];
+  Segment g = segment_of(a, n, s);
+  for (;;) {
+    const int units = a.H * ((g.keys + kKeys - 1) / kKeys);
+    if (off < units) break;
+    off -= units;
+    g = segment_of(a, n, ++s);
+  }
+  const int tile = off / a.H;
+  Unit out = unit_of(a, g, off - tile * a.H, tile * kKeys, kKeys);
+  if (x.refused[s >> 5] >> (s & 31) & 1u) out.t1 = out.t0;
+  return out;
+}
+#endif
+
+}  // namespace lv

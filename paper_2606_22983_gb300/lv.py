@@ -214,6 +214,8 @@ def _load():
         "lv_batch_plan": [vp, vp, vp, vp, i32, i32, i32, vp],
         "lv_batch_share": [vp, i32],
         "lv_batch_plan_shared": [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp],
+        "lv_attention_weights": [vp, i32, ctypes.POINTER(lv_heads), vp, ctypes.POINTER(lv_weights), i32,
+                                 ctypes.c_float, vp],
         "lv_select_kept": [vp, ctypes.POINTER(lv_weights), vp, vp, i32, i32, i32, vp, i32, vp],
         "lv_kv_compact": [vp, vp, vp, i32, vp, i32, ctypes.POINTER(lv_weights), vp, vp],
         "lv_session_truncate": [vp, vp, vp, i32, vp],
@@ -259,7 +261,7 @@ EXPORTED = ("lv_pool_create", "lv_pool_destroy", "lv_pool_host_ptr", "lv_pool_im
             "lv_controller_speech", "lv_controller_turn_begin", "lv_controller_turn_loaded",
             "lv_controller_records", "lv_controller_counters_get", "lv_batch_create",
             "lv_batch_destroy", "lv_batch_plan", "lv_batch_share", "lv_batch_plan_shared",
-            "lv_select_kept", "lv_kv_compact", "lv_session_truncate", "lv_kv_write", "lv_attention",
+            "lv_attention_weights", "lv_select_kept", "lv_kv_compact", "lv_session_truncate", "lv_kv_write", "lv_attention",
             "lv_selftest_attention")
 
 
@@ -525,6 +527,11 @@ def lv_attention(batch, layer, q: lv_heads, out: lv_heads, lse, scale, stream=No
 
 def lv_selftest_attention(batch, what, limit_us=0):
     _check(_lib.lv_selftest_attention(batch, what, limit_us), "lv_selftest_attention")
+
+
+def lv_attention_weights(batch, layer, q: lv_heads, lse, weights: lv_weights, last, scale, stream=None):
+    _check(_lib.lv_attention_weights(batch, layer, ctypes.byref(q), ptr(lse), ctypes.byref(weights), last, scale,
+                                     stream_handle(stream)), "lv_attention_weights")
 
 
 def lv_select_kept(pool, weights: lv_weights, sids, keeps, n, first, last, kept, most, stream=None):

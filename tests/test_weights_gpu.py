@@ -1,0 +1,374 @@
+"""Attention weights added up for the cached tokens: against the definition in 64 bits, what the call refuses and
+reports, and a run of it with the attention before it and the choice of tokens after it."""
+import numpy as np
+import pytest
+
+from tests._attention import Step
+from tests._shared import SharedStep
+
+pytestmark = pytest.mark.gpu
+
+
+def _weights(s, seed=3, slack=0):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    w = torch.randn((s.pool.S, s.heads, s.pool.max_blocks * s.page + slack), generator=g, device="cuda").exp()
+    return w * 0.01
+
+
+def _want(s, w, lse, layer, scale, last=0, skip=(), q=None):
+    """The weights afterwards in 64 bits, and how far 32 bits may be off: each weight by its score's error (the
+    sum of |q k| times 2^-19, what head_dim products lose in 32 bits, and twice 2^-20 for the exponent's
+    roundings, of which lse's conversion to powers of two takes |lse| 2^-23), and by one rounding for each addition."""
+    import torch
+    q = (s.q if q is None else q).double()
+    out, tol = w.double().clone(), torch.zeros_like(w, dtype=torch.float64)
+    adds = torch.ones_like(out)
+    at = 0
+    prefixed = isinstance(s, SharedStep)
+    for i in range(s.requests if prefixed else s.n):
+        m = s.new[i]
+        before = s.before(i) if prefixed else 0
+        k, hidden = s.rows_of(i, 0, layer), ~s.seen(i)
+        lo = max(0, m - last) if last else 0
+        for h in range(s.heads * s.group if m > lo else 0):
+            kk, x, z = k[:, h // s.group], q[at + lo:at + m, h], lse[at + lo:at + m, h].double()[:, None]
+            y = torch.exp((x @ kk.T) * scale - z)
+            off = (x.abs() @ kk.abs().T) * scale * 2.0 ** -19 + 2.0 ** -19 + z.abs() * 2.0 ** -23
+            live = ~hidden[lo:] & torch.isfinite(z)
+            y, off = torch.where(live, y, 0.0), torch.where(live, y * off, 0.0)
+            n = live.sum(0).double()
+            for what, part in (("own", slice(before, None)), ("prefix", slice(0, before))):
+                if (what == "prefix" and not before) or (what, i) in skip:
+                    continue
+                sid = s.sids[i] if what == "own" else s.psid(i)
+                span = (int(sid), h // s.group, slice(0, y[:, part].shape[1]))
+                out[span] += y[:, part].sum(0)
+                tol[span] += off[:, part].sum(0)
+                adds[span] += n[part]
+        at += m
+    return out, tol + adds * 2.0 ** -24 * out.abs() + 1e-30
+
+
+def _check(got, want, tol, before):
+    import torch
+    assert (got.double() - want).abs().le(tol).all(), ((got.double() - want).abs() / tol).max().item()
+    untouched = want == before.double()
+    assert torch.equal(got[untouched], before[untouched])
+
+
+def _run(s, layer=1, scale=None, last=0, slack=0, **kw):
+    scale = s.dim ** -0.5 if scale is None else scale
+    s.plan(**kw)
+    _, lse = s.batch.attention(layer, s.q, scale=scale, return_lse=True)
+    w = _weights(s, slack=slack)
+    before = w.clone()
+    s.batch.add_weights(layer, s.q, lse, w, last=last, scale=scale)
+    assert s.pool.sync(raise_on_error=False) == 0
+    _check(w, *_want(s, before, lse, layer, scale, last), before)
+    again = before.clone()
+    s.batch.add_weights(layer, s.q, lse, again, last=last, scale=scale)
+    assert (again == w).all()                     # bit for bit
+    return w, lse, before
+
+
+STEPS = {
+    "one": dict(cached=[0], new=[1]),
+    "keys": dict(cached=[127, 128, 255, 256, 63], new=[1, 1, 1, 1, 1]),
+    "tokens": dict(cached=[30, 2000, 0, 777], new=[1, 1, 1, 2]),
+    "mixed": dict(cached=[9, 0, 300, 16, 40], new=[3, 200, 0, 1, 70]),
+    "prompt": dict(cached=[0], new=[700]),
+    "chunk": dict(cached=[1500], new=[130]),
+    "many": dict(cached=[(7 * i) % 400 for i in range(300)], new=[1 + i % 3 for i in range(300)]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("step", STEPS)
+def test_weights(step, dtype):
+    import torch
+    s = Step(**STEPS[step], heads=2, group=4, dim=64, pad=3, dtype=getattr(torch, dtype))
+    try:
+        _run(s)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("heads,group,dim,page", [(1, 1, 128, 16), (4, 8, 128, 16), (2, 7, 96, 32), (1, 16, 64, 64), (3, 5, 80, 8),
+                                                  (1, 200, 64, 16), (2, 3, 256, 16), (2, 4, 64, 5), (1, 2, 8, 1), (2, 48, 72, 24)])
+def test_shapes(heads, group, dim, page):
+    s = Step([33, 250, 0, 64, 515], [1, 40, 7, 0, 2], heads=heads, group=group, dim=dim, page=page)
+    try:
+        _run(s, slack=1)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (100, 4), (129, 130), (1000, 0), (16, 300)])
+@pytest.mark.parametrize("last", [0, 5])
+def test_windows(window, sinks, last):
+    """Under a window only what a row sees has a weight; blocks that none sees may be elsewhere."""
+    absent = {(1, 5)} if window == 100 else ()
+    s = Step([20, 700, 0, 130], [3, 1, 400, 40], heads=2, group=4, dim=64, window=window, sinks=sinks, absent=absent)
+    try:
+        _run(s, last=last)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("last", [1, 16, 64, 1000])
+def test_last_rows(last):
+    s = Step([20, 700, 5], [300, 1, 33], heads=2, group=4, dim=128)
+    try:
+        _run(s, last=last)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("last", [0, 2])
+@pytest.mark.parametrize("shape", [
+    dict(cached=[30, 200, 0, 77], new=[1, 1, 1, 1], of=[0, 0, 0, 0], prefix=[1001]),
+    dict(cached=[9, 0, 300, 16, 40, 2], new=[3, 2, 0, 1, 4, 1], of=[0, 0, 0, -1, 1, 1], prefix=[700, 129], plens=[333, 0]),
+    dict(cached=[0, 100, 17, 5], new=[150, 33, 260, 1], of=[0, 0, -1, 1], prefix=[391, 128])])
+def test_behind_prefixes(shape, last):
+    s = SharedStep(**shape, heads=2, group=4, dim=64, pad=1)
+    try:
+        _run(s, last=last)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("sharp", [10.0, 60.0])
+def test_far_scores(sharp):
+    s = Step([900, 40], [1, 30], heads=2, group=4, dim=64, sharp=sharp)
+    try:
+        _run(s)
+    finally:
+        s.close()
+
+
+def test_rows_without_a_sum_and_odd_values():
+    """A row whose lse is -inf has no weights, one of +inf zeros; a NaN stays with the keys of its row."""
+    import torch
+    s = Step([100, 60, 30], [1, 2, 1], heads=1, group=4, dim=64)
+    try:
+        s.plan()
+        _, lse = s.batch.attention(0, s.q, scale=0.125, return_lse=True)
+        odd = lse.clone()
+        odd[0, 1], odd[1], odd[3, 2] = -float("inf"), float("inf"), float("nan")
+        w = _weights(s)
+        before = w.clone()
+        s.batch.add_weights(0, s.q, odd, w, scale=0.125)
+        assert s.pool.sync(raise_on_error=False) == 0
+        assert torch.isnan(w[s.sids[2], 0, :31]).all() and not torch.isnan(w[s.sids[2], 0, 31:]).any()
+        w[s.sids[2]] = before[s.sids[2]]
+        odd[3] = -float("inf")
+        _check(w, *_want(s, before, odd, 0, 0.125), before)
+        # a NaN key is its own token's alone, and rows that are nobody's have no effect
+        page = s.table[s.sids[0], 2]
+        s.kv[0, page, 3, 0, 5] = float("nan")
+        s.kv[0, page, 4, 0, 5] = float("inf")
+        w = before.clone()
+        s.batch.add_weights(0, s.q, lse, w, scale=0.125)
+        assert s.pool.sync(raise_on_error=False) == 0
+        row = w[s.sids[0], 0]
+        assert torch.isnan(row[35]) and not torch.isfinite(row[36])
+        row[35:37] = before[s.sids[0], 0, 35:37]
+        s.kv[0, page, 3:5, 0, 5] = 0
+        want, tol = _want(s, before, lse, 0, 0.125)
+        want[s.sids[0], 0, 35:37], tol[s.sids[0], 0, 35:37] = before[s.sids[0], 0, 35:37].double(), 1e-30
+        _check(w, want, tol, before)
+    finally:
+        s.close()
+
+
+def test_left_out():
+    """Sessions that come twice, and contexts that the weights have no room for."""
+    from paper_2606_22983_gb300 import lv
+    s = Step([200, 90, 40], [1, 2, 1], heads=2, group=4, dim=64)
+    try:
+        s.plan()
+        _, lse = s.batch.attention(0, s.q, scale=0.125, return_lse=True)
+        w = _weights(s)
+        before = w.clone()
+        s.batch.add_weights(0, s.q, lse, w[..., :100], scale=0.125)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_BOUNDS and s.pool.stats()["error_detail"] == 0
+        s.pool.clear_error()
+        _check(w, *_want(s, before, lse, 0, 0.125, skip={("own", 0)}), before)
+        sids = s.sids.copy()
+        sids[2] = sids[0]
+        s.batch.plan(sids, np.array([1, 2, 1], np.int32))
+        _, lse = s.batch.attention(0, s.q, scale=0.125, return_lse=True)
+        w = before.clone()
+        s.batch.add_weights(0, s.q, lse, w, scale=0.125)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_DOUBLE_MAP and s.pool.stats()["error_detail"] == 2
+        s.pool.clear_error()
+        _check(w, *_want(s, before, lse, 0, 0.125, skip={("own", 2)}), before)
+    finally:
+        s.close()
+
+
+def test_a_prefix_in_two_runs():
+    from paper_2606_22983_gb300 import lv
+    s = SharedStep([64, 3, 150, 8], [1, 2, 5, 1], [0, 0, 1, 0], [260, 515], heads=2, group=4, dim=64)
+    try:
+        s.plan()
+        _, lse = s.batch.attention(0, s.q, scale=0.125, return_lse=True)
+        w = _weights(s)
+        before = w.clone()
+        s.batch.add_weights(0, s.q, lse, w, scale=0.125)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_DOUBLE_MAP and s.pool.stats()["error_detail"] == 3
+        s.pool.clear_error()
+        _check(w, *_want(s, before, lse, 0, 0.125, skip={("prefix", 3)}), before)
+    finally:
+        s.close()
+
+
+def test_refusals():
+    import torch
+    from paper_2606_22983_gb300 import lv
+    s = Step([200, 90], [1, 2], heads=2, group=4, dim=64)
+    try:
+        w, lse = _weights(s), torch.zeros((3, 8), device="cuda")
+        q = s.batch._put(lv.lv_heads(), s.q, 8, "q")
+        arg = s.pool.weights_arg(w[None], 1)
+        h = s.batch.handle
+        with pytest.raises(lv.LvError) as e:                     # not planned
+            lv.lv_attention_weights(h, 0, q, lse, arg, 0, 1.0, 0)
+        assert e.value.status == lv.LV_ERR_INVALID
+        s.plan()
+        wrong = lv.lv_heads(data=q.data, row_stride=q.row_stride, head_stride=q.head_stride, dtype=lv.LV_F16)
+        host = lv.lv_weights(data=np.zeros(4, np.float32).ctypes.data, tokens=1)
+        for a in ((2, q, lse, arg, 0, 1.0), (-1, q, lse, arg, 0, 1.0), (0, q, lse, arg, -1, 1.0), (0, q, None, arg, 0, 1.0),
+                  (0, q, lse, arg, 0, 0.0), (0, q, lse, arg, 0, float("nan")), (0, q, lse, arg, 0, 3e38), (0, wrong, lse, arg, 0, 1.0),
+                  (0, q, lse, host, 0, 1.0), (0, q, lse.cpu(), arg, 0, 1.0), (0, q, lse.data_ptr() + 2, arg, 0, 1.0)):
+            with pytest.raises(lv.LvError) as e:
+                lv.lv_attention_weights(h, *a, 0)
+            assert e.value.status == lv.LV_ERR_INVALID, a
+        for a in ((s.q[:2], lse, w), (s.q, lse[:2], w), (s.q, lse.double(), w), (s.q, lse[:, ::2], w), (s.q, lse, w[:1]),
+                  (s.q, lse, w.half()), (s.q, lse.T.contiguous().T, w), (s.q, lse, w[None])):
+            with pytest.raises(ValueError):
+                s.batch.add_weights(0, *a)
+        assert torch.equal(w, _weights(s)) and s.pool.sync(raise_on_error=False) == 0
+        # a step without rows; one whose attention ran out of a wait
+        s.batch.plan(s.sids[:0], s.sids[:0])
+        s.batch.add_weights(0, s.q[:0], lse[:0], w)
+        s.plan()
+        lv.lv_selftest_attention(h, lv.LV_HOLD_COPIES, 2000)
+        _, lse = s.batch.attention(0, s.q, return_lse=True)
+        lv.lv_selftest_attention(h, lv.LV_HOLD_NONE)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_TIMEOUT
+        s.pool.clear_error()
+        s.batch.add_weights(0, s.q, lse, w)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE and s.pool.stats()["error_detail"] == -1
+        assert torch.equal(w, _weights(s))
+    finally:
+        s.close()
+
+
+def test_strides_and_streams():
+    import torch
+    s = Step([20, 300, 7], [2, 40, 2], heads=2, group=4, dim=64)
+    try:
+        want, lse, before = _run(s)
+        wide = torch.zeros((s.rows, 8, 3 * 64 + 1), dtype=s.dtype, device="cuda")
+        q = wide[..., 65:129]
+        q.copy_(s.q)
+        w = torch.zeros((s.heads, s.pool.S, before.shape[2] + 9), device="cuda").transpose(0, 1)[..., 4:]
+        w[..., :before.shape[2]] = before
+        s.batch.add_weights(1, q, lse, w, scale=0.125)
+        assert s.pool.sync(raise_on_error=False) == 0
+        assert torch.equal(w[..., :before.shape[2]], want) and (w[..., before.shape[2]:] == 0).all()
+        side = torch.cuda.Stream()
+        w = before.clone()
+        torch.cuda.synchronize()
+        s.batch.add_weights(1, s.q, lse, w, scale=0.125, stream=side)
+        side.synchronize()
+        assert torch.equal(w, want)
+    finally:
+        s.close()
+
+
+def test_replayed():
+    """Captured with the attention before it: each replay adds the step's weights that is planned then."""
+    import torch
+    from paper_2606_22983_gb300 import lv
+    s = Step([200, 900, 30], [1, 1, 1], heads=2, group=4, dim=64, max_tokens=9)
+    try:
+        w, side = _weights(s), torch.cuda.Stream()
+        go = lambda: s.batch.attention(0, s.q, scale=0.125, return_lse=True)
+        s.plan()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            _, lse = go()
+            s.batch.add_weights(0, s.q, lse, w, scale=0.125)
+        before = w.clone()
+        for sids, new in (([0, 1, 2], [1, 1, 1]), ([1, 2], [2, 1]), ([2], [1])):
+            s.batch.plan(s.sids[sids], np.array(new, np.int32), num_tokens=3, max_len=1 if max(new) == 1 else 2)
+            graph.replay()
+            assert s.pool.sync(raise_on_error=False) == 0
+            t = type("T", (), dict(requests=0, n=len(sids), new=new, heads=2, group=4, q=s.q, sids=s.sids[sids],
+                                   rows_of=lambda self, i, kv, layer: s.rows_of(sids[i], kv, layer),
+                                   seen=lambda self, i: torch.arange(s.total[sids[i]], device="cuda")[None] <=
+                                   torch.arange(s.total[sids[i]] - new[i], s.total[sids[i]], device="cuda")[:, None]))()
+            _check(w, *_want(t, before, lse, 0, 0.125), before)
+            before = w.clone()
+        big = torch.randn((9, 8, 64), device="cuda").to(s.dtype)
+        s.batch.plan(s.sids, np.array([3, 3, 3], np.int32), np.array([0, 0, 0], np.int32))      # more rows than captured
+        s.batch.attention(0, big)
+        assert s.pool.sync(raise_on_error=False) == 0
+        graph.replay()
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE and torch.equal(w, before)
+    finally:
+        s.close()
+
+
+def test_a_session_cut_by_its_weights():
+    """Steps that add up weights, the eviction of tokens by them, and the steps after it, in which
+    attention sees the kept tokens and no others."""
+    import torch
+    s = Step([190, 333], [10, 7], heads=2, group=4, dim=64)
+    try:
+        w = torch.zeros((2, s.pool.S, 2, s.pool.max_blocks * 16), device="cuda")
+        s.plan()
+        for layer in range(2):
+            _, lse = s.batch.attention(layer, s.q, return_lse=True)
+            s.batch.add_weights(layer, s.q, lse, w[layer], last=4)
+        keeps = np.array([60, 75], np.int32)
+        old = [[s.rows_of(i, kv, layer) for kv in range(2) for layer in range(2)] for i in range(2)]
+        kept = s.pool.evict_tokens(s.sids, keeps, w, first=4, last=12)
+        assert s.pool.sync(raise_on_error=False) == 0
+        for i in range(2):
+            n, c = keeps[i], s.total[i]
+            assert (kept[i, :, :, :4].cpu() == torch.arange(4)).all()
+            assert (kept[i, :, :, n - 12:n].cpu() == torch.arange(c - 12, c)).all()
+            for k, x in enumerate(old[i]):
+                kv, layer = divmod(k, 2)
+                s.total[i] = c
+                new = Step.rows_of(s, i, kv, layer)[:n]
+                for h in range(2):
+                    assert torch.equal(new[:, h], x[kept[i, layer, h, :n].long(), h])
+            assert (w[:, s.sids[i], :, n:] == 0).all() and (w[:, s.sids[i], :, :4] > 0).all()
+        # two more tokens of each
+        s.table = None
+        for i in range(2):
+            s.pool.append(int(s.sids[i]), 2)
+        s.table = s.pool.tables()[0].copy()
+        s.cached, s.new = [int(x) for x in keeps], [2, 2]
+        s.total, s.rows = [a + 2 for a in s.cached], 4
+        s.batch.plan(s.sids, np.array(s.new, np.int32))
+        x = torch.randn((4, 4, 64), generator=s.gen, device="cuda").to(s.dtype)
+        for layer in range(2):
+            s.batch.write(layer, x[:, :2], x[:, 2:])
+        q = s.q[:4]
+        s.q = q
+        for layer in range(2):
+            before = w[layer].clone()
+            out, lse = s.batch.attention(layer, q, scale=0.125, return_lse=True)
+            s.check(out, lse, layer, 0.125)
+            s.batch.add_weights(layer, q, lse, w[layer], scale=0.125)
+            assert s.pool.sync(raise_on_error=False) == 0
+            _check(w[layer], *_want(s, before, lse, layer, 0.125), before)
+    finally:
+        s.close()
