@@ -18,9 +18,9 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblv.so")
 
 SOURCES = ["lv_api.cu", "lv_kernels.cu", "lv_noalloc.cu", "lv_sched.cu", "lv_controller.cu", "lv_batch.cu", "lv_attend.cu",
-           "lv_attend_tc.cu", "lv_keep.cu", "lv_weights.cu"]
+           "lv_attend_tc.cu", "lv_keep.cu", "lv_weights.cu", "lv_weights_tc.cu"]
 HEADERS = [os.path.join(CSRC, "lv_internal.cuh"), os.path.join(CSRC, "lv_batch.cuh"),
-           os.path.join(CSRC, "lv_keep.cuh"), os.path.join(CSRC, "lv_weights.cuh"), os.path.join(INCLUDE, "lv.h")]
+           os.path.join(CSRC, "lv_keep.cuh"), os.path.join(CSRC, "lv_tc.cuh"), os.path.join(CSRC, "lv_weights.cuh"), os.path.join(INCLUDE, "lv.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2", "--expt-relaxed-constexpr"]
 

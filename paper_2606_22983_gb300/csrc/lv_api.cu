@@ -1751,15 +1751,15 @@ lv_status make_maps(lv_batch* b) {
   return LV_OK;
 }
 
-// A map of the queries [rows][H][G][D], a box 64 columns of the G heads of 128 / G rows; false
+// A map of the queries [rows][H][G][D], a box 64 columns of the G heads of 128 / G rows (or `rows`); false
 // where their strides or G do not allow one.
-bool query_map(const lv_batch* b, const lv_heads* q, CUtensorMap* m) {
+bool query_map(const lv_batch* b, const lv_heads* q, CUtensorMap* m, int32_t rows = 0) {
   const int64_t lim = 1ll << 39;      // (a map's strides are below 2^40 bytes)
   const int64_t head = q->head_stride * 2, row = q->row_stride * 2;
   if (b->G > 128 || head <= 0 || row <= 0 || head * b->G >= lim || row >= lim) return false;
   const cuuint64_t D = b->pool->head_dim, H = b->pool->kv_heads, G = b->G;
   return encode_map(b, m, q->data, {D, G, H, (cuuint64_t)b->num_tokens},
-                    {(cuuint64_t)head, G * (cuuint64_t)head, (cuuint64_t)row}, {64, (cuuint32_t)G, 1, (cuuint32_t)(128 / G)});
+                    {(cuuint64_t)head, G * (cuuint64_t)head, (cuuint64_t)row}, {64, (cuuint32_t)G, 1, (cuuint32_t)(rows ? rows : 128 / G)});
 }
 
 bool device_array(const lv_pool* pool, const void* p, size_t align) {
@@ -1807,7 +1807,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
     return fail(LV_ERR_OOM);
   }
   if (lv::configure_attend() != cudaSuccess || lv::configure_attend_tc() != cudaSuccess ||
-      lv::configure_weights() != cudaSuccess)
+      lv::configure_weights() != cudaSuccess || lv::configure_weights_tc() != cudaSuccess)
     return fail(LV_ERR_CUDA);
   b->max_tiles = d->max_requests + (int32_t)(((long long)d->max_tokens * b->G + 15) / 16);
   const int most = std::max(rows_ctas(b), pool->num_sms);
@@ -2209,7 +2209,21 @@ lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, co
   a.scale = scale2;
   a.ctl = pool->d.ctl;
   a.wait_ns = b->wait_ns;
-  LV_TRY(lv::launch_weights_plain(a, b->d.dtype == LV_BF16, pool->num_sms, as_stream(stream)));
+  a.hold = b->hold;
+  a.head_out = b->head;
+  cudaStream_t s = as_stream(stream);
+  const bool bf16 = b->d.dtype == LV_BF16;
+  if (!b->box_rows) {
+    LV_TRY(lv::launch_weights_plain(a, bf16, pool->num_sms, s));
+    return LV_OK;
+  }
+  CUtensorMap qmap, few;
+  lv::WeightMaps m{&b->maps[2 * layer], nullptr, nullptr, b->box_rows, b->G >= 16 ? 1 : 16 / b->G};
+  if (heads_aligned(q, 16) && query_map(b, q, &qmap) && query_map(b, q, &few, m.few_rows)) {
+    m.q = &qmap;
+    m.q_few = &few;
+  }
+  LV_TRY(lv::launch_weights_tc(a, m, bf16, b->dp, pool->num_sms, s));
   return LV_OK;
 }
 

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_weights_plain(const __grid_co
       }
       ks[r * ld + d] = v;
     }
-    float sum = 0.f;
+    LongSum all;
     for (int R0 = u.t0 * a.G; R0 < u.t1 * a.G; R0 += kPlainRows) {
       __syncthreads();
       for (int e = tid; e < kPlainRows * a.D; e += kPlainThreads) {
@@ -86,12 +86,15 @@ __global__ void __launch_bounds__(kPlainThreads) k_weights_plain(const __grid_co
 #pragma unroll
         for (int r = 0; r < kPlainRows / 2; ++r) s[r] += v * qq[r * a.D + d];
       }
+      float sum = 0.f;
 #pragma unroll
       for (int r = 0; r < kPlainRows / 2; ++r) {
         const int at = half * (kPlainRows / 2) + r, token = s_token[at];
         if (token >= 0 && sees(a, u.g, token, u.key0 + key)) sum += exp2_fast(s[r] * a.scale + s_b[at]);
       }
+      all.add(sum);
     }
+    float sum = all.sum;
     if (half == 1) s_sum[key] = sum;
     __syncthreads();
     if (half == 0 && u.key0 + key < u.g.keys) {

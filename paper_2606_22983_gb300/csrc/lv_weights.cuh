@@ -30,8 +30,33 @@ struct WeightArgs {
   float scale;                 // scale * log2(e)
   long long* ctl;
   long long wait_ns;
+  int32_t hold;                // LV_HOLD_NONE but in a self-test
+  StepHead* head_out;          // the same head, for a wait that ran out
 };
 
+// Sums of many terms in 32 bits: what the additions lose is kept beside them (Kahan), so that the sum's error
+// does not grow with a prompt's length (32 768 rows of a key added one after the other were off by 1.6e-6).
+struct LongSum {
+  float sum = 0.f, lost = 0.f;
+#ifdef __CUDACC__
+  __device__ __forceinline__ void add(float x) {
+    const float y = x - lost, t = sum + y;
+    lost = (t - sum) - y;
+    sum = t;
+  }
+#endif
+};
+
+// The tensor-core kernel's maps: K in boxes of 64 columns and box_rows keys; the queries in boxes of 64 columns,
+// G heads and 128 / G rows, or few_rows of them (null: plain loads).
+struct WeightMaps {
+  const CUtensorMap* k;
+  const CUtensorMap* q;
+  const CUtensorMap* q_few;
+  int box_rows, few_rows;
+};
+cudaError_t launch_weights_tc(const WeightArgs& a, const WeightMaps& m, bool bf16, int dp, int num_sms, cudaStream_t s);
+cudaError_t configure_weights_tc();
 cudaError_t launch_weights_plain(const WeightArgs& a, bool bf16, int num_sms, cudaStream_t s);
 cudaError_t configure_weights();
 
@@ -53,12 +78,12 @@ struct Unit {
 
 constexpr int kMostSegments = 2 * 4096;
 
-// What a CTA of NT threads knows of the segments.
+// What a CTA knows of the segments, divided among NT of its threads.
 template <int NT>
 struct SegmentIndex {
   int before[NT + 1];                        // units before thread t's segments
   uint32_t refused[kMostSegments / 32];
-  long long ws[NT / 32];
+  int ws[NT / 32];
 };
 
 __device__ __forceinline__ Segment segment_of(const WeightArgs& a, int n, int s) {
@@ -113,17 +138,17 @@ template <int NT, int kKeys>
 __device__ int index_segments(const WeightArgs& a, const StepHead& step, SegmentIndex<NT>& x, int* first_of) {
   const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
   const int tid = threadIdx.x, lane = tid & 31;
-  for (int s = tid; s < a.S; s += NT) first_of[s] = kMostSegments;
-  for (int s = tid; s < (count + 31) / 32; s += NT) x.refused[s] = 0;
+  for (int s = tid; s < a.S; s += blockDim.x) first_of[s] = kMostSegments;
+  for (int s = tid; s < (count + 31) / 32; s += blockDim.x) x.refused[s] = 0;
   __syncthreads();
-  for (int s = tid; s < count; s += NT) {
+  for (int s = tid; s < count; s += blockDim.x) {
     const Segment g = segment_of(a, n, s);
     if (g.keys > 0) atomicMin(&first_of[g.sid], s);
   }
   __syncthreads();
   const int per = (count + NT - 1) / NT;
   int mine = 0;
-  for (int s = min(tid * per, count); s < min((tid + 1) * per, count); ++s) {
+  for (int s = min(tid * per, count); s < min((tid + 1) * per, count) && tid < NT; ++s) {
     const Segment g = segment_of(a, n, s);
     if (g.keys == 0) continue;
     const bool again = first_of[g.sid] != s, far = g.keys > a.w_tokens;
@@ -139,11 +164,13 @@ __device__ int index_segments(const WeightArgs& a, const StepHead& step, Segment
     const int y = __shfl_up_sync(0xffffffffu, sum, o);
     if (lane >= o) sum += y;
   }
-  if (lane == 31) x.ws[tid >> 5] = sum;
+  if (lane == 31 && tid < NT) x.ws[tid >> 5] = sum;
   __syncthreads();
-  int before = 0;
-  for (int v = 0; v < tid >> 5; ++v) before += (int)x.ws[v];
-  x.before[tid + 1] = before + sum;
+  if (tid < NT) {
+    int before = 0;
+    for (int v = 0; v < tid >> 5; ++v) before += x.ws[v];
+    x.before[tid + 1] = before + sum;
+  }
   if (tid == 0) x.before[0] = 0;
   __syncthreads();
   return x.before[NT];

@@ -372,3 +372,28 @@ def test_a_session_cut_by_its_weights():
             _check(w[layer], *_want(s, before, lse, layer, 0.125), before)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("what", ["LV_HOLD_COPIES", "LV_HOLD_PRODUCTS"])
+@pytest.mark.parametrize("new", [[1, 1], [300, 1]])
+def test_waits_that_run_out(new, what):
+    """A wait inside the kernel ends with a report; the step is refused until it is planned again."""
+    from paper_2606_22983_gb300 import lv
+    s = Step([2000, 700], new, heads=2, group=4, dim=64)
+    try:
+        s.plan()
+        _, lse = s.batch.attention(0, s.q, return_lse=True)
+        w = _weights(s)
+        before = w.clone()
+        lv.lv_selftest_attention(s.batch.handle, getattr(lv, what), 2000)
+        s.batch.add_weights(0, s.q, lse, w)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_TIMEOUT
+        s.pool.clear_error()
+        lv.lv_selftest_attention(s.batch.handle, lv.LV_HOLD_NONE)
+        w.copy_(before)
+        s.batch.add_weights(0, s.q, lse, w)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE and (w == before).all()
+        s.pool.clear_error()
+        _run(s)
+    finally:
+        s.close()
