@@ -780,7 +780,8 @@ lv_status create_impl(const lv_pool_desc* desc, cudaStream_t s, lv_pool** out) {
     }
   }
   if (lv::configure_exchange_tma(d) != cudaSuccess) return fail(LV_ERR_CUDA);
-  if (lv::configure_step_kernels() != cudaSuccess || lv::configure_schedule() != cudaSuccess) return fail(LV_ERR_CUDA);
+  if (lv::configure_step_kernels() != cudaSuccess || lv::configure_schedule() != cudaSuccess ||
+      lv::configure_keep() != cudaSuccess) return fail(LV_ERR_CUDA);
   if (const char* env = std::getenv("LV_STAGE_STAGES")) {   // TMA pack/unpack stages per CTA
     const int st = std::atoi(env);
     if (st >= 2 && st <= 16) d.stages = st;

@@ -17,29 +17,339 @@ __device__ __forceinline__ uint32_t blocks_of(int32_t tokens, int32_t T) {
 // ---------------------------------------------------------------- choice
 // A weight's place in the order of the numbers: larger for larger ones, equal for the two zeros, and the
 // largest for every NaN.
-__device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t u = __float_as_uint(x);
-  if (x != x) return 0xffffffffu;
-  if (x == 0.f) return 0x80000000u;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+__device__ __forceinline__ uint32_t order_key(uint32_t bits) {
+  if ((bits << 1) > 0xff000000u) return 0xffffffffu;      // a NaN
+  if ((bits << 1) == 0) return 0x80000000u;
+  return bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
 }
 
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
-constexpr int kBins = 2048;      // 11 bits of the key at a time: 11, 11 and 10
+constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
+constexpr int kBins = 2048;            // 11 bits of the key, or 12 in halves of words
+constexpr int kSample = 2048;
+constexpr int kMostWords = 2048;       // of 32 tokens, in a list that is read once
 
-// One list: request blockIdx.y's tokens in (layer, head) blockIdx.x.  Tokens before lo and from hi on
-// stay; of those between, the `need` of largest key.  The key of the last of them is found by its digits
-// from above, a histogram of the candidates each; then the tokens are gone through in order, those above it
-// kept and of those equal to it the first.
-__global__ void __launch_bounds__(kSelThreads) k_select_kept(const __grid_constant__ SelectArgs a) {
-  __shared__ int bins[kBins];
-  __shared__ int sums[2][kSelWarps];
-  __shared__ uint32_t s_digit;
-  __shared__ int s_above;
+// Keys near the border between kept and not that are gathered: an eighth of the longest list, which the bounds
+// by the sample hold where its weights spread over some octaves.
+__host__ __device__ constexpr int few_of(int words) { return words * 4 > 2048 ? words * 4 : 2048; }
+
+struct SelectShared {
+  int bins[kBins];
+  int sums[2][kSelWarps];
+  int few, above, low;         // tokens near the border, above it, and of its lowest key
+  int digit, before, inside;
+  uint32_t lo_key, hi_key;
+  uint32_t last_key[32];
+  int last_at[32];
+  int last;
+};
+
+// What select_once keeps beside it, for lists of `words` words of 32 tokens.
+struct OnceShared {
+  uint32_t* above;
+  uint32_t* low;
+  int* place;
+  uint32_t* key;       // of those near the border, [few_of(words)]
+  int* at;
+  static size_t bytes(int words) { return (size_t)words * 12 + (size_t)few_of(words) * 8; }
+  __device__ OnceShared(uint32_t* p, int words)
+      : above(p), low(p + words), place(reinterpret_cast<int*>(p + 2 * words)), key(p + 3 * words),
+        at(reinterpret_cast<int*>(p + 3 * words + few_of(words))) {}
+};
+
+// A list's tokens lo..hi, of which `need` of the largest keys are to be found.
+struct List {
+  const float* w;      // of token lo
+  int n, need;
+  int32_t* out;
+  int lo;
+};
+
+// Inclusive sums over the CTA; *all receives the total.  A barrier lies between its uses.
+__device__ __forceinline__ int scan_up(int v, int* sums, int* all) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) sums[wid] = x;
+  __syncthreads();
+  int total = 0, before = 0;
+#pragma unroll
+  for (int k = 0; k < kSelWarps; ++k) {
+    if (k == wid) before = total;
+    total += sums[k];
+  }
+  *all = total;
+  return before + x;
+}
+
+// Any list: the key of the last kept token by its digits from above, a histogram of the candidates each; then
+// the tokens in order, those above it kept and of those equal to it the first.  The list is read four times.
+__device__ __noinline__ void select_by_digits(const List& t, SelectShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  uint32_t have = 0;
+  int need = t.need, shift = 32;
+  while (shift > 0) {
+    const int bits = shift > 11 ? 11 : shift;      // 11, 11, 10
+    shift -= bits;
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kSelThreads) sh.bins[b] = 0;
+    __syncthreads();
+    for (int j = tid; j < t.n; j += kSelThreads) {
+      const uint32_t k = order_key(__float_as_uint(t.w[j]));
+      if (shift + bits == 32 || (k >> (shift + bits)) == (have >> (shift + bits)))
+        atomicAdd(&sh.bins[k >> shift & ((1u << bits) - 1u)], 1);
+    }
+    __syncthreads();
+    // from the top bin down: the bin in which `need` is reached
+    constexpr int kPer = kBins / kSelThreads;
+    int mine[kPer], sum = 0, all;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) sum += mine[e] = sh.bins[kBins - 1 - (tid * kPer + e)];
+    int above = scan_up(sum, sh.sums[0], &all) - sum;
+    if (above < need && above + sum >= need) {
+      int e = 0;
+      while (above + mine[e] < need) above += mine[e++];
+      sh.digit = kBins - 1 - (tid * kPer + e);
+      sh.before = above;
+    }
+    __syncthreads();
+    have |= (uint32_t)sh.digit << shift;
+    need -= sh.before;
+  }
+  int kept = 0, ties = 0;
+  for (int j0 = 0; j0 < t.n; j0 += kSelThreads) {
+    const int j = j0 + tid;
+    const uint32_t k = j < t.n ? order_key(__float_as_uint(t.w[j])) : 0;
+    const bool tie = k == have;
+    int all;
+    __syncthreads();
+    const int rank = ties + scan_up(tie, sh.sums[0], &all);
+    ties += all;
+    const bool stay = k > have || (tie && rank <= need);
+    const int at = kept + scan_up(stay, sh.sums[1], &all);
+    kept += all;
+    if (stay) t.out[at - 1] = t.lo + j;
+  }
+}
+
+// The bounds between which the border lies by a sample of the list, as bins of the key's first 12 bits (an
+// eighth of an octave): at 3.5 deviations of the sample's rank, so that it lies outside in some 1 of 2000 lists.
+__device__ __forceinline__ void bounds_by_sample(const List& t, SelectShared& sh) {
+  const int tid = threadIdx.x;
+  float x[kSample / kSelThreads];
+#pragma unroll
+  for (int e = 0; e < kSample / kSelThreads; ++e)
+    x[e] = t.w[(uint32_t)(((unsigned long long)(e * kSelThreads + tid) * (uint32_t)t.n) / kSample)];
+  for (int b = tid; b < kBins / 4; b += kSelThreads) reinterpret_cast<int4*>(sh.bins)[b] = make_int4(0, 0, 0, 0);
+  if (tid == 0) {
+    sh.lo_key = 0;
+    sh.hi_key = 0xffffffffu;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kSample / kSelThreads; ++e) {
+    const uint32_t k = order_key(__float_as_uint(x[e]));
+    atomicAdd(&sh.bins[k >> 21], k >> 20 & 1u ? 1 << 16 : 1);
+  }
+  __syncthreads();
+  const float p = (float)t.need / (float)t.n, margin = 3.5f * sqrtf(p * (1.f - p) * kSample) + 1.f;
+  const int r_hi = (int)(p * kSample - margin), r_lo = (int)(p * kSample + margin) + 1;
+  constexpr int kPer = kBins / kSelThreads;
+  uint32_t mine[kPer];
+  int sum = 0, all;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    mine[e] = sh.bins[kBins - 1 - (tid * kPer + e)];
+    sum += (mine[e] & 0xffffu) + (mine[e] >> 16);
+  }
+  int above = scan_up(sum, sh.sums[0], &all) - sum;
+  if (above < r_lo && above + sum >= min(max(r_hi, 1), r_lo)) {
+#pragma unroll
+    for (int e = 0; e < 2 * kPer; ++e) {
+      const uint32_t bin = (uint32_t)(2 * (kBins - 1 - (tid * kPer + e / 2)) + (e & 1 ? 0 : 1)) << 20;
+      const int upto = above + (e & 1 ? mine[e / 2] & 0xffffu : mine[e / 2] >> 16);
+      if (above < r_hi && upto >= r_hi) sh.hi_key = bin | 0xfffffu;
+      if (above < r_lo && upto >= r_lo) sh.lo_key = bin;
+      above = upto;
+    }
+  }
+  __syncthreads();
+}
+
+// A list of up to 32 * kMostWords tokens, read once: a word a 32 tokens says which are above the bounds, which
+// have the lowest key in them (zeros do, where the border is among them), and those between are gathered.  The
+// border is then found among these: by their place between the bounds in 256 steps, finer until at most 32
+// share one, which a warp ranks.  False where it is not found so: the bounds do not hold it, too many keys
+// lie in them, or too many are equal at the border.
+__device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, const OnceShared& o, int room) {
+  uint32_t *const above = o.above, *const low = o.low;
+  int* const place = o.place;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int words = (t.n + 31) >> 5;
+  if (tid == 0) sh.few = sh.above = sh.low = sh.last = 0;
+  uint32_t lo_key = 0, hi_key = 0xffffffffu;
+  if (t.n > room) {
+    bounds_by_sample(t, sh);
+    lo_key = sh.lo_key;
+    hi_key = sh.hi_key;
+  } else {
+    __syncthreads();
+  }
+  const uint32_t below = (1u << lane) - 1u;
+  constexpr int kUnroll = 8;
+  int n_above = 0, n_low = 0;
+  for (int w0 = wid * kUnroll; w0 < words; w0 += kSelWarps * kUnroll) {
+    uint32_t key[kUnroll], in[kUnroll];
+    const float* from = t.w + 32 * w0 + lane;
+    const int end = t.n - 32 * w0 - lane;
+#pragma unroll
+    for (int e = 0; e < kUnroll; ++e) key[e] = 32 * e < end ? __float_as_uint(__ldcs(from + 32 * e)) : 0u;
+    uint32_t up = 0, down = 0;
+    int total = 0;
+#pragma unroll
+    for (int e = 0; e < kUnroll; ++e) {
+      key[e] = 32 * e < end ? order_key(key[e]) : 0u;      // (0 is below every key)
+      const uint32_t a = __ballot_sync(0xffffffffu, key[e] > hi_key);
+      const uint32_t b = __ballot_sync(0xffffffffu, key[e] == lo_key && 32 * e < end);
+      in[e] = __ballot_sync(0xffffffffu, key[e] > lo_key && key[e] <= hi_key);
+      if (lane == e) up = a, down = b;
+      n_above += __popc(a);
+      n_low += __popc(b);
+      total += __popc(in[e]);
+    }
+    if (lane < kUnroll && w0 + lane < words) {
+      above[w0 + lane] = up;
+      low[w0 + lane] = down;
+    }
+    if (total == 0) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sh.few, total);
+    at = __shfl_sync(0xffffffffu, at, 0);
+#pragma unroll
+    for (int e = 0; e < kUnroll; ++e) {
+      const int to = at + __popc(in[e] & below);
+      if ((in[e] >> lane & 1u) && to < room) {
+        o.key[to] = key[e];
+        o.at[to] = 32 * (w0 + e) + lane;
+      }
+      at += __popc(in[e]);
+    }
+  }
+  if (lane == 0) {
+    atomicAdd(&sh.above, n_above);
+    atomicAdd(&sh.low, n_low);
+  }
+  __syncthreads();
+  const int few = sh.few;
+  int r = t.need - sh.above;      // of those in the bounds
+  if (few > room || r < 0 || r > few + sh.low) return false;
+  if (r >= few) {
+    // all between, and of the lowest ones the first
+    for (int j = tid; j < few; j += kSelThreads) atomicOr(&above[o.at[j] >> 5], 1u << (o.at[j] & 31));
+    r -= few;
+    const int per = (words + kSelThreads - 1) / kSelThreads;
+    if (r > 0) {
+      const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
+      int mine = 0, all;
+      for (int w = w0; w < w1; ++w) mine += __popc(low[w]);
+      int left = r - (scan_up(mine, sh.sums[0], &all) - mine);
+      for (int w = w0; w < w1 && left > 0; ++w) {
+        uint32_t x = low[w];
+        const int have = __popc(x);
+        if (have > left) {
+          uint32_t rest = x;
+          for (int k = 0; k < left; ++k) rest &= rest - 1;
+          x ^= rest;
+        }
+        atomicOr(&above[w], x);
+        left -= have;
+      }
+    }
+  } else if (r > 0) {
+    const uint32_t width = hi_key - lo_key - 1;      // of key - lo_key - 1 at most
+    int shift = max(0, 24 - __clz(width | 1u)), up = 32;
+    uint32_t at = 0;      // (key - lo_key - 1) >> up of the border
+    for (;;) {
+      sh.bins[tid] = 0;
+      __syncthreads();
+      const uint32_t digits = up - shift >= 32 ? ~0u : (1u << (up - shift)) - 1u;
+      for (int j = tid; j < few; j += kSelThreads) {
+        const uint32_t d = o.key[j] - lo_key - 1;
+        if (up == 32 || d >> up == at) atomicAdd(&sh.bins[d >> shift & digits], 1);
+      }
+      __syncthreads();
+      const int mine = sh.bins[kSelThreads - 1 - tid];
+      int all;
+      const int upto = scan_up(mine, sh.sums[0], &all);
+      if (upto - mine < r && upto >= r) {
+        sh.digit = kSelThreads - 1 - tid;
+        sh.before = upto - mine;
+        sh.inside = mine;
+      }
+      __syncthreads();
+      at = (up == 32 ? 0u : at << (up - shift)) + (uint32_t)sh.digit;
+      r -= sh.before;
+      up = shift;
+      if (sh.inside <= 32) break;
+      if (shift == 0) return false;
+      shift = max(0, shift - 8);
+    }
+    for (int j = tid; j < few; j += kSelThreads) {
+      const uint32_t d = (o.key[j] - lo_key - 1) >> up;
+      const int where = o.at[j];
+      if (d > at) {
+        atomicOr(&above[where >> 5], 1u << (where & 31));
+      } else if (d == at) {
+        const int k = atomicAdd(&sh.last, 1);
+        sh.last_key[k] = o.key[j];
+        sh.last_at[k] = where;
+      }
+    }
+    __syncthreads();
+    if (wid == 0) {
+      const int count = sh.last;
+      const uint32_t k = lane < count ? sh.last_key[lane] : 0u;
+      const int where = lane < count ? sh.last_at[lane] : 0;
+      int rank = 0;
+      for (int j = 0; j < count; ++j) {
+        const uint32_t kj = __shfl_sync(0xffffffffu, k, j);
+        const int wj = __shfl_sync(0xffffffffu, where, j);
+        rank += kj > k || (kj == k && wj < where);
+      }
+      if (lane < count && rank < r) atomicOr(&above[where >> 5], 1u << (where & 31));
+    }
+  }
+  __syncthreads();
+  // the kept ones' places: what the words before keep
+  const int per = (words + kSelThreads - 1) / kSelThreads;
+  const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
+  int mine = 0, all;
+  for (int w = w0; w < w1; ++w) mine += __popc(above[w]);
+  int before = scan_up(mine, sh.sums[1], &all) - mine;
+  for (int w = w0; w < w1; ++w) {
+    place[w] = before;
+    before += __popc(above[w]);
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int w = wid; w < words; w += kSelWarps) {
+    const uint32_t x = above[w];
+    if (x >> lane & 1u) t.out[place[w] + __popc(x & below)] = t.lo + 32 * w + lane;
+  }
+  return true;
+}
+
+// One list: request blockIdx.y's tokens in (layer, head) blockIdx.x.  Tokens before lo and from hi on stay,
+// and of those between the `need` of largest key.
+__global__ void __launch_bounds__(kSelThreads) k_select_kept(const __grid_constant__ SelectArgs a, int words) {
+  __shared__ SelectShared sh;
+  extern __shared__ uint32_t dyn[];
+  const int tid = threadIdx.x;
   const int i = blockIdx.y, layer = blockIdx.x / a.H, head = blockIdx.x - layer * a.H;
   dep_wait();
-  dep_trigger();
   const int sid = a.sids[i];
   int32_t* out = a.kept + ((int64_t)i * gridDim.x + blockIdx.x) * a.most;
   int keep = a.keeps[i], c = 0;
@@ -53,86 +363,25 @@ __global__ void __launch_bounds__(kSelThreads) k_select_kept(const __grid_consta
     keep = 0;
   }
   keep = min(keep, c);
-  const float* w = a.w.data + layer * a.w.layer_stride + (bad ? 0 : sid) * a.w.session_stride + head * a.w.head_stride;
   const int lo = min(a.first, keep), hi = max(c - min(a.last, keep - lo), lo);
-  int need = keep - lo - (c - hi);
-  uint32_t last = 0xffffffffu;      // the last kept key, with `need` of its equals
-  int ties = 0;
-  if (keep == 0) {
-  } else if (need == hi - lo) {
-    last = 0;
-    ties = need;
-  } else if (need > 0) {
-    uint32_t have = 0;
-    int shift = 32;
-    while (shift > 0) {
-      const int bits = shift > 11 ? 11 : shift;      // 11, 11, 10
-      shift -= bits;
-      for (int b = tid; b < kBins; b += kSelThreads) bins[b] = 0;
-      __syncthreads();
-      for (int j = lo + tid; j < hi; j += kSelThreads) {
-        const uint32_t k = order_key(w[j]);
-        if (shift + bits == 32 || (k >> (shift + bits)) == (have >> (shift + bits)))
-          atomicAdd(&bins[k >> shift & ((1u << bits) - 1u)], 1);
-      }
-      __syncthreads();
-      // from the top bin down: the bin in which `need` is reached
-      constexpr int kPer = kBins / kSelThreads;
-      int mine[kPer], sum = 0;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) sum += mine[e] = bins[kBins - 1 - (tid * kPer + e)];
-      int x = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      if (lane == 31) sums[0][wid] = x;
-      __syncthreads();
-      int above = x - sum;
-      for (int v = 0; v < wid; ++v) above += sums[0][v];
-      if (above < need && above + sum >= need) {
-        int e = 0;
-        while (above + mine[e] < need) above += mine[e++];
-        s_digit = kBins - 1 - (tid * kPer + e);
-        s_above = above;
-      }
-      __syncthreads();
-      have |= s_digit << shift;
-      need -= s_above;
-    }
-    last = have;
-    ties = need;
-  }
-  // the kept ones, in order
-  int kept_before = 0, ties_before = 0;
-  for (int j0 = 0; j0 < c && keep > 0; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const bool between = j >= lo && j < hi;
-    const uint32_t k = between ? order_key(w[j]) : 0;
-    const bool tie = between && (k == last || need == hi - lo);
-    const uint32_t tie_votes = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) sums[0][wid] = __popc(tie_votes);
-    __syncthreads();
-    int t = ties_before + __popc(tie_votes & ((1u << lane) - 1u)), all_ties = 0;
-    for (int v = 0; v < kSelWarps; ++v) {
-      if (v < wid) t += sums[0][v];
-      all_ties += sums[0][v];
-    }
-    ties_before += all_ties;
-    const bool stay = j < c && (!between || (tie ? t < ties : k > last));
-    const uint32_t votes = __ballot_sync(0xffffffffu, stay);
-    if (lane == 0) sums[1][wid] = __popc(votes);
-    __syncthreads();
-    int at = kept_before + __popc(votes & ((1u << lane) - 1u)), all = 0;
-    for (int v = 0; v < kSelWarps; ++v) {
-      if (v < wid) at += sums[1][v];
-      all += sums[1][v];
-    }
-    kept_before += all;
-    if (stay && at < keep) out[at] = j;
-  }
+  List t;
+  t.n = hi - lo;
+  t.need = keep - lo - (c - hi);
+  t.lo = lo;
+  t.out = out + lo;
+  t.w = a.w.data + layer * a.w.layer_stride + (bad ? 0 : sid) * a.w.session_stride + head * a.w.head_stride + lo;
+  // the first and last ones, and what is behind the list
+  for (int j = tid; j < lo; j += kSelThreads) out[j] = j;
+  if (keep > 0)
+    for (int j = tid; j < c - hi; j += kSelThreads) out[lo + t.need + j] = hi + j;
   for (int j = keep + tid; j < a.most; j += kSelThreads) out[j] = -1;
+  if (t.need == 0) return;
+  if (t.need == t.n) {
+    for (int j = tid; j < t.n; j += kSelThreads) t.out[j] = lo + j;
+    return;
+  }
+  if (t.n > 32 * words || !select_once(t, sh, OnceShared(dyn, words), few_of(words)))
+    select_by_digits(t, sh);
 }
 
 // ---------------------------------------------------------------- compaction
@@ -301,8 +550,15 @@ __global__ void __launch_bounds__(kCutThreads) k_truncate(DevPool p, const int32
 
 }  // namespace
 
+cudaError_t configure_keep() {
+  return cudaFuncSetAttribute(k_select_kept, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)OnceShared::bytes(kMostWords));
+}
+
 cudaError_t launch_select_kept(const SelectArgs& a, int n, cudaStream_t s) {
-  return launch_dependent(k_select_kept, dim3(a.p.J / 2 * a.H, n), kSelThreads, 0, s, a);
+  // words for the longest context that there may be
+  const int64_t tokens = (int64_t)a.p.maxB * a.p.T < a.w.tokens ? (int64_t)a.p.maxB * a.p.T : a.w.tokens;
+  const int words = (int)((tokens + 31) / 32 < kMostWords ? (tokens + 31) / 32 : kMostWords);
+  return launch_dependent(k_select_kept, dim3(a.p.J / 2 * a.H, n), kSelThreads, OnceShared::bytes(words), s, a, words);
 }
 
 cudaError_t launch_compact(const CompactArgs& a, int n, int row_bytes, int num_sms, cudaStream_t s) {

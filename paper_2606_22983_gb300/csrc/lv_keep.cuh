@@ -26,6 +26,7 @@ struct CompactArgs {
   int32_t* lens;           // [n]
 };
 
+cudaError_t configure_keep();
 cudaError_t launch_select_kept(const SelectArgs& a, int n, cudaStream_t s);
 cudaError_t launch_compact(const CompactArgs& a, int n, int row_bytes, int num_sms, cudaStream_t s);
 cudaError_t launch_truncate(const DevPool& p, const int32_t* sids, const int32_t* lens, int n, cudaStream_t s);
