@@ -3,6 +3,8 @@
 // pages behind them given back.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "lv_batch.cuh"
 #include "lv_keep.cuh"
 
@@ -23,7 +25,16 @@ __device__ __forceinline__ uint32_t order_key(uint32_t bits) {
   return bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
 }
 
+// The number whose key it is, the nearest infinity where that is a NaN's.
+__device__ __forceinline__ float number_of(uint32_t key) {
+  if (key >= 0xff800000u) return INFINITY;
+  if (key <= 0x007fffffu) return -INFINITY;
+  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
 constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
+constexpr int kStepBits = 8;           // log2(kSelThreads): steps between the bounds
+static_assert(1 << kStepBits == kSelThreads, "a thread a step");
 constexpr int kBins = 2048;            // 11 bits of the key, or 12 in halves of words
 constexpr int kSample = 2048;
 constexpr int kMostWords = 2048;       // of 32 tokens, in a list that is read once
@@ -33,9 +44,10 @@ constexpr int kMostWords = 2048;       // of 32 tokens, in a list that is read o
 __host__ __device__ constexpr int few_of(int words) { return words * 4 > 2048 ? words * 4 : 2048; }
 
 struct SelectShared {
-  int bins[kBins];
+  int* bins;                   // [kBins]
+  int steps[kSelThreads];      // a histogram of those near the border
   int sums[2][kSelWarps];
-  int few, above, low;         // tokens near the border, above it, and of its lowest key
+  int few, above, low;         // tokens near the border, above it, and of the lowest key there
   int digit, before, inside;
   uint32_t lo_key, hi_key;
   uint32_t last_key[32];
@@ -43,18 +55,19 @@ struct SelectShared {
   int last;
 };
 
-// What select_once keeps beside it, for lists of `words` words of 32 tokens.
+// What select_once keeps beside it, for lists of `words` words of 32 tokens, a multiple of 32.  (The first histogram,
+// and at the end the kept ones' numbers, lie where the keys near the border do.)
 struct OnceShared {
-  uint32_t* above;
-  uint32_t* low;
-  int* place;
   uint32_t* key;       // of those near the border, [few_of(words)]
-  int* at;
-  static size_t bytes(int words) { return (size_t)words * 12 + (size_t)few_of(words) * 8; }
+  uint4* word;         // [words]: which of 32 tokens are above the bounds, have the lowest key in them, lie between
+  int* batch;          // [words / 32] kept ones of 1024 tokens
+  uint16_t* at;        // [few_of(words)]
+  static size_t bytes(int words) { return (size_t)words * 16 + words / 8 + (size_t)few_of(words) * 6; }
   __device__ OnceShared(uint32_t* p, int words)
-      : above(p), low(p + words), place(reinterpret_cast<int*>(p + 2 * words)), key(p + 3 * words),
-        at(reinterpret_cast<int*>(p + 3 * words + few_of(words))) {}
+      : key(p), word(reinterpret_cast<uint4*>(p + few_of(words))), batch(reinterpret_cast<int*>(word + words)),
+        at(reinterpret_cast<uint16_t*>(batch + words / 32)) {}
 };
+static_assert(few_of(0) >= kBins && 4 * few_of(0) >= 1024 * kSelWarps, "the histogram's room, and a KiB for each warp");
 
 // A list's tokens lo..hi, of which `need` of the largest keys are to be found.
 struct List {
@@ -142,7 +155,7 @@ __device__ __forceinline__ void bounds_by_sample(const List& t, SelectShared& sh
   float x[kSample / kSelThreads];
 #pragma unroll
   for (int e = 0; e < kSample / kSelThreads; ++e)
-    x[e] = t.w[(uint32_t)(((unsigned long long)(e * kSelThreads + tid) * (uint32_t)t.n) / kSample)];
+    x[e] = t.w[(uint32_t)(e * kSelThreads + tid) * (uint32_t)t.n / kSample];      // (n is at most 2^16)
   for (int b = tid; b < kBins / 4; b += kSelThreads) reinterpret_cast<int4*>(sh.bins)[b] = make_int4(0, 0, 0, 0);
   if (tid == 0) {
     sh.lo_key = 0;
@@ -161,10 +174,12 @@ __device__ __forceinline__ void bounds_by_sample(const List& t, SelectShared& sh
   uint32_t mine[kPer];
   int sum = 0, all;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    mine[e] = sh.bins[kBins - 1 - (tid * kPer + e)];
-    sum += (mine[e] & 0xffffu) + (mine[e] >> 16);
+  for (int e = 0; e < kPer; e += 4) {      // (a thread's bins downward)
+    const int4 x = reinterpret_cast<const int4*>(sh.bins)[(kBins - (tid * kPer + e)) / 4 - 1];
+    mine[e] = x.w, mine[e + 1] = x.z, mine[e + 2] = x.y, mine[e + 3] = x.x;
   }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) sum += (mine[e] & 0xffffu) + (mine[e] >> 16);
   int above = scan_up(sum, sh.sums[0], &all) - sum;
   if (above < r_lo && above + sum >= min(max(r_hi, 1), r_lo)) {
 #pragma unroll
@@ -179,65 +194,80 @@ __device__ __forceinline__ void bounds_by_sample(const List& t, SelectShared& sh
   __syncthreads();
 }
 
+// Inclusive sums over the warp.
+__device__ __forceinline__ int warp_up(int x) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if ((int)(threadIdx.x & 31) >= o) x += y;
+  }
+  return x;
+}
+
 // A list of up to 32 * kMostWords tokens, read once: a word a 32 tokens says which are above the bounds, which
-// have the lowest key in them (zeros do, where the border is among them), and those between are gathered.  The
-// border is then found among these: by their place between the bounds in 256 steps, finer until at most 32
-// share one, which a warp ranks.  False where it is not found so: the bounds do not hold it, too many keys
-// lie in them, or too many are equal at the border.
+// have the lowest key in them (zeros do, where the border is among them), and which lie between; these are
+// listed.  The border is then found among them: by their place between the bounds in kSelThreads steps, finer
+// until at most 32 share one, which a warp ranks.  False where it is not found so: the bounds do not hold it,
+// too many keys lie in them, or too many are equal at the border.
+//
+// What bounds it is instructions, not the list's bytes: so tokens are compared as numbers and told apart by
+// votes (some nine instructions for 32 of them), and a lane goes through the few set bits of a word by
+// itself.
 __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, const OnceShared& o, int room) {
-  uint32_t *const above = o.above, *const low = o.low;
-  int* const place = o.place;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int words = (t.n + 31) >> 5;
+  const int words = (t.n + 31) >> 5, batches = (t.n + 1023) >> 10;
+  __syncthreads();
   if (tid == 0) sh.few = sh.above = sh.low = sh.last = 0;
-  uint32_t lo_key = 0, hi_key = 0xffffffffu;
+  // (the two zeros are equal, and a NaN is not at or below any bound)
+  float lo_x = -INFINITY, hi_x = INFINITY;
   if (t.n > room) {
     bounds_by_sample(t, sh);
-    lo_key = sh.lo_key;
-    hi_key = sh.hi_key;
+    lo_x = number_of(sh.lo_key);
+    hi_x = number_of(sh.hi_key);
   } else {
     __syncthreads();
   }
-  const uint32_t below = (1u << lane) - 1u;
   constexpr int kUnroll = 8;
   int n_above = 0, n_low = 0;
-  for (int w0 = wid * kUnroll; w0 < words; w0 += kSelWarps * kUnroll) {
-    uint32_t key[kUnroll], in[kUnroll];
+  auto some_words = [&](int w0, auto full) {
+    constexpr bool kFull = decltype(full)::value;
+    float x[kUnroll];
     const float* from = t.w + 32 * w0 + lane;
     const int end = t.n - 32 * w0 - lane;
 #pragma unroll
-    for (int e = 0; e < kUnroll; ++e) key[e] = 32 * e < end ? __float_as_uint(__ldcs(from + 32 * e)) : 0u;
-    uint32_t up = 0, down = 0;
-    int total = 0;
+    for (int e = 0; e < kUnroll; ++e) x[e] = kFull || 32 * e < end ? __ldcs(from + 32 * e) : 0.f;
 #pragma unroll
     for (int e = 0; e < kUnroll; ++e) {
-      key[e] = 32 * e < end ? order_key(key[e]) : 0u;      // (0 is below every key)
-      const uint32_t a = __ballot_sync(0xffffffffu, key[e] > hi_key);
-      const uint32_t b = __ballot_sync(0xffffffffu, key[e] == lo_key && 32 * e < end);
-      in[e] = __ballot_sync(0xffffffffu, key[e] > lo_key && key[e] <= hi_key);
-      if (lane == e) up = a, down = b;
-      n_above += __popc(a);
-      n_low += __popc(b);
-      total += __popc(in[e]);
+      const bool there = kFull || 32 * e < end, to_hi = x[e] <= hi_x;
+      uint4 v;
+      v.x = __ballot_sync(0xffffffffu, there && !to_hi);
+      v.y = __ballot_sync(0xffffffffu, there && x[e] == lo_x);
+      v.z = __ballot_sync(0xffffffffu, there && x[e] > lo_x && to_hi);
+      v.w = 0;
+      if (lane == 0) o.word[w0 + e] = v;
     }
-    if (lane < kUnroll && w0 + lane < words) {
-      above[w0 + lane] = up;
-      low[w0 + lane] = down;
+  };
+  for (int b = wid; b < batches; b += kSelWarps) {
+#pragma unroll 1
+    for (int g = 0; g < 32; g += kUnroll) {
+      if (1024 * b + 32 * (g + kUnroll) <= t.n) some_words(32 * b + g, std::true_type());
+      else some_words(32 * b + g, std::false_type());
     }
-    if (total == 0) continue;
+    __syncwarp();
+    // a lane a word: those between are listed, in any order
+    const uint4 v = o.word[32 * b + lane];
+    n_above += __popc(v.x);
+    n_low += __popc(v.y);
+    const int mine = __popc(v.z), upto = warp_up(mine);
     int at = 0;
-    if (lane == 0) at = atomicAdd(&sh.few, total);
-    at = __shfl_sync(0xffffffffu, at, 0);
-#pragma unroll
-    for (int e = 0; e < kUnroll; ++e) {
-      const int to = at + __popc(in[e] & below);
-      if ((in[e] >> lane & 1u) && to < room) {
-        o.key[to] = key[e];
-        o.at[to] = 32 * (w0 + e) + lane;
-      }
-      at += __popc(in[e]);
-    }
+    if (lane == 31 && upto) at = atomicAdd(&sh.few, upto);
+    at = __shfl_sync(0xffffffffu, at, 31) + upto - mine;
+    for (uint32_t m = v.z; m; m &= m - 1, ++at)
+      if (at < room) o.at[at] = (uint16_t)(1024 * b + 32 * lane + __ffs(m) - 1);
+    __syncwarp();
   }
+  n_above = __reduce_add_sync(0xffffffffu, n_above);
+  n_low = __reduce_add_sync(0xffffffffu, n_low);
   if (lane == 0) {
     atomicAdd(&sh.above, n_above);
     atomicAdd(&sh.low, n_low);
@@ -246,42 +276,49 @@ __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, con
   const int few = sh.few;
   int r = t.need - sh.above;      // of those in the bounds
   if (few > room || r < 0 || r > few + sh.low) return false;
+  auto keep = [&](int j) { atomicOr(&o.word[j >> 5].x, 1u << (j & 31)); };
   if (r >= few) {
     // all between, and of the lowest ones the first
-    for (int j = tid; j < few; j += kSelThreads) atomicOr(&above[o.at[j] >> 5], 1u << (o.at[j] & 31));
-    r -= few;
-    const int per = (words + kSelThreads - 1) / kSelThreads;
-    if (r > 0) {
+    for (int j = tid; j < few; j += kSelThreads) keep(o.at[j]);
+    if (r > few) {
+      const int per = (words + kSelThreads - 1) / kSelThreads;
       const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
       int mine = 0, all;
-      for (int w = w0; w < w1; ++w) mine += __popc(low[w]);
-      int left = r - (scan_up(mine, sh.sums[0], &all) - mine);
+      for (int w = w0; w < w1; ++w) mine += __popc(o.word[w].y);
+      int left = r - few - (scan_up(mine, sh.sums[0], &all) - mine);
       for (int w = w0; w < w1 && left > 0; ++w) {
-        uint32_t x = low[w];
+        uint32_t x = o.word[w].y;
         const int have = __popc(x);
         if (have > left) {
           uint32_t rest = x;
           for (int k = 0; k < left; ++k) rest &= rest - 1;
           x ^= rest;
         }
-        atomicOr(&above[w], x);
+        atomicOr(&o.word[w].x, x);
         left -= have;
       }
     }
   } else if (r > 0) {
+    const uint32_t lo_key = order_key(__float_as_uint(lo_x)), hi_key = order_key(__float_as_uint(hi_x));
     const uint32_t width = hi_key - lo_key - 1;      // of key - lo_key - 1 at most
-    int shift = max(0, 24 - __clz(width | 1u)), up = 32;
+    int shift = max(0, 32 - kStepBits - __clz(width | 1u)), up = 32;
     uint32_t at = 0;      // (key - lo_key - 1) >> up of the border
     for (;;) {
-      sh.bins[tid] = 0;
+      sh.steps[tid] = 0;
       __syncthreads();
       const uint32_t digits = up - shift >= 32 ? ~0u : (1u << (up - shift)) - 1u;
       for (int j = tid; j < few; j += kSelThreads) {
-        const uint32_t d = o.key[j] - lo_key - 1;
-        if (up == 32 || d >> up == at) atomicAdd(&sh.bins[d >> shift & digits], 1);
+        uint32_t d;
+        if (up == 32) {
+          d = order_key(__float_as_uint(t.w[o.at[j]])) - lo_key - 1;
+          o.key[j] = d;
+        } else {
+          d = o.key[j];
+        }
+        if (up == 32 || d >> up == at) atomicAdd(&sh.steps[d >> shift & digits], 1);
       }
       __syncthreads();
-      const int mine = sh.bins[kSelThreads - 1 - tid];
+      const int mine = sh.steps[kSelThreads - 1 - tid];
       int all;
       const int upto = scan_up(mine, sh.sums[0], &all);
       if (upto - mine < r && upto >= r) {
@@ -295,17 +332,16 @@ __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, con
       up = shift;
       if (sh.inside <= 32) break;
       if (shift == 0) return false;
-      shift = max(0, shift - 8);
+      shift = max(0, shift - kStepBits);
     }
     for (int j = tid; j < few; j += kSelThreads) {
-      const uint32_t d = (o.key[j] - lo_key - 1) >> up;
-      const int where = o.at[j];
+      const uint32_t d = o.key[j] >> up;
       if (d > at) {
-        atomicOr(&above[where >> 5], 1u << (where & 31));
+        keep(o.at[j]);
       } else if (d == at) {
         const int k = atomicAdd(&sh.last, 1);
         sh.last_key[k] = o.key[j];
-        sh.last_at[k] = where;
+        sh.last_at[k] = o.at[j];
       }
     }
     __syncthreads();
@@ -319,39 +355,50 @@ __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, con
         const int wj = __shfl_sync(0xffffffffu, where, j);
         rank += kj > k || (kj == k && wj < where);
       }
-      if (lane < count && rank < r) atomicOr(&above[where >> 5], 1u << (where & 31));
+      if (lane < count && rank < r) keep(where);
     }
   }
   __syncthreads();
-  // the kept ones' places: what the words before keep
-  const int per = (words + kSelThreads - 1) / kSelThreads;
-  const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
-  int mine = 0, all;
-  for (int w = w0; w < w1; ++w) mine += __popc(above[w]);
-  int before = scan_up(mine, sh.sums[1], &all) - mine;
-  for (int w = w0; w < w1; ++w) {
-    place[w] = before;
-    before += __popc(above[w]);
+  // how many each 1024 tokens keep; then what comes before them, and their numbers through shared memory
+  for (int b = wid; b < batches; b += kSelWarps) {
+    const int all = __reduce_add_sync(0xffffffffu, __popc(o.word[32 * b + lane].x));
+    if (lane == 0) o.batch[b] = all;
   }
   __syncthreads();
-#pragma unroll 4
-  for (int w = wid; w < words; w += kSelWarps) {
-    const uint32_t x = above[w];
-    if (x >> lane & 1u) t.out[place[w] + __popc(x & below)] = t.lo + 32 * w + lane;
+  uint16_t* const numbers = reinterpret_cast<uint16_t*>(o.key) + 512 * wid;
+  for (int b = wid; b < batches; b += kSelWarps) {
+    int before = 0;
+    for (int k = lane; k < b; k += 32) before += o.batch[k];
+    int32_t* out = t.out + __reduce_add_sync(0xffffffffu, before);
+    const uint32_t mine = o.word[32 * b + lane].x;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {      // (512 tokens' numbers at once)
+      const uint32_t x = lane >> 4 == half ? mine : 0u;
+      const int upto = warp_up(__popc(x)), all = __shfl_sync(0xffffffffu, upto, 31);
+      int at = upto - __popc(x);
+      for (uint32_t m = x; m; m &= m - 1) numbers[at++] = (uint16_t)(32 * lane + __ffs(m) - 1);
+      __syncwarp();
+      const int from = t.lo + 1024 * b;
+      for (int k = lane; k < all; k += 32) out[k] = from + numbers[k];
+      out += all;
+      __syncwarp();
+    }
   }
   return true;
 }
 
-// One list: request blockIdx.y's tokens in (layer, head) blockIdx.x.  Tokens before lo and from hi on stay,
+// One list: a request's tokens in a layer and head.  Tokens before lo and from hi on stay,
 // and of those between the `need` of largest key.
-__global__ void __launch_bounds__(kSelThreads) k_select_kept(const __grid_constant__ SelectArgs a, int words) {
+__global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_constant__ SelectArgs a, int words) {
   __shared__ SelectShared sh;
   extern __shared__ uint32_t dyn[];
   const int tid = threadIdx.x;
-  const int i = blockIdx.y, layer = blockIdx.x / a.H, head = blockIdx.x - layer * a.H;
+  const int lists = a.p.J / 2 * a.H, i = blockIdx.x / lists, list = blockIdx.x - i * lists;
+  const int layer = list / a.H, head = list - layer * a.H;
+  if (tid == 0) sh.bins = reinterpret_cast<int*>(dyn);
   dep_wait();
   const int sid = a.sids[i];
-  int32_t* out = a.kept + ((int64_t)i * gridDim.x + blockIdx.x) * a.most;
+  int32_t* out = a.kept + ((int64_t)i * lists + list) * a.most;
   int keep = a.keeps[i], c = 0;
   bool bad = sid < 0 || sid >= a.p.S || keep < 0 || keep > a.most;
   if (!bad) {
@@ -359,7 +406,7 @@ __global__ void __launch_bounds__(kSelThreads) k_select_kept(const __grid_consta
     bad = c > a.w.tokens;
   }
   if (bad) {
-    if (blockIdx.x == 0 && tid == 0) report(a.p.ctl, LV_ERR_BOUNDS, i);
+    if (list == 0 && tid == 0) report(a.p.ctl, LV_ERR_BOUNDS, i);
     keep = 0;
   }
   keep = min(keep, c);
@@ -557,8 +604,8 @@ cudaError_t configure_keep() {
 cudaError_t launch_select_kept(const SelectArgs& a, int n, cudaStream_t s) {
   // words for the longest context that there may be
   const int64_t tokens = (int64_t)a.p.maxB * a.p.T < a.w.tokens ? (int64_t)a.p.maxB * a.p.T : a.w.tokens;
-  const int words = (int)((tokens + 31) / 32 < kMostWords ? (tokens + 31) / 32 : kMostWords);
-  return launch_dependent(k_select_kept, dim3(a.p.J / 2 * a.H, n), kSelThreads, OnceShared::bytes(words), s, a, words);
+  const int words = (int)((tokens + 1023) / 1024 * 32 < kMostWords ? (tokens + 1023) / 1024 * 32 : kMostWords);
+  return launch_dependent(k_select_kept, dim3(a.p.J / 2 * a.H * n), kSelThreads, OnceShared::bytes(words), s, a, words);
 }
 
 cudaError_t launch_compact(const CompactArgs& a, int n, int row_bytes, int num_sms, cudaStream_t s) {
