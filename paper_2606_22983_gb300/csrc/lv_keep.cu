@@ -37,6 +37,7 @@ constexpr int kStepBits = 8;           // log2(kSelThreads): steps between the b
 static_assert(1 << kStepBits == kSelThreads, "a thread a step");
 constexpr int kBins = 2048;            // 11 bits of the key, or 12 in halves of words
 constexpr int kSample = 2048;
+constexpr int kTurns = 64;             // requests whose lists are taken by their lengths
 constexpr int kMostWords = 2048;       // of 32 tokens, in a list that is read once
 
 // Keys near the border between kept and not that are gathered: an eighth of the longest list, which the bounds
@@ -49,6 +50,7 @@ struct SelectShared {
   int sums[2][kSelWarps];
   int few, above, low;         // tokens near the border, above it, and of the lowest key there
   int digit, before, inside;
+  int turn, ctx[kTurns];
   uint32_t lo_key, hi_key;
   uint32_t last_key[32];
   int last_at[32];
@@ -389,14 +391,31 @@ __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, con
 
 // One list: a request's tokens in a layer and head.  Tokens before lo and from hi on stay,
 // and of those between the `need` of largest key.
-__global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_constant__ SelectArgs a, int words) {
+__global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_constant__ SelectArgs a, int n, int words) {
   __shared__ SelectShared sh;
   extern __shared__ uint32_t dyn[];
   const int tid = threadIdx.x;
-  const int lists = a.p.J / 2 * a.H, i = blockIdx.x / lists, list = blockIdx.x - i * lists;
+  const int lists = a.p.J / 2 * a.H, turn = blockIdx.x / lists, list = blockIdx.x - turn * lists;
   const int layer = list / a.H, head = list - layer * a.H;
   if (tid == 0) sh.bins = reinterpret_cast<int*>(dyn);
   dep_wait();
+  int i = turn;
+  if (n > 1 && n <= kTurns) {
+    // the longest first, so that none of them ends last
+    if (tid < n) {
+      const int sid = a.sids[tid];
+      sh.ctx[tid] = sid >= 0 && sid < a.p.S ? a.p.sess[sid].ctx_tokens : -1;
+    }
+    __syncthreads();
+    if (tid < n) {
+      const int mine = sh.ctx[tid];
+      int before = 0;
+      for (int j = 0; j < n; ++j) before += sh.ctx[j] > mine || (sh.ctx[j] == mine && j < tid);
+      if (before == turn) sh.turn = tid;
+    }
+    __syncthreads();
+    i = sh.turn;
+  }
   const int sid = a.sids[i];
   int32_t* out = a.kept + ((int64_t)i * lists + list) * a.most;
   int keep = a.keeps[i], c = 0;
@@ -605,7 +624,7 @@ cudaError_t launch_select_kept(const SelectArgs& a, int n, cudaStream_t s) {
   // words for the longest context that there may be
   const int64_t tokens = (int64_t)a.p.maxB * a.p.T < a.w.tokens ? (int64_t)a.p.maxB * a.p.T : a.w.tokens;
   const int words = (int)((tokens + 1023) / 1024 * 32 < kMostWords ? (tokens + 1023) / 1024 * 32 : kMostWords);
-  return launch_dependent(k_select_kept, dim3(a.p.J / 2 * a.H * n), kSelThreads, OnceShared::bytes(words), s, a, words);
+  return launch_dependent(k_select_kept, dim3(a.p.J / 2 * a.H * n), kSelThreads, OnceShared::bytes(words), s, a, n, words);
 }
 
 cudaError_t launch_compact(const CompactArgs& a, int n, int row_bytes, int num_sms, cudaStream_t s) {
