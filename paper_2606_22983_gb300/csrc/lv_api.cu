@@ -1658,6 +1658,7 @@ struct lv_batch {
   int32_t* arrived = nullptr;
   int32_t* ticket = nullptr;
   int32_t* unit_tickets = nullptr;      // lv_attention_weights
+  uint32_t* refused = nullptr;
   lv::StepHead* head = nullptr;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
@@ -1821,6 +1822,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
         (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->unit_tickets, 2)) != LV_OK ||
+        (st = batch_alloc(b, &b->refused, lv::kMostSegments / 32)) != LV_OK ||
         (st = batch_alloc(b, &b->head, 1)) != LV_OK ||
         (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
         (st = batch_alloc(b, &b->part_ml, rows)) != LV_OK)
@@ -2195,6 +2197,7 @@ lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, co
   a.pre_reqs = b->pre_reqs;
   a.head = b->head;
   a.tickets = b->unit_tickets;
+  a.refused = b->refused;
   a.q = static_cast<const uint8_t*>(q->data);
   a.q_row = q->row_stride;
   a.q_head = q->head_stride;

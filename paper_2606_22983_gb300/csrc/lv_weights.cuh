@@ -19,6 +19,7 @@ struct WeightArgs {
   const PlanReq* pre_reqs;     // of the prefixes; null: no room for them
   const StepHead* head;
   int32_t* tickets;            // units given out, CTAs done; zero between calls
+  uint32_t* refused;           // [kMostSegments / 32] a bit a segment (every CTA writes the same)
   const uint8_t* q;
   int64_t q_row, q_head;       // in elements
   const float* lse;            // [num_tokens][Hq]
@@ -59,6 +60,7 @@ cudaError_t launch_weights_tc(const WeightArgs& a, const WeightMaps& m, bool bf1
 cudaError_t configure_weights_tc();
 cudaError_t launch_weights_plain(const WeightArgs& a, bool bf16, int num_sms, cudaStream_t s);
 cudaError_t configure_weights();
+constexpr int kMostSegments = 2 * 4096;
 
 #ifdef __CUDACC__
 // The weights' work: a segment is the context of one request with the request's rows, or a prefix with the rows
@@ -76,14 +78,16 @@ struct Unit {
   int t0, t1;                  // tokens [t0, t1) of the segment see some of its keys
 };
 
-constexpr int kMostSegments = 2 * 4096;
+// Units are taken in kClasses goes, those that most rows see first, so that no long one begins last: a
+// segment's keys are seen by the fewer rows the later they are, so a class is a stretch of them.
+constexpr int kClasses = 4;
 
 // What a CTA knows of the segments, divided among NT of its threads.
 template <int NT>
 struct SegmentIndex {
-  int before[NT + 1];                        // units before thread t's segments
-  uint32_t refused[kMostSegments / 32];
+  int before[kClasses * NT + 1];             // units before thread t's segments in class c
   int ws[NT / 32];
+  int most;                                  // rows' tokens of a segment
 };
 
 __device__ __forceinline__ Segment segment_of(const WeightArgs& a, int n, int s) {
@@ -131,7 +135,17 @@ __device__ __forceinline__ bool counts(const WeightArgs& a, const Segment& g, in
   return r >= a.row_starts[lo + 1] - a.last;
 }
 
-// Every thread of the CTA calls it: fills x and returns the units in all.  first_of: room for a word a session.
+// Tiles of kKeys keys of g before the end of class c.
+template <int kKeys>
+__device__ __forceinline__ int class_end(const Segment& g, int c, int most) {
+  const int all = (g.keys + kKeys - 1) / kKeys;
+  if (c == kClasses - 1) return all;
+  const int more_than = (int)((long long)most * (kClasses - 1 - c) / kClasses);      // tokens see its keys
+  if (g.tokens <= more_than) return 0;
+  return g.req < 0 ? all : min(all, (int)(((long long)g.first + g.tokens - more_than + kKeys - 1) / kKeys));
+}
+
+// Every thread of the CTA (whole warps) calls it: fills x and returns the units in all.  first_of: room for a word a session.
 // The segments whose session an earlier one has, or that the weights have no room for, are refused (their
 // units are empty).
 template <int NT, int kKeys>
@@ -139,41 +153,59 @@ __device__ int index_segments(const WeightArgs& a, const StepHead& step, Segment
   const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
   const int tid = threadIdx.x, lane = tid & 31;
   for (int s = tid; s < a.S; s += blockDim.x) first_of[s] = kMostSegments;
-  for (int s = tid; s < (count + 31) / 32; s += blockDim.x) x.refused[s] = 0;
+  if (tid == 0) x.most = 0;
   __syncthreads();
   for (int s = tid; s < count; s += blockDim.x) {
     const Segment g = segment_of(a, n, s);
     if (g.keys > 0) atomicMin(&first_of[g.sid], s);
   }
   __syncthreads();
-  const int per = (count + NT - 1) / NT;
-  int mine = 0;
-  for (int s = min(tid * per, count); s < min((tid + 1) * per, count) && tid < NT; ++s) {
-    const Segment g = segment_of(a, n, s);
-    if (g.keys == 0) continue;
-    const bool again = first_of[g.sid] != s, far = g.keys > a.w_tokens;
-    if (again || far) {
-      atomicOr(&x.refused[s >> 5], 1u << (s & 31));
-      if (blockIdx.x == 0) report(a.ctl, again ? LV_ERR_DOUBLE_MAP : LV_ERR_BOUNDS, s < n ? s : s - n);
+  for (int s0 = tid - lane; s0 < count; s0 += blockDim.x) {
+    const int s = s0 + lane;
+    bool again = false, far = false;
+    if (s < count) {
+      const Segment g = segment_of(a, n, s);
+      again = g.keys > 0 && first_of[g.sid] != s;
+      far = g.keys > a.w_tokens;
+      if ((again || far) && blockIdx.x == 0) report(a.ctl, again ? LV_ERR_DOUBLE_MAP : LV_ERR_BOUNDS, s < n ? s : s - n);
     }
-    mine += a.H * ((g.keys + kKeys - 1) / kKeys);
+    const uint32_t votes = __ballot_sync(0xffffffffu, again || far);
+    if (lane == 0) a.refused[s0 >> 5] = votes;
   }
-  int sum = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += y;
-  }
-  if (lane == 31 && tid < NT) x.ws[tid >> 5] = sum;
+  const int per = (count + NT - 1) / NT, s0 = min(tid * per, count), s1 = tid < NT ? min(s0 + per, count) : s0;
+  int longest = 0;
+  for (int s = s0; s < s1; ++s) longest = max(longest, segment_of(a, n, s).tokens);
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 0 && longest) atomicMax(&x.most, longest);
   __syncthreads();
-  if (tid < NT) {
-    int before = 0;
-    for (int v = 0; v < tid >> 5; ++v) before += x.ws[v];
-    x.before[tid + 1] = before + sum;
+  const int most = x.most;
+  int total = 0;
+#pragma unroll 1
+  for (int c = 0; c < kClasses; ++c) {
+    int mine = 0;
+    for (int s = s0; s < s1; ++s) {
+      const Segment g = segment_of(a, n, s);
+      mine += a.H * (class_end<kKeys>(g, c, most) - (c ? class_end<kKeys>(g, c - 1, most) : 0));
+    }
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    if (lane == 31 && tid < NT) x.ws[tid >> 5] = sum;
+    __syncthreads();
+    int before = total;
+    for (int v = 0; v < NT / 32; ++v) {
+      if (v < tid >> 5) before += x.ws[v];
+      total += x.ws[v];
+    }
+    if (tid < NT) x.before[c * NT + tid + 1] = before + sum;
+    __syncthreads();
   }
   if (tid == 0) x.before[0] = 0;
   __syncthreads();
-  return x.before[NT];
+  return total;
 }
 
 // Unit u of all; no tokens where there is nothing to do.
@@ -181,23 +213,25 @@ template <int NT, int kKeys>
 __device__ __forceinline__ Unit find_unit(const WeightArgs& a, const StepHead& step, const SegmentIndex<NT>& x, int u) {
   const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
   const int per = (count + NT - 1) / NT;
-  int lo = 0, hi = NT - 1;      // the last thread whose segments do not begin after u
+  int lo = 0, hi = kClasses * NT - 1;      // the last thread and class whose segments do not begin after u
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (x.before[mid] <= u) lo = mid;
     else hi = mid - 1;
   }
-  int s = lo * per, off = u - x.before[lo];
+  const int c = lo / NT, most = x.most;
+  int s = (lo - c * NT) * per, off = u - x.before[lo], t0;
   Segment g = segment_of(a, n, s);
   for (;;) {
-    const int units = a.H * ((g.keys + kKeys - 1) / kKeys);
+    t0 = c ? class_end<kKeys>(g, c - 1, most) : 0;
+    const int units = a.H * (class_end<kKeys>(g, c, most) - t0);
     if (off < units) break;
     off -= units;
     g = segment_of(a, n, ++s);
   }
   const int tile = off / a.H;
-  Unit out = unit_of(a, g, off - tile * a.H, tile * kKeys, kKeys);
-  if (x.refused[s >> 5] >> (s & 31) & 1u) out.t1 = out.t0;
+  Unit out = unit_of(a, g, off - tile * a.H, (t0 + tile) * kKeys, kKeys);
+  if (a.refused[s >> 5] >> (s & 31) & 1u) out.t1 = out.t0;
   return out;
 }
 #endif

@@ -7,21 +7,22 @@ namespace lv {
 
 namespace {
 
-// Roles of a CTA's thirteen warps.
-constexpr int kSumWarps = 8;              // two warpgroups, one for each half of a unit's keys
-constexpr int kWarpK = 8, kWarpQ = 9, kWarpMma = 10, kWarpRows = 11, kWarpUnits = 12;
-constexpr int kThreads = 416;
+// Roles of a CTA's twenty warps.
+constexpr int kSumWarps = 16;             // a warpgroup for each buffer of scores and half of a unit's keys
+constexpr int kWarpK = 16, kWarpQ = 17, kWarpMma = 18, kWarpUnits = 19;
+constexpr int kThreads = 640;
 constexpr int kHalf = 128, kUnitKeys = 2 * kHalf;
 constexpr int kCols = 128;                // rows of the step (packed) a product has as columns
 constexpr int kIndexThreads = 64;
-constexpr int kUnits = 4;                 // found ahead
+constexpr int kUnits = 8;                 // found ahead at most,
+constexpr int kAhead = 5;                 // where no more products than this are left to be issued
 constexpr float kLog2e = 1.44269504088896341f;
 
 template <int DP>
 struct WShape {
   static constexpr int kBlocks = DP / 64;                  // 128-byte wide column blocks
   static constexpr int kTile = kHalf * DP * 2;             // bytes of half a unit's K, and of a tile of queries
-  static constexpr int kKStages = DP == 128 ? 4 : 8;
+  static constexpr int kKStages = DP == 128 ? 3 : 6;
   static constexpr int kQStages = DP == 128 ? 3 : 4;
   static constexpr int kQ = kKStages * kTile;
   static constexpr int kMisc = kQ + kQStages * kTile;
@@ -30,7 +31,7 @@ struct WShape {
 struct WBars {
   uint64_t k_full[8], k_empty[8], q_full[4], q_empty[4];
   uint64_t s_full[2][2], s_empty[2][2];    // a buffer of scores, a half
-  uint64_t b_full[2], b_empty[2];          // the rows' terms beside it
+  uint64_t part_full, part_empty;          // sums of a unit's second buffer
   uint64_t unit_full[kUnits], unit_empty[kUnits];
   uint64_t drain;
   uint32_t tmem;
@@ -39,7 +40,9 @@ struct WBars {
 
 struct Misc {
   WBars bars;
-  float b[2][kCols];
+  float b[kSumWarps][kCols];      // the rows' terms, a copy a warp
+  float part[kUnitKeys];
+  volatile int issued;            // tiles of queries
   Unit units[kUnits];
   SegmentIndex<kIndexThreads> index;
 };
@@ -69,12 +72,11 @@ struct Chunks {
 //
 // One CTA an SM; units are taken in order from a counter, long ones (the first keys of a context, which
 // all rows see) first.
-//   warp 12  finds units ahead
-//   warp 8   K of a unit into a ring of shared memory, by TMA: a box a page and 64 columns
-//   warp 9   queries into a ring of their own, by TMA
-//   warp 11  the rows' terms b
-//   warp 10  products into two buffers of TMEM for each half
-//   0 .. 7   exponentials and sums, a thread a key
+//   warp 19  finds units ahead
+//   warp 16  K of a unit into a ring of shared memory, by TMA: a box a page and 64 columns
+//   warp 17  queries into a ring of their own, by TMA
+//   warp 18  products into two buffers of TMEM for each half
+//   0 .. 15  the rows' terms, exponentials and sums, a thread a key in every second product
 template <int DP, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1)
 k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUtensorMap kmap,
@@ -106,15 +108,16 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
         bar_init(&bars.s_full[i][h], products);
         bar_init(&bars.s_empty[i][h], 4);
       }
-      bar_init(&bars.b_full[i], 1);
-      bar_init(&bars.b_empty[i], kSumWarps);
     }
+    bar_init(&bars.part_full, kSumWarps / 2);
+    bar_init(&bars.part_empty, kSumWarps / 2);
     for (int i = 0; i < kUnits; ++i) {
       bar_init(&bars.unit_full[i], 1);
-      bar_init(&bars.unit_empty[i], kSumWarps + 4);
+      bar_init(&bars.unit_empty[i], kSumWarps + 3);
     }
     bar_init(&bars.drain, 1);
     bars.bad = 0;
+    m.issued = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == kWarpMma) {
@@ -154,63 +157,96 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
   };
 
   if (wid < kSumWarps) {
-    const int half = wid >> 2, row = threadIdx.x & 127;
-    const uint32_t s_at = tmem + ((uint32_t)(wid & 3) << 21) + kCols * half;      // this warp's 32 lanes of TMEM
-    uint32_t b_par = 0, s_par = 0;      // a bit a buffer
-    int buf = 0;
+    const int buf = wid >> 3, half = wid >> 2 & 1, row = threadIdx.x & 127;
+    // this warp's 32 lanes of its buffer and half in TMEM
+    const uint32_t s_at = tmem + ((uint32_t)(wid & 3) << 21) + kCols * (2 * buf + half);
     const float2 c2 = make_float2(a.scale, a.scale);
+    uint32_t s_par = 0, part_par = 0;
+    int turn = 0;           // the buffer of the next product
+    const int Hq = a.H * a.G;
+    float* const b = m.b[wid];
+    int in_col[kCols / 32];      // tokens before this lane's columns in a product
+#pragma unroll
+    for (int k = 0; k < kCols / 32; ++k) in_col[k] = (32 * k + lane) / a.G;
     while (ok && next_unit()) {
       const Chunks ch(a, u);
       const int key = u.key0 + kHalf * half + row;
       const bool there = half < ch.halves, mine = key < u.g.keys;
+      // the unit's sums are those of the first buffer's threads, which add the second's; a unit of one
+      // product is its buffer's alone
+      const bool writes = ch.count > 1 ? buf == 0 : buf == turn, joins = ch.count > 1;
       float* w = a.w + u.g.sid * a.w_session + u.head * a.w_head + key;
-      const float before = mine ? *w : 0.f;
+      const float before = mine && writes ? *w : 0.f;
       // the packed rows that see the key: from its own position on, to the window's end
       const long long from = u.g.req < 0 ? 0 : (long long)(key - u.g.first) * a.G;
       const long long to = u.g.req < 0 || a.window == 0 || key < a.sinks ? 1ll << 40 : from + (long long)a.window * a.G;
       const bool check_b = u.g.req < 0 && a.last > 0;
       LongSum all;
-      for (int i = 0; i < ch.count; ++i) {
-        if (!(ok = bar_wait(&bars, &bars.b_full[buf], b_par >> buf & 1, a.wait_ns))) break;
-        b_par ^= 1u << buf;
+      // the sums of four columns' rows, asked for a product ahead
+      float z[kCols / 32];
+      const int tokens = ch.step / a.G;
+      auto ask = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < kCols / 32; ++k) {
+          z[k] = -INFINITY;
+          const int c = 32 * k + lane;
+          if (i >= ch.count || c >= ch.rows(i)) continue;
+          int token = u.t0 + i * tokens + in_col[k], hq = u.head * a.G + c - in_col[k] * a.G;
+          if (a.G > kCols) {      // (a product does not begin at a token's first head)
+            const int R = ch.begin + i * ch.step + c;
+            token = R / a.G;
+            hq = u.head * a.G + R - token * a.G;
+          }
+          if (!check_b || counts(a, u.g, n, token)) z[k] = a.lse[(int64_t)(u.g.qrow + token) * Hq + hq];
+        }
+      };
+      if (there) ask(turn ^ buf);
+      for (int i = turn ^ buf; i < ch.count; i += 2) {
         if (there) {
-          if (!(ok = bar_wait(&bars, &bars.s_full[buf][half], s_par >> buf & 1, a.wait_ns))) break;
-          s_par ^= 1u << buf;
+#pragma unroll
+          for (int k = 0; k < kCols / 32; ++k) b[32 * k + lane] = z[k] == -INFINITY ? z[k] : -z[k] * kLog2e;
+          __syncwarp();
+          ask(i + 2);
+          if (!(ok = bar_wait(&bars, &bars.s_full[buf][half], s_par, a.wait_ns))) break;
+          s_par ^= 1;
           tc_fence_after();
           const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
           const int c_lo = clamp_col(from - R0), c_hi = mine ? min(rows, clamp_col(to - R0)) : 0;
-          const uint32_t at = s_at + 2 * kCols * buf;
-          const float* b = m.b[buf];
           float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
+          const bool full = c_lo == 0 && c_hi == kCols && !check_b, all_full = __all_sync(0xffffffffu, full);
 #pragma unroll 1
           for (int c0 = 0; c0 < rows; c0 += 32) {
             uint32_t x[32];
-            tc_ld32(x, at + c0);
-            const uint32_t seen = low_bits(c_hi - c0) & ~low_bits(c_lo - c0);
-            const bool open = __all_sync(0xffffffffu, seen == ~0u) && !check_b;
-            tc_wait_ld();
-            tc_loaded<32>(x);
+            tc_ld32(x, s_at + c0);
             const float* s = reinterpret_cast<const float*>(x);
-            if (open) {
+            if (all_full) {
+              tc_wait_ld();
+              tc_loaded<32>(x);
 #pragma unroll
               for (int j = 0; j < 32; j += 4) {
                 const float4 bb = *reinterpret_cast<const float4*>(b + c0 + j);
-                float2 y = fma2(make_float2(s[j], s[j + 1]), c2, make_float2(bb.x, bb.y));
-                float2 z = fma2(make_float2(s[j + 2], s[j + 3]), c2, make_float2(bb.z, bb.w));
-                y.x = exp2_fast(y.x);
-                y.y = exp2_fast(y.y);
-                z.x = exp2_fast(z.x);
-                z.y = exp2_fast(z.y);
-                acc0 = add2(acc0, y);
-                acc1 = add2(acc1, z);
+                float2 y0 = fma2(make_float2(s[j], s[j + 1]), c2, make_float2(bb.x, bb.y));
+                float2 y1 = fma2(make_float2(s[j + 2], s[j + 3]), c2, make_float2(bb.z, bb.w));
+                y0.x = exp2_fast(y0.x);
+                y0.y = exp2_fast(y0.y);
+                y1.x = exp2_fast(y1.x);
+                y1.y = exp2_fast(y1.y);
+                acc0 = add2(acc0, y0);
+                acc1 = add2(acc1, y1);
               }
-            } else if (__any_sync(0xffffffffu, seen != 0)) {
+            } else {
+              uint32_t seen = low_bits(c_hi - c0) & ~low_bits(c_lo - c0);
+              if (check_b) seen &= __ballot_sync(0xffffffffu, b[c0 + lane] != -INFINITY);
+              tc_wait_ld();
+              tc_loaded<32>(x);
+              if (!__any_sync(0xffffffffu, seen != 0)) continue;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                const float bb = b[c0 + j];
-                const float y = seen >> j & 1u && bb != -INFINITY ? exp2_fast(fmaf(s[j], a.scale, bb)) : 0.f;
-                if (j & 1) acc1.x += y;
-                else acc0.x += y;
+              for (int j = 0; j < 32; j += 2) {
+                const float2 bb = *reinterpret_cast<const float2*>(b + c0 + j);
+                float2 y = fma2(make_float2(s[j], s[j + 1]), c2, bb);
+                y.x = exp2_fast(seen >> j & 1u ? y.x : -INFINITY);
+                y.y = exp2_fast(seen >> (j + 1) & 1u ? y.y : -INFINITY);
+                acc0 = add2(acc0, y);
               }
             }
           }
@@ -219,38 +255,67 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
           acc0 = add2(acc0, acc1);
           all.add(acc0.x + acc0.y);
         }
-        warp_arrive(&bars.b_empty[buf]);
-        buf ^= 1;
       }
-      if (ok && mine && all.sum != 0.f) *w = before + all.sum;
+      turn ^= ch.count & 1;
+      if (!ok) break;
+      if (joins) {
+        float* part = m.part + kHalf * half + row;
+        if (buf == 1) {
+          if (!(ok = bar_wait(&bars, &bars.part_empty, ~part_par & 1u, a.wait_ns))) break;
+          *part = all.sum;
+          warp_arrive(&bars.part_full);
+        } else {
+          if (!(ok = bar_wait(&bars, &bars.part_full, part_par, a.wait_ns))) break;
+          all.add(*part);
+          warp_arrive(&bars.part_empty);
+        }
+        part_par ^= 1;
+      }
+      if (writes && mine && all.sum != 0.f) *w = before + all.sum;
     }
     tc_fence_before();
   } else if (wid == kWarpK) {
-    // lane i finds the page of box i of half a unit's keys; one thread then issues the copies
-    const int boxes = kHalf / box_rows;
+    // lane i finds the page of box i of a unit's keys, before the unit before it is done; one thread then
+    // issues the copies
+    const int boxes = kHalf / box_rows;      // of a half
     int stage = 0;
     uint32_t par = 0;
     long long halves = 0;
-    while (ok && next_unit()) {
-      const Chunks ch(a, u);
+    int page = 0, off = 0;
+    auto find = [&]() {
+      const int key = u.key0 + lane * box_rows;
       const int32_t* table = u.g.req < 0 ? a.pool_table + (size_t)u.g.sid * a.maxB : a.tables + (size_t)u.g.req * a.maxB;
-      for (int h = 0; ok && h < ch.halves; ++h) {
-        const int key = u.key0 + kHalf * h + lane * box_rows;
-        const int b = a.t_shift >= 0 ? key >> a.t_shift : key / a.T, off = key - b * a.T;
-        int page = -1;
-        if (lane < boxes && key < u.g.keys) page = table[b];
-        if ((uint32_t)page >= a.hbm_pages) page = (int)a.hbm_pages;      // outside the array: zeros
+      const int b = a.t_shift >= 0 ? key >> a.t_shift : key / a.T;
+      off = key - b * a.T;
+      page = lane < 2 * boxes && key < u.g.keys ? table[b] : -1;
+    };
+    bool more = next_unit();
+    if (more) find();
+    while (more) {
+      const int head = u.head, count = u.g.keys - u.key0 > kHalf ? 2 : 1;
+      const int pages = (uint32_t)page < a.hbm_pages ? page : (int)a.hbm_pages;      // none: outside the array, zeros
+      const int offs = off;
+      for (int h = 0; ok && h < count; ++h) {
         if (!(ok = bar_wait(&bars, &bars.k_empty[stage], ~par & 1u, a.wait_ns))) break;
         uint64_t* full = &bars.k_full[stage];
         const uint32_t dst = k_s + stage * S::kTile;
         if (elected()) bar_expect(full, S::kTile);
 #pragma unroll 1
-        for (int i = 0; i < boxes; ++i) {
-          const int pg = __shfl_sync(0xffffffffu, page, i), of = __shfl_sync(0xffffffffu, off, i);
+        for (int i = 0; i < boxes; i += 4) {
+          int pg[4], of[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            pg[e] = __shfl_sync(0xffffffffu, pages, (boxes * h + i + e) & 31);
+            of[e] = __shfl_sync(0xffffffffu, offs, (boxes * h + i + e) & 31);
+          }
           if (elected()) {
 #pragma unroll
-            for (int x = 0; x < S::kBlocks; ++x)
-              tma_box(dst + x * kHalf * 128 + i * box_rows * 128, &kmap, 64 * x, u.head, of, pg, full);
+            for (int e = 0; e < 4; ++e) {
+              if (i + e >= boxes) break;
+#pragma unroll
+              for (int x = 0; x < S::kBlocks; ++x)
+                tma_box(dst + x * kHalf * 128 + (i + e) * box_rows * 128, &kmap, 64 * x, head, of[e], pg[e], full);
+            }
           }
           __syncwarp();
         }
@@ -259,7 +324,12 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
           stage = 0;
           par ^= 1;
         }
+        if (h + 1 == count) {
+          more = next_unit();
+          if (more) find();
+        }
       }
+      if (!ok) break;
     }
     if (LV_RARE(bars.bad)) {      // let what is on its way land before the shared memory is given up
       for (long long i = halves < S::kKStages ? 0 : halves - S::kKStages; i < halves; ++i) {
@@ -269,16 +339,16 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       }
     }
   } else if (wid == kWarpQ) {
-    int stage = 0;
+    int stage = 0, issued = 0;
     uint32_t par = 0;
     long long tiles = 0;
     while (ok && next_unit()) {
       const Chunks ch(a, u);
       for (int i = 0; ok && i < ch.count; ++i) {
+        const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
         if (!(ok = bar_wait(&bars, &bars.q_empty[stage], ~par & 1u, a.wait_ns))) break;
         const uint32_t dst = q_s + stage * S::kTile;
         uint64_t* full = &bars.q_full[stage];
-        const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
         if (q_tma) {
           const bool few = rows <= few_rows * a.G;
           if (elected()) {
@@ -318,6 +388,8 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
           if (elected()) bar_arrive(full);
           __syncwarp();
         }
+        ++issued;
+        if (lane == 0) m.issued = issued;
         if (++stage == S::kQStages) {
           stage = 0;
           par ^= 1;
@@ -332,107 +404,119 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       }
     }
   } else if (wid == kWarpMma) {
-    const uint32_t kd0 = desc_low(k_s, 16), qd0 = desc_low(q_s, 16);
-    int ks = 0, qs = 0, buf = 0;
-    uint32_t k_par = 0, q_par = 0, s_par = 0;      // s_par: a bit for (buffer, half)
-    while (ok && next_unit()) {
-      const Chunks ch(a, u);
-      int at[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        at[h] = ks;
-        if (h >= ch.halves) break;
-        if (!(ok = bar_wait(&bars, &bars.k_full[ks], k_par, a.wait_ns))) break;
-        if (++ks == S::kKStages) {
-          ks = 0;
-          k_par ^= 1;
-        }
-      }
-      for (int i = 0; ok && i < ch.count; ++i) {
-        if (!(ok = bar_wait(&bars, &bars.q_full[qs], q_par, a.wait_ns))) break;
-        const int cols = (ch.rows(i) + 15) & ~15;
-        const uint32_t desc = mma_desc<kBf16>(kHalf, cols, false), qd = qd0 + qs * (S::kTile >> 4);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (h >= ch.halves) break;
-          if (!(ok = bar_wait(&bars, &bars.s_empty[buf][h], ~(s_par >> (2 * buf + h)) & 1u, a.wait_ns))) break;
-          s_par ^= 1u << (2 * buf + h);
-          tc_fence_after();
-          if (elected()) {
-            const uint32_t kd = kd0 + at[h] * (S::kTile >> 4);
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-              const uint32_t o = ((k / 4) * (kHalf * 128) + (k % 4) * 32) >> 4;
-              tc_mma_ss(tmem + kCols * (2 * buf + h), kd + o, qd + o, desc, k > 0);
-            }
-            tc_commit(&bars.s_full[buf][h]);
-            if (i + 1 == ch.count) tc_commit(&bars.k_empty[at[h]]);
-            if (h + 1 == ch.halves) tc_commit(&bars.q_empty[qs]);
+    // by one thread (a warp that votes at each wait took some 200 cycles for it, four times a product)
+    if (elected()) {
+      const uint32_t kd0 = desc_low(k_s, 16), qd0 = desc_low(q_s, 16);
+      int ks = 0, qs = 0, buf = 0;
+      uint32_t k_par = 0, q_par = 0, s_par = 0;      // s_par: a bit for (buffer, half)
+      auto products = [&]() -> bool {
+        for (;;) {
+          if (!bar_wait1(&bars, &bars.unit_full[unit_at], unit_par, a.wait_ns)) return false;
+          u = m.units[unit_at];
+          bar_arrive(&bars.unit_empty[unit_at]);
+          if (++unit_at == kUnits) {
+            unit_at = 0;
+            unit_par ^= 1;
           }
-          __syncwarp();
+          if (u.t0 >= u.t1) return true;
+          const Chunks ch(a, u);
+          int at[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            at[h] = ks;
+            if (h >= ch.halves) break;
+            if (!bar_wait1(&bars, &bars.k_full[ks], k_par, a.wait_ns)) return false;
+            if (++ks == S::kKStages) {
+              ks = 0;
+              k_par ^= 1;
+            }
+          }
+          // a product's barriers are asked while the products before it are still being issued: the answers of
+          // three asked one after the other as each is needed took as long as half a product
+          bool q_in = bar_try(&bars.q_full[qs], q_par);
+          bool s_out[2];
+          auto ask = [&](int bf) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              s_out[h] = h >= ch.halves || bar_try(&bars.s_empty[bf][h], ~(s_par >> (2 * bf + h)) & 1u);
+          };
+          ask(buf);
+#pragma unroll 1
+          for (int i = 0; i < ch.count; ++i) {
+            const int cols = (ch.rows(i) + 15) & ~15;
+            const uint32_t desc = mma_desc<kBf16>(kHalf, cols, false), qd = qd0 + qs * (S::kTile >> 4);
+            const int q_now = qs;
+            if (LV_RARE(!q_in) && !bar_wait_slow(&bars, &bars.q_full[qs], q_par, a.wait_ns)) return false;
+            if (++qs == S::kQStages) {
+              qs = 0;
+              q_par ^= 1;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (h >= ch.halves) break;
+              if (LV_RARE(!s_out[h]) &&
+                  !bar_wait_slow(&bars, &bars.s_empty[buf][h], ~(s_par >> (2 * buf + h)) & 1u, a.wait_ns))
+                return false;
+              s_par ^= 1u << (2 * buf + h);
+              tc_fence_after();
+              const uint32_t kd = kd0 + at[h] * (S::kTile >> 4);
+#pragma unroll
+              for (int k = 0; k < DP / 16; ++k) {
+                const uint32_t o = ((k / 4) * (kHalf * 128) + (k % 4) * 32) >> 4;
+                tc_mma_ss(tmem + kCols * (2 * buf + h), kd + o, qd + o, desc, k > 0);
+              }
+              tc_commit(&bars.s_full[buf][h]);
+              if (i + 1 == ch.count) tc_commit(&bars.k_empty[at[h]]);
+              if (h + 1 == ch.halves) tc_commit(&bars.q_empty[q_now]);
+              if (h == 0 && i + 1 < ch.count) q_in = bar_try(&bars.q_full[qs], q_par);
+            }
+            buf ^= 1;
+            if (i + 1 < ch.count) ask(buf);
+          }
         }
-        buf ^= 1;
-        if (++qs == S::kQStages) {
-          qs = 0;
-          q_par ^= 1;
-        }
+      };
+      if (!products()) {      // let the products under way end
+        tc_commit(&bars.drain);
+        const unsigned long long t0 = now_ns();
+        while (!bar_try(&bars.drain, 0))
+          if ((long long)(now_ns() - t0) > a.wait_ns) break;
       }
     }
-    if (LV_RARE(bars.bad)) {      // let the products under way end
-      if (elected()) tc_commit(&bars.drain);
-      const unsigned long long t0 = now_ns();
-      while (!bar_try(&bars.drain, 0))
-        if ((long long)(now_ns() - t0) > a.wait_ns) break;
-      __syncwarp();
-    }
-  } else if (wid == kWarpRows) {
-    uint32_t par = 0;      // a bit a buffer
-    int buf = 0;
-    const int Hq = a.H * a.G;
-    while (ok && next_unit()) {
-      const Chunks ch(a, u);
-      for (int i = 0; ok && i < ch.count; ++i) {
-        const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
-        float b[kCols / 32];
-#pragma unroll
-        for (int k = 0; k < kCols / 32; ++k) {
-          const int c = 32 * k + lane, R = R0 + c, token = R / a.G;
-          float z = -INFINITY;
-          if (c < rows && counts(a, u.g, n, token))
-            z = a.lse[(int64_t)(u.g.qrow + token) * Hq + u.head * a.G + (R - token * a.G)];
-          b[k] = z == -INFINITY ? z : -z * kLog2e;
-        }
-        if (!(ok = bar_wait(&bars, &bars.b_empty[buf], ~(par >> buf) & 1u, a.wait_ns))) break;
-        par ^= 1u << buf;
-#pragma unroll
-        for (int k = 0; k < kCols / 32; ++k) m.b[buf][32 * k + lane] = b[k];
-        warp_arrive(&bars.b_full[buf]);
-        buf ^= 1;
-      }
-    }
+    __syncwarp();
   } else {
+    // Units are taken when few products of those before are left to be issued: a CTA that held long ones ahead
+    // would end last.  Short ones come four at a time until few are left, a lane finding each, as a
+    // ticket and its unit take some two microseconds and the copies of one 1.4.
     int at = 0;
     uint32_t par = 0;
-    int t = blockIdx.x, following = 0;
-    auto ask = [&]() {
-      if (lane == 0) following = gridDim.x + atomicAdd(&a.tickets[0], 1);
-    };
-    for (;;) {
-      ask();
+    int handed = 0;
+    const bool brief = (long long)m.index.most * a.G <= 2 * kCols;
+    int taken = 0;
+    for (bool end = false; !end;) {
+      while (handed - m.issued > kAhead && !bars.bad) __nanosleep(100);
+      const int batch = brief && units - taken > 8 * (int)gridDim.x ? 4 : 1;
+      int t = 0;
+      if (lane == 0) t = atomicAdd(&a.tickets[0], batch);
+      taken = __shfl_sync(0xffffffffu, t, 0);
+      t = taken + lane;
       Unit x{};
-      if (t < units) x = find_unit<kIndexThreads, kUnitKeys>(a, step, m.index, t);
-      const bool end = t >= units;
-      if (end || x.t0 < x.t1) {
-        if (!bar_wait(&bars, &bars.unit_empty[at], ~par & 1u, a.wait_ns)) break;
-        if (lane == 0) m.units[at] = x;
+      if (lane < batch && t < units) x = find_unit<kIndexThreads, kUnitKeys>(a, step, m.index, t);
+      end = taken + batch > units || units == 0;
+      int products = x.t0 < x.t1 ? Chunks(a, x).count : 0;
+      for (int j = 0; j <= batch; ++j) {      // (the last: the end, where it is)
+        const bool marker = j == batch;
+        const int some = marker ? (int)end : __shfl_sync(0xffffffffu, products, j & 31);
+        if (!some) continue;
+        if (!(ok = bar_wait(&bars, &bars.unit_empty[at], ~par & 1u, a.wait_ns))) break;
+        if (lane == (marker ? 0 : j)) m.units[at] = marker ? Unit{} : x;
         warp_arrive(&bars.unit_full[at]);
+        handed += marker ? 0 : some;
         if (++at == kUnits) {
           at = 0;
           par ^= 1;
         }
       }
-      if (end) break;
-      t = __shfl_sync(0xffffffffu, following, 0);
+      if (!ok || bars.bad) break;
     }
     // the last CTA that has taken its last unit sets the counters back
     if (lane == 0) {
