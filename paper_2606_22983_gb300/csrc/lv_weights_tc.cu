@@ -22,8 +22,8 @@ template <int DP>
 struct WShape {
   static constexpr int kBlocks = DP / 64;                  // 128-byte wide column blocks
   static constexpr int kTile = kHalf * DP * 2;             // bytes of half a unit's K, and of a tile of queries
-  static constexpr int kKStages = DP == 128 ? 3 : 6;
-  static constexpr int kQStages = DP == 128 ? 3 : 4;
+  static constexpr int kKStages = DP == 128 ? 4 : 6;
+  static constexpr int kQStages = DP == 128 ? 2 : 4;
   static constexpr int kQ = kKStages * kTile;
   static constexpr int kMisc = kQ + kQStages * kTile;
 };
@@ -73,8 +73,8 @@ struct Chunks {
 // One CTA an SM; units are taken in order from a counter, long ones (the first keys of a context, which
 // all rows see) first.
 //   warp 19  finds units ahead
-//   warp 16  K of a unit into a ring of shared memory, by TMA: a box a page and 64 columns
-//   warp 17  queries into a ring of their own, by TMA
+//   warp 16  K of a unit's first half into a ring of shared memory, by TMA: a box a page and 64 columns
+//   warp 17  K of its second half, and queries into a ring of their own
 //   warp 18  products into two buffers of TMEM for each half
 //   0 .. 15  the rows' terms, exponentials and sums, a thread a key in every second product
 template <int DP, bool kBf16>
@@ -156,6 +156,61 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
     return u.t0 < u.t1;
   };
 
+  // K of a half of each unit, for a warp: lane i finds the page of box i of its keys; one thread then issues the
+  // copies.  (Half the 64 boxes of a unit of 16-token pages took 1200 cycles to issue, by one warp all of them 2400,
+  // which is nearly what their bytes take.)
+  struct KHalf {
+    int of, slot, page, off;      // which half; tiles of K before it
+  } k_half{0, 0, -1, 0};
+  const int boxes = kHalf / box_rows;
+  auto find = [&](KHalf& x) {
+    const int key = u.key0 + kHalf * x.of + lane * box_rows;
+    const int32_t* table = u.g.req < 0 ? a.pool_table + (size_t)u.g.sid * a.maxB : a.tables + (size_t)u.g.req * a.maxB;
+    const int b = a.t_shift >= 0 ? key >> a.t_shift : key / a.T;
+    x.off = key - b * a.T;
+    x.page = lane < boxes && key < u.g.keys ? table[b] : -1;
+  };
+  auto load = [&](KHalf& x, const Unit& v, int page, int off) -> bool {
+    const int halves = v.g.keys - v.key0 > kHalf ? 2 : 1;
+    if (x.of < halves) {
+      const int at = x.slot + x.of, stage = at % S::kKStages;
+      if (!bar_wait(&bars, &bars.k_empty[stage], ~(at / S::kKStages) & 1u, a.wait_ns)) return false;
+      if ((uint32_t)page >= a.hbm_pages) page = (int)a.hbm_pages;      // none: outside the array, zeros
+      uint64_t* full = &bars.k_full[stage];
+      const uint32_t dst = k_s + stage * S::kTile;
+      if (elected()) bar_expect(full, S::kTile);
+#pragma unroll 1
+      for (int i = 0; i < boxes; i += 4) {
+        int pg[4], of[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pg[e] = __shfl_sync(0xffffffffu, page, (i + e) & 31);
+          of[e] = __shfl_sync(0xffffffffu, off, (i + e) & 31);
+        }
+        if (elected()) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (i + e >= boxes) break;
+#pragma unroll
+            for (int y = 0; y < S::kBlocks; ++y)
+              tma_box(dst + y * kHalf * 128 + (i + e) * box_rows * 128, &kmap, 64 * y, v.head, of[e], pg[e], full);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    x.slot += halves;
+    return true;
+  };
+  // after a wait that ran out: what is on its way lands before the shared memory is given up
+  auto drain = [&](const KHalf& x) {
+    for (int i = max(0, x.slot - S::kKStages); i < x.slot; ++i) {
+      const unsigned long long t0 = now_ns();
+      while (!bar_try(&bars.k_full[i % S::kKStages], (uint32_t)(i / S::kKStages) & 1u))
+        if ((long long)(now_ns() - t0) > a.wait_ns) break;
+    }
+  };
+
   if (wid < kSumWarps) {
     const int buf = wid >> 3, half = wid >> 2 & 1, row = threadIdx.x & 127;
     // this warp's 32 lanes of its buffer and half in TMEM
@@ -165,9 +220,13 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
     int turn = 0;           // the buffer of the next product
     const int Hq = a.H * a.G;
     float* const b = m.b[wid];
-    int in_col[kCols / 32];      // tokens before this lane's columns in a product
+    int in_col[kCols / 32];      // where the sums of this lane's columns lie, from a product's first
 #pragma unroll
-    for (int k = 0; k < kCols / 32; ++k) in_col[k] = (32 * k + lane) / a.G;
+    for (int k = 0; k < kCols / 32; ++k) {
+      const int c = 32 * k + lane, token = c / a.G;
+      in_col[k] = token * Hq + c - token * a.G;
+    }
+    const int step_words = a.G > kCols ? 0 : kCols / a.G * Hq;      // and the next product's
     while (ok && next_unit()) {
       const Chunks ch(a, u);
       const int key = u.key0 + kHalf * half + row;
@@ -178,26 +237,31 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       float* w = a.w + u.g.sid * a.w_session + u.head * a.w_head + key;
       const float before = mine && writes ? *w : 0.f;
       // the packed rows that see the key: from its own position on, to the window's end
-      const long long from = u.g.req < 0 ? 0 : (long long)(key - u.g.first) * a.G;
-      const long long to = u.g.req < 0 || a.window == 0 || key < a.sinks ? 1ll << 40 : from + (long long)a.window * a.G;
-      const bool check_b = u.g.req < 0 && a.last > 0;
+      const bool all_see = u.g.req < 0, no_end = all_see || a.window == 0 || key < a.sinks, check_b = all_see && a.last > 0;
+      const long long from = all_see ? 0 : (long long)(key - u.g.first) * a.G;
+      // a product whose rows lie between these all see all keys of the half
+      const int key_lo = u.key0 + kHalf * half, key_hi = key_lo + kHalf - 1;
+      const long long open_lo = all_see ? 0 : (long long)(key_hi - u.g.first) * a.G;
+      const long long open_hi = all_see || a.window == 0 || key_hi < a.sinks ? 1ll << 40
+                                : (long long)(key_lo - u.g.first + a.window) * a.G;
       LongSum all;
       // the sums of four columns' rows, asked for a product ahead
       float z[kCols / 32];
-      const int tokens = ch.step / a.G;
+      const float* const lse = a.lse + (int64_t)(u.g.qrow + u.t0) * Hq + u.head * a.G;
       auto ask = [&](int i) {
+        const int rows = i < ch.count ? ch.rows(i) : 0;
+        const float* at = lse + (int64_t)i * step_words;
 #pragma unroll
         for (int k = 0; k < kCols / 32; ++k) {
           z[k] = -INFINITY;
           const int c = 32 * k + lane;
-          if (i >= ch.count || c >= ch.rows(i)) continue;
-          int token = u.t0 + i * tokens + in_col[k], hq = u.head * a.G + c - in_col[k] * a.G;
-          if (a.G > kCols) {      // (a product does not begin at a token's first head)
-            const int R = ch.begin + i * ch.step + c;
-            token = R / a.G;
-            hq = u.head * a.G + R - token * a.G;
+          if (c >= rows) continue;
+          if (a.G > kCols || check_b) {      // (a product need not begin at a token's first head; rows that do not count)
+            const int R = ch.begin + i * ch.step + c, token = R / a.G;
+            if (counts(a, u.g, n, token)) z[k] = lse[(int64_t)(token - u.t0) * Hq + (R - token * a.G)];
+          } else {
+            z[k] = at[in_col[k]];
           }
-          if (!check_b || counts(a, u.g, n, token)) z[k] = a.lse[(int64_t)(u.g.qrow + token) * Hq + hq];
         }
       };
       if (there) ask(turn ^ buf);
@@ -211,17 +275,16 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
           s_par ^= 1;
           tc_fence_after();
           const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
-          const int c_lo = clamp_col(from - R0), c_hi = mine ? min(rows, clamp_col(to - R0)) : 0;
           float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
-          const bool full = c_lo == 0 && c_hi == kCols && !check_b, all_full = __all_sync(0xffffffffu, full);
+          if (rows == kCols && R0 >= open_lo && R0 + kCols <= open_hi && !check_b) {
+            // (keys past the end have sums of whatever the page holds, which nobody takes)
 #pragma unroll 1
-          for (int c0 = 0; c0 < rows; c0 += 32) {
-            uint32_t x[32];
-            tc_ld32(x, s_at + c0);
-            const float* s = reinterpret_cast<const float*>(x);
-            if (all_full) {
+            for (int c0 = 0; c0 < kCols; c0 += 32) {
+              uint32_t x[32];
+              tc_ld32(x, s_at + c0);
               tc_wait_ld();
               tc_loaded<32>(x);
+              const float* s = reinterpret_cast<const float*>(x);
 #pragma unroll
               for (int j = 0; j < 32; j += 4) {
                 const float4 bb = *reinterpret_cast<const float4*>(b + c0 + j);
@@ -234,12 +297,20 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
                 acc0 = add2(acc0, y0);
                 acc1 = add2(acc1, y1);
               }
-            } else {
+            }
+          } else {
+            const int c_lo = clamp_col(from - R0);
+            const int c_hi = !mine ? 0 : no_end ? rows : min(rows, clamp_col(from + (long long)a.window * a.G - R0));
+#pragma unroll 1
+            for (int c0 = 0; c0 < rows; c0 += 32) {
               uint32_t seen = low_bits(c_hi - c0) & ~low_bits(c_lo - c0);
               if (check_b) seen &= __ballot_sync(0xffffffffu, b[c0 + lane] != -INFINITY);
+              if (!__any_sync(0xffffffffu, seen != 0)) continue;
+              uint32_t x[32];
+              tc_ld32(x, s_at + c0);
               tc_wait_ld();
               tc_loaded<32>(x);
-              if (!__any_sync(0xffffffffu, seen != 0)) continue;
+              const float* s = reinterpret_cast<const float*>(x);
 #pragma unroll
               for (int j = 0; j < 32; j += 2) {
                 const float2 bb = *reinterpret_cast<const float2*>(b + c0 + j);
@@ -275,75 +346,27 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
     }
     tc_fence_before();
   } else if (wid == kWarpK) {
-    // lane i finds the page of box i of a unit's keys, before the unit before it is done; one thread then
-    // issues the copies
-    const int boxes = kHalf / box_rows;      // of a half
-    int stage = 0;
-    uint32_t par = 0;
-    long long halves = 0;
-    int page = 0, off = 0;
-    auto find = [&]() {
-      const int key = u.key0 + lane * box_rows;
-      const int32_t* table = u.g.req < 0 ? a.pool_table + (size_t)u.g.sid * a.maxB : a.tables + (size_t)u.g.req * a.maxB;
-      const int b = a.t_shift >= 0 ? key >> a.t_shift : key / a.T;
-      off = key - b * a.T;
-      page = lane < 2 * boxes && key < u.g.keys ? table[b] : -1;
-    };
+    k_half.of = 0;
     bool more = next_unit();
-    if (more) find();
+    if (more) find(k_half);
     while (more) {
-      const int head = u.head, count = u.g.keys - u.key0 > kHalf ? 2 : 1;
-      const int pages = (uint32_t)page < a.hbm_pages ? page : (int)a.hbm_pages;      // none: outside the array, zeros
-      const int offs = off;
-      for (int h = 0; ok && h < count; ++h) {
-        if (!(ok = bar_wait(&bars, &bars.k_empty[stage], ~par & 1u, a.wait_ns))) break;
-        uint64_t* full = &bars.k_full[stage];
-        const uint32_t dst = k_s + stage * S::kTile;
-        if (elected()) bar_expect(full, S::kTile);
-#pragma unroll 1
-        for (int i = 0; i < boxes; i += 4) {
-          int pg[4], of[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            pg[e] = __shfl_sync(0xffffffffu, pages, (boxes * h + i + e) & 31);
-            of[e] = __shfl_sync(0xffffffffu, offs, (boxes * h + i + e) & 31);
-          }
-          if (elected()) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (i + e >= boxes) break;
-#pragma unroll
-              for (int x = 0; x < S::kBlocks; ++x)
-                tma_box(dst + x * kHalf * 128 + (i + e) * box_rows * 128, &kmap, 64 * x, head, of[e], pg[e], full);
-            }
-          }
-          __syncwarp();
-        }
-        ++halves;
-        if (++stage == S::kKStages) {
-          stage = 0;
-          par ^= 1;
-        }
-        if (h + 1 == count) {
-          more = next_unit();
-          if (more) find();
-        }
-      }
-      if (!ok) break;
+      const Unit now = u;
+      // (the next unit's pages are looked up before this one's copies may wait)
+      const int page = k_half.page, off = k_half.off;
+      if (!(ok = load(k_half, now, page, off))) break;
+      more = next_unit();
+      if (more) find(k_half);
     }
-    if (LV_RARE(bars.bad)) {      // let what is on its way land before the shared memory is given up
-      for (long long i = halves < S::kKStages ? 0 : halves - S::kKStages; i < halves; ++i) {
-        const unsigned long long t0 = now_ns();
-        while (!bar_try(&bars.k_full[i % S::kKStages], (uint32_t)(i / S::kKStages) & 1u))
-          if ((long long)(now_ns() - t0) > a.wait_ns) break;
-      }
-    }
+    if (LV_RARE(bars.bad)) drain(k_half);
   } else if (wid == kWarpQ) {
     int stage = 0, issued = 0;
     uint32_t par = 0;
     long long tiles = 0;
+    k_half.of = 1;
     while (ok && next_unit()) {
       const Chunks ch(a, u);
+      find(k_half);
+      if (!(ok = load(k_half, u, k_half.page, k_half.off))) break;
       for (int i = 0; ok && i < ch.count; ++i) {
         const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
         if (!(ok = bar_wait(&bars, &bars.q_empty[stage], ~par & 1u, a.wait_ns))) break;
@@ -396,6 +419,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
         }
       }
     }
+    if (LV_RARE(bars.bad)) drain(k_half);
     if (LV_RARE(bars.bad) && q_tma) {
       for (long long i = tiles < S::kQStages ? 0 : tiles - S::kQStages; i < tiles; ++i) {
         const unsigned long long t0 = now_ns();
