@@ -76,6 +76,7 @@ struct Unit {
   Segment g;
   int head, key0;
   int t0, t1;                  // tokens [t0, t1) of the segment see some of its keys
+  int products;                // the tensor-core kernel's
 };
 
 // Units are taken in kClasses goes, those that most rows see first, so that no long one begins last: a
@@ -106,7 +107,7 @@ __device__ __forceinline__ Segment segment_of(const WeightArgs& a, int n, int s)
 // Which tokens of g see keys of [key0, key0 + keys): those from the first key's position on, and under a
 // window up to where it has left the last one.
 __device__ __forceinline__ Unit unit_of(const WeightArgs& a, const Segment& g, int head, int key0, int keys) {
-  Unit u{g, head, key0, 0, g.tokens};
+  Unit u{g, head, key0, 0, g.tokens, 0};
   if (g.req < 0) return u;
   if (a.last > 0) u.t0 = max(0, g.tokens - a.last);
   u.t0 = max(u.t0, key0 - g.first);

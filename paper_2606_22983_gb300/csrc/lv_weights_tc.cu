@@ -1,5 +1,7 @@
 // Attention weights added up for the cached tokens, on the fifth-generation tensor cores (lv_weights.cuh has
 // how the work is cut).
+#include <climits>
+
 #include "lv_tc.cuh"
 #include "lv_weights.cuh"
 
@@ -51,18 +53,13 @@ static_assert(WShape<64>::kMisc + sizeof(Misc) <= 227 * 1024, "shared memory of 
 
 // The n lowest bits, all of them from 32 on, none below 1.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
-__device__ __forceinline__ int clamp_col(long long x) { return (int)(x < 0 ? 0 : x > kCols ? kCols : x); }
+__device__ __forceinline__ int clamp_col(int x) { return min(max(x, 0), kCols); }
 
 // A unit's products: its packed rows [begin, end) in tiles of `step`.
 struct Chunks {
   int begin, end, step, count, halves;
-  __device__ __forceinline__ Chunks(const WeightArgs& a, const Unit& u) {
-    begin = u.t0 * a.G;
-    end = u.t1 * a.G;
-    step = a.G > kCols ? kCols : kCols / a.G * a.G;
-    count = (end - begin + step - 1) / step;
-    halves = u.g.keys - u.key0 > kHalf ? 2 : 1;
-  }
+  __device__ __forceinline__ Chunks(const WeightArgs& a, const Unit& u, int step_)
+      : begin(u.t0 * a.G), end(u.t1 * a.G), step(step_), count(u.products), halves(u.g.keys - u.key0 > kHalf ? 2 : 1) {}
   __device__ __forceinline__ int rows(int i) const { return min(step, end - begin - i * step); }
 };
 
@@ -139,6 +136,8 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
   const int units = fits ? index_segments<kIndexThreads, kUnitKeys>(a, step, m.index, reinterpret_cast<int*>(dyn)) : 0;
   fence_async();
   __syncthreads();
+
+  const int step_rows = a.G > kCols ? kCols : kCols / a.G * a.G;
 
   // the units of the CTA in order, for a role: false at the end or where a wait ran out
   int unit_at = 0;
@@ -227,56 +226,67 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       in_col[k] = token * Hq + c - token * a.G;
     }
     const int step_words = a.G > kCols ? 0 : kCols / a.G * Hq;      // and the next product's
+    // the sums of four columns' rows, asked for a product ahead
+    float z[kCols / 32];
+    bool asked = false;      // for the unit to come
+    auto ask = [&](const Unit& v, const Chunks& c_of, int i) {
+      const int rows = i < c_of.count ? c_of.rows(i) : 0;
+      const float* const lse = a.lse + (int64_t)(v.g.qrow + v.t0) * Hq + v.head * a.G;
+      const float* at = lse + (int64_t)i * step_words;
+      const bool odd = a.G > kCols || (v.g.req < 0 && a.last > 0);
+#pragma unroll
+      for (int k = 0; k < kCols / 32; ++k) {
+        z[k] = -INFINITY;
+        const int c = 32 * k + lane;
+        if (c >= rows) continue;
+        if (odd) {      // (a product need not begin at a token's first head; rows that do not count)
+          const int R = c_of.begin + i * c_of.step + c, token = R / a.G;
+          if (counts(a, v.g, n, token)) z[k] = lse[(int64_t)(token - v.t0) * Hq + (R - token * a.G)];
+        } else {
+          z[k] = at[in_col[k]];
+        }
+      }
+    };
     while (ok && next_unit()) {
-      const Chunks ch(a, u);
+      const Chunks ch(a, u, step_rows);
       const int key = u.key0 + kHalf * half + row;
       const bool there = half < ch.halves, mine = key < u.g.keys;
-      // the unit's sums are those of the first buffer's threads, which add the second's; a unit of one
-      // product is its buffer's alone
-      const bool writes = ch.count > 1 ? buf == 0 : buf == turn, joins = ch.count > 1;
+      // the threads of the unit's last product write; those of the other buffer, which have the products before
+      // it and every second one from there, leave theirs
+      const int next_turn = turn ^ (ch.count & 1);
+      const bool joins = ch.count > 1, writes = buf != next_turn;
       float* w = a.w + u.g.sid * a.w_session + u.head * a.w_head + key;
-      const float before = mine && writes ? *w : 0.f;
       // the packed rows that see the key: from its own position on, to the window's end
       const bool all_see = u.g.req < 0, no_end = all_see || a.window == 0 || key < a.sinks, check_b = all_see && a.last > 0;
-      const long long from = all_see ? 0 : (long long)(key - u.g.first) * a.G;
+      auto row_of = [&](long long token) { return (int)(token < 0 ? 0 : token > u.g.tokens ? u.g.tokens : token) * a.G; };
+      const int from = all_see ? 0 : row_of((long long)key - u.g.first);
       // a product whose rows lie between these all see all keys of the half
       const int key_lo = u.key0 + kHalf * half, key_hi = key_lo + kHalf - 1;
-      const long long open_lo = all_see ? 0 : (long long)(key_hi - u.g.first) * a.G;
-      const long long open_hi = all_see || a.window == 0 || key_hi < a.sinks ? 1ll << 40
-                                : (long long)(key_lo - u.g.first + a.window) * a.G;
+      const int open_lo = all_see ? 0 : row_of((long long)key_hi - u.g.first);
+      const int open_hi = all_see || a.window == 0 || key_hi < a.sinks ? INT_MAX : row_of((long long)key_lo - u.g.first + a.window);
       LongSum all;
-      // the sums of four columns' rows, asked for a product ahead
-      float z[kCols / 32];
-      const float* const lse = a.lse + (int64_t)(u.g.qrow + u.t0) * Hq + u.head * a.G;
-      auto ask = [&](int i) {
-        const int rows = i < ch.count ? ch.rows(i) : 0;
-        const float* at = lse + (int64_t)i * step_words;
-#pragma unroll
-        for (int k = 0; k < kCols / 32; ++k) {
-          z[k] = -INFINITY;
-          const int c = 32 * k + lane;
-          if (c >= rows) continue;
-          if (a.G > kCols || check_b) {      // (a product need not begin at a token's first head; rows that do not count)
-            const int R = ch.begin + i * ch.step + c, token = R / a.G;
-            if (counts(a, u.g, n, token)) z[k] = lse[(int64_t)(token - u.t0) * Hq + (R - token * a.G)];
-          } else {
-            z[k] = at[in_col[k]];
-          }
-        }
-      };
-      if (there) ask(turn ^ buf);
+      if (!asked && there) ask(u, ch, turn ^ buf);
+      asked = false;
       for (int i = turn ^ buf; i < ch.count; i += 2) {
         if (there) {
 #pragma unroll
           for (int k = 0; k < kCols / 32; ++k) b[32 * k + lane] = z[k] == -INFINITY ? z[k] : -z[k] * kLog2e;
           __syncwarp();
-          ask(i + 2);
+          if (i + 2 < ch.count) {
+            ask(u, ch, i + 2);
+          } else if (__all_sync(0xffffffffu, bar_try(&bars.unit_full[unit_at], unit_par))) {
+            // the next unit's first ones, where it is known: they would be waited for at its begin
+            const Unit v = m.units[unit_at];
+            const Chunks next(a, v, step_rows);
+            asked = v.t0 < v.t1 && half < next.halves;
+            if (asked) ask(v, next, turn ^ (ch.count & 1) ^ buf);
+          }
           if (!(ok = bar_wait(&bars, &bars.s_full[buf][half], s_par, a.wait_ns))) break;
           s_par ^= 1;
           tc_fence_after();
           const int R0 = ch.begin + i * ch.step, rows = ch.rows(i);
           float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
-          if (rows == kCols && R0 >= open_lo && R0 + kCols <= open_hi && !check_b) {
+          if (rows == kCols && R0 >= open_lo && R0 <= open_hi - kCols && !check_b) {
             // (keys past the end have sums of whatever the page holds, which nobody takes)
 #pragma unroll 1
             for (int c0 = 0; c0 < kCols; c0 += 32) {
@@ -300,7 +310,8 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
             }
           } else {
             const int c_lo = clamp_col(from - R0);
-            const int c_hi = !mine ? 0 : no_end ? rows : min(rows, clamp_col(from + (long long)a.window * a.G - R0));
+            const int c_hi = !mine ? 0 : no_end ? rows
+                             : min(rows, clamp_col(row_of((long long)key - u.g.first + a.window) - R0));
 #pragma unroll 1
             for (int c0 = 0; c0 < rows; c0 += 32) {
               uint32_t seen = low_bits(c_hi - c0) & ~low_bits(c_lo - c0);
@@ -327,22 +338,24 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
           all.add(acc0.x + acc0.y);
         }
       }
-      turn ^= ch.count & 1;
+      turn = next_turn;
       if (!ok) break;
+      float sum = all.sum;
       if (joins) {
         float* part = m.part + kHalf * half + row;
-        if (buf == 1) {
+        if (!writes) {
           if (!(ok = bar_wait(&bars, &bars.part_empty, ~part_par & 1u, a.wait_ns))) break;
-          *part = all.sum;
+          *part = sum;
           warp_arrive(&bars.part_full);
         } else {
           if (!(ok = bar_wait(&bars, &bars.part_full, part_par, a.wait_ns))) break;
-          all.add(*part);
+          sum += *part;      // (the same whichever of the two is whose)
           warp_arrive(&bars.part_empty);
         }
         part_par ^= 1;
       }
-      if (writes && mine && all.sum != 0.f) *w = before + all.sum;
+      // (one addition to the word in this call; nothing waits for it)
+      if (writes && mine && sum != 0.f) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(w), "f"(sum) : "memory");
     }
     tc_fence_before();
   } else if (wid == kWarpK) {
@@ -364,7 +377,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
     long long tiles = 0;
     k_half.of = 1;
     while (ok && next_unit()) {
-      const Chunks ch(a, u);
+      const Chunks ch(a, u, step_rows);
       find(k_half);
       if (!(ok = load(k_half, u, k_half.page, k_half.off))) break;
       for (int i = 0; ok && i < ch.count; ++i) {
@@ -443,7 +456,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
             unit_par ^= 1;
           }
           if (u.t0 >= u.t1) return true;
-          const Chunks ch(a, u);
+          const Chunks ch(a, u, step_rows);
           int at[2];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -526,7 +539,8 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       Unit x{};
       if (lane < batch && t < units) x = find_unit<kIndexThreads, kUnitKeys>(a, step, m.index, t);
       end = taken + batch > units || units == 0;
-      int products = x.t0 < x.t1 ? Chunks(a, x).count : 0;
+      const int products = x.t0 < x.t1 ? ((x.t1 - x.t0) * a.G + step_rows - 1) / step_rows : 0;
+      x.products = products;
       for (int j = 0; j <= batch; ++j) {      // (the last: the end, where it is)
         const bool marker = j == batch;
         const int some = marker ? (int)end : __shfl_sync(0xffffffffu, products, j & 31);
