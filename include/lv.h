@@ -719,7 +719,7 @@ lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* fir
    or no tokens: no prefix), as if they came before its own.  positions count from the prefix's begin;
    kv_lens, tables and slots are of the request's own session.  Requests that follow one another and
    continue the same tokens of the same session read them once, for all their rows and heads together.
-   lv_attention works on such a step in two launches.  Device-detected, with the request left out:
+   lv_attention works on such a step in two or three launches.  Device-detected, with the request left out:
    LV_ERR_BOUNDS for a prefix's session id or length out of range, LV_ERR_STATE for a block of it that
    is not in HBM; it must stay where it is until the step's last call.  LV_ERR_INVALID for a batch
    without room for num_tokens rows.  A captured lv_attention also keeps whether the plan before its capture was given

@@ -2157,6 +2157,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.pre_kind = b->pre_kind;
   a.pre_o = b->pre_o;
   a.pre_ml = b->pre_ml;
+  a.pre_rows = (int64_t)b->share_rows * b->G;
   lv::AttnArgs x = a;      // over the prefixes, by the pool's tables
   x.tables = pool->d.table;
   x.tiles = b->pre_tiles;
@@ -2164,6 +2165,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   x.head = b->pre_head;
   x.tile_rows = tile_rows(b->pre_kind);
   LV_TRY(launch(x, b->pre_kind, b->pre_ctas, lv::kPrefix));
+  if (b->pre_kind == lv::ATTN_TC) LV_TRY(lv::launch_join_prefixes(x, pool->num_sms, s));
   LV_TRY(launch(a, b->kind, b->ctas, lv::kJoined));
   return LV_OK;
 }

@@ -145,7 +145,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
     const int h = head * a.G + g;
     const bool joined = kMode == kJoined && kLast && t.req >= kSharedTile;
     float2 pre = make_float2(-INFINITY, 0.f);
-    if (joined) pre = __ldcg(&a.pre_ml[r * (a.H * a.G) + h]);
+    if (joined) pre = *pre_ml_at(a, head, r, g);
     float top = pre.x;
     for (int i = lane; i < count; i += 32) top = fmaxf(top, __ldcg(&a.part_ml[at(i)]).x);
 #pragma unroll
@@ -189,19 +189,21 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
       continue;
     }
     if constexpr (kMode == kPrefix) {
-      float* o = a.pre_o + (r * (a.H * a.G) + h) * DP + kCols * lane;
 #pragma unroll
-      for (int e = 0; e < kCols; e += 2) *reinterpret_cast<float2*>(o + e) = make_float2(acc[e], acc[e + 1]);
-      if (lane == 0) a.pre_ml[r * (a.H * a.G) + h] = make_float2(top, sum);
+      for (int e = 0; e < kCols; e += 2) {
+        const int col = kCols * lane + e;
+        reinterpret_cast<float2*>(pre_at(a, head, col, r, g))[col / 2 & 1] = make_float2(acc[e], acc[e + 1]);
+      }
+      if (lane == 0) *pre_ml_at(a, head, r, g) = make_float2(top, sum);
       continue;
     }
     if (joined) {
       const float f = pre.x == top ? 1.f : exp2_fast(pre.x - top);
-      const float* o = a.pre_o + (r * (a.H * a.G) + h) * DP + kCols * lane;
       sum += pre.y * f;
 #pragma unroll
       for (int e = 0; e < kCols; e += 2) {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(o + e));
+        const int col = kCols * lane + e;
+        const float2 v = reinterpret_cast<const float2*>(pre_at(a, head, col, r, g))[col / 2 & 1];
         acc[e] += v.x * f;
         acc[e + 1] += v.y * f;
       }
@@ -571,21 +573,20 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
           const int64_t r = C.t.qrow + token;
           const int h = head * a.G + g;
           if constexpr (kMode == kPrefix) {
-            float* po = a.pre_o + (r * (a.H * a.G) + h) * DP;
 #pragma unroll
             for (int d = 0; d < DP / 8; ++d)
-              *reinterpret_cast<float2*>(po + 8 * d + 2 * (lane & 3)) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
-            if ((lane & 3) == 0) a.pre_ml[r * (a.H * a.G) + h] = make_float2(top[i], sum[i]);
+              reinterpret_cast<float2*>(pre_at(a, head, 8 * d + 2 * (lane & 3), r, g))[lane & 1] =
+                  make_float2(o[d][2 * i], o[d][2 * i + 1]);
+            if ((lane & 3) == 0) *pre_ml_at(a, head, r, g) = make_float2(top[i], sum[i]);
             continue;
           }
           if (kMode == kJoined && C.t.req >= kSharedTile) {
-            const float2 pre = __ldcg(&a.pre_ml[r * (a.H * a.G) + h]);
-            const float* po = a.pre_o + (r * (a.H * a.G) + h) * DP + 2 * (lane & 3);
+            const float2 pre = *pre_ml_at(a, head, r, g);
             const float2 f = join_factors(top[i], pre, &top[i]);
             sum[i] = sum[i] * f.x + pre.y * f.y;
 #pragma unroll
             for (int d = 0; d < DP / 8; ++d) {
-              const float2 v = __ldcg(reinterpret_cast<const float2*>(po + 8 * d));
+              const float2 v = reinterpret_cast<const float2*>(pre_at(a, head, 8 * d + 2 * (lane & 3), r, g))[lane & 1];
               o[d][2 * i] = o[d][2 * i] * f.x + v.x * f.y;
               o[d][2 * i + 1] = o[d][2 * i + 1] * f.x + v.y * f.y;
             }

@@ -49,18 +49,18 @@ __device__ __forceinline__ float4* part_at(const AttnArgs& a, int64_t slot, int 
 // the output, or (not last) to the first of the pieces' own slots.
 template <int DP, bool kBf16, int kMode>
 __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int p0, int step, int count, bool last,
-                                          int row, bool mine, bool shared, uint16_t* out, int64_t r, int hq) {
+                                          int row, bool mine, bool shared, uint16_t* out, int64_t r, int head, int g) {
+  const int hq = head * a.G + g;
   auto slot = [&](int i) {
     const int p = p0 + min(i, count - 1) * step;
     return part_slot(first + p, p == 0);
   };
   auto ml_of = [&](int i) { return __ldcg(&a.part_ml[slot(i) * a.tile_rows + row]); };
-  const int64_t at_pre = r * (a.H * a.G) + hq;
   const bool joined = kMode == kJoined && shared && last;
   float top = -INFINITY, sum = 0.f;
   if (mine) {
     float2 pre = make_float2(-INFINITY, 0.f);
-    if (joined) pre = __ldcg(&a.pre_ml[at_pre]);
+    if (joined) pre = *pre_ml_at(a, head, r, g);
     top = pre.x;
     for (int i = 0; i < count; i += 4) {
       float x[4];
@@ -97,19 +97,13 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
         for (int c = 0; c < 16; ++c) o[c * a.tile_rows] = acc[c];
         continue;
       }
-      if constexpr (kMode == kPrefix) {
-        float4* o = reinterpret_cast<float4*>(a.pre_o + at_pre * DP + c0);
-#pragma unroll
-        for (int c = 0; c < 16; ++c) o[c] = acc[c];
-        continue;
-      }
       if (joined) {
         const float f = pre.x == top ? 1.f : exp2_fast(pre.x - top);
-        const float4* o = reinterpret_cast<const float4*>(a.pre_o + at_pre * DP + c0);
+        const float4* o = pre_at(a, head, c0, r, g);
         sum += pre.y * f;
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
-          const float4 v = __ldcg(o + c);
+          const float4 v = o[c * a.pre_rows];
           acc[c].x += v.x * f;
           acc[c].y += v.y * f;
           acc[c].z += v.z * f;
@@ -138,8 +132,6 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
     }
     if (!last)
       a.part_ml[slot(0) * a.tile_rows + row] = make_float2(top, sum);
-    else if (kMode == kPrefix)
-      a.pre_ml[at_pre] = make_float2(top, sum);
     else if (a.lse)
       a.lse[r * (a.H * a.G) + hq] =
           sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
@@ -438,16 +430,15 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       // the pair's end
       tc_fence_after();
       const bool whole = pr.u0 == 0 && pr.u1 == pr.t.units;
-      const int hq = pr.head * a.G + (R - token * a.G);
+      const int g = R - token * a.G, hq = pr.head * a.G + g;
       const int64_t r = pr.t.qrow + token;
       const bool mine = row < rows;
       float top2 = sm.top * a.scale;      // in log2
       // whole pairs behind a prefix: this and its sums, joined
-      const int64_t at_pre = r * (a.H * a.G) + hq;
       const bool joined = kMode == kJoined && whole && pr.shared();
       float2 f = make_float2(1.f, 0.f);
       if (joined) {
-        const float2 pre = __ldcg(&a.pre_ml[at_pre]);
+        const float2 pre = *pre_ml_at(a, pr.head, r, g);
         f = join_factors(top2, pre, &top2);
         sm.sum = sm.sum * f.x + pre.y * f.y;
       }
@@ -470,19 +461,19 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         tc_loaded<32>(o);
         uint32_t w[16];
         if (kMode == kPrefix && whole) {
-          float4* po = reinterpret_cast<float4*>(a.pre_o + at_pre * DP + col);
+          float4* po = pre_at(a, pr.head, col, r, g);
           if (mine) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              po[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+              po[e * a.pre_rows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
                                   __uint_as_float(o[4 * e + 3]));
           }
         } else if (whole) {
           if (joined) {
-            const float4* po = reinterpret_cast<const float4*>(a.pre_o + at_pre * DP + col);
+            const float4* po = pre_at(a, pr.head, col, r, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float4 v = __ldcg(po + e);
+              const float4 v = po[e * a.pre_rows];
               const float add[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
               for (int k = 0; k < 4; ++k)
@@ -525,6 +516,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       }
       if (!whole) {
         if (mine) a.part_ml[slot * a.tile_rows + t_row] = make_float2(top2, sm.sum);
+        if constexpr (kMode == kPrefix) continue;      // (k_join_prefixes joins them)
         // (a warp writes, counts and joins its own 32 rows of the pair's pieces)
         const Pieces ps = pieces_of(pr.t, pr.head, pr.lead, pr.share);
         // true when `count` warps have come to set `set` of piece `of`, this one last
@@ -543,7 +535,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         };
         if (ps.count <= kAlone) {
           if (last(0, ps.count, 0))
-            join_rows<DP, kBf16, kMode>(a, ps.first, 0, 1, ps.count, true, t_row, mine, pr.shared(), out, r, hq);
+            join_rows<DP, kBf16, kMode>(a, ps.first, 0, 1, ps.count, true, t_row, mine, pr.shared(), out, r, pr.head, g);
         } else {
           const int g0 = (int)(blockIdx.x - ps.first) / kGroup * kGroup, n = min(kGroup, ps.count - g0);
           const int groups = (ps.count + kGroup - 1) / kGroup;
@@ -551,13 +543,13 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 #pragma unroll 1
             for (int step = 0; step < 2; ++step) {
               join_rows<DP, kBf16, kMode>(a, ps.first, step ? 0 : g0, step ? kGroup : 1, step ? groups : n, step == 1, t_row,
-                                          mine, pr.shared(), out, r, hq);
+                                          mine, pr.shared(), out, r, pr.head, g);
               if (step || !last(0, groups, 0)) break;
             }
           }
         }
       } else if (kMode == kPrefix) {
-        if (mine) a.pre_ml[at_pre] = make_float2(top2, sm.sum);
+        if (mine) *pre_ml_at(a, pr.head, r, g) = make_float2(top2, sm.sum);
       } else if (mine && a.lse) {
         a.lse[r * (a.H * a.G) + hq] =
             sm.sum == 0.f ? -INFINITY : (top2 - weight_bias<kBf16>()) * 0.693147180559945f + logf(sm.sum);
@@ -830,6 +822,55 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   }
 }
 
+// The pieces of a cut (prefix tile, head), joined in their order: a warp 32 rows and 16 columns of them, a lane a
+// row.  A pair of 512 rows behind 8192 keys is cut into 19 pieces: 20 MB for 4 heads, which the last CTAs to come
+// joined by themselves in some 10 us of 38; here all SMs read them.
+constexpr int kJoinThreads = 128, kJoinCols = 16;
+template <int DP>
+__global__ void __launch_bounds__(kJoinThreads) k_join_prefixes(const __grid_constant__ AttnArgs a) {
+  dep_wait();
+  dep_trigger();
+  const StepHead step = load_words(a.head);
+  if (!step_fits<kPrefix>(a, step, ATTN_TC)) return;
+  const int lane = threadIdx.x & 31, blocks = (a.tile_rows + 31) / 32, cols = DP / kJoinCols;
+  const int tasks = step.requests * a.H * blocks * cols, share = a.work[0].share, lead = a.work[0].lead;
+  for (int i = (blockIdx.x * kJoinThreads + threadIdx.x) >> 5; i < tasks; i += gridDim.x * (kJoinThreads / 32)) {
+    const int c0 = i % cols * kJoinCols, block = i / cols % blocks, pair = i / cols / blocks;
+    const int tile = pair / a.H, head = pair - tile * a.H, row = 32 * block + lane;
+    const AttnTile t = load_words(&a.tiles[tile]);
+    const Pieces ps = pieces_of(t, head, lead, share);
+    if (ps.count <= 1 || 32 * block >= t.rows) continue;
+    auto slot = [&](int p) { return part_slot(ps.first + p, p == 0); };
+    auto ml_of = [&](int p) { return a.part_ml[slot(p) * a.tile_rows + min(row, t.rows - 1)]; };
+    float top = -INFINITY, sum = 0.f;
+    for (int p = 0; p < ps.count; ++p) top = fmaxf(top, ml_of(p).x);
+    float4 acc[kJoinCols / 4];
+#pragma unroll
+    for (int c = 0; c < kJoinCols / 4; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < ps.count; ++p) {
+      const float2 ml = ml_of(p);
+      const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
+      const float4* o = part_at<DP>(a, slot(p), c0, min(row, t.rows - 1));
+      sum += ml.y * f;
+#pragma unroll
+      for (int c = 0; c < kJoinCols / 4; ++c) {
+        const float4 v = o[c * a.tile_rows];
+        acc[c].x += v.x * f;
+        acc[c].y += v.y * f;
+        acc[c].z += v.z * f;
+        acc[c].w += v.w * f;
+      }
+    }
+    if (row >= t.rows) continue;
+    const int R = t.row0 + row, token = R / a.G, g = R - token * a.G;
+    float4* to = pre_at(a, head, c0, t.qrow + token, g);
+#pragma unroll
+    for (int c = 0; c < kJoinCols / 4; ++c) to[c * a.pre_rows] = acc[c];
+    if (c0 == 0) *pre_ml_at(a, head, t.qrow + token, g) = make_float2(top, sum);
+  }
+}
+
 template <int DP, bool kBf16, int kMode>
 cudaError_t run(const AttnArgs& a, const TcMaps& m, int ctas, cudaStream_t s) {
   static const CUtensorMap none{};
@@ -859,6 +900,10 @@ cudaError_t configure_attend_tc() {
                         set<64, kJoined>(), set<128, kJoined>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
+}
+
+cudaError_t launch_join_prefixes(const AttnArgs& a, int num_sms, cudaStream_t s) {
+  return launch_dependent(a.dp == 64 ? k_join_prefixes<64> : k_join_prefixes<128>, dim3(4 * num_sms), kJoinThreads, 0, s, a);
 }
 
 cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, AttnMode mode, cudaStream_t s) {

@@ -143,7 +143,7 @@ __device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests,
   const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
   units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
   const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
-  if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, requests};
+  if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, kGroups ? n_tiles : requests};
   // (zero already but after an attention that ran out of a wait)
   static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
   for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += NT)
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut_shared(const __grid_c
     a.pre.reqs[i] = g;
   }
   __syncthreads();      // (before other threads of this CTA read them)
-  cut_line<kCutThreads, true>(a.pre, a.n, a.n, ws, first_tile);
+  cut_line<kCutThreads, true>(a.pre, a.n, 0, ws, first_tile);
 }
 
 // ---------------------------------------------------------------- KV write

@@ -57,7 +57,7 @@ struct StepHead {
                         // that came are counted, and another call on the list would join them as its own)
   int32_t num_tokens;   // the plan's; rows past it are of no request whatever positions and slots hold
   int32_t live;         // rows of requests
-  int32_t requests;     // how many, and kSharedStep where the plan was given prefixes
+  int32_t requests;     // how many, and kSharedStep where the plan was given prefixes; of a prefixes' line: its tiles
 };
 constexpr int32_t kSharedStep = 1 << 16;
 static_assert(sizeof(StepHead) == 16, "read as one word");
@@ -157,8 +157,10 @@ struct AttnArgs {
   const StepHead* own_head;     // the step's, where head is the prefixes'
   const StepHead* pre_head;     // and the prefixes', with the kernel that attended over them
   int32_t pre_kind;
-  float* pre_o;            // [rows][Hq][dp] sums over each row's prefix, and
-  float2* pre_ml;          // [rows][Hq] their maximum (in log2) and weight
+  float* pre_o;            // [H][dp / 4][pre_rows][4] sums over each packed row's prefix (of the step's rows, G
+                           // to a row), so that lanes that have a row each read and write 16 bytes side by side, and
+  float2* pre_ml;          // [H][pre_rows] their maximum (in log2) and weight
+  int64_t pre_rows;
 };
 
 // What an attention kernel works on: the requests' contexts (kWhole), the prefixes, whose sums it leaves in
@@ -203,6 +205,8 @@ struct TcMaps {
   const CUtensorMap* q;    // boxes of 64 columns, G heads and 128 / G rows; null: plain loads
   int box_rows;
 };
+// The pieces of prefixes that k_attend_tc has cut, joined to pre_o and pre_ml.
+cudaError_t launch_join_prefixes(const AttnArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, AttnMode mode, cudaStream_t s);
 
 // A launch that may be scheduled while the previous kernel on `s` still runs; the kernel waits
@@ -264,6 +268,13 @@ __device__ __forceinline__ bool step_fits(const AttnArgs& a, const StepHead& hea
   }
   const StepHead own = load_words(a.own_head);
   return fits && own.requests >= kSharedStep && own.kind >= 0 && own.num_tokens == head.num_tokens;
+}
+// Four columns from `col` on of the prefix's sums of packed row g of the step's row r; their maximum and weight.
+__device__ __forceinline__ float4* pre_at(const AttnArgs& a, int head, int col, int64_t r, int g) {
+  return reinterpret_cast<float4*>(a.pre_o) + ((int64_t)head * (a.dp / 4) + col / 4) * a.pre_rows + r * a.G + g;
+}
+__device__ __forceinline__ float2* pre_ml_at(const AttnArgs& a, int head, int64_t r, int g) {
+  return a.pre_ml + head * a.pre_rows + r * a.G + g;
 }
 // Sums (with maximum and weight ml.x, ml.y) that are joined with others of maximum top: the factor of either.
 __device__ __forceinline__ float2 join_factors(float top, float2 ml, float* joint) {
