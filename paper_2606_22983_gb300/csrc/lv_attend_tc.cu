@@ -823,9 +823,9 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 }
 
 // The pieces of a cut (prefix tile, head), joined in their order: a warp 32 rows and 16 columns of them, a lane a
-// row.  A pair of 512 rows behind 8192 keys is cut into 19 pieces: 20 MB for 4 heads, which the last CTAs to come
+// row, four pieces' loads on their way at once (one after the other they took 18 us).  A pair of 512 rows behind 8192 keys is cut into 19 pieces: 20 MB for 4 heads, which the last CTAs to come
 // joined by themselves in some 10 us of 38; here all SMs read them.
-constexpr int kJoinThreads = 128, kJoinCols = 16;
+constexpr int kJoinThreads = 128, kJoinCols = 16, kJoinPieces = 4;
 template <int DP>
 __global__ void __launch_bounds__(kJoinThreads) k_join_prefixes(const __grid_constant__ AttnArgs a) {
   dep_wait();
@@ -841,25 +841,43 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_prefixes(const __grid_con
     const Pieces ps = pieces_of(t, head, lead, share);
     if (ps.count <= 1 || 32 * block >= t.rows) continue;
     auto slot = [&](int p) { return part_slot(ps.first + p, p == 0); };
-    auto ml_of = [&](int p) { return a.part_ml[slot(p) * a.tile_rows + min(row, t.rows - 1)]; };
+    const int at = min(row, t.rows - 1);
     float top = -INFINITY, sum = 0.f;
-    for (int p = 0; p < ps.count; ++p) top = fmaxf(top, ml_of(p).x);
     float4 acc[kJoinCols / 4];
 #pragma unroll
     for (int c = 0; c < kJoinCols / 4; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = 0; p < ps.count; ++p) {
-      const float2 ml = ml_of(p);
-      const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
-      const float4* o = part_at<DP>(a, slot(p), c0, min(row, t.rows - 1));
-      sum += ml.y * f;
+    for (int p0 = 0; p0 < ps.count; p0 += kJoinPieces) {
+      float2 ml[kJoinPieces];
+      float4 v[kJoinPieces][kJoinCols / 4];
 #pragma unroll
-      for (int c = 0; c < kJoinCols / 4; ++c) {
-        const float4 v = o[c * a.tile_rows];
-        acc[c].x += v.x * f;
-        acc[c].y += v.y * f;
-        acc[c].z += v.z * f;
-        acc[c].w += v.w * f;
+      for (int e = 0; e < kJoinPieces; ++e) {
+        ml[e] = make_float2(-INFINITY, 0.f);
+        if (p0 + e >= ps.count) continue;
+        const int64_t from = slot(p0 + e);
+        ml[e] = a.part_ml[from * a.tile_rows + at];
+#pragma unroll
+        for (int c = 0; c < kJoinCols / 4; ++c) v[e][c] = part_at<DP>(a, from, c0 + 4 * c, at)[0];
+      }
+      float high = top;
+#pragma unroll
+      for (int e = 0; e < kJoinPieces; ++e) high = fmaxf(high, ml[e].x);
+      const float f0 = top == high ? 1.f : exp2_fast(top - high);
+      top = high;
+      sum *= f0;
+#pragma unroll
+      for (int c = 0; c < kJoinCols / 4; ++c) acc[c] = make_float4(acc[c].x * f0, acc[c].y * f0, acc[c].z * f0, acc[c].w * f0);
+#pragma unroll
+      for (int e = 0; e < kJoinPieces; ++e) {
+        if (p0 + e >= ps.count) break;
+        const float f = ml[e].x == top ? 1.f : exp2_fast(ml[e].x - top);
+        sum += ml[e].y * f;
+#pragma unroll
+        for (int c = 0; c < kJoinCols / 4; ++c) {
+          acc[c].x += v[e][c].x * f;
+          acc[c].y += v[e][c].y * f;
+          acc[c].z += v[e][c].z * f;
+          acc[c].w += v[e][c].w * f;
+        }
       }
     }
     if (row >= t.rows) continue;
