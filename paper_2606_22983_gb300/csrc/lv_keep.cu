@@ -451,11 +451,11 @@ __global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_con
 }
 
 // ---------------------------------------------------------------- compaction
-constexpr int kCheckThreads = 512, kCheckCtas = 8;
+constexpr int kCheckThreads = 1024, kCheckCtas = 16;
 
 // Request blockIdx.x / kCheckCtas by a cluster: its session, that its blocks are in HBM, and its lists, which
 // have to ascend within the context.  lens[i] receives what it may be cut to, or -1 where nothing moves.
-__global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThreads)
+__global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThreads, 1)
     k_compact_check(const __grid_constant__ CompactArgs a) {
   namespace cg = cooperative_groups;
   __shared__ int s_bad;
@@ -482,6 +482,7 @@ __global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThrea
       const int lists = a.p.J / 2 * a.H;
       for (int l = rank; l < lists; l += kCheckCtas) {
         const int32_t* x = a.kept + ((int64_t)i * lists + l) * a.most;
+#pragma unroll 4
         for (int j = tid; j < keep; j += kCheckThreads) {
           const int v = x[j], before = j > 0 ? x[j - 1] : -1;
           if (v <= before || v >= c) bad = LV_ERR_BOUNDS;
@@ -502,9 +503,14 @@ __global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThrea
 
 // Moves rows [0, keep) of one list's K or V: row j of the head from the slot of token kept[j], in chunks of
 // rows in order: as the lists ascend, kept[j] >= j, so a chunk whose loads come before its stores reads
-// nothing that an earlier one wrote over.  A row's vectors lie together; `parts` CTAs share them.
+// nothing that an earlier one wrote over.  A row's vectors lie together; `parts` CTAs share them.  A chunk's
+// places are looked up (list, then table) while the chunk before it is on its way.
+constexpr int kMoveRows = 256;      // of a chunk at most
 template <typename V, int U>
-__global__ void __launch_bounds__(kMoveThreads) k_compact(const __grid_constant__ CompactArgs a, int vecs, int part_vecs) {
+__global__ void __launch_bounds__(kMoveThreads, 4) k_compact(const __grid_constant__ CompactArgs a, int vecs, int part_vecs) {
+  // of a chunk's rows: where from, where to (null: it stays); three chunks', as a thread may write the next one's
+  // while another stores by the one's before
+  __shared__ V* place[3][2][kMoveRows];
   dep_wait();
   dep_trigger();
   const int i = blockIdx.y, tid = threadIdx.x;
@@ -517,32 +523,60 @@ __global__ void __launch_bounds__(kMoveThreads) k_compact(const __grid_constant_
   if (keep >= c) return;
   const int32_t* kept = a.kept + ((int64_t)i * lists + list) * a.most;
   const int32_t* table = a.p.table + (size_t)sid * a.p.maxB;
-  V* base = reinterpret_cast<V*>(a.p.kv[2 * layer + kv]);
+  const int v0 = part * part_vecs, mine = min(part_vecs, vecs - v0);
+  V* const base = reinterpret_cast<V*>(a.p.kv[2 * layer + kv]) + head * vecs + v0;
   const uint64_t page_vecs = (uint64_t)a.p.P / sizeof(V);
   const uint32_t T = a.p.T, token_vecs = (uint32_t)a.H * vecs;
-  const int v0 = part * part_vecs, mine = min(part_vecs, vecs - v0);
   auto slot = [&](int token) -> V* {
     const uint32_t b = a.t_shift >= 0 ? (uint32_t)token >> a.t_shift : (uint32_t)token / T;
-    return base + (uint64_t)table[b] * page_vecs + (uint64_t)((uint32_t)token - b * T) * token_vecs + head * vecs + v0;
+    return base + (uint64_t)table[b] * page_vecs + (uint64_t)((uint32_t)token - b * T) * token_vecs;
   };
-  const int rows = kMoveThreads * U / part_vecs;      // of a chunk
+  const int rows = min(kMoveThreads * U / part_vecs, kMoveRows);      // of a chunk
+  V *from = nullptr, *to = nullptr;
+  auto look = [&](int j) {      // thread j's row of the next chunk
+    from = to = nullptr;
+    if (tid >= rows || j >= keep) return;
+    const int token = kept[j];
+    if (token == j) return;
+    from = slot(token);
+    to = slot(j);
+  };
+  look(tid);
+  int buf = 0;
+  if (tid < rows) {
+    place[0][0][tid] = from;
+    place[0][1][tid] = to;
+  }
+  __syncthreads();
+  // this thread's vectors: the same rows and columns of every chunk
+  int row[U], col[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = u * kMoveThreads + tid;
+    row[u] = at / part_vecs;
+    col[u] = at - row[u] * part_vecs;
+    if (row[u] >= rows || col[u] >= mine) row[u] = -1;
+  }
   for (int j0 = 0; j0 < keep; j0 += rows) {
+    const int next = buf == 2 ? 0 : buf + 1;
     V x[U];
-    V* to[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = u * kMoveThreads + tid, r = at / part_vecs, v = at - r * part_vecs, j = j0 + r;
-      to[u] = nullptr;
-      if (r >= rows || j >= keep || v >= mine) continue;
-      const int from = kept[j];
-      if (from == j) continue;
-      x[u] = slot(from)[v];
-      to[u] = slot(j) + v;
+      const V* p = row[u] >= 0 ? place[buf][0][row[u]] : nullptr;
+      if (p) x[u] = p[col[u]];
+    }
+    look(j0 + rows + tid);
+    if (tid < rows) {
+      place[next][0][tid] = from;
+      place[next][1][tid] = to;
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (to[u]) *to[u] = x[u];
+    for (int u = 0; u < U; ++u) {
+      V* p = row[u] >= 0 ? place[buf][1][row[u]] : nullptr;
+      if (p) p[col[u]] = x[u];
+    }
+    buf = next;
   }
   if (part || kv) return;
   if (a.w.data) {
@@ -617,6 +651,8 @@ __global__ void __launch_bounds__(kCutThreads) k_truncate(DevPool p, const int32
 }  // namespace
 
 cudaError_t configure_keep() {
+  const cudaError_t e = cudaFuncSetAttribute(k_compact_check, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(k_select_kept, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)OnceShared::bytes(kMostWords));
 }
 
