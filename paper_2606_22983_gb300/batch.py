@@ -47,7 +47,7 @@ class KVBatch:
         self.pool, self.q_heads, self.dtype = pool, q_heads, dtype
         self.max_requests, self.max_tokens = max_requests, max_tokens
         self.num_tokens = 0
-        self._shared = False         # the planned step has prefixes
+        self._shared = 0             # launches over the planned step's prefixes
         self.handle = None
         i32 = dict(dtype=torch.int32, device=pool.device)
         rows, requests = max(max_tokens, 0), max(max_requests, 0)
@@ -62,7 +62,7 @@ class KVBatch:
         self._device = self.row_starts.get_device()
         self._used_on = {lv.stream_handle(None, self._device)}      # streams that keep the arrays above in use
         self._scale = 1.0 / math.sqrt(pool.head_dim)
-        self._a, self._b = lv.lv_heads(), lv.lv_heads()      # a call's two tensor arguments
+        self._a, self._b, self._w = lv.lv_heads(), lv.lv_heads(), lv.lv_weights()      # a call's tensor arguments
         # an output that attention() makes itself
         self._own = lv.lv_heads(row_stride=q_heads * pool.head_dim, head_stride=pool.head_dim,
                                 dtype=_KINDS[dtype])
@@ -99,8 +99,8 @@ class KVBatch:
                 raise ValueError("expected a tensor on the pool's device")
         else:
             x = np.ascontiguousarray(x, dtype=np.int32)
-        if n is not None and len(x) != n:
-            raise ValueError(f"expected {n} entries, got {len(x)}")
+        if n is not None and x.shape[0] != n:
+            raise ValueError(f"expected {n} entries, got {x.shape[0]}")
         return x
 
     def plan(self, sids, lens, firsts=None, *, prefixes=None, prefix_lens=None, num_tokens=None, max_len=None,
@@ -112,7 +112,7 @@ class KVBatch:
         prefixes: sessions whose first prefix_lens[i] tokens (None: all of them) the rows of request i see
         before its own session's (-1: none).  Requests of one prefix that follow one another read it once."""
         sids = self._ints(sids)
-        n = len(sids)
+        n = sids.shape[0]
         lens = self._ints(lens, n)
         if firsts is not None:
             firsts = self._ints(firsts, n)
@@ -139,8 +139,13 @@ class KVBatch:
         else:
             lv.lv_batch_plan_shared(self.handle, sids, firsts, lens, prefixes, prefix_lens, n, num_tokens, max_len, s)
         self.num_tokens = num_tokens
-        self._shared = prefixes is not None and n > 0
-        self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH or self._shared)
+        # launches that an attention has before its own: over prefixes, and the join of those by the kernel for many
+        # rows, which takes them where there are more than one tile of the other's, in pages that TMA reads
+        self._shared = 0
+        if prefixes is not None and n > 0:
+            self._shared = 1 + (num_tokens * (self.q_heads // self.pool.kv_heads) > 16 and
+                                self.pool.T % 8 == 0 and self.pool.head_dim <= 128)
+        self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH or self._shared > 0)
 
     def _stream(self, stream):
         """The handle of a call's stream, and whether it is another than the current one."""
@@ -230,11 +235,11 @@ class KVBatch:
         theirs in the row of the session that holds it.  ``KVPool.select_kept`` chooses by such weights."""
         s, away = self._stream(stream)
         q_arg = self._put(self._a, q, self.q_heads, "q")
-        if lse.shape[0] < self.num_tokens or lse.dim() != 2 or lse.shape[1] != self.q_heads or \
+        if lse.dim() != 2 or lse.shape[0] < self.num_tokens or lse.shape[1] != self.q_heads or \
                 lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.get_device() != self._device:
             raise ValueError(f"lse: expected a contiguous f32 tensor [{self.num_tokens}, {self.q_heads}] on "
                              f"{self.pool.device}, got {tuple(lse.shape)} of {lse.dtype} on {lse.device}")
-        w = self.pool.weights_arg(weights[None], 1)
+        w = self.pool._put_weights(self._w, weights, False)
         if away or s not in self._used_on:
             self._use(s, q, lse, weights)
         lv.lv_attention_weights(self.handle, layer, q_arg, lse, w, last, self._scale if scale is None else scale, s)

@@ -150,13 +150,18 @@ bool is_device_ptr(const void* p) {
 
 // The address the GPU uses for p: p itself for device or managed memory, the
 // device alias of mapped page-locked host memory, else nullptr (pageable memory).
-const void* gpu_view(const void* p) {
+// on_device (or null): whether it is device or managed memory.
+const void* gpu_view(const void* p, bool* on_device = nullptr) {
+  if (on_device) *on_device = false;
   cudaPointerAttributes a{};
   if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
     cudaGetLastError();
     return nullptr;
   }
-  if (a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged) return p;
+  if (a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged) {
+    if (on_device) *on_device = true;
+    return p;
+  }
   if (a.type == cudaMemoryTypeHost) return a.devicePointer;
   return nullptr;
 }
@@ -179,8 +184,9 @@ class Staging {
     *dev = nullptr;
     if (bytes == 0) return LV_OK;
     if (user == nullptr) return LV_ERR_INVALID;
-    if (const void* v = gpu_view(user)) {
-      if (!near || is_device_ptr(user)) {
+    bool on_device;
+    if (const void* v = gpu_view(user, &on_device)) {
+      if (!near || on_device) {
         *dev = v;
         return LV_OK;
       }

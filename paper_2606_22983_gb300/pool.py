@@ -50,6 +50,7 @@ class KVPool:
                 kv = torch.zeros((self.J, hbm_pages, self.P), dtype=torch.uint8, device=self.device)
             self.kv = kv
             self._device = kv[0].get_device()
+            self._weights = lv.lv_weights()      # a call's weights
             ptrs = (ctypes.c_void_p * self.J)(*[self.kv[j].data_ptr() for j in range(self.J)])
             self._ptrs = ptrs
             d = lv.lv_pool_desc()
@@ -193,25 +194,29 @@ class KVPool:
                 raise ValueError("expected a tensor on the pool's device")
         else:
             x = np.ascontiguousarray(x, dtype=np.int32)
-        if n is not None and len(x) != n:
-            raise ValueError(f"expected {n} entries, got {len(x)}")
+        if n is not None and x.shape[0] != n:
+            raise ValueError(f"expected {n} entries, got {x.shape[0]}")
         return x
 
-    def weights_arg(self, w, layers=None):
-        """What the library reads of weights ``w``, [layers, sessions, kv_heads, tokens] of f32 on the
-        pool's device with tokens contiguous."""
-        want = (self.L if layers is None else layers, self.S, self.kv_heads)
-        if w.dim() != 4 or tuple(w.shape[:3]) != want or w.dtype is not torch.float32 or \
-                (w.stride(3) != 1 and w.shape[3] > 1) or w.get_device() != self._device:
+    def _put_weights(self, arg, w, layers=True):
+        """arg describes weights ``w`` of f32 on the pool's device, [layers, sessions, kv_heads, tokens], or a
+        layer's without the first (layers False), with tokens contiguous."""
+        shape, stride = w.shape, w.stride()
+        want = (self.L, self.S, self.kv_heads) if layers else (self.S, self.kv_heads)
+        if shape[:-1] != want or w.dtype is not torch.float32 or (stride[-1] != 1 and shape[-1] > 1) or \
+                w.get_device() != self._device:
             raise ValueError(f"weights: expected an f32 tensor {[*want, 'tokens']} on {self.device} with contiguous "
-                             f"tokens, got {tuple(w.shape)} of {w.dtype} on {w.device}")
-        a, b, c, _ = w.stride()
-        return lv.lv_weights(data=w.data_ptr(), layer_stride=a, session_stride=b, head_stride=c, tokens=w.shape[3])
+                             f"tokens, got {tuple(shape)} of {w.dtype} on {w.device}")
+        arg.data, arg.tokens = w.data_ptr(), shape[-1]
+        arg.head_stride, arg.session_stride, arg.layer_stride = stride[-2], stride[-3], stride[0]
+        return arg
 
     def _on_stream(self):
         """The handle of the pool's stream, and that stream for PyTorch where it is not the current one."""
+        if self.stream is None:
+            return lv.stream_handle(None, self._device), None
         s = lv.stream_handle(self.stream, self._device)
-        if self.stream is None or s == lv.stream_handle(None, self._device):
+        if s == lv.stream_handle(None, self._device):
             return s, None
         return s, (torch.cuda.ExternalStream(s, device=self.device) if s else torch.cuda.default_stream(self.device))
 
@@ -236,7 +241,7 @@ class KVPool:
         largest of keeps (has to be given where they are on the device).  With a stream of the pool's own, the
         caller orders it with what made the arguments and what reads the result."""
         sids = self._ints(sids)
-        n = len(sids)
+        n = sids.shape[0]
         keeps = self._ints(keeps, n)
         if most is None:
             if isinstance(keeps, torch.Tensor) and keeps.is_cuda:
@@ -244,7 +249,7 @@ class KVPool:
             most = max(int(np.asarray(keeps).max(initial=1)), 1)
         s, away = self._on_stream()
         kept = self._new_ints((n, self.L, self.kv_heads, most), away, sids, keeps, weights)
-        lv.lv_select_kept(self.handle, self.weights_arg(weights), sids, keeps, n, first, last, kept, most, s)
+        lv.lv_select_kept(self.handle, self._put_weights(self._weights, weights), sids, keeps, n, first, last, kept, most, s)
         self.launches += n > 0
         return kept
 
@@ -253,28 +258,29 @@ class KVPool:
         and their weights with them.  Returns the lengths that ``truncate`` takes: int32 [len(sids)] on the
         device, -1 for a request that was refused."""
         sids = self._ints(sids)
-        n = len(sids)
+        n = sids.shape[0]
         keeps, kept = self._ints(keeps, n), self._ints(kept, n)
         if kept.ndim != 4 or tuple(kept.shape[1:3]) != (self.L, self.kv_heads):
             raise ValueError(f"kept: expected {[n, self.L, self.kv_heads, 'most']}, got {list(kept.shape)}")
         s, away = self._on_stream()
         lens = self._new_ints((n,), away, sids, keeps, kept, weights)
         lv.lv_kv_compact(self.handle, sids, keeps, n, kept, kept.shape[3],
-                         None if weights is None else self.weights_arg(weights), lens, s)
+                         None if weights is None else self._put_weights(self._weights, weights), lens, s)
         self.launches += 2 * (n > 0)
         return lens
 
     def truncate(self, sids, lens):
         """Cuts the contexts of sessions ``sids`` to ``lens`` tokens and frees the blocks behind them."""
         sids = self._ints(sids)
-        lens = self._ints(lens, len(sids))
+        n = sids.shape[0]
+        lens = self._ints(lens, n)
         s, away = self._on_stream()
         if away is not None:
             for x in (sids, lens):
                 if isinstance(x, torch.Tensor) and x.is_cuda:
                     x.record_stream(away)
-        lv.lv_session_truncate(self.handle, sids, lens, len(sids), s)
-        self.launches += len(sids) > 0
+        lv.lv_session_truncate(self.handle, sids, lens, n, s)
+        self.launches += n > 0
 
     def evict_tokens(self, sids, keeps, weights, *, first=0, last=0, most=None):
         """``select_kept``, ``compact`` and ``truncate``: sessions ``sids`` keep keeps[i] tokens in every layer and

@@ -285,7 +285,7 @@ def test_refusals():
     from paper_2606_22983_gb300 import lv
     s = Kept([50], dim=8, heads=1)
     try:
-        h, w, sids, one = s.pool.handle, s.pool.weights_arg(s.weights), s.sids, _i32([10])
+        h, w, sids, one = s.pool.handle, s.pool._put_weights(lv.lv_weights(), s.weights), s.sids, _i32([10])
         out = torch.zeros((1, 2, 1, 10), dtype=torch.int32, device="cuda")
         sel = lambda **k: (lambda d: lv.lv_select_kept(h, d["w"], d["sids"], d["keeps"], d["n"], d["first"], d["last"], d["kept"],
                                                        d["most"], None))({**dict(w=w, sids=sids, keeps=one, n=1, first=0, last=0,

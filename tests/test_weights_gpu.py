@@ -231,7 +231,7 @@ def test_refusals():
     try:
         w, lse = _weights(s), torch.zeros((3, 8), device="cuda")
         q = s.batch._put(lv.lv_heads(), s.q, 8, "q")
-        arg = s.pool.weights_arg(w[None], 1)
+        arg = s.pool._put_weights(lv.lv_weights(), w, False)
         h = s.batch.handle
         with pytest.raises(lv.LvError) as e:                     # not planned
             lv.lv_attention_weights(h, 0, q, lse, arg, 0, 1.0, 0)
