@@ -712,7 +712,7 @@ lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* fir
 /* A prefix that several sessions share (the instructions in front of an assistant's talks) is held
    once, by a session of its own, and the others' contexts continue it.  lv_batch_share makes
    room, once, for steps of up to `rows` rows (1..max_tokens) with prefixes: rows * Hq sums of
-   head_dim 32-bit values, and a workspace like lv_batch_create's.  LV_ERR_INVALID for a batch with a window or that has the room.
+   head_dim 32-bit values.  LV_ERR_INVALID for a batch with a window or that has the room.
    Synchronous, as lv_batch_create.
    lv_batch_plan_shared plans a step as lv_batch_plan does, in which request i's rows also see the
    first prefix_lens[i] tokens of session prefixes[i] (prefix_lens NULL: all it holds; prefixes[i] < 0

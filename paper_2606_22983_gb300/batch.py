@@ -139,11 +139,12 @@ class KVBatch:
         else:
             lv.lv_batch_plan_shared(self.handle, sids, firsts, lens, prefixes, prefix_lens, n, num_tokens, max_len, s)
         self.num_tokens = num_tokens
-        # launches that an attention has before its own: over prefixes, and the join of their pieces where both
-        # are the kernel for many rows (as lv_batch_plan chooses it)
-        group = self.q_heads // self.pool.kv_heads
-        many = self.pool.T % 8 == 0 and self.pool.head_dim <= 128 and min(max_len, num_tokens) * group > 16
-        self._shared = (1 + many) if prefixes is not None and n > 0 else 0
+        # launches that an attention has before its own: over prefixes, and the join of those by the kernel for many
+        # rows, which takes them where there are more than one tile of the other's, in pages that TMA reads
+        self._shared = 0
+        if prefixes is not None and n > 0:
+            self._shared = 1 + (num_tokens * (self.q_heads // self.pool.kv_heads) > 16 and
+                                self.pool.T % 8 == 0 and self.pool.head_dim <= 128)
         self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH or self._shared > 0)
 
     def _stream(self, stream):

@@ -1688,11 +1688,6 @@ struct lv_batch {
   lv::StepHead* pre_head = nullptr;
   float* pre_o = nullptr;
   float2* pre_ml = nullptr;
-  int32_t* pre_arrived = nullptr;  // their kernel's own, as it may run beside the other
-  float* pre_part_o = nullptr;
-  float2* pre_part_ml = nullptr;
-  float* late_o = nullptr;
-  float2* late_ml = nullptr;
   bool shared = false;             // the planned step has prefixes, attended over by
   lv::AttnKind pre_kind = lv::ATTN_ROWS;
   int32_t pre_ctas = 0;
@@ -1790,11 +1785,6 @@ int rows_shares(const lv_batch* b) {
   return std::max(1, b->pool->num_sms * lv::attend_rows_ctas(b->dp) / b->pool->kv_heads);
 }
 int rows_ctas(const lv_batch* b) { return rows_shares(b) * b->pool->kv_heads; }
-// Rows of partial results: two slots a CTA.
-size_t part_rows(const lv_batch* b) {
-  const size_t rows = (size_t)2 * rows_ctas(b) * lv::kRowsRows;
-  return b->box_rows ? std::max(rows, (size_t)2 * b->pool->num_sms * lv::kTcRows) : rows;
-}
 
 lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   const int H = pool->kv_heads, D = pool->head_dim;
@@ -1829,7 +1819,9 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
     return fail(LV_ERR_CUDA);
   b->max_tiles = d->max_requests + (int32_t)(((long long)d->max_tokens * b->G + 15) / 16);
   const int most = std::max(rows_ctas(b), pool->num_sms);
-  const size_t rows = part_rows(b);
+  // rows of partial results: two slots a CTA
+  size_t rows = (size_t)2 * rows_ctas(b) * lv::kRowsRows;
+  if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows);
   try {
     if ((st = batch_alloc(b, &b->reqs, d->max_requests)) != LV_OK ||
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
@@ -1953,11 +1945,6 @@ lv_status plan_step(lv_batch* b, const int32_t* sids, const int32_t* firsts, con
       a.pre.tiles = b->pre_tiles;
       a.pre.work = b->pre_work;
       a.pre.head = b->pre_head;
-      a.pre.arrived = b->pre_arrived;
-      a.beside = kind == lv::ATTN_ROWS && pre_kind == lv::ATTN_TC;
-      a.num_sms = pool->num_sms;
-      a.key_ns = (float)pool->head_dim * 4 / 42.f;      // (what both take: k_batch_cut_shared)
-      a.unit_ns = 1500.f;
     }
     b->planned = false;      // (the old step's arrays are being written over)
     LV_TRY(lv::launch_plan(a, s));
@@ -2042,18 +2029,14 @@ lv_status lv_batch_share(lv_batch* b, int32_t rows) {
   DeviceGuard g(b->pool->device);
   const size_t kept = b->allocs.size();
   const int most = std::max(rows_ctas(b), b->pool->num_sms);
-  const size_t heads = (size_t)rows * b->d.num_q_heads, late = (size_t)rows_ctas(b) * lv::kLate * lv::kRowsRows;
+  const size_t heads = (size_t)rows * b->d.num_q_heads;
   lv_status st;
   try {
     if ((st = batch_alloc(b, &b->pre_reqs, b->d.max_requests)) == LV_OK &&
         (st = batch_alloc(b, &b->continued, b->d.max_requests)) == LV_OK &&
         (st = batch_alloc(b, &b->pre_tiles, b->max_tiles)) == LV_OK &&
         (st = batch_alloc(b, &b->pre_work, most)) == LV_OK && (st = batch_alloc(b, &b->pre_head, 1)) == LV_OK &&
-        (st = batch_alloc(b, &b->pre_o, heads * b->dp)) == LV_OK && (st = batch_alloc(b, &b->pre_ml, heads)) == LV_OK &&
-        (st = batch_alloc(b, &b->pre_arrived, (size_t)most * lv::kArriveWords)) == LV_OK &&
-        (st = batch_alloc(b, &b->pre_part_o, part_rows(b) * b->dp)) == LV_OK &&
-        (st = batch_alloc(b, &b->pre_part_ml, part_rows(b))) == LV_OK &&
-        (st = batch_alloc(b, &b->late_o, late * b->dp)) == LV_OK && (st = batch_alloc(b, &b->late_ml, late)) == LV_OK) {
+        (st = batch_alloc(b, &b->pre_o, heads * b->dp)) == LV_OK && (st = batch_alloc(b, &b->pre_ml, heads)) == LV_OK) {
       // (waits: the batch may be used on any stream next)
       if (cudaMemset(b->pre_head, 0xff, sizeof(lv::StepHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
         st = LV_ERR_CUDA;
@@ -2181,21 +2164,15 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.pre_o = b->pre_o;
   a.pre_ml = b->pre_ml;
   a.pre_rows = (int64_t)b->share_rows * b->G;
-  a.late_o = b->late_o;
-  a.late_ml = b->late_ml;
   lv::AttnArgs x = a;      // over the prefixes, by the pool's tables
   x.tables = pool->d.table;
   x.tiles = b->pre_tiles;
   x.work = b->pre_work;
   x.head = b->pre_head;
   x.tile_rows = tile_rows(b->pre_kind);
-  x.arrived = b->pre_arrived;
-  x.part_o = b->pre_part_o;
-  x.part_ml = b->pre_part_ml;
-  const bool beside = b->kind == lv::ATTN_ROWS && b->pre_kind == lv::ATTN_TC;
-  LV_TRY(launch(x, b->pre_kind, b->pre_ctas, beside ? lv::kBeside : lv::kPrefix));
-  if (b->pre_kind == lv::ATTN_TC && !beside) LV_TRY(lv::launch_join_prefixes(x, pool->num_sms, s));
-  LV_TRY(launch(a, b->kind, b->ctas, beside ? lv::kJoinedLate : lv::kJoined));
+  LV_TRY(launch(x, b->pre_kind, b->pre_ctas, lv::kPrefix));
+  if (b->pre_kind == lv::ATTN_TC) LV_TRY(lv::launch_join_prefixes(x, pool->num_sms, s));
+  LV_TRY(launch(a, b->kind, b->ctas, lv::kJoined));
   return LV_OK;
 }
 

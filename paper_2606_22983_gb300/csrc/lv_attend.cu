@@ -126,30 +126,6 @@ struct RowsShape {
   static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
 };
 
-// A row's end: its sums (a warp's, kCols columns a lane) normalised to the output, and the logarithm.
-template <int DP, bool kBf16>
-__device__ __forceinline__ void put_row(const AttnArgs& a, const float* acc, float top, float sum, int64_t r, int h) {
-  const int lane = threadIdx.x & 31;
-  constexpr int kCols = DP / 32;
-  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-  uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head + kCols * lane;
-  if (kCols * lane < a.D) {
-#pragma unroll
-    for (int e = 0; e < kCols; e += 2) {
-      const uint32_t w = pack16<kBf16>(acc[e] * inv, acc[e + 1] * inv);
-      if (a.o_vec) {
-        *reinterpret_cast<uint32_t*>(out + e) = w;
-      } else {
-        out[e] = (uint16_t)w;
-        out[e + 1] = (uint16_t)(w >> 16);
-      }
-    }
-  }
-  if (a.lse && lane == 0)
-    a.lse[r * (a.H * a.G) + h] =
-        sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
-}
-
 // Pieces p0, p0 + step, ... (count of them) of a cut pair joined by a CTA, a warp a row: every piece's
 // sums weighted by its maximum against the largest, in the pieces' order.  To the output, or
 // (not kLast) to the first of the pieces' own slots.
@@ -167,7 +143,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
     const int R = t.row0 + row, token = R / a.G, g = R - token * a.G;
     const int64_t r = t.qrow + token;
     const int h = head * a.G + g;
-    const bool joined = behind_prefixes(kMode) && kLast && t.req >= kSharedTile;
+    const bool joined = kMode == kJoined && kLast && t.req >= kSharedTile;
     float2 pre = make_float2(-INFINITY, 0.f);
     if (joined) pre = *pre_ml_at(a, head, r, g);
     float top = pre.x;
@@ -212,7 +188,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
       if (lane == 0) a.part_ml[at(0)] = make_float2(top, sum);
       continue;
     }
-    if constexpr (over_prefixes(kMode)) {
+    if constexpr (kMode == kPrefix) {
 #pragma unroll
       for (int e = 0; e < kCols; e += 2) {
         const int col = kCols * lane + e;
@@ -232,34 +208,23 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const AttnTile& t, 
         acc[e + 1] += v.y * f;
       }
     }
-    put_row<DP, kBf16>(a, acc, top, sum, r, h);
-  }
-}
-
-// Whole pairs of a CTA that were left until the prefixes' sums are done: joined with these, a warp a row.
-template <int DP, bool kBf16>
-__device__ __forceinline__ void put_late(const AttnArgs& a, const AttnTile* late, int count, int head) {
-  const int lane = threadIdx.x & 31;
-  constexpr int kCols = DP / 32;
-  for (int n = 0; n < count; ++n) {
-    const AttnTile& t = late[n];
-    for (int row = threadIdx.x >> 5; row < t.rows; row += kWarps) {
-      const int64_t at = ((int64_t)blockIdx.x * kLate + n) * kRowsRows + row;
-      const int R = t.row0 + row, token = R / a.G, g = R - token * a.G;
-      const int64_t r = t.qrow + token;
-      const float2 ml = a.late_ml[at], pre = *pre_ml_at(a, head, r, g);
-      float top, acc[kCols];
-      const float2 f = join_factors(ml.x, pre, &top);
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + h * a.o_head + kCols * lane;
+    if (kCols * lane < a.D) {
 #pragma unroll
       for (int e = 0; e < kCols; e += 2) {
-        const int col = kCols * lane + e;
-        const float2 x = *reinterpret_cast<const float2*>(a.late_o + at * DP + col);
-        const float2 v = reinterpret_cast<const float2*>(pre_at(a, head, col, r, g))[col / 2 & 1];
-        acc[e] = x.x * f.x + v.x * f.y;
-        acc[e + 1] = x.y * f.x + v.y * f.y;
+        const uint32_t w = pack16<kBf16>(acc[e] * inv, acc[e + 1] * inv);
+        if (a.o_vec) {
+          *reinterpret_cast<uint32_t*>(out + e) = w;
+        } else {
+          out[e] = (uint16_t)w;
+          out[e + 1] = (uint16_t)(w >> 16);
+        }
       }
-      put_row<DP, kBf16>(a, acc, top, ml.y * f.x + pre.y * f.y, r, head * a.G + g);
     }
+    if (a.lse && lane == 0)
+      a.lse[r * (a.H * a.G) + h] =
+          sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
   }
 }
 
@@ -309,23 +274,18 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
   }
-  // (kJoinedLate: the kernel before this is the prefixes', which has let it start once all before that had ended;
-  // its sums are waited for when the CTA's share is done, by all CTAs, so that whatever comes next finds both
-  // done)
-  if (kMode != kJoinedLate) dep_wait();
-  else asm volatile("fence.acq_rel.gpu;" ::: "memory");      // (nothing that an earlier kernel left in L1)
+  dep_wait();
   dep_trigger();
 
   const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
   const CtaWork work = load_words(&a.work[group]);
   const StepHead step = load_words(a.head);
   if (LV_RARE(!step_fits<kMode>(a, step, ATTN_ROWS))) {
-    if (kMode == kJoinedLate) dep_wait();
-    if (!over_prefixes(kMode) && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
+    if (kMode != kPrefix && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
     return;
   }
-  const bool dead = !over_prefixes(kMode) && step.live < a.num_tokens;
-  auto req_of = [&](const AttnTile& t) { return (size_t)(behind_prefixes(kMode) ? t.req & (kSharedTile - 1) : t.req); };
+  const bool dead = kMode != kPrefix && step.live < a.num_tokens;
+  auto req_of = [&](const AttnTile& t) { return (size_t)(kMode == kJoined ? t.req & (kSharedTile - 1) : t.req); };
   auto key_of = [&](const AttnTile& t, int u) { return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kU; };
   auto hidden = [&](const AttnTile& t, int key) { return key >= t.kv_hi || (key < t.kv_lo && key >= a.sinks); };
   auto find_page = [&](Walk& x) {
@@ -412,9 +372,6 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
     if (more) load(s);
     if (!kTma) copy_commit();
   }
-  __shared__ AttnTile late[kMode == kJoinedLate ? kLate : 1];
-  int n_late = 0;
-  bool waited = false;       // the prefixes' sums are done
   int stage = 0;
   uint32_t par = 0;
   int cuts = 0, was_first = 0, was_last = 0;      // (counts: thread 0's)
@@ -428,7 +385,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = lane / 4 + 8 * i, R = C.t.row0 + min(row, C.t.rows - 1), token = R / a.G;
-      pos[i] = over_prefixes(kMode) ? C.t.kv_hi - 1 : C.t.first + token;
+      pos[i] = kMode == kPrefix ? C.t.kv_hi - 1 : C.t.first + token;
       const uint16_t* x = q + (C.t.qrow + token) * a.q_row + (int64_t)(head * a.G + (R - token * a.G)) * a.q_head;
       auto two = [&](int d) -> uint32_t {      // elements d, d + 1; zeros past the rows and columns
         if (row >= C.t.rows || d >= a.D) return 0u;
@@ -449,7 +406,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) top[i] = -INFINITY, sum[i] = 0.f;
-    const int p_hi = C.t.kv_hi - 1, p_lo = over_prefixes(kMode) ? p_hi : C.t.first + C.t.row0 / a.G;
+    const int p_hi = C.t.kv_hi - 1, p_lo = kMode == kPrefix ? p_hi : C.t.first + C.t.row0 / a.G;
 
 #pragma unroll 1
     for (int u = C.u; u < C.u_end; u += kWarps) {
@@ -605,7 +562,6 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       }
     }
     const bool whole = C.u_begin == 0 && C.u_end == C.t.units;
-    const bool later = kMode == kJoinedLate && whole && !waited && C.t.req >= kSharedTile;
     if (wid == 0) {
       const int64_t slot = part_slot(blockIdx.x, C.u_begin == 0);
 #pragma unroll
@@ -616,7 +572,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
           const int R = C.t.row0 + row, token = R / a.G, g = R - token * a.G;
           const int64_t r = C.t.qrow + token;
           const int h = head * a.G + g;
-          if constexpr (over_prefixes(kMode)) {
+          if constexpr (kMode == kPrefix) {
 #pragma unroll
             for (int d = 0; d < DP / 8; ++d)
               reinterpret_cast<float2*>(pre_at(a, head, 8 * d + 2 * (lane & 3), r, g))[lane & 1] =
@@ -624,16 +580,7 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
             if ((lane & 3) == 0) *pre_ml_at(a, head, r, g) = make_float2(top[i], sum[i]);
             continue;
           }
-          if (later) {
-            const int64_t at = ((int64_t)blockIdx.x * kLate + n_late) * kRowsRows + row;
-#pragma unroll
-            for (int d = 0; d < DP / 8; ++d)
-              *reinterpret_cast<float2*>(a.late_o + at * DP + 8 * d + 2 * (lane & 3)) =
-                  make_float2(o[d][2 * i], o[d][2 * i + 1]);
-            if ((lane & 3) == 0) a.late_ml[at] = make_float2(top[i], sum[i]);
-            continue;
-          }
-          if (behind_prefixes(kMode) && C.t.req >= kSharedTile) {
+          if (kMode == kJoined && C.t.req >= kSharedTile) {
             const float2 pre = *pre_ml_at(a, head, r, g);
             const float2 f = join_factors(top[i], pre, &top[i]);
             sum[i] = sum[i] * f.x + pre.y * f.y;
@@ -670,16 +617,6 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
         }
       }
     }
-    if (kMode == kJoinedLate && later) {
-      if (threadIdx.x == 0) late[n_late] = C.t;
-      if (++n_late == kLate) {
-        __syncthreads();
-        dep_wait();
-        waited = true;
-        put_late<DP, kBf16>(a, late, n_late, head);
-        n_late = 0;
-      }
-    }
     if (!whole) {
       const Pieces ps = pieces_of(C.t, 0, work.lead, work.share);
       const int n = C.w < C.end ? 0 : 1;      // a cut first tile, then the share's last
@@ -699,11 +636,6 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
       }
       cuts |= 1 << n;
     }
-  }
-  if (kMode == kJoinedLate) {
-    __syncthreads();
-    dep_wait();
-    put_late<DP, kBf16>(a, late, n_late, head);
   }
   if (cuts) {
     __syncthreads();
@@ -791,9 +723,7 @@ cudaError_t run_mode(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap*
 }  // namespace
 
 cudaError_t configure_attend() {
-  for (cudaError_t e : {set_mode<kWhole>(), set_mode<kPrefix>(), set_mode<kJoined>(), set_rows<64, true, kJoinedLate>(),
-                        set_rows<128, true, kJoinedLate>(), set_rows<64, false, kJoinedLate>(),
-                        set_rows<128, false, kJoinedLate>()})
+  for (cudaError_t e : {set_mode<kWhole>(), set_mode<kPrefix>(), set_mode<kJoined>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }
@@ -803,11 +733,6 @@ int attend_rows_ctas(int dp) { return dp == 256 ? RowsShape<256>::kCtas : RowsSh
 
 cudaError_t launch_attend_rows(const AttnArgs& a, const CUtensorMap* k, const CUtensorMap* v, bool bf16, int ctas,
                                AttnMode mode, cudaStream_t s) {
-  if (mode == kJoinedLate) {      // (beside the kernel for many rows: no more than 128 columns)
-    if (a.dp == 64)
-      return k ? run_rows<64, true, kJoinedLate>(a, k, v, bf16, ctas, s) : run_rows<64, false, kJoinedLate>(a, k, v, bf16, ctas, s);
-    return k ? run_rows<128, true, kJoinedLate>(a, k, v, bf16, ctas, s) : run_rows<128, false, kJoinedLate>(a, k, v, bf16, ctas, s);
-  }
   return mode == kPrefix   ? run_mode<kPrefix>(a, k, v, bf16, ctas, s)
          : mode == kJoined ? run_mode<kJoined>(a, k, v, bf16, ctas, s)
                            : run_mode<kWhole>(a, k, v, bf16, ctas, s);

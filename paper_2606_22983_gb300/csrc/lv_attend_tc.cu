@@ -56,7 +56,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
     return part_slot(first + p, p == 0);
   };
   auto ml_of = [&](int i) { return __ldcg(&a.part_ml[slot(i) * a.tile_rows + row]); };
-  const bool joined = behind_prefixes(kMode) && shared && last;
+  const bool joined = kMode == kJoined && shared && last;
   float top = -INFINITY, sum = 0.f;
   if (mine) {
     float2 pre = make_float2(-INFINITY, 0.f);
@@ -97,12 +97,6 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
         for (int c = 0; c < 16; ++c) o[c * a.tile_rows] = acc[c];
         continue;
       }
-      if constexpr (kMode == kBeside) {
-        float4* o = pre_at(a, head, c0, r, g);
-#pragma unroll
-        for (int c = 0; c < 16; ++c) o[c * a.pre_rows] = acc[c];
-        continue;
-      }
       if (joined) {
         const float f = pre.x == top ? 1.f : exp2_fast(pre.x - top);
         const float4* o = pre_at(a, head, c0, r, g);
@@ -138,8 +132,6 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, int64_t first, int 
     }
     if (!last)
       a.part_ml[slot(0) * a.tile_rows + row] = make_float2(top, sum);
-    else if (kMode == kBeside)
-      *pre_ml_at(a, head, r, g) = make_float2(top, sum);
     else if (a.lse)
       a.lse[r * (a.H * a.G) + hq] =
           sum == 0.f ? -INFINITY : (top - weight_bias<kBf16>()) * 0.693147180559945f + logf(sum);
@@ -184,8 +176,8 @@ struct Pairs {
     }
     return false;
   }
-  __device__ __forceinline__ size_t req() const { return behind_prefixes(kMode) ? t.req & (kSharedTile - 1) : t.req; }
-  __device__ __forceinline__ bool shared() const { return behind_prefixes(kMode) && t.req >= kSharedTile; }
+  __device__ __forceinline__ size_t req() const { return kMode == kJoined ? t.req & (kSharedTile - 1) : t.req; }
+  __device__ __forceinline__ bool shared() const { return kMode == kJoined && t.req >= kSharedTile; }
   __device__ __forceinline__ int key_of(int u) const {
     return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kKeys;
   }
@@ -389,7 +381,6 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   tc_fence_after();
   const uint32_t tmem = bars.tmem;
   dep_wait();
-  if (kMode == kBeside) dep_trigger();
 
   if (wid < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
@@ -412,9 +403,9 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const bool live = rows > (row & ~31);                 // rows in this warp
       const int R0 = pr.t.row0 + half * half_rows;
       const int R = R0 + min(row, rows - 1), token = R / a.G;
-      const int end = pr.t.kv_hi - 1, pos = over_prefixes(kMode) ? end : pr.t.first + token;
-      const int p_lo = over_prefixes(kMode) ? end : pr.t.first + R0 / a.G;
-      const int p_hi = over_prefixes(kMode) ? end : pr.t.first + (R0 + rows - 1) / a.G;
+      const int end = pr.t.kv_hi - 1, pos = kMode == kPrefix ? end : pr.t.first + token;
+      const int p_lo = kMode == kPrefix ? end : pr.t.first + R0 / a.G;
+      const int p_hi = kMode == kPrefix ? end : pr.t.first + (R0 + rows - 1) / a.G;
       Softmax<DP, kBf16> sm;
       for (int u = pr.u0; u < pr.u1; ++u) {
         if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par, a.wait_ns))) break;
@@ -444,14 +435,14 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const bool mine = row < rows;
       float top2 = sm.top * a.scale;      // in log2
       // whole pairs behind a prefix: this and its sums, joined
-      const bool joined = behind_prefixes(kMode) && whole && pr.shared();
+      const bool joined = kMode == kJoined && whole && pr.shared();
       float2 f = make_float2(1.f, 0.f);
       if (joined) {
         const float2 pre = *pre_ml_at(a, pr.head, r, g);
         f = join_factors(top2, pre, &top2);
         sm.sum = sm.sum * f.x + pre.y * f.y;
       }
-      const float inv = !whole || over_prefixes(kMode) ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
+      const float inv = !whole || kMode == kPrefix ? 1.f : sm.sum > 0.f || sm.sum != sm.sum ? 1.f / sm.sum : 0.f;
       const int64_t slot = part_slot(blockIdx.x, pr.u0 == 0);
       const int t_row = half * half_rows + row;
       uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + r * a.o_row + hq * a.o_head;
@@ -469,7 +460,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         tc_wait_ld();
         tc_loaded<32>(o);
         uint32_t w[16];
-        if (over_prefixes(kMode) && whole) {
+        if (kMode == kPrefix && whole) {
           float4* po = pre_at(a, pr.head, col, r, g);
           if (mine) {
 #pragma unroll
@@ -557,7 +548,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             }
           }
         }
-      } else if (over_prefixes(kMode)) {
+      } else if (kMode == kPrefix) {
         if (mine) *pre_ml_at(a, pr.head, r, g) = make_float2(top2, sm.sum);
       } else if (mine && a.lse) {
         a.lse[r * (a.H * a.G) + hq] =
@@ -805,8 +796,8 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       }
       // rows of no request
       const StepHead step = load_words(a.head);
-      const bool fits = !over_prefixes(kMode) && step_fits<kMode>(a, step, ATTN_TC);
-      if (!over_prefixes(kMode) && LV_RARE(!fits) && blockIdx.x == 0 && lane == 0) report(a.ctl, LV_ERR_STATE, -1);
+      const bool fits = kMode != kPrefix && step_fits<kMode>(a, step, ATTN_TC);
+      if (kMode != kPrefix && LV_RARE(!fits) && blockIdx.x == 0 && lane == 0) report(a.ctl, LV_ERR_STATE, -1);
       if (ok && fits && step.live < a.num_tokens) {
         const int Hq = a.H * a.G;
         for (int r = blockIdx.x; r < a.num_tokens; r += gridDim.x) {
@@ -924,7 +915,7 @@ cudaError_t run_mode(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, cu
 
 cudaError_t configure_attend_tc() {
   for (cudaError_t e : {set<64, kWhole>(), set<128, kWhole>(), set<64, kPrefix>(), set<128, kPrefix>(),
-                        set<64, kJoined>(), set<128, kJoined>(), set<64, kBeside>(), set<128, kBeside>()})
+                        set<64, kJoined>(), set<128, kJoined>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }
@@ -934,8 +925,7 @@ cudaError_t launch_join_prefixes(const AttnArgs& a, int num_sms, cudaStream_t s)
 }
 
 cudaError_t launch_attend_tc(const AttnArgs& a, const TcMaps& m, bool bf16, int ctas, AttnMode mode, cudaStream_t s) {
-  return mode == kBeside   ? run_mode<kBeside>(a, m, bf16, ctas, s)
-         : mode == kPrefix ? run_mode<kPrefix>(a, m, bf16, ctas, s)
+  return mode == kPrefix   ? run_mode<kPrefix>(a, m, bf16, ctas, s)
          : mode == kJoined ? run_mode<kJoined>(a, m, bf16, ctas, s)
                            : run_mode<kWhole>(a, m, bf16, ctas, s);
 }

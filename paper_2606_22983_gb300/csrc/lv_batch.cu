@@ -76,8 +76,7 @@ __device__ __forceinline__ AttnTile make_tile(const PlanLine& a, const PlanReq& 
 // scans of two barriers each (tiles, owned rows, units, shares of either size; the last two and a vote only
 // where there may be pairs apart), some 5 us for 64 requests of one tile and 10 for 1024.
 template <int NT, bool kGroups>
-__device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests, int shares, long long* ws,
-                                         int* first_tile) {
+__device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests, long long* ws, int* first_tile) {
   // each request's first tile: a scan over the requests, a thread taking several in a row
   const int per = (n + NT - 1) / NT, q0 = min((int)threadIdx.x * per, n), q1 = min(q0 + per, n);
   long long own = 0, tiles, live = 0;
@@ -131,7 +130,7 @@ __device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests,
   });
   long long units, shorts = 0, longs = 0, at_short = 0, at_long = 0;
   const long long at_unit = cta_scan<NT>(my_units, ws, &units);
-  const bool few = (long long)n_tiles * a.line_heads <= shares;      // (or no pair has shares of its own)
+  const bool few = (long long)n_tiles * a.line_heads <= a.shares;      // (or no pair has shares of its own)
   if (few) {
     at_short = cta_scan<NT>(my_short, ws, &shorts);
     at_long = cta_scan<NT>(my_long, ws, &longs);
@@ -140,10 +139,10 @@ __device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests,
   // Pairs apart in shares of their own: uncut ones of up to `uncut` units where that holds them all,
   // else cut short (a cut costs what some 8 units of a warp do, so in the middle there is nothing).
   const long long needed = cut_free ? longs : shorts;
-  const bool apart = few && needed * a.line_heads <= shares;
+  const bool apart = few && needed * a.line_heads <= a.shares;
   const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
   units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
-  const long long share = apart ? size : max((units + shares - 1) / shares, (long long)a.min_share);
+  const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
   if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, kGroups ? n_tiles : requests};
   // (zero already but after an attention that ran out of a wait)
   static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
@@ -285,7 +284,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_batch_rows(const __grid_consta
     __syncthreads();
     if (!last) return;
     __threadfence();
-    cut_line<kPlanThreads, false>(a.own, a.n, a.n, a.own.shares, ws, first_tile);
+    cut_line<kPlanThreads, false>(a.own, a.n, a.n, ws, first_tile);
   }
 }
 
@@ -294,22 +293,23 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut(const __grid_constant
   __shared__ int first_tile[kMaxRequests];
   dep_wait();
   dep_trigger();
-  cut_line<kCutThreads, false>(a.own, a.n, a.n, a.own.shares, ws, first_tile);
+  cut_line<kCutThreads, false>(a.own, a.n, a.n, ws, first_tile);
 }
 
-// The same for a step with prefixes: CTA 0 cuts the requests' own contexts, CTA 1 the prefixes, after both have found
-// the runs of requests that continue the same tokens of the same session, each of which is one request of all
-// their rows.  A run ends before the next request that begins one or has none: a bit a request, and the words
+// The same for a step with prefixes: CTA 0 cuts the requests' own contexts, CTA 1 finds the runs of requests
+// that continue the same tokens of the same session, makes each a request of all their rows, and cuts the
+// prefixes.  A run ends before the next request that begins one or has none: a bit a request, and the words
 // after a request's own searched for the next.
-// Where the two lines' kernels run beside one another, the SMs are divided by what each has to do, and as many CTAs
-// of either line get work as its SMs hold: the prefixes' units take some 1.5 us of an SM, a
-// token's K and V rows of a head what an SM reads, some 42 bytes a ns.
 __global__ void __launch_bounds__(kCutThreads) k_batch_cut_shared(const __grid_constant__ PlanArgs a) {
   __shared__ long long ws[kCutThreads / 32];
   __shared__ int first_tile[kMaxRequests];
   __shared__ uint32_t ends[kMaxRequests / 32 + 1];
   dep_wait();
   dep_trigger();
+  if (blockIdx.x == 0) {
+    cut_line<kCutThreads, false>(a.own, a.n, a.n | kSharedStep, ws, first_tile);
+    return;
+  }
   for (int i0 = 0; i0 < a.n; i0 += kCutThreads) {
     const int i = i0 + (int)threadIdx.x;
     const int2 none = make_int2(-1, 0);
@@ -319,7 +319,6 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut_shared(const __grid_c
   }
   __syncthreads();
   const int words = (a.n + 31) >> 5;
-  long long units = 0, keys = 0;
   for (int i = threadIdx.x; i < a.n; i += kCutThreads) {
     const int2 me = __ldcg(&a.continued[i]);
     PlanReq g{0, 0, 0, 0};
@@ -331,23 +330,10 @@ __global__ void __launch_bounds__(kCutThreads) k_batch_cut_shared(const __grid_c
       const int r0 = __ldcg(&a.row_starts[i]);
       g = PlanReq{me.y - 1, __ldcg(&a.row_starts[end]) - r0, r0, me.x};
     }
-    if (blockIdx.x == 1) a.pre.reqs[i] = g;
-    units += (long long)tiles_of(a.pre, g.len) * ((g.first + (1 << a.pre.unit_shift)) >> a.pre.unit_shift);
-    const PlanReq r = load_words(&a.own.reqs[i]);
-    if (r.len > 0) keys += r.first + r.len;
+    a.pre.reqs[i] = g;
   }
-  int own_shares = a.own.shares, pre_shares = a.pre.shares;
-  if (a.beside) {
-    units = cta_sum<kCutThreads>(units, ws);
-    keys = cta_sum<kCutThreads>(keys, ws);
-    const float pre = (float)units * a.pre.line_heads * a.unit_ns, own = (float)keys * a.pre.line_heads * a.key_ns;
-    const int sms = units == 0 ? 0 : min(max((int)(a.num_sms * (pre / (pre + own)) + 0.5f), 1), a.num_sms - 1);
-    pre_shares = max(sms, 1);
-    own_shares = max((int)((long long)a.own.shares * (a.num_sms - sms) / a.num_sms), 1);
-  }
-  __syncthreads();      // (before other threads of this CTA read the runs)
-  if (blockIdx.x == 0) cut_line<kCutThreads, false>(a.own, a.n, a.n | kSharedStep, own_shares, ws, first_tile);
-  else cut_line<kCutThreads, true>(a.pre, a.n, 0, pre_shares, ws, first_tile);
+  __syncthreads();      // (before other threads of this CTA read them)
+  cut_line<kCutThreads, true>(a.pre, a.n, 0, ws, first_tile);
 }
 
 // ---------------------------------------------------------------- KV write

@@ -109,10 +109,6 @@ struct PlanArgs {
   int64_t* slots;
   int2* continued;         // [n] each request's prefix and how much of it, for prefixes (else null)
   int32_t* ticket;         // CTAs of the plan that are done, zero between calls
-  int32_t beside;          // the two lines' kernels run beside one another, on SMs of their own
-  int32_t num_sms;
-  float key_ns;            // what an SM takes for a key of one KV head and layer that it reads,
-  float unit_ns;           // and for a unit of the prefixes' line
   PlanLine own, pre;
 };
 
@@ -165,23 +161,11 @@ struct AttnArgs {
                            // to a row), so that lanes that have a row each read and write 16 bytes side by side, and
   float2* pre_ml;          // [H][pre_rows] their maximum (in log2) and weight
   int64_t pre_rows;
-  float* late_o;           // kJoinedLate: [ctas][kLate][kRowsRows][dp] sums of whole pairs whose prefixes' are not done yet,
-  float2* late_ml;         // [ctas][kLate][kRowsRows] their maximum and weight
 };
-constexpr int kLate = 8;
 
 // What an attention kernel works on: the requests' contexts (kWhole), the prefixes, whose sums it leaves in
-// pre_o and pre_ml (kPrefix: but for the cut pairs, whose pieces k_join_prefixes joins), or the requests' own
-// contexts, joined with those sums (kJoined).
-//
-// Where few rows a request read their own contexts and the prefixes' rows together are many (a decode step), the two
-// kernels run beside one another: the prefixes' takes some of the SMs and joins its pieces itself (kBeside),
-// the other starts on the rest, and waits for the first's sums at the end of a CTA's work (kJoinedLate).
-// One reads HBM, the other computes: 64 tokens behind 8192 keys of one prefix and 200 to 2500 of their own
-// took 64 us one after the other.
-enum AttnMode : int { kWhole = 0, kPrefix = 1, kJoined = 2, kBeside = 3, kJoinedLate = 4 };
-constexpr bool over_prefixes(int mode) { return mode == kPrefix || mode == kBeside; }
-constexpr bool behind_prefixes(int mode) { return mode == kJoined || mode == kJoinedLate; }
+// pre_o and pre_ml (kPrefix), or the requests' own contexts, joined with those sums (kJoined).
+enum AttnMode : int { kWhole = 0, kPrefix = 1, kJoined = 2 };
 
 constexpr long long kAttnWaitNs = 1000000000ll;   // one second a wait
 
@@ -278,7 +262,7 @@ template <int kMode>
 __device__ __forceinline__ bool step_fits(const AttnArgs& a, const StepHead& head, int kind) {
   bool fits = head.kind == kind && head.num_tokens <= a.num_tokens;
   if constexpr (kMode == kWhole) return fits && head.requests < kSharedStep;
-  if constexpr (behind_prefixes(kMode)) {
+  if constexpr (kMode == kJoined) {
     const StepHead pre = load_words(a.pre_head);
     return fits && head.requests >= kSharedStep && pre.kind == a.pre_kind && pre.num_tokens == head.num_tokens;
   }
