@@ -40,7 +40,8 @@
  * output after the stream has completed.
  * Calls that allocate from the same tier (swap-out: host slots; swap-in and
  * append: HBM pages) must be ordered with respect to each other.
- * A free (lv_cancel, the old locations of lv_remap) may overlap an allocation.
+ * A free (lv_cancel, the old locations of lv_remap, lv_session_truncate) may overlap
+ * an allocation.
  * A device-driven step (lv_turn, lv_make_resident, lv_evict) and
  * lv_swap_exchange must also be ordered with calls that change the table of a
  * session they may take blocks from or load (lv_remap, lv_session_append,
@@ -712,7 +713,7 @@ lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* fir
 /* A prefix that several sessions share (the instructions in front of an assistant's talks) is held
    once, by a session of its own, and the others' contexts continue it.  lv_batch_share makes
    room, once, for steps of up to `rows` rows (1..max_tokens) with prefixes: rows * Hq sums of
-   head_dim 32-bit values.  LV_ERR_INVALID for a batch with a window or that has the room.
+   head_dim (rounded up to 64, 128 or 256) 32-bit values.  LV_ERR_INVALID for a batch with a window or that has the room.
    Synchronous, as lv_batch_create.
    lv_batch_plan_shared plans a step as lv_batch_plan does, in which request i's rows also see the
    first prefix_lens[i] tokens of session prefixes[i] (prefix_lens NULL: all it holds; prefixes[i] < 0
@@ -774,8 +775,9 @@ typedef struct lv_weights {
    order that does not change from call to call.  LV_ERR_INVALID as for lv_attention, and for last < 0.  Device-detected, and those weights
    left as they are: LV_ERR_BOUNDS for a request (or one whose prefix has) more tokens than weights->tokens, LV_ERR_DOUBLE_MAP
    for one whose session an earlier one of the step has (the first request's tokens are added; prefixes come
-   after all requests, those of one session and length that do not follow one another count as several); LV_ERR_STATE
-   with detail -1 where lv_kv_write reports it, and for a step whose attention ran out of a wait. */
+   after all requests, and those of one session and length that do not follow one another count as several; the detail
+   is the request's index); LV_ERR_STATE with detail -1 where lv_kv_write reports it, and for a step whose attention
+   ran out of a wait; LV_ERR_TIMEOUT as lv_attention does, when some of the weights have been added. */
 lv_status lv_attention_weights(lv_batch* batch, int32_t layer, const lv_heads* q, const float* lse,
                                const lv_weights* weights, int32_t last, float scale, lv_stream stream);
 
@@ -803,7 +805,7 @@ lv_status lv_select_kept(lv_pool* pool, const lv_weights* weights, const int32_t
    to its tokens 0..keeps[i), and (weights not NULL) their weights with them, with zeros behind them up to the
    context's end.  The lists ascend strictly and end within the context, whose blocks are all in HBM; keeps[i] at
    or above the context's length moves nothing.  The context stays as long as it is, and rows behind keeps[i] as they
-   are.  Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE) are given up.  lens (int32 [n]) receives
+   are; steps over these sessions, or behind them as prefixes, are planned anew.  Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE) are given up.  lens (int32 [n]) receives
    what lv_session_truncate takes: min(keeps[i], context), or -1 for a request that was refused, of which
    nothing moved.  n and most as above.  Device-detected: LV_ERR_BOUNDS for an id, a length or a list out of range,
    LV_ERR_STATE for a block that is not in HBM, LV_ERR_DOUBLE_MAP for a session that an earlier request names;
@@ -861,7 +863,7 @@ lv_status lv_timing_read(lv_pool* pool, lv_kernel_timing* out /* [LV_TIMING_KIND
 enum { LV_FAULT_NONE = 0, LV_FAULT_HOST_ALLOC = 1, LV_FAULT_HBM_ALLOC = 2, LV_FAULT_COPY = 3 };
 lv_status lv_inject_fault(lv_pool* pool, int32_t kind, int32_t after);
 lv_status lv_selftest_wait(lv_pool* pool, int64_t limit_us, lv_stream stream);
-/* The same inside the attention kernels: in the batch's later lv_attention calls every second CTA
+/* The same inside the attention kernels: in the batch's later lv_attention and lv_attention_weights calls every second CTA
    waits for copies (LV_HOLD_COPIES; only pages that are read by TMA are waited for), or for a pair's
    last product (LV_HOLD_PRODUCTS; the kernel of many rows), that are never counted as done, with
    a limit of limit_us (1000 to 1000000) a wait.  LV_HOLD_NONE: as usual again. */

@@ -18,6 +18,7 @@ constexpr int kCols = 128;                // rows of the step (packed) a product
 constexpr int kIndexThreads = 64;
 constexpr int kUnits = 8;                 // found ahead at most,
 constexpr int kAhead = 5;                 // where no more products than this are left to be issued
+constexpr long long kUnitWaits = 64;      // a wait for a unit, in those for copies: millions of rows may come before it
 constexpr float kLog2e = 1.44269504088896341f;
 
 template <int DP>
@@ -145,7 +146,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
   bool ok = true;
   Unit u;
   auto next_unit = [&]() -> bool {
-    if (!(ok = bar_wait(&bars, &bars.unit_full[unit_at], unit_par, a.wait_ns))) return false;
+    if (!(ok = bar_wait(&bars, &bars.unit_full[unit_at], unit_par, kUnitWaits * a.wait_ns))) return false;
     u = m.units[unit_at];
     warp_arrive(&bars.unit_empty[unit_at]);
     if (++unit_at == kUnits) {
@@ -448,7 +449,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       uint32_t k_par = 0, q_par = 0, s_par = 0;      // s_par: a bit for (buffer, half)
       auto products = [&]() -> bool {
         for (;;) {
-          if (!bar_wait1(&bars, &bars.unit_full[unit_at], unit_par, a.wait_ns)) return false;
+          if (!bar_wait1(&bars, &bars.unit_full[unit_at], unit_par, kUnitWaits * a.wait_ns)) return false;
           u = m.units[unit_at];
           bar_arrive(&bars.unit_empty[unit_at]);
           if (++unit_at == kUnits) {
