@@ -110,6 +110,7 @@ enum { LV_POLICY_NEXT_USE = 0, LV_POLICY_LRU = 1 };
    rows are written once, when their token is appended, so only the last,
    partially filled block of a session changes: lv_session_append and
    lv_make_resident drop that block's clean copy when they add rows to it.
+   (lv_kv_compact, which moves rows, drops those of the blocks it moves to.)
    Clean copies are not reclaimed for other blocks: the host tier should hold
    a slot for every block (with fewer, an eviction fails with LV_ERR_NO_HOST as
    in the exclusive mode). */
@@ -711,21 +712,21 @@ lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* fir
                         int32_t n, int32_t num_tokens, int32_t max_len, lv_stream stream);
 
 /* A prefix that several sessions share (the instructions in front of an assistant's talks) is held
-   once, by a session of its own, and the others' contexts continue it.  lv_batch_share makes
-   room, once, for steps of up to `rows` rows (1..max_tokens) with prefixes: rows * Hq sums of
-   head_dim (rounded up to 64, 128 or 256) 32-bit values.  LV_ERR_INVALID for a batch with a window or that has the room.
-   Synchronous, as lv_batch_create.
-   lv_batch_plan_shared plans a step as lv_batch_plan does, in which request i's rows also see the
-   first prefix_lens[i] tokens of session prefixes[i] (prefix_lens NULL: all it holds; prefixes[i] < 0
-   or no tokens: no prefix), as if they came before its own.  positions count from the prefix's begin;
-   kv_lens, tables and slots are of the request's own session.  Requests that follow one another and
-   continue the same tokens of the same session read them once, for all their rows and heads together.
-   lv_attention works on such a step in two or three launches.  Device-detected, with the request left out:
-   LV_ERR_BOUNDS for a prefix's session id or length out of range, LV_ERR_STATE for a block of it that
-   is not in HBM; it must stay where it is until the step's last call.  LV_ERR_INVALID for a batch
-   without room for num_tokens rows.  A captured lv_attention also keeps whether the plan before its capture was given
-   prefixes (and the kernel for them, chosen by whether num_tokens * Hq / H is above 16): after a plan of the other
-   kind it does nothing and reports LV_ERR_STATE with detail -1. */
+   once, by a session of its own, and the others' contexts continue it. lv_batch_share makes room,
+   once, for steps of up to `rows` rows (1..max_tokens) with prefixes: rows * Hq sums of head_dim
+   (rounded up to 64, 128 or 256) 32-bit values. LV_ERR_INVALID for a batch with a window or that has
+   the room. Synchronous, as lv_batch_create. lv_batch_plan_shared plans a step as lv_batch_plan does,
+   in which request i's rows also see the first prefix_lens[i] tokens of session prefixes[i]
+   (prefix_lens NULL: all it holds; prefixes[i] < 0 or no tokens: no prefix), as if they came before
+   its own. positions count from the prefix's begin; kv_lens, tables and slots are of the request's own
+   session. Requests that follow one another and continue the same tokens of the same session read them
+   once, for all their rows and heads together. lv_attention works on such a step in two or three
+   launches. Device-detected, with the request left out: LV_ERR_BOUNDS for a prefix's session id or
+   length out of range, LV_ERR_STATE for a block of it that is not in HBM; it must stay where it is
+   until the step's last call. LV_ERR_INVALID for a batch without room for num_tokens rows. A captured
+   lv_attention also keeps whether the plan before its capture was given prefixes (and the kernel for
+   them, chosen by whether num_tokens * Hq / H is above 16): after a plan of the other kind it does
+   nothing and reports LV_ERR_STATE with detail -1. */
 lv_status lv_batch_share(lv_batch* batch, int32_t rows);
 lv_status lv_batch_plan_shared(lv_batch* batch, const int32_t* sids, const int32_t* firsts, const int32_t* lens,
                                const int32_t* prefixes, const int32_t* prefix_lens, int32_t n, int32_t num_tokens,
@@ -766,50 +767,55 @@ typedef struct lv_weights {
   int32_t reserved;            /* must be 0 */
 } lv_weights;
 
-/* Adds up the attention weights that the cached tokens of `layer` get from the planned step's rows, after its
-   lv_attention: w[s][h][j] += sum of exp(scale * q[r][g] . k[j][h] - lse[r][g]) over the rows r of session s that
-   see token j and the query heads g of KV head h; for a row behind a prefix, the prefix's tokens too, in the row of the
-   session that holds them.  q, scale and lse are those of that call (lse is needed); last > 0: only the
-   last `last` rows of each request count (a prompt's end, say), 0: all.  A row whose lse is -inf has no weights.
-   weights: the layer's, with layer_stride not looked at (data is where the layer begins).  Sums are made in 32 bits, in an
-   order that does not change from call to call.  LV_ERR_INVALID as for lv_attention, and for last < 0.  Device-detected, and those weights
-   left as they are: LV_ERR_BOUNDS for a request (or one whose prefix has) more tokens than weights->tokens, LV_ERR_DOUBLE_MAP
-   for one whose session an earlier one of the step has (the first request's tokens are added; prefixes come
-   after all requests, and those of one session and length that do not follow one another count as several; the detail
-   is the request's index); LV_ERR_STATE with detail -1 where lv_kv_write reports it, and for a step whose attention
-   ran out of a wait; LV_ERR_TIMEOUT as lv_attention does, when some of the weights have been added. */
+/* Adds up the attention weights that the cached tokens of `layer` get from the planned step's rows,
+   after its lv_attention: w[s][h][j] += sum of exp(scale * q[r][g] . k[j][h] - lse[r][g]) over the
+   rows r of session s that see token j and the query heads g of KV head h; for a row behind a prefix,
+   the prefix's tokens too, in the row of the session that holds them. q, scale and lse are those of
+   that call (lse is needed); last > 0: only the last `last` rows of each request count (a prompt's
+   end, say), 0: all. A row whose lse is -inf has no weights. weights: the layer's, with layer_stride
+   not looked at (data is where the layer begins). Sums are made in 32 bits, in an order that does not
+   change from call to call. LV_ERR_INVALID as for lv_attention, and for last < 0. Device-detected, and
+   those weights left as they are: LV_ERR_BOUNDS for a request (or one whose prefix has) more tokens
+   than weights->tokens, LV_ERR_DOUBLE_MAP for one whose session an earlier one of the step has (the
+   first request's tokens are added; prefixes come after all requests, and those of one session and
+   length that do not follow one another count as several; the detail is the request's index);
+   LV_ERR_STATE with detail -1 where lv_kv_write reports it, and for a step whose attention ran out of
+   a wait; LV_ERR_TIMEOUT as lv_attention does, when some of the weights have been added. */
 lv_status lv_attention_weights(lv_batch* batch, int32_t layer, const lv_heads* q, const float* lse,
                                const lv_weights* weights, int32_t last, float scale, lv_stream stream);
 
 /* ------------------------------------- keeping a part of the cache */
 
-/* A long session may keep only the tokens that its queries look at: those whose attention weights add up to
-   most, for each layer and KV head its own.  lv_select_kept chooses them by weights that
+/* A long session may keep only the tokens that its queries look at: those whose attention weights add
+   up to most, for each layer and KV head its own. lv_select_kept chooses them by weights that
    lv_attention_weights (or the caller) adds up, lv_kv_compact moves their K and V to the front of the
-   session's pages, and lv_session_truncate gives the pages behind them back.  Attention does not depend on the
-   order of keys, and they stay in it; what it needs of their positions is in the K rows as they were written.  The
-   positions of later steps (lv_batch_plan) count the tokens that are left: a caller that rotates K and Q by
-   position adds the number of tokens evicted so far.  Not from the paper, which moves whole sessions. */
+   session's pages, and lv_session_truncate gives the pages behind them back. Attention does not depend
+   on the order of keys, and they stay in it; what it needs of their positions is in the K rows as they
+   were written. The positions of later steps (lv_batch_plan) count the tokens that are left: a caller
+   that rotates K and Q by position adds the number of tokens evicted so far. Not from the paper, which
+   moves whole sessions. */
 
-/* Chooses keeps[i] tokens of session sids[i] (all, where it has fewer) for each layer and KV head: the first `first`
-   of the context, as many of the last `last` as then fit, and of the others those of the largest weight,
-   the lowest position first where weights are equal (the zeros are; a NaN is above every number, and NaNs
-   are equal).  kept (int32 [n][num_layers][H][most]) receives their positions, ascending, and -1 behind them.
-   n is 0..4096; first, last >= 0; most 1..2^31 - 1.  Device-detected: LV_ERR_BOUNDS, with nothing kept, for a session id
-   or keeps[i] out of range (0..most) or a context longer than weights->tokens; the detail is the request's
-   index. */
+/* Chooses keeps[i] tokens of session sids[i] (all, where it has fewer) for each layer and KV head: the
+   first `first` of the context, as many of the last `last` as then fit, and of the others those of the
+   largest weight, the lowest position first where weights are equal (the zeros are; a NaN is above
+   every number, and NaNs are equal). kept (int32 [n][num_layers][H][most]) receives their positions,
+   ascending, and -1 behind them. n is 0..4096; first, last >= 0; most 1..2^31 - 1. Device-detected:
+   LV_ERR_BOUNDS, with nothing kept, for a session id or keeps[i] out of range (0..most) or a context
+   longer than weights->tokens; the detail is the request's index. */
 lv_status lv_select_kept(lv_pool* pool, const lv_weights* weights, const int32_t* sids, const int32_t* keeps,
                          int32_t n, int32_t first, int32_t last, int32_t* kept, int32_t most, lv_stream stream);
 
-/* Moves, in every layer and KV head, the K and V rows of tokens kept[i][layer][head][0..keeps[i]) of session sids[i]
-   to its tokens 0..keeps[i), and (weights not NULL) their weights with them, with zeros behind them up to the
-   context's end.  The lists ascend strictly and end within the context, whose blocks are all in HBM; keeps[i] at
-   or above the context's length moves nothing.  The context stays as long as it is, and rows behind keeps[i] as they
-   are; steps over these sessions, or behind them as prefixes, are planned anew.  Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE) are given up.  lens (int32 [n]) receives
-   what lv_session_truncate takes: min(keeps[i], context), or -1 for a request that was refused, of which
-   nothing moved.  n and most as above.  Device-detected: LV_ERR_BOUNDS for an id, a length or a list out of range,
-   LV_ERR_STATE for a block that is not in HBM, LV_ERR_DOUBLE_MAP for a session that an earlier request names;
-   the detail is the request's index. */
+/* Moves, in every layer and KV head, the K and V rows of tokens kept[i][layer][head][0..keeps[i]) of
+   session sids[i] to its tokens 0..keeps[i), and (weights not NULL) their weights with them, with
+   zeros behind them up to the context's end. The lists ascend strictly and end within the context,
+   whose blocks are all in HBM; keeps[i] at or above the context's length moves nothing. The context
+   stays as long as it is, and rows behind keeps[i] as they are; steps over these sessions, or behind
+   them as prefixes, are planned anew. Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE)
+   are given up. lens (int32 [n]) receives what lv_session_truncate takes: min(keeps[i], context), or
+   -1 for a request that was refused, of which nothing moved. n and most as above. Device-detected:
+   LV_ERR_BOUNDS for an id, a length or a list out of range, LV_ERR_STATE for a block that is not in
+   HBM, LV_ERR_DOUBLE_MAP for a session that an earlier request names; the detail is the request's
+   index. */
 lv_status lv_kv_compact(lv_pool* pool, const int32_t* sids, const int32_t* keeps, int32_t n, const int32_t* kept,
                         int32_t most, const lv_weights* weights, int32_t* lens, lv_stream stream);
 
