@@ -2226,7 +2226,7 @@ lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, co
   cudaStream_t s = as_stream(stream);
   const bool bf16 = b->d.dtype == LV_BF16;
   if (!b->box_rows) {
-    LV_TRY(lv::launch_weights_plain(a, bf16, pool->num_sms, s));
+    LV_TRY(lv::launch_weights_plain(a, bf16, b->dp, pool->num_sms, s));
     return LV_OK;
   }
   CUtensorMap qmap, few;

@@ -58,7 +58,7 @@ struct WeightMaps {
 };
 cudaError_t launch_weights_tc(const WeightArgs& a, const WeightMaps& m, bool bf16, int dp, int num_sms, cudaStream_t s);
 cudaError_t configure_weights_tc();
-cudaError_t launch_weights_plain(const WeightArgs& a, bool bf16, int num_sms, cudaStream_t s);
+cudaError_t launch_weights_plain(const WeightArgs& a, bool bf16, int dp, int num_sms, cudaStream_t s);
 cudaError_t configure_weights();
 constexpr int kMostSegments = 2 * 4096;
 
