@@ -9,6 +9,15 @@ both -- whose room in the context a turn or ``KVPool.append`` has made:
         batch.write(layer, k, v)
         out = batch.attention(layer, q)
 
+Sessions behind one long beginning continue a session that holds it (``prefix_rows`` and ``plan``'s
+``prefixes``: it is read once for all of them), and a cache that grows too long keeps the tokens that its
+rows have weighed most:
+
+        out, lse = batch.attention(layer, q, return_lse=True)
+        batch.add_weights(layer, q, lse, weights[layer])
+    ...
+    pool.evict_tokens(weights, sids, keeps)      # select_kept, compact and truncate
+
 ``row_starts``, ``kv_lens``, ``tables``, ``positions`` and ``slots`` are device tensors that
 ``plan`` fills.  A captured ``write`` or ``attention`` works on the step planned last when it is replayed;
 it keeps the rows and the attention's kernel (chosen from the rows a request) of the plan before its

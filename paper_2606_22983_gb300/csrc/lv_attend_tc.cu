@@ -823,8 +823,9 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 }
 
 // The pieces of a cut (prefix tile, head), joined in their order: a warp 32 rows and 16 columns of them, a lane a
-// row, four pieces' loads on their way at once (one after the other they took 18 us).  A pair of 512 rows behind 8192 keys is cut into 19 pieces: 20 MB for 4 heads, which the last CTAs to come
-// joined by themselves in some 10 us of 38; here all SMs read them.
+// row, four pieces' loads on their way at once (one after the other they took 18 us).  512 rows of each of 4 heads
+// behind 8192 keys are cut into 19 pieces a pair: 20 MB, which the last CTAs to come joined by themselves (76 us for
+// that attention, 64 as it is); here all SMs read them, in 11 us.
 constexpr int kJoinThreads = 128, kJoinCols = 16, kJoinPieces = 4;
 template <int DP>
 __global__ void __launch_bounds__(kJoinThreads) k_join_prefixes(const __grid_constant__ AttnArgs a) {

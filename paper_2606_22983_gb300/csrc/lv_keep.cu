@@ -212,9 +212,10 @@ __device__ __forceinline__ int warp_up(int x) {
 // until at most 32 share one, which a warp ranks.  False where it is not found so: the bounds do not hold it,
 // too many keys lie in them, or too many are equal at the border.
 //
-// What bounds it is instructions, not the list's bytes: so tokens are compared as numbers and told apart by
-// votes (some nine instructions for 32 of them), and a lane goes through the few set bits of a word by
-// itself.
+// What bounds it is instructions and the chain of barriers, not the list's bytes: so tokens are compared as numbers
+// and told apart by votes (some nine instructions for 32 of them), and a lane goes through the few set bits of a
+// word by itself.  12 sessions of 4000 to 30 000 tokens, 48 layers of 4 heads: 142 MB in 83 us in a graph, 1.7 TB/s, by
+// digits 296.  Samples of 1024 and 512: 91 and 113, as more lies between the bounds.
 __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, const OnceShared& o, int room) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int words = (t.n + 31) >> 5, batches = (t.n + 1023) >> 10;
@@ -391,6 +392,7 @@ __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, con
 
 // One list: a request's tokens in a layer and head.  Tokens before lo and from hi on stay,
 // and of those between the `need` of largest key.
+// 256 threads, six CTAs an SM: with 128, 512 and 64 threads a list the same lists took 96, 104 and 129 us.
 __global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_constant__ SelectArgs a, int n, int words) {
   __shared__ SelectShared sh;
   extern __shared__ uint32_t dyn[];
@@ -455,6 +457,7 @@ constexpr int kCheckThreads = 1024, kCheckCtas = 16;
 
 // Request blockIdx.x / kCheckCtas by a cluster: its session, that its blocks are in HBM, and its lists, which
 // have to ascend within the context.  lens[i] receives what it may be cut to, or -1 where nothing moves.
+// The lists are read once here and once by k_compact: a kernel that moved rows while it checked could stop half-way.
 __global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThreads, 1)
     k_compact_check(const __grid_constant__ CompactArgs a) {
   namespace cg = cooperative_groups;
@@ -505,6 +508,8 @@ __global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThrea
 // rows in order: as the lists ascend, kept[j] >= j, so a chunk whose loads come before its stores reads
 // nothing that an earlier one wrote over.  A row's vectors lie together; `parts` CTAs share them.  A chunk's
 // places are looked up (list, then table) while the chunk before it is on its way.
+// What bounds it: HBM, both ways.  4 sessions of 6000 to 14 000 tokens cut to a quarter in 48 layers of 4 heads of
+// 128, bf16: 1.9 GB in 329 us with the checks, 5.8 TB/s, 410 before the look-ups were taken ahead.
 constexpr int kMoveRows = 256;      // of a chunk at most
 template <typename V, int U>
 __global__ void __launch_bounds__(kMoveThreads, 4) k_compact(const __grid_constant__ CompactArgs a, int vecs, int part_vecs) {
@@ -668,7 +673,8 @@ cudaError_t launch_compact(const CompactArgs& a, int n, int row_bytes, int num_s
   if (e != cudaSuccess) return e;
   const int lists = a.p.J / 2 * a.H;
   const int vecs = row_bytes % 16 == 0 ? row_bytes / 16 : row_bytes;
-  // rows shared by several CTAs, down to 32 bytes of each, where there are few lists
+  // rows shared by several CTAs, down to 32 bytes of each, where there are few lists: the lists of one layer do not
+  // fill the SMs, and a list's rows have to be moved in order
   int part = vecs;
   if (row_bytes % 16 == 0)
     while (part > 2 && (int64_t)2 * lists * n * ((vecs + part - 1) / part) < 2 * num_sms) part = (part + 1) / 2;

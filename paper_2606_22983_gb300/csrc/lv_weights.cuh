@@ -80,7 +80,8 @@ struct Unit {
 };
 
 // Units are taken in kClasses goes, those that most rows see first, so that no long one begins last: a
-// segment's keys are seen by the fewer rows the later they are, so a class is a stretch of them.
+// segment's keys are seen by the fewer rows the later they are, so a class is a stretch of them.  (In the order of the
+// keys the last CTA of 4 prompts of 4096 had 1.66 times the mean's products.)
 constexpr int kClasses = 4;
 
 // What a CTA knows of the segments, divided among NT of its threads.
