@@ -57,6 +57,7 @@ class KVBatch:
         self.max_requests, self.max_tokens = max_requests, max_tokens
         self.num_tokens = 0
         self._shared = 0             # launches over the planned step's prefixes
+        self._max_rows = 0           # of a request or prefix in it
         self.handle = None
         i32 = dict(dtype=torch.int32, device=pool.device)
         rows, requests = max(max_tokens, 0), max(max_requests, 0)
@@ -152,9 +153,12 @@ class KVBatch:
         # rows, which takes them where there are more than one tile of the other's, in pages that TMA reads
         self._shared = 0
         if prefixes is not None and n > 0:
-            self._shared = 1 + (num_tokens * (self.q_heads // self.pool.kv_heads) > 16 and
-                                self.pool.T % 8 == 0 and self.pool.head_dim <= 128)
+            self._shared = 1 + (num_tokens * (self.q_heads // self.pool.kv_heads) > 16 and self._tiled())
+        self._max_rows = num_tokens if self._shared else min(max_len, num_tokens)
         self.pool.launches += 1 + (n > _PLAN_ONE_LAUNCH or self._shared > 0)
+
+    def _tiled(self):
+        return self.pool.T % 8 == 0 and self.pool.head_dim <= 128
 
     def _stream(self, stream):
         """The handle of a call's stream, and whether it is another than the current one."""
@@ -252,4 +256,7 @@ class KVBatch:
         if away or s not in self._used_on:
             self._use(s, q, lse, weights)
         lv.lv_attention_weights(self.handle, layer, q_arg, lse, w, last, self._scale if scale is None else scale, s)
-        self.pool.launches += 1
+        # (and the sums of tokens that many rows see, whose rows are shared out)
+        group = self.q_heads // self.pool.kv_heads
+        rows = min(last, self._max_rows) if last > 0 and not self._shared else self._max_rows
+        self.pool.launches += 1 + (self._tiled() and group <= 128 and rows * group > 512)

@@ -1664,6 +1664,7 @@ struct lv_batch {
   int32_t* arrived = nullptr;
   int32_t* ticket = nullptr;
   int32_t* unit_tickets = nullptr;      // lv_attention_weights
+  lv::CutUnit* cuts = nullptr;
   uint32_t* refused = nullptr;
   lv::StepHead* head = nullptr;
   float* part_o = nullptr;
@@ -1676,7 +1677,7 @@ struct lv_batch {
   std::vector<CUtensorMap> rows_maps;   // [2L], boxes of the rows kernel's units; empty: T has no whole ones
   // the planned step
   bool planned = false;
-  int32_t num_tokens = 0;
+  int32_t num_tokens = 0, max_len = 0;
   lv::AttnKind kind = lv::ATTN_ROWS;
   int32_t ctas = 0;
   // lv_batch_share: room for the sums over prefixes of share_rows rows, and the prefixes' line of work
@@ -1827,7 +1828,8 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
-        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->unit_tickets, 2)) != LV_OK ||
+        (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->unit_tickets, 3)) != LV_OK ||
+        (b->box_rows && (st = batch_alloc(b, &b->cuts, lv::kCutUnits)) != LV_OK) ||
         (st = batch_alloc(b, &b->refused, lv::kMostSegments / 32)) != LV_OK ||
         (st = batch_alloc(b, &b->head, 1)) != LV_OK ||
         (st = batch_alloc(b, &b->part_o, rows * b->dp)) != LV_OK ||
@@ -1838,7 +1840,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   }
   // (waits: the batch may be used on any stream next)
   if (cudaMemset(b->ticket, 0, sizeof(int32_t)) != cudaSuccess ||
-      cudaMemset(b->unit_tickets, 0, 2 * sizeof(int32_t)) != cudaSuccess ||
+      cudaMemset(b->unit_tickets, 0, 3 * sizeof(int32_t)) != cudaSuccess ||
       cudaMemset(b->head, 0xff, sizeof(lv::StepHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
     return fail(LV_ERR_CUDA);
   *out = b;
@@ -1950,6 +1952,7 @@ lv_status plan_step(lv_batch* b, const int32_t* sids, const int32_t* firsts, con
     LV_TRY(lv::launch_plan(a, s));
     b->planned = true;
     b->num_tokens = num_tokens;
+    b->max_len = max_len;
     b->kind = kind;
     b->ctas = a.own.ctas;
     b->shared = prefixes != nullptr;
@@ -2206,6 +2209,15 @@ lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, co
   a.head = b->head;
   a.tickets = b->unit_tickets;
   a.refused = b->refused;
+  // the memory of attention's pieces serves these, in the same stream order
+  const long long rows = b->shared ? b->num_tokens : last > 0 ? std::min(last, b->max_len) : b->max_len;
+  if (b->box_rows && b->G <= 128 && rows * b->G > lv::kCutRows) {      // (products begin at a token's first head)
+    a.cuts = b->cuts;
+    a.cut_count = b->unit_tickets + 2;
+    a.pieces = b->part_o;
+    a.cut_units = lv::kCutUnits;
+    a.cut_pieces = 2 * pool->num_sms * lv::kTcRows * b->dp / 256;
+  }
   a.q = static_cast<const uint8_t*>(q->data);
   a.q_row = q->row_stride;
   a.q_head = q->head_stride;

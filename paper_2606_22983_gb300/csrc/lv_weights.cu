@@ -58,10 +58,11 @@ __global__ void __launch_bounds__(kPlainThreads) k_weights_plain(const __grid_co
     return;
   }
   const int n = step.requests & (kSharedStep - 1);
-  const int units = index_segments<kPlainThreads, kPlainKeys>(a, step, x, reinterpret_cast<int*>(dyn));
+  const int units = index_segments<kPlainThreads, kPlainKeys, false>(a, step, x, reinterpret_cast<int*>(dyn), 0);
   const uint4 zero = make_uint4(0, 0, 0, 0);
   for (int i = blockIdx.x; i < units; i += gridDim.x) {
-    const Unit u = find_unit<kPlainThreads, kPlainKeys>(a, step, x, i);
+    int piece;
+    const Unit u = find_unit<kPlainThreads, kPlainKeys, false>(a, step, x, i, 0, piece);
     if (u.t0 >= u.t1) continue;
     __syncthreads();
 #pragma unroll 4

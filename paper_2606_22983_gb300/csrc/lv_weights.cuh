@@ -6,6 +6,12 @@
 
 namespace lv {
 
+// A unit whose rows several CTAs share: where its pieces' sums lie, and the weights that they go to.
+struct alignas(16) CutUnit {
+  float* w;
+  int32_t keys, pieces, piece0, pad[3];
+};
+
 struct WeightArgs {
   const uint8_t* k;        // the layer's K sub-page array
   int64_t P;
@@ -20,6 +26,10 @@ struct WeightArgs {
   const StepHead* head;
   int32_t* tickets;            // units given out, CTAs done; zero between calls
   uint32_t* refused;           // [kMostSegments / 32] a bit a segment (every CTA writes the same)
+  CutUnit* cuts;               // [cut_units]
+  int32_t* cut_count;          // of them
+  float* pieces;               // [cut_pieces][256] their sums
+  int32_t cut_units, cut_pieces;      // 0: none is cut
   const uint8_t* q;
   int64_t q_row, q_head;       // in elements
   const float* lse;            // [num_tokens][Hq]
@@ -62,10 +72,19 @@ cudaError_t launch_weights_plain(const WeightArgs& a, bool bf16, int dp, int num
 cudaError_t configure_weights();
 constexpr int kMostSegments = 2 * 4096;
 
+// The tensor-core kernel's units have pieces of about a kGoes-th of what a CTA has to do in all, and of kMinPiece
+// products at least; so none is cut where no key is seen by more than kCutRows rows (a product has 64 of them or more).
+// One prompt of 4096 with 4 KV heads is 64 units, of which the longest has 256 products and an SM 57 in all: 260 us
+// whole, 89 cut; 4 of them 283 and 264, 500 tokens at 16 000 keys 73 either way.  2 and 4 goes: 293 and 267 for the 4; with
+// 16 products at least 86 for the one at 4 goes, with 4 no change.
+constexpr int kGoes = 8, kMinPiece = 8, kCutRows = 64 * kMinPiece;
+constexpr int kCutUnits = 512;
+
 #ifdef __CUDACC__
 // The weights' work: a segment is the context of one request with the request's rows, or a prefix with the rows
 // of all that continue it; a unit is kKeys keys of a segment for one KV head, with all rows that see some of
-// them.  So every word of the weights belongs to one unit, whose sums are made in one order.
+// them.  So every word of the weights belongs to one unit, whose sums are made in one order.  Long units are cut into
+// pieces by rows, whose sums a second kernel adds up in their order.
 struct Segment {
   int first, tokens, qrow;     // position of its first row; its rows' tokens; the first of them in the step
   int keys;
@@ -89,7 +108,10 @@ template <int NT>
 struct SegmentIndex {
   int before[kClasses * NT + 1];             // units before thread t's segments in class c
   int ws[NT / 32];
-  int most;                                  // rows' tokens of a segment
+  int most, seen;                            // rows' tokens of a segment, and that see a unit's keys
+  int cuts[kClasses];                        // pieces of a unit of the class at most
+  int tickets[kClasses + 1];                 // pieces before the class
+  unsigned long long products;               // in all, about
 };
 
 __device__ __forceinline__ Segment segment_of(const WeightArgs& a, int n, int s) {
@@ -147,15 +169,31 @@ __device__ __forceinline__ int class_end(const Segment& g, int c, int most) {
   return g.req < 0 ? all : min(all, (int)(((long long)g.first + g.tokens - more_than + kKeys - 1) / kKeys));
 }
 
-// Every thread of the CTA (whole warps) calls it: fills x and returns the units in all.  first_of: room for a word a session.
+// How many tokens see some of `keys` keys, behind the sinks.
+__device__ __forceinline__ int most_seen(const WeightArgs& a, const Segment& g, int keys) {
+  if (g.req < 0) return g.tokens;
+  const int rows = a.last > 0 ? min(a.last, g.tokens) : g.tokens;
+  return a.window > 0 ? (int)min((long long)rows, (long long)a.window + keys) : rows;
+}
+// About how many products of step_rows rows a segment has.
+__device__ __forceinline__ unsigned long long products_of(const WeightArgs& a, const Segment& g, int rows, int keys, int step_rows) {
+  const float seen = (float)rows * (g.keys - (g.req < 0 || a.window > 0 ? 0.f : 0.5f * rows));
+  return (unsigned long long)(seen * a.H * a.G / ((float)keys * step_rows));
+}
+
+// Every thread of the CTA (whole warps) calls it: fills x and returns the units in all, or with kCut the pieces, of
+// products of step_rows rows.  first_of: room for a word a session.
 // The segments whose session an earlier one has, or that the weights have no room for, are refused (their
 // units are empty).
-template <int NT, int kKeys>
-__device__ int index_segments(const WeightArgs& a, const StepHead& step, SegmentIndex<NT>& x, int* first_of) {
+template <int NT, int kKeys, bool kCut>
+__device__ int index_segments(const WeightArgs& a, const StepHead& step, SegmentIndex<NT>& x, int* first_of, int step_rows) {
   const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
   const int tid = threadIdx.x, lane = tid & 31;
   for (int s = tid; s < a.S; s += blockDim.x) first_of[s] = kMostSegments;
-  if (tid == 0) x.most = 0;
+  if (tid == 0) {
+    x.most = x.seen = 0;
+    x.products = 0;
+  }
   __syncthreads();
   for (int s = tid; s < count; s += blockDim.x) {
     const Segment g = segment_of(a, n, s);
@@ -176,11 +214,29 @@ __device__ int index_segments(const WeightArgs& a, const StepHead& step, Segment
   }
   const int per = (count + NT - 1) / NT, s0 = min(tid * per, count), s1 = tid < NT ? min(s0 + per, count) : s0;
   int longest = 0;
-  for (int s = s0; s < s1; ++s) longest = max(longest, segment_of(a, n, s).tokens);
+  [[maybe_unused]] int seen = 0;
+  for (int s = s0; s < s1; ++s) {
+    const Segment g = segment_of(a, n, s);
+    longest = max(longest, g.tokens);
+    if constexpr (kCut) seen = max(seen, most_seen(a, g, kKeys));
+  }
   longest = __reduce_max_sync(0xffffffffu, longest);
   if (lane == 0 && longest) atomicMax(&x.most, longest);
+  if constexpr (kCut) {
+    seen = __reduce_max_sync(0xffffffffu, seen);
+    if (lane == 0 && seen) atomicMax(&x.seen, seen);
+  }
   __syncthreads();
   const int most = x.most;
+  const bool cuts = kCut && (long long)x.seen * a.G > (long long)step_rows * kMinPiece;
+  if (cuts) {
+    unsigned long long products = 0;
+    for (int s = s0; s < s1; ++s) {
+      const Segment g = segment_of(a, n, s);
+      products += products_of(a, g, most_seen(a, g, kKeys), kKeys, step_rows);
+    }
+    if (products) atomicAdd(&x.products, products);
+  }
   int total = 0;
 #pragma unroll 1
   for (int c = 0; c < kClasses; ++c) {
@@ -206,13 +262,51 @@ __device__ int index_segments(const WeightArgs& a, const StepHead& step, Segment
     __syncthreads();
   }
   if (tid == 0) x.before[0] = 0;
+  if (kCut && tid == 0) {
+    // the pieces of a class's longest unit, for all of them: a class that finds no room is left whole, as those behind
+    // it are, which are shorter
+    x.cuts[0] = 1;
+    x.tickets[kClasses] = total;
+    if (blockIdx.x == 0) *a.cut_count = 0;
+  }
+  if (tid == 0 && cuts) {
+    const long long goal = max((long long)kMinPiece, (long long)x.products / ((long long)gridDim.x * kGoes));
+    bool cut = true;
+    int units = 0, tickets = 0;
+    for (int c = 0; c < kClasses; ++c) {
+      const int here = x.before[(c + 1) * NT] - x.before[c * NT];
+      int cuts = 1;
+      if (cut) {
+        const long long rows = min((long long)most * (kClasses - c) / kClasses, (long long)x.seen) * a.G;
+        cuts = (int)min((rows + step_rows * goal - 1) / (step_rows * goal), 1024ll);
+        cut = cuts > 1 && units + here <= a.cut_units && tickets + (long long)here * cuts <= a.cut_pieces;
+        if (!cut) cuts = 1;
+      }
+      x.cuts[c] = cuts;
+      x.tickets[c] = tickets;
+      units += here;
+      if (cut && blockIdx.x == 0) *a.cut_count = units;
+      tickets += here * cuts;
+    }
+    x.tickets[kClasses] = tickets;
+  }
   __syncthreads();
-  return total;
+  return kCut ? x.tickets[kClasses] : total;
 }
 
-// Unit u of all; no tokens where there is nothing to do.
-template <int NT, int kKeys>
-__device__ __forceinline__ Unit find_unit(const WeightArgs& a, const StepHead& step, const SegmentIndex<NT>& x, int u) {
+// Unit or piece `ticket` of all; no tokens where there is nothing to do.  of: the piece of a cut unit, -1 of a whole one.
+template <int NT, int kKeys, bool kCut>
+__device__ __forceinline__ Unit find_unit(const WeightArgs& a, const StepHead& step, const SegmentIndex<NT>& x, int ticket,
+                                          int step_rows, int& of) {
+  of = -1;
+  int in = 0, cuts = kCut ? x.cuts[0] : 1, piece = 0, u = ticket;
+  if (kCut && cuts > 1) {
+    while (in + 1 < kClasses && ticket >= x.tickets[in + 1]) ++in;
+    cuts = x.cuts[in];
+    u = (ticket - x.tickets[in]) / cuts;
+    piece = ticket - x.tickets[in] - u * cuts;
+    u += x.before[in * NT];
+  }
   const int n = step.requests & (kSharedStep - 1), count = step.requests >= kSharedStep ? 2 * n : n;
   const int per = (count + NT - 1) / NT;
   int lo = 0, hi = kClasses * NT - 1;      // the last thread and class whose segments do not begin after u
@@ -234,6 +328,17 @@ __device__ __forceinline__ Unit find_unit(const WeightArgs& a, const StepHead& s
   const int tile = off / a.H;
   Unit out = unit_of(a, g, off - tile * a.H, (t0 + tile) * kKeys, kKeys);
   if (a.refused[s >> 5] >> (s & 31) & 1u) out.t1 = out.t0;
+  if (kCut && cuts > 1) {      // (its rows in pieces of whole products; the last ones may be none)
+    const int tokens = step_rows / a.G, products = max(0, out.t1 - out.t0 + tokens - 1) / tokens;
+    const int size = max((products + cuts - 1) / cuts, kMinPiece), pieces = (products + size - 1) / size;
+    if (piece == 0)
+      a.cuts[u] = CutUnit{a.w + g.sid * a.w_session + out.head * a.w_head + out.key0, min(kKeys, g.keys - out.key0),
+                          pieces > 1 ? pieces : 0, ticket, {}};
+    if (pieces > 1) of = ticket;
+    const long long t0 = out.t0 + (long long)piece * size * tokens;
+    out.t1 = (int)min((long long)out.t1, t0 + (long long)size * tokens);
+    out.t0 = (int)min(t0, (long long)out.t1);
+  }
   return out;
 }
 #endif

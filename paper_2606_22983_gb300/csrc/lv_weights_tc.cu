@@ -47,6 +47,7 @@ struct Misc {
   float part[kUnitKeys];
   volatile int issued;            // tiles of queries
   Unit units[kUnits];
+  int pieces[kUnits];             // find_unit's
   SegmentIndex<kIndexThreads> index;
 };
 static_assert(WShape<128>::kMisc + sizeof(Misc) <= 227 * 1024, "shared memory of a CTA");
@@ -71,9 +72,11 @@ struct Chunks {
 // What bounds it: few rows, the bytes of K: 61 single tokens over 2 to 16 k keys, 0.42 GB in 80 us, 5.3 TB/s.  Many
 // rows, the shared memory (both operands of S, 1024 wavefronts a product of 256 keys and 128 rows, the queries' copies,
 // and the rows' terms, which every warp reads) and what a product's scores wait for beside it: 4 prompts of
-// 4096, 32 query heads of 128, 281 us, where the tensor pipe is active 43 % of the time.  Terms read for a key
-// of each half at once (a thread 64 columns of both) took 311, as a half's scores then wait for the other's.
+// 4096, 32 query heads of 128, 264 us, 1.04 PFLOP/s.  Terms read for a key of each half at once (a thread 64 columns
+// of both) took a tenth more, as a half's scores then wait for the other's.
 //
+// kCut: units may come in pieces, some of a unit's rows each, whose sums k_weights_join adds up.  (A kernel of its own
+// for steps without: finding their units took 4 us more of 58 otherwise.)
 // One CTA an SM; units are taken in order from a counter, long ones (the first keys of a context, which
 // all rows see) first.
 //   warp 19  finds units ahead
@@ -81,7 +84,7 @@ struct Chunks {
 //   warp 17  K of its second half, and queries into a ring of their own
 //   warp 18  products into two buffers of TMEM for each half
 //   0 .. 15  the rows' terms, exponentials and sums, a thread a key in every second product
-template <int DP, bool kBf16>
+template <int DP, bool kBf16, bool kCut>
 __global__ void __launch_bounds__(kThreads, 1)
 k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUtensorMap kmap,
              const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap q_few, int box_rows, int few_rows,
@@ -140,20 +143,22 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
   if (!fits && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
   const int n = step.requests & (kSharedStep - 1);
   // (the sessions' words are in what the copies fill later)
-  const int units = fits ? index_segments<kIndexThreads, kUnitKeys>(a, step, m.index, reinterpret_cast<int*>(dyn)) : 0;
+  const int step_rows = a.G > kCols ? kCols : kCols / a.G * a.G;
+  const int units =
+      fits ? index_segments<kIndexThreads, kUnitKeys, kCut>(a, step, m.index, reinterpret_cast<int*>(dyn), step_rows) : 0;
   fence_async();
   __syncthreads();
-
-  const int step_rows = a.G > kCols ? kCols : kCols / a.G * a.G;
 
   // the units of the CTA in order, for a role: false at the end or where a wait ran out
   int unit_at = 0;
   uint32_t unit_par = 0;
   bool ok = true;
   Unit u;
+  int piece = -1;
   auto next_unit = [&]() -> bool {
     if (!(ok = bar_wait(&bars, &bars.unit_full[unit_at], unit_par, kUnitWaits * a.wait_ns))) return false;
     u = m.units[unit_at];
+    if constexpr (kCut) piece = m.pieces[unit_at];
     warp_arrive(&bars.unit_empty[unit_at]);
     if (++unit_at == kUnits) {
       unit_at = 0;
@@ -262,7 +267,9 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       // it and every second one from there, leave theirs
       const int next_turn = turn ^ (ch.count & 1);
       const bool joins = ch.count > 1, writes = buf != next_turn;
-      float* w = a.w + u.g.sid * a.w_session + u.head * a.w_head + key;
+      // (a piece's sums are added to the weights by k_weights_join)
+      const bool whole = !kCut || piece < 0;
+      float* w = whole ? a.w + u.g.sid * a.w_session + u.head * a.w_head + key : a.pieces + (int64_t)piece * kUnitKeys + kHalf * half + row;
       // the packed rows that see the key: from its own position on, to the window's end
       const bool all_see = u.g.req < 0, no_end = all_see || a.window == 0 || key < a.sinks, check_b = all_see && a.last > 0;
       auto row_of = [&](long long token) { return (int)(token < 0 ? 0 : token > u.g.tokens ? u.g.tokens : token) * a.G; };
@@ -362,7 +369,8 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
         part_par ^= 1;
       }
       // (one addition to the word in this call; nothing waits for it)
-      if (writes && mine && sum != 0.f) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(w), "f"(sum) : "memory");
+      if (!whole && writes && mine) __stcg(w, sum);
+      else if (writes && mine && sum != 0.f) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(w), "f"(sum) : "memory");
     }
     tc_fence_before();
   } else if (wid == kWarpK) {
@@ -544,7 +552,8 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       taken = __shfl_sync(0xffffffffu, t, 0);
       t = taken + lane;
       Unit x{};
-      if (lane < batch && t < units) x = find_unit<kIndexThreads, kUnitKeys>(a, step, m.index, t);
+      int of = -1;
+      if (lane < batch && t < units) x = find_unit<kIndexThreads, kUnitKeys, kCut>(a, step, m.index, t, step_rows, of);
       end = taken + batch > units || units == 0;
       const int products = x.t0 < x.t1 ? ((x.t1 - x.t0) * a.G + step_rows - 1) / step_rows : 0;
       x.products = products;
@@ -553,7 +562,10 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
         const int some = marker ? (int)end : __shfl_sync(0xffffffffu, products, j & 31);
         if (!some) continue;
         if (!(ok = bar_wait(&bars, &bars.unit_empty[at], ~par & 1u, a.wait_ns))) break;
-        if (lane == (marker ? 0 : j)) m.units[at] = marker ? Unit{} : x;
+        if (lane == (marker ? 0 : j)) {
+          m.units[at] = marker ? Unit{} : x;
+          if constexpr (kCut) m.pieces[at] = of;
+        }
         warp_arrive(&bars.unit_full[at]);
         handed += marker ? 0 : some;
         if (++at == kUnits) {
@@ -587,18 +599,33 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
 template <int DP, bool kBf16>
 cudaError_t run(const WeightArgs& a, const WeightMaps& m, int ctas, cudaStream_t s) {
   static const CUtensorMap none{};
-  return launch_dependent(k_weights_tc<DP, kBf16>, dim3(ctas), kThreads, WShape<DP>::kMisc + sizeof(Misc), s, a, *m.k,
+  return launch_dependent(a.cut_units ? k_weights_tc<DP, kBf16, true> : k_weights_tc<DP, kBf16, false>, dim3(ctas), kThreads, WShape<DP>::kMisc + sizeof(Misc), s, a, *m.k,
                           m.q ? *m.q : none, m.q_few ? *m.q_few : none, m.box_rows, m.few_rows, m.q ? 1 : 0);
 }
 
 template <int DP>
 cudaError_t set() {
-  for (auto k : {k_weights_tc<DP, true>, k_weights_tc<DP, false>}) {
+  for (auto k : {k_weights_tc<DP, true, true>, k_weights_tc<DP, true, false>, k_weights_tc<DP, false, true>,
+                 k_weights_tc<DP, false, false>}) {
     const cudaError_t e =
         cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, WShape<DP>::kMisc + (int)sizeof(Misc));
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
+}
+
+// w[j] += the sums of a cut unit's pieces, in their order: a CTA a unit, a thread a key.
+__global__ void __launch_bounds__(kUnitKeys) k_weights_join(const __grid_constant__ WeightArgs a) {
+  dep_wait();
+  const StepHead step = load_words(a.head);
+  if (step.kind < 0 || step.num_tokens > a.num_tokens || (int)blockIdx.x >= *a.cut_count) return;
+  const CutUnit c = load_words(&a.cuts[blockIdx.x]);
+  if ((int)threadIdx.x >= c.keys) return;
+  const float* x = a.pieces + (int64_t)c.piece0 * kUnitKeys + threadIdx.x;
+  LongSum sum;
+#pragma unroll 4
+  for (int i = 0; i < c.pieces; ++i) sum.add(__ldcg(x + (int64_t)i * kUnitKeys));
+  if (sum.sum != 0.f) c.w[threadIdx.x] += sum.sum;
 }
 
 }  // namespace
@@ -609,8 +636,10 @@ cudaError_t configure_weights_tc() {
 }
 
 cudaError_t launch_weights_tc(const WeightArgs& a, const WeightMaps& m, bool bf16, int dp, int num_sms, cudaStream_t s) {
-  if (dp == 64) return bf16 ? run<64, true>(a, m, num_sms, s) : run<64, false>(a, m, num_sms, s);
-  return bf16 ? run<128, true>(a, m, num_sms, s) : run<128, false>(a, m, num_sms, s);
+  const cudaError_t e = dp == 64 ? (bf16 ? run<64, true>(a, m, num_sms, s) : run<64, false>(a, m, num_sms, s))
+                                 : (bf16 ? run<128, true>(a, m, num_sms, s) : run<128, false>(a, m, num_sms, s));
+  if (e != cudaSuccess || !a.cut_units) return e;
+  return launch_dependent(k_weights_join, dim3(a.cut_units), kUnitKeys, 0, s, a);
 }
 
 }  // namespace lv

@@ -397,3 +397,58 @@ def test_waits_that_run_out(new, what):
         _run(s)
     finally:
         s.close()
+
+
+CUT = {
+    "prompt": dict(cached=[0], new=[3000], heads=1, group=8, dim=64),
+    "chunks": dict(cached=[5000, 40, 0], new=[700, 1, 2100], heads=2, group=4, dim=128, dtype="float16"),
+    "short": dict(cached=[100], new=[2500], heads=1, group=48, dim=64, page=8),
+    "tail": dict(cached=[0, 300], new=[2600, 900], heads=1, group=16, dim=64, last=500),
+    "window": dict(cached=[0, 20], new=[2300, 1700], heads=2, group=7, dim=64, window=600, sinks=3),
+    "beside": dict(cached=[(97 * i) % 1500 for i in range(200)] + [0], new=[1] * 200 + [1500], heads=1, group=16, dim=64),
+}
+
+
+@pytest.mark.parametrize("step", CUT)
+def test_cut_units(step):
+    """Keys that many rows see, shared out by rows; the sums are the same bit for bit each time."""
+    import torch
+    c = dict(CUT[step])
+    last = c.pop("last", 0)
+    s = Step(c.pop("cached"), c.pop("new"), **{**c, "dtype": getattr(torch, c.get("dtype", "bfloat16"))})
+    try:
+        w, lse, before = _run(s, last=last)
+        for _ in range(3):
+            again = before.clone()
+            s.batch.add_weights(1, s.q, lse, again, last=last, scale=s.dim ** -0.5)
+            s.batch.attention(1, s.q, scale=s.dim ** -0.5)      # (it counts and joins in the same memory)
+            assert torch.equal(again, w)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("last", [0, 300])
+def test_cut_prefixes(last):
+    s = SharedStep(cached=[0, 100, 17, 5], new=[500, 433, 860, 1], of=[0, 0, 0, 1], prefix=[391, 128], heads=1, group=16, dim=64)
+    try:
+        _run(s, last=last)
+    finally:
+        s.close()
+
+
+def test_cut_units_after_a_wait_that_ran_out():
+    """Pieces that came before a wait ran out are not counted in the next step."""
+    from paper_2606_22983_gb300 import lv
+    s = Step([0], [2500], heads=1, group=16, dim=64)
+    try:
+        s.plan()
+        _, lse = s.batch.attention(0, s.q, return_lse=True)
+        for what in (lv.LV_HOLD_COPIES, lv.LV_HOLD_PRODUCTS):
+            lv.lv_selftest_attention(s.batch.handle, what, 2000)
+            s.batch.add_weights(0, s.q, lse, _weights(s))
+            assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_TIMEOUT
+            s.pool.clear_error()
+            lv.lv_selftest_attention(s.batch.handle, lv.LV_HOLD_NONE)
+            _run(s)
+    finally:
+        s.close()
