@@ -256,7 +256,7 @@ class KVBatch:
         if away or s not in self._used_on:
             self._use(s, q, lse, weights)
         lv.lv_attention_weights(self.handle, layer, q_arg, lse, w, last, self._scale if scale is None else scale, s)
-        # (and the sums of tokens that many rows see, whose rows are shared out)
+        # (and the sums of tokens that more than eight products' rows see, which are shared out)
         group = self.q_heads // self.pool.kv_heads
         rows = min(last, self._max_rows) if last > 0 and not self._shared else self._max_rows
-        self.pool.launches += 1 + (self._tiled() and group <= 128 and rows * group > 512)
+        self.pool.launches += 1 + (self._tiled() and group <= 128 and rows > 128 // group * 8)

@@ -2211,7 +2211,7 @@ lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, co
   a.refused = b->refused;
   // the memory of attention's pieces serves these, in the same stream order
   const long long rows = b->shared ? b->num_tokens : last > 0 ? std::min(last, b->max_len) : b->max_len;
-  if (b->box_rows && b->G <= 128 && rows * b->G > lv::kCutRows) {      // (products begin at a token's first head)
+  if (b->box_rows && b->G <= 128 && rows * b->G > lv::product_rows(b->G) * lv::kMinPiece) {      // (whole tokens)
     a.cuts = b->cuts;
     a.cut_count = b->unit_tickets + 2;
     a.pieces = b->part_o;

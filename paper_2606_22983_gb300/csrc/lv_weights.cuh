@@ -73,12 +73,13 @@ cudaError_t configure_weights();
 constexpr int kMostSegments = 2 * 4096;
 
 // The tensor-core kernel's units have pieces of about a kGoes-th of what a CTA has to do in all, and of kMinPiece
-// products at least; so none is cut where no key is seen by more than kCutRows rows (a product has 64 of them or more).
+// products at least.
 // One prompt of 4096 with 4 KV heads is 64 units, of which the longest has 256 products and an SM 57 in all: 260 us
 // whole, 89 cut; 4 of them 283 and 264, 500 tokens at 16 000 keys 73 either way.  2 and 4 goes: 293 and 267 for the 4; with
 // 16 products at least 86 for the one at 4 goes, with 4 no change.
-constexpr int kGoes = 8, kMinPiece = 8, kCutRows = 64 * kMinPiece;
-constexpr int kCutUnits = 512;
+constexpr int kGoes = 8, kMinPiece = 8, kCutUnits = 512;
+// Packed rows of a product, whole tokens of G.
+__host__ __device__ constexpr int product_rows(int G) { return G > 128 ? 128 : 128 / G * G; }
 
 #ifdef __CUDACC__
 // The weights' work: a segment is the context of one request with the request's rows, or a prefix with the rows

@@ -143,7 +143,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
   if (!fits && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
   const int n = step.requests & (kSharedStep - 1);
   // (the sessions' words are in what the copies fill later)
-  const int step_rows = a.G > kCols ? kCols : kCols / a.G * a.G;
+  const int step_rows = product_rows(a.G);
   const int units =
       fits ? index_segments<kIndexThreads, kUnitKeys, kCut>(a, step, m.index, reinterpret_cast<int*>(dyn), step_rows) : 0;
   fence_async();

@@ -452,3 +452,41 @@ def test_cut_units_after_a_wait_that_ran_out():
             _run(s)
     finally:
         s.close()
+
+
+def test_replayed_with_other_lengths():
+    """A captured call takes a step of shorter or longer requests than the one before its capture: units that it does
+    not cut, and cuts where there are none, give the weights all the same."""
+    import torch
+    s = Step([0, 40], [1200, 3], heads=1, group=16, dim=64)
+    try:
+        side, lse = torch.cuda.Stream(), torch.empty((s.rows, 16), device="cuda")
+        steps = {"long": (np.array([1200, 3], np.int32), 1200), "short": (np.array([2, 3], np.int32), 3)}
+        graphs, w = {}, torch.zeros_like(_weights(s))
+
+        def plan(name):
+            new, most = steps[name]
+            s.batch.plan(s.sids, new, num_tokens=s.rows, max_len=most)
+            lse.copy_(s.batch.attention(0, s.q, return_lse=True)[1])
+
+        for name in steps:
+            plan(name)
+            torch.cuda.synchronize()
+            graphs[name] = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graphs[name], stream=side):
+                s.batch.add_weights(0, s.q, lse, w)
+        for name in ("long", "short", "long"):
+            plan(name)
+            want = torch.zeros_like(w)
+            s.batch.add_weights(0, s.q, lse, want)
+            for captured, graph in graphs.items():
+                w.zero_()
+                graph.replay()
+                assert s.pool.sync(raise_on_error=False) == 0
+                if captured == name or name == "short":
+                    assert torch.equal(w, want)
+                else:      # (the same products' sums, added up in another order: a few roundings of 2^-24, as all are
+                    # positive and what an addition loses is kept)
+                    assert (w - want).abs().le(2.0 ** -20 * want).all()
+    finally:
+        s.close()
