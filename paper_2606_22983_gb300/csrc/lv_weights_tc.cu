@@ -70,10 +70,10 @@ struct Chunks {
 // as it reads it from TMEM, and writes one word at the end.  No maximum is needed, as the sums are known, and no V.
 //
 // What bounds it: few rows, the bytes of K: 61 single tokens over 2 to 16 k keys, 0.42 GB in 80 us, 5.3 TB/s.  Many
-// rows, the shared memory (both operands of S, 1024 wavefronts a product of 256 keys and 128 rows, the queries' copies,
-// and the rows' terms, which every warp reads) and what a product's scores wait for beside it: 4 prompts of
-// 4096, 32 query heads of 128, 264 us, 1.04 PFLOP/s.  Terms read for a key of each half at once (a thread 64 columns
-// of both) took a tenth more, as a half's scores then wait for the other's.
+// rows, products and sums that wait for one another, a product of 256 keys and 128 rows some 2100 cycles (the tensor
+// pipe active 49 % of them, issue 53 %, shared memory by the tensor core 46 % and by threads 41 %): 4 prompts of 4096, 32
+// query heads of 128, 264 us, 1.04 PFLOP/s.  Terms read for a key of each half at once (a thread 64 columns of both)
+// took a tenth more, as a half's scores then wait for the other's.
 //
 // kCut: units may come in pieces, some of a unit's rows each, whose sums k_weights_join adds up.  (A kernel of its own
 // for steps without: finding their units took 4 us more of 58 otherwise.)
