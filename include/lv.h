@@ -779,8 +779,11 @@ typedef struct lv_weights {
    than weights->tokens, LV_ERR_DOUBLE_MAP for one whose session an earlier one of the step has (the
    first request's tokens are added; prefixes come after all requests, and those of one session and
    length that do not follow one another count as several; the detail is the request's index);
-   LV_ERR_STATE with detail -1 where lv_kv_write reports it, and for a step whose attention ran out of
-   a wait; LV_ERR_TIMEOUT as lv_attention does, when some of the weights have been added. */
+   LV_ERR_STATE with detail -1, and nothing added, where lv_kv_write reports it, for a step whose
+   attention ran out of a wait, and where the last lv_attention on the step did nothing (a captured one
+   that was replayed after a plan of another kind): there is no lse of this step then. A captured call
+   keeps num_tokens, and works on the step of any plan of no more rows whose attention has run.
+   LV_ERR_TIMEOUT as lv_attention does, when some of the weights have been added. */
 lv_status lv_attention_weights(lv_batch* batch, int32_t layer, const lv_heads* q, const float* lse,
                                const lv_weights* weights, int32_t last, float scale, lv_stream stream);
 

@@ -1664,6 +1664,7 @@ struct lv_batch {
   int32_t* arrived = nullptr;
   int32_t* ticket = nullptr;
   int32_t* unit_tickets = nullptr;      // lv_attention_weights
+  int32_t* no_lse = nullptr;            // whether the last attention on the step did nothing
   lv::CutUnit* cuts = nullptr;
   uint32_t* refused = nullptr;
   lv::StepHead* head = nullptr;
@@ -1829,6 +1830,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
         (st = batch_alloc(b, &b->ticket, 1)) != LV_OK || (st = batch_alloc(b, &b->unit_tickets, 3)) != LV_OK ||
+        (st = batch_alloc(b, &b->no_lse, 1)) != LV_OK ||
         (b->box_rows && (st = batch_alloc(b, &b->cuts, lv::kCutUnits)) != LV_OK) ||
         (st = batch_alloc(b, &b->refused, lv::kMostSegments / 32)) != LV_OK ||
         (st = batch_alloc(b, &b->head, 1)) != LV_OK ||
@@ -1841,6 +1843,7 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   // (waits: the batch may be used on any stream next)
   if (cudaMemset(b->ticket, 0, sizeof(int32_t)) != cudaSuccess ||
       cudaMemset(b->unit_tickets, 0, 3 * sizeof(int32_t)) != cudaSuccess ||
+      cudaMemset(b->no_lse, 0, sizeof(int32_t)) != cudaSuccess ||
       cudaMemset(b->head, 0xff, sizeof(lv::StepHead)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
     return fail(LV_ERR_CUDA);
   *out = b;
@@ -1886,6 +1889,7 @@ lv::PlanLine line_of(const lv_batch* b, lv::AttnKind kind, int32_t num_tokens) {
   a.work = b->work;
   a.arrived = b->arrived;
   a.head = b->head;
+  a.no_lse = b->no_lse;
   return a;
 }
 
@@ -1947,6 +1951,7 @@ lv_status plan_step(lv_batch* b, const int32_t* sids, const int32_t* firsts, con
       a.pre.tiles = b->pre_tiles;
       a.pre.work = b->pre_work;
       a.pre.head = b->pre_head;
+      a.pre.no_lse = nullptr;
     }
     b->planned = false;      // (the old step's arrays are being written over)
     LV_TRY(lv::launch_plan(a, s));
@@ -2144,6 +2149,7 @@ lv_status lv_attention(lv_batch* b, int32_t layer, const lv_heads* q, const lv_h
   a.ctl = pool->d.ctl;
   a.wait_ns = b->wait_ns;
   a.hold = b->hold;
+  a.no_lse = b->no_lse;
   CUtensorMap qmap;
   const bool any_tc = b->kind == lv::ATTN_TC || (b->shared && b->pre_kind == lv::ATTN_TC);
   const bool q_tma = any_tc && a.q_vec && query_map(b, q, &qmap);
@@ -2235,6 +2241,7 @@ lv_status lv_attention_weights(lv_batch* b, int32_t layer, const lv_heads* q, co
   a.wait_ns = b->wait_ns;
   a.hold = b->hold;
   a.head_out = b->head;
+  a.no_lse = b->no_lse;
   cudaStream_t s = as_stream(stream);
   const bool bf16 = b->d.dtype == LV_BF16;
   if (!b->box_rows) {

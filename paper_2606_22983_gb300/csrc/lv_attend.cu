@@ -280,10 +280,9 @@ k_attend_rows(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtens
   const int group = blockIdx.x / a.H, head = blockIdx.x - group * a.H;
   const CtaWork work = load_words(&a.work[group]);
   const StepHead step = load_words(a.head);
-  if (LV_RARE(!step_fits<kMode>(a, step, ATTN_ROWS))) {
-    if (kMode != kPrefix && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
-    return;
-  }
+  const bool fits = step_fits<kMode>(a, step, ATTN_ROWS);
+  if (kMode != kPrefix && blockIdx.x == 0 && threadIdx.x == 0) tell(a, fits);
+  if (LV_RARE(!fits)) return;
   const bool dead = kMode != kPrefix && step.live < a.num_tokens;
   auto req_of = [&](const AttnTile& t) { return (size_t)(kMode == kJoined ? t.req & (kSharedTile - 1) : t.req); };
   auto key_of = [&](const AttnTile& t, int u) { return (u < t.sink_units ? u : t.win_unit + u - t.sink_units) * kU; };

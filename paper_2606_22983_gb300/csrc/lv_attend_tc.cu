@@ -797,7 +797,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       // rows of no request
       const StepHead step = load_words(a.head);
       const bool fits = kMode != kPrefix && step_fits<kMode>(a, step, ATTN_TC);
-      if (kMode != kPrefix && LV_RARE(!fits) && blockIdx.x == 0 && lane == 0) report(a.ctl, LV_ERR_STATE, -1);
+      if (kMode != kPrefix && blockIdx.x == 0 && lane == 0) tell(a, fits);
       if (ok && fits && step.live < a.num_tokens) {
         const int Hq = a.H * a.G;
         for (int r = blockIdx.x; r < a.num_tokens; r += gridDim.x) {

@@ -143,7 +143,10 @@ __device__ __forceinline__ void cut_line(const PlanLine& a, int n, int requests,
   const int lead = apart ? -1 : a.lead, size = cut_free ? a.uncut : a.min_share;
   units = apart ? needed * size * a.line_heads : (units + (long long)n_tiles * lead) * a.line_heads;
   const long long share = apart ? size : max((units + a.shares - 1) / a.shares, (long long)a.min_share);
-  if (threadIdx.x == 0) *a.head = StepHead{a.kind, a.num_tokens, (int)live, kGroups ? n_tiles : requests};
+  if (threadIdx.x == 0) {
+    *a.head = StepHead{a.kind, a.num_tokens, (int)live, kGroups ? n_tiles : requests};
+    if (!kGroups) *a.no_lse = 0;
+  }
   // (zero already but after an attention that ran out of a wait)
   static_assert(kArriveWords % 4 == 0, "cleared by 16 bytes");
   for (int i = threadIdx.x; i < a.ctas * (kArriveWords / 4); i += NT)

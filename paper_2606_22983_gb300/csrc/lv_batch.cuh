@@ -91,6 +91,7 @@ struct PlanLine {
   CtaWork* work;           // [shares]
   int32_t* arrived;        // [ctas][kArriveWords] pieces of cut pairs that are done, all zero between calls
   StepHead* head;
+  int32_t* no_lse;         // the step's, set to zero with its line (null: the prefixes' line)
 };
 
 struct PlanArgs {
@@ -153,6 +154,7 @@ struct AttnArgs {
   long long* ctl;
   long long wait_ns;       // of each wait on a copy or a product
   int32_t hold;            // LV_HOLD_NONE but in a self-test
+  int32_t* no_lse;         // one where the last attention on the step did nothing, so that its lse is no sum of the step's
   // steps behind prefixes (kPrefix, kJoined)
   const StepHead* own_head;     // the step's, where head is the prefixes'
   const StepHead* pre_head;     // and the prefixes', with the kernel that attended over them
@@ -270,6 +272,11 @@ __device__ __forceinline__ bool step_fits(const AttnArgs& a, const StepHead& hea
   }
   const StepHead own = load_words(a.own_head);
   return fits && own.requests >= kSharedStep && own.kind >= 0 && own.num_tokens == head.num_tokens;
+}
+// For one thread: whether the attention works on the step, for those who read its lse; a report where it does not.
+__device__ __forceinline__ void tell(const AttnArgs& a, bool fits) {
+  *a.no_lse = !fits;
+  if (LV_RARE(!fits)) report(a.ctl, LV_ERR_STATE, -1);
 }
 // Four columns from `col` on of the prefix's sums of packed row g of the step's row r; their maximum and weight.
 __device__ __forceinline__ float4* pre_at(const AttnArgs& a, int head, int col, int64_t r, int g) {

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_weights_plain(const __grid_co
   dep_wait();
   dep_trigger();
   const StepHead step = load_words(a.head);
-  if (step.kind < 0 || step.num_tokens > a.num_tokens) {
+  if (!weights_fit(a, step)) {
     if (blockIdx.x == 0 && tid == 0) report(a.ctl, LV_ERR_STATE, -1);
     return;
   }

@@ -43,6 +43,7 @@ struct WeightArgs {
   long long wait_ns;
   int32_t hold;                // LV_HOLD_NONE but in a self-test
   StepHead* head_out;          // the same head, for a wait that ran out
+  const int32_t* no_lse;       // one where the last attention on the step did nothing
 };
 
 // Sums of many terms in 32 bits: what the additions lose is kept beside them (Kahan), so that the sum's error
@@ -114,6 +115,12 @@ struct SegmentIndex {
   int tickets[kClasses + 1];                 // pieces before the class
   unsigned long long products;               // in all, about
 };
+
+// Whether the step on the device is one that the call may work on, and its last attention ran (one that was refused, or
+// that gave up over the prefixes, has left the lse of another step or none).
+__device__ __forceinline__ bool weights_fit(const WeightArgs& a, const StepHead& step) {
+  return step.kind >= 0 && step.num_tokens <= a.num_tokens && *a.no_lse == 0;
+}
 
 __device__ __forceinline__ Segment segment_of(const WeightArgs& a, int n, int s) {
   const bool pre = s >= n;

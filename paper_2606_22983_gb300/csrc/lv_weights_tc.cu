@@ -139,7 +139,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
   dep_wait();
 
   const StepHead step = load_words(a.head);
-  const bool fits = step.kind >= 0 && step.num_tokens <= a.num_tokens;
+  const bool fits = weights_fit(a, step);
   if (!fits && blockIdx.x == 0 && threadIdx.x == 0) report(a.ctl, LV_ERR_STATE, -1);
   const int n = step.requests & (kSharedStep - 1);
   // (the sessions' words are in what the copies fill later)
@@ -618,7 +618,7 @@ cudaError_t set() {
 __global__ void __launch_bounds__(kUnitKeys) k_weights_join(const __grid_constant__ WeightArgs a) {
   dep_wait();
   const StepHead step = load_words(a.head);
-  if (step.kind < 0 || step.num_tokens > a.num_tokens || (int)blockIdx.x >= *a.cut_count) return;
+  if (!weights_fit(a, step) || (int)blockIdx.x >= *a.cut_count) return;
   const CutUnit c = load_words(&a.cuts[blockIdx.x]);
   if ((int)threadIdx.x >= c.keys) return;
   const float* x = a.pieces + (int64_t)c.piece0 * kUnitKeys + threadIdx.x;

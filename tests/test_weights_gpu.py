@@ -490,3 +490,84 @@ def test_replayed_with_other_lengths():
                     assert (w - want).abs().le(2.0 ** -20 * want).all()
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("new", [[1, 1], [300, 1]])
+def test_after_a_wait_that_ran_out_over_a_prefix(new):
+    """The attention has left no sums then: nothing is added until the step is planned again."""
+    from paper_2606_22983_gb300 import lv
+    s = SharedStep([200, 30], new, [0, 0], [3000], heads=2, group=4, dim=64)
+    try:
+        s.plan()
+        lv.lv_selftest_attention(s.batch.handle, lv.LV_HOLD_COPIES, 2000)
+        _, lse = s.batch.attention(0, s.q, return_lse=True)
+        lv.lv_selftest_attention(s.batch.handle, lv.LV_HOLD_NONE)
+        assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_TIMEOUT
+        s.pool.clear_error()
+        lse.zero_()
+        w = _weights(s)
+        before = w.clone()
+        for _ in range(2):
+            s.batch.add_weights(0, s.q, lse, w)
+            assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE and s.pool.stats()["error_detail"] == -1
+            s.pool.clear_error()
+            assert (w == before).all()
+            s.batch.attention(0, s.q)
+            assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE
+            s.pool.clear_error()
+        _run(s)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("captured", ["prefix", "none", "long", "short"])
+def test_replayed_behind_an_attention_that_is_refused(captured):
+    """Attention and weights in one graph, replayed after a plan whose attention is another: the attention leaves the sums
+    of the step before, and nothing is added; after a plan of its own kind the graph works again, as calls outside it do."""
+    import torch
+    from paper_2606_22983_gb300 import lv
+    s = SharedStep([200, 900], [300, 1], [0, 0], [600], heads=2, group=4, dim=64)
+    try:
+        sids = s.sids[:2]
+        new = np.array([300, 1], np.int32)
+
+        def plan(kind):
+            if kind == "prefix":
+                s.plan()
+            else:
+                s.batch.plan(sids, new if kind != "short" else np.array([2, 1], np.int32), num_tokens=s.rows,
+                             max_len=2 if kind == "short" else 300)
+
+        def both():
+            _, lse = s.batch.attention(0, s.q, scale=0.125, return_lse=True)
+            s.batch.add_weights(0, s.q, lse, w, scale=0.125)
+
+        w, side = _weights(s), torch.cuda.Stream()
+        before = w.clone()
+        plan(captured)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            both()
+        graph.replay()
+        assert s.pool.sync(raise_on_error=False) == 0
+        want = w.clone()
+        assert not torch.equal(want, before)
+        for other in {"prefix": ("long", "short"), "none": ("prefix", "short"), "long": ("short",), "short": ("long", "prefix")}[captured]:
+            plan(other)
+            w.copy_(before)
+            graph.replay()
+            assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE and s.pool.stats()["error_detail"] == -1
+            s.pool.clear_error()
+            assert torch.equal(w, before)
+            both()                               # (an attention that runs is followed by its weights)
+            assert s.pool.sync(raise_on_error=False) == 0 and not torch.equal(w, before)
+            graph.replay()
+            assert s.pool.sync(raise_on_error=False) == lv.LV_ERR_STATE
+            s.pool.clear_error()
+            plan(captured)                       # a new plan's sums may come from elsewhere
+            w.copy_(before)
+            graph.replay()
+            assert s.pool.sync(raise_on_error=False) == 0 and torch.equal(w, want)
+    finally:
+        s.close()
