@@ -1681,9 +1681,9 @@ struct lv_batch {
   int32_t num_tokens = 0, max_len = 0;
   lv::AttnKind kind = lv::ATTN_ROWS;
   int32_t ctas = 0;
+  lv::PlanReq* pre_reqs = nullptr;
   // lv_batch_share: room for the sums over prefixes of share_rows rows, and the prefixes' line of work
   int32_t share_rows = 0;
-  lv::PlanReq* pre_reqs = nullptr;
   int2* continued = nullptr;
   lv::AttnTile* pre_tiles = nullptr;
   lv::CtaWork* pre_work = nullptr;
@@ -1825,7 +1825,10 @@ lv_status create_batch(lv_pool* pool, const lv_batch_desc* d, lv_batch** out) {
   size_t rows = (size_t)2 * rows_ctas(b) * lv::kRowsRows;
   if (b->box_rows) rows = std::max(rows, (size_t)2 * pool->num_sms * lv::kTcRows);
   try {
+    // (pre_reqs from the begin: a captured lv_attention_weights keeps its place, and may be replayed after a plan
+    // with prefixes that lv_batch_share has made room for since)
     if ((st = batch_alloc(b, &b->reqs, d->max_requests)) != LV_OK ||
+        (st = batch_alloc(b, &b->pre_reqs, d->max_requests)) != LV_OK ||
         (st = batch_alloc(b, &b->tiles, b->max_tiles)) != LV_OK ||
         (st = batch_alloc(b, &b->work, most)) != LV_OK ||
         (st = batch_alloc(b, &b->arrived, (size_t)most * lv::kArriveWords)) != LV_OK ||
@@ -2040,8 +2043,7 @@ lv_status lv_batch_share(lv_batch* b, int32_t rows) {
   const size_t heads = (size_t)rows * b->d.num_q_heads;
   lv_status st;
   try {
-    if ((st = batch_alloc(b, &b->pre_reqs, b->d.max_requests)) == LV_OK &&
-        (st = batch_alloc(b, &b->continued, b->d.max_requests)) == LV_OK &&
+    if ((st = batch_alloc(b, &b->continued, b->d.max_requests)) == LV_OK &&
         (st = batch_alloc(b, &b->pre_tiles, b->max_tiles)) == LV_OK &&
         (st = batch_alloc(b, &b->pre_work, most)) == LV_OK && (st = batch_alloc(b, &b->pre_head, 1)) == LV_OK &&
         (st = batch_alloc(b, &b->pre_o, heads * b->dp)) == LV_OK && (st = batch_alloc(b, &b->pre_ml, heads)) == LV_OK) {

@@ -22,7 +22,7 @@ struct WeightArgs {
   const int32_t* pool_table;   // the pool's, by session
   const int32_t* row_starts;
   const PlanReq* reqs;
-  const PlanReq* pre_reqs;     // of the prefixes; null: no room for them
+  const PlanReq* pre_reqs;     // of the prefixes, where the step has some
   const StepHead* head;
   int32_t* tickets;            // units given out, CTAs done; zero between calls
   uint32_t* refused;           // [kMostSegments / 32] a bit a segment (every CTA writes the same)

@@ -571,3 +571,30 @@ def test_replayed_behind_an_attention_that_is_refused(captured):
             assert s.pool.sync(raise_on_error=False) == 0 and torch.equal(w, want)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("dim", [64, 256])
+def test_captured_before_there_was_room_for_prefixes(dim):
+    """A call captured on a batch that gets its room for prefixes later works on a step behind one all the same."""
+    import torch
+    from paper_2606_22983_gb300 import lv
+    from paper_2606_22983_gb300.batch import KVBatch
+    s = SharedStep([64, 3, 150, 8], [1, 2, 5, 1], [0, 0, 1, -1], [260, 515], heads=2, group=4, dim=dim)
+    try:
+        s.batch.close()
+        s.batch = KVBatch(s.pool, q_heads=8, max_requests=4, max_tokens=s.rows, dtype=s.dtype)
+        s.batch.plan(s.sids[:4], np.asarray(s.new[:4], np.int32))
+        lse, w = torch.empty((s.rows, 8), device="cuda"), _weights(s)
+        before, side = w.clone(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            s.batch.add_weights(0, s.q, lse, w, scale=0.125)
+        lv.lv_batch_share(s.batch.handle, s.rows)
+        s.plan()
+        lse.copy_(s.batch.attention(0, s.q, scale=0.125, return_lse=True)[1])
+        graph.replay()
+        assert s.pool.sync(raise_on_error=False) == 0
+        _check(w, *_want(s, before, lse, 0, 0.125), before)
+    finally:
+        s.close()
