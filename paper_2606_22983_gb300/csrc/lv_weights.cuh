@@ -53,7 +53,7 @@ struct LongSum {
 #ifdef __CUDACC__
   __device__ __forceinline__ void add(float x) {
     const float y = x - lost, t = sum + y;
-    lost = (t - sum) - y;
+    lost = fabsf(t) < INFINITY ? (t - sum) - y : 0.f;      // (an infinite sum loses nothing, and stays)
     sum = t;
   }
 #endif

@@ -598,3 +598,28 @@ def test_captured_before_there_was_room_for_prefixes(dim):
         _check(w, *_want(s, before, lse, 0, 0.125), before)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("shape", [dict(cached=[100], new=[300], heads=2, group=4, dim=64),
+                                   dict(cached=[100], new=[300], heads=2, group=4, dim=256),
+                                   dict(cached=[0], new=[2500], heads=1, group=16, dim=64)])
+def test_infinite_weights(shape):
+    """A row whose exponentials exceed 32 bits makes the weights of the keys it sees infinite, and no others."""
+    import torch
+    s = Step(**shape)
+    try:
+        s.plan()
+        scale = s.dim ** -0.5
+        _, lse = s.batch.attention(0, s.q, scale=scale, return_lse=True)
+        before = _weights(s)
+        want, w = before.clone(), before.clone()
+        s.batch.add_weights(0, s.q, lse, want, scale=scale)
+        lse[20, 1] = -1e5                       # (scores are far above -1e4)
+        s.batch.add_weights(0, s.q, lse, w, scale=scale)
+        assert s.pool.sync(raise_on_error=False) == 0
+        sees = s.cached[0] + 21
+        row, other = w[s.sids[0], 0], want[s.sids[0], 0]
+        assert (row[:sees] == float("inf")).all()
+        assert torch.equal(row[sees:], other[sees:]) and torch.equal(w[s.sids[0], 1:], want[s.sids[0], 1:])
+    finally:
+        s.close()
