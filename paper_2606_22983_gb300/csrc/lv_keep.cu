@@ -629,17 +629,27 @@ __global__ void __launch_bounds__(kCutThreads) k_truncate(DevPool p, const int32
   for (int b = nb + tid; b < end; b += kCutThreads) {
     const size_t at = (size_t)sid * p.maxB + b;
     const int e = p.table[at];
-    p.table[at] = -1;
     if (p.incl) drop_clean(p, at);
     if (e >= 0 && e < p.hbm_pages) {
       p.own_hbm[e] = kOwnerNone;
-      atomicAnd(&p.bits_hbm[e >> 5], ~(1u << (e & 31)));
       ++in_hbm;
     } else if (e <= -2 && -(long long)e - 2 < p.host_pages) {
-      const int s = -e - 2;
-      p.own_host[s] = kOwnerNone;
-      atomicAnd(&p.bits_host[s >> 5], ~(1u << (s & 31)));
+      p.own_host[-e - 2] = kOwnerNone;
       ++in_host;
+    }
+  }
+  // (an allocation may run beside this one, and takes a page as soon as its bit is clear: the owner that it then
+  // writes comes after the word above)
+  __threadfence();
+  for (int b = nb + tid; b < end; b += kCutThreads) {
+    const size_t at = (size_t)sid * p.maxB + b;
+    const int e = p.table[at];
+    p.table[at] = -1;
+    if (e >= 0 && e < p.hbm_pages) {
+      atomicAnd(&p.bits_hbm[e >> 5], ~(1u << (e & 31)));
+    } else if (e <= -2 && -(long long)e - 2 < p.host_pages) {
+      const int s = -e - 2;
+      atomicAnd(&p.bits_host[s >> 5], ~(1u << (s & 31)));
     }
   }
   in_hbm = __reduce_add_sync(0xffffffffu, in_hbm);

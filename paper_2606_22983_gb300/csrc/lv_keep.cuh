@@ -38,6 +38,7 @@ __device__ __forceinline__ void drop_clean(const DevPool& p, size_t at) {
   if (g < 0 || g >= p.host_pages) return;
   p.shadow[at] = -1;
   p.own_host[g] = kOwnerNone;
+  __threadfence();      // (as soon as the bit is clear an allocation beside this may give the slot an owner)
   atomicAnd(&p.bits_host[g >> 5], ~(1u << (g & 31)));
   atomicAdd(reinterpret_cast<unsigned long long*>(&p.ctl[C_HOST_ALLOC]), (unsigned long long)-1ll);
   atomicAdd(reinterpret_cast<unsigned long long*>(&p.ctl[C_CLEAN]), (unsigned long long)-1ll);

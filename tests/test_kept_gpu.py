@@ -369,3 +369,42 @@ def test_evict_tokens_on_a_stream_and_replayed():
             _check_cut(s, lens)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("tiers", ["LV_TIERS_EXCLUSIVE", "LV_TIERS_INCLUSIVE"])
+def test_cuts_beside_appends(tiers):
+    """Contexts are cut on one stream while others grow on another: every page has one owner, and its bit."""
+    import torch
+    from paper_2606_22983_gb300 import lv
+    s = Kept([4000, 5, 3000, 9], dim=8, heads=1, layers=1, page=8, tiers=getattr(lv, tiers), spare=6000)
+    try:
+        a, b = torch.cuda.Stream(), torch.cuda.Stream()
+        cut, grow = (0, 2), (1, 3)
+        sids = torch.from_numpy(s.sids[list(cut)].astype(np.int32)).cuda()
+        lens = [torch.tensor([4000 - 40 * k, 3000 - 30 * k], dtype=torch.int32, device="cuda") for k in range(1, 60)]
+        pages, count = torch.empty(64, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        for k, x in enumerate(lens):
+            lv.lv_session_truncate(s.pool.handle, sids, x, 2, a)
+            lv.lv_session_append(s.pool.handle, int(s.sids[grow[k % 2]]), 60, pages, count, b)
+        torch.cuda.synchronize()
+        assert s.pool.sync(raise_on_error=False) == 0
+        ctx = s.pool.get_sessions()["ctx_tokens"]
+        want = {0: 4000 - 40 * 59, 1: 5 + 60 * 30, 2: 3000 - 30 * 59, 3: 9 + 60 * 29}
+        tables, hbm, _ = s.pool.tables()
+        owned = np.full(len(hbm), -1, np.int64)
+        for i, sid in enumerate(s.sids):
+            assert ctx[sid] == want[i]
+            nb = -(-want[i] // 8)
+            row = tables[sid]
+            assert (row[:nb] >= 0).all() and (row[nb:] == -1).all()
+            assert (owned[row[:nb]] == -1).all()
+            owned[row[:nb]] = (int(sid) << 16) | np.arange(nb)
+        assert np.array_equal(hbm.astype(np.int64), owned)
+        assert s.pool.stats()["hbm_allocated"] == (owned >= 0).sum()
+        # and the bits: what is taken next is what nobody has, the lowest first
+        free = np.flatnonzero(owned < 0)
+        got = s.pool.append(int(s.sids[1]), 800)
+        assert s.pool.sync(raise_on_error=False) == 0 and got.tolist() == free[:len(got)].tolist()
+    finally:
+        s.close()
