@@ -1998,6 +1998,9 @@ __device__ __forceinline__ void release_apply(const DevPool& p, long long q, lon
         (uint32_t)(v.z == kOwnerFreeing) << 2 | (uint32_t)(v.w == kOwnerFreeing) << 3;
     for (int k = 0; k < 4; ++k)
       if (m >> k & 1u) own[base + k] = kOwnerNone;
+    // (an allocation on another stream may take a page as soon as its bit is clear: the owner that it then
+    // writes comes after the words above)
+    if (m) __threadfence();
   }
   uint32_t w = m << (4 * lane8);
   w |= __shfl_xor_sync(0xffffffffu, w, 1);
