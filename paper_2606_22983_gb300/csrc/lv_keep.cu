@@ -70,6 +70,7 @@ struct OnceShared {
         at(reinterpret_cast<uint16_t*>(batch + words / 32)) {}
 };
 static_assert(few_of(0) >= kBins && 4 * few_of(0) >= 1024 * kSelWarps, "the histogram's room, and a KiB for each warp");
+static_assert(few_of(0) % 4 == 0 && few_of(kMostWords) % 4 == 0 && few_of(32) % 4 == 0, "words of 16 bytes lie behind them");
 
 // A list's tokens lo..hi, of which `need` of the largest keys are to be found.
 struct List {
@@ -395,7 +396,7 @@ __device__ __forceinline__ bool select_once(const List& t, SelectShared& sh, con
 // 256 threads, six CTAs an SM: with 128, 512 and 64 threads a list the same lists took 96, 104 and 129 us.
 __global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_constant__ SelectArgs a, int n, int words) {
   __shared__ SelectShared sh;
-  extern __shared__ uint32_t dyn[];
+  extern __shared__ __align__(16) uint32_t dyn[];
   const int tid = threadIdx.x;
   const int lists = a.p.J / 2 * a.H, turn = blockIdx.x / lists, list = blockIdx.x - turn * lists;
   const int layer = list / a.H, head = list - layer * a.H;

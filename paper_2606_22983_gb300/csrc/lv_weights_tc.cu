@@ -43,13 +43,14 @@ struct WBars {
 
 struct Misc {
   WBars bars;
-  float b[kSumWarps][kCols];      // the rows' terms, a copy a warp
+  alignas(16) float b[kSumWarps][kCols];      // the rows' terms, a copy a warp, read by 16 bytes
   float part[kUnitKeys];
   volatile int issued;            // tiles of queries
   Unit units[kUnits];
   int pieces[kUnits];             // find_unit's
   SegmentIndex<kIndexThreads> index;
 };
+static_assert(WShape<128>::kMisc % 16 == 0 && WShape<64>::kMisc % 16 == 0, "its place in shared memory");
 static_assert(WShape<128>::kMisc + sizeof(Misc) <= 227 * 1024, "shared memory of a CTA");
 static_assert(WShape<64>::kMisc + sizeof(Misc) <= 227 * 1024, "shared memory of a CTA");
 
