@@ -113,7 +113,7 @@ __device__ __noinline__ void select_by_digits(const List& t, SelectShared& sh) {
     __syncthreads();
     for (int b = tid; b < kBins; b += kSelThreads) sh.bins[b] = 0;
     __syncthreads();
-    for (int j = tid; j < t.n; j += kSelThreads) {
+    for (uint32_t j = tid; j < (uint32_t)t.n; j += kSelThreads) {
       const uint32_t k = order_key(__float_as_uint(t.w[j]));
       if (shift + bits == 32 || (k >> (shift + bits)) == (have >> (shift + bits)))
         atomicAdd(&sh.bins[k >> shift & ((1u << bits) - 1u)], 1);
@@ -136,9 +136,9 @@ __device__ __noinline__ void select_by_digits(const List& t, SelectShared& sh) {
     need -= sh.before;
   }
   int kept = 0, ties = 0;
-  for (int j0 = 0; j0 < t.n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const uint32_t k = j < t.n ? order_key(__float_as_uint(t.w[j])) : 0;
+  for (uint32_t j0 = 0; j0 < (uint32_t)t.n; j0 += kSelThreads) {
+    const uint32_t j = j0 + tid;
+    const uint32_t k = j < (uint32_t)t.n ? order_key(__float_as_uint(t.w[j])) : 0;
     const bool tie = k == have;
     int all;
     __syncthreads();
@@ -147,7 +147,7 @@ __device__ __noinline__ void select_by_digits(const List& t, SelectShared& sh) {
     const bool stay = k > have || (tie && rank <= need);
     const int at = kept + scan_up(stay, sh.sums[1], &all);
     kept += all;
-    if (stay) t.out[at - 1] = t.lo + j;
+    if (stay) t.out[at - 1] = t.lo + (int)j;
   }
 }
 
@@ -439,14 +439,15 @@ __global__ void __launch_bounds__(kSelThreads, 6) k_select_kept(const __grid_con
   t.lo = lo;
   t.out = out + lo;
   t.w = a.w.data + layer * a.w.layer_stride + (bad ? 0 : sid) * a.w.session_stride + head * a.w.head_stride + lo;
-  // the first and last ones, and what is behind the list
-  for (int j = tid; j < lo; j += kSelThreads) out[j] = j;
+  // the first and last ones, and what is behind the list.  (Unsigned here and below: the step past the end of a list
+  // of 2^31 - 1 leaves 31 bits.)
+  for (uint32_t j = tid; j < (uint32_t)lo; j += kSelThreads) out[j] = (int)j;
   if (keep > 0)
-    for (int j = tid; j < c - hi; j += kSelThreads) out[lo + t.need + j] = hi + j;
-  for (int j = keep + tid; j < a.most; j += kSelThreads) out[j] = -1;
+    for (uint32_t j = tid; j < (uint32_t)(c - hi); j += kSelThreads) out[lo + t.need + j] = hi + (int)j;
+  for (uint32_t j = (uint32_t)keep + tid; j < (uint32_t)a.most; j += kSelThreads) out[j] = -1;
   if (t.need == 0) return;
   if (t.need == t.n) {
-    for (int j = tid; j < t.n; j += kSelThreads) t.out[j] = lo + j;
+    for (uint32_t j = tid; j < (uint32_t)t.n; j += kSelThreads) t.out[j] = lo + (int)j;
     return;
   }
   if (t.n > 32 * words || !select_once(t, sh, OnceShared(dyn, words), few_of(words)))
@@ -487,7 +488,7 @@ __global__ void __cluster_dims__(kCheckCtas, 1, 1) __launch_bounds__(kCheckThrea
       for (int l = rank; l < lists; l += kCheckCtas) {
         const int32_t* x = a.kept + ((int64_t)i * lists + l) * a.most;
 #pragma unroll 4
-        for (int j = tid; j < keep; j += kCheckThreads) {
+        for (uint32_t j = tid; j < (uint32_t)keep; j += kCheckThreads) {
           const int v = x[j], before = j > 0 ? x[j - 1] : -1;
           if (v <= before || v >= c) bad = LV_ERR_BOUNDS;
         }
@@ -539,13 +540,13 @@ __global__ void __launch_bounds__(kMoveThreads, 4) k_compact(const __grid_consta
   };
   const int rows = min(kMoveThreads * U / part_vecs, kMoveRows);      // of a chunk
   V *from = nullptr, *to = nullptr;
-  auto look = [&](int j) {      // thread j's row of the next chunk
+  auto look = [&](uint32_t j) {      // thread j's row of the next chunk
     from = to = nullptr;
-    if (tid >= rows || j >= keep) return;
+    if (tid >= rows || j >= (uint32_t)keep) return;
     const int token = kept[j];
-    if (token == j) return;
+    if (token == (int)j) return;
     from = slot(token);
-    to = slot(j);
+    to = slot((int)j);
   };
   look(tid);
   int buf = 0;
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) k_compact(const __grid_consta
     col[u] = at - row[u] * part_vecs;
     if (row[u] >= rows || col[u] >= mine) row[u] = -1;
   }
-  for (int j0 = 0; j0 < keep; j0 += rows) {
+  for (uint32_t j0 = 0; j0 < (uint32_t)keep; j0 += rows) {
     const int next = buf == 2 ? 0 : buf + 1;
     V x[U];
 #pragma unroll
@@ -587,14 +588,14 @@ __global__ void __launch_bounds__(kMoveThreads, 4) k_compact(const __grid_consta
   if (part || kv) return;
   if (a.w.data) {
     float* w = a.w.data + layer * a.w.layer_stride + sid * a.w.session_stride + head * a.w.head_stride;
-    for (int j0 = 0; j0 < keep; j0 += kMoveThreads) {
-      const int j = j0 + tid;
-      const float y = j < keep ? w[kept[j]] : 0.f;
+    for (uint32_t j0 = 0; j0 < (uint32_t)keep; j0 += kMoveThreads) {
+      const uint32_t j = j0 + tid;
+      const float y = j < (uint32_t)keep ? w[kept[j]] : 0.f;
       __syncthreads();
-      if (j < keep) w[j] = y;
+      if (j < (uint32_t)keep) w[j] = y;
     }
     __syncthreads();
-    for (int j = keep + tid; j < c; j += kMoveThreads) w[j] = 0.f;
+    for (uint32_t j = (uint32_t)keep + tid; j < (uint32_t)c; j += kMoveThreads) w[j] = 0.f;
   }
   // the blocks' rows are others now: what the host tier holds of them is no copy any more
   if (a.p.incl && list == 0) {

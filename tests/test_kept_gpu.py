@@ -408,3 +408,22 @@ def test_cuts_beside_appends(tiers):
         assert s.pool.sync(raise_on_error=False) == 0 and got.tolist() == free[:len(got)].tolist()
     finally:
         s.close()
+
+
+def test_the_longest_lists():
+    """Lists with room for 2^31 - 1 tokens, the most there may be: filled to their end, and taken by compaction."""
+    import torch
+    s = Kept([40, 30], heads=1, dim=8, layers=1)
+    try:
+        most = 2 ** 31 - 1
+        kept = s.choose(1, 7, 1, 2)
+        kv, w = s.moved([1], [7], [None, kept])
+        got = s.pool.select_kept(s.sids[1:], _i32([7]), s.weights, first=1, last=2, most=most)
+        assert s.pool.sync(raise_on_error=False) == 0 and got.shape == (1, 1, 1, most)
+        assert np.array_equal(got[0, :, :, :7].cpu().numpy(), kept)
+        assert int(got[0, 0, 0, 7:].max()) == int(got[0, 0, 0, 7:].min()) == -1
+        lens = s.pool.compact(s.sids[1:], _i32([7]), got, s.weights)
+        assert s.pool.sync(raise_on_error=False) == 0 and lens.tolist() == [7]
+        assert np.array_equal(s.kv.cpu().numpy(), kv) and np.array_equal(s.weights.cpu().numpy(), w)
+    finally:
+        s.close()
