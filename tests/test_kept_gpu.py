@@ -427,3 +427,16 @@ def test_the_longest_lists():
         assert np.array_equal(s.kv.cpu().numpy(), kv) and np.array_equal(s.weights.cpu().numpy(), w)
     finally:
         s.close()
+
+
+def test_choice_of_more_sessions_than_are_ordered_by_length():
+    """80 sessions, one of them long: the lists come in the sessions' order, with the long one's room in shared memory."""
+    total = [17 + 31 * i % 500 for i in range(79)] + [66000]
+    s = Kept(total, heads=1, dim=8, layers=1)
+    try:
+        keeps = [1 + t // 3 for t in total]
+        got = s.pool.select_kept(s.sids, _i32(keeps), s.weights, first=2, last=3)
+        assert s.pool.sync(raise_on_error=False) == 0
+        _chosen(s, keeps, got.cpu().numpy(), 2, 3)
+    finally:
+        s.close()
