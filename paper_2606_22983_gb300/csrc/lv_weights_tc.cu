@@ -34,7 +34,9 @@ struct WShape {
 struct WBars {
   uint64_t k_full[8], k_empty[8], q_full[4], q_empty[4];
   uint64_t s_full[2][2], s_empty[2][2];    // a buffer of scores, a half
-  uint64_t part_full, part_empty;          // sums of a unit's second buffer
+  // Sums of a unit's second buffer.  part_full by turns: threads that leave their sums go on without a wait for the
+  // others that do, and may take the next ones before those have come; one barrier for both would look full to them.
+  uint64_t part_full[2], part_empty;
   uint64_t unit_full[kUnits], unit_empty[kUnits];
   uint64_t drain;
   uint32_t tmem;
@@ -117,7 +119,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
         bar_init(&bars.s_empty[i][h], 4);
       }
     }
-    bar_init(&bars.part_full, kSumWarps / 2);
+    for (int i = 0; i < 2; ++i) bar_init(&bars.part_full[i], kSumWarps / 2);
     bar_init(&bars.part_empty, kSumWarps / 2);
     for (int i = 0; i < kUnits; ++i) {
       bar_init(&bars.unit_full[i], 1);
@@ -228,7 +230,7 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
     // this warp's 32 lanes of its buffer and half in TMEM
     const uint32_t s_at = tmem + ((uint32_t)(wid & 3) << 21) + kCols * (2 * buf + half);
     const float2 c2 = make_float2(a.scale, a.scale);
-    uint32_t s_par = 0, part_par = 0;
+    uint32_t s_par = 0, parts = 0;      // parts: units whose sums were joined
     int turn = 0;           // the buffer of the next product
     const int Hq = a.H * a.G;
     float* const b = m.b[wid];
@@ -359,15 +361,15 @@ k_weights_tc(const __grid_constant__ WeightArgs a, const __grid_constant__ CUten
       if (joins) {
         float* part = m.part + kHalf * half + row;
         if (!writes) {
-          if (!(ok = bar_wait(&bars, &bars.part_empty, ~part_par & 1u, a.wait_ns))) break;
+          if (!(ok = bar_wait(&bars, &bars.part_empty, ~parts & 1u, a.wait_ns))) break;
           *part = sum;
-          warp_arrive(&bars.part_full);
+          warp_arrive(&bars.part_full[parts & 1]);
         } else {
-          if (!(ok = bar_wait(&bars, &bars.part_full, part_par, a.wait_ns))) break;
+          if (!(ok = bar_wait(&bars, &bars.part_full[parts & 1], parts >> 1 & 1u, a.wait_ns))) break;
           sum += *part;      // (the same whichever of the two is whose)
           warp_arrive(&bars.part_empty);
         }
-        part_par ^= 1;
+        ++parts;
       }
       // (one addition to the word in this call; nothing waits for it)
       if (!whole && writes && mine) __stcg(w, sum);

@@ -623,3 +623,47 @@ def test_infinite_weights(shape):
         assert torch.equal(row[sees:], other[sees:]) and torch.equal(w[s.sids[0], 1:], want[s.sids[0], 1:])
     finally:
         s.close()
+
+
+HALVES = {
+    # contexts that end in the first half of their last 256 keys, beside longer ones: units of one half and of two
+    "one size": dict(cached=[300] * 40, new=[70] * 40, heads=2, group=16, dim=64),
+    "sizes": dict(cached=[(97 * i) % 700 for i in range(60)], new=[1 + (41 * i) % 120 for i in range(60)], heads=4, group=8, dim=128),
+    "long rows": dict(cached=[512, 255, 88, 144, 0, 1110, 274, 1716, 511, 2636, 58, 3775, 299], new=[4, 2, 6, 3, 10, 8, 75, 7, 8, 11, 24, 5, 40],
+                      heads=4, group=100, dim=128, page=24),
+}
+
+
+@pytest.mark.parametrize("step", HALVES)
+def test_units_of_one_half_beside_two(step):
+    """A half without keys leaves its sums at once, however far the other is."""
+    import torch
+    s = Step(**HALVES[step])
+    try:
+        w, lse, before = _run(s)
+        for _ in range(20):
+            again = before.clone()
+            s.batch.add_weights(1, s.q, lse, again, scale=s.dim ** -0.5)
+            assert torch.equal(again, w)
+        assert s.pool.sync(raise_on_error=False) == 0
+    finally:
+        s.close()
+
+
+def test_prefixes_of_one_half():
+    """Three prefixes of 128 tokens in front of contexts of all lengths, the last rows of each."""
+    import torch
+    cached = [2476, 3568, 8, 1670, 0, 832, 0, 127, 115, 244, 3670, 0, 127, 216, 0, 256, 177, 2530, 1024, 0, 210, 127, 277, 1024, 256,
+              256, 127, 7, 2383, 1, 319, 1, 0, 12, 0, 163, 3810, 128, 1024, 121]
+    new = [4, 4, 1307, 1, 1, 1, 1, 1, 1427, 1445, 1, 880, 0, 1, 0, 1, 1035, 1275, 2, 1352, 507, 1, 1, 1, 1, 4, 1, 1, 1, 1, 3, 1244,
+           898, 354, 617, 0, 1066, 0, 1057, 1]
+    s = SharedStep(cached, new, [-1] * 7 + [0] * 11 + [1] * 14 + [2] * 8, [128, 128, 128], heads=2, group=16, dim=96, page=32)
+    try:
+        w, lse, before = _run(s, last=3)
+        for _ in range(20):
+            again = before.clone()
+            s.batch.add_weights(1, s.q, lse, again, last=3, scale=s.dim ** -0.5)
+            assert torch.equal(again, w)
+        assert s.pool.sync(raise_on_error=False) == 0
+    finally:
+        s.close()
