@@ -248,7 +248,9 @@ __device__ __forceinline__ float max128(const float* s) {
 // starts on the first 64 keys while the others' weights are computed, and on the next 32 (prompts 798 us
 // with 96 and 32 keys, 754 with three pieces).  The first are taken
 // against the maximum so far, beside the search for this unit's; only where that shows a row to
-// have outgrown it are they taken again (and in a pair's first unit).
+// have outgrown it are they taken again (and in a pair's first unit).  Lanes past the tile's rows have the scores of
+// whatever lay in shared memory before.  They begin with a maximum that nothing outgrows, as the other rows'
+// roundings would differ from call to call if these had a say.
 constexpr int kFirst = 64;
 template <int DP, bool kBf16>
 struct Softmax {
@@ -276,7 +278,7 @@ struct Softmax {
     // fetched anew in every pair)
     uint32_t w[kFirst / 2];
     float part, high = -INFINITY;
-    if (fresh) high = max128(s);
+    if (fresh) high = fmaxf(max128(s), top);
 #pragma unroll 1
     for (bool again = fresh;; again = true) {
       if (again) {
@@ -407,6 +409,7 @@ k_attend_tc(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const int p_lo = kMode == kPrefix ? end : pr.t.first + R0 / a.G;
       const int p_hi = kMode == kPrefix ? end : pr.t.first + (R0 + rows - 1) / a.G;
       Softmax<DP, kBf16> sm;
+      if (row >= rows) sm.top = INFINITY;
       for (int u = pr.u0; u < pr.u1; ++u) {
         if (!(ok = bar_wait(&bars, &bars.s_full[half], s_par, a.wait_ns))) break;
         s_par ^= 1;

@@ -304,3 +304,24 @@ def test_strides_and_streams():
         assert torch.equal(got, want) and torch.equal(l2, lse)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("group", [5, 7, 12, 100])
+@pytest.mark.parametrize("kind", ["alone", "behind"])
+def test_the_same_each_time(group, kind):
+    """Groups whose rows do not fill the tensor core's: what shared memory held before has no say in the result."""
+    import torch
+    cached, new = [128, 512, 3, 40], [700, 900, 60, 333]
+    kw = dict(heads=2, group=group, dim=64)
+    s = SharedStep(cached, new, [0, 0, -1, 0], [900], **kw) if kind == "behind" else Step(cached, new, **kw)
+    try:
+        s.plan()
+        far = 30 * s.q                                     # (what an attention between leaves there)
+        want, want_lse = s.batch.attention(1, s.q, scale=0.125, return_lse=True)
+        for k in range(8):
+            s.batch.attention(1, far if k & 1 else s.q.flip(0), scale=0.125)
+            out, lse = s.batch.attention(1, s.q, scale=0.125, return_lse=True)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        assert s.pool.sync(raise_on_error=False) == 0
+    finally:
+        s.close()
