@@ -16,7 +16,7 @@ rows have weighed most:
         out, lse = batch.attention(layer, q, return_lse=True)
         batch.add_weights(layer, q, lse, weights[layer])
     ...
-    pool.evict_tokens(weights, sids, keeps)      # select_kept, compact and truncate
+    pool.evict_tokens(sids, keeps, weights)      # select_kept, compact and truncate
 
 ``row_starts``, ``kv_lens``, ``tables``, ``positions`` and ``slots`` are device tensors that
 ``plan`` fills.  A captured ``write`` or ``attention`` works on the step planned last when it is replayed;
@@ -100,19 +100,6 @@ class KVBatch:
             self.row_starts = self.kv_lens = self.tables = self.positions = self.slots = None
             self.pool.detach(self)
 
-    def _ints(self, x, n=None):
-        """An int32 array the library can read: a tensor as it is, else a numpy array."""
-        if isinstance(x, torch.Tensor):
-            if x.dtype is not torch.int32 or not x.is_contiguous():
-                raise ValueError("expected a contiguous int32 tensor")
-            if x.is_cuda and x.get_device() != self._device:
-                raise ValueError("expected a tensor on the pool's device")
-        else:
-            x = np.ascontiguousarray(x, dtype=np.int32)
-        if n is not None and x.shape[0] != n:
-            raise ValueError(f"expected {n} entries, got {x.shape[0]}")
-        return x
-
     def plan(self, sids, lens, firsts=None, *, prefixes=None, prefix_lens=None, num_tokens=None, max_len=None,
              stream=None):
         """Plans a step: request i is session sids[i] with lens[i] new tokens from position firsts[i]
@@ -121,15 +108,15 @@ class KVBatch:
 
         prefixes: sessions whose first prefix_lens[i] tokens (None: all of them) the rows of request i see
         before its own session's (-1: none).  Requests of one prefix that follow one another read it once."""
-        sids = self._ints(sids)
+        sids = self.pool._ints(sids)
         n = sids.shape[0]
-        lens = self._ints(lens, n)
+        lens = self.pool._ints(lens, n)
         if firsts is not None:
-            firsts = self._ints(firsts, n)
+            firsts = self.pool._ints(firsts, n)
         if prefixes is not None:
-            prefixes = self._ints(prefixes, n)
+            prefixes = self.pool._ints(prefixes, n)
             if prefix_lens is not None:
-                prefix_lens = self._ints(prefix_lens, n)
+                prefix_lens = self.pool._ints(prefix_lens, n)
         elif prefix_lens is not None:
             raise ValueError("prefix_lens needs prefixes")
         if isinstance(lens, torch.Tensor) and lens.is_cuda:

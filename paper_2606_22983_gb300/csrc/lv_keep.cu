@@ -61,7 +61,8 @@ struct SelectShared {
 // and at the end the kept ones' numbers, lie where the keys near the border do.)
 struct OnceShared {
   uint32_t* key;       // of those near the border, [few_of(words)]
-  uint4* word;         // [words]: which of 32 tokens are above the bounds, have the lowest key in them, lie between
+  uint4* word;         // [words]: which of 32 tokens are above the bounds, have the lowest key in them, lie between;
+                       // and a word that makes it one store of 16 bytes
   int* batch;          // [words / 32] kept ones of 1024 tokens
   uint16_t* at;        // [few_of(words)]
   static size_t bytes(int words) { return (size_t)words * 16 + words / 8 + (size_t)few_of(words) * 6; }

@@ -126,12 +126,6 @@ __device__ __forceinline__ void tc_ld32(uint32_t* x, uint32_t at) {
       : LV_R8(x, 0), LV_R8(x, 8), LV_R8(x, 16), LV_R8(x, 24)
       : "r"(at));
 }
-__device__ __forceinline__ void tc_ld16(uint32_t* x, uint32_t at) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : LV_R8(x, 0), LV_R8(x, 8)
-      : "r"(at));
-}
 __device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* x) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
