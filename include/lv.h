@@ -43,9 +43,9 @@
  * A free (lv_cancel, the old locations of lv_remap, lv_session_truncate) may overlap
  * an allocation.
  * A device-driven step (lv_turn, lv_make_resident, lv_evict) and
- * lv_swap_exchange must also be ordered with calls that change the table of a
- * session they may take blocks from or load (lv_remap, lv_session_append,
- * another step).  A block that they find elsewhere than expected is
+ * lv_swap_exchange must also be ordered with calls that change the table or the
+ * rows of a session they may take blocks from or load (lv_remap,
+ * lv_session_append, lv_session_truncate, lv_kv_compact, another step).  A block that they find elsewhere than expected is
  * LV_ERR_STATE, and nothing moves.
  *
  * Threads.  A pool keeps host-side state (scratch alternation, pending
@@ -723,7 +723,8 @@ lv_status lv_batch_plan(lv_batch* batch, const int32_t* sids, const int32_t* fir
    once, for all their rows and heads together. lv_attention works on such a step in two or three
    launches. Device-detected, with the request left out: LV_ERR_BOUNDS for a prefix's session id or
    length out of range, LV_ERR_STATE for a block of it that is not in HBM; it must stay where it is
-   until the step's last call. LV_ERR_INVALID for a batch without room for num_tokens rows. A captured
+   until the step's last call. (It has no turns of its own, so that the victims' ranking takes it early:
+   LV_RUNNING in its state keeps it in HBM, as it does any session.) LV_ERR_INVALID for a batch without room for num_tokens rows. A captured
    lv_attention also keeps whether the plan before its capture was given prefixes (and the kernel for
    them, chosen by whether num_tokens * Hq / H is above 16): after a plan of the other kind it does
    nothing and reports LV_ERR_STATE with detail -1. */
@@ -774,7 +775,8 @@ typedef struct lv_weights {
    that call (lse is needed); last > 0: only the last `last` rows of each request count (a prompt's
    end, say), 0: all. A row whose lse is -inf has no weights. weights: the layer's, with layer_stride
    not looked at (data is where the layer begins). Sums are made in 32 bits, in an order that does not
-   change from call to call. LV_ERR_INVALID as for lv_attention, and for last < 0. Device-detected, and
+   change from call to call; rows of different sessions and heads must not overlap, and calls that add
+   to the same weights, or read them, are ordered with respect to each other. LV_ERR_INVALID as for lv_attention, and for last < 0. Device-detected, and
    those weights left as they are: LV_ERR_BOUNDS for a request (or one whose prefix has) more tokens
    than weights->tokens, LV_ERR_DOUBLE_MAP for one whose session an earlier one of the step has (the
    first request's tokens are added; prefixes come after all requests, and those of one session and
@@ -813,7 +815,8 @@ lv_status lv_select_kept(lv_pool* pool, const lv_weights* weights, const int32_t
    zeros behind them up to the context's end. The lists ascend strictly and end within the context,
    whose blocks are all in HBM; keeps[i] at or above the context's length moves nothing. The context
    stays as long as it is, and rows behind keeps[i] as they are; steps over these sessions, or behind
-   them as prefixes, are planned anew. Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE)
+   them as prefixes, are planned anew. What lv_swap_out or lv_swap_in has copied of them is committed or
+   cancelled before: a copy made earlier would bring the old rows back. Clean host copies of the blocks moved to (LV_TIERS_INCLUSIVE)
    are given up. lens (int32 [n]) receives what lv_session_truncate takes: min(keeps[i], context), or
    -1 for a request that was refused, of which nothing moved. n and most as above. Device-detected:
    LV_ERR_BOUNDS for an id, a length or a list out of range, LV_ERR_STATE for a block that is not in
@@ -823,7 +826,8 @@ lv_status lv_kv_compact(lv_pool* pool, const int32_t* sids, const int32_t* keeps
                         int32_t most, const lv_weights* weights, int32_t* lens, lv_stream stream);
 
 /* Shortens the contexts of sessions sids[i] to lens[i] tokens (one that is no longer, and lens[i] < 0:
-   nothing).  Blocks behind the end are freed, in whichever tier they are, with their clean copies.  n is 0..4096.
+   nothing).  Blocks behind the end are freed, in whichever tier they are, with their clean copies; moves of
+   them that are under way (lv_swap_out, lv_swap_in) are committed or cancelled before.  n is 0..4096.
    Device-detected: LV_ERR_BOUNDS for a session id out of range, LV_ERR_DOUBLE_MAP for a session that an
    earlier request names (the first one holds); the detail is the request's index. */
 lv_status lv_session_truncate(lv_pool* pool, const int32_t* sids, const int32_t* lens, int32_t n, lv_stream stream);

@@ -75,7 +75,9 @@ struct Chunks {
 // What bounds it: few rows, the bytes of K: 61 single tokens over 2 to 16 k keys, 0.42 GB in 80 us, 5.3 TB/s.  Many
 // rows, products and sums that wait for one another, a product of 256 keys and 128 rows some 2100 cycles (the tensor
 // pipe active 49 % of them, issue 53 %, shared memory by the tensor core 46 % and by threads 41 %): 4 prompts of 4096, 32
-// query heads of 128, 264 us, 1.04 PFLOP/s.  Terms read for a key of each half at once (a thread 64 columns of both)
+// query heads of 128, 270 us, 1.02 PFLOP/s.  These have 8 heads a KV head.  Groups that do not divide 128 have fewer rows a
+// product (7 heads: 126) and take the columns one by one under a mask in all of them, not beside the diagonal alone: 4
+// prompts with 28 query heads 292 us, where a seventh less work than 32 is asked.  Terms read for a key of each half at once (a thread 64 columns of both)
 // took a tenth more, as a half's scores then wait for the other's.
 //
 // kCut: units may come in pieces, some of a unit's rows each, whose sums k_weights_join adds up.  (A kernel of its own
