@@ -667,3 +667,47 @@ def test_prefixes_of_one_half():
         assert s.pool.sync(raise_on_error=False) == 0
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (256, 16), (64, 5)])
+def test_the_most_sessions(dim, page):
+    """4095 requests of one token each behind the 4096th session's: a segment for each, in steps of one run and of 2000."""
+    import torch
+    from paper_2606_22983_gb300.batch import KVBatch
+    from paper_2606_22983_gb300.pool import KVPool
+    S, n, P, G = 4096, 4095, 300, 2
+    blocks = -(-P // page)
+    pages = n + blocks
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    kv = torch.randn((2, pages, page, 1, dim), generator=gen, device="cuda").to(torch.bfloat16)
+    pool = KVPool(layers=1, kv_heads=1, head_dim=dim, page_tokens=page, max_sessions=S, max_blocks=blocks, hbm_pages=pages,
+                  hbm_budget_pages=pages, host_pages=0, kv=kv.view(torch.uint8).view(2, pages, page * dim * 2))
+    try:
+        table = np.full((S, blocks), -1, np.int32)
+        table[:n, 0], table[n] = np.arange(n), np.arange(n, pages)
+        ctx = np.ones(S, np.int32)
+        ctx[n] = P
+        pool.import_placement(table, ctx)
+        batch = KVBatch(pool, q_heads=G, max_requests=S, max_tokens=n, prefix_rows=n)
+        q = torch.randn((n, G, dim), generator=gen, device="cuda").to(torch.bfloat16)
+        sids = np.random.default_rng(1).permutation(n).astype(np.int32)
+        own = kv[0, :n, 0, 0].double()[torch.from_numpy(sids).long().cuda()]
+        before = kv[0, n:, :, 0].reshape(-1, dim)[:P].double()
+        for many in (n, 2000):
+            batch.plan(sids, np.ones(n, np.int32), prefixes=np.where(np.arange(n) < many, n, -1).astype(np.int32))
+            _, lse = batch.attention(0, q, scale=0.1, return_lse=True)
+            w = torch.zeros((S, 1, blocks * page), device="cuda")
+            batch.add_weights(0, q, lse, w, scale=0.1)
+            assert pool.sync(raise_on_error=False) == 0
+            x, z = q.double(), lse.double()[:, :, None]
+            dot = torch.einsum("rgd,kd->rgk", x.abs(), before.abs()).amax() * 0.1
+            mine = torch.exp(torch.einsum("rgd,rd->rg", x, own)[:, :, None] * 0.1 - z)[:, :, 0].sum(1)
+            pre = torch.exp(torch.einsum("rgd,kd->rgk", x[:many], before) * 0.1 - z[:many]).sum((0, 1))
+            # (as in _want, with the largest sum of |q k| for all, and its additions of 2 and of 2 * many)
+            tol = (dot + (x.abs().sum(2).amax() * own.abs().amax()) * 0.1) * 2.0 ** -19 + 2.0 ** -18 + z.abs().amax() * 2.0 ** -23
+            got = w[:, 0].double()
+            assert ((got[torch.from_numpy(sids).long().cuda(), 0] - mine).abs() <= tol * mine).all()
+            assert ((got[n, :P] - pre).abs() <= (tol + 2 * many * 2.0 ** -24) * pre).all()
+            assert (got[:n, 1:] == 0).all() and (got[n, P:] == 0).all()
+    finally:
+        pool.close()
