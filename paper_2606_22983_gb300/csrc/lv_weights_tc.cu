@@ -77,7 +77,7 @@ struct Chunks {
 // pipe active 49 % of them, issue 53 %, shared memory by the tensor core 46 % and by threads 41 %): 4 prompts of 4096, 32
 // query heads of 128, 270 us, 1.02 PFLOP/s.  These have 8 heads a KV head.  Groups that do not divide 128 have fewer rows a
 // product (7 heads: 126) and take the columns one by one under a mask in all of them, not beside the diagonal alone: 4
-// prompts with 28 query heads 292 us, where a seventh less work than 32 is asked.  Terms read for a key of each half at once (a thread 64 columns of both)
+// prompts with 28 query heads 292 us, where an eighth less work than 32 is asked.  Terms read for a key of each half at once (a thread 64 columns of both)
 // took a tenth more, as a half's scores then wait for the other's.
 //
 // kCut: units may come in pieces, some of a unit's rows each, whose sums k_weights_join adds up.  (A kernel of its own
